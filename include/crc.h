@@ -436,8 +436,129 @@ int crc_transfer_replay(const crc_problem *p, const crc_transfer *plan, int64_t 
                         const void *pool_host, int64_t pool_experts, void *slots_dev,
                         void *stream);
 
+/* ------------------------------------------------------------------------ */
+/* Operators around the router heads: the norm that makes the hidden state  */
+/* they read, the experts' products that follow the Top-K, and the 8-bit    */
+/* form of an expert (which halves S_exp, the bytes of its transfer).  No   */
+/* counterpart in the paper, whose step begins at the hidden state and ends */
+/* at the cache decisions (Sec. 2).  Calls without a state: device-side     */
+/* failures are reported by crc_device_error().                             */
+/* ------------------------------------------------------------------------ */
+
+/* Element types.  CRC_E4M3 (sign, 4 exponent, 3 mantissa bits; largest value
+ * 448, no infinities) always comes with one fp32 scale a row: a row stands
+ * for q * scale, scale = max |row| / 448 as this library writes it (1 for a
+ * row of zeros; a NaN or an infinity in the row goes on to the scale). */
+enum { CRC_BF16 = 1, CRC_F32 = 2, CRC_E4M3 = 3 };
+
+/* Root-mean-square norm of M rows of d elements, with the residual's addition:
+ *   s = x + residual,  rstd = (mean s^2 + eps)^(-1/2),  y = s rstd weight,
+ * in fp32 from the unrounded s; each output is rounded once.
+ *   x_dev             stream_type (CRC_BF16 or CRC_F32), rows x_stride elements
+ *                     apart (>= d, a multiple of 8)
+ *   residual_dev      stream_type [M][d], or NULL (s = x)
+ *   weight_dev        bf16 [d]
+ *   residual_out_dev  stream_type [M][d]: s, the next residual; may be
+ *                     residual_dev, or x_dev when x_stride = d; or NULL
+ *   out_dev           bf16 [M][d]: y, or NULL
+ *   out8_dev, scale8_dev  e4m3 [M][d] and fp32 [M]: y in 8 bits, both or none
+ *   rstd_dev          fp32 [M]: the statistic that the gradient takes, or NULL
+ * Arrays of rows 16-byte aligned (out8_dev 8).  d % 8 == 0, d <= 32768, else
+ * CRC_EUNSUPPORTED.  M = 0 is a no-op. */
+int crc_rms_norm(const void *x_dev, int64_t x_stride, const void *residual_dev,
+                 const uint16_t *weight_dev, int32_t stream_type, int64_t M, int32_t d, double eps,
+                 void *residual_out_dev, uint16_t *out_dev, uint8_t *out8_dev, float *scale8_dev,
+                 float *rstd_dev, void *stream);
+
+/* Its gradient.  With v = dy weight and xhat = s rstd,
+ *   dx = dres + rstd (v - xhat mean(v xhat)),   dw = sum over rows of dy xhat;
+ * dx is the gradient with respect to x and to the residual alike.
+ *   dy_dev    bf16 [M][d], the gradient of the loss with respect to y
+ *   s_dev     stream_type [M][d], residual_out_dev of the forward call
+ *   rstd_dev  fp32 [M] of the forward call
+ *   dres_dev  stream_type [M][d], the gradient that arrives at s by the
+ *             residual path, or NULL
+ *   dx_dev    stream_type [M][d]; may be dres_dev or s_dev
+ *   dw_dev    fp32 [d], or NULL; summed in a fixed order (no atomics).  Needs
+ *             workspace_dev with crc_rms_norm_grad_workspace_bytes(M, d)
+ *             bytes, 256-byte aligned.
+ * M = 0 sets dw to zero. */
+size_t crc_rms_norm_grad_workspace_bytes(int64_t M, int32_t d);
+int crc_rms_norm_grad(const uint16_t *dy_dev, const void *s_dev, const uint16_t *weight_dev,
+                      const float *rstd_dev, const void *dres_dev, int32_t stream_type, int64_t M,
+                      int32_t d, void *dx_dev, float *dw_dev, void *workspace_dev,
+                      size_t workspace_bytes, void *stream);
+
+/* bf16 rows in 8 bits: out8 = e4m3(x / scale), scale = max |row| / 448.
+ *   x_dev bf16, rows x_stride elements apart (>= d, a multiple of 8), 16-byte
+ *   aligned; out8_dev e4m3 [M][d], 8-byte aligned; scale8_dev fp32 [M].
+ * d as in crc_rms_norm.  M = 0 is a no-op. */
+int crc_quantize_rows(const uint16_t *x_dev, int64_t x_stride, int64_t M, int32_t d,
+                      uint8_t *out8_dev, float *scale8_dev, void *stream);
+
+/* One layer's experts and where they lie.  An expert is three matrices, gate
+ * and up [f][d] and down [d][f] (3 d f elements, the expert_bytes of a
+ * crc_problem); slot s of the arrays below holds one expert, so they may be the
+ * slots that crc_transfer_replay fills (gate, up and down one after the
+ * other in each slot: gate_up_dev = the slots, down_dev = gate_up_dev + 2 f d
+ * elements, both strides the slot's bytes) or a whole layer. */
+typedef struct crc_moe {
+    int32_t N;                   /* routed experts, 16 <= N <= 128, N % 16 == 0  */
+    int32_t K;                   /* Top-K, 1 <= K <= min(N, 32)                  */
+    int32_t d;                   /* hidden size, d % 16 == 0 (bf16: d % 8 == 0)  */
+    int32_t f;                   /* width of an expert, f % 16 == 0              */
+    int32_t slots;               /* expert slots in the arrays below             */
+    int32_t weight_type;         /* CRC_BF16 or CRC_E4M3                         */
+    int32_t renormalize;         /* gates: 0 = p^R of the choices, 1 = those
+                                    divided by their sum                         */
+    int32_t reserved;            /* must be 0                                    */
+    const void *gate_up_dev;     /* [slots][2][f][d], 16-byte aligned            */
+    const void *down_dev;        /* [slots][d][f], 16-byte aligned               */
+    int64_t gate_up_stride;      /* bytes between slots, a multiple of 16        */
+    int64_t down_stride;
+    const float *gate_up_scale_dev;   /* CRC_E4M3: [slots][2][f], else NULL      */
+    const float *down_scale_dev;      /* CRC_E4M3: [slots][d], else NULL         */
+    int64_t gate_up_scale_stride;     /* bytes between slots, a multiple of 4    */
+    int64_t down_scale_stride;
+    const uint16_t *router_dev;  /* bf16 [N][d], 16-byte aligned: W^R (the first N
+                                    rows of a layer of w_cat)                    */
+    const int32_t *expert_slot_dev;   /* [N]: each expert's slot, -1 (or any value
+                                    outside 0 .. slots - 1) if it has none;
+                                    NULL: expert e is in slot e                  */
+} crc_moe;
+
+/* The mixture-of-experts layer for a few tokens (one decoded token of every
+ * stream, a few draft tokens), M <= 1024 and M K <= 8192:
+ *   z = router x, S = TopK(z) in the total order, g = softmax(z) over S
+ *   (divided by its sum with renormalize),
+ *   out = sum over e in S of g_e down_e (silu(gate_e x) * (up_e x)).
+ * An expert without a slot adds nothing (the cache decisions put every selected
+ * expert in a slot: UpdateCache protects S); the other gates stay as they are.
+ *   x_dev      bf16, rows x_stride elements apart (>= d, a multiple of 8), 16-byte
+ *              aligned.  May be NULL when x8_dev and scores_dev are given.
+ *   x8_dev, x8_scale_dev  e4m3 [M][d] (16-byte aligned) and fp32 [M], from
+ *              crc_rms_norm: what the experts multiply in place of x (the
+ *              router reads x); CRC_E4M3 weights only; or both NULL
+ *   scores_dev fp32 rows of N native router probabilities, scores_stride elements
+ *              apart (>= N), e.g. those of crc_route_scores: S = TopK(p^R) is
+ *              taken from them and router_dev is not read; or NULL
+ *   out_dev    bf16 [M][d], 16-byte aligned, not overlapping the inputs
+ *   topk_dev   uint8 [M][K], S in rank order, or NULL
+ *   gates_dev  fp32 [M][K], g in rank order, or NULL
+ *   workspace_dev  crc_moe_workspace_bytes(m, M) bytes, 256-byte aligned; calls
+ *              that may overlap on the GPU need one each
+ * Products are summed in fp32; the product of silu and up is rounded to bf16 (as
+ * wide as x) for the second product, the K experts are summed in fp32 in rank
+ * order and out is rounded once.  Results do not depend on the order in which
+ * blocks run.  M = 0 is a no-op. */
+size_t crc_moe_workspace_bytes(const crc_moe *m, int32_t M);
+int crc_moe_layer(const crc_moe *m, const uint16_t *x_dev, int64_t x_stride, const uint8_t *x8_dev,
+                  const float *x8_scale_dev, const float *scores_dev, int64_t scores_stride,
+                  int32_t M, uint16_t *out_dev, uint8_t *topk_dev, float *gates_dev,
+                  void *workspace_dev, size_t workspace_bytes, void *stream);
+
 /* Synchronises the device and returns (then clears) the error latched by
- * calls without a state (crc_route_scores), CRC_OK if none. */
+ * calls without a state (crc_route_scores, crc_moe_layer), CRC_OK if none. */
 int crc_device_error(void);
 
 /* Number of kernels the library has launched in this process. */
@@ -454,8 +575,9 @@ uint64_t crc_launch_count(void);
  * other host threads. */
 enum { CRC_KERNEL_ROUTER = 0, CRC_KERNEL_SCAN = 1, CRC_KERNEL_STATE = 2, CRC_KERNEL_SYNTH = 3,
        CRC_KERNEL_FUSED = 4, CRC_KERNEL_LOSS = 5, CRC_KERNEL_LOSS_MEANS = 6,
-       CRC_KERNEL_SHORT = 7,
-       CRC_KERNEL_KINDS = 8 };
+       CRC_KERNEL_SHORT = 7, CRC_KERNEL_NORM = 8, CRC_KERNEL_QUANTIZE = 9,
+       CRC_KERNEL_MOE_ROUTE = 10, CRC_KERNEL_MOE = 11,
+       CRC_KERNEL_KINDS = 12 };
 typedef struct crc_kernel_times {
     uint64_t launches[CRC_KERNEL_KINDS];
     double ms[CRC_KERNEL_KINDS];

@@ -58,11 +58,23 @@ class crc_report(ctypes.Structure):
 
 
 KERNEL_KINDS = {"router": 0, "scan": 1, "state": 2, "synth": 3, "fused": 4, "loss": 5,
-                "loss_means": 6, "short": 7}
+                "loss_means": 6, "short": 7, "norm": 8, "quantize": 9, "moe_route": 10, "moe": 11}
 
 
 class crc_kernel_times(ctypes.Structure):
-    _fields_ = [("launches", ctypes.c_uint64 * 8), ("ms", ctypes.c_double * 8)]
+    _fields_ = [("launches", ctypes.c_uint64 * 12), ("ms", ctypes.c_double * 12)]
+
+
+class crc_moe(ctypes.Structure):
+    _fields_ = [("N", ctypes.c_int32), ("K", ctypes.c_int32), ("d", ctypes.c_int32),
+                ("f", ctypes.c_int32), ("slots", ctypes.c_int32),
+                ("weight_type", ctypes.c_int32), ("renormalize", ctypes.c_int32),
+                ("reserved", ctypes.c_int32), ("gate_up_dev", ctypes.c_void_p),
+                ("down_dev", ctypes.c_void_p), ("gate_up_stride", ctypes.c_int64),
+                ("down_stride", ctypes.c_int64), ("gate_up_scale_dev", ctypes.c_void_p),
+                ("down_scale_dev", ctypes.c_void_p), ("gate_up_scale_stride", ctypes.c_int64),
+                ("down_scale_stride", ctypes.c_int64), ("router_dev", ctypes.c_void_p),
+                ("expert_slot_dev", ctypes.c_void_p)]
 
 
 class CrcError(RuntimeError):
@@ -75,8 +87,8 @@ _lib = None
 _lock = threading.Lock()
 
 # (name, restype, argtypes) of every exported symbol
-P, I32, U32, U64, SZ, D = (ctypes.c_void_p, ctypes.c_int32, ctypes.c_uint32, ctypes.c_uint64,
-                           ctypes.c_size_t, ctypes.c_double)
+P, I32, I64, U32, U64, SZ, D = (ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_uint32,
+                                ctypes.c_uint64, ctypes.c_size_t, ctypes.c_double)
 PP = ctypes.POINTER(crc_problem)
 EXPORTS = [
     ("crc_state_bytes", SZ, [PP]),
@@ -112,6 +124,13 @@ EXPORTS = [
     ("crc_profile_end", ctypes.c_int, [ctypes.POINTER(crc_kernel_times)]),
     ("crc_synth_hidden", ctypes.c_int, [I32, I32, I32, I32, I32, U32, D, D, P, P, P, P]),
     ("crc_synth_weights", ctypes.c_int, [I32, I32, I32, U32, I32, P, P]),
+    ("crc_rms_norm", ctypes.c_int, [P, I64, P, P, I32, I64, I32, D, P, P, P, P, P, P]),
+    ("crc_rms_norm_grad_workspace_bytes", SZ, [I64, I32]),
+    ("crc_rms_norm_grad", ctypes.c_int, [P, P, P, P, P, I32, I64, I32, P, P, P, SZ, P]),
+    ("crc_quantize_rows", ctypes.c_int, [P, I64, I64, I32, P, P, P]),
+    ("crc_moe_workspace_bytes", SZ, [ctypes.POINTER(crc_moe), I32]),
+    ("crc_moe_layer", ctypes.c_int,
+     [ctypes.POINTER(crc_moe), P, I64, P, P, P, I64, I32, P, P, P, P, SZ, P]),
 ]
 
 
@@ -345,6 +364,46 @@ def crc_synth_weights(L, N, d, seed, copy_init, w_ptr, stream=None):
         "crc_synth_weights")
 
 
+# element types (crc.h CRC_BF16 ...)
+BF16, F32, E4M3 = 1, 2, 3
+
+
+def crc_rms_norm(x_ptr, x_stride: int, residual_ptr, weight_ptr, stream_type: int, M: int, d: int,
+                 eps: float, residual_out_ptr, out_ptr, out8_ptr, scale8_ptr, rstd_ptr,
+                 stream=None):
+    _ck(load().crc_rms_norm(x_ptr, x_stride, residual_ptr, weight_ptr, stream_type, M, d, eps,
+                            residual_out_ptr, out_ptr, out8_ptr, scale8_ptr, rstd_ptr,
+                            _stream(stream)), "crc_rms_norm")
+
+
+def crc_rms_norm_grad_workspace_bytes(M: int, d: int) -> int:
+    return int(load().crc_rms_norm_grad_workspace_bytes(M, d))
+
+
+def crc_rms_norm_grad(dy_ptr, s_ptr, weight_ptr, rstd_ptr, dres_ptr, stream_type: int, M: int,
+                      d: int, dx_ptr, dw_ptr, ws_ptr, ws_bytes: int, stream=None):
+    _ck(load().crc_rms_norm_grad(dy_ptr, s_ptr, weight_ptr, rstd_ptr, dres_ptr, stream_type, M, d,
+                                 dx_ptr, dw_ptr, ws_ptr, ws_bytes, _stream(stream)),
+        "crc_rms_norm_grad")
+
+
+def crc_quantize_rows(x_ptr, x_stride: int, M: int, d: int, out8_ptr, scale8_ptr, stream=None):
+    _ck(load().crc_quantize_rows(x_ptr, x_stride, M, d, out8_ptr, scale8_ptr, _stream(stream)),
+        "crc_quantize_rows")
+
+
+def crc_moe_workspace_bytes(m: crc_moe, M: int) -> int:
+    return int(load().crc_moe_workspace_bytes(ctypes.byref(m), M))
+
+
+def crc_moe_layer(m: crc_moe, x_ptr, x_stride: int, x8_ptr, x8_scale_ptr, scores_ptr,
+                  scores_stride: int, M: int, out_ptr, topk_ptr, gates_ptr, ws_ptr, ws_bytes: int,
+                  stream=None):
+    _ck(load().crc_moe_layer(ctypes.byref(m), x_ptr, x_stride, x8_ptr, x8_scale_ptr, scores_ptr,
+                             scores_stride, M, out_ptr, topk_ptr, gates_ptr, ws_ptr, ws_bytes,
+                             _stream(stream)), "crc_moe_layer")
+
+
 # --------------------------------------------------------------------------- #
 # torch conveniences (allocation and marshalling only)
 # --------------------------------------------------------------------------- #
@@ -548,6 +607,207 @@ def synth_hidden(B, T, L, d, seed=0, rho_t=0.9, rho_l=0.8, t0=0, carry=None, att
     crc_synth_hidden(B, T, L, d, t0, seed, rho_t, rho_l, _ptr(attempts), out.data_ptr(),
                      carry.data_ptr(), stream)
     return out, carry
+
+
+def _stream_type(t) -> int:
+    import torch
+    if t.dtype == torch.bfloat16:
+        return BF16
+    if t.dtype == torch.float32:
+        return F32
+    raise ValueError(f"the residual stream is bfloat16 or float32, not {t.dtype}")
+
+
+def _check(t, name: str, shape, dtype, dense: bool = True):
+    """A tensor argument of the stated shape and type on the GPU, or None."""
+    if t is None:
+        return
+    if t.shape != shape or t.dtype != dtype or not t.is_cuda:
+        raise ValueError(f"{name}: a {dtype} CUDA tensor of shape {tuple(shape)} is wanted, "
+                         f"got {t.dtype} {tuple(t.shape)} on {t.device}")
+    if dense and not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
+
+
+def _rows(t, name: str):
+    """(rows, elements a row, elements between rows) of a 2-D tensor."""
+    if t.dim() != 2 or not t.is_cuda:
+        raise ValueError(f"{name} must be a 2-D CUDA tensor")
+    M, d = t.shape
+    if t.stride(1) != 1 and d != 1:
+        raise ValueError(f"the rows of {name} must be contiguous")
+    return M, d, (t.stride(0) if M > 1 else (d + 7) // 8 * 8)
+
+
+def rms_norm(x, weight, eps: float = 1e-6, residual=None, residual_out=None, out=None, out8=None,
+             scale8=None, rstd=None, stream=None):
+    """crc_rms_norm on rows x [M][d] (bf16 or fp32, rows may be strided).
+
+    Writes y = norm(x + residual) * weight to `out` (bf16; made when no output is
+    given), to out8 / scale8 (float8_e4m3fn and fp32 [M]) if given, x + residual to
+    residual_out and the rows' statistic to rstd (fp32 [M]).  Returns out."""
+    import torch
+    M, d, ldx = _rows(x, "x")
+    kind = _stream_type(x)
+    _check(weight, "weight", (d,), torch.bfloat16)
+    _check(residual, "residual", (M, d), x.dtype)
+    _check(residual_out, "residual_out", (M, d), x.dtype)
+    if out is None and out8 is None:
+        out = torch.empty((M, d), dtype=torch.bfloat16, device=x.device)
+    _check(out, "out", (M, d), torch.bfloat16)
+    _check(out8, "out8", (M, d), torch.float8_e4m3fn)
+    _check(scale8, "scale8", (M,), torch.float32)
+    _check(rstd, "rstd", (M,), torch.float32)
+    crc_rms_norm(x.data_ptr(), ldx, _ptr(residual), weight.data_ptr(), kind, M, d, eps,
+                 _ptr(residual_out), _ptr(out), _ptr(out8), _ptr(scale8), _ptr(rstd), stream)
+    return out
+
+
+def rms_norm_grad(dy, s, weight, rstd, dres=None, dx=None, dw=None, want_dw: bool = True,
+                  workspace=None, stream=None):
+    """crc_rms_norm_grad: (dx, dw) from dy (bf16), s = x + residual and rstd of the
+    forward call, and dres, the gradient that arrives at s directly."""
+    import torch
+    M, d = dy.shape
+    kind = _stream_type(s)
+    _check(dy, "dy", (M, d), torch.bfloat16)
+    _check(s, "s", (M, d), s.dtype)
+    _check(weight, "weight", (d,), torch.bfloat16)
+    _check(rstd, "rstd", (M,), torch.float32)
+    _check(dres, "dres", (M, d), s.dtype)
+    if dx is None:
+        dx = torch.empty_like(s)
+    _check(dx, "dx", (M, d), s.dtype)
+    if want_dw and dw is None:
+        dw = torch.empty(d, dtype=torch.float32, device=dy.device)
+    _check(dw, "dw", (d,), torch.float32)
+    if dw is not None and workspace is None:
+        workspace = torch.empty(crc_rms_norm_grad_workspace_bytes(M, d), dtype=torch.uint8,
+                                device=dy.device)
+    crc_rms_norm_grad(dy.data_ptr(), s.data_ptr(), weight.data_ptr(), rstd.data_ptr(), _ptr(dres),
+                      kind, M, d, dx.data_ptr(), _ptr(dw), _ptr(workspace),
+                      0 if workspace is None else workspace.nbytes, stream)
+    return dx, dw
+
+
+def quantize_rows(x, out8=None, scale=None, stream=None):
+    """crc_quantize_rows: bf16 rows [..][d] as (float8_e4m3fn, fp32 scale a row).
+    A 2-D x may have strided rows; more dimensions must be contiguous."""
+    import torch
+    if x.dtype != torch.bfloat16:
+        raise ValueError("x must be bfloat16")
+    lead, d = x.shape[:-1], x.shape[-1]
+    if x.dim() != 2:
+        if not x.is_contiguous():
+            raise ValueError("x must be contiguous, or have two dimensions")
+        x = x.reshape(-1, d)
+    M, d, ldx = _rows(x, "x")
+    if out8 is None:
+        out8 = torch.empty((*lead, d), dtype=torch.float8_e4m3fn, device=x.device)
+    if scale is None:
+        scale = torch.empty(lead, dtype=torch.float32, device=x.device)
+    _check(out8, "out8", (*lead, d), torch.float8_e4m3fn)
+    _check(scale, "scale", lead, torch.float32)
+    crc_quantize_rows(x.data_ptr(), ldx, M, d, out8.data_ptr(), scale.data_ptr(), stream)
+    return out8, scale
+
+
+def expert_views(slots, f: int, d: int):
+    """The matrices in the expert slots [C][3 * f * d] of one layer (bf16 or
+    float8_e4m3fn elements, e.g. `slots_dev[l]` of transfer_replay viewed in that
+    type): gate_up [C][2][f][d] and down [C][d][f], views of the slots."""
+    C, n = slots.shape
+    if n < 3 * f * d or (slots.stride(1) != 1):
+        raise ValueError("a slot holds 3 * f * d contiguous elements")
+    st = slots.stride(0)
+    gate_up = slots.as_strided((C, 2, f, d), (st, f * d, d, 1))
+    down = slots.as_strided((C, d, f), (st, f, 1), slots.storage_offset() + 2 * f * d)
+    return gate_up, down
+
+
+class MoeLayer:
+    """One layer's experts for crc_moe_layer: gate_up [slots][2][f][d] and down
+    [slots][d][f], bf16, or float8_e4m3fn with gate_up_scale [slots][2][f] and
+    down_scale [slots][d] (the slots may be strided, see expert_views); router
+    bf16 [N][d]; expert_slot int32 [N] (None: expert e is in slot e).  Keeps
+    references to all of them and no copy: what is written to them later (an
+    expert copied to a slot, a new expert_slot map) counts from the next call."""
+
+    def __init__(self, gate_up, down, K: int, router=None, expert_slot=None, gate_up_scale=None,
+                 down_scale=None, renormalize: bool = True, N: int | None = None):
+        import torch
+        if gate_up.dim() != 4 or gate_up.shape[1] != 2:
+            raise ValueError("gate_up has the shape [slots][2][f][d]")
+        slots, _, f, d = gate_up.shape
+        kinds = {torch.bfloat16: BF16, torch.float8_e4m3fn: E4M3}
+        if gate_up.dtype not in kinds or not gate_up.is_cuda:
+            raise ValueError("gate_up must be a bfloat16 or float8_e4m3fn CUDA tensor")
+        _check(down, "down", (slots, d, f), gate_up.dtype, dense=False)
+        if gate_up.stride()[1:] != (f * d, d, 1) or down.stride()[1:] != (f, 1):
+            raise ValueError("an expert's matrices must be contiguous")
+        if N is None:
+            N = (router.shape[0] if router is not None else
+                 expert_slot.shape[0] if expert_slot is not None else slots)
+        _check(router, "router", (N, d), torch.bfloat16)
+        _check(expert_slot, "expert_slot", (N,), torch.int32)
+        if expert_slot is None and N > slots:
+            raise ValueError("more experts than slots: an expert_slot map is wanted")
+        for t, name, shape in ((gate_up_scale, "gate_up_scale", (slots, 2, f)),
+                               (down_scale, "down_scale", (slots, d))):
+            if (t is None) != (gate_up.dtype == torch.bfloat16):
+                raise ValueError(f"{name} belongs to 8-bit experts")
+            _check(t, name, shape, torch.float32, dense=False)
+        if gate_up_scale is not None and (gate_up_scale.stride()[1:] != (f, 1)
+                                          or down_scale.stride(1) != 1):
+            raise ValueError("an expert's scales must be contiguous")
+        es = gate_up.element_size()
+        self.N, self.K, self.d, self.f = N, K, d, f
+        self.tensors = (gate_up, down, router, expert_slot, gate_up_scale, down_scale)
+        self.c = crc_moe(N=N, K=K, d=d, f=f, slots=slots, weight_type=kinds[gate_up.dtype],
+                         renormalize=int(renormalize), reserved=0,
+                         gate_up_dev=gate_up.data_ptr(), down_dev=down.data_ptr(),
+                         gate_up_stride=gate_up.stride(0) * es, down_stride=down.stride(0) * es,
+                         gate_up_scale_dev=_ptr(gate_up_scale), down_scale_dev=_ptr(down_scale),
+                         gate_up_scale_stride=0 if gate_up_scale is None
+                         else gate_up_scale.stride(0) * 4,
+                         down_scale_stride=0 if down_scale is None else down_scale.stride(0) * 4,
+                         router_dev=_ptr(router), expert_slot_dev=_ptr(expert_slot))
+        if self.workspace_bytes(1) == 0:
+            raise CrcError(CRC_EUNSUPPORTED, "crc_moe_workspace_bytes")
+
+    def workspace_bytes(self, M: int) -> int:
+        return crc_moe_workspace_bytes(self.c, M)
+
+    def __call__(self, x, out=None, x8=None, x_scale=None, scores=None, topk=None, gates=None,
+                 workspace=None, stream=None):
+        """out [M][d] of rows x [M][d] (bf16, rows may be strided); x8 / x_scale:
+        the rows in 8 bits for the experts; scores: fp32 probabilities [M][N] (rows
+        may be strided) in place of the router; topk (uint8) and gates (fp32)
+        [M][K] are written if given.  x may be None when x8 and scores are given."""
+        import torch
+        d = self.d
+        src = x if x is not None else x8
+        if src is None:
+            raise ValueError("x or x8 is wanted")
+        M, _, ldx = _rows(src, "x")
+        _check(x, "x", (M, d), torch.bfloat16, dense=False)
+        _check(x8, "x8", (M, d), torch.float8_e4m3fn)
+        _check(x_scale, "x_scale", (M,), torch.float32)
+        lds = 0
+        if scores is not None:
+            _check(scores, "scores", (M, self.N), torch.float32, dense=False)
+            lds = max(_rows(scores, "scores")[2], self.N)
+        if out is None:
+            out = torch.empty((M, d), dtype=torch.bfloat16, device=src.device)
+        _check(out, "out", (M, d), torch.bfloat16)
+        _check(topk, "topk", (M, self.K), torch.uint8)
+        _check(gates, "gates", (M, self.K), torch.float32)
+        if workspace is None:
+            workspace = torch.empty(self.workspace_bytes(M), dtype=torch.uint8, device=src.device)
+        crc_moe_layer(self.c, _ptr(x), ldx, _ptr(x8), _ptr(x_scale), _ptr(scores), lds, M,
+                      out.data_ptr(), _ptr(topk), _ptr(gates), workspace.data_ptr(),
+                      workspace.nbytes, stream)
+        return out
 
 
 def _stats_struct(stats: dict) -> crc_stats:
