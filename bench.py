@@ -237,11 +237,13 @@ KERNEL_SOURCES = {
                "policy_lrfu.cu", "policy_spatio.cu", "policy_scan.cuh", "cache_scan.cuh",
                "crc_device.cuh"],
     "loss": ["loss.cu", "cache_scan.cuh", "crc_device.cuh"],
+    "moe": ["moe.cu", "moe_route.cuh", "crc_device.cuh"],
+    "norm": ["norm.cu"],
 }
 
 
 def kernel_family(kernel: str) -> str:
-    for fam in ("policy", "fused", "short", "router", "loss"):
+    for fam in ("moe", "norm", "policy", "fused", "short", "router", "loss"):
         if fam in kernel:
             return fam
     return "scan"
