@@ -1,31 +1,35 @@
 // The mixture-of-experts layer for a few tokens: entry points, workspace and
 // the experts' kernels.
+#include <cudaTypedefs.h>
 #include <cuda_bf16.h>
-#include <cuda_fp8.h>
 #include <cuda_runtime.h>
 
 #include "crc_internal.h"
+#include "moe_experts.cuh"
 #include "moe_route.cuh"
 
 namespace crc {
+
+PFN_cuTensorMapEncodeTiled_v12000 encode_fn();      // router.cu
+
 namespace {
 
 constexpr int kMoeMaxTokens = 1024;
 constexpr int kMoeMaxEntries = 8192;      // M K
-constexpr int kCtrlWords = 64;
 
 inline bool aligned(const void* p, size_t a) { return reinterpret_cast<uintptr_t>(p) % a == 0; }
 inline size_t up256(size_t n) { return (n + 255) & ~(size_t)255; }
 
 struct MoeLayout {
-    size_t ctrl, ids, gates, xscale, h, y, total;
+    size_t ctrl, hmax, ids, gates, xscale, h, y, total;     // hmax right behind ctrl
 };
 
 MoeLayout moe_layout(const crc_moe& m, int M) {
     const size_t E = (size_t)M * m.K;
     MoeLayout l;
     l.ctrl = 0;
-    l.ids = up256(kCtrlWords * 4);
+    l.hmax = kCtrlWords * 4;
+    l.ids = up256(l.hmax + E * 4);
     l.gates = l.ids + up256(E);
     l.xscale = l.gates + up256(E * 4);
     l.h = l.xscale + up256((size_t)M * 4);
@@ -65,96 +69,66 @@ int check_moe(const crc_moe* m) {
     return CRC_OK;
 }
 
-struct MoeArgs {
-    crc_moe m;
-    const uint16_t* x;
-    const uint8_t* x8;
-    const float* xs8;
-    long long ldx;
-    int M;
-    const uint8_t* ids;
-    const float* gates;
-    __nv_bfloat16* h;                // [M K][f]
-    float* y;                        // [M K][d]
-    uint16_t* out;
-};
-
-__device__ __forceinline__ int slot_of(const crc_moe& m, int e) {
-    const int s = m.expert_slot_dev ? m.expert_slot_dev[e] : e;
-    return s >= 0 && s < m.slots ? s : -1;
-}
-__device__ __forceinline__ float e4m3(uint8_t v) {
-    __nv_fp8_e4m3 q;
-    q.__x = v;
-    return (float)q;
-}
-__device__ __forceinline__ float weight_at(const void* row, int i, bool w8) {
-    return w8 ? e4m3(static_cast<const uint8_t*>(row)[i])
-              : __bfloat162float(static_cast<const __nv_bfloat16*>(row)[i]);
-}
-
-// h = silu(gate x) * up x: a warp a (choice, element of f).
-__global__ void moe_gate_up_kernel(MoeArgs a) {
-    pdl_wait();
-    const crc_moe& m = a.m;
-    const int lane = threadIdx.x & 31;
-    const long long i = (long long)blockIdx.x * (blockDim.x >> 5) + (threadIdx.x >> 5);
-    if (i >= (long long)a.M * m.K * m.f) return;
-    const int entry = (int)(i / m.f), j = (int)(i % m.f), tok = entry / m.K;
-    const int s = slot_of(m, a.ids[entry]);
-    if (s < 0) return;
+// Tensor maps of the weights.  gate and up as (d, 16 rows, gate / up, f / 16,
+// slots), a box of one 128-byte row x 16 x 2 x 4: four groups of 16 gate rows
+// and the 16 up rows of the same elements.  down as (f, d, slots), 128 rows a box.
+bool make_expert_maps(CUtensorMap* m13, CUtensorMap* m2, const crc_moe& m) {
+    auto enc = encode_fn();
+    if (!enc) return false;
     const bool w8 = m.weight_type == CRC_E4M3;
-    const size_t row = (size_t)m.d * (w8 ? 1 : 2);
-    const uint8_t* wg = static_cast<const uint8_t*>(m.gate_up_dev) + s * m.gate_up_stride + j * row;
-    const uint8_t* wu = wg + (size_t)m.f * row;
-    float g = 0.f, u = 0.f;
-    for (int k = lane; k < m.d; k += 32) {
-        const float x = a.x8 ? e4m3(a.x8[(size_t)tok * m.d + k])
-                             : __uint_as_float((uint32_t)a.x[tok * a.ldx + k] << 16);
-        g = fmaf(x, weight_at(wg, k, w8), g);
-        u = fmaf(x, weight_at(wu, k, w8), u);
-    }
-    g = warp_sum(g);
-    u = warp_sum(u);
-    if (a.x8) {
-        g *= a.xs8[tok];
-        u *= a.xs8[tok];
-    }
-    if (w8) {
-        const float* sc = reinterpret_cast<const float*>(
-            reinterpret_cast<const uint8_t*>(m.gate_up_scale_dev) + s * m.gate_up_scale_stride);
-        g *= sc[j];
-        u *= sc[m.f + j];
-    }
-    if (lane == 0) a.h[(size_t)entry * m.f + j] = __float2bfloat16_rn(g / (1.f + expf(-g)) * u);
+    const cuuint64_t es = w8 ? 1 : 2, d = m.d, f = m.f, slots = m.slots;
+    const cuuint32_t bk = w8 ? 128 : 64;
+    const CUtensorMapDataType type =
+        w8 ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16;
+    const cuuint32_t ones[5] = {1, 1, 1, 1, 1};
+    const cuuint64_t dims13[5] = {d, 16, 2, f / 16, slots};
+    const cuuint64_t str13[4] = {d * es, f * d * es, 16 * d * es, (cuuint64_t)m.gate_up_stride};
+    const cuuint32_t box13[5] = {bk, 16, 2, 4, 1};
+    const cuuint64_t dims2[3] = {f, d, slots};
+    const cuuint64_t str2[2] = {f * es, (cuuint64_t)m.down_stride};
+    const cuuint32_t box2[3] = {bk, 128, 1};
+    return enc(m13, type, 5, const_cast<void*>(m.gate_up_dev), dims13, str13, box13, ones,
+               CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+               CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS &&
+           enc(m2, type, 3, const_cast<void*>(m.down_dev), dims2, str2, box2, ones,
+               CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+               CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-// out = sum_k gate_k down_k h_k: a warp a (token, element of d).
-__global__ void moe_down_kernel(MoeArgs a) {
-    const crc_moe& m = a.m;
-    const int lane = threadIdx.x & 31;
-    const long long i = (long long)blockIdx.x * (blockDim.x >> 5) + (threadIdx.x >> 5);
-    if (i >= (long long)a.M * m.d) return;
-    const int tok = (int)(i / m.d), c = (int)(i % m.d);
-    const bool w8 = m.weight_type == CRC_E4M3;
-    float out = 0.f;
-    for (int k = 0; k < m.K; ++k) {
-        const int entry = tok * m.K + k;
-        const int s = slot_of(m, a.ids[entry]);
-        if (s < 0) continue;
-        const uint8_t* w = static_cast<const uint8_t*>(m.down_dev) + s * m.down_stride +
-                           (size_t)c * m.f * (w8 ? 1 : 2);
-        float y = 0.f;
-        for (int j = lane; j < m.f; j += 32)
-            y = fmaf(__bfloat162float(a.h[(size_t)entry * m.f + j]), weight_at(w, j, w8), y);
-        y = warp_sum(y);
-        if (w8)
-            y *= reinterpret_cast<const float*>(
-                reinterpret_cast<const uint8_t*>(m.down_scale_dev) + s * m.down_scale_stride)[c];
-        out = fmaf(a.gates[entry], y, out);
+template <bool W8, int NT>
+int launch_experts(const crc_moe& m, const MoeArgs& a, cudaStream_t stream) {
+    using Cfg = MoeCfg<W8, NT>;
+    auto kern = moe_experts_kernel<W8, NT>;
+    static PerDevice ready;
+    const int up = ready.get(current_device(), [&] {
+        return cuda_status(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                                Cfg::SMEM)) == CRC_OK;
+    });
+    if (!up) return CRC_ECUDA;
+    CUtensorMap m13, m2;
+    if (!make_expert_maps(&m13, &m2, m)) return CRC_ECUDA;
+    // no more CTAs than items there can be
+    const long long experts = (long long)a.M * a.K < a.N ? (long long)a.M * a.K : a.N;
+    const long long items = (experts + (long long)a.M * a.K / NT) * (a.ft + a.dt);
+    cudaLaunchAttribute at[1];
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    cudaLaunchConfig_t c = {};
+    c.gridDim = dim3((unsigned)(items < sm_count() ? items : sm_count()));
+    c.blockDim = dim3(kMoeThreads);
+    c.dynamicSmemBytes = Cfg::SMEM;
+    c.stream = stream;
+    c.attrs = at;
+    c.numAttrs = 1;
+    cudaError_t e;
+    {
+        ProfScope prof(CRC_KERNEL_MOE, stream);
+        e = cudaLaunchKernelEx(&c, kern, m13, m2, a);
     }
-    if (lane == 0) reinterpret_cast<__nv_bfloat16*>(a.out)[(size_t)tok * m.d + c] =
-                       __float2bfloat16_rn(out);
+    note_launch();
+    return cuda_status(e);
 }
 
 int launch_route(const MoeRouteArgs& r, cudaStream_t stream) {
@@ -235,28 +209,41 @@ int crc_moe_layer(const crc_moe* m, const uint16_t* x_dev, int64_t x_stride, con
     r.xscale = m->weight_type == CRC_E4M3 && !x8_dev ? reinterpret_cast<float*>(ws + l.xscale)
                                                      : nullptr;
     r.ctrl = reinterpret_cast<uint32_t*>(ws + l.ctrl);
-    r.ctrl_words = kCtrlWords;
-    if ((rc = launch_route(r, st))) return rc;
-    MoeArgs a;
-    a.m = *m;
-    a.x = x_dev;
-    a.x8 = x8_dev;
-    a.xs8 = x8_scale_dev;
-    a.ldx = x_stride;
-    a.M = M;
+    const bool w8 = m->weight_type == CRC_E4M3;
+    r.ctrl_words = kCtrlWords + (w8 ? M * m->K : 0);
+    MoeArgs a = {};
+    a.x = x8_dev ? x8_dev : reinterpret_cast<const uint8_t*>(x_dev);
+    a.x_bytes = x8_dev ? m->d : 2 * x_stride;
+    a.xs = x8_dev ? x8_scale_dev : r.xscale;
+    a.x_split = w8 && !x8_dev;
     a.ids = r.ids;
     a.gates = r.gates;
+    a.expert_slot = m->expert_slot_dev;
+    a.s13 = m->gate_up_scale_dev;
+    a.s2 = m->down_scale_dev;
+    a.s13_stride = m->gate_up_scale_stride / 4;
+    a.s2_stride = m->down_scale_stride / 4;
     a.h = reinterpret_cast<__nv_bfloat16*>(ws + l.h);
     a.y = reinterpret_cast<float*>(ws + l.y);
-    a.out = out_dev;
-    {
-        ProfScope prof(CRC_KERNEL_MOE, st);
-        moe_gate_up_kernel<<<(unsigned)(((long long)M * m->K * m->f + 7) / 8), 256, 0, st>>>(a);
-        moe_down_kernel<<<(unsigned)(((long long)M * m->d + 7) / 8), 256, 0, st>>>(a);
-    }
-    note_launch();
-    note_launch();
-    return cuda_status(cudaGetLastError());
+    a.hmax = reinterpret_cast<uint32_t*>(ws + l.hmax);
+    a.ctrl = r.ctrl;
+    a.err = device_error_word();
+    a.out = reinterpret_cast<__nv_bfloat16*>(out_dev);
+    a.M = M;
+    a.N = m->N;
+    a.K = m->K;
+    a.d = m->d;
+    a.f = m->f;
+    a.slots = m->slots;
+    const int bk = w8 ? 128 : 64;
+    a.kb1 = (m->d + bk - 1) / bk;
+    a.kb2 = (m->f + bk - 1) / bk;
+    a.ft = (m->f + 63) / 64;
+    a.dt = (m->d + 127) / 128;
+    if ((rc = launch_route(r, st))) return rc;
+    // an expert has at most one row a token, so 16-row tiles hold 16 tokens' rows
+    if (w8) return M <= 16 ? launch_experts<true, 16>(*m, a, st) : launch_experts<true, 64>(*m, a, st);
+    return M <= 16 ? launch_experts<false, 16>(*m, a, st) : launch_experts<false, 64>(*m, a, st);
 }
 
 }  // extern "C"
