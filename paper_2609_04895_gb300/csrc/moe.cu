@@ -131,6 +131,16 @@ int launch_experts(const crc_moe& m, const MoeArgs& a, cudaStream_t stream) {
     return cuda_status(e);
 }
 
+// Rows of a tile: twice an expert's mean share of the choices, so that few experts
+// need a second pass over their weights, or the tokens if that is fewer.
+// Narrow tiles leave room for more row blocks in flight.
+int row_tile(int M, int K, int N) {
+    const int E = M * K;
+    for (int nt = 16; nt < 64; nt *= 2)
+        if (E <= 128 * nt && (M <= nt || 2 * E <= nt * N)) return nt;
+    return 64;
+}
+
 int launch_route(const MoeRouteArgs& r, cudaStream_t stream) {
     cudaLaunchConfig_t c = {};
     c.blockDim = dim3(kRouteThreads);
@@ -241,9 +251,14 @@ int crc_moe_layer(const crc_moe* m, const uint16_t* x_dev, int64_t x_stride, con
     a.ft = (m->f + 63) / 64;
     a.dt = (m->d + 127) / 128;
     if ((rc = launch_route(r, st))) return rc;
-    // an expert has at most one row a token, so 16-row tiles hold 16 tokens' rows
-    if (w8) return M <= 16 ? launch_experts<true, 16>(*m, a, st) : launch_experts<true, 64>(*m, a, st);
-    return M <= 16 ? launch_experts<false, 16>(*m, a, st) : launch_experts<false, 64>(*m, a, st);
+    const int nt = row_tile(M, m->K, m->N);
+    if (w8)
+        return nt == 16   ? launch_experts<true, 16>(*m, a, st)
+               : nt == 32 ? launch_experts<true, 32>(*m, a, st)
+                          : launch_experts<true, 64>(*m, a, st);
+    return nt == 16   ? launch_experts<false, 16>(*m, a, st)
+           : nt == 32 ? launch_experts<false, 32>(*m, a, st)
+                      : launch_experts<false, 64>(*m, a, st);
 }
 
 }  // extern "C"

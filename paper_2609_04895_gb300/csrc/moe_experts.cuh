@@ -1,0 +1,846 @@
+// The experts' products of the mixture-of-experts layer for a few tokens, one
+// persistent kernel:
+//
+//   h_r = silu(G_e x_t) * (U_e x_t)      for every choice r = (token t, expert e)
+//   y_r = D_e h_r,   out_t = sum over t's choices of g_r y_r
+//
+// A few tokens read every active expert's weights once and multiply each by a
+// handful of rows, so the kernel is built to stream weights: they are the A
+// operand (128 weight rows of one tcgen05.mma), the rows that take the expert
+// its N columns (16 at least).  TMA fetches 128-row x 128-byte blocks of
+// weights into a ring that holds as much as shared memory has room for; with
+// 8-bit weights a block is 128 x 128 elements and goes to the tensor cores as it
+// lies in memory.
+//
+// Work items, claimed in order from one counter, so that a CTA waits only for
+// items that running CTAs hold (no co-residency is needed):
+//   1. (row tile, 64 elements of f): gate and up rows of the same elements in one
+//      128-row block, 16 and 16 to a warp's quarter of TMEM, so that silu(gate)
+//      meets up by one exchange inside the warp; h goes to the workspace;
+//   2. (row tile, 128 elements of d): waits until h of the tile is complete (its
+//      weights are on their way meanwhile), y goes to the workspace in fp32;
+//   then all CTAs add up the choices of their share of the tokens, in rank order.
+//
+// 8-bit weights with 16-bit rows: a row is split into two e4m3 pieces of
+// x / s, hi + lo / 16 with s a power of two from the row's largest value, which
+// hold a bf16 value exactly down to 2^-13 of that value; the pieces are two columns of
+// the same product.  So h keeps 16 bits, and no weight is converted.
+#pragma once
+
+#include <cuda_bf16.h>
+
+#include "crc_device.cuh"
+#include "moe_route.cuh"
+
+namespace crc {
+
+constexpr int kMoeThreads = 384;     // warps 0 TMA, 1 MMA, 2-3 idle, 4-7 epilogue, 8-11 rows
+constexpr int kMoeWarps = kMoeThreads / 32;
+constexpr int kMoeMaxTiles = 256;    // row tiles of NT: N + M K / NT at most, M K <= 128 NT
+constexpr int kItemRing = 4;
+constexpr int kCtrlNext = 0, kCtrlDone2 = 1, kCtrlDone1 = 2;
+constexpr int kCtrlWords = kCtrlDone1 + kMoeMaxTiles;
+
+template <bool W8, int NT>
+struct MoeCfg {
+    static constexpr int A_BYTES = 128 * 128;                  // 128 weight rows x 128 bytes
+    static constexpr int BK = W8 ? 128 : 64;                   // elements of a block's row
+    static constexpr int COLS = NT * (W8 ? 2 : 1);             // accumulator columns
+    static constexpr int B_BYTES = COLS * 128;
+    static constexpr int SB = NT == 16 ? 8 : NT == 32 ? 6 : W8 ? 3 : 5;
+    static constexpr int LIST = 128 * NT;                      // choices (M K) at most
+    static constexpr int TMEM_COLS = 2 * (COLS < 16 ? 16 : COLS) < 32 ? 32 : 2 * COLS;
+    static constexpr int TABLE_BYTES = 3 * 128 * 4 + kMoeWarps * 128 * 2 + 3 * kMoeMaxTiles * 2 +
+                                       LIST * 2 + 64;
+    static constexpr int BAR_BYTES = 512;
+    static constexpr int SA =
+        (232448 - 1024 - BAR_BYTES - TABLE_BYTES - SB * B_BYTES) / A_BYTES;
+    static constexpr int SMEM = 1024 + BAR_BYTES + TABLE_BYTES + SB * B_BYTES + SA * A_BYTES;
+    static constexpr int DEPTH = NT == 64 ? 2 : 4;             // row blocks a thread has in flight
+    static_assert(SA > SB && SA <= 16, "weight ring");
+};
+
+struct MoeArgs {
+    const uint8_t* x;                // rows: bf16, or e4m3 with `x_split` 0 and 8-bit weights
+    long long x_bytes;               // bytes between rows
+    const float* xs;                 // [M] scale of x's rows (8-bit weights)
+    int x_split;                     // 8-bit weights: x is bf16 and goes in two pieces
+    const uint8_t* ids;              // [M][K]
+    const float* gates;              // [M][K]
+    const int32_t* expert_slot;      // [N] or null
+    const float *s13, *s2;           // scales of 8-bit weight rows, slots s13_stride floats apart
+    long long s13_stride, s2_stride;
+    __nv_bfloat16* h;                // [M K][f], rows by expert
+    float* y;                        // [M K][d], rows by choice
+    uint32_t* hmax;                  // [M K] largest magnitude of h's rows, zeroed (8-bit weights)
+    uint32_t* ctrl;                  // kCtrlWords, zeroed
+    uint32_t* err;
+    __nv_bfloat16* out;              // [M][d]
+    int M, N, K, d, f, slots;
+    int kb1, kb2;                    // blocks of d, of f
+    int ft, dt;                      // items a row tile: ceil(f / 64), ceil(d / 128)
+};
+
+// One lane of a converged warp.
+__device__ __forceinline__ uint32_t elect_lane() {
+    uint32_t r;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(r));
+    return r;
+}
+// D[tmem] (+)= A[smem] * B[smem]^T, issued by the lane whose `lead` is set.
+template <bool W8>
+__device__ __forceinline__ void umma(uint32_t d_tmem, uint64_t adesc, uint64_t bdesc,
+                                     uint32_t idesc, uint32_t accumulate, uint32_t lead) {
+    if constexpr (W8)
+        asm volatile(
+            "{\n\t.reg .pred p, e;\n\t"
+            "setp.ne.b32 p, %4, 0;\n\t"
+            "setp.ne.b32 e, %5, 0;\n\t"
+            "@e tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}\n" ::"r"(d_tmem),
+            "l"(adesc), "l"(bdesc), "r"(idesc), "r"(accumulate), "r"(lead)
+            : "memory");
+    else
+        asm volatile(
+            "{\n\t.reg .pred p, e;\n\t"
+            "setp.ne.b32 p, %4, 0;\n\t"
+            "setp.ne.b32 e, %5, 0;\n\t"
+            "@e tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}\n" ::"r"(d_tmem),
+            "l"(adesc), "l"(bdesc), "r"(idesc), "r"(accumulate), "r"(lead)
+            : "memory");
+}
+__device__ __forceinline__ void umma_commit_by(uint64_t* bar, uint32_t lead) {
+    asm volatile(
+        "{\n\t.reg .pred e;\n\t"
+        "setp.ne.b32 e, %1, 0;\n\t"
+        "@e tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n\t}" ::"r"(
+            smem_u32(bar)),
+        "r"(lead)
+        : "memory");
+}
+// Instruction descriptor, kind::f8f6f4: e4m3 A and B (K-major), fp32 D, M x N.
+__device__ __forceinline__ uint32_t idesc_e4m3_f32(int M, int N) {
+    return (1u << 4) | ((uint32_t)(N >> 3) << 17) | ((uint32_t)(M >> 4) << 24);
+}
+
+__device__ __forceinline__ void tma_load_5d(void* dst, const CUtensorMap* map, uint64_t* bar,
+                                            int c0, int c1, int c2, int c3, int c4,
+                                            uint64_t policy) {
+    asm volatile(
+        "cp.async.bulk.tensor.5d.shared::cluster.global.tile.mbarrier::complete_tx::bytes"
+        ".L2::cache_hint [%0], [%1, {%2, %3, %4, %5, %6}], [%7], %8;" ::"r"(smem_u32(dst)),
+        "l"(reinterpret_cast<uint64_t>(map)), "r"(c0), "r"(c1), "r"(c2), "r"(c3), "r"(c4),
+        "r"(smem_u32(bar)), "l"(policy)
+        : "memory");
+}
+__device__ __forceinline__ uint64_t l2_evict_normal_policy() {
+    uint64_t p;
+    asm volatile("createpolicy.fractional.L2::evict_normal.b64 %0, 1.0;" : "=l"(p));
+    return p;
+}
+
+__device__ __forceinline__ uint32_t ld_acquire(const uint32_t* p) {
+    uint32_t v;
+    asm volatile("ld.acquire.gpu.global.u32 %0, [%1];" : "=r"(v) : "l"(p) : "memory");
+    return v;
+}
+// Wait until *p reaches n; false on timeout.
+__device__ __forceinline__ bool wait_count(const uint32_t* p, uint32_t n) {
+    if (ld_acquire(p) >= n) return true;
+    const uint64_t t0 = globaltimer_ns();
+    while (true) {
+#pragma unroll 1
+        for (int i = 0; i < 256; ++i)
+            if (ld_acquire(p) >= n) return true;
+        if (globaltimer_ns() - t0 > kWaitLimitNs) return false;
+    }
+}
+
+// Two bf16 (one word) times inv as e4m3 pieces: hi, and lo = 16 (v - hi).
+__device__ __forceinline__ void split_pair(uint32_t w, float inv, uint32_t& hi, uint32_t& lo) {
+    const float a = __uint_as_float(w << 16) * inv, b = __uint_as_float(w & 0xffff0000u) * inv;
+    uint16_t h, l;
+    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(h) : "f"(b), "f"(a));
+    uint32_t back;
+    asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(back) : "h"(h));
+    float fa, fb;
+    asm("{\n\t.reg .b16 x, y;\n\tmov.b32 {x, y}, %2;\n\tcvt.f32.f16 %0, x;\n\tcvt.f32.f16 %1, y;\n\t}"
+        : "=f"(fa), "=f"(fb)
+        : "r"(back));
+    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;"
+        : "=h"(l)
+        : "f"((b - fb) * 16.f), "f"((a - fa) * 16.f));
+    hi = h;
+    lo = l;
+}
+// Sixteen bf16 -> sixteen bytes of each piece.
+__device__ __forceinline__ void split16(const uint4 (&v)[2], float inv, uint4& hi, uint4& lo) {
+    const uint32_t w[8] = {v[0].x, v[0].y, v[0].z, v[0].w, v[1].x, v[1].y, v[1].z, v[1].w};
+    uint32_t ho[4], lw[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        uint32_t h0, l0, h1, l1;
+        split_pair(w[2 * i], inv, h0, l0);
+        split_pair(w[2 * i + 1], inv, h1, l1);
+        ho[i] = h0 | h1 << 16;
+        lw[i] = l0 | l1 << 16;
+    }
+    hi = make_uint4(ho[0], ho[1], ho[2], ho[3]);
+    lo = make_uint4(lw[0], lw[1], lw[2], lw[3]);
+}
+
+template <bool W8, int NT>
+struct MoeShared {
+    using Cfg = MoeCfg<W8, NT>;
+    uint8_t *a, *b;
+    uint64_t *a_full, *a_empty, *b_full, *t_full, *t_empty, *i_full, *i_empty, *drain;
+    uint32_t* tmem_slot;
+    int* items;
+    int* slot;             // [128] slot of each expert, -1 without
+    int* start;            // [128] first row of each expert
+    int* count;            // [128] rows of each expert, then [0] = row tiles
+    uint16_t* wcnt;        // [warps][128]
+    uint16_t *tile_e, *tile_row, *tile_rows;   // [kMoeMaxTiles]
+    uint16_t* list;        // choices sorted by expert, then by index
+
+    __device__ __forceinline__ explicit MoeShared(uint8_t* base) {
+        a = base;
+        b = a + Cfg::SA * Cfg::A_BYTES;
+        uint8_t* p = b + Cfg::SB * Cfg::B_BYTES;
+        a_full = reinterpret_cast<uint64_t*>(p);
+        a_empty = a_full + Cfg::SA;
+        b_full = a_empty + Cfg::SA;
+        t_full = b_full + Cfg::SB;
+        t_empty = t_full + 2;
+        i_full = t_empty + 2;
+        i_empty = i_full + kItemRing;
+        drain = i_empty + kItemRing;
+        tmem_slot = reinterpret_cast<uint32_t*>(drain + 1);
+        items = reinterpret_cast<int*>(tmem_slot + 1);
+        static_assert((2 * Cfg::SA + Cfg::SB + 4 + 2 * kItemRing + 1) * 8 + 4 + 4 * kItemRing <=
+                          Cfg::BAR_BYTES,
+                      "barrier space");
+        slot = reinterpret_cast<int*>(p + Cfg::BAR_BYTES);
+        start = slot + 128;
+        count = start + 128;
+        wcnt = reinterpret_cast<uint16_t*>(count + 128);
+        tile_e = wcnt + kMoeWarps * 128;
+        tile_row = tile_e + kMoeMaxTiles;
+        tile_rows = tile_row + kMoeMaxTiles;
+        list = tile_rows + kMoeMaxTiles;
+    }
+};
+
+// Sorts the choices by expert (stable) and cuts each expert's rows into tiles of
+// NT.  Every CTA builds the same tables.  All threads.
+//
+// One warp does it when the choices are one a lane (one token of up to 32 choices,
+// four of 8): 1.4 us less than the general form, four barriers of which are waits.
+template <bool W8, int NT>
+__device__ __forceinline__ void build_small_tables(const MoeArgs& a, const MoeShared<W8, NT>& s) {
+    const int lane = threadIdx.x & 31, E = a.M * a.K;
+    int e = lane < E ? (int)__ldcg(a.ids + lane) : 128;
+    if (e < 128 && s.slot[e] < 0) e = 128;
+    const uint32_t peers = __match_any_sync(kFull, e);
+    const bool lead = e < 128 && lane == __ffs(peers) - 1;
+    const uint32_t leads = __ballot_sync(kFull, lead);
+    int pos = __popc(peers & ((1u << lane) - 1u)), row0 = 0, tile = 0;
+    for (uint32_t rest = leads; rest; rest &= rest - 1) {
+        const int l = __ffs(rest) - 1;
+        const int other = __shfl_sync(kFull, e, l);
+        const int n = __popc(__shfl_sync(kFull, peers, l));
+        if (other < e) {
+            row0 += n;
+            ++tile;
+        }
+    }
+    if (e < 128) s.list[row0 + pos] = (uint16_t)lane;
+    if (lead) {                      // an expert has one row a token at most: one tile
+        s.tile_e[tile] = (uint16_t)e;
+        s.tile_row[tile] = (uint16_t)row0;
+        s.tile_rows[tile] = (uint16_t)__popc(peers);
+    }
+    if (lane == 0) s.count[0] = __popc(leads);
+}
+
+template <bool W8, int NT>
+__device__ __forceinline__ void build_tables(const MoeArgs& a, const MoeShared<W8, NT>& s) {
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int E = a.M * a.K;
+    if (E <= 32 && a.M <= NT) {
+        if (warp == 0) build_small_tables<W8, NT>(a, s);
+        __syncthreads();
+        return;
+    }
+    uint8_t* ids = s.a;              // scratch: the weight ring is not in use yet
+    for (int i = threadIdx.x; i < E; i += kMoeThreads) {
+        const int e = (int)__ldcg(a.ids + i);
+        ids[i] = (uint8_t)(s.slot[e] < 0 ? 128 : e);
+    }
+    for (int i = threadIdx.x; i < kMoeWarps * 128; i += kMoeThreads) s.wcnt[i] = 0;
+    __syncthreads();
+    // a warp takes a contiguous piece of the choices, 32 at a time
+    const int groups = (E + 31) / 32;
+    const int g0 = groups * warp / kMoeWarps, g1 = groups * (warp + 1) / kMoeWarps;
+    uint16_t* mine = s.wcnt + warp * 128;
+    for (int g = g0; g < g1; ++g) {
+        const int i = 32 * g + lane;
+        const int e = i < E ? (int)ids[i] : 128;
+        const uint32_t peers = __match_any_sync(kFull, e);
+        if (e < 128 && lane == __ffs(peers) - 1) mine[e] += (uint16_t)__popc(peers);
+        __syncwarp();
+    }
+    __syncthreads();
+    if (warp < 4) {                  // rows of an expert before each warp's piece
+        const int e = threadIdx.x;
+        int c[kMoeWarps], n = 0;
+#pragma unroll
+        for (int w = 0; w < kMoeWarps; ++w) c[w] = s.wcnt[w * 128 + e];
+#pragma unroll
+        for (int w = 0; w < kMoeWarps; ++w) {
+            s.wcnt[w * 128 + e] = (uint16_t)n;
+            n += c[w];
+        }
+        s.count[e] = n;
+    }
+    __syncthreads();
+    if (warp == 0) {                 // exclusive sums over experts: rows and tiles
+        int c[4], rows = 0, tiles = 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            c[i] = s.count[4 * lane + i];
+            rows += c[i];
+            tiles += (c[i] + NT - 1) / NT;
+        }
+        int r = rows, t = tiles;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int ur = __shfl_up_sync(kFull, r, o), ut = __shfl_up_sync(kFull, t, o);
+            if (lane >= o) {
+                r += ur;
+                t += ut;
+            }
+        }
+        const int all = __shfl_sync(kFull, t, 31);
+        r -= rows;
+        t -= tiles;
+        __syncwarp();
+        if (lane == 0) s.count[0] = all;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            s.start[4 * lane + i] = r;
+            for (int k = 0; k < c[i]; k += NT, ++t) {
+                s.tile_e[t] = (uint16_t)(4 * lane + i);
+                s.tile_row[t] = (uint16_t)(r + k);
+                s.tile_rows[t] = (uint16_t)(c[i] - k < NT ? c[i] - k : NT);
+            }
+            r += c[i];
+        }
+    }
+    __syncthreads();
+    for (int g = g0; g < g1; ++g) {
+        const int i = 32 * g + lane;
+        const int e = i < E ? (int)ids[i] : 128;
+        const uint32_t peers = __match_any_sync(kFull, e);
+        if (e < 128) {
+            const int before = __popc(peers & ((1u << lane) - 1u));
+            s.list[s.start[e] + mine[e] + before] = (uint16_t)i;
+        }
+        __syncwarp();
+        if (e < 128 && lane == __ffs(peers) - 1) mine[e] += (uint16_t)__popc(peers);
+        __syncwarp();
+    }
+    // the ring's stages go from generic reads and writes to TMA
+    fence_proxy_async_smem();
+    __syncthreads();
+}
+
+// A work item.
+struct MoeItem {
+    int phase, tile, j;      // phase 0: 64 elements of f; 1: 128 elements of d
+    int e, row0, rows;
+};
+template <bool W8, int NT>
+__device__ __forceinline__ MoeItem moe_item(const MoeArgs& a, const MoeShared<W8, NT>& s, int i) {
+    MoeItem it;
+    const int p1 = s.count[0] * a.ft;
+    it.phase = i >= p1;
+    const int k = it.phase ? i - p1 : i, per = it.phase ? a.dt : a.ft;
+    it.tile = k / per;
+    it.j = k - it.tile * per;
+    it.e = s.tile_e[it.tile];
+    it.row0 = s.tile_row[it.tile];
+    it.rows = s.tile_rows[it.tile];
+    return it;
+}
+
+// The row warps' place in their ring.  Block n takes the place of block n - SB,
+// which is free once that block's MMAs are complete: the weight stage of the
+// same block says so (SB < SA, so that stage cannot have moved on by two phases),
+// and one commit a block serves both rings.
+template <bool W8, int NT>
+struct RowRing {
+    using Cfg = MoeCfg<W8, NT>;
+    int stage = 0, free = 0;
+    uint32_t free_phase = 0;
+    int block = 0;                   // up to SB
+    __device__ __forceinline__ void advance() {
+        if (++stage == Cfg::SB) stage = 0;
+        if (block < Cfg::SB) {
+            ++block;
+        } else if (++free == Cfg::SA) {
+            free = 0;
+            free_phase ^= 1;
+        }
+    }
+};
+
+// The rows' blocks of one item into the ring (four warps).  A thread's unit is
+// 16 bytes of one row's 128-byte block: chunk tid % 8 of rows tid / 8, + 16, ...
+// SPLIT: 16 bf16 elements become 16 bytes of hi and of lo.
+template <bool W8, int NT, bool SPLIT>
+__device__ __forceinline__ bool produce_rows(const MoeShared<W8, NT>& s, const uint8_t* (&src)[NT / 16],
+                                             const float (&inv)[NT / 16], uint32_t have, int n8,
+                                             int kb, int K, int tid, RowRing<W8, NT>& ring) {
+    using Cfg = MoeCfg<W8, NT>;
+    constexpr int U = NT / 16, D = Cfg::DEPTH, V = SPLIT ? 2 : 1;
+    constexpr int STEP = SPLIT ? 2 * 128 : 128;                // bytes of a row's block
+    constexpr int CE = SPLIT || W8 ? 16 : 8;                   // elements of a unit
+    const int chunk = tid & 7, lane = tid & 31;
+    uint4 v[D][U][V];
+    auto load = [&](int k, uint4 (&r)[U][V]) {
+        const bool in = k * Cfg::BK + chunk * CE < K;
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int q = 0; q < V; ++q)
+                r[u][q] = in && (have >> u & 1u)
+                              ? __ldcg(reinterpret_cast<const uint4*>(src[u] + (size_t)k * STEP) + q)
+                              : make_uint4(0, 0, 0, 0);
+    };
+#pragma unroll
+    for (int i = 0; i < D; ++i) load(i, v[i]);
+    for (int k0 = 0; k0 < kb; k0 += D) {
+#pragma unroll
+        for (int i = 0; i < D; ++i) {
+            const int k = k0 + i;
+            if (k >= kb) break;
+            if (ring.block >= Cfg::SB && !mbar_wait(&s.a_empty[ring.free], ring.free_phase))
+                return false;
+            uint8_t* dst = s.b + ring.stage * Cfg::B_BYTES;
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                if (!(have >> u & 1u)) continue;
+                const int row = (tid >> 3) + 16 * u;
+                if constexpr (SPLIT) {
+                    uint4 hi, lo;
+                    split16(v[i][u], inv[u], hi, lo);
+                    const int low = n8 + row;
+                    *reinterpret_cast<uint4*>(dst + row * 128 + ((chunk ^ (row & 7)) << 4)) = hi;
+                    *reinterpret_cast<uint4*>(dst + low * 128 + ((chunk ^ (low & 7)) << 4)) = lo;
+                } else {
+                    *reinterpret_cast<uint4*>(dst + row * 128 + ((chunk ^ (row & 7)) << 4)) =
+                        v[i][u][0];
+                }
+            }
+            fence_proxy_async_smem();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&s.b_full[ring.stage]);
+            ring.advance();
+            if (k + D < kb) load(k + D, v[i]);
+        }
+    }
+    return true;
+}
+
+template <bool W8, int NT>
+__global__ void __launch_bounds__(kMoeThreads, 1)
+    moe_experts_kernel(const __grid_constant__ CUtensorMap map13,
+                       const __grid_constant__ CUtensorMap map2, MoeArgs a) {
+    using Cfg = MoeCfg<W8, NT>;
+    extern __shared__ uint8_t smem_raw[];
+    MoeShared<W8, NT> s(reinterpret_cast<uint8_t*>(
+        (reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023)));
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < Cfg::SA; ++i) {
+            mbar_init(&s.a_full[i], 1);
+            mbar_init(&s.a_empty[i], 1);
+        }
+        for (int i = 0; i < Cfg::SB; ++i) mbar_init(&s.b_full[i], 4);
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(&s.t_full[i], 1);
+            mbar_init(&s.t_empty[i], 4);
+        }
+        for (int i = 0; i < kItemRing; ++i) {
+            mbar_init(&s.i_full[i], 1);
+            mbar_init(&s.i_empty[i], 9);
+        }
+        mbar_init(s.drain, 1);
+        fence_mbar_init();
+        tma_prefetch_desc(&map13);
+        tma_prefetch_desc(&map2);
+    }
+    if (warp == 1) {
+        tmem_alloc(s.tmem_slot, Cfg::TMEM_COLS);
+        tmem_relinquish();
+    }
+    // the map from experts to slots is an input: the routing kernel does not write it
+    if (threadIdx.x < 128) {
+        const int e = threadIdx.x;
+        const int at = e >= a.N ? -1 : a.expert_slot ? a.expert_slot[e] : e;
+        s.slot[e] = at >= 0 && at < a.slots ? at : -1;
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = *s.tmem_slot;
+
+    pdl_wait();                       // the choices and the zeroed counters are in place
+    int next = 0;
+    if (threadIdx.x == 0) next = (int)atomicAdd(&a.ctrl[kCtrlNext], 1u);
+    build_tables<W8, NT>(a, s);
+    const int tiles = s.count[0];
+    const int total = tiles * (a.ft + a.dt);
+
+    if (warp == 0) {
+        // ------------------------------------------------------ weights by TMA
+        if (lane == 0) {
+            const uint64_t once = l2_evict_first_policy(), again = l2_evict_normal_policy();
+            int stage = 0, issued = 0, islot = 0;
+            uint32_t phase = 0, iphase = 0;
+            bool failed = false;
+            while (!failed) {
+                const int item = next < total ? next : -1;
+                if (!mbar_wait(&s.i_empty[islot], iphase ^ 1)) {
+                    failed = true;
+                    break;
+                }
+                s.items[islot] = item;
+                mbar_arrive(&s.i_full[islot]);
+                if (++islot == kItemRing) {
+                    islot = 0;
+                    iphase ^= 1;
+                }
+                if (item < 0) break;
+                next = (int)atomicAdd(&a.ctrl[kCtrlNext], 1u);
+                const MoeItem it = moe_item<W8, NT>(a, s, item);
+                const int slot = s.slot[it.e];
+                // an expert with several row tiles (all but the last are full) is
+                // read again, from L2
+                const uint64_t pol = it.rows == NT ? again : once;
+                const int kb = it.phase ? a.kb2 : a.kb1;
+                for (int k = 0; k < kb; ++k) {
+                    if (!mbar_wait(&s.a_empty[stage], phase ^ 1)) {
+                        failed = true;
+                        break;
+                    }
+                    mbar_arrive_expect_tx(&s.a_full[stage], Cfg::A_BYTES);
+                    uint8_t* dst = s.a + stage * Cfg::A_BYTES;
+                    if (it.phase == 0)
+                        tma_load_5d(dst, &map13, &s.a_full[stage], k * Cfg::BK, 0, 0, it.j * 4,
+                                    slot, pol);
+                    else
+                        tma_load_3d(dst, &map2, &s.a_full[stage], k * Cfg::BK, it.j * 128, slot,
+                                    pol);
+                    ++issued;
+                    if (++stage == Cfg::SA) {
+                        stage = 0;
+                        phase ^= 1;
+                    }
+                }
+            }
+            if (failed) latch_error(a.err, CRC_ETIMEOUT);
+            // Never leave with copies in flight.
+            for (int k = issued < Cfg::SA ? issued : Cfg::SA; k > 0; --k) {
+                if (--stage < 0) {
+                    stage = Cfg::SA - 1;
+                    phase ^= 1;
+                }
+                if (!mbar_wait(&s.a_full[stage], phase)) latch_error(a.err, CRC_ETIMEOUT);
+            }
+        }
+    } else if (warp == 1) {
+        // ------------------------------------------------------ MMA
+        // The whole warp walks the blocks with uniform control flow and one lane
+        // issues: descriptors then live in uniform registers.
+        const uint32_t lead = elect_lane();
+        const uint64_t a0 = sw128_kmajor_desc(smem_u32(s.a)), b0 = sw128_kmajor_desc(smem_u32(s.b));
+        const int p1 = __reduce_max_sync(kFull, tiles * a.ft);
+        int stage = 0, bstage = 0, islot = 0, acc = 0;
+        uint32_t phase = 0, bphase = 0, iphase = 0, aphase = 0;
+        bool failed = false;
+        while (true) {
+            if (__any_sync(kFull, !mbar_wait(&s.i_full[islot], iphase))) {
+                failed = true;
+                break;
+            }
+            const int item = __reduce_max_sync(kFull, s.items[islot]);
+            if (lead) mbar_arrive(&s.i_empty[islot]);
+            if (++islot == kItemRing) {
+                islot = 0;
+                iphase ^= 1;
+            }
+            if (item < 0) break;
+            const bool second = item >= p1;
+            const int rows = __reduce_max_sync(kFull, moe_item<W8, NT>(a, s, item).rows);
+            const bool split = W8 && (second || a.x_split);
+            const int n = split ? 2 * ((rows + 7) & ~7) : (rows + 15) & ~15;
+            const uint32_t idesc = W8 ? idesc_e4m3_f32(128, n) : idesc_bf16_f32(128, n);
+            if (__any_sync(kFull, !mbar_wait(&s.t_empty[acc], aphase ^ 1))) {
+                failed = true;
+                break;
+            }
+            tc_fence_after();
+            const uint32_t dt = tmem + (uint32_t)(acc * Cfg::COLS);
+            const int kb = second ? a.kb2 : a.kb1;
+            for (int k = 0; k < kb; ++k) {
+                const bool ok = mbar_wait(&s.b_full[bstage], bphase) &&
+                                mbar_wait(&s.a_full[stage], phase);
+                if (__any_sync(kFull, !ok)) {
+                    failed = true;
+                    break;
+                }
+                tc_fence_after();
+                const uint64_t ad = a0 + (uint64_t)(stage * (Cfg::A_BYTES >> 4));
+                const uint64_t bd = b0 + (uint64_t)(bstage * (Cfg::B_BYTES >> 4));
+#pragma unroll
+                for (int q = 0; q < 4; ++q)             // 32 bytes of K a step
+                    umma<W8>(dt, ad + 2 * q, bd + 2 * q, idesc, (k | q) != 0, lead);
+                umma_commit_by(&s.a_empty[stage], lead);
+                if (++stage == Cfg::SA) {
+                    stage = 0;
+                    phase ^= 1;
+                }
+                if (++bstage == Cfg::SB) {
+                    bstage = 0;
+                    bphase ^= 1;
+                }
+            }
+            if (failed) break;
+            umma_commit_by(&s.t_full[acc], lead);
+            acc ^= 1;
+            if (acc == 0) aphase ^= 1;
+        }
+        if (failed && lead) latch_error(a.err, CRC_ETIMEOUT);
+        // All issued MMAs must be complete before TMEM is released.
+        umma_commit_by(s.drain, lead);
+        if (!mbar_wait(s.drain, 0)) latch_error(a.err, CRC_ETIMEOUT);
+    } else if (warp >= 8) {
+        // ------------------------------------------------------ rows
+        const int tid = threadIdx.x - 256;
+        RowRing<W8, NT> ring;
+        int islot = 0;
+        uint32_t iphase = 0;
+        bool failed = false;
+        while (true) {
+            if (!mbar_wait(&s.i_full[islot], iphase)) {
+                failed = true;
+                break;
+            }
+            const int item = s.items[islot];
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&s.i_empty[islot]);
+            if (++islot == kItemRing) {
+                islot = 0;
+                iphase ^= 1;
+            }
+            if (item < 0) break;
+            const MoeItem it = moe_item<W8, NT>(a, s, item);
+            if (it.phase) {           // h of the whole tile, from all its items
+                bool ok = true;
+                if (lane == 0) ok = wait_count(&a.ctrl[kCtrlDone1 + it.tile], 4u * a.ft);
+                if (!__shfl_sync(kFull, (int)ok, 0)) {
+                    failed = true;
+                    break;
+                }
+                __syncwarp();         // lane 0's acquire orders the whole warp's loads
+            }
+            const bool split = W8 && (it.phase || a.x_split);
+            const int n8 = (it.rows + 7) & ~7;
+            const uint8_t* src[NT / 16];
+            float inv[NT / 16];
+            uint32_t have = 0;
+#pragma unroll
+            for (int u = 0; u < NT / 16; ++u) {
+                const int r = (tid >> 3) + 16 * u;
+                src[u] = nullptr;
+                inv[u] = 1.f;
+                if (r >= it.rows) continue;
+                have |= 1u << u;
+                if (it.phase) {
+                    src[u] = reinterpret_cast<const uint8_t*>(a.h + (size_t)(it.row0 + r) * a.f);
+                    if (W8)
+                        inv[u] = 1.f / split_scale(__uint_as_float(__ldcg(a.hmax + it.row0 + r)));
+                } else {
+                    const int tok = s.list[it.row0 + r] / a.K;
+                    src[u] = a.x + tok * a.x_bytes;
+                    if (W8 && split) inv[u] = 1.f / __ldcg(a.xs + tok);
+                }
+                src[u] += (tid & 7) * (split ? 32 : 16);
+            }
+            const int kb = it.phase ? a.kb2 : a.kb1, K = it.phase ? a.f : a.d;
+            bool ok;
+            if (W8 && split)
+                ok = produce_rows<W8, NT, W8>(s, src, inv, have, n8, kb, K, tid, ring);
+            else
+                ok = produce_rows<W8, NT, false>(s, src, inv, have, n8, kb, K, tid, ring);
+            if (!ok) {
+                failed = true;
+                break;
+            }
+        }
+        if (failed && lane == 0) latch_error(a.err, CRC_ETIMEOUT);
+    } else if (warp >= 4) {
+        // ------------------------------------------------------ epilogue
+        const int quarter = warp & 3;
+        int islot = 0, acc = 0;
+        uint32_t iphase = 0, aphase = 0;
+        bool failed = false;
+        while (true) {
+            if (!mbar_wait(&s.i_full[islot], iphase)) {
+                failed = true;
+                break;
+            }
+            const int item = s.items[islot];
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&s.i_empty[islot]);
+            if (++islot == kItemRing) {
+                islot = 0;
+                iphase ^= 1;
+            }
+            if (item < 0) break;
+            const MoeItem it = moe_item<W8, NT>(a, s, item);
+            const int slot = s.slot[it.e];
+            const bool split = W8 && (it.phase || a.x_split);
+            const int n8 = (it.rows + 7) & ~7;
+            // this lane's weight row: an element of f (gate in the low half of the
+            // warp, up in the high half), or of d
+            const int wrow = it.phase ? it.j * 128 + quarter * 32 + lane
+                                      : it.j * 64 + quarter * 16 + (lane & 15);
+            const bool in = wrow < (it.phase ? a.d : a.f);
+            float sw = 1.f;
+            if (W8 && in)
+                sw = it.phase ? a.s2[slot * a.s2_stride + wrow]
+                              : a.s13[slot * a.s13_stride + (lane >> 4) * a.f + wrow];
+            if (!mbar_wait(&s.t_full[acc], aphase)) {
+                failed = true;
+                break;
+            }
+            tc_fence_after();
+            const uint32_t tb =
+                tmem + (uint32_t)(acc * Cfg::COLS) + ((uint32_t)(quarter * 32) << 16);
+#pragma unroll 1
+            for (int c0 = 0; c0 < it.rows; c0 += 16) {
+                float v[16];
+                tmem_ld16f(tb + c0, v);
+                if (W8 && split) {
+                    float lo[16];
+                    tmem_ld16f(tb + n8 + c0, lo);
+                    tmem_ld_wait();
+                    pin16(v);
+                    pin16(lo);
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) v[i] = fmaf(lo[i], 0.0625f, v[i]);
+                } else {
+                    tmem_ld_wait();
+                    pin16(v);
+                }
+                if (c0 + 16 >= it.rows) {          // read whole: hand it back
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(&s.t_empty[acc]);
+                }
+                const int n = it.rows - c0 < 16 ? it.rows - c0 : 16;
+                if (it.phase == 0) {
+#pragma unroll
+                    for (int c = 0; c < 16; c += 2) {
+                        if (c >= n) break;
+                        float p0 = v[c], p1 = v[c + 1];
+                        if (W8) {
+                            const int r = it.row0 + c0 + c;
+                            const int r1 = c + 1 < n ? r + 1 : r;
+                            p0 *= sw * __ldcg(a.xs + s.list[r] / a.K);
+                            p1 *= sw * __ldcg(a.xs + s.list[r1] / a.K);
+                        }
+                        // low half: column c, high half: column c + 1
+                        const float got = __shfl_xor_sync(kFull, lane < 16 ? p1 : p0, 16);
+                        const float gate = lane < 16 ? p0 : got, up = lane < 16 ? got : p1;
+                        const float hv = gate / (1.f + __expf(-gate)) * up;
+                        const __nv_bfloat16 hb = __float2bfloat16_rn(hv);
+                        const int col = c + (lane >> 4);
+                        const int row = it.row0 + c0 + col;
+                        if (in && col < n) a.h[(size_t)row * a.f + wrow] = hb;
+                        if (W8) {
+                            uint32_t m =
+                                in ? (uint32_t)(__bfloat16_as_ushort(hb) & 0x7fffu) << 16 : 0u;
+#pragma unroll
+                            for (int o = 8; o > 0; o >>= 1)
+                                m = max(m, __shfl_xor_sync(kFull, m, o));
+                            if ((lane & 15) == 0 && col < n && m) atomicMax(a.hmax + row, m);
+                        }
+                    }
+                } else {
+#pragma unroll
+                    for (int c = 0; c < 16; ++c) {
+                        if (c >= n) break;
+                        float p = v[c];
+                        const int row = it.row0 + c0 + c;
+                        if (W8) p *= sw * split_scale(__uint_as_float(__ldcg(a.hmax + row)));
+                        if (in) a.y[(size_t)s.list[row] * a.d + wrow] = p;
+                    }
+                }
+            }
+            acc ^= 1;
+            if (acc == 0) aphase ^= 1;
+            __syncwarp();
+            if (lane == 0) {
+                __threadfence();
+                atomicAdd(&a.ctrl[it.phase ? kCtrlDone2 : kCtrlDone1 + it.tile], 1u);
+            }
+        }
+        if (failed && lane == 0) latch_error(a.err, CRC_ETIMEOUT);
+    }
+    __syncwarp();
+    tc_fence_before();
+    __syncthreads();
+    if (warp == 1) {
+        tc_fence_after();
+        tmem_dealloc(tmem, Cfg::TMEM_COLS);
+    }
+
+    // -------------------------------------------------------- the choices' sum
+    if (threadIdx.x == 0) {
+        const bool ok = wait_count(&a.ctrl[kCtrlDone2], 4u * (uint32_t)(tiles * a.dt));
+        if (!ok) latch_error(a.err, CRC_ETIMEOUT);
+        s.items[0] = ok;
+    }
+    __syncthreads();
+    if (!s.items[0]) return;
+    const int quads = a.d / 4;
+    const long long all = (long long)a.M * quads;
+    for (long long i = (long long)blockIdx.x * kMoeThreads + threadIdx.x; i < all;
+         i += (long long)gridDim.x * kMoeThreads) {
+        const int tok = (int)(i / quads), c = (int)(i - (long long)tok * quads) * 4;
+        float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+        for (int k = 0; k < a.K; ++k) {
+            const int r = tok * a.K + k;
+            if (s.slot[__ldcg(a.ids + r)] < 0) continue;
+            const float g = __ldcg(a.gates + r);
+            const float4 y = __ldcg(reinterpret_cast<const float4*>(a.y + (size_t)r * a.d + c));
+            o.x = fmaf(g, y.x, o.x);
+            o.y = fmaf(g, y.y, o.y);
+            o.z = fmaf(g, y.z, o.z);
+            o.w = fmaf(g, y.w, o.w);
+        }
+        const __nv_bfloat162 p = __floats2bfloat162_rn(o.x, o.y), q = __floats2bfloat162_rn(o.z, o.w);
+        uint2 w;
+        w.x = *reinterpret_cast<const uint32_t*>(&p);
+        w.y = *reinterpret_cast<const uint32_t*>(&q);
+        *reinterpret_cast<uint2*>(a.out + (size_t)tok * a.d + c) = w;
+    }
+}
+
+}  // namespace crc

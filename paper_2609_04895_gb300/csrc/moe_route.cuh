@@ -164,7 +164,7 @@ __global__ void __launch_bounds__(kRouteThreads)
         const uint4 zero = make_uint4(0, 0, 0, 0);
         // The order of k inside a product is free as long as both operands share
         // it: a thread's 16 contiguous bytes of a row serve two k16 steps.
-#pragma unroll 4
+#pragma unroll 8
         for (int c = c0; c < c1; ++c) {
             const bool in = 32 * c + 8 * t < a.d;
             const uint4 xa = in && r0 ? *reinterpret_cast<const uint4*>(x0 + 32 * c) : zero;
