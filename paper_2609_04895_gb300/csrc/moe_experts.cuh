@@ -34,7 +34,7 @@
 
 namespace crc {
 
-constexpr int kMoeThreads = 384;     // warps 0 TMA, 1 MMA, 2-3 idle, 4-7 epilogue, 8-11 rows
+constexpr int kMoeThreads = 512;     // warps 0 TMA, 1 MMA, 2-3 idle, 4-7 epilogue, 8-15 rows
 constexpr int kMoeWarps = kMoeThreads / 32;
 constexpr int kMoeMaxTiles = 256;    // row tiles of NT: N + M K / NT at most, M K <= 128 NT
 constexpr int kItemRing = 4;
@@ -56,7 +56,7 @@ struct MoeCfg {
     static constexpr int SA =
         (232448 - 1024 - BAR_BYTES - TABLE_BYTES - SB * B_BYTES) / A_BYTES;
     static constexpr int SMEM = 1024 + BAR_BYTES + TABLE_BYTES + SB * B_BYTES + SA * A_BYTES;
-    static constexpr int DEPTH = NT == 64 ? 2 : 4;             // row blocks a thread has in flight
+    static constexpr int DEPTH = NT == 16 ? 4 : NT == 32 ? 2 : 1;   // row blocks a thread has in flight
     static_assert(SA > SB && SA <= 16, "weight ring");
 };
 
@@ -375,34 +375,40 @@ __device__ __forceinline__ MoeItem moe_item(const MoeArgs& a, const MoeShared<W8
     return it;
 }
 
-// The row warps' place in their ring.  Block n takes the place of block n - SB,
-// which is free once that block's MMAs are complete: the weight stage of the
-// same block says so (SB < SA, so that stage cannot have moved on by two phases),
-// and one commit a block serves both rings.
+// A row group's place in the ring of row blocks.  Two groups of four warps take
+// the blocks alternately.  Block n takes the place of block n - SB, which is free
+// once that block's MMAs are complete: the weight stage of the same block says so
+// (SB < SA, so that stage cannot have moved on by two phases), and one commit a
+// block serves both rings.
 template <bool W8, int NT>
 struct RowRing {
     using Cfg = MoeCfg<W8, NT>;
-    int stage = 0, free = 0;
+    int next;                        // this group's next block, counted over all items
+    int stage, free;                 // its place; the weight stage of block next - SB
     uint32_t free_phase = 0;
-    int block = 0;                   // up to SB
+    __device__ __forceinline__ explicit RowRing(int group)
+        : next(group), stage(group), free(group - Cfg::SB) {}
     __device__ __forceinline__ void advance() {
-        if (++stage == Cfg::SB) stage = 0;
-        if (block < Cfg::SB) {
-            ++block;
-        } else if (++free == Cfg::SA) {
-            free = 0;
+        next += 2;
+        stage += 2;
+        if (stage >= Cfg::SB) stage -= Cfg::SB;
+        free += 2;
+        if (free >= Cfg::SA) {
+            free -= Cfg::SA;
             free_phase ^= 1;
         }
     }
 };
 
-// The rows' blocks of one item into the ring (four warps).  A thread's unit is
+// A group's row blocks of one item into the ring (four warps).  base: the item's
+// first block, counted over all items.  A thread's unit is
 // 16 bytes of one row's 128-byte block: chunk tid % 8 of rows tid / 8, + 16, ...
 // SPLIT: 16 bf16 elements become 16 bytes of hi and of lo.
 template <bool W8, int NT, bool SPLIT>
 __device__ __forceinline__ bool produce_rows(const MoeShared<W8, NT>& s, const uint8_t* (&src)[NT / 16],
                                              const float (&inv)[NT / 16], uint32_t have, int n8,
-                                             int kb, int K, int tid, RowRing<W8, NT>& ring) {
+                                             int base, int kb, int K, int tid,
+                                             RowRing<W8, NT>& ring) {
     using Cfg = MoeCfg<W8, NT>;
     constexpr int U = NT / 16, D = Cfg::DEPTH, V = SPLIT ? 2 : 1;
     constexpr int STEP = SPLIT ? 2 * 128 : 128;                // bytes of a row's block
@@ -419,14 +425,15 @@ __device__ __forceinline__ bool produce_rows(const MoeShared<W8, NT>& s, const u
                               ? __ldcg(reinterpret_cast<const uint4*>(src[u] + (size_t)k * STEP) + q)
                               : make_uint4(0, 0, 0, 0);
     };
+    const int first = ring.next - base;
 #pragma unroll
-    for (int i = 0; i < D; ++i) load(i, v[i]);
-    for (int k0 = 0; k0 < kb; k0 += D) {
+    for (int i = 0; i < D; ++i) load(first + 2 * i, v[i]);
+    for (int k0 = first; k0 < kb; k0 += 2 * D) {
 #pragma unroll
         for (int i = 0; i < D; ++i) {
-            const int k = k0 + i;
+            const int k = k0 + 2 * i;
             if (k >= kb) break;
-            if (ring.block >= Cfg::SB && !mbar_wait(&s.a_empty[ring.free], ring.free_phase))
+            if (ring.next >= Cfg::SB && !mbar_wait(&s.a_empty[ring.free], ring.free_phase))
                 return false;
             uint8_t* dst = s.b + ring.stage * Cfg::B_BYTES;
 #pragma unroll
@@ -448,7 +455,7 @@ __device__ __forceinline__ bool produce_rows(const MoeShared<W8, NT>& s, const u
             __syncwarp();
             if (lane == 0) mbar_arrive(&s.b_full[ring.stage]);
             ring.advance();
-            if (k + D < kb) load(k + D, v[i]);
+            if (k + 2 * D < kb) load(k + 2 * D, v[i]);
         }
     }
     return true;
@@ -476,7 +483,7 @@ __global__ void __launch_bounds__(kMoeThreads, 1)
         }
         for (int i = 0; i < kItemRing; ++i) {
             mbar_init(&s.i_full[i], 1);
-            mbar_init(&s.i_empty[i], 9);
+            mbar_init(&s.i_empty[i], 13);        // MMA, 4 epilogue, 8 row warps
         }
         mbar_init(s.drain, 1);
         fence_mbar_init();
@@ -525,13 +532,14 @@ __global__ void __launch_bounds__(kMoeThreads, 1)
                     iphase ^= 1;
                 }
                 if (item < 0) break;
-                next = (int)atomicAdd(&a.ctrl[kCtrlNext], 1u);
                 const MoeItem it = moe_item<W8, NT>(a, s, item);
                 const int slot = s.slot[it.e];
                 // an expert with several row tiles (all but the last are full) is
                 // read again, from L2
                 const uint64_t pol = it.rows == NT ? again : once;
                 const int kb = it.phase ? a.kb2 : a.kb1;
+                const int first = stage;
+                const uint32_t first_phase = phase;
                 for (int k = 0; k < kb; ++k) {
                     if (!mbar_wait(&s.a_empty[stage], phase ^ 1)) {
                         failed = true;
@@ -551,6 +559,15 @@ __global__ void __launch_bounds__(kMoeThreads, 1)
                         phase ^= 1;
                     }
                 }
+                if (failed) break;
+                // The next item is claimed once this one's first block is consumed: a
+                // CTA that waits for h would otherwise take items that idle CTAs could
+                // have (one Qwen3-shaped token: all 128 down items on 56 CTAs).
+                if (kb <= Cfg::SA && !mbar_wait(&s.a_empty[first], first_phase)) {
+                    failed = true;
+                    break;
+                }
+                next = (int)atomicAdd(&a.ctrl[kCtrlNext], 1u);
             }
             if (failed) latch_error(a.err, CRC_ETIMEOUT);
             // Never leave with copies in flight.
@@ -630,9 +647,9 @@ __global__ void __launch_bounds__(kMoeThreads, 1)
         if (!mbar_wait(s.drain, 0)) latch_error(a.err, CRC_ETIMEOUT);
     } else if (warp >= 8) {
         // ------------------------------------------------------ rows
-        const int tid = threadIdx.x - 256;
-        RowRing<W8, NT> ring;
-        int islot = 0;
+        const int tid = threadIdx.x & 127;
+        RowRing<W8, NT> ring((warp - 8) >> 2);
+        int islot = 0, base = 0;
         uint32_t iphase = 0;
         bool failed = false;
         while (true) {
@@ -684,13 +701,14 @@ __global__ void __launch_bounds__(kMoeThreads, 1)
             const int kb = it.phase ? a.kb2 : a.kb1, K = it.phase ? a.f : a.d;
             bool ok;
             if (W8 && split)
-                ok = produce_rows<W8, NT, W8>(s, src, inv, have, n8, kb, K, tid, ring);
+                ok = produce_rows<W8, NT, W8>(s, src, inv, have, n8, base, kb, K, tid, ring);
             else
-                ok = produce_rows<W8, NT, false>(s, src, inv, have, n8, kb, K, tid, ring);
+                ok = produce_rows<W8, NT, false>(s, src, inv, have, n8, base, kb, K, tid, ring);
             if (!ok) {
                 failed = true;
                 break;
             }
+            base += kb;
         }
         if (failed && lane == 0) latch_error(a.err, CRC_ETIMEOUT);
     } else if (warp >= 4) {

@@ -117,6 +117,20 @@ __device__ __forceinline__ void mma_bf16_16x8x16(float (&c)[4], uint32_t a0, uin
         : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 
+// Largest magnitude of eight bf16, as the bits of a float: a NaN counts as the largest.
+__device__ __forceinline__ uint32_t max_abs(const uint4& v) {
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+    uint32_t m = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) m = max(m, max(w[i] << 16 & 0x7fffffffu, w[i] & 0x7fff0000u));
+    return m;
+}
+
+__device__ __forceinline__ uint32_t dsm_u32(uint32_t addr) {
+    uint32_t v;
+    asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(addr));
+    return v;
+}
 __device__ __forceinline__ float dsm_f32(uint32_t addr) {
     float v;
     asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(addr));
@@ -138,101 +152,114 @@ __device__ __forceinline__ float split_scale(float amax) {
     return __uint_as_float((ex < 8u ? 1u : ex - 7u) << 23);
 }
 
+// A warp multiplies two tiles of 8 experts; with fewer than 128 experts the
+// warps that are left split d further.
 __global__ void __launch_bounds__(kRouteThreads)
     moe_route_kernel(MoeRouteArgs a) {
-    __shared__ float part[kRouteTokens][kMoeMaxN];
-    __shared__ float amax_sm[kRouteTokens];
-    zero_ctrl(a);
+    constexpr int WARPS = kRouteThreads / 32, BATCH = 8;
+    __shared__ float part[WARPS][kRouteTokens][16];
+    __shared__ uint32_t amax_sm[WARPS][kRouteTokens];
     pdl_launch_dependents();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int rank = (int)cluster_ctarank();
     const int t0 = (int)(blockIdx.x / kRouteCtas) * kRouteTokens;
     const int g = lane >> 2, t = lane & 3;
-    // this CTA's chunks of 32 elements of d
-    const int nch = (a.d + 31) / 32;
-    const int c0 = nch * rank / kRouteCtas, c1 = nch * (rank + 1) / kRouteCtas;
-    const int tiles = a.N / 8;                       // tiles of 8 experts: this warp's warp, warp + 8
-    const bool lo = warp < tiles, hi = warp + 8 < tiles;
-    const bool r0 = t0 + g < a.M, r1 = t0 + g + 8 < a.M;
-    const uint16_t* x0 = a.x + (long long)(r0 ? t0 + g : 0) * a.ldx + 8 * t;
-    const uint16_t* x1 = a.x + (long long)(r1 ? t0 + g + 8 : 0) * a.ldx + 8 * t;
-    const uint16_t* w0 = a.w + (size_t)(lo ? warp * 8 + g : 0) * a.d + 8 * t;
-    const uint16_t* w1 = a.w + (size_t)(hi ? (warp + 8) * 8 + g : 0) * a.d + 8 * t;
+    const int pairs = a.N / 16, split = WARPS / pairs;     // tile pairs; warps a pair
+    const int pair = warp / split;
     float acc0[4] = {}, acc1[4] = {};
-    float am0 = 0.f, am1 = 0.f;
-    if (lo) {
+    uint32_t am0 = 0, am1 = 0;
+    if (pair < pairs) {
+        // this warp's chunks of 32 elements of d
+        const int nch = (a.d + 31) / 32, slices = kRouteCtas * split;
+        const int slice = rank * split + warp % split;
+        const int c0 = nch * slice / slices, c1 = nch * (slice + 1) / slices;
+        const bool r0 = t0 + g < a.M, r1 = t0 + g + 8 < a.M;
+        const uint16_t* x0 = a.x + (long long)(r0 ? t0 + g : 0) * a.ldx + 8 * t;
+        const uint16_t* x1 = a.x + (long long)(r1 ? t0 + g + 8 : 0) * a.ldx + 8 * t;
+        const uint16_t* w0 = a.w + (size_t)(pair * 16 + g) * a.d + 8 * t;
+        const uint16_t* w1 = w0 + (size_t)8 * a.d;
         const uint4 zero = make_uint4(0, 0, 0, 0);
-        // The order of k inside a product is free as long as both operands share
-        // it: a thread's 16 contiguous bytes of a row serve two k16 steps.
-#pragma unroll 8
-        for (int c = c0; c < c1; ++c) {
-            const bool in = 32 * c + 8 * t < a.d;
-            const uint4 xa = in && r0 ? *reinterpret_cast<const uint4*>(x0 + 32 * c) : zero;
-            const uint4 xb = in && r1 ? *reinterpret_cast<const uint4*>(x1 + 32 * c) : zero;
-            const uint4 wa = in ? *reinterpret_cast<const uint4*>(w0 + 32 * c) : zero;
-            const uint4 wb = in && hi ? *reinterpret_cast<const uint4*>(w1 + 32 * c) : zero;
-            mma_bf16_16x8x16(acc0, xa.x, xb.x, xa.y, xb.y, wa.x, wa.y);
-            mma_bf16_16x8x16(acc0, xa.z, xb.z, xa.w, xb.w, wa.z, wa.w);
-            if (hi) {
-                mma_bf16_16x8x16(acc1, xa.x, xb.x, xa.y, xb.y, wb.x, wb.y);
-                mma_bf16_16x8x16(acc1, xa.z, xb.z, xa.w, xb.w, wb.z, wb.w);
-            }
-            if (a.xscale && warp == 0) {
-                const uint32_t ua[4] = {xa.x, xa.y, xa.z, xa.w}, ub[4] = {xb.x, xb.y, xb.z, xb.w};
+        // Every load of a batch is asked for before the first is used: one token is
+        // bound by the latency of memory.
+        for (int c = c0; c < c1; c += BATCH) {
+            uint4 xa[BATCH], xb[BATCH], wa[BATCH], wb[BATCH];
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    // magnitudes as integers: a NaN counts as the largest
-                    am0 = __uint_as_float(max(__float_as_uint(am0),
-                                              max(ua[i] << 16 & 0x7fffffffu,
-                                                  ua[i] & 0x7fff0000u)));
-                    am1 = __uint_as_float(max(__float_as_uint(am1),
-                                              max(ub[i] << 16 & 0x7fffffffu,
-                                                  ub[i] & 0x7fff0000u)));
+            for (int i = 0; i < BATCH; ++i) {
+                const int k = 32 * (c + i);
+                const bool in = c + i < c1 && k + 8 * t < a.d;
+                wa[i] = in ? *reinterpret_cast<const uint4*>(w0 + k) : zero;
+                wb[i] = in ? *reinterpret_cast<const uint4*>(w1 + k) : zero;
+                xa[i] = in && r0 ? *reinterpret_cast<const uint4*>(x0 + k) : zero;
+                xb[i] = in && r1 ? *reinterpret_cast<const uint4*>(x1 + k) : zero;
+            }
+            // The order of k inside a product is free as long as both operands share
+            // it: a thread's 16 contiguous bytes of a row serve two k16 steps.
+#pragma unroll
+            for (int i = 0; i < BATCH; ++i) {
+                if (c + i >= c1) break;
+                mma_bf16_16x8x16(acc0, xa[i].x, xb[i].x, xa[i].y, xb[i].y, wa[i].x, wa[i].y);
+                mma_bf16_16x8x16(acc1, xa[i].x, xb[i].x, xa[i].y, xb[i].y, wb[i].x, wb[i].y);
+                mma_bf16_16x8x16(acc0, xa[i].z, xb[i].z, xa[i].w, xb[i].w, wa[i].z, wa[i].w);
+                mma_bf16_16x8x16(acc1, xa[i].z, xb[i].z, xa[i].w, xb[i].w, wb[i].z, wb[i].w);
+                if (a.xscale) {
+                    am0 = max(am0, max_abs(xa[i]));
+                    am1 = max(am1, max_abs(xb[i]));
                 }
             }
         }
-        const int n = warp * 8 + 2 * t;
-        part[g][n] = acc0[0];
-        part[g][n + 1] = acc0[1];
-        part[g + 8][n] = acc0[2];
-        part[g + 8][n + 1] = acc0[3];
-        if (hi) {
-            part[g][n + 64] = acc1[0];
-            part[g][n + 65] = acc1[1];
-            part[g + 8][n + 64] = acc1[2];
-            part[g + 8][n + 65] = acc1[3];
-        }
     }
-    if (a.xscale && warp == 0) {
+    const int n = 2 * t;
+    part[warp][g][n] = acc0[0];
+    part[warp][g][n + 1] = acc0[1];
+    part[warp][g + 8][n] = acc0[2];
+    part[warp][g + 8][n + 1] = acc0[3];
+    part[warp][g][n + 8] = acc1[0];
+    part[warp][g][n + 9] = acc1[1];
+    part[warp][g + 8][n + 8] = acc1[2];
+    part[warp][g + 8][n + 9] = acc1[3];
+    if (a.xscale) {
 #pragma unroll
         for (int o = 1; o < 4; o <<= 1) {
-            am0 = __uint_as_float(max(__float_as_uint(am0),
-                                      __shfl_xor_sync(kFull, __float_as_uint(am0), o)));
-            am1 = __uint_as_float(max(__float_as_uint(am1),
-                                      __shfl_xor_sync(kFull, __float_as_uint(am1), o)));
+            am0 = max(am0, __shfl_xor_sync(kFull, am0, o));
+            am1 = max(am1, __shfl_xor_sync(kFull, am1, o));
         }
         if (t == 0) {
-            amax_sm[g] = am0;
-            amax_sm[g + 8] = am1;
+            amax_sm[warp][g] = am0;
+            amax_sm[warp][g + 8] = am1;
         }
     }
+    zero_ctrl(a);
     cluster_sync();
     // tokens rank and rank + 8 of the cluster: a warp each
     const int tok = rank + 8 * warp;
     if (warp < 2 && t0 + tok < a.M) {
-        float v[4] = {0.f, 0.f, 0.f, 0.f};
-        float am = 0.f;
+        float v[4];
+        uint32_t am = 0;
 #pragma unroll
-        for (int r = 0; r < kRouteCtas; ++r) {
-            const uint32_t at = cluster_map(&part[tok][0], (uint32_t)r);
+        for (int i = 0; i < 4; ++i) {
+            v[i] = 0.f;
+            const int e = lane + 32 * i;
+            if (e >= a.N) continue;
+            const float* mine = &part[(e >> 4) * split][tok][e & 15];
+            for (int w = 0; w < split; ++w) {
+                float p[kRouteCtas];
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-                if (lane + 32 * i < a.N) v[i] += dsm_f32(at + 4u * (lane + 32 * i));
-            if (a.xscale) am = __uint_as_float(max(__float_as_uint(am),
-                                  __float_as_uint(dsm_f32(cluster_map(&amax_sm[tok], r)))));
+                for (int r = 0; r < kRouteCtas; ++r)
+                    p[r] = dsm_f32(cluster_map(mine + w * kRouteTokens * 16, (uint32_t)r));
+#pragma unroll
+                for (int r = 0; r < kRouteCtas; ++r) v[i] += p[r];
+            }
         }
         const size_t m = (size_t)(t0 + tok);
-        if (a.xscale && lane == 0) a.xscale[m] = split_scale(am);
+        if (a.xscale) {              // the warps of the first tile pair have seen all of x
+            if (lane < kRouteCtas * split)
+                am = dsm_u32(cluster_map(&amax_sm[lane % split][tok], (uint32_t)(lane / split)));
+            if (split == 8)          // 64 slices: two a lane
+                am = max(am, dsm_u32(cluster_map(&amax_sm[lane % split][tok],
+                                                 (uint32_t)(lane / split + 4))));
+            am = __reduce_max_sync(kFull, am);
+            if (lane == 0) a.xscale[m] = split_scale(__uint_as_float(am));
+        }
         route_token(v, a.N, a.K, false, a.renorm, lane, a.ids + m * a.K, a.gates + m * a.K,
                     a.ids_out ? a.ids_out + m * a.K : nullptr,
                     a.gates_out ? a.gates_out + m * a.K : nullptr);
@@ -255,12 +282,8 @@ __global__ void __launch_bounds__(kRouteThreads)
     if (a.xscale) {
         const uint16_t* x = a.x + m * a.ldx;
         uint32_t am = 0;
-        for (int i = 8 * lane; i < a.d; i += 256) {
-            const uint4 u = *reinterpret_cast<const uint4*>(x + i);
-            const uint32_t w[4] = {u.x, u.y, u.z, u.w};
-#pragma unroll
-            for (int j = 0; j < 4; ++j) am = max(am, max(w[j] << 16 & 0x7fffffffu, w[j] & 0x7fff0000u));
-        }
+        for (int i = 8 * lane; i < a.d; i += 256)
+            am = max(am, max_abs(*reinterpret_cast<const uint4*>(x + i)));
         am = __reduce_max_sync(kFull, am);
         if (lane == 0) a.xscale[m] = split_scale(__uint_as_float(am));
     }
