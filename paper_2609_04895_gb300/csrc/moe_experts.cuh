@@ -35,7 +35,6 @@
 namespace crc {
 
 constexpr int kMoeThreads = 512;     // warps 0 TMA, 1 MMA, 2-3 idle, 4-7 epilogue, 8-15 rows
-constexpr int kMoeWarps = kMoeThreads / 32;
 constexpr int kMoeMaxTiles = 256;    // row tiles of NT: N + M K / NT at most, M K <= 128 NT
 constexpr int kItemRing = 4;
 constexpr int kCtrlNext = 0, kCtrlDone2 = 1, kCtrlDone1 = 2;
@@ -50,8 +49,7 @@ struct MoeCfg {
     static constexpr int SB = NT == 16 ? 8 : NT == 32 ? 6 : W8 ? 3 : 5;
     static constexpr int LIST = 128 * NT;                      // choices (M K) at most
     static constexpr int TMEM_COLS = 2 * (COLS < 16 ? 16 : COLS) < 32 ? 32 : 2 * COLS;
-    static constexpr int TABLE_BYTES = 3 * 128 * 4 + kMoeWarps * 128 * 2 + 3 * kMoeMaxTiles * 2 +
-                                       LIST * 2 + 64;
+    static constexpr int TABLE_BYTES = 3 * 128 * 4 + 3 * kMoeMaxTiles * 2 + LIST * 2 + 64;
     static constexpr int BAR_BYTES = 512;
     static constexpr int SA =
         (232448 - 1024 - BAR_BYTES - TABLE_BYTES - SB * B_BYTES) / A_BYTES;
@@ -200,9 +198,8 @@ struct MoeShared {
     int* slot;             // [128] slot of each expert, -1 without
     int* start;            // [128] first row of each expert
     int* count;            // [128] rows of each expert, then [0] = row tiles
-    uint16_t* wcnt;        // [warps][128]
     uint16_t *tile_e, *tile_row, *tile_rows;   // [kMoeMaxTiles]
-    uint16_t* list;        // choices sorted by expert, then by index
+    uint16_t* list;        // choices sorted by expert, then by token
 
     __device__ __forceinline__ explicit MoeShared(uint8_t* base) {
         a = base;
@@ -224,15 +221,14 @@ struct MoeShared {
         slot = reinterpret_cast<int*>(p + Cfg::BAR_BYTES);
         start = slot + 128;
         count = start + 128;
-        wcnt = reinterpret_cast<uint16_t*>(count + 128);
-        tile_e = wcnt + kMoeWarps * 128;
+        tile_e = reinterpret_cast<uint16_t*>(count + 128);
         tile_row = tile_e + kMoeMaxTiles;
         tile_rows = tile_row + kMoeMaxTiles;
         list = tile_rows + kMoeMaxTiles;
     }
 };
 
-// Sorts the choices by expert (stable) and cuts each expert's rows into tiles of
+// Sorts the choices by expert, then by token, and cuts each expert's rows into tiles of
 // NT.  Every CTA builds the same tables.  All threads.
 //
 // One warp does it when the choices are one a lane (one token of up to 32 choices,
@@ -266,6 +262,7 @@ __device__ __forceinline__ void build_small_tables(const MoeArgs& a, const MoeSh
 
 template <bool W8, int NT>
 __device__ __forceinline__ void build_tables(const MoeArgs& a, const MoeShared<W8, NT>& s) {
+    using Cfg = MoeCfg<W8, NT>;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int E = a.M * a.K;
     if (E <= 32 && a.M <= NT) {
@@ -273,34 +270,29 @@ __device__ __forceinline__ void build_tables(const MoeArgs& a, const MoeShared<W
         __syncthreads();
         return;
     }
-    uint8_t* ids = s.a;              // scratch: the weight ring is not in use yet
+    // Scratch in the weight ring, which is not in use yet: the choices, and for
+    // every expert the set of its tokens as bits with the count of those before
+    // each word.  (An expert is chosen once a token at most.)
+    const int words = (a.M + 31) / 32;
+    uint32_t* set = reinterpret_cast<uint32_t*>(s.a);                  // [128][words]
+    uint16_t* before = reinterpret_cast<uint16_t*>(set + 128 * words); // [128][words]
+    uint8_t* ids = reinterpret_cast<uint8_t*>(before + 128 * words);   // [E]
+    static_assert(Cfg::LIST + 128 * 32 * 6 <= Cfg::SA * Cfg::A_BYTES, "scratch");
+    for (int i = threadIdx.x; i < 128 * words; i += kMoeThreads) set[i] = 0u;
+    __syncthreads();
     for (int i = threadIdx.x; i < E; i += kMoeThreads) {
-        const int e = (int)__ldcg(a.ids + i);
-        ids[i] = (uint8_t)(s.slot[e] < 0 ? 128 : e);
-    }
-    for (int i = threadIdx.x; i < kMoeWarps * 128; i += kMoeThreads) s.wcnt[i] = 0;
-    __syncthreads();
-    // a warp takes a contiguous piece of the choices, 32 at a time
-    const int groups = (E + 31) / 32;
-    const int g0 = groups * warp / kMoeWarps, g1 = groups * (warp + 1) / kMoeWarps;
-    uint16_t* mine = s.wcnt + warp * 128;
-    for (int g = g0; g < g1; ++g) {
-        const int i = 32 * g + lane;
-        const int e = i < E ? (int)ids[i] : 128;
-        const uint32_t peers = __match_any_sync(kFull, e);
-        if (e < 128 && lane == __ffs(peers) - 1) mine[e] += (uint16_t)__popc(peers);
-        __syncwarp();
+        const int e = (int)__ldcg(a.ids + i), tok = i / a.K;
+        const bool resident = s.slot[e] >= 0;
+        ids[i] = (uint8_t)(resident ? e : 255);
+        if (resident) atomicOr(&set[e * words + (tok >> 5)], 1u << (tok & 31));
     }
     __syncthreads();
-    if (warp < 4) {                  // rows of an expert before each warp's piece
+    if (threadIdx.x < 128) {
         const int e = threadIdx.x;
-        int c[kMoeWarps], n = 0;
-#pragma unroll
-        for (int w = 0; w < kMoeWarps; ++w) c[w] = s.wcnt[w * 128 + e];
-#pragma unroll
-        for (int w = 0; w < kMoeWarps; ++w) {
-            s.wcnt[w * 128 + e] = (uint16_t)n;
-            n += c[w];
+        int n = 0;
+        for (int w = 0; w < words; ++w) {
+            before[e * words + w] = (uint16_t)n;
+            n += __popc(set[e * words + w]);
         }
         s.count[e] = n;
     }
@@ -339,17 +331,11 @@ __device__ __forceinline__ void build_tables(const MoeArgs& a, const MoeShared<W
         }
     }
     __syncthreads();
-    for (int g = g0; g < g1; ++g) {
-        const int i = 32 * g + lane;
-        const int e = i < E ? (int)ids[i] : 128;
-        const uint32_t peers = __match_any_sync(kFull, e);
-        if (e < 128) {
-            const int before = __popc(peers & ((1u << lane) - 1u));
-            s.list[s.start[e] + mine[e] + before] = (uint16_t)i;
-        }
-        __syncwarp();
-        if (e < 128 && lane == __ffs(peers) - 1) mine[e] += (uint16_t)__popc(peers);
-        __syncwarp();
+    for (int i = threadIdx.x; i < E; i += kMoeThreads) {
+        const int e = ids[i], tok = i / a.K;
+        if (e == 255) continue;
+        const int at = e * words + (tok >> 5);
+        s.list[s.start[e] + before[at] + __popc(set[at] & ((1u << (tok & 31)) - 1u))] = (uint16_t)i;
     }
     // the ring's stages go from generic reads and writes to TMA
     fence_proxy_async_smem();
@@ -843,15 +829,24 @@ __global__ void __launch_bounds__(kMoeThreads, 1)
          i += (long long)gridDim.x * kMoeThreads) {
         const int tok = (int)(i / quads), c = (int)(i - (long long)tok * quads) * 4;
         float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-        for (int k = 0; k < a.K; ++k) {
-            const int r = tok * a.K + k;
-            if (s.slot[__ldcg(a.ids + r)] < 0) continue;
-            const float g = __ldcg(a.gates + r);
-            const float4 y = __ldcg(reinterpret_cast<const float4*>(a.y + (size_t)r * a.d + c));
-            o.x = fmaf(g, y.x, o.x);
-            o.y = fmaf(g, y.y, o.y);
-            o.z = fmaf(g, y.z, o.z);
-            o.w = fmaf(g, y.w, o.w);
+        for (int k0 = 0; k0 < a.K; k0 += 8) {      // all loads of eight choices at once
+            float g[8];
+            float4 y[8];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                const int r = tok * a.K + k0 + k;
+                const bool in = k0 + k < a.K && s.slot[__ldcg(a.ids + r)] >= 0;
+                g[k] = in ? __ldcg(a.gates + r) : 0.f;
+                y[k] = in ? __ldcg(reinterpret_cast<const float4*>(a.y + (size_t)r * a.d + c))
+                          : make_float4(0.f, 0.f, 0.f, 0.f);
+            }
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                o.x = fmaf(g[k], y[k].x, o.x);
+                o.y = fmaf(g[k], y[k].y, o.y);
+                o.z = fmaf(g[k], y[k].z, o.z);
+                o.w = fmaf(g[k], y[k].w, o.w);
+            }
         }
         const __nv_bfloat162 p = __floats2bfloat162_rn(o.x, o.y), q = __floats2bfloat162_rn(o.z, o.w);
         uint2 w;

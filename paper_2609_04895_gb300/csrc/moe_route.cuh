@@ -5,8 +5,8 @@
 //   g_e = exp(z_e - max z) / sum exp(z - max z), divided by its sum over S on request
 //
 // A cluster of eight CTAs takes 16 tokens: each CTA multiplies one eighth of d
-// for all experts and the CTAs' partial logits are summed, in rank order,
-// through distributed shared memory; then a warp takes a token.  Splitting d
+// for all experts and puts its partial logits into the shared memory of the CTA
+// that owns the token (rank = token mod 8), where a warp sums them in rank order.  Splitting d
 // reads every element of x and W^R once per cluster (one token of N = 128,
 // d = 2048: 64 KB of W^R a CTA, against 512 KB on one), and the sum of eight short
 // chains is nearer to the exact logit than one long one.
@@ -69,7 +69,7 @@ __device__ __forceinline__ void route_token(const float (&v)[4], int N, int K, b
     uint32_t key[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) key[i] = lane + 32 * i < N ? score_key(v[i]) : 0u;
-    float mx = 0.f, total = 1.f, chosen = 0.f, mine = 0.f;
+    uint32_t mine = 0u, top = 0u;     // lane k: the k-th choice
     int my_id = 0;
     for (int k = 0; k < K; ++k) {
         const uint32_t best = __reduce_max_sync(
@@ -79,31 +79,31 @@ __device__ __forceinline__ void route_token(const float (&v)[4], int N, int K, b
         for (int i = 3; i >= 0; --i)
             if (key[i] == best) at = (uint32_t)(lane + 32 * i);
         const uint32_t e = __reduce_min_sync(kFull, at);    // ties to the lowest index
-        if (k == 0 && !probs) {
-            mx = score_of(best);
-            float s = 0.f;
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-                if (lane + 32 * i < N) s += expf(v[i] - mx);
-            total = warp_sum(s);
-        }
+        if (k == 0) top = best;
 #pragma unroll
         for (int i = 0; i < 4; ++i)
             if ((uint32_t)(lane + 32 * i) == e) key[i] = 0u;
-        const float z = score_of(best);
-        const float p = probs ? z : expf(z - mx) / total;
-        chosen += p;
         if (lane == k) {
-            mine = p;
+            mine = best;
             my_id = (int)e;
         }
     }
+    float p = lane < K ? score_of(mine) : 0.f;
+    if (!probs) {
+        const float mx = score_of(top);
+        float s = 0.f;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (lane + 32 * i < N) s += expf(v[i] - mx);
+        s = warp_sum(s);
+        p = lane < K ? expf(p - mx) / s : 0.f;
+    }
+    if (renorm) p /= warp_sum(p);
     if (lane < K) {
-        if (renorm) mine /= chosen;
         ids[lane] = (uint8_t)my_id;
-        gates[lane] = mine;
+        gates[lane] = p;
         if (ids_out) ids_out[lane] = (uint8_t)my_id;
-        if (gates_out) gates_out[lane] = mine;
+        if (gates_out) gates_out[lane] = p;
     }
 }
 
@@ -126,15 +126,12 @@ __device__ __forceinline__ uint32_t max_abs(const uint4& v) {
     return m;
 }
 
-__device__ __forceinline__ uint32_t dsm_u32(uint32_t addr) {
-    uint32_t v;
-    asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(addr));
-    return v;
+__device__ __forceinline__ void dsm_store2(uint32_t addr, float x, float y) {
+    asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(addr), "f"(x), "f"(y)
+                 : "memory");
 }
-__device__ __forceinline__ float dsm_f32(uint32_t addr) {
-    float v;
-    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(addr));
-    return v;
+__device__ __forceinline__ void dsm_store(uint32_t addr, uint32_t v) {
+    asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(addr), "r"(v) : "memory");
 }
 
 __device__ __forceinline__ void zero_ctrl(const MoeRouteArgs& a) {
@@ -157,8 +154,10 @@ __device__ __forceinline__ float split_scale(float amax) {
 __global__ void __launch_bounds__(kRouteThreads)
     moe_route_kernel(MoeRouteArgs a) {
     constexpr int WARPS = kRouteThreads / 32, BATCH = 8;
-    __shared__ float part[WARPS][kRouteTokens][16];
-    __shared__ uint32_t amax_sm[WARPS][kRouteTokens];
+    // partial logits of this CTA's two tokens: [token / 8][rank][warp][16 experts]
+    __shared__ float part[2][kRouteCtas][WARPS * 16];
+    __shared__ uint32_t amax[2][kRouteCtas][WARPS];
+    asm volatile("barrier.cluster.arrive.relaxed;" ::: "memory");
     pdl_launch_dependents();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int rank = (int)cluster_ctarank();
@@ -208,63 +207,53 @@ __global__ void __launch_bounds__(kRouteThreads)
             }
         }
     }
-    const int n = 2 * t;
-    part[warp][g][n] = acc0[0];
-    part[warp][g][n + 1] = acc0[1];
-    part[warp][g + 8][n] = acc0[2];
-    part[warp][g + 8][n + 1] = acc0[3];
-    part[warp][g][n + 8] = acc1[0];
-    part[warp][g][n + 9] = acc1[1];
-    part[warp][g + 8][n + 8] = acc1[2];
-    part[warp][g + 8][n + 9] = acc1[3];
     if (a.xscale) {
 #pragma unroll
         for (int o = 1; o < 4; o <<= 1) {
             am0 = max(am0, __shfl_xor_sync(kFull, am0, o));
             am1 = max(am1, __shfl_xor_sync(kFull, am1, o));
         }
-        if (t == 0) {
-            amax_sm[warp][g] = am0;
-            amax_sm[warp][g + 8] = am1;
-        }
     }
     zero_ctrl(a);
-    cluster_sync();
-    // tokens rank and rank + 8 of the cluster: a warp each
-    const int tok = rank + 8 * warp;
-    if (warp < 2 && t0 + tok < a.M) {
-        float v[4];
-        uint32_t am = 0;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            v[i] = 0.f;
-            const int e = lane + 32 * i;
-            if (e >= a.N) continue;
-            const float* mine = &part[(e >> 4) * split][tok][e & 15];
-            for (int w = 0; w < split; ++w) {
-                float p[kRouteCtas];
-#pragma unroll
-                for (int r = 0; r < kRouteCtas; ++r)
-                    p[r] = dsm_f32(cluster_map(mine + w * kRouteTokens * 16, (uint32_t)r));
-#pragma unroll
-                for (int r = 0; r < kRouteCtas; ++r) v[i] += p[r];
-            }
+    asm volatile("barrier.cluster.wait;" ::: "memory");     // every CTA has begun
+    {
+        // rows g and g + 8 are tokens of CTA g
+        const uint32_t at = cluster_map(&part[0][rank][warp * 16 + 2 * t], (uint32_t)g);
+        const uint32_t next = (uint32_t)sizeof part[0];
+        if (t0 + g < a.M) {
+            dsm_store2(at, acc0[0], acc0[1]);
+            dsm_store2(at + 32, acc1[0], acc1[1]);
+            if (a.xscale && t == 0) dsm_store(cluster_map(&amax[0][rank][warp], (uint32_t)g), am0);
         }
-        const size_t m = (size_t)(t0 + tok);
-        if (a.xscale) {              // the warps of the first tile pair have seen all of x
-            if (lane < kRouteCtas * split)
-                am = dsm_u32(cluster_map(&amax_sm[lane % split][tok], (uint32_t)(lane / split)));
-            if (split == 8)          // 64 slices: two a lane
-                am = max(am, dsm_u32(cluster_map(&amax_sm[lane % split][tok],
-                                                 (uint32_t)(lane / split + 4))));
-            am = __reduce_max_sync(kFull, am);
-            if (lane == 0) a.xscale[m] = split_scale(__uint_as_float(am));
+        if (t0 + g + 8 < a.M) {
+            dsm_store2(at + next, acc0[2], acc0[3]);
+            dsm_store2(at + next + 32, acc1[2], acc1[3]);
+            if (a.xscale && t == 0) dsm_store(cluster_map(&amax[1][rank][warp], (uint32_t)g), am1);
         }
-        route_token(v, a.N, a.K, false, a.renorm, lane, a.ids + m * a.K, a.gates + m * a.K,
-                    a.ids_out ? a.ids_out + m * a.K : nullptr,
-                    a.gates_out ? a.gates_out + m * a.K : nullptr);
     }
-    cluster_sync();                  // no CTA leaves while its partial logits are read
+    cluster_sync();                  // nothing is written to this CTA after it
+    const int tok = rank + 8 * warp;
+    if (warp >= 2 || t0 + tok >= a.M) return;
+    float v[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        v[i] = 0.f;
+        const int e = lane + 32 * i;
+        if (e >= a.N) continue;
+        for (int w = 0; w < split; ++w)
+#pragma unroll
+            for (int r = 0; r < kRouteCtas; ++r)
+                v[i] += part[warp][r][((e >> 4) * split + w) * 16 + (e & 15)];
+    }
+    const size_t m = (size_t)(t0 + tok);
+    if (a.xscale) {                  // the warps without a tile pair have left zeros
+        const uint32_t* am = &amax[warp][0][0];
+        const uint32_t top = __reduce_max_sync(kFull, max(am[lane], am[lane + 32]));
+        if (lane == 0) a.xscale[m] = split_scale(__uint_as_float(top));
+    }
+    route_token(v, a.N, a.K, false, a.renorm, lane, a.ids + m * a.K, a.gates + m * a.K,
+                a.ids_out ? a.ids_out + m * a.K : nullptr,
+                a.gates_out ? a.gates_out + m * a.K : nullptr);
 }
 
 // The same from given probabilities: a warp a token.
