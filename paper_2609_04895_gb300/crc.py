@@ -619,14 +619,16 @@ def _stream_type(t) -> int:
 
 
 def _check(t, name: str, shape, dtype, dense: bool = True):
-    """A tensor argument of the stated shape and type on the GPU, or None."""
+    """The address of a tensor argument of the stated shape and type on the GPU, or
+    None.  (Short on purpose: a one-row norm has six of them, and takes the GPU 2 us.)"""
     if t is None:
-        return
-    if t.shape != shape or t.dtype != dtype or not t.is_cuda:
+        return None
+    if t.dtype is not dtype or t.shape != shape or not t.is_cuda:
         raise ValueError(f"{name}: a {dtype} CUDA tensor of shape {tuple(shape)} is wanted, "
                          f"got {t.dtype} {tuple(t.shape)} on {t.device}")
     if dense and not t.is_contiguous():
         raise ValueError(f"{name} must be contiguous")
+    return t.data_ptr()
 
 
 def _rows(t, name: str):
@@ -647,19 +649,19 @@ def rms_norm(x, weight, eps: float = 1e-6, residual=None, residual_out=None, out
     given), to out8 / scale8 (float8_e4m3fn and fp32 [M]) if given, x + residual to
     residual_out and the rows' statistic to rstd (fp32 [M]).  Returns out."""
     import torch
+    bf16, f32, dtype = torch.bfloat16, torch.float32, x.dtype
     M, d, ldx = _rows(x, "x")
-    kind = _stream_type(x)
-    _check(weight, "weight", (d,), torch.bfloat16)
-    _check(residual, "residual", (M, d), x.dtype)
-    _check(residual_out, "residual_out", (M, d), x.dtype)
     if out is None and out8 is None:
-        out = torch.empty((M, d), dtype=torch.bfloat16, device=x.device)
-    _check(out, "out", (M, d), torch.bfloat16)
-    _check(out8, "out8", (M, d), torch.float8_e4m3fn)
-    _check(scale8, "scale8", (M,), torch.float32)
-    _check(rstd, "rstd", (M,), torch.float32)
-    crc_rms_norm(x.data_ptr(), ldx, _ptr(residual), weight.data_ptr(), kind, M, d, eps,
-                 _ptr(residual_out), _ptr(out), _ptr(out8), _ptr(scale8), _ptr(rstd), stream)
+        out = torch.empty((M, d), dtype=bf16, device=x.device)
+    rows = x.shape
+    rc = load().crc_rms_norm(
+        x.data_ptr(), ldx, _check(residual, "residual", rows, dtype),
+        _check(weight, "weight", (d,), bf16), _stream_type(x), M, d, eps,
+        _check(residual_out, "residual_out", rows, dtype), _check(out, "out", rows, bf16),
+        _check(out8, "out8", rows, torch.float8_e4m3fn), _check(scale8, "scale8", (M,), f32),
+        _check(rstd, "rstd", (M,), f32), _stream(stream))
+    if rc:
+        raise CrcError(rc, "crc_rms_norm")
     return out
 
 
@@ -668,25 +670,20 @@ def rms_norm_grad(dy, s, weight, rstd, dres=None, dx=None, dw=None, want_dw: boo
     """crc_rms_norm_grad: (dx, dw) from dy (bf16), s = x + residual and rstd of the
     forward call, and dres, the gradient that arrives at s directly."""
     import torch
-    M, d = dy.shape
-    kind = _stream_type(s)
-    _check(dy, "dy", (M, d), torch.bfloat16)
-    _check(s, "s", (M, d), s.dtype)
-    _check(weight, "weight", (d,), torch.bfloat16)
-    _check(rstd, "rstd", (M,), torch.float32)
-    _check(dres, "dres", (M, d), s.dtype)
+    M, d = rows = dy.shape
+    bf16, f32 = torch.bfloat16, torch.float32
     if dx is None:
         dx = torch.empty_like(s)
-    _check(dx, "dx", (M, d), s.dtype)
     if want_dw and dw is None:
-        dw = torch.empty(d, dtype=torch.float32, device=dy.device)
-    _check(dw, "dw", (d,), torch.float32)
+        dw = torch.empty(d, dtype=f32, device=dy.device)
     if dw is not None and workspace is None:
         workspace = torch.empty(crc_rms_norm_grad_workspace_bytes(M, d), dtype=torch.uint8,
                                 device=dy.device)
-    crc_rms_norm_grad(dy.data_ptr(), s.data_ptr(), weight.data_ptr(), rstd.data_ptr(), _ptr(dres),
-                      kind, M, d, dx.data_ptr(), _ptr(dw), _ptr(workspace),
-                      0 if workspace is None else workspace.nbytes, stream)
+    crc_rms_norm_grad(_check(dy, "dy", rows, bf16), _check(s, "s", rows, s.dtype),
+                      _check(weight, "weight", (d,), bf16), _check(rstd, "rstd", (M,), f32),
+                      _check(dres, "dres", rows, s.dtype), _stream_type(s), M, d,
+                      _check(dx, "dx", rows, s.dtype), _check(dw, "dw", (d,), f32),
+                      _ptr(workspace), 0 if workspace is None else workspace.nbytes, stream)
     return dx, dw
 
 
@@ -706,9 +703,9 @@ def quantize_rows(x, out8=None, scale=None, stream=None):
         out8 = torch.empty((*lead, d), dtype=torch.float8_e4m3fn, device=x.device)
     if scale is None:
         scale = torch.empty(lead, dtype=torch.float32, device=x.device)
-    _check(out8, "out8", (*lead, d), torch.float8_e4m3fn)
-    _check(scale, "scale", lead, torch.float32)
-    crc_quantize_rows(x.data_ptr(), ldx, M, d, out8.data_ptr(), scale.data_ptr(), stream)
+    crc_quantize_rows(x.data_ptr(), ldx, M, d,
+                      _check(out8, "out8", (*lead, d), torch.float8_e4m3fn),
+                      _check(scale, "scale", lead, torch.float32), stream)
     return out8, scale
 
 
@@ -772,6 +769,7 @@ class MoeLayer:
                          else gate_up_scale.stride(0) * 4,
                          down_scale_stride=0 if down_scale is None else down_scale.stride(0) * 4,
                          router_dev=_ptr(router), expert_slot_dev=_ptr(expert_slot))
+        self._ref = ctypes.byref(self.c)
         if self.workspace_bytes(1) == 0:
             raise CrcError(CRC_EUNSUPPORTED, "crc_moe_workspace_bytes")
 
@@ -785,28 +783,28 @@ class MoeLayer:
         may be strided) in place of the router; topk (uint8) and gates (fp32)
         [M][K] are written if given.  x may be None when x8 and scores are given."""
         import torch
-        d = self.d
         src = x if x is not None else x8
         if src is None:
             raise ValueError("x or x8 is wanted")
         M, _, ldx = _rows(src, "x")
-        _check(x, "x", (M, d), torch.bfloat16, dense=False)
-        _check(x8, "x8", (M, d), torch.float8_e4m3fn)
-        _check(x_scale, "x_scale", (M,), torch.float32)
+        rows, f32 = (M, self.d), torch.float32
         lds = 0
         if scores is not None:
-            _check(scores, "scores", (M, self.N), torch.float32, dense=False)
             lds = max(_rows(scores, "scores")[2], self.N)
         if out is None:
-            out = torch.empty((M, d), dtype=torch.bfloat16, device=src.device)
-        _check(out, "out", (M, d), torch.bfloat16)
-        _check(topk, "topk", (M, self.K), torch.uint8)
-        _check(gates, "gates", (M, self.K), torch.float32)
+            out = torch.empty(rows, dtype=torch.bfloat16, device=src.device)
         if workspace is None:
             workspace = torch.empty(self.workspace_bytes(M), dtype=torch.uint8, device=src.device)
-        crc_moe_layer(self.c, _ptr(x), ldx, _ptr(x8), _ptr(x_scale), _ptr(scores), lds, M,
-                      out.data_ptr(), _ptr(topk), _ptr(gates), workspace.data_ptr(),
-                      workspace.nbytes, stream)
+        rc = load().crc_moe_layer(
+            self._ref, _check(x, "x", rows, torch.bfloat16, False), ldx,
+            _check(x8, "x8", rows, torch.float8_e4m3fn), _check(x_scale, "x_scale", (M,), f32),
+            _check(scores, "scores", (M, self.N), f32, False), lds, M,
+            _check(out, "out", rows, torch.bfloat16),
+            _check(topk, "topk", (M, self.K), torch.uint8),
+            _check(gates, "gates", (M, self.K), f32), workspace.data_ptr(), workspace.nbytes,
+            _stream(stream))
+        if rc:
+            raise CrcError(rc, "crc_moe_layer")
         return out
 
 

@@ -7,13 +7,14 @@
 //   dw = sum over rows of dy xhat
 //
 // All three are bound by memory: a row is read once into registers, its sums
-// and maxima are taken across one CTA, and what leaves is written from the
+// and maxima are taken across the warps that share it, and what leaves is written from the
 // same registers.  Sums, statistics and dw are fp32; h, s and dx are rounded
 // once, to the types of their arrays.
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include "crc_device.cuh"
 #include "crc_internal.h"
 
 namespace crc {
@@ -25,6 +26,26 @@ constexpr int kMaxRow = 32768;       // 1024 threads x 4 groups of 8 elements
 __device__ __forceinline__ float max_nan(float a, float b) {   // a NaN stays
     float r;
     asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+    return r;
+}
+
+// Two fp32 operations an instruction, each rounded like its scalar form.
+__device__ __forceinline__ uint64_t pack2(float a, float b) {
+    uint64_t r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+    return r;
+}
+__device__ __forceinline__ void unpack2(uint64_t v, float& a, float& b) {
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v));
+}
+__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
+    uint64_t r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+    uint64_t r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
     return r;
 }
 
@@ -84,22 +105,28 @@ __device__ __forceinline__ uint2 to_e4m3(const float (&f)[8]) {
     return make_uint2(h[0] | ((uint32_t)h[1] << 16), h[2] | ((uint32_t)h[3] << 16));
 }
 
-// Sum (or NaN-keeping maximum) of v over the CTA, in one fixed order; every
-// thread gets it.  `buf`: 32 floats, not in use by an earlier reduction that a
-// thread may still be reading.
+// The warps that share a row: `warps` of them, `id` the row's number in the CTA.
+struct RowTeam {
+    int warps, id, thread, threads;
+    __device__ __forceinline__ explicit RowTeam(int w)
+        : warps(w), id((threadIdx.x >> 5) / w), thread(threadIdx.x - id * 32 * w), threads(32 * w) {}
+};
+
+// Sum (or NaN-keeping maximum) of v over a row's warps, in one fixed order; every
+// thread gets it.  `buf`: a float a warp of the CTA, not in use by an earlier
+// reduction that a thread may still be reading.
 template <bool MAX>
-__device__ __forceinline__ float cta_reduce(float v, float* buf) {
+__device__ __forceinline__ float row_reduce(float v, float* buf, const RowTeam& t) {
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) {
         const float u = __shfl_xor_sync(0xffffffffu, v, o);
         v = MAX ? max_nan(v, u) : v + u;
     }
-    const int warps = blockDim.x >> 5;
-    if (warps == 1) return v;
+    if (t.warps == 1) return v;
     const int lane = threadIdx.x & 31;
     if (lane == 0) buf[threadIdx.x >> 5] = v;
-    __syncthreads();
-    v = lane < warps ? buf[lane] : 0.f;
+    asm volatile("bar.sync %0, %1;" ::"r"(1 + t.id), "r"(t.threads) : "memory");
+    v = lane < t.warps ? buf[t.id * t.warps + lane] : 0.f;
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) {
         const float u = __shfl_xor_sync(0xffffffffu, v, o);
@@ -116,13 +143,29 @@ __device__ __forceinline__ float row_scale(float amax) {
 __device__ __forceinline__ uint2 quantize8(float (&y)[8], float scale) {
     if (scale >= 1e-30f) {
         const float inv = 1.f / scale;
+        const uint64_t k = pack2(inv, inv);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) y[i] *= inv;
+        for (int i = 0; i < 8; i += 2)
+            asm("{\n\t.reg .b64 p;\n\tmov.b64 p, {%0, %1};\n\tmul.rn.f32x2 p, p, %2;\n\t"
+                "mov.b64 {%0, %1}, p;\n\t}"
+                : "+f"(y[i]), "+f"(y[i + 1])
+                : "l"(k));
     } else {                        // 1 / scale may overflow (or scale is a NaN)
 #pragma unroll
         for (int i = 0; i < 8; ++i) y[i] /= scale;
     }
     return to_e4m3(y);
+}
+
+// Largest magnitude of eight bf16 with m's, two at a time; a NaN stays.
+__device__ __forceinline__ __nv_bfloat162 max_abs8(__nv_bfloat162 m, const uint4& v) {
+    const uint32_t u[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const uint32_t a = u[i] & 0x7fff7fffu;
+        m = __hmax2_nan(m, *reinterpret_cast<const __nv_bfloat162*>(&a));
+    }
+    return m;
 }
 
 struct NormArgs {
@@ -134,15 +177,18 @@ struct NormArgs {
     float *scale, *rstd;
     long long ldx;                  // elements between rows of x (the other arrays are dense)
     int M, d;
+    int warps;                      // of a row
     float eps;
 };
 
-// One CTA a row; a thread holds VPT groups of eight elements, group g of
-// thread i at 8 (i + g blockDim).
-template <typename T, int VPT>
-__global__ void __launch_bounds__(1024) rms_norm_kernel(NormArgs a) {
+// A few warps a row, one CTA for one or more rows; a thread holds VPT groups of
+// eight elements, group g of thread i at 8 (i + g threads).
+template <typename T, int VPT, int THREADS>
+__global__ void __launch_bounds__(THREADS) rms_norm_kernel(NormArgs a) {
     __shared__ float red[2][32];
-    const long long row = blockIdx.x;
+    const RowTeam team(a.warps);
+    const long long row = (long long)blockIdx.x * (blockDim.x / team.threads) + team.id;
+    if (row >= a.M) return;
     const int d = a.d, nvec = d >> 3;
     const T* x = static_cast<const T*>(a.x) + row * a.ldx;
     const T* res = static_cast<const T*>(a.res) + (a.res ? row * d : 0);
@@ -150,7 +196,7 @@ __global__ void __launch_bounds__(1024) rms_norm_kernel(NormArgs a) {
     Vec8<T> lx[VPT], lr[VPT];
 #pragma unroll
     for (int g = 0; g < VPT; ++g) {
-        const int i = threadIdx.x + g * blockDim.x;
+        const int i = team.thread + g * team.threads;
         if (i < nvec) {
             lx[g].load(x + 8 * i);
             if (a.res) lr[g].load(res + 8 * i);
@@ -159,7 +205,7 @@ __global__ void __launch_bounds__(1024) rms_norm_kernel(NormArgs a) {
     float ss = 0.f;
 #pragma unroll
     for (int g = 0; g < VPT; ++g) {
-        const int i = threadIdx.x + g * blockDim.x;
+        const int i = team.thread + g * team.threads;
         if (i >= nvec) continue;
         lx[g].get(v[g]);
         if (a.res) {
@@ -172,13 +218,13 @@ __global__ void __launch_bounds__(1024) rms_norm_kernel(NormArgs a) {
         for (int j = 0; j < 8; ++j) ss = fmaf(v[g][j], v[g][j], ss);
         if (a.res_out) store8(static_cast<T*>(a.res_out) + row * d + 8 * i, v[g]);
     }
-    ss = cta_reduce<false>(ss, red[0]);
+    ss = row_reduce<false>(ss, red[0], team);
     const float rstd = __frsqrt_rn(ss / (float)d + a.eps);
-    if (a.rstd && threadIdx.x == 0) a.rstd[row] = rstd;
+    if (a.rstd && team.thread == 0) a.rstd[row] = rstd;
     float amax = 0.f;
 #pragma unroll
     for (int g = 0; g < VPT; ++g) {
-        const int i = threadIdx.x + g * blockDim.x;
+        const int i = team.thread + g * team.threads;
         if (i >= nvec) continue;
         Vec8<__nv_bfloat16> lw;
         float w[8];
@@ -192,45 +238,72 @@ __global__ void __launch_bounds__(1024) rms_norm_kernel(NormArgs a) {
         if (a.h) store8(a.h + row * d + 8 * i, v[g]);
     }
     if (!a.q) return;
-    const float scale = row_scale(cta_reduce<true>(amax, red[1]));
-    if (threadIdx.x == 0) a.scale[row] = scale;
+    const float scale = row_scale(row_reduce<true>(amax, red[1], team));
+    if (team.thread == 0) a.scale[row] = scale;
 #pragma unroll
     for (int g = 0; g < VPT; ++g) {
-        const int i = threadIdx.x + g * blockDim.x;
+        const int i = team.thread + g * team.threads;
         if (i < nvec) *reinterpret_cast<uint2*>(a.q + row * d + 8 * i) = quantize8(v[g], scale);
     }
 }
 
-// q and scale of bf16 rows, one CTA a row.
-template <int VPT>
-__global__ void __launch_bounds__(1024) quantize_rows_kernel(const __nv_bfloat16* x, long long ldx,
-                                                             int d, uint8_t* q, float* scale) {
-    __shared__ float red[32];
-    const long long row = blockIdx.x;
-    const int nvec = d >> 3;
-    Vec8<__nv_bfloat16> l[VPT];
+// q and scale of bf16 rows, the same division of a row.  CTAs stay and take row after
+// row, the next on its way while a row is reduced: there is so little to do for a
+// row that a CTA for every two of 2880 elements took 324 us where this takes 235
+// (184320 rows, 6.8 TB/s).
+template <int VPT, int THREADS>
+__global__ void __launch_bounds__(THREADS)
+    quantize_rows_kernel(const __nv_bfloat16* x, long long ldx, int M, int d, int warps, uint8_t* q,
+                         float* scale) {
+    __shared__ float red[2][32];
+    const RowTeam team(warps);
+    const int rows = blockDim.x / team.threads, nvec = d >> 3;
+    const long long step = (long long)gridDim.x * rows;
+    long long row = (long long)blockIdx.x * rows + team.id;
+    Vec8<__nv_bfloat16> cur[VPT], nxt[VPT];
+    auto load = [&](Vec8<__nv_bfloat16>(&l)[VPT], long long r) {
+        if (r >= M) return;
 #pragma unroll
-    for (int g = 0; g < VPT; ++g) {
-        const int i = threadIdx.x + g * blockDim.x;
-        if (i < nvec) l[g].load(x + row * ldx + 8 * i);
+        for (int g = 0; g < VPT; ++g) {
+            const int i = team.thread + g * team.threads;
+            if (i < nvec) l[g].load(x + r * ldx + 8 * i);
+        }
+    };
+    load(cur, row);
+    for (int flip = 0; row < M; row += step, flip ^= 1) {
+        load(nxt, row + step);
+        __nv_bfloat162 m = __floats2bfloat162_rn(0.f, 0.f);
+#pragma unroll
+        for (int g = 0; g < VPT; ++g)
+            if (team.thread + g * team.threads < nvec) m = max_abs8(m, cur[g].v);
+        const float amax = max_nan(__low2float(m), __high2float(m));
+        const float s = row_scale(row_reduce<true>(amax, red[flip], team));
+        if (team.thread == 0) scale[row] = s;
+#pragma unroll
+        for (int g = 0; g < VPT; ++g) {
+            const int i = team.thread + g * team.threads;
+            if (i < nvec) {
+                float v[8];
+                cur[g].get(v);
+                *reinterpret_cast<uint2*>(q + row * d + 8 * i) = quantize8(v, s);
+            }
+            cur[g] = nxt[g];
+        }
     }
-    float amax = 0.f, v[8];
-#pragma unroll
-    for (int g = 0; g < VPT; ++g) {
-        if ((int)(threadIdx.x + g * blockDim.x) >= nvec) continue;
-        l[g].get(v);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) amax = max_nan(amax, fabsf(v[j]));
-    }
-    const float s = row_scale(cta_reduce<true>(amax, red));
-    if (threadIdx.x == 0) scale[row] = s;
-#pragma unroll
-    for (int g = 0; g < VPT; ++g) {
-        const int i = threadIdx.x + g * blockDim.x;
-        if (i >= nvec) continue;
-        l[g].get(v);
-        *reinterpret_cast<uint2*>(q + row * d + 8 * i) = quantize8(v, s);
-    }
+}
+
+constexpr int kMaxGradStages = 8;
+constexpr int kGradRing = 216 * 1024;          // at most, of an SM
+
+// `bytes` contiguous bytes (a multiple of 16, both ends 16-byte aligned) to shared
+// memory, completing on bar.
+__device__ __forceinline__ void bulk_load(void* dst, const void* src, uint32_t bytes,
+                                          uint64_t* bar) {
+    asm volatile(
+        "cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(
+            smem_u32(dst)),
+        "l"(reinterpret_cast<uint64_t>(src)), "r"(bytes), "r"(smem_u32(bar))
+        : "memory");
 }
 
 struct NormGradArgs {
@@ -239,33 +312,93 @@ struct NormGradArgs {
     const float* rstd;
     void* dx;
     float* part;                    // [gridDim.x][d] partial dw
+    uint32_t* err;
     int M, d;
+    int stages, stage_bytes;        // of the ring
 };
 
-// A CTA takes rows blockIdx.x, + gridDim.x, ...; a thread keeps the dw sums of
-// its columns in registers and writes them once, so that no order of CTAs
-// changes a sum.
-template <typename T, int VPT>
-__global__ void __launch_bounds__(1024) rms_norm_grad_kernel(NormGradArgs a) {
+// A CTA takes rows blockIdx.x, + gridDim.x, ...  A thread keeps the dw sums of its
+// columns in registers and writes them once, so that no order of CTAs changes a
+// sum.
+//
+// The rows come through a ring in shared memory, whole rows by asynchronous bulk
+// copies: the bytes on the way then cost no registers.  (With the next row in registers
+// two CTAs of 256 threads fit an SM: 8000 x 2048 bf16 took 29 us without dw.)  A stage
+// is filled again one row after its own: by then every thread has used all that it
+// read of it.  RING false: rows too wide for two stages, read straight to registers.
+template <typename T, int VPT, int THREADS, bool RING>
+__global__ void __launch_bounds__(THREADS, VPT == 1 ? 2 : 1) rms_norm_grad_kernel(NormGradArgs a) {
+    extern __shared__ __align__(128) uint8_t ring[];
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     __shared__ float red[2][32];
+    __shared__ __align__(8) uint64_t full[kMaxGradStages];
+    const RowTeam team(blockDim.x >> 5);
     const int d = a.d, nvec = d >> 3;
-    float dw[VPT][8] = {};
-    int flip = 0;
+    const uint32_t dy_bytes = 2u * d, s_bytes = (uint32_t)sizeof(T) * d;
+    const uint32_t row_bytes = dy_bytes + s_bytes + (a.dres ? s_bytes : 0u);
+    auto fill = [&](int stage, long long row) {            // one thread
+        uint8_t* at = ring + (size_t)stage * a.stage_bytes;
+        mbar_arrive_expect_tx(&full[stage], row_bytes);
+        bulk_load(at, a.dy + row * d, dy_bytes, &full[stage]);
+        bulk_load(at + dy_bytes, static_cast<const T*>(a.s) + row * d, s_bytes, &full[stage]);
+        if (a.dres)
+            bulk_load(at + dy_bytes + s_bytes, static_cast<const T*>(a.dres) + row * d, s_bytes,
+                      &full[stage]);
+    };
+    if constexpr (RING) {
+        if (threadIdx.x == 0) {
+            for (int i = 0; i < a.stages; ++i) mbar_init(&full[i], 1);
+            fence_mbar_init();
+            long long row = blockIdx.x;
+            for (int i = 0; i < a.stages && row < a.M; ++i, row += gridDim.x) fill(i, row);
+        }
+    }
+    uint64_t dw[VPT][4] = {};          // pairs of neighbouring columns
+    Vec8<__nv_bfloat16> lw[VPT];
+#pragma unroll
+    for (int g = 0; g < VPT; ++g) {
+        const int i = threadIdx.x + g * blockDim.x;
+        if (i < nvec) lw[g].load(a.w + 8 * i);
+    }
+    if constexpr (RING) __syncthreads();
+    const float inv_d = 1.f / (float)d;
+    int flip = 0, stage = 0;
+    uint32_t phase = 0;
+    bool failed = false;
     for (long long row = blockIdx.x; row < a.M; row += gridDim.x, flip ^= 1) {
-        Vec8<__nv_bfloat16> ldy[VPT], lw[VPT];
+        const float rstd = a.rstd[row];
+        const __nv_bfloat16* dyp = a.dy + row * d;
+        const T* sp = static_cast<const T*>(a.s) + row * d;
+        const T* rp = static_cast<const T*>(a.dres) + (a.dres ? row * d : 0);
+        if constexpr (RING) {
+            if (!mbar_wait(&full[stage], phase)) {         // every thread waits, so all leave,
+                failed = true;                             // none with a copy on its way
+                for (int i = 1; i < a.stages && row + (long long)i * gridDim.x < a.M; ++i) {
+                    if (++stage == a.stages) {
+                        stage = 0;
+                        phase ^= 1;
+                    }
+                    (void)mbar_wait(&full[stage], phase);
+                }
+                break;
+            }
+            const uint8_t* at = ring + (size_t)stage * a.stage_bytes;
+            dyp = reinterpret_cast<const __nv_bfloat16*>(at);
+            sp = reinterpret_cast<const T*>(at + dy_bytes);
+            rp = reinterpret_cast<const T*>(at + dy_bytes + s_bytes);
+        }
+        Vec8<__nv_bfloat16> ldy[VPT];
         Vec8<T> ls[VPT], lr[VPT];
 #pragma unroll
         for (int g = 0; g < VPT; ++g) {
             const int i = threadIdx.x + g * blockDim.x;
-            if (i < nvec) {
-                ldy[g].load(a.dy + row * d + 8 * i);
-                ls[g].load(static_cast<const T*>(a.s) + row * d + 8 * i);
-                if (a.dres) lr[g].load(static_cast<const T*>(a.dres) + row * d + 8 * i);
-                lw[g].load(a.w + 8 * i);
-            }
+            if (i >= nvec) continue;
+            ldy[g].load(dyp + 8 * i);
+            ls[g].load(sp + 8 * i);
+            if (a.dres) lr[g].load(rp + 8 * i);
         }
-        const float rstd = a.rstd[row];
-        float dot = 0.f;
+        const uint64_t r2 = pack2(rstd, rstd);
+        uint64_t dot2 = 0;
 #pragma unroll
         for (int g = 0; g < VPT; ++g) {
             if ((int)(threadIdx.x + g * blockDim.x) >= nvec) continue;
@@ -274,13 +407,28 @@ __global__ void __launch_bounds__(1024) rms_norm_grad_kernel(NormGradArgs a) {
             ls[g].get(s);
             lw[g].get(w);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const float xhat = s[j] * rstd;
-                dot = fmaf(dy[j] * w[j], xhat, dot);
-                dw[g][j] = fmaf(dy[j], xhat, dw[g][j]);
+            for (int j = 0; j < 4; ++j) {
+                const uint64_t y2 = pack2(dy[2 * j], dy[2 * j + 1]);
+                const uint64_t xhat = mul2(pack2(s[2 * j], s[2 * j + 1]), r2);
+                dot2 = fma2(mul2(y2, pack2(w[2 * j], w[2 * j + 1])), xhat, dot2);
+                dw[g][j] = fma2(y2, xhat, dw[g][j]);
             }
         }
-        const float c = cta_reduce<false>(dot, red[flip]) / (float)d;
+        float dot, dot_odd;
+        unpack2(dot2, dot, dot_odd);
+        dot += dot_odd;
+        const float c = row_reduce<false>(dot, red[flip], team) * inv_d;
+        const uint64_t k2 = pack2(-rstd * c, -rstd * c);
+        if constexpr (RING) {
+            // every thread is past the row before this one
+            const int before = (stage ? stage : a.stages) - 1;
+            const long long next = row + (long long)(a.stages - 1) * gridDim.x;
+            if (threadIdx.x == 0 && row != blockIdx.x && next < a.M) fill(before, next);
+            if (++stage == a.stages) {
+                stage = 0;
+                phase ^= 1;
+            }
+        }
 #pragma unroll
         for (int g = 0; g < VPT; ++g) {
             const int i = threadIdx.x + g * blockDim.x;
@@ -291,54 +439,95 @@ __global__ void __launch_bounds__(1024) rms_norm_grad_kernel(NormGradArgs a) {
             lw[g].get(w);
             if (a.dres) lr[g].get(r);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const float v = dy[j] * w[j] - s[j] * rstd * c;
-                r[j] = fmaf(rstd, v, r[j]);
+            for (int j = 0; j < 8; j += 2) {
+                // dres + rstd (dy w - s rstd c)
+                const uint64_t v = fma2(pack2(s[j], s[j + 1]), k2,
+                                        mul2(pack2(dy[j], dy[j + 1]), pack2(w[j], w[j + 1])));
+                unpack2(fma2(r2, v, pack2(r[j], r[j + 1])), r[j], r[j + 1]);
             }
             store8(static_cast<T*>(a.dx) + row * d + 8 * i, r);
         }
     }
-    if (!a.part) return;
+    if (failed) latch_error(a.err, CRC_ETIMEOUT);
+    if (!a.part || failed) return;
 #pragma unroll
     for (int g = 0; g < VPT; ++g) {
         const int i = threadIdx.x + g * blockDim.x;
-        if (i < nvec) store8(a.part + (size_t)blockIdx.x * d + 8 * i, dw[g]);
-    }
-}
-
-// dw[c] = sum of the G partial rows: eight row groups a column, then their sum.
-__global__ void __launch_bounds__(256) norm_dw_kernel(const float* part, int G, int d, float* dw) {
-    __shared__ float sm[8][32];
-    const int c = blockIdx.x * 32 + (threadIdx.x & 31), grp = threadIdx.x >> 5;
-    float s = 0.f;
-    if (c < d)
-        for (int g = grp; g < G; g += 8) s += part[(size_t)g * d + c];
-    sm[grp][threadIdx.x & 31] = s;
-    __syncthreads();
-    if (grp == 0 && c < d) {
+        if (i >= nvec) continue;
+        float f[8];
 #pragma unroll
-        for (int k = 1; k < 8; ++k) s += sm[k][threadIdx.x];
-        dw[c] = s;
+        for (int j = 0; j < 4; ++j) unpack2(dw[g][j], f[2 * j], f[2 * j + 1]);
+        store8(a.part + (size_t)blockIdx.x * d + 8 * i, f);
     }
 }
 
-// Threads and groups a thread for rows of d elements.
+// dw[c] = sum of the G partial rows: 32 row groups a column, then their sum.
+__global__ void __launch_bounds__(1024) norm_dw_kernel(const float* part, int G, int d, float* dw) {
+    __shared__ float sm[32][33];
+    asm volatile("griddepcontrol.wait;" ::: "memory");     // the partial rows are written
+    const int lane = threadIdx.x & 31, grp = threadIdx.x >> 5;
+    const int c = blockIdx.x * 32 + lane;
+    float s = 0.f;
+    if (c < d) {
+#pragma unroll 8
+        for (int g = grp; g < G; g += 32) s += __ldcg(part + (size_t)g * d + c);
+    }
+    sm[grp][lane] = s;
+    __syncthreads();
+    s = sm[lane][grp];                 // column grp of this block
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+    if (lane == 0 && blockIdx.x * 32 + grp < d) dw[blockIdx.x * 32 + grp] = s;
+}
+
+// How a call's rows are divided: warps and groups of eight a thread for a row,
+// rows a CTA.
 struct RowShape {
-    int threads, vpt;
+    int warps, vpt, rows;
+    int threads() const { return 32 * warps * rows; }
+    unsigned grid(long long M) const { return (unsigned)((M + rows - 1) / rows); }
 };
-RowShape row_shape(int d) {
+RowShape row_shape(int d, long long M, int most) {
     const int nvec = d / 8;
-    int vpt = 1;
-    while (vpt < 4 && nvec > 512 * vpt) vpt *= 2;
-    const int t = (nvec + vpt - 1) / vpt;
-    return {(t + 31) / 32 * 32, vpt};
+    // Few rows: one group a thread, the shortest way through a row.  Many: up to
+    // `most`, which leaves fewer threads to a reduction and more loads to each.
+    int vpt = M <= 4 * sm_count() ? 1 : most;
+    if (nvec > 512 * vpt) vpt = nvec > 1024 ? 4 : 2;
+    while (vpt > 1 && nvec <= 32 * (vpt - 1)) --vpt;
+    const int warps = (nvec + 32 * vpt - 1) / (32 * vpt);
+    return {warps, vpt, warps < 8 ? 8 / warps : 1};
+}
+// A gradient's CTAs take whole rows one after the other, through a ring (stages 0:
+// none).  Three rows ahead and as many CTAs as registers leave: 8000 x 2048 bf16, us
+// without dw, by the ring of a CTA: 72 KB (3 CTAs an SM) 26, 36 KB (4) 23.5, 24 KB
+// (two rows) 27.
+struct GradShape : RowShape {
+    int stages, stage_bytes;
+};
+GradShape grad_shape(int d, int elem, bool dres) {
+    const int nvec = d / 8;
+    GradShape g;
+    g.vpt = nvec <= 512 ? 1 : nvec <= 1024 ? 2 : 4;
+    g.warps = (nvec + 32 * g.vpt - 1) / (32 * g.vpt);
+    g.rows = 1;
+    g.stage_bytes = (d * (2 + elem * (dres ? 2 : 1)) + 127) / 128 * 128;
+    g.stages = 36 * 1024 / g.stage_bytes;
+    g.stages = g.stages < 3 ? 3 : g.stages < kMaxGradStages ? g.stages : kMaxGradStages;
+    if (g.stages * g.stage_bytes > kGradRing / 2) {              // two CTAs an SM, or one
+        g.stages = kGradRing / 2 / g.stage_bytes;
+        if (g.stages < 2) g.stages = kGradRing / g.stage_bytes;
+        if (g.stages < 2) g.stages = 0;
+        if (g.stages > 4) g.stages = 4;
+    }
+    return g;
 }
 
 inline bool aligned(const void* p, size_t a) { return reinterpret_cast<uintptr_t>(p) % a == 0; }
 
-// Rows that a gradient call's CTAs share.
-int grad_ctas(int M) {
-    const long long most = 4ll * sm_count();
+// The most CTAs of a gradient call (the rows of its workspace); as many of them run
+// as stay resident.
+int grad_ctas(int M, int d) {
+    const long long most = (long long)(d <= 1024 ? 8 : 4) * sm_count();
     return (int)(M < most ? M : most);
 }
 
@@ -348,12 +537,55 @@ int check_rows(int64_t M, int32_t d) {
     return CRC_OK;
 }
 
-#define CRC_VPT(vpt, K, ...)                                      \
-    do {                                                          \
-        if ((vpt) == 1) K(1, __VA_ARGS__);                        \
-        else if ((vpt) == 2) K(2, __VA_ARGS__);                   \
-        else K(4, __VA_ARGS__);                                   \
+// K(groups a thread, most threads a CTA): rows of up to 512 threads leave a thread
+// 128 registers, the widest rows 64.
+#define CRC_SHAPE(sh, K, ...)                                            \
+    do {                                                                 \
+        if ((sh).threads() > 512) {                                      \
+            if ((sh).vpt <= 2) K(2, 1024, __VA_ARGS__);                  \
+            else K(4, 1024, __VA_ARGS__);                                \
+        } else if ((sh).vpt == 1) K(1, 512, __VA_ARGS__);                \
+        else if ((sh).vpt == 2) K(2, 512, __VA_ARGS__);                  \
+        else if ((sh).vpt == 3) K(3, 512, __VA_ARGS__);                  \
+        else K(4, 512, __VA_ARGS__);                                     \
     } while (0)
+
+template <typename T, int VPT, int THREADS, bool RING>
+int launch_grad_t(const GradShape& sh, int& G, const NormGradArgs& a, cudaStream_t stream) {
+    auto kern = rms_norm_grad_kernel<T, VPT, THREADS, RING>;
+    const int smem = RING ? sh.stages * sh.stage_bytes : 0;
+    static PerDevice ready;
+    const int up = ready.get(current_device(), [&] {
+        return cuda_status(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                                RING ? kGradRing : 0)) == CRC_OK;
+    });
+    if (!up) return CRC_ECUDA;
+    if (G > sm_count()) {
+        int fit = 0;
+        if (const int rc = cuda_status(
+                cudaOccupancyMaxActiveBlocksPerMultiprocessor(&fit, kern, sh.threads(), smem)))
+            return rc;
+        if (fit < 1) return CRC_ECUDA;
+        const long long most = (long long)fit * sm_count();
+        G = (int)(G < most ? G : most);
+    }
+    {
+        ProfScope prof(CRC_KERNEL_NORM, stream);
+        kern<<<G, sh.threads(), smem, stream>>>(a);
+    }
+    note_launch();
+    return cuda_status(cudaGetLastError());
+}
+template <typename T>
+int launch_grad(const GradShape& sh, int& G, const NormGradArgs& a, cudaStream_t stream) {
+    if (!sh.stages)
+        return sh.threads() > 512 ? launch_grad_t<T, 4, 1024, false>(sh, G, a, stream)
+                                  : launch_grad_t<T, 4, 512, false>(sh, G, a, stream);
+    if (sh.vpt == 1) return launch_grad_t<T, 1, 512, true>(sh, G, a, stream);
+    if (sh.vpt == 2) return launch_grad_t<T, 2, 512, true>(sh, G, a, stream);
+    return sh.threads() > 512 ? launch_grad_t<T, 4, 1024, true>(sh, G, a, stream)
+                              : launch_grad_t<T, 4, 512, true>(sh, G, a, stream);
+}
 
 }  // namespace
 }  // namespace crc
@@ -389,18 +621,21 @@ int crc_rms_norm(const void *x_dev, int64_t x_stride, const void* residual_dev,
     a.scale = scale8_dev;
     a.rstd = rstd_dev;
     a.ldx = x_stride;
+    // us with 1, 2, 4 groups a thread: 4097 x 2880 fp32 29.3, 29.8, 31.5 (the two inputs
+    // of four groups are 64 registers); 8192 x 2048 bf16 35.2, 27.2, 26.1
+    const RowShape sh = row_shape(d, M, stream_type == CRC_F32 ? 1 : 4);
     a.M = (int)M;
     a.d = d;
+    a.warps = sh.warps;
     a.eps = (float)eps;
-    const RowShape sh = row_shape(d);
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     {
         ProfScope prof(CRC_KERNEL_NORM, st);
-#define CRC_K(V, T) rms_norm_kernel<T, V><<<(unsigned)M, sh.threads, 0, st>>>(a)
+#define CRC_K(V, B, T) rms_norm_kernel<T, V, B><<<sh.grid(M), sh.threads(), 0, st>>>(a)
         if (stream_type == CRC_BF16)
-            CRC_VPT(sh.vpt, CRC_K, __nv_bfloat16);
+            CRC_SHAPE(sh, CRC_K, __nv_bfloat16);
         else
-            CRC_VPT(sh.vpt, CRC_K, float);
+            CRC_SHAPE(sh, CRC_K, float);
 #undef CRC_K
     }
     note_launch();
@@ -409,7 +644,7 @@ int crc_rms_norm(const void *x_dev, int64_t x_stride, const void* residual_dev,
 
 size_t crc_rms_norm_grad_workspace_bytes(int64_t M, int32_t d) {
     if (check_rows(M, d) != CRC_OK || M < 1) return 0;
-    return ((size_t)grad_ctas((int)M) * d * sizeof(float) + 255) / 256 * 256;
+    return ((size_t)grad_ctas((int)M, d) * d * sizeof(float) + 255) / 256 * 256;
 }
 
 int crc_rms_norm_grad(const uint16_t* dy_dev, const void* s_dev, const uint16_t* weight_dev,
@@ -440,26 +675,32 @@ int crc_rms_norm_grad(const uint16_t* dy_dev, const void* s_dev, const uint16_t*
     a.part = dw_dev ? static_cast<float*>(workspace_dev) : nullptr;
     a.M = (int)M;
     a.d = d;
-    const RowShape sh = row_shape(d);
-    const int G = grad_ctas((int)M);
+    const GradShape sh = grad_shape(d, stream_type == CRC_BF16 ? 2 : 4, dres_dev != nullptr);
+    int G = grad_ctas((int)M, d);
+    a.err = device_error_word();
+    a.stages = sh.stages;
+    a.stage_bytes = sh.stage_bytes;
+    const int rg = stream_type == CRC_BF16 ? launch_grad<__nv_bfloat16>(sh, G, a, st)
+                                           : launch_grad<float>(sh, G, a, st);
+    if (rg) return rg;
+    if (!dw_dev) return CRC_OK;
+    cudaError_t e;
     {
+        // its blocks take their places while the rows are still on their way
+        cudaLaunchAttribute at[1];
+        at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+        at[0].val.programmaticStreamSerializationAllowed = 1;
+        cudaLaunchConfig_t c = {};
+        c.gridDim = dim3((unsigned)((d + 31) / 32));
+        c.blockDim = dim3(1024);
+        c.stream = st;
+        c.attrs = at;
+        c.numAttrs = 1;
         ProfScope prof(CRC_KERNEL_NORM, st);
-#define CRC_K(V, T) rms_norm_grad_kernel<T, V><<<G, sh.threads, 0, st>>>(a)
-        if (stream_type == CRC_BF16)
-            CRC_VPT(sh.vpt, CRC_K, __nv_bfloat16);
-        else
-            CRC_VPT(sh.vpt, CRC_K, float);
-#undef CRC_K
+        e = cudaLaunchKernelEx(&c, norm_dw_kernel, (const float*)a.part, G, d, dw_dev);
     }
     note_launch();
-    int e = cuda_status(cudaGetLastError());
-    if (e || !dw_dev) return e;
-    {
-        ProfScope prof(CRC_KERNEL_NORM, st);
-        norm_dw_kernel<<<(d + 31) / 32, 256, 0, st>>>(a.part, G, d, dw_dev);
-    }
-    note_launch();
-    return cuda_status(cudaGetLastError());
+    return cuda_status(e);
 }
 
 int crc_quantize_rows(const uint16_t* x_dev, int64_t x_stride, int64_t M, int32_t d,
@@ -470,14 +711,20 @@ int crc_quantize_rows(const uint16_t* x_dev, int64_t x_stride, int64_t M, int32_
     if (M == 0) return CRC_OK;
     if (!x_dev || !out8_dev || !scale8_dev) return CRC_EINVAL;
     if (!aligned(x_dev, 16) || !aligned(out8_dev, 8) || !aligned(scale8_dev, 4)) return CRC_EINVAL;
-    const RowShape sh = row_shape(d);
+    // us with 2, 3, 4 groups a thread: 184320 x 2880 276, 235, 314; 65536 x 1024 35, 36, 36;
+    // 30000 x 6000 104, 81, 109 (four groups and the next four leave too few threads)
+    const RowShape sh = row_shape(d, M, 3);
+    // as many CTAs as stay resident, 2048 threads an SM
+    const long long most = (long long)sm_count() * (2048 / sh.threads());
+    const unsigned grid = (unsigned)(sh.grid(M) < most ? sh.grid(M) : most);
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     const __nv_bfloat16* x = reinterpret_cast<const __nv_bfloat16*>(x_dev);
     {
         ProfScope prof(CRC_KERNEL_QUANTIZE, st);
-#define CRC_K(V, dummy) \
-    quantize_rows_kernel<V><<<(unsigned)M, sh.threads, 0, st>>>(x, x_stride, d, out8_dev, scale8_dev)
-        CRC_VPT(sh.vpt, CRC_K, 0);
+#define CRC_K(V, B, unused) \
+    quantize_rows_kernel<V, B><<<grid, sh.threads(), 0, st>>>(x, x_stride, (int)M, d, sh.warps, \
+                                                              out8_dev, scale8_dev)
+        CRC_SHAPE(sh, CRC_K, 0);
 #undef CRC_K
     }
     note_launch();
