@@ -37,6 +37,7 @@ namespace crc {
 constexpr int kMoeThreads = 512;     // warps 0 TMA, 1 MMA, 2-3 idle, 4-7 epilogue, 8-15 rows
 constexpr int kMoeMaxTiles = 256;    // row tiles of NT: N + M K / NT at most, M K <= 128 NT
 constexpr int kItemRing = 4;
+// Control words: the next item; phase-2 warps done; phase-1 warps done, by row tile.
 constexpr int kCtrlNext = 0, kCtrlDone2 = 1, kCtrlDone1 = 2;
 constexpr int kCtrlWords = kCtrlDone1 + kMoeMaxTiles;
 
@@ -54,7 +55,7 @@ struct MoeCfg {
     static constexpr int SA =
         (232448 - 1024 - BAR_BYTES - TABLE_BYTES - SB * B_BYTES) / A_BYTES;
     static constexpr int SMEM = 1024 + BAR_BYTES + TABLE_BYTES + SB * B_BYTES + SA * A_BYTES;
-    static constexpr int DEPTH = NT == 16 ? 4 : NT == 32 ? 2 : 1;   // row blocks a thread has in flight
+    static constexpr int DEPTH = NT == 16 ? 6 : NT == 32 ? 2 : 1;   // row blocks a thread has in flight
     static_assert(SA > SB && SA <= 16, "weight ring");
 };
 
@@ -447,6 +448,24 @@ __device__ __forceinline__ bool produce_rows(const MoeShared<W8, NT>& s, const u
     return true;
 }
 
+// Gates of up to eight choices from r on; a bit for each whose expert has a slot.
+struct Gates {
+    float g[8];
+    uint32_t have;
+    __device__ __forceinline__ void load(const MoeArgs& a, const int* slot, int r, int n) {
+        have = 0;
+        int id[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            id[k] = k < n ? (int)__ldcg(a.ids + r + k) : 0;
+            g[k] = k < n ? __ldcg(a.gates + r + k) : 0.f;
+        }
+#pragma unroll
+        for (int k = 0; k < 8; ++k)
+            if (k < n && slot[id[k]] >= 0) have |= 1u << k;
+    }
+};
+
 template <bool W8, int NT>
 __global__ void __launch_bounds__(kMoeThreads, 1)
     moe_experts_kernel(const __grid_constant__ CUtensorMap map13,
@@ -816,6 +835,14 @@ __global__ void __launch_bounds__(kMoeThreads, 1)
     }
 
     // -------------------------------------------------------- the choices' sum
+    // Four elements of d of one token a thread; all loads of eight choices are under
+    // way at once, and the first gates before the last y is there.
+    const int quads = a.d / 4;
+    const long long all = (long long)a.M * quads;
+    long long i = (long long)blockIdx.x * kMoeThreads + threadIdx.x;
+    int tok = i < all ? (int)(i / quads) : 0;
+    Gates gates;
+    if (i < all) gates.load(a, s.slot, tok * a.K, a.K);
     if (threadIdx.x == 0) {
         const bool ok = wait_count(&a.ctrl[kCtrlDone2], 4u * (uint32_t)(tiles * a.dt));
         if (!ok) latch_error(a.err, CRC_ETIMEOUT);
@@ -823,29 +850,25 @@ __global__ void __launch_bounds__(kMoeThreads, 1)
     }
     __syncthreads();
     if (!s.items[0]) return;
-    const int quads = a.d / 4;
-    const long long all = (long long)a.M * quads;
-    for (long long i = (long long)blockIdx.x * kMoeThreads + threadIdx.x; i < all;
-         i += (long long)gridDim.x * kMoeThreads) {
-        const int tok = (int)(i / quads), c = (int)(i - (long long)tok * quads) * 4;
+    while (i < all) {
+        const int c = (int)(i - (long long)tok * quads) * 4;
         float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-        for (int k0 = 0; k0 < a.K; k0 += 8) {      // all loads of eight choices at once
-            float g[8];
+        for (int k0 = 0; k0 < a.K; k0 += 8) {
+            const int r = tok * a.K + k0;
+            if (k0) gates.load(a, s.slot, r, a.K - k0);
             float4 y[8];
 #pragma unroll
-            for (int k = 0; k < 8; ++k) {
-                const int r = tok * a.K + k0 + k;
-                const bool in = k0 + k < a.K && s.slot[__ldcg(a.ids + r)] >= 0;
-                g[k] = in ? __ldcg(a.gates + r) : 0.f;
-                y[k] = in ? __ldcg(reinterpret_cast<const float4*>(a.y + (size_t)r * a.d + c))
-                          : make_float4(0.f, 0.f, 0.f, 0.f);
-            }
+            for (int k = 0; k < 8; ++k)
+                y[k] = gates.have >> k & 1u
+                           ? __ldcg(reinterpret_cast<const float4*>(a.y + (size_t)(r + k) * a.d + c))
+                           : make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
             for (int k = 0; k < 8; ++k) {
-                o.x = fmaf(g[k], y[k].x, o.x);
-                o.y = fmaf(g[k], y[k].y, o.y);
-                o.z = fmaf(g[k], y[k].z, o.z);
-                o.w = fmaf(g[k], y[k].w, o.w);
+                if (!(gates.have >> k & 1u)) continue;
+                o.x = fmaf(gates.g[k], y[k].x, o.x);
+                o.y = fmaf(gates.g[k], y[k].y, o.y);
+                o.z = fmaf(gates.g[k], y[k].z, o.z);
+                o.w = fmaf(gates.g[k], y[k].w, o.w);
             }
         }
         const __nv_bfloat162 p = __floats2bfloat162_rn(o.x, o.y), q = __floats2bfloat162_rn(o.z, o.w);
@@ -853,6 +876,10 @@ __global__ void __launch_bounds__(kMoeThreads, 1)
         w.x = *reinterpret_cast<const uint32_t*>(&p);
         w.y = *reinterpret_cast<const uint32_t*>(&q);
         *reinterpret_cast<uint2*>(a.out + (size_t)tok * a.d + c) = w;
+        i += (long long)gridDim.x * kMoeThreads;
+        if (i >= all) break;
+        tok = (int)(i / quads);
+        gates.load(a, s.slot, tok * a.K, a.K);
     }
 }
 
