@@ -748,11 +748,30 @@ __global__ void __launch_bounds__(kMoeThreads, 1)
             if (W8 && in)
                 sw = it.phase ? a.s2[slot * a.s2_stride + wrow]
                               : a.s13[slot * a.s13_stride + (lane >> 4) * a.f + wrow];
+            // scales of the rows: lane l holds those of rows l, l + 32
+            constexpr int RS = (NT + 31) / 32;
+            float rs[RS];
+            if (W8 && it.phase == 0) {
+#pragma unroll
+                for (int u = 0; u < RS; ++u) {
+                    const int r = lane + 32 * u;
+                    rs[u] = r < it.rows ? __ldcg(a.xs + s.list[it.row0 + r] / a.K) : 0.f;
+                }
+            }
             if (!mbar_wait(&s.t_full[acc], aphase)) {
                 failed = true;
                 break;
             }
             tc_fence_after();
+            if (W8 && it.phase) {     // h's largest values: final since its rows were read
+#pragma unroll
+                for (int u = 0; u < RS; ++u) {
+                    const int r = lane + 32 * u;
+                    rs[u] = r < it.rows
+                                ? split_scale(__uint_as_float(__ldcg(a.hmax + it.row0 + r)))
+                                : 0.f;
+                }
+            }
             const uint32_t tb =
                 tmem + (uint32_t)(acc * Cfg::COLS) + ((uint32_t)(quarter * 32) << 16);
 #pragma unroll 1
@@ -777,42 +796,50 @@ __global__ void __launch_bounds__(kMoeThreads, 1)
                     if (lane == 0) mbar_arrive(&s.t_empty[acc]);
                 }
                 const int n = it.rows - c0 < 16 ? it.rows - c0 : 16;
+                if (W8) {
+                    const float r = RS == 2 && c0 >= 32 ? rs[RS - 1] : rs[0];
+#pragma unroll
+                    for (int c = 0; c < 16; ++c)
+                        v[c] *= sw * __shfl_sync(kFull, r, (c0 & 16) + c);
+                }
                 if (it.phase == 0) {
+                    uint32_t top[8];
 #pragma unroll
                     for (int c = 0; c < 16; c += 2) {
-                        if (c >= n) break;
-                        float p0 = v[c], p1 = v[c + 1];
-                        if (W8) {
-                            const int r = it.row0 + c0 + c;
-                            const int r1 = c + 1 < n ? r + 1 : r;
-                            p0 *= sw * __ldcg(a.xs + s.list[r] / a.K);
-                            p1 *= sw * __ldcg(a.xs + s.list[r1] / a.K);
-                        }
                         // low half: column c, high half: column c + 1
-                        const float got = __shfl_xor_sync(kFull, lane < 16 ? p1 : p0, 16);
-                        const float gate = lane < 16 ? p0 : got, up = lane < 16 ? got : p1;
-                        const float hv = gate / (1.f + __expf(-gate)) * up;
+                        const float got =
+                            __shfl_xor_sync(kFull, lane < 16 ? v[c + 1] : v[c], 16);
+                        const float gate = lane < 16 ? v[c] : got, up = lane < 16 ? got : v[c + 1];
+                        const float hv = __fdividef(gate, 1.f + __expf(-gate)) * up;
                         const __nv_bfloat16 hb = __float2bfloat16_rn(hv);
                         const int col = c + (lane >> 4);
-                        const int row = it.row0 + c0 + col;
-                        if (in && col < n) a.h[(size_t)row * a.f + wrow] = hb;
-                        if (W8) {
-                            uint32_t m =
-                                in ? (uint32_t)(__bfloat16_as_ushort(hb) & 0x7fffu) << 16 : 0u;
+                        const bool mine = in && col < n;
+                        if (mine) a.h[(size_t)(it.row0 + c0 + col) * a.f + wrow] = hb;
+                        if (W8)
+                            top[c / 2] = mine ? (uint32_t)__bfloat16_as_ushort(hb) << 16 & 0x7fffffffu : 0u;
+                    }
+                    if (W8) {
+                        // the largest of 16 lanes for eight columns at once: each exchange
+                        // halves the columns that a lane keeps
 #pragma unroll
-                            for (int o = 8; o > 0; o >>= 1)
-                                m = max(m, __shfl_xor_sync(kFull, m, o));
-                            if ((lane & 15) == 0 && col < n && m) atomicMax(a.hmax + row, m);
-                        }
+                        for (int o = 8, m = 4; o > 1; o >>= 1, m >>= 1)
+#pragma unroll
+                            for (int i = 0; i < m; ++i) {
+                                const bool upper = lane & o;
+                                const uint32_t keep = upper ? top[i + m] : top[i];
+                                const uint32_t give = upper ? top[i] : top[i + m];
+                                top[i] = max(keep, __shfl_xor_sync(kFull, give, o));
+                            }
+                        const uint32_t m = max(top[0], __shfl_xor_sync(kFull, top[0], 1));
+                        const int col = 2 * ((lane & 8 ? 4 : 0) + (lane & 4 ? 2 : 0) +
+                                             (lane & 2 ? 1 : 0)) + (lane >> 4);
+                        if (!(lane & 1) && col < n && m) atomicMax(a.hmax + it.row0 + c0 + col, m);
                     }
                 } else {
 #pragma unroll
                     for (int c = 0; c < 16; ++c) {
                         if (c >= n) break;
-                        float p = v[c];
-                        const int row = it.row0 + c0 + c;
-                        if (W8) p *= sw * split_scale(__uint_as_float(__ldcg(a.hmax + row)));
-                        if (in) a.y[(size_t)s.list[row] * a.d + wrow] = p;
+                        if (in) a.y[(size_t)s.list[it.row0 + c0 + c] * a.d + wrow] = v[c];
                     }
                 }
             }
