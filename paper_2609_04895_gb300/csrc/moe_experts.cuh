@@ -50,7 +50,8 @@ struct MoeCfg {
     static constexpr int SB = NT == 16 ? 8 : NT == 32 ? 6 : W8 ? 3 : 5;
     static constexpr int LIST = 128 * NT;                      // choices (M K) at most
     static constexpr int TMEM_COLS = 2 * (COLS < 16 ? 16 : COLS) < 32 ? 32 : 2 * COLS;
-    static constexpr int TABLE_BYTES = 3 * 128 * 4 + 3 * kMoeMaxTiles * 2 + LIST * 2 + 64;
+    static constexpr int TABLE_BYTES = 3 * 128 * 4 + 3 * kMoeMaxTiles * 2 + LIST * 2 +
+                                       kItemRing * NT * 4 + 64;
     static constexpr int BAR_BYTES = 512;
     static constexpr int SA =
         (232448 - 1024 - BAR_BYTES - TABLE_BYTES - SB * B_BYTES) / A_BYTES;
@@ -196,6 +197,7 @@ struct MoeShared {
     uint64_t *a_full, *a_empty, *b_full, *t_full, *t_empty, *i_full, *i_empty, *drain;
     uint32_t* tmem_slot;
     int* items;
+    float* hscale;         // [kItemRing][NT] scales of h's rows (8-bit weights)
     int* slot;             // [128] slot of each expert, -1 without
     int* start;            // [128] first row of each expert
     int* count;            // [128] rows of each expert, then [0] = row tiles
@@ -226,6 +228,7 @@ struct MoeShared {
         tile_row = tile_e + kMoeMaxTiles;
         tile_rows = tile_row + kMoeMaxTiles;
         list = tile_rows + kMoeMaxTiles;
+        hscale = reinterpret_cast<float*>(list + Cfg::LIST);
     }
 };
 
@@ -662,7 +665,7 @@ __global__ void __launch_bounds__(kMoeThreads, 1)
                 failed = true;
                 break;
             }
-            const int item = s.items[islot];
+            const int item = s.items[islot], ring_slot = islot;
             __syncwarp();
             if (lane == 0) mbar_arrive(&s.i_empty[islot]);
             if (++islot == kItemRing) {
@@ -694,8 +697,13 @@ __global__ void __launch_bounds__(kMoeThreads, 1)
                 have |= 1u << u;
                 if (it.phase) {
                     src[u] = reinterpret_cast<const uint8_t*>(a.h + (size_t)(it.row0 + r) * a.f);
-                    if (W8)
-                        inv[u] = 1.f / split_scale(__uint_as_float(__ldcg(a.hmax + it.row0 + r)));
+                    if (W8) {
+                        const float hs =
+                            split_scale(__uint_as_float(__ldcg(a.hmax + it.row0 + r)));
+                        inv[u] = 1.f / hs;
+                        // for the epilogue, from the group whose block is the item's first
+                        if (ring.next == base && (tid & 7) == 0) s.hscale[ring_slot * NT + r] = hs;
+                    }
                 } else {
                     const int tok = s.list[it.row0 + r] / a.K;
                     src[u] = a.x + tok * a.x_bytes;
@@ -728,12 +736,6 @@ __global__ void __launch_bounds__(kMoeThreads, 1)
                 break;
             }
             const int item = s.items[islot];
-            __syncwarp();
-            if (lane == 0) mbar_arrive(&s.i_empty[islot]);
-            if (++islot == kItemRing) {
-                islot = 0;
-                iphase ^= 1;
-            }
             if (item < 0) break;
             const MoeItem it = moe_item<W8, NT>(a, s, item);
             const int slot = s.slot[it.e];
@@ -763,14 +765,18 @@ __global__ void __launch_bounds__(kMoeThreads, 1)
                 break;
             }
             tc_fence_after();
-            if (W8 && it.phase) {     // h's largest values: final since its rows were read
+            if (W8 && it.phase) {
 #pragma unroll
                 for (int u = 0; u < RS; ++u) {
                     const int r = lane + 32 * u;
-                    rs[u] = r < it.rows
-                                ? split_scale(__uint_as_float(__ldcg(a.hmax + it.row0 + r)))
-                                : 0.f;
+                    rs[u] = r < it.rows ? s.hscale[islot * NT + r] : 0.f;
                 }
+            }
+            __syncwarp();             // the item's place is free when its scales are read
+            if (lane == 0) mbar_arrive(&s.i_empty[islot]);
+            if (++islot == kItemRing) {
+                islot = 0;
+                iphase ^= 1;
             }
             const uint32_t tb =
                 tmem + (uint32_t)(acc * Cfg::COLS) + ((uint32_t)(quarter * 32) << 16);
@@ -803,9 +809,10 @@ __global__ void __launch_bounds__(kMoeThreads, 1)
                         v[c] *= sw * __shfl_sync(kFull, r, (c0 & 16) + c);
                 }
                 if (it.phase == 0) {
-                    uint32_t top[8];
+                    uint32_t top[8] = {};
 #pragma unroll
                     for (int c = 0; c < 16; c += 2) {
+                        if (c >= n) break;
                         // low half: column c, high half: column c + 1
                         const float got =
                             __shfl_xor_sync(kFull, lane < 16 ? v[c + 1] : v[c], 16);
