@@ -245,7 +245,7 @@ int crc_moe_layer(const crc_moe* m, const uint16_t* x_dev, int64_t x_stride, con
     a.d = m->d;
     a.f = m->f;
     a.slots = m->slots;
-    const int bk = w8 ? 128 : 64;
+    const int bk = w8 ? 256 : 128;           // elements of 256 bytes
     a.kb1 = (m->d + bk - 1) / bk;
     a.kb2 = (m->f + bk - 1) / bk;
     a.ft = (m->f + 63) / 64;

@@ -7,10 +7,11 @@
 // A few tokens read every active expert's weights once and multiply each by a
 // handful of rows, so the kernel is built to stream weights: they are the A
 // operand (128 weight rows of one tcgen05.mma), the rows that take the expert
-// its N columns (16 at least).  TMA fetches 128-row x 128-byte blocks of
-// weights into a ring that holds as much as shared memory has room for; with
-// 8-bit weights a block is 128 x 128 elements and goes to the tensor cores as it
-// lies in memory.
+// its N columns (16 at least).  TMA fetches blocks of 128 rows x 256 bytes of
+// weights into a ring that holds as much as shared memory has room for; 8-bit
+// weights go to the tensor cores as they lie in memory.  256 bytes and not one
+// 128-byte swizzle row: a block costs the MMA warp 150 ns beside its MMAs and their
+// commit (70 ns for 128 bytes), which bounds a CTA's stream when few run.
 //
 // Work items, claimed in order from one counter, so that a CTA waits only for
 // items that running CTAs hold (no co-residency is needed):
@@ -43,11 +44,12 @@ constexpr int kCtrlWords = kCtrlDone1 + kMoeMaxTiles;
 
 template <bool W8, int NT>
 struct MoeCfg {
-    static constexpr int A_BYTES = 128 * 128;                  // 128 weight rows x 128 bytes
-    static constexpr int BK = W8 ? 128 : 64;                   // elements of a block's row
+    // a block: two halves of 128 bytes (one swizzle row) of 128 weight rows
+    static constexpr int A_HALF = 128 * 128, A_BYTES = 2 * A_HALF;
+    static constexpr int BK = W8 ? 256 : 128;                  // elements of a block's row
     static constexpr int COLS = NT * (W8 ? 2 : 1);             // accumulator columns
-    static constexpr int B_BYTES = COLS * 128;
-    static constexpr int SB = NT == 16 ? 8 : NT == 32 ? 6 : W8 ? 3 : 5;
+    static constexpr int B_HALF = COLS * 128, B_BYTES = 2 * B_HALF;
+    static constexpr int SB = NT == 64 && W8 ? 2 : 3;
     static constexpr int LIST = 128 * NT;                      // choices (M K) at most
     static constexpr int TMEM_COLS = 2 * (COLS < 16 ? 16 : COLS) < 32 ? 32 : 2 * COLS;
     static constexpr int TABLE_BYTES = 3 * 128 * 4 + 3 * kMoeMaxTiles * 2 + LIST * 2 +
@@ -56,7 +58,7 @@ struct MoeCfg {
     static constexpr int SA =
         (232448 - 1024 - BAR_BYTES - TABLE_BYTES - SB * B_BYTES) / A_BYTES;
     static constexpr int SMEM = 1024 + BAR_BYTES + TABLE_BYTES + SB * B_BYTES + SA * A_BYTES;
-    static constexpr int DEPTH = NT == 16 ? 6 : NT == 32 ? 2 : 1;   // row blocks a thread has in flight
+    static constexpr int DEPTH = NT == 16 ? 3 : 1;             // row blocks a thread has in flight
     static_assert(SA > SB && SA <= 16, "weight ring");
 };
 
@@ -391,19 +393,19 @@ struct RowRing {
 };
 
 // A group's row blocks of one item into the ring (four warps).  base: the item's
-// first block, counted over all items.  A thread's unit is
-// 16 bytes of one row's 128-byte block: chunk tid % 8 of rows tid / 8, + 16, ...
-// SPLIT: 16 bf16 elements become 16 bytes of hi and of lo.
+// first block, counted over all items.  A thread's unit is 16 bytes of one row's
+// 256: chunk tid % 16 of rows tid / 16, + 8, ...  SPLIT: 16 bf16 elements become 16
+// bytes of hi and of lo.
 template <bool W8, int NT, bool SPLIT>
-__device__ __forceinline__ bool produce_rows(const MoeShared<W8, NT>& s, const uint8_t* (&src)[NT / 16],
-                                             const float (&inv)[NT / 16], uint32_t have, int n8,
+__device__ __forceinline__ bool produce_rows(const MoeShared<W8, NT>& s, const uint8_t* (&src)[NT / 8],
+                                             const float (&inv)[NT / 8], uint32_t have, int n8,
                                              int base, int kb, int K, int tid,
                                              RowRing<W8, NT>& ring) {
     using Cfg = MoeCfg<W8, NT>;
-    constexpr int U = NT / 16, D = Cfg::DEPTH, V = SPLIT ? 2 : 1;
-    constexpr int STEP = SPLIT ? 2 * 128 : 128;                // bytes of a row's block
+    constexpr int U = NT / 8, D = Cfg::DEPTH, V = SPLIT ? 2 : 1;
+    constexpr int STEP = SPLIT ? 2 * 256 : 256;                // bytes of a row's block
     constexpr int CE = SPLIT || W8 ? 16 : 8;                   // elements of a unit
-    const int chunk = tid & 7, lane = tid & 31;
+    const int chunk = tid & 15, lane = tid & 31;
     uint4 v[D][U][V];
     auto load = [&](int k, uint4 (&r)[U][V]) {
         const bool in = k * Cfg::BK + chunk * CE < K;
@@ -425,19 +427,19 @@ __device__ __forceinline__ bool produce_rows(const MoeShared<W8, NT>& s, const u
             if (k >= kb) break;
             if (ring.next >= Cfg::SB && !mbar_wait(&s.a_empty[ring.free], ring.free_phase))
                 return false;
-            uint8_t* dst = s.b + ring.stage * Cfg::B_BYTES;
+            uint8_t* dst = s.b + ring.stage * Cfg::B_BYTES + (chunk >> 3) * Cfg::B_HALF;
 #pragma unroll
             for (int u = 0; u < U; ++u) {
                 if (!(have >> u & 1u)) continue;
-                const int row = (tid >> 3) + 16 * u;
+                const int row = (tid >> 4) + 8 * u;
                 if constexpr (SPLIT) {
                     uint4 hi, lo;
                     split16(v[i][u], inv[u], hi, lo);
                     const int low = n8 + row;
-                    *reinterpret_cast<uint4*>(dst + row * 128 + ((chunk ^ (row & 7)) << 4)) = hi;
-                    *reinterpret_cast<uint4*>(dst + low * 128 + ((chunk ^ (low & 7)) << 4)) = lo;
+                    *reinterpret_cast<uint4*>(dst + row * 128 + (((chunk ^ row) & 7) << 4)) = hi;
+                    *reinterpret_cast<uint4*>(dst + low * 128 + (((chunk ^ low) & 7) << 4)) = lo;
                 } else {
-                    *reinterpret_cast<uint4*>(dst + row * 128 + ((chunk ^ (row & 7)) << 4)) =
+                    *reinterpret_cast<uint4*>(dst + row * 128 + (((chunk ^ row) & 7) << 4)) =
                         v[i][u][0];
                 }
             }
@@ -555,12 +557,16 @@ __global__ void __launch_bounds__(kMoeThreads, 1)
                     }
                     mbar_arrive_expect_tx(&s.a_full[stage], Cfg::A_BYTES);
                     uint8_t* dst = s.a + stage * Cfg::A_BYTES;
-                    if (it.phase == 0)
-                        tma_load_5d(dst, &map13, &s.a_full[stage], k * Cfg::BK, 0, 0, it.j * 4,
-                                    slot, pol);
-                    else
-                        tma_load_3d(dst, &map2, &s.a_full[stage], k * Cfg::BK, it.j * 128, slot,
-                                    pol);
+#pragma unroll
+                    for (int half = 0; half < 2; ++half) {     // past the row's end: zeros
+                        const int x = k * Cfg::BK + half * (Cfg::BK / 2);
+                        if (it.phase == 0)
+                            tma_load_5d(dst + half * Cfg::A_HALF, &map13, &s.a_full[stage], x, 0, 0,
+                                        it.j * 4, slot, pol);
+                        else
+                            tma_load_3d(dst + half * Cfg::A_HALF, &map2, &s.a_full[stage], x,
+                                        it.j * 128, slot, pol);
+                    }
                     ++issued;
                     if (++stage == Cfg::SA) {
                         stage = 0;
@@ -632,8 +638,10 @@ __global__ void __launch_bounds__(kMoeThreads, 1)
                 const uint64_t ad = a0 + (uint64_t)(stage * (Cfg::A_BYTES >> 4));
                 const uint64_t bd = b0 + (uint64_t)(bstage * (Cfg::B_BYTES >> 4));
 #pragma unroll
-                for (int q = 0; q < 4; ++q)             // 32 bytes of K a step
-                    umma<W8>(dt, ad + 2 * q, bd + 2 * q, idesc, (k | q) != 0, lead);
+                for (int q = 0; q < 8; ++q)             // 32 bytes of K a step
+                    umma<W8>(dt, ad + (q >> 2) * (Cfg::A_HALF >> 4) + 2 * (q & 3),
+                             bd + (q >> 2) * (Cfg::B_HALF >> 4) + 2 * (q & 3), idesc, (k | q) != 0,
+                             lead);
                 umma_commit_by(&s.a_empty[stage], lead);
                 if (++stage == Cfg::SA) {
                     stage = 0;
@@ -685,12 +693,12 @@ __global__ void __launch_bounds__(kMoeThreads, 1)
             }
             const bool split = W8 && (it.phase || a.x_split);
             const int n8 = (it.rows + 7) & ~7;
-            const uint8_t* src[NT / 16];
-            float inv[NT / 16];
+            const uint8_t* src[NT / 8];
+            float inv[NT / 8];
             uint32_t have = 0;
 #pragma unroll
-            for (int u = 0; u < NT / 16; ++u) {
-                const int r = (tid >> 3) + 16 * u;
+            for (int u = 0; u < NT / 8; ++u) {
+                const int r = (tid >> 4) + 8 * u;
                 src[u] = nullptr;
                 inv[u] = 1.f;
                 if (r >= it.rows) continue;
@@ -702,14 +710,14 @@ __global__ void __launch_bounds__(kMoeThreads, 1)
                             split_scale(__uint_as_float(__ldcg(a.hmax + it.row0 + r)));
                         inv[u] = 1.f / hs;
                         // for the epilogue, from the group whose block is the item's first
-                        if (ring.next == base && (tid & 7) == 0) s.hscale[ring_slot * NT + r] = hs;
+                        if (ring.next == base && (tid & 15) == 0) s.hscale[ring_slot * NT + r] = hs;
                     }
                 } else {
                     const int tok = s.list[it.row0 + r] / a.K;
                     src[u] = a.x + tok * a.x_bytes;
                     if (W8 && split) inv[u] = 1.f / __ldcg(a.xs + tok);
                 }
-                src[u] += (tid & 7) * (split ? 32 : 16);
+                src[u] += (tid & 15) * (split ? 32 : 16);
             }
             const int kb = it.phase ? a.kb2 : a.kb1, K = it.phase ? a.f : a.d;
             bool ok;
