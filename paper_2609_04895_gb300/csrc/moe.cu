@@ -20,8 +20,18 @@ constexpr int kMoeMaxEntries = 8192;      // M K
 inline bool aligned(const void* p, size_t a) { return reinterpret_cast<uintptr_t>(p) % a == 0; }
 inline size_t up256(size_t n) { return (n + 255) & ~(size_t)255; }
 
+// Rows of a tile: twice an expert's mean share of the choices, so that few experts
+// need a second pass over their weights, or the tokens if that is fewer.
+// Narrow tiles leave room for more row blocks in flight.
+int row_tile(int M, int K, int N) {
+    const int E = M * K;
+    for (int nt = 16; nt < 64; nt *= 2)
+        if (E <= 128 * nt && (M <= nt || 2 * E <= nt * N)) return nt;
+    return 64;
+}
+
 struct MoeLayout {
-    size_t ctrl, hmax, ids, gates, xscale, h, y, total;     // hmax right behind ctrl
+    size_t ctrl, hmax, ids, gates, xscale, h, y, xq, hq, total;     // hmax right behind ctrl
 };
 
 MoeLayout moe_layout(const crc_moe& m, int M) {
@@ -34,7 +44,10 @@ MoeLayout moe_layout(const crc_moe& m, int M) {
     l.xscale = l.gates + up256(E * 4);
     l.h = l.xscale + up256((size_t)M * 4);
     l.y = l.h + up256(E * m.f * 2);
-    l.total = l.y + up256(E * m.d * 4);
+    l.xq = l.y + up256(E * m.d * 4);
+    const bool pieces = m.weight_type == CRC_E4M3 && row_tile(M, m.K, m.N) == 64;
+    l.hq = l.xq + (pieces ? up256((size_t)M * 2 * m.d) : 0);
+    l.total = l.hq + (pieces ? up256(E * 2 * m.f) : 0);
     return l;
 }
 
@@ -111,7 +124,8 @@ int launch_experts(const crc_moe& m, const MoeArgs& a, cudaStream_t stream) {
     if (!make_expert_maps(&m13, &m2, m)) return CRC_ECUDA;
     // no more CTAs than items there can be
     const long long experts = (long long)a.M * a.K < a.N ? (long long)a.M * a.K : a.N;
-    const long long items = (experts + (long long)a.M * a.K / NT) * (a.ft + a.dt);
+    const long long items =
+        (experts + (long long)a.M * a.K / NT) * (a.ft + a.dt + 1) + a.M / kSplitTokens + 1;
     cudaLaunchAttribute at[1];
     at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     at[0].val.programmaticStreamSerializationAllowed = 1;
@@ -129,16 +143,6 @@ int launch_experts(const crc_moe& m, const MoeArgs& a, cudaStream_t stream) {
     }
     note_launch();
     return cuda_status(e);
-}
-
-// Rows of a tile: twice an expert's mean share of the choices, so that few experts
-// need a second pass over their weights, or the tokens if that is fewer.
-// Narrow tiles leave room for more row blocks in flight.
-int row_tile(int M, int K, int N) {
-    const int E = M * K;
-    for (int nt = 16; nt < 64; nt *= 2)
-        if (E <= 128 * nt && (M <= nt || 2 * E <= nt * N)) return nt;
-    return 64;
 }
 
 int launch_route(const MoeRouteArgs& r, cudaStream_t stream) {
@@ -235,6 +239,8 @@ int crc_moe_layer(const crc_moe* m, const uint16_t* x_dev, int64_t x_stride, con
     a.s2_stride = m->down_scale_stride / 4;
     a.h = reinterpret_cast<__nv_bfloat16*>(ws + l.h);
     a.y = reinterpret_cast<float*>(ws + l.y);
+    a.xq = ws + l.xq;
+    a.hq = ws + l.hq;
     a.hmax = reinterpret_cast<uint32_t*>(ws + l.hmax);
     a.ctrl = r.ctrl;
     a.err = device_error_word();

@@ -25,7 +25,12 @@
 // 8-bit weights with 16-bit rows: a row is split into two e4m3 pieces of
 // x / s, hi + lo / 16 with s a power of two from the row's largest value, which
 // hold a bf16 value exactly down to 2^-13 of that value; the pieces are two columns of
-// the same product.  So h keeps 16 bits, and no weight is converted.
+// the same product.  So h keeps 16 bits, and no weight is converted.  With tiles of
+// 16 and 32 rows the row warps split on the way into shared memory, for every item
+// anew.  With 64 that is what bounds the kernel (three conversions a pair of
+// elements), so rows are split once, by items of their own before either phase, and
+// the pieces are copied: 200 GPT-OSS-shaped tokens 197 -> 165 us, 1000 Qwen3-shaped 423
+// -> 287 (with tiles of 32 rows, 200 Qwen3-shaped, it costs: 122 -> 128).
 #pragma once
 
 #include <cuda_bf16.h>
@@ -38,9 +43,13 @@ namespace crc {
 constexpr int kMoeThreads = 512;     // warps 0 TMA, 1 MMA, 2-3 idle, 4-7 epilogue, 8-15 rows
 constexpr int kMoeMaxTiles = 256;    // row tiles of NT: N + M K / NT at most, M K <= 128 NT
 constexpr int kItemRing = 4;
-// Control words: the next item; phase-2 warps done; phase-1 warps done, by row tile.
-constexpr int kCtrlNext = 0, kCtrlDone2 = 1, kCtrlDone1 = 2;
-constexpr int kCtrlWords = kCtrlDone1 + kMoeMaxTiles;
+// Control words: the next item; phase-2 warps done; warps done splitting x; phase-1
+// warps done and warps done splitting h, by row tile.
+constexpr int kCtrlNext = 0, kCtrlDone2 = 1, kCtrlXSplit = 2, kCtrlDone1 = 3;
+constexpr int kCtrlHSplit = kCtrlDone1 + kMoeMaxTiles;
+constexpr int kCtrlWords = kCtrlHSplit + kMoeMaxTiles;
+constexpr int kSplitTokens = 16;     // of an item that splits x
+
 
 template <bool W8, int NT>
 struct MoeCfg {
@@ -59,6 +68,7 @@ struct MoeCfg {
         (232448 - 1024 - BAR_BYTES - TABLE_BYTES - SB * B_BYTES) / A_BYTES;
     static constexpr int SMEM = 1024 + BAR_BYTES + TABLE_BYTES + SB * B_BYTES + SA * A_BYTES;
     static constexpr int DEPTH = NT == 16 ? 3 : 1;             // row blocks a thread has in flight
+    static constexpr bool PRE = W8 && NT == 64;                // rows are split by items of their own
     static_assert(SA > SB && SA <= 16, "weight ring");
 };
 
@@ -74,6 +84,7 @@ struct MoeArgs {
     long long s13_stride, s2_stride;
     __nv_bfloat16* h;                // [M K][f], rows by expert
     float* y;                        // [M K][d], rows by choice
+    uint8_t *xq, *hq;                // [M][hi, lo][d], [M K][hi, lo][f]: rows split once
     uint32_t* hmax;                  // [M K] largest magnitude of h's rows, zeroed (8-bit weights)
     uint32_t* ctrl;                  // kCtrlWords, zeroed
     uint32_t* err;
@@ -276,21 +287,33 @@ __device__ __forceinline__ void build_tables(const MoeArgs& a, const MoeShared<W
         __syncthreads();
         return;
     }
-    // Scratch in the weight ring, which is not in use yet: the choices, and for
-    // every expert the set of its tokens as bits with the count of those before
-    // each word.  (An expert is chosen once a token at most.)
+    // Scratch in the weight ring, which is not in use yet: for every expert the set
+    // of its tokens as bits, with the count of those before each word.  (An expert is
+    // chosen once a token at most.)
     const int words = (a.M + 31) / 32;
     uint32_t* set = reinterpret_cast<uint32_t*>(s.a);                  // [128][words]
     uint16_t* before = reinterpret_cast<uint16_t*>(set + 128 * words); // [128][words]
-    uint8_t* ids = reinterpret_cast<uint8_t*>(before + 128 * words);   // [E]
-    static_assert(Cfg::LIST + 128 * 32 * 6 <= Cfg::SA * Cfg::A_BYTES, "scratch");
+    static_assert(128 * 32 * 6 <= Cfg::SA * Cfg::A_BYTES, "scratch");
     for (int i = threadIdx.x; i < 128 * words; i += kMoeThreads) set[i] = 0u;
+    // a thread's choices: four neighbours in each of `quads` words, all asked at once
+    constexpr int QUADS = (Cfg::LIST + 4 * kMoeThreads - 1) / (4 * kMoeThreads);
+    uint32_t ids[QUADS];
+#pragma unroll
+    for (int q = 0; q < QUADS; ++q) {
+        const int i = 4 * (threadIdx.x + q * kMoeThreads);
+        ids[q] = i < E ? __ldcg(reinterpret_cast<const uint32_t*>(a.ids) + i / 4) : 0u;
+    }
     __syncthreads();
-    for (int i = threadIdx.x; i < E; i += kMoeThreads) {
-        const int e = (int)__ldcg(a.ids + i), tok = i / a.K;
-        const bool resident = s.slot[e] >= 0;
-        ids[i] = (uint8_t)(resident ? e : 255);
-        if (resident) atomicOr(&set[e * words + (tok >> 5)], 1u << (tok & 31));
+#pragma unroll
+    for (int q = 0; q < QUADS; ++q) {
+        const int i = 4 * (threadIdx.x + q * kMoeThreads);
+        int tok = i / a.K, k = i - tok * a.K;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int e = (int)(ids[q] >> (8 * j) & 0xffu);
+            if (i + j < E && s.slot[e] >= 0) atomicOr(&set[e * words + (tok >> 5)], 1u << (tok & 31));
+            if (++k == a.K) k = 0, ++tok;
+        }
     }
     __syncthreads();
     if (threadIdx.x < 128) {
@@ -337,11 +360,20 @@ __device__ __forceinline__ void build_tables(const MoeArgs& a, const MoeShared<W
         }
     }
     __syncthreads();
-    for (int i = threadIdx.x; i < E; i += kMoeThreads) {
-        const int e = ids[i], tok = i / a.K;
-        if (e == 255) continue;
-        const int at = e * words + (tok >> 5);
-        s.list[s.start[e] + before[at] + __popc(set[at] & ((1u << (tok & 31)) - 1u))] = (uint16_t)i;
+#pragma unroll
+    for (int q = 0; q < QUADS; ++q) {
+        const int i = 4 * (threadIdx.x + q * kMoeThreads);
+        int tok = i / a.K, k = i - tok * a.K;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int e = (int)(ids[q] >> (8 * j) & 0xffu);
+            if (i + j < E && s.slot[e] >= 0) {
+                const int at = e * words + (tok >> 5);
+                s.list[s.start[e] + before[at] + __popc(set[at] & ((1u << (tok & 31)) - 1u))] =
+                    (uint16_t)(i + j);
+            }
+            if (++k == a.K) k = 0, ++tok;
+        }
     }
     // the ring's stages go from generic reads and writes to TMA
     fence_proxy_async_smem();
@@ -349,18 +381,48 @@ __device__ __forceinline__ void build_tables(const MoeArgs& a, const MoeShared<W
 }
 
 // A work item.
+enum { kGateUp = 0, kDown = 1, kSplitX = 2, kSplitH = 3 };
 struct MoeItem {
-    int phase, tile, j;      // phase 0: 64 elements of f; 1: 128 elements of d
-    int e, row0, rows;
+    int kind, tile, j;       // kGateUp: 64 elements of f; kDown: 128 elements of d;
+    int e, row0, rows;       // kSplitX: tokens from row0 on; kSplitH: the tile's rows
+};
+// First items of the kinds, in the order kSplitX, kGateUp, kSplitH, kDown.
+struct MoeItems {
+    int gate_up, split_h, down, end;
+    template <bool W8, int NT>
+    __device__ __forceinline__ static MoeItems of(const MoeArgs& a, int tiles) {
+        MoeItems n;
+        n.gate_up = MoeCfg<W8, NT>::PRE && a.x_split && tiles ? (a.M + kSplitTokens - 1) / kSplitTokens
+                                                              : 0;
+        n.split_h = n.gate_up + tiles * a.ft;
+        n.down = n.split_h + (MoeCfg<W8, NT>::PRE ? tiles : 0);
+        n.end = n.down + tiles * a.dt;
+        return n;
+    }
 };
 template <bool W8, int NT>
-__device__ __forceinline__ MoeItem moe_item(const MoeArgs& a, const MoeShared<W8, NT>& s, int i) {
+__device__ __forceinline__ MoeItem moe_item(const MoeArgs& a, const MoeShared<W8, NT>& s,
+                                            const MoeItems& n, int i) {
     MoeItem it;
-    const int p1 = s.count[0] * a.ft;
-    it.phase = i >= p1;
-    const int k = it.phase ? i - p1 : i, per = it.phase ? a.dt : a.ft;
-    it.tile = k / per;
-    it.j = k - it.tile * per;
+    it.j = 0;
+    if (i >= n.down) {
+        it.kind = kDown;
+        it.tile = (i - n.down) / a.dt;
+        it.j = i - n.down - it.tile * a.dt;
+    } else if (MoeCfg<W8, NT>::PRE && i >= n.split_h) {
+        it.kind = kSplitH;
+        it.tile = i - n.split_h;
+    } else if (!MoeCfg<W8, NT>::PRE || i >= n.gate_up) {
+        it.kind = kGateUp;
+        it.tile = (i - n.gate_up) / a.ft;
+        it.j = i - n.gate_up - it.tile * a.ft;
+    } else {
+        it.kind = kSplitX;
+        it.tile = it.e = 0;
+        it.row0 = i * kSplitTokens;
+        it.rows = min(kSplitTokens, a.M - it.row0);
+        return it;
+    }
     it.e = s.tile_e[it.tile];
     it.row0 = s.tile_row[it.tile];
     it.rows = s.tile_rows[it.tile];
@@ -394,17 +456,19 @@ struct RowRing {
 
 // A group's row blocks of one item into the ring (four warps).  base: the item's
 // first block, counted over all items.  A thread's unit is 16 bytes of one row's
-// 256: chunk tid % 16 of rows tid / 16, + 8, ...  SPLIT: 16 bf16 elements become 16
-// bytes of hi and of lo.
-template <bool W8, int NT, bool SPLIT>
+// 256: chunk tid % 16 of rows tid / 16, + 8, ...  MODE kCopy: as they are; kSplit: 16 bf16
+// elements become 16 bytes of hi and of lo; kPieces: hi and lo are copied, K bytes
+// apart.
+enum { kCopy = 0, kSplit = 1, kPieces = 2 };
+template <bool W8, int NT, int MODE>
 __device__ __forceinline__ bool produce_rows(const MoeShared<W8, NT>& s, const uint8_t* (&src)[NT / 8],
                                              const float (&inv)[NT / 8], uint32_t have, int n8,
                                              int base, int kb, int K, int tid,
                                              RowRing<W8, NT>& ring) {
     using Cfg = MoeCfg<W8, NT>;
-    constexpr int U = NT / 8, D = Cfg::DEPTH, V = SPLIT ? 2 : 1;
-    constexpr int STEP = SPLIT ? 2 * 256 : 256;                // bytes of a row's block
-    constexpr int CE = SPLIT || W8 ? 16 : 8;                   // elements of a unit
+    constexpr int U = NT / 8, D = Cfg::DEPTH, V = MODE == kCopy ? 1 : 2;
+    constexpr int STEP = MODE == kSplit ? 2 * 256 : 256;       // bytes of a row's block
+    constexpr int CE = W8 ? 16 : 8;                            // elements of a unit
     const int chunk = tid & 15, lane = tid & 31;
     uint4 v[D][U][V];
     auto load = [&](int k, uint4 (&r)[U][V]) {
@@ -414,7 +478,8 @@ __device__ __forceinline__ bool produce_rows(const MoeShared<W8, NT>& s, const u
 #pragma unroll
             for (int q = 0; q < V; ++q)
                 r[u][q] = in && (have >> u & 1u)
-                              ? __ldcg(reinterpret_cast<const uint4*>(src[u] + (size_t)k * STEP) + q)
+                              ? __ldcg(reinterpret_cast<const uint4*>(
+                                    src[u] + (size_t)k * STEP + q * (MODE == kPieces ? K : 16)))
                               : make_uint4(0, 0, 0, 0);
     };
     const int first = ring.next - base;
@@ -432,9 +497,9 @@ __device__ __forceinline__ bool produce_rows(const MoeShared<W8, NT>& s, const u
             for (int u = 0; u < U; ++u) {
                 if (!(have >> u & 1u)) continue;
                 const int row = (tid >> 4) + 8 * u;
-                if constexpr (SPLIT) {
-                    uint4 hi, lo;
-                    split16(v[i][u], inv[u], hi, lo);
+                if constexpr (MODE != kCopy) {
+                    uint4 hi = v[i][u][0], lo = v[i][u][V - 1];
+                    if constexpr (MODE == kSplit) split16(v[i][u], inv[u], hi, lo);
                     const int low = n8 + row;
                     *reinterpret_cast<uint4*>(dst + row * 128 + (((chunk ^ row) & 7) << 4)) = hi;
                     *reinterpret_cast<uint4*>(dst + low * 128 + (((chunk ^ low) & 7) << 4)) = lo;
@@ -451,6 +516,24 @@ __device__ __forceinline__ bool produce_rows(const MoeShared<W8, NT>& s, const u
         }
     }
     return true;
+}
+
+// n elements (a multiple of 16) of `rows` bf16 rows into two pieces: a thread a chunk of
+// 16.  src(r), inv(r): row r and 1 / its scale; dst: rows of hi and lo, n bytes each.
+template <class Src, class Inv>
+__device__ __forceinline__ void split_rows(int rows, int n, int thread, int threads, Src src, Inv inv,
+                                           uint8_t* dst) {
+    const int chunks = n / 16;
+    for (int i = thread; i < rows * chunks; i += threads) {
+        const int r = i / chunks, c = i - r * chunks;
+        const uint4* at = reinterpret_cast<const uint4*>(src(r)) + 2 * c;
+        const uint4 v[2] = {__ldcg(at), __ldcg(at + 1)};
+        uint4 hi, lo;
+        split16(v, inv(r), hi, lo);
+        uint8_t* to = dst + (size_t)r * 2 * n + 16 * c;
+        *reinterpret_cast<uint4*>(to) = hi;
+        *reinterpret_cast<uint4*>(to + n) = lo;
+    }
 }
 
 // Gates of up to eight choices from r on; a bit for each whose expert has a slot.
@@ -520,7 +603,7 @@ __global__ void __launch_bounds__(kMoeThreads, 1)
     if (threadIdx.x == 0) next = (int)atomicAdd(&a.ctrl[kCtrlNext], 1u);
     build_tables<W8, NT>(a, s);
     const int tiles = s.count[0];
-    const int total = tiles * (a.ft + a.dt);
+    const MoeItems items = MoeItems::of<W8, NT>(a, tiles);
 
     if (warp == 0) {
         // ------------------------------------------------------ weights by TMA
@@ -530,7 +613,7 @@ __global__ void __launch_bounds__(kMoeThreads, 1)
             uint32_t phase = 0, iphase = 0;
             bool failed = false;
             while (!failed) {
-                const int item = next < total ? next : -1;
+                const int item = next < items.end ? next : -1;
                 if (!mbar_wait(&s.i_empty[islot], iphase ^ 1)) {
                     failed = true;
                     break;
@@ -542,12 +625,16 @@ __global__ void __launch_bounds__(kMoeThreads, 1)
                     iphase ^= 1;
                 }
                 if (item < 0) break;
-                const MoeItem it = moe_item<W8, NT>(a, s, item);
+                const MoeItem it = moe_item<W8, NT>(a, s, items, item);
+                if (it.kind >= kSplitX) {
+                    next = (int)atomicAdd(&a.ctrl[kCtrlNext], 1u);
+                    continue;
+                }
                 const int slot = s.slot[it.e];
                 // an expert with several row tiles (all but the last are full) is
                 // read again, from L2
                 const uint64_t pol = it.rows == NT ? again : once;
-                const int kb = it.phase ? a.kb2 : a.kb1;
+                const int kb = it.kind == kDown ? a.kb2 : a.kb1;
                 const int first = stage;
                 const uint32_t first_phase = phase;
                 for (int k = 0; k < kb; ++k) {
@@ -560,7 +647,7 @@ __global__ void __launch_bounds__(kMoeThreads, 1)
 #pragma unroll
                     for (int half = 0; half < 2; ++half) {     // past the row's end: zeros
                         const int x = k * Cfg::BK + half * (Cfg::BK / 2);
-                        if (it.phase == 0)
+                        if (it.kind == kGateUp)
                             tma_load_5d(dst + half * Cfg::A_HALF, &map13, &s.a_full[stage], x, 0, 0,
                                         it.j * 4, slot, pol);
                         else
@@ -599,7 +686,7 @@ __global__ void __launch_bounds__(kMoeThreads, 1)
         // issues: descriptors then live in uniform registers.
         const uint32_t lead = elect_lane();
         const uint64_t a0 = sw128_kmajor_desc(smem_u32(s.a)), b0 = sw128_kmajor_desc(smem_u32(s.b));
-        const int p1 = __reduce_max_sync(kFull, tiles * a.ft);
+        const MoeItems my = MoeItems::of<W8, NT>(a, __reduce_max_sync(kFull, tiles));
         int stage = 0, bstage = 0, islot = 0, acc = 0;
         uint32_t phase = 0, bphase = 0, iphase = 0, aphase = 0;
         bool failed = false;
@@ -615,8 +702,9 @@ __global__ void __launch_bounds__(kMoeThreads, 1)
                 iphase ^= 1;
             }
             if (item < 0) break;
-            const bool second = item >= p1;
-            const int rows = __reduce_max_sync(kFull, moe_item<W8, NT>(a, s, item).rows);
+            if (Cfg::PRE && (item < my.gate_up || (item >= my.split_h && item < my.down))) continue;
+            const bool second = item >= my.down;
+            const int rows = __reduce_max_sync(kFull, moe_item<W8, NT>(a, s, my, item).rows);
             const bool split = W8 && (second || a.x_split);
             const int n = split ? 2 * ((rows + 7) & ~7) : (rows + 15) & ~15;
             const uint32_t idesc = W8 ? idesc_e4m3_f32(128, n) : idesc_bf16_f32(128, n);
@@ -681,17 +769,46 @@ __global__ void __launch_bounds__(kMoeThreads, 1)
                 iphase ^= 1;
             }
             if (item < 0) break;
-            const MoeItem it = moe_item<W8, NT>(a, s, item);
-            if (it.phase) {           // h of the whole tile, from all its items
+            const MoeItem it = moe_item<W8, NT>(a, s, items, item);
+            // what the item reads: x in pieces, h of the whole tile, h in pieces
+            const bool x_pieces = Cfg::PRE && a.x_split && it.kind == kGateUp;
+            if (x_pieces || it.kind == kSplitH || it.kind == kDown) {
+                const uint32_t* at = &a.ctrl[x_pieces ? kCtrlXSplit
+                                             : Cfg::PRE && it.kind == kDown ? kCtrlHSplit + it.tile
+                                                                            : kCtrlDone1 + it.tile];
+                const uint32_t n = x_pieces ? 8u * items.gate_up
+                                   : Cfg::PRE && it.kind == kDown ? 8u : 4u * a.ft;
                 bool ok = true;
-                if (lane == 0) ok = wait_count(&a.ctrl[kCtrlDone1 + it.tile], 4u * a.ft);
+                if (lane == 0) ok = wait_count(at, n);
                 if (!__shfl_sync(kFull, (int)ok, 0)) {
                     failed = true;
                     break;
                 }
                 __syncwarp();         // lane 0's acquire orders the whole warp's loads
             }
-            const bool split = W8 && (it.phase || a.x_split);
+            if (Cfg::PRE && it.kind >= kSplitX) {
+                const int t = threadIdx.x - 256;
+                if (it.kind == kSplitX)
+                    split_rows(it.rows, a.d, t, 256, [&](int r) { return a.x + (it.row0 + r) * a.x_bytes; },
+                               [&](int r) { return 1.f / __ldcg(a.xs + it.row0 + r); },
+                               a.xq + (size_t)it.row0 * 2 * a.d);
+                else
+                    split_rows(it.rows, a.f, t, 256,
+                               [&](int r) { return a.h + (size_t)(it.row0 + r) * a.f; },
+                               [&](int r) {
+                                   return 1.f / split_scale(__uint_as_float(
+                                                    __ldcg(a.hmax + it.row0 + r)));
+                               },
+                               a.hq + (size_t)it.row0 * 2 * a.f);
+                __syncwarp();
+                if (lane == 0) {
+                    __threadfence();
+                    atomicAdd(&a.ctrl[it.kind == kSplitX ? kCtrlXSplit : kCtrlHSplit + it.tile], 1u);
+                }
+                continue;
+            }
+            const bool down = it.kind == kDown;
+            const bool split = W8 && (down || a.x_split);
             const int n8 = (it.rows + 7) & ~7;
             const uint8_t* src[NT / 8];
             float inv[NT / 8];
@@ -703,28 +820,30 @@ __global__ void __launch_bounds__(kMoeThreads, 1)
                 inv[u] = 1.f;
                 if (r >= it.rows) continue;
                 have |= 1u << u;
-                if (it.phase) {
-                    src[u] = reinterpret_cast<const uint8_t*>(a.h + (size_t)(it.row0 + r) * a.f);
+                if (down) {
+                    const size_t row = (size_t)(it.row0 + r);
+                    src[u] = Cfg::PRE ? a.hq + row * 2 * a.f
+                                      : reinterpret_cast<const uint8_t*>(a.h + row * a.f);
                     if (W8) {
-                        const float hs =
-                            split_scale(__uint_as_float(__ldcg(a.hmax + it.row0 + r)));
+                        const float hs = split_scale(__uint_as_float(__ldcg(a.hmax + row)));
                         inv[u] = 1.f / hs;
                         // for the epilogue, from the group whose block is the item's first
                         if (ring.next == base && (tid & 15) == 0) s.hscale[ring_slot * NT + r] = hs;
                     }
                 } else {
                     const int tok = s.list[it.row0 + r] / a.K;
-                    src[u] = a.x + tok * a.x_bytes;
-                    if (W8 && split) inv[u] = 1.f / __ldcg(a.xs + tok);
+                    src[u] = x_pieces ? a.xq + (size_t)tok * 2 * a.d : a.x + tok * a.x_bytes;
+                    if (W8 && !Cfg::PRE && split) inv[u] = 1.f / __ldcg(a.xs + tok);
                 }
-                src[u] += (tid & 15) * (split ? 32 : 16);
+                src[u] += (tid & 15) * (split && !Cfg::PRE ? 32 : 16);
             }
-            const int kb = it.phase ? a.kb2 : a.kb1, K = it.phase ? a.f : a.d;
+            const int kb = down ? a.kb2 : a.kb1, K = down ? a.f : a.d;
             bool ok;
             if (W8 && split)
-                ok = produce_rows<W8, NT, W8>(s, src, inv, have, n8, base, kb, K, tid, ring);
+                ok = produce_rows<W8, NT, !W8 ? kCopy : Cfg::PRE ? kPieces : kSplit>(
+                    s, src, inv, have, n8, base, kb, K, tid, ring);
             else
-                ok = produce_rows<W8, NT, false>(s, src, inv, have, n8, base, kb, K, tid, ring);
+                ok = produce_rows<W8, NT, kCopy>(s, src, inv, have, n8, base, kb, K, tid, ring);
             if (!ok) {
                 failed = true;
                 break;
@@ -745,23 +864,33 @@ __global__ void __launch_bounds__(kMoeThreads, 1)
             }
             const int item = s.items[islot];
             if (item < 0) break;
-            const MoeItem it = moe_item<W8, NT>(a, s, item);
+            const MoeItem it = moe_item<W8, NT>(a, s, items, item);
+            if (Cfg::PRE && it.kind >= kSplitX) {
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&s.i_empty[islot]);
+                if (++islot == kItemRing) {
+                    islot = 0;
+                    iphase ^= 1;
+                }
+                continue;
+            }
+            const bool down = it.kind == kDown;
             const int slot = s.slot[it.e];
-            const bool split = W8 && (it.phase || a.x_split);
+            const bool split = W8 && (down || a.x_split);
             const int n8 = (it.rows + 7) & ~7;
             // this lane's weight row: an element of f (gate in the low half of the
             // warp, up in the high half), or of d
-            const int wrow = it.phase ? it.j * 128 + quarter * 32 + lane
+            const int wrow = down ? it.j * 128 + quarter * 32 + lane
                                       : it.j * 64 + quarter * 16 + (lane & 15);
-            const bool in = wrow < (it.phase ? a.d : a.f);
+            const bool in = wrow < (down ? a.d : a.f);
             float sw = 1.f;
             if (W8 && in)
-                sw = it.phase ? a.s2[slot * a.s2_stride + wrow]
+                sw = down ? a.s2[slot * a.s2_stride + wrow]
                               : a.s13[slot * a.s13_stride + (lane >> 4) * a.f + wrow];
             // scales of the rows: lane l holds those of rows l, l + 32
             constexpr int RS = (NT + 31) / 32;
             float rs[RS];
-            if (W8 && it.phase == 0) {
+            if (W8 && !down) {
 #pragma unroll
                 for (int u = 0; u < RS; ++u) {
                     const int r = lane + 32 * u;
@@ -773,7 +902,7 @@ __global__ void __launch_bounds__(kMoeThreads, 1)
                 break;
             }
             tc_fence_after();
-            if (W8 && it.phase) {
+            if (W8 && down) {
 #pragma unroll
                 for (int u = 0; u < RS; ++u) {
                     const int r = lane + 32 * u;
@@ -816,7 +945,7 @@ __global__ void __launch_bounds__(kMoeThreads, 1)
                     for (int c = 0; c < 16; ++c)
                         v[c] *= sw * __shfl_sync(kFull, r, (c0 & 16) + c);
                 }
-                if (it.phase == 0) {
+                if (!down) {
                     uint32_t top[8] = {};
 #pragma unroll
                     for (int c = 0; c < 16; c += 2) {
@@ -863,7 +992,7 @@ __global__ void __launch_bounds__(kMoeThreads, 1)
             __syncwarp();
             if (lane == 0) {
                 __threadfence();
-                atomicAdd(&a.ctrl[it.phase ? kCtrlDone2 : kCtrlDone1 + it.tile], 1u);
+                atomicAdd(&a.ctrl[down ? kCtrlDone2 : kCtrlDone1 + it.tile], 1u);
             }
         }
         if (failed && lane == 0) latch_error(a.err, CRC_ETIMEOUT);
