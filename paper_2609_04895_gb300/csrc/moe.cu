@@ -31,7 +31,7 @@ int row_tile(int M, int K, int N) {
 }
 
 struct MoeLayout {
-    size_t ctrl, hmax, ids, gates, xscale, h, y, xq, hq, total;     // hmax right behind ctrl
+    size_t ctrl, hmax, logits, ids, gates, xscale, h, y, xq, hq, total;     // hmax right behind ctrl
 };
 
 MoeLayout moe_layout(const crc_moe& m, int M) {
@@ -39,7 +39,8 @@ MoeLayout moe_layout(const crc_moe& m, int M) {
     MoeLayout l;
     l.ctrl = 0;
     l.hmax = kCtrlWords * 4;
-    l.ids = up256(l.hmax + E * 4);
+    l.logits = up256(l.hmax + E * 4);
+    l.ids = l.logits + (few_choices(M, m.K) ? up256((size_t)M * m.N * 4) : 0);
     l.gates = l.ids + up256(E);
     l.xscale = l.gates + up256(E * 4);
     l.h = l.xscale + up256((size_t)M * 4);
@@ -151,7 +152,10 @@ int launch_route(const MoeRouteArgs& r, cudaStream_t stream) {
     c.stream = stream;
     cudaError_t e;
     ProfScope prof(CRC_KERNEL_MOE_ROUTE, stream);
-    if (r.scores) {
+    if (r.logits) {
+        c.gridDim = dim3((unsigned)((r.N + 7) / 8), (unsigned)r.M);
+        e = cudaLaunchKernelEx(&c, moe_logits_kernel, r);
+    } else if (r.scores) {
         c.gridDim = dim3((unsigned)((r.M + 7) / 8));
         e = cudaLaunchKernelEx(&c, moe_topk_kernel, r);
     } else {
@@ -216,6 +220,7 @@ int crc_moe_layer(const crc_moe* m, const uint16_t* x_dev, int64_t x_stride, con
     r.K = m->K;
     r.d = m->d;
     r.renorm = m->renormalize;
+    r.logits = few_choices(M, m->K) && !scores_dev ? reinterpret_cast<float*>(ws + l.logits) : nullptr;
     r.ids = ws + l.ids;
     r.gates = reinterpret_cast<float*>(ws + l.gates);
     r.ids_out = topk_dev;
@@ -232,6 +237,10 @@ int crc_moe_layer(const crc_moe* m, const uint16_t* x_dev, int64_t x_stride, con
     a.x_split = w8 && !x8_dev;
     a.ids = r.ids;
     a.gates = r.gates;
+    a.logits = r.logits;
+    a.ids_out = topk_dev;
+    a.gates_out = gates_dev;
+    a.renorm = m->renormalize;
     a.expert_slot = m->expert_slot_dev;
     a.s13 = m->gate_up_scale_dev;
     a.s2 = m->down_scale_dev;

@@ -49,6 +49,11 @@ constexpr int kCtrlNext = 0, kCtrlDone2 = 1, kCtrlXSplit = 2, kCtrlDone1 = 3;
 constexpr int kCtrlHSplit = kCtrlDone1 + kMoeMaxTiles;
 constexpr int kCtrlWords = kCtrlHSplit + kMoeMaxTiles;
 constexpr int kSplitTokens = 16;     // of an item that splits x
+// Choices of which a warp has one a lane, of tokens of which each warp has one at most.
+constexpr int kFewChoices = 32, kFewTokens = 16;
+__host__ __device__ inline bool few_choices(int M, int K) {
+    return M * K <= kFewChoices && M <= kFewTokens;
+}
 
 
 template <bool W8, int NT>
@@ -62,7 +67,7 @@ struct MoeCfg {
     static constexpr int LIST = 128 * NT;                      // choices (M K) at most
     static constexpr int TMEM_COLS = 2 * (COLS < 16 ? 16 : COLS) < 32 ? 32 : 2 * COLS;
     static constexpr int TABLE_BYTES = 3 * 128 * 4 + 3 * kMoeMaxTiles * 2 + LIST * 2 +
-                                       kItemRing * NT * 4 + 64;
+                                       kItemRing * NT * 4 + kFewChoices * 5 + 64;
     static constexpr int BAR_BYTES = 512;
     static constexpr int SA =
         (232448 - 1024 - BAR_BYTES - TABLE_BYTES - SB * B_BYTES) / A_BYTES;
@@ -79,6 +84,10 @@ struct MoeArgs {
     int x_split;                     // 8-bit weights: x is bf16 and goes in two pieces
     const uint8_t* ids;              // [M][K]
     const float* gates;              // [M][K]
+    const float* logits;             // [M][N], few choices: ids and gates are taken here
+    uint8_t* ids_out;                // then the caller's, or null
+    float* gates_out;
+    int renorm;
     const int32_t* expert_slot;      // [N] or null
     const float *s13, *s2;           // scales of 8-bit weight rows, slots s13_stride floats apart
     long long s13_stride, s2_stride;
@@ -153,6 +162,10 @@ __device__ __forceinline__ uint64_t l2_evict_normal_policy() {
     return p;
 }
 
+// One more, behind this warp's writes (after a __syncwarp).
+__device__ __forceinline__ void add_release(uint32_t* p) {
+    asm volatile("red.release.gpu.global.add.u32 [%0], 1;" ::"l"(p) : "memory");
+}
 __device__ __forceinline__ uint32_t ld_acquire(const uint32_t* p) {
     uint32_t v;
     asm volatile("ld.acquire.gpu.global.u32 %0, [%1];" : "=r"(v) : "l"(p) : "memory");
@@ -211,6 +224,8 @@ struct MoeShared {
     uint32_t* tmem_slot;
     int* items;
     float* hscale;         // [kItemRing][NT] scales of h's rows (8-bit weights)
+    float* few_gates;      // [kFewChoices]
+    uint8_t* few_ids;      // [kFewChoices]
     int* slot;             // [128] slot of each expert, -1 without
     int* start;            // [128] first row of each expert
     int* count;            // [128] rows of each expert, then [0] = row tiles
@@ -242,6 +257,8 @@ struct MoeShared {
         tile_rows = tile_row + kMoeMaxTiles;
         list = tile_rows + kMoeMaxTiles;
         hscale = reinterpret_cast<float*>(list + Cfg::LIST);
+        few_gates = hscale + kItemRing * NT;
+        few_ids = reinterpret_cast<uint8_t*>(few_gates + kFewChoices);
     }
 };
 
@@ -253,7 +270,8 @@ struct MoeShared {
 template <bool W8, int NT>
 __device__ __forceinline__ void build_small_tables(const MoeArgs& a, const MoeShared<W8, NT>& s) {
     const int lane = threadIdx.x & 31, E = a.M * a.K;
-    int e = lane < E ? (int)__ldcg(a.ids + lane) : 128;
+    int e = 128;
+    if (lane < E) e = a.logits ? s.few_ids[lane] : __ldcg(a.ids + lane);
     if (e < 128 && s.slot[e] < 0) e = 128;
     const uint32_t peers = __match_any_sync(kFull, e);
     const bool lead = e < 128 && lane == __ffs(peers) - 1;
@@ -282,7 +300,23 @@ __device__ __forceinline__ void build_tables(const MoeArgs& a, const MoeShared<W
     using Cfg = MoeCfg<W8, NT>;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int E = a.M * a.K;
-    if (E <= 32 && a.M <= NT) {
+    if (few_choices(a.M, a.K)) {
+        if (a.logits) {               // Top-K and gates, a warp a token
+            if (warp < a.M) {
+                float v[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int e = lane + 32 * i;
+                    v[i] = e < a.N ? __ldcg(a.logits + warp * a.N + e) : 0.f;
+                }
+                const int r = warp * a.K;
+                const bool out = blockIdx.x == 0;
+                route_token(v, a.N, a.K, false, a.renorm, lane, s.few_ids + r, s.few_gates + r,
+                            out && a.ids_out ? a.ids_out + r : nullptr,
+                            out && a.gates_out ? a.gates_out + r : nullptr);
+            }
+            __syncthreads();
+        }
         if (warp == 0) build_small_tables<W8, NT>(a, s);
         __syncthreads();
         return;
@@ -540,17 +574,21 @@ __device__ __forceinline__ void split_rows(int rows, int n, int thread, int thre
 struct Gates {
     float g[8];
     uint32_t have;
-    __device__ __forceinline__ void load(const MoeArgs& a, const int* slot, int r, int n) {
+    template <class Shared>
+    __device__ __forceinline__ void load(const MoeArgs& a, const Shared& s, int r, int n) {
         have = 0;
         int id[8];
 #pragma unroll
         for (int k = 0; k < 8; ++k) {
-            id[k] = k < n ? (int)__ldcg(a.ids + r + k) : 0;
-            g[k] = k < n ? __ldcg(a.gates + r + k) : 0.f;
+            id[k] = 0;
+            g[k] = 0.f;
+            if (k >= n) continue;
+            id[k] = a.logits ? s.few_ids[r + k] : __ldcg(a.ids + r + k);
+            g[k] = a.logits ? s.few_gates[r + k] : __ldcg(a.gates + r + k);
         }
 #pragma unroll
         for (int k = 0; k < 8; ++k)
-            if (k < n && slot[id[k]] >= 0) have |= 1u << k;
+            if (k < n && s.slot[id[k]] >= 0) have |= 1u << k;
     }
 };
 
@@ -801,10 +839,8 @@ __global__ void __launch_bounds__(kMoeThreads, 1)
                                },
                                a.hq + (size_t)it.row0 * 2 * a.f);
                 __syncwarp();
-                if (lane == 0) {
-                    __threadfence();
-                    atomicAdd(&a.ctrl[it.kind == kSplitX ? kCtrlXSplit : kCtrlHSplit + it.tile], 1u);
-                }
+                if (lane == 0)
+                    add_release(&a.ctrl[it.kind == kSplitX ? kCtrlXSplit : kCtrlHSplit + it.tile]);
                 continue;
             }
             const bool down = it.kind == kDown;
@@ -990,10 +1026,7 @@ __global__ void __launch_bounds__(kMoeThreads, 1)
             acc ^= 1;
             if (acc == 0) aphase ^= 1;
             __syncwarp();
-            if (lane == 0) {
-                __threadfence();
-                atomicAdd(&a.ctrl[down ? kCtrlDone2 : kCtrlDone1 + it.tile], 1u);
-            }
+            if (lane == 0) add_release(&a.ctrl[down ? kCtrlDone2 : kCtrlDone1 + it.tile]);
         }
         if (failed && lane == 0) latch_error(a.err, CRC_ETIMEOUT);
     }
@@ -1013,7 +1046,7 @@ __global__ void __launch_bounds__(kMoeThreads, 1)
     long long i = (long long)blockIdx.x * kMoeThreads + threadIdx.x;
     int tok = i < all ? (int)(i / quads) : 0;
     Gates gates;
-    if (i < all) gates.load(a, s.slot, tok * a.K, a.K);
+    if (i < all) gates.load(a, s, tok * a.K, a.K);
     if (threadIdx.x == 0) {
         const bool ok = wait_count(&a.ctrl[kCtrlDone2], 4u * (uint32_t)(tiles * a.dt));
         if (!ok) latch_error(a.err, CRC_ETIMEOUT);
@@ -1026,7 +1059,7 @@ __global__ void __launch_bounds__(kMoeThreads, 1)
         float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
         for (int k0 = 0; k0 < a.K; k0 += 8) {
             const int r = tok * a.K + k0;
-            if (k0) gates.load(a, s.slot, r, a.K - k0);
+            if (k0) gates.load(a, s, r, a.K - k0);
             float4 y[8];
 #pragma unroll
             for (int k = 0; k < 8; ++k)
@@ -1050,7 +1083,7 @@ __global__ void __launch_bounds__(kMoeThreads, 1)
         i += (long long)gridDim.x * kMoeThreads;
         if (i >= all) break;
         tok = (int)(i / quads);
-        gates.load(a, s.slot, tok * a.K, a.K);
+        gates.load(a, s, tok * a.K, a.K);
     }
 }
 
