@@ -132,6 +132,19 @@ __device__ __forceinline__ void umma(uint32_t d_tmem, uint64_t adesc, uint64_t b
             "l"(adesc), "l"(bdesc), "r"(idesc), "r"(accumulate), "r"(lead)
             : "memory");
 }
+// Whether the phase of that parity has completed, without waiting (try_wait may
+// suspend the thread).
+__device__ __forceinline__ bool mbar_test(uint64_t* bar, uint32_t parity) {
+    uint32_t ok;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+        "selp.u32 %0, 1, 0, p;\n\t}\n"
+        : "=r"(ok)
+        : "r"(smem_u32(bar)), "r"(parity)
+        : "memory");
+    return ok != 0;
+}
 __device__ __forceinline__ void umma_commit_by(uint64_t* bar, uint32_t lead) {
     asm volatile(
         "{\n\t.reg .pred e;\n\t"
@@ -753,22 +766,20 @@ __global__ void __launch_bounds__(kMoeThreads, 1)
             tc_fence_after();
             const uint32_t dt = tmem + (uint32_t)(acc * Cfg::COLS);
             const int kb = second ? a.kb2 : a.kb1;
+            bool there = false;
             for (int k = 0; k < kb; ++k) {
-                const bool ok = mbar_wait(&s.b_full[bstage], bphase) &&
-                                mbar_wait(&s.a_full[stage], phase);
-                if (__any_sync(kFull, !ok)) {
-                    failed = true;
-                    break;
+                if (!there) {
+                    const bool ok = mbar_wait(&s.b_full[bstage], bphase) &&
+                                    mbar_wait(&s.a_full[stage], phase);
+                    if (__any_sync(kFull, !ok)) {
+                        failed = true;
+                        break;
+                    }
                 }
                 tc_fence_after();
                 const uint64_t ad = a0 + (uint64_t)(stage * (Cfg::A_BYTES >> 4));
                 const uint64_t bd = b0 + (uint64_t)(bstage * (Cfg::B_BYTES >> 4));
-#pragma unroll
-                for (int q = 0; q < 8; ++q)             // 32 bytes of K a step
-                    umma<W8>(dt, ad + (q >> 2) * (Cfg::A_HALF >> 4) + 2 * (q & 3),
-                             bd + (q >> 2) * (Cfg::B_HALF >> 4) + 2 * (q & 3), idesc, (k | q) != 0,
-                             lead);
-                umma_commit_by(&s.a_empty[stage], lead);
+                uint64_t* free = &s.a_empty[stage];
                 if (++stage == Cfg::SA) {
                     stage = 0;
                     phase ^= 1;
@@ -777,6 +788,17 @@ __global__ void __launch_bounds__(kMoeThreads, 1)
                     bstage = 0;
                     bphase ^= 1;
                 }
+                // the next block is asked for before this one's MMAs: the answer takes as
+                // long as they do
+                const bool next = mbar_test(&s.b_full[bstage], bphase) &
+                                  mbar_test(&s.a_full[stage], phase) & (k + 1 < kb);
+#pragma unroll
+                for (int q = 0; q < 8; ++q)             // 32 bytes of K a step
+                    umma<W8>(dt, ad + (q >> 2) * (Cfg::A_HALF >> 4) + 2 * (q & 3),
+                             bd + (q >> 2) * (Cfg::B_HALF >> 4) + 2 * (q & 3), idesc, (k | q) != 0,
+                             lead);
+                umma_commit_by(free, lead);
+                there = __all_sync(kFull, next);
             }
             if (failed) break;
             umma_commit_by(&s.t_full[acc], lead);
