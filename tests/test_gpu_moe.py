@@ -176,6 +176,57 @@ def test_layer_matches_its_definition(P, size, kind):
     assert P.crc.crc_device_error() == 0
 
 
+@pytest.mark.parametrize("size", [
+    (32, 2, 64, 48, 16),            # as many choices as one warp has lanes
+    (32, 1, 64, 48, 16),
+    (32, 1, 64, 48, 17),            # more tokens than warps
+    (32, 1, 64, 48, 32),
+    (32, 4, 64, 48, 9),             # one choice more than lanes and some
+    (128, 32, 128, 64, 1),
+    (96, 3, 4104, 80, 3),           # more than one batch of loads a row
+    (112, 7, 328, 64, 40),
+    (64, 6, 448, 208, 100),         # tiles of 32 rows
+], ids=str)
+@pytest.mark.parametrize("kind", ["bf16", "w8", "w8x8"])
+def test_sizes_around_the_rules(P, size, kind):
+    N, K, d, f, M = size
+    if kind != "bf16":
+        d = d // 16 * 16
+    c = Case(P, N, K, d, f, M, w8=kind != "bf16", x8=kind == "w8x8", seed=7 * N + M)
+    check(c, *c.run())
+    # the same tokens from given probabilities
+    pr = torch.softmax(c.x.float() @ c.router.float().t(), -1)
+    check(c, *c.run(scores=pr), z=pr.double(), probs=True)
+    assert P.crc.crc_device_error() == 0
+
+
+@pytest.mark.parametrize("kind", ["bf16", "w8", "w8x8"])
+@pytest.mark.parametrize("M", [40, 100, 300])
+def test_every_token_takes_the_same_experts(P, kind, M):
+    """Many row tiles an expert, whatever the tile that the mean calls for."""
+    c = Case(P, 64, 3, 256, 96, M, w8=kind != "bf16", seed=M)
+    common = torch.randn(256, device="cuda", generator=torch.Generator("cuda").manual_seed(1))
+    c.x = (c.x.float() * 0.25 + common).to(torch.bfloat16)
+    c.router[:3] += (common * 0.1).to(torch.bfloat16)
+    if kind == "w8x8":
+        c.x8, c.xs = bits8(c.x)
+    out, topk, gates = c.run()
+    assert (topk.long().sort(-1).values == torch.arange(3, device="cuda")).all()
+    check(c, out, topk, gates)
+
+
+@pytest.mark.parametrize("kind", ["bf16", "w8", "w8x8"])
+@pytest.mark.parametrize("M", [1, 3])
+def test_few_choices_without_a_slot(P, kind, M):
+    c = Case(P, 64, 8, 256, 96, M, w8=kind != "bf16", x8=kind == "w8x8", slots=16, seed=M)
+    check(c, *c.run())
+    c.slot.fill_(-1)
+    out = torch.full((M, 256), float("nan"), dtype=torch.bfloat16, device="cuda")
+    _, topk, gates = c.run(out=out)
+    assert (out == 0).all()
+    check_routing(c, topk, gates)
+
+
 def test_smallest_hidden_size(P):
     c = Case(P, 16, 2, 8, 16, 3)
     check(c, *c.run())
@@ -301,8 +352,9 @@ def test_same_bits_every_time_and_on_another_stream(P, kind):
             assert torch.equal(a, b)
 
 
-def test_captured_in_a_graph(P):
-    c = Case(P, 64, 4, 256, 128, 9)
+@pytest.mark.parametrize("M,w8", [(2, False), (9, False), (9, True), (70, True)])
+def test_captured_in_a_graph(P, M, w8):
+    c = Case(P, 64, 4, 256, 128, M, w8=w8)
     ref, _, _ = c.run()
     ref = ref.clone()
     ws = torch.empty(c.layer.workspace_bytes(c.M), dtype=torch.uint8, device="cuda")
