@@ -547,8 +547,10 @@ typedef struct crc_moe {
  *   gates_dev  fp32 [M][K], g in rank order, or NULL
  *   workspace_dev  crc_moe_workspace_bytes(m, M) bytes, 256-byte aligned; calls
  *              that may overlap on the GPU need one each
- * Products are summed in fp32; the product of silu and up is rounded to bf16 (as
- * wide as x) for the second product, the K experts are summed in fp32 in rank
+ * Two kernels.  Products are summed in fp32; the product of silu and up enters the
+ * second product in two pieces (bf16 weights: 16 significant bits of it; e4m3: two
+ * e4m3 pieces, 6e-4 off), as does a bf16 x with e4m3 weights (exact down to 2^-13 of
+ * the row's largest value); the K experts are summed in fp32 in rank
  * order and out is rounded once.  Results do not depend on the order in which
  * blocks run.  M = 0 is a no-op. */
 size_t crc_moe_workspace_bytes(const crc_moe *m, int32_t M);

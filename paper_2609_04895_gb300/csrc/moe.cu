@@ -44,9 +44,9 @@ MoeLayout moe_layout(const crc_moe& m, int M) {
     l.gates = l.ids + up256(E);
     l.xscale = l.gates + up256(E * 4);
     l.h = l.xscale + up256((size_t)M * 4);
-    l.y = l.h + up256(E * m.f * 2);
+    l.y = l.h + up256(E * m.f * 4);
     l.xq = l.y + up256(E * m.d * 4);
-    const bool pieces = m.weight_type == CRC_E4M3 && row_tile(M, m.K, m.N) == 64;
+    const bool pieces = m.weight_type == CRC_E4M3 && row_tile(M, m.K, m.N) > 16;
     l.hq = l.xq + (pieces ? up256((size_t)M * 2 * m.d) : 0);
     l.total = l.hq + (pieces ? up256(E * 2 * m.f) : 0);
     return l;
@@ -246,7 +246,7 @@ int crc_moe_layer(const crc_moe* m, const uint16_t* x_dev, int64_t x_stride, con
     a.s2 = m->down_scale_dev;
     a.s13_stride = m->gate_up_scale_stride / 4;
     a.s2_stride = m->down_scale_stride / 4;
-    a.h = reinterpret_cast<__nv_bfloat16*>(ws + l.h);
+    a.h = reinterpret_cast<float*>(ws + l.h);
     a.y = reinterpret_cast<float*>(ws + l.y);
     a.xq = ws + l.xq;
     a.hq = ws + l.hq;

@@ -22,15 +22,16 @@
 //      weights are on their way meanwhile), y goes to the workspace in fp32;
 //   then all CTAs add up the choices of their share of the tokens, in rank order.
 //
-// 8-bit weights with 16-bit rows: a row is split into two e4m3 pieces of
-// x / s, hi + lo / 16 with s a power of two from the row's largest value, which
-// hold a bf16 value exactly down to 2^-13 of that value; the pieces are two columns of
-// the same product.  So h keeps 16 bits, and no weight is converted.  With tiles of
-// 16 and 32 rows the row warps split on the way into shared memory, for every item
-// anew.  With 64 that is what bounds the kernel (three conversions a pair of
-// elements), so rows are split once, by items of their own before either phase, and
-// the pieces are copied: 200 GPT-OSS-shaped tokens 197 -> 165 us, 1000 Qwen3-shaped 423
-// -> 287 (with tiles of 32 rows, 200 Qwen3-shaped, it costs: 122 -> 128).
+// Rows wider than the weights go in two pieces, hi and lo, as two columns of the same
+// product (columns cost nothing: an MMA reads 128 weight rows for 16 as for 64).  h is
+// kept in fp32 and multiplied as hi + lo in bf16 (16 significant bits); one bf16 would
+// double the error of the bf16 output.  With 8-bit weights a row is x / s = hi + lo / 16
+// in e4m3, s a power of two from the row's largest value: a bf16 x exactly down to
+// 2^-13 of that value, h to 6e-4.  No weight is converted.  With tiles of
+// 16 rows the row warps split on the way into shared memory, for every item anew.  With
+// more rows that would bound the kernel (three conversions a pair of elements), so
+// rows are split once, by items of their own before either phase, and the pieces are
+// copied: 200 tokens of the d = 4096 shape 423 -> 378 us, 1000 Qwen3-shaped 423 -> 287.
 #pragma once
 
 #include <cuda_bf16.h>
@@ -61,9 +62,9 @@ struct MoeCfg {
     // a block: two halves of 128 bytes (one swizzle row) of 128 weight rows
     static constexpr int A_HALF = 128 * 128, A_BYTES = 2 * A_HALF;
     static constexpr int BK = W8 ? 256 : 128;                  // elements of a block's row
-    static constexpr int COLS = NT * (W8 ? 2 : 1);             // accumulator columns
+    static constexpr int COLS = 2 * NT;                        // accumulator columns: two pieces
     static constexpr int B_HALF = COLS * 128, B_BYTES = 2 * B_HALF;
-    static constexpr int SB = NT == 64 && W8 ? 2 : 3;
+    static constexpr int SB = NT == 64 ? 2 : 3;
     static constexpr int LIST = 128 * NT;                      // choices (M K) at most
     static constexpr int TMEM_COLS = 2 * (COLS < 16 ? 16 : COLS) < 32 ? 32 : 2 * COLS;
     static constexpr int TABLE_BYTES = 3 * 128 * 4 + 3 * kMoeMaxTiles * 2 + LIST * 2 +
@@ -72,8 +73,8 @@ struct MoeCfg {
     static constexpr int SA =
         (232448 - 1024 - BAR_BYTES - TABLE_BYTES - SB * B_BYTES) / A_BYTES;
     static constexpr int SMEM = 1024 + BAR_BYTES + TABLE_BYTES + SB * B_BYTES + SA * A_BYTES;
-    static constexpr int DEPTH = NT == 16 ? 3 : 1;             // row blocks a thread has in flight
-    static constexpr bool PRE = W8 && NT == 64;                // rows are split by items of their own
+    static constexpr int DEPTH = NT > 16 ? 1 : W8 ? 2 : 3;     // row blocks a thread has in flight
+    static constexpr bool PRE = W8 && NT > 16;                 // rows are split by items of their own
     static_assert(SA > SB && SA <= 16, "weight ring");
 };
 
@@ -91,7 +92,7 @@ struct MoeArgs {
     const int32_t* expert_slot;      // [N] or null
     const float *s13, *s2;           // scales of 8-bit weight rows, slots s13_stride floats apart
     long long s13_stride, s2_stride;
-    __nv_bfloat16* h;                // [M K][f], rows by expert
+    float* h;                        // [M K][f], rows by expert
     float* y;                        // [M K][d], rows by choice
     uint8_t *xq, *hq;                // [M][hi, lo][d], [M K][hi, lo][f]: rows split once
     uint32_t* hmax;                  // [M K] largest magnitude of h's rows, zeroed (8-bit weights)
@@ -196,9 +197,8 @@ __device__ __forceinline__ bool wait_count(const uint32_t* p, uint32_t n) {
     }
 }
 
-// Two bf16 (one word) times inv as e4m3 pieces: hi, and lo = 16 (v - hi).
-__device__ __forceinline__ void split_pair(uint32_t w, float inv, uint32_t& hi, uint32_t& lo) {
-    const float a = __uint_as_float(w << 16) * inv, b = __uint_as_float(w & 0xffff0000u) * inv;
+// Two floats as e4m3 pieces: hi, and lo = 16 (v - hi).
+__device__ __forceinline__ void split_floats(float a, float b, uint32_t& hi, uint32_t& lo) {
     uint16_t h, l;
     asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(h) : "f"(b), "f"(a));
     uint32_t back;
@@ -220,10 +220,43 @@ __device__ __forceinline__ void split16(const uint4 (&v)[2], float inv, uint4& h
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         uint32_t h0, l0, h1, l1;
-        split_pair(w[2 * i], inv, h0, l0);
-        split_pair(w[2 * i + 1], inv, h1, l1);
+        split_floats(__uint_as_float(w[2 * i] << 16) * inv,
+                     __uint_as_float(w[2 * i] & 0xffff0000u) * inv, h0, l0);
+        split_floats(__uint_as_float(w[2 * i + 1] << 16) * inv,
+                     __uint_as_float(w[2 * i + 1] & 0xffff0000u) * inv, h1, l1);
         ho[i] = h0 | h1 << 16;
         lw[i] = l0 | l1 << 16;
+    }
+    hi = make_uint4(ho[0], ho[1], ho[2], ho[3]);
+    lo = make_uint4(lw[0], lw[1], lw[2], lw[3]);
+}
+
+// Sixteen floats -> sixteen bytes of each e4m3 piece; eight -> eight bf16 of each
+// bf16 piece, hi + lo.
+__device__ __forceinline__ void split16(const uint4 (&v)[4], float inv, uint4& hi, uint4& lo) {
+    uint32_t ho[4], lw[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        uint32_t h0, l0, h1, l1;
+        split_floats(__uint_as_float(v[i].x) * inv, __uint_as_float(v[i].y) * inv, h0, l0);
+        split_floats(__uint_as_float(v[i].z) * inv, __uint_as_float(v[i].w) * inv, h1, l1);
+        ho[i] = h0 | h1 << 16;
+        lw[i] = l0 | l1 << 16;
+    }
+    hi = make_uint4(ho[0], ho[1], ho[2], ho[3]);
+    lo = make_uint4(lw[0], lw[1], lw[2], lw[3]);
+}
+__device__ __forceinline__ void split8(const uint4 (&v)[2], uint4& hi, uint4& lo) {
+    const uint32_t w[8] = {v[0].x, v[0].y, v[0].z, v[0].w, v[1].x, v[1].y, v[1].z, v[1].w};
+    uint32_t ho[4], lw[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const float a = __uint_as_float(w[2 * i]), b = __uint_as_float(w[2 * i + 1]);
+        const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
+        const __nv_bfloat162 l =
+            __floats2bfloat162_rn(a - __low2float(h), b - __high2float(h));
+        ho[i] = *reinterpret_cast<const uint32_t*>(&h);
+        lw[i] = *reinterpret_cast<const uint32_t*>(&l);
     }
     hi = make_uint4(ho[0], ho[1], ho[2], ho[3]);
     lo = make_uint4(lw[0], lw[1], lw[2], lw[3]);
@@ -503,18 +536,19 @@ struct RowRing {
 
 // A group's row blocks of one item into the ring (four warps).  base: the item's
 // first block, counted over all items.  A thread's unit is 16 bytes of one row's
-// 256: chunk tid % 16 of rows tid / 16, + 8, ...  MODE kCopy: as they are; kSplit: 16 bf16
-// elements become 16 bytes of hi and of lo; kPieces: hi and lo are copied, K bytes
-// apart.
-enum { kCopy = 0, kSplit = 1, kPieces = 2 };
+// 256: chunk tid % 16 of rows tid / 16, + 8, ...  MODE kCopy: as they are; kSplit: bf16
+// elements become hi and lo (8-bit weights); kSplitF: fp32 elements do (h); kPieces:
+// hi and lo are copied, K bytes apart.
+enum { kCopy = 0, kSplit = 1, kPieces = 2, kSplitF = 3 };
 template <bool W8, int NT, int MODE>
 __device__ __forceinline__ bool produce_rows(const MoeShared<W8, NT>& s, const uint8_t* (&src)[NT / 8],
                                              const float (&inv)[NT / 8], uint32_t have, int n8,
                                              int base, int kb, int K, int tid,
                                              RowRing<W8, NT>& ring) {
     using Cfg = MoeCfg<W8, NT>;
-    constexpr int U = NT / 8, D = Cfg::DEPTH, V = MODE == kCopy ? 1 : 2;
-    constexpr int STEP = MODE == kSplit ? 2 * 256 : 256;       // bytes of a row's block
+    constexpr int U = NT / 8, D = Cfg::DEPTH;
+    constexpr int V = MODE == kCopy ? 1 : MODE == kSplitF && W8 ? 4 : 2;   // loads a unit
+    constexpr int STEP = MODE == kPieces ? 256 : 256 * V;      // bytes of a row's block
     constexpr int CE = W8 ? 16 : 8;                            // elements of a unit
     const int chunk = tid & 15, lane = tid & 31;
     uint4 v[D][U][V];
@@ -546,7 +580,10 @@ __device__ __forceinline__ bool produce_rows(const MoeShared<W8, NT>& s, const u
                 const int row = (tid >> 4) + 8 * u;
                 if constexpr (MODE != kCopy) {
                     uint4 hi = v[i][u][0], lo = v[i][u][V - 1];
-                    if constexpr (MODE == kSplit) split16(v[i][u], inv[u], hi, lo);
+                    if constexpr (MODE == kSplitF && !W8)
+                        split8(v[i][u], hi, lo);
+                    else if constexpr (MODE != kPieces)
+                        split16(v[i][u], inv[u], hi, lo);
                     const int low = n8 + row;
                     *reinterpret_cast<uint4*>(dst + row * 128 + (((chunk ^ row) & 7) << 4)) = hi;
                     *reinterpret_cast<uint4*>(dst + low * 128 + (((chunk ^ low) & 7) << 4)) = lo;
@@ -565,16 +602,19 @@ __device__ __forceinline__ bool produce_rows(const MoeShared<W8, NT>& s, const u
     return true;
 }
 
-// n elements (a multiple of 16) of `rows` bf16 rows into two pieces: a thread a chunk of
-// 16.  src(r), inv(r): row r and 1 / its scale; dst: rows of hi and lo, n bytes each.
-template <class Src, class Inv>
+// n elements (a multiple of 16) of `rows` rows, bf16 (V = 2) or fp32 (V = 4), into two e4m3
+// pieces: a thread a chunk of 16.  src(r), inv(r): row r and 1 / its scale; dst: rows
+// of hi and lo, n bytes each.
+template <int V, class Src, class Inv>
 __device__ __forceinline__ void split_rows(int rows, int n, int thread, int threads, Src src, Inv inv,
                                            uint8_t* dst) {
     const int chunks = n / 16;
     for (int i = thread; i < rows * chunks; i += threads) {
         const int r = i / chunks, c = i - r * chunks;
-        const uint4* at = reinterpret_cast<const uint4*>(src(r)) + 2 * c;
-        const uint4 v[2] = {__ldcg(at), __ldcg(at + 1)};
+        const uint4* at = reinterpret_cast<const uint4*>(src(r)) + V * c;
+        uint4 v[V];
+#pragma unroll
+        for (int j = 0; j < V; ++j) v[j] = __ldcg(at + j);
         uint4 hi, lo;
         split16(v, inv(r), hi, lo);
         uint8_t* to = dst + (size_t)r * 2 * n + 16 * c;
@@ -756,7 +796,7 @@ __global__ void __launch_bounds__(kMoeThreads, 1)
             if (Cfg::PRE && (item < my.gate_up || (item >= my.split_h && item < my.down))) continue;
             const bool second = item >= my.down;
             const int rows = __reduce_max_sync(kFull, moe_item<W8, NT>(a, s, my, item).rows);
-            const bool split = W8 && (second || a.x_split);
+            const bool split = second || (W8 && a.x_split);
             const int n = split ? 2 * ((rows + 7) & ~7) : (rows + 15) & ~15;
             const uint32_t idesc = W8 ? idesc_e4m3_f32(128, n) : idesc_bf16_f32(128, n);
             if (__any_sync(kFull, !mbar_wait(&s.t_empty[acc], aphase ^ 1))) {
@@ -849,11 +889,11 @@ __global__ void __launch_bounds__(kMoeThreads, 1)
             if (Cfg::PRE && it.kind >= kSplitX) {
                 const int t = threadIdx.x - 256;
                 if (it.kind == kSplitX)
-                    split_rows(it.rows, a.d, t, 256, [&](int r) { return a.x + (it.row0 + r) * a.x_bytes; },
+                    split_rows<2>(it.rows, a.d, t, 256, [&](int r) { return a.x + (it.row0 + r) * a.x_bytes; },
                                [&](int r) { return 1.f / __ldcg(a.xs + it.row0 + r); },
                                a.xq + (size_t)it.row0 * 2 * a.d);
                 else
-                    split_rows(it.rows, a.f, t, 256,
+                    split_rows<4>(it.rows, a.f, t, 256,
                                [&](int r) { return a.h + (size_t)(it.row0 + r) * a.f; },
                                [&](int r) {
                                    return 1.f / split_scale(__uint_as_float(
@@ -866,7 +906,7 @@ __global__ void __launch_bounds__(kMoeThreads, 1)
                 continue;
             }
             const bool down = it.kind == kDown;
-            const bool split = W8 && (down || a.x_split);
+            const bool split = down || (W8 && a.x_split);
             const int n8 = (it.rows + 7) & ~7;
             const uint8_t* src[NT / 8];
             float inv[NT / 8];
@@ -893,15 +933,18 @@ __global__ void __launch_bounds__(kMoeThreads, 1)
                     src[u] = x_pieces ? a.xq + (size_t)tok * 2 * a.d : a.x + tok * a.x_bytes;
                     if (W8 && !Cfg::PRE && split) inv[u] = 1.f / __ldcg(a.xs + tok);
                 }
-                src[u] += (tid & 15) * (split && !Cfg::PRE ? 32 : 16);
+                src[u] += (tid & 15) * (Cfg::PRE || !split ? 16 : !down ? 32 : W8 ? 64 : 32);
             }
             const int kb = down ? a.kb2 : a.kb1, K = down ? a.f : a.d;
             bool ok;
-            if (W8 && split)
+            if (!split)
+                ok = produce_rows<W8, NT, kCopy>(s, src, inv, have, n8, base, kb, K, tid, ring);
+            else if (Cfg::PRE || !down)
                 ok = produce_rows<W8, NT, !W8 ? kCopy : Cfg::PRE ? kPieces : kSplit>(
                     s, src, inv, have, n8, base, kb, K, tid, ring);
             else
-                ok = produce_rows<W8, NT, kCopy>(s, src, inv, have, n8, base, kb, K, tid, ring);
+                ok = produce_rows<W8, NT, Cfg::PRE ? kPieces : kSplitF>(s, src, inv, have, n8, base,
+                                                                        kb, K, tid, ring);
             if (!ok) {
                 failed = true;
                 break;
@@ -934,7 +977,7 @@ __global__ void __launch_bounds__(kMoeThreads, 1)
             }
             const bool down = it.kind == kDown;
             const int slot = s.slot[it.e];
-            const bool split = W8 && (down || a.x_split);
+            const bool split = down || (W8 && a.x_split);
             const int n8 = (it.rows + 7) & ~7;
             // this lane's weight row: an element of f (gate in the low half of the
             // warp, up in the high half), or of d
@@ -979,14 +1022,14 @@ __global__ void __launch_bounds__(kMoeThreads, 1)
             for (int c0 = 0; c0 < it.rows; c0 += 16) {
                 float v[16];
                 tmem_ld16f(tb + c0, v);
-                if (W8 && split) {
+                if (split) {
                     float lo[16];
                     tmem_ld16f(tb + n8 + c0, lo);
                     tmem_ld_wait();
                     pin16(v);
                     pin16(lo);
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) v[i] = fmaf(lo[i], 0.0625f, v[i]);
+                    for (int i = 0; i < 16; ++i) v[i] = fmaf(lo[i], W8 ? 0.0625f : 1.f, v[i]);
                 } else {
                     tmem_ld_wait();
                     pin16(v);
@@ -1013,12 +1056,11 @@ __global__ void __launch_bounds__(kMoeThreads, 1)
                             __shfl_xor_sync(kFull, lane < 16 ? v[c + 1] : v[c], 16);
                         const float gate = lane < 16 ? v[c] : got, up = lane < 16 ? got : v[c + 1];
                         const float hv = __fdividef(gate, 1.f + __expf(-gate)) * up;
-                        const __nv_bfloat16 hb = __float2bfloat16_rn(hv);
                         const int col = c + (lane >> 4);
                         const bool mine = in && col < n;
-                        if (mine) a.h[(size_t)(it.row0 + c0 + col) * a.f + wrow] = hb;
+                        if (mine) a.h[(size_t)(it.row0 + c0 + col) * a.f + wrow] = hv;
                         if (W8)
-                            top[c / 2] = mine ? (uint32_t)__bfloat16_as_ushort(hb) << 16 & 0x7fffffffu : 0u;
+                            top[c / 2] = mine ? __float_as_uint(hv) & 0x7fffffffu : 0u;
                     }
                     if (W8) {
                         // the largest of 16 lanes for eight columns at once: each exchange
