@@ -237,8 +237,8 @@ KERNEL_SOURCES = {
                "policy_lrfu.cu", "policy_spatio.cu", "policy_scan.cuh", "cache_scan.cuh",
                "crc_device.cuh"],
     "loss": ["loss.cu", "cache_scan.cuh", "crc_device.cuh"],
-    "moe": ["moe.cu", "moe_experts.cuh", "moe_route.cuh", "crc_device.cuh"],
-    "norm": ["norm.cu"],
+    "moe": ["moe.cu", "moe_experts.cuh", "moe_route.cuh", "pdl.cuh", "crc_device.cuh"],
+    "norm": ["norm.cu", "pdl.cuh", "crc_device.cuh"],
 }
 
 

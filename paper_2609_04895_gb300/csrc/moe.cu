@@ -127,47 +127,31 @@ int launch_experts(const crc_moe& m, const MoeArgs& a, cudaStream_t stream) {
     const long long experts = (long long)a.M * a.K < a.N ? (long long)a.M * a.K : a.N;
     const long long items =
         (experts + (long long)a.M * a.K / NT) * (a.ft + a.dt + 1) + a.M / kSplitTokens + 1;
-    cudaLaunchAttribute at[1];
-    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    at[0].val.programmaticStreamSerializationAllowed = 1;
-    cudaLaunchConfig_t c = {};
-    c.gridDim = dim3((unsigned)(items < sm_count() ? items : sm_count()));
-    c.blockDim = dim3(kMoeThreads);
-    c.dynamicSmemBytes = Cfg::SMEM;
-    c.stream = stream;
-    c.attrs = at;
-    c.numAttrs = 1;
     cudaError_t e;
     {
         ProfScope prof(CRC_KERNEL_MOE, stream);
-        e = cudaLaunchKernelEx(&c, kern, m13, m2, a);
+        e = launch_dependent(kern, dim3((unsigned)(items < sm_count() ? items : sm_count())),
+                             kMoeThreads, Cfg::SMEM, stream, 1, m13, m2, a);
     }
     note_launch();
     return cuda_status(e);
 }
 
 int launch_route(const MoeRouteArgs& r, cudaStream_t stream) {
-    cudaLaunchConfig_t c = {};
-    c.blockDim = dim3(kRouteThreads);
-    c.stream = stream;
     cudaError_t e;
-    ProfScope prof(CRC_KERNEL_MOE_ROUTE, stream);
-    if (r.logits) {
-        c.gridDim = dim3((unsigned)((r.N + 7) / 8), (unsigned)r.M);
-        e = cudaLaunchKernelEx(&c, moe_logits_kernel, r);
-    } else if (r.scores) {
-        c.gridDim = dim3((unsigned)((r.M + 7) / 8));
-        e = cudaLaunchKernelEx(&c, moe_topk_kernel, r);
-    } else {
-        cudaLaunchAttribute at[1];
-        at[0].id = cudaLaunchAttributeClusterDimension;
-        at[0].val.clusterDim.x = kRouteCtas;
-        at[0].val.clusterDim.y = 1;
-        at[0].val.clusterDim.z = 1;
-        c.attrs = at;
-        c.numAttrs = 1;
-        c.gridDim = dim3((unsigned)((r.M + kRouteTokens - 1) / kRouteTokens * kRouteCtas));
-        e = cudaLaunchKernelEx(&c, moe_route_kernel, r);
+    {
+        ProfScope prof(CRC_KERNEL_MOE_ROUTE, stream);
+        if (r.logits)
+            e = launch_dependent(moe_logits_kernel, dim3((unsigned)((r.N + 7) / 8), (unsigned)r.M),
+                                 kRouteThreads, 0, stream, 1, r);
+        else if (r.scores)
+            e = launch_dependent(moe_topk_kernel, dim3((unsigned)((r.M + 7) / 8)), kRouteThreads, 0,
+                                 stream, 1, r);
+        else
+            e = launch_dependent(
+                moe_route_kernel,
+                dim3((unsigned)((r.M + kRouteTokens - 1) / kRouteTokens * kRouteCtas)),
+                kRouteThreads, 0, stream, kRouteCtas, r);
     }
     note_launch();
     return cuda_status(e);

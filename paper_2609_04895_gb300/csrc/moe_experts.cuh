@@ -342,27 +342,30 @@ __device__ __forceinline__ void build_small_tables(const MoeArgs& a, const MoeSh
 }
 
 template <bool W8, int NT>
-__device__ __forceinline__ void build_tables(const MoeArgs& a, const MoeShared<W8, NT>& s) {
+__device__ __forceinline__ void build_tables(const MoeArgs& a, const MoeShared<W8, NT>& s,
+                                             int slot_e) {
     using Cfg = MoeCfg<W8, NT>;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int E = a.M * a.K;
-    if (few_choices(a.M, a.K)) {
-        if (a.logits) {               // Top-K and gates, a warp a token
-            if (warp < a.M) {
-                float v[4];
+    const bool few = few_choices(a.M, a.K), route = few && a.logits && warp < a.M;
+    float v[4];                       // asked for before the slots are waited for
+    if (route) {
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const int e = lane + 32 * i;
-                    v[i] = e < a.N ? __ldcg(a.logits + warp * a.N + e) : 0.f;
-                }
-                const int r = warp * a.K;
-                const bool out = blockIdx.x == 0;
-                route_token(v, a.N, a.K, false, a.renorm, lane, s.few_ids + r, s.few_gates + r,
-                            out && a.ids_out ? a.ids_out + r : nullptr,
-                            out && a.gates_out ? a.gates_out + r : nullptr);
-            }
-            __syncthreads();
+        for (int i = 0; i < 4; ++i) {
+            const int e = lane + 32 * i;
+            v[i] = e < a.N ? __ldcg(a.logits + warp * a.N + e) : 0.f;
         }
+    }
+    if (threadIdx.x < 128) s.slot[threadIdx.x] = slot_e >= 0 && slot_e < a.slots ? slot_e : -1;
+    if (few) {
+        if (route) {                  // Top-K and gates, a warp a token
+            const int r = warp * a.K;
+            const bool out = blockIdx.x == 0;
+            route_token(v, a.N, a.K, false, a.renorm, lane, s.few_ids + r, s.few_gates + r,
+                        out && a.ids_out ? a.ids_out + r : nullptr,
+                        out && a.gates_out ? a.gates_out + r : nullptr);
+        }
+        __syncthreads();
         if (warp == 0) build_small_tables<W8, NT>(a, s);
         __syncthreads();
         return;
@@ -678,21 +681,17 @@ __global__ void __launch_bounds__(kMoeThreads, 1)
         tmem_alloc(s.tmem_slot, Cfg::TMEM_COLS);
         tmem_relinquish();
     }
-    // the map from experts to slots is an input: the routing kernel does not write it
-    if (threadIdx.x < 128) {
-        const int e = threadIdx.x;
-        const int at = e >= a.N ? -1 : a.expert_slot ? a.expert_slot[e] : e;
-        s.slot[e] = at >= 0 && at < a.slots ? at : -1;
-    }
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem = *s.tmem_slot;
 
-    pdl_wait();                       // the choices and the zeroed counters are in place
+    pdl_begin();                      // the choices and the zeroed counters are in place
     int next = 0;
     if (threadIdx.x == 0) next = (int)atomicAdd(&a.ctrl[kCtrlNext], 1u);
-    build_tables<W8, NT>(a, s);
+    int slot_e = -1;                  // of expert threadIdx.x
+    if (threadIdx.x < a.N) slot_e = a.expert_slot ? __ldcg(a.expert_slot + threadIdx.x) : threadIdx.x;
+    build_tables<W8, NT>(a, s, slot_e);
     const int tiles = s.count[0];
     const MoeItems items = MoeItems::of<W8, NT>(a, tiles);
 

@@ -13,6 +13,7 @@
 #pragma once
 
 #include "crc_device.cuh"
+#include "pdl.cuh"
 
 namespace crc {
 
@@ -37,13 +38,6 @@ struct MoeRouteArgs {
     uint32_t* ctrl;                  // zeroed
     int ctrl_words;
 };
-
-__device__ __forceinline__ void pdl_launch_dependents() {
-    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-}
-__device__ __forceinline__ void pdl_wait() {
-    asm volatile("griddepcontrol.wait;" ::: "memory");
-}
 
 // Scores as integers in the same order; NaN lowest, 0 left for "none".
 __device__ __forceinline__ uint32_t score_key(float v) {
@@ -159,7 +153,7 @@ __global__ void __launch_bounds__(kRouteThreads)
     __shared__ float part[2][kRouteCtas][WARPS * 16];
     __shared__ uint32_t amax[2][kRouteCtas][WARPS];
     asm volatile("barrier.cluster.arrive.relaxed;" ::: "memory");
-    pdl_launch_dependents();
+    pdl_begin();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int rank = (int)cluster_ctarank();
     const int t0 = (int)(blockIdx.x / kRouteCtas) * kRouteTokens;
@@ -263,7 +257,7 @@ __global__ void __launch_bounds__(kRouteThreads)
 __global__ void __launch_bounds__(kRouteThreads)
     moe_logits_kernel(MoeRouteArgs a) {
     constexpr int BATCH = 16;         // rows of 4096 elements at once
-    pdl_launch_dependents();
+    pdl_begin();
     zero_ctrl(a);
     const int lane = threadIdx.x & 31;
     const int e = (int)blockIdx.x * (kRouteThreads / 32) + (threadIdx.x >> 5);
@@ -306,8 +300,8 @@ __global__ void __launch_bounds__(kRouteThreads)
 // The same from given probabilities: a warp a token.
 __global__ void __launch_bounds__(kRouteThreads)
     moe_topk_kernel(MoeRouteArgs a) {
+    pdl_begin();
     zero_ctrl(a);
-    pdl_launch_dependents();
     const int lane = threadIdx.x & 31;
     const long long m = (long long)blockIdx.x * (kRouteThreads / 32) + (threadIdx.x >> 5);
     if (m >= a.M) return;

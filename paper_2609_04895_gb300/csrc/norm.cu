@@ -16,6 +16,7 @@
 
 #include "crc_device.cuh"
 #include "crc_internal.h"
+#include "pdl.cuh"
 
 namespace crc {
 namespace {
@@ -186,6 +187,7 @@ struct NormArgs {
 template <typename T, int VPT, int THREADS>
 __global__ void __launch_bounds__(THREADS) rms_norm_kernel(NormArgs a) {
     __shared__ float red[2][32];
+    pdl_begin();
     const RowTeam team(a.warps);
     const long long row = (long long)blockIdx.x * (blockDim.x / team.threads) + team.id;
     if (row >= a.M) return;
@@ -256,6 +258,7 @@ __global__ void __launch_bounds__(THREADS)
     quantize_rows_kernel(const __nv_bfloat16* x, long long ldx, int M, int d, int warps, uint8_t* q,
                          float* scale) {
     __shared__ float red[2][32];
+    pdl_begin();
     const RowTeam team(warps);
     const int rows = blockDim.x / team.threads, nvec = d >> 3;
     const long long step = (long long)gridDim.x * rows;
@@ -329,7 +332,7 @@ struct NormGradArgs {
 template <typename T, int VPT, int THREADS, bool RING>
 __global__ void __launch_bounds__(THREADS, VPT == 1 ? 2 : 1) rms_norm_grad_kernel(NormGradArgs a) {
     extern __shared__ __align__(128) uint8_t ring[];
-    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    pdl_begin();
     __shared__ float red[2][32];
     __shared__ __align__(8) uint64_t full[kMaxGradStages];
     const RowTeam team(blockDim.x >> 5);
@@ -464,7 +467,7 @@ __global__ void __launch_bounds__(THREADS, VPT == 1 ? 2 : 1) rms_norm_grad_kerne
 // dw[c] = sum of the G partial rows: 32 row groups a column, then their sum.
 __global__ void __launch_bounds__(1024) norm_dw_kernel(const float* part, int G, int d, float* dw) {
     __shared__ float sm[32][33];
-    asm volatile("griddepcontrol.wait;" ::: "memory");     // the partial rows are written
+    pdl_begin();                      // the partial rows are written
     const int lane = threadIdx.x & 31, grp = threadIdx.x >> 5;
     const int c = blockIdx.x * 32 + lane;
     float s = 0.f;
@@ -569,12 +572,13 @@ int launch_grad_t(const GradShape& sh, int& G, const NormGradArgs& a, cudaStream
         const long long most = (long long)fit * sm_count();
         G = (int)(G < most ? G : most);
     }
+    cudaError_t e;
     {
         ProfScope prof(CRC_KERNEL_NORM, stream);
-        kern<<<G, sh.threads(), smem, stream>>>(a);
+        e = launch_dependent(kern, dim3((unsigned)G), sh.threads(), smem, stream, 1, a);
     }
     note_launch();
-    return cuda_status(cudaGetLastError());
+    return cuda_status(e);
 }
 template <typename T>
 int launch_grad(const GradShape& sh, int& G, const NormGradArgs& a, cudaStream_t stream) {
@@ -629,9 +633,11 @@ int crc_rms_norm(const void *x_dev, int64_t x_stride, const void* residual_dev,
     a.warps = sh.warps;
     a.eps = (float)eps;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
+    cudaError_t e;
     {
         ProfScope prof(CRC_KERNEL_NORM, st);
-#define CRC_K(V, B, T) rms_norm_kernel<T, V, B><<<sh.grid(M), sh.threads(), 0, st>>>(a)
+#define CRC_K(V, B, T) \
+    e = launch_dependent(rms_norm_kernel<T, V, B>, dim3(sh.grid(M)), sh.threads(), 0, st, 1, a)
         if (stream_type == CRC_BF16)
             CRC_SHAPE(sh, CRC_K, __nv_bfloat16);
         else
@@ -639,7 +645,7 @@ int crc_rms_norm(const void *x_dev, int64_t x_stride, const void* residual_dev,
 #undef CRC_K
     }
     note_launch();
-    return cuda_status(cudaGetLastError());
+    return cuda_status(e);
 }
 
 size_t crc_rms_norm_grad_workspace_bytes(int64_t M, int32_t d) {
@@ -686,18 +692,9 @@ int crc_rms_norm_grad(const uint16_t* dy_dev, const void* s_dev, const uint16_t*
     if (!dw_dev) return CRC_OK;
     cudaError_t e;
     {
-        // its blocks take their places while the rows are still on their way
-        cudaLaunchAttribute at[1];
-        at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-        at[0].val.programmaticStreamSerializationAllowed = 1;
-        cudaLaunchConfig_t c = {};
-        c.gridDim = dim3((unsigned)((d + 31) / 32));
-        c.blockDim = dim3(1024);
-        c.stream = st;
-        c.attrs = at;
-        c.numAttrs = 1;
         ProfScope prof(CRC_KERNEL_NORM, st);
-        e = cudaLaunchKernelEx(&c, norm_dw_kernel, (const float*)a.part, G, d, dw_dev);
+        e = launch_dependent(norm_dw_kernel, dim3((unsigned)((d + 31) / 32)), 1024, 0, st, 1,
+                             (const float*)a.part, G, d, dw_dev);
     }
     note_launch();
     return cuda_status(e);
@@ -719,16 +716,17 @@ int crc_quantize_rows(const uint16_t* x_dev, int64_t x_stride, int64_t M, int32_
     const unsigned grid = (unsigned)(sh.grid(M) < most ? sh.grid(M) : most);
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     const __nv_bfloat16* x = reinterpret_cast<const __nv_bfloat16*>(x_dev);
+    cudaError_t e;
     {
         ProfScope prof(CRC_KERNEL_QUANTIZE, st);
-#define CRC_K(V, B, unused) \
-    quantize_rows_kernel<V, B><<<grid, sh.threads(), 0, st>>>(x, x_stride, (int)M, d, sh.warps, \
-                                                              out8_dev, scale8_dev)
+#define CRC_K(V, B, unused)                                                                     \
+    e = launch_dependent(quantize_rows_kernel<V, B>, dim3(grid), sh.threads(), 0, st, 1, x,      \
+                         (long long)x_stride, (int)M, (int)d, sh.warps, out8_dev, scale8_dev)
         CRC_SHAPE(sh, CRC_K, 0);
 #undef CRC_K
     }
     note_launch();
-    return cuda_status(cudaGetLastError());
+    return cuda_status(e);
 }
 
 }  // extern "C"

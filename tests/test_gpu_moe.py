@@ -401,3 +401,41 @@ def test_refusals_of_the_binding(P):
         c.layer(c.x.cpu())
     with pytest.raises(P.CrcError):
         c.layer(c.x, workspace=torch.empty(256, dtype=torch.uint8, device="cuda"))
+
+
+@pytest.mark.parametrize("M", [1, 7, 40])
+@pytest.mark.parametrize("kind", ["bf16", "w8x8"])
+def test_a_chain_of_calls_needs_no_waits_between_them(P, kind, M):
+    """Norm, layer and slot map one after the other on one stream, in place and in one
+    workspace, with nothing between them, equal the same with a wait after each call."""
+    w8 = kind != "bf16"
+    layers = [Case(P, 64, 4, 512, 128, M, w8=w8, slots=80, seed=i) for i in range(3)]
+    weight = torch.ones(512, dtype=torch.bfloat16, device="cuda")
+    ws = torch.empty(max(c.layer.workspace_bytes(M) for c in layers), dtype=torch.uint8,
+                     device="cuda")
+    maps = [torch.stack([c.slot.roll(k) for k in range(64)]) for c in layers]
+
+    def run(wait):
+        g = torch.Generator(device="cuda").manual_seed(9)
+        stream = randn(g, M, 512)
+        x = randn(g, M, 512)
+        h, q = torch.empty_like(x), torch.empty((M, 512), dtype=torch.float8_e4m3fn, device="cuda")
+        sc = torch.empty(M, device="cuda")
+        seen = []
+        for t in range(20):
+            for i, c in enumerate(layers):
+                c.slot.copy_(maps[i][(3 * t + i) % 64])
+                wait()
+                P.rms_norm(x, weight, residual=stream, residual_out=stream, out=h,
+                           out8=q if w8 else None, scale8=sc if w8 else None)
+                wait()
+                c.layer(h, out=x, x8=q if w8 else None, x_scale=sc if w8 else None, workspace=ws)
+                wait()
+            seen.append(x.clone())
+        return torch.stack(seen), stream.clone()
+
+    slow = run(torch.cuda.synchronize)
+    for _ in range(3):
+        fast = run(lambda: None)
+        assert torch.equal(fast[0], slow[0]) and torch.equal(fast[1], slow[1])
+    assert torch.isfinite(slow[0].float()).all()
