@@ -56,7 +56,6 @@ __host__ __device__ inline bool few_choices(int M, int K) {
     return M * K <= kFewChoices && M <= kFewTokens;
 }
 
-
 template <bool W8, int NT>
 struct MoeCfg {
     // a block: two halves of 128 bytes (one swizzle row) of 128 weight rows
@@ -66,7 +65,7 @@ struct MoeCfg {
     static constexpr int B_HALF = COLS * 128, B_BYTES = 2 * B_HALF;
     static constexpr int SB = NT == 64 ? 2 : 3;
     static constexpr int LIST = 128 * NT;                      // choices (M K) at most
-    static constexpr int TMEM_COLS = 2 * (COLS < 16 ? 16 : COLS) < 32 ? 32 : 2 * COLS;
+    static constexpr int TMEM_COLS = 2 * COLS;                 // two accumulators
     static constexpr int TABLE_BYTES = 3 * 128 * 4 + 3 * kMoeMaxTiles * 2 + LIST * 2 +
                                        kItemRing * NT * 4 + kFewChoices * 5 + 64;
     static constexpr int BAR_BYTES = 512;
@@ -312,7 +311,7 @@ struct MoeShared {
 // NT.  Every CTA builds the same tables.  All threads.
 //
 // One warp does it when the choices are one a lane (one token of up to 32 choices,
-// four of 8): 1.4 us less than the general form, four barriers of which are waits.
+// four of 8), without the general form's barriers.
 template <bool W8, int NT>
 __device__ __forceinline__ void build_small_tables(const MoeArgs& a, const MoeShared<W8, NT>& s) {
     const int lane = threadIdx.x & 31, E = a.M * a.K;
@@ -468,6 +467,7 @@ enum { kGateUp = 0, kDown = 1, kSplitX = 2, kSplitH = 3 };
 struct MoeItem {
     int kind, tile, j;       // kGateUp: 64 elements of f; kDown: 128 elements of d;
     int e, row0, rows;       // kSplitX: tokens from row0 on; kSplitH: the tile's rows
+    bool ok;                 // checking builds: within the arrays
 };
 // First items of the kinds, in the order kSplitX, kGateUp, kSplitH, kDown.
 struct MoeItems {
@@ -504,11 +504,16 @@ __device__ __forceinline__ MoeItem moe_item(const MoeArgs& a, const MoeShared<W8
         it.tile = it.e = 0;
         it.row0 = i * kSplitTokens;
         it.rows = min(kSplitTokens, a.M - it.row0);
+        it.ok = CRC_IN_BOUNDS(it.rows > 0, a.err);
         return it;
     }
     it.e = s.tile_e[it.tile];
     it.row0 = s.tile_row[it.tile];
     it.rows = s.tile_rows[it.tile];
+    it.ok = CRC_IN_BOUNDS(it.tile < s.count[0] && it.e < a.N && s.slot[it.e] >= 0 &&
+                              s.slot[it.e] < a.slots && it.rows > 0 && it.rows <= NT &&
+                              it.row0 + it.rows <= a.M * a.K,
+                          a.err);
     return it;
 }
 
@@ -720,7 +725,7 @@ __global__ void __launch_bounds__(kMoeThreads, 1)
                     next = (int)atomicAdd(&a.ctrl[kCtrlNext], 1u);
                     continue;
                 }
-                const int slot = s.slot[it.e];
+                const int slot = it.ok ? s.slot[it.e] : 0;
                 // an expert with several row tiles (all but the last are full) is
                 // read again, from L2
                 const uint64_t pol = it.rows == NT ? again : once;
@@ -887,12 +892,14 @@ __global__ void __launch_bounds__(kMoeThreads, 1)
             }
             if (Cfg::PRE && it.kind >= kSplitX) {
                 const int t = threadIdx.x - 256;
+                const int rows = it.ok ? it.rows : 0;
                 if (it.kind == kSplitX)
-                    split_rows<2>(it.rows, a.d, t, 256, [&](int r) { return a.x + (it.row0 + r) * a.x_bytes; },
+                    split_rows<2>(rows, a.d, t, 256,
+                                  [&](int r) { return a.x + (it.row0 + r) * a.x_bytes; },
                                [&](int r) { return 1.f / __ldcg(a.xs + it.row0 + r); },
                                a.xq + (size_t)it.row0 * 2 * a.d);
                 else
-                    split_rows<4>(it.rows, a.f, t, 256,
+                    split_rows<4>(rows, a.f, t, 256,
                                [&](int r) { return a.h + (size_t)(it.row0 + r) * a.f; },
                                [&](int r) {
                                    return 1.f / split_scale(__uint_as_float(
@@ -915,7 +922,7 @@ __global__ void __launch_bounds__(kMoeThreads, 1)
                 const int r = (tid >> 4) + 8 * u;
                 src[u] = nullptr;
                 inv[u] = 1.f;
-                if (r >= it.rows) continue;
+                if (r >= it.rows || !it.ok) continue;
                 have |= 1u << u;
                 if (down) {
                     const size_t row = (size_t)(it.row0 + r);
@@ -981,12 +988,12 @@ __global__ void __launch_bounds__(kMoeThreads, 1)
             // this lane's weight row: an element of f (gate in the low half of the
             // warp, up in the high half), or of d
             const int wrow = down ? it.j * 128 + quarter * 32 + lane
-                                      : it.j * 64 + quarter * 16 + (lane & 15);
-            const bool in = wrow < (down ? a.d : a.f);
+                                  : it.j * 64 + quarter * 16 + (lane & 15);
+            const bool in = it.ok && wrow < (down ? a.d : a.f);
             float sw = 1.f;
             if (W8 && in)
                 sw = down ? a.s2[slot * a.s2_stride + wrow]
-                              : a.s13[slot * a.s13_stride + (lane >> 4) * a.f + wrow];
+                          : a.s13[slot * a.s13_stride + (lane >> 4) * a.f + wrow];
             // scales of the rows: lane l holds those of rows l, l + 32
             constexpr int RS = (NT + 31) / 32;
             float rs[RS];
