@@ -111,6 +111,9 @@ struct RowTeam {
     int warps, id, thread, threads;
     __device__ __forceinline__ explicit RowTeam(int w)
         : warps(w), id((threadIdx.x >> 5) / w), thread(threadIdx.x - id * 32 * w), threads(32 * w) {}
+    // the whole CTA
+    __device__ __forceinline__ RowTeam()
+        : warps(blockDim.x >> 5), id(0), thread(threadIdx.x), threads(blockDim.x) {}
 };
 
 // Sum (or NaN-keeping maximum) of v over a row's warps, in one fixed order; every
@@ -296,6 +299,7 @@ __global__ void __launch_bounds__(THREADS)
 }
 
 constexpr int kMaxGradStages = 8;
+constexpr int kMaxGradTeams = 8;
 constexpr int kGradRing = 216 * 1024;          // at most, of an SM
 
 // `bytes` contiguous bytes (a multiple of 16, both ends 16-byte aligned) to shared
@@ -317,26 +321,32 @@ struct NormGradArgs {
     float* part;                    // [gridDim.x][d] partial dw
     uint32_t* err;
     int M, d;
-    int stages, stage_bytes;        // of the ring
+    int warps;                      // of a row
+    int stages, stage_bytes;        // of a team's ring
 };
 
-// A CTA takes rows blockIdx.x, + gridDim.x, ...  A thread keeps the dw sums of its
-// columns in registers and writes them once, so that no order of CTAs changes a
-// sum.
+// Teams of warps, one or more a CTA, take row after row.  A thread keeps the dw sums of
+// its columns in registers; at the end a CTA adds its teams' up and writes one row of
+// partial sums, so that no order of CTAs changes a sum.  CTAs of 256 threads, four an SM:
+// one of 1024 has a quarter of the partial sums and took 30.0 us where these take 26.5
+// (8000 x 2048 bf16); short rows share one (8000 x 512: 14.1 us with a CTA a row, 10.1 so).
 //
 // The rows come through a ring in shared memory, whole rows by asynchronous bulk
 // copies: the bytes on the way then cost no registers.  (With the next row in registers
 // two CTAs of 256 threads fit an SM: 8000 x 2048 bf16 took 29 us without dw.)  A stage
 // is filled again one row after its own: by then every thread has used all that it
 // read of it.  RING false: rows too wide for two stages, read straight to registers.
-template <typename T, int VPT, int THREADS, bool RING>
+template <typename T, int VPT, int THREADS, bool RING, bool TEAMS>
 __global__ void __launch_bounds__(THREADS, VPT == 1 ? 2 : 1) rms_norm_grad_kernel(NormGradArgs a) {
-    extern __shared__ __align__(128) uint8_t ring[];
+    extern __shared__ __align__(128) uint8_t smem[];
     pdl_begin();
     __shared__ float red[2][32];
-    __shared__ __align__(8) uint64_t full[kMaxGradStages];
-    const RowTeam team(blockDim.x >> 5);
-    const int d = a.d, nvec = d >> 3;
+    __shared__ __align__(8) uint64_t bars[TEAMS ? kMaxGradTeams : 1][kMaxGradStages];
+    const RowTeam team = TEAMS ? RowTeam(a.warps) : RowTeam();
+    const int d = a.d, nvec = d >> 3, teams = TEAMS ? blockDim.x / team.threads : 1;
+    const long long first = (long long)blockIdx.x * teams + team.id, step = (long long)gridDim.x * teams;
+    uint8_t* ring = smem + (size_t)team.id * a.stages * a.stage_bytes;
+    uint64_t* full = bars[team.id];
     const uint32_t dy_bytes = 2u * d, s_bytes = (uint32_t)sizeof(T) * d;
     const uint32_t row_bytes = dy_bytes + s_bytes + (a.dres ? s_bytes : 0u);
     auto fill = [&](int stage, long long row) {            // one thread
@@ -349,18 +359,18 @@ __global__ void __launch_bounds__(THREADS, VPT == 1 ? 2 : 1) rms_norm_grad_kerne
                       &full[stage]);
     };
     if constexpr (RING) {
-        if (threadIdx.x == 0) {
+        if (team.thread == 0) {
             for (int i = 0; i < a.stages; ++i) mbar_init(&full[i], 1);
             fence_mbar_init();
-            long long row = blockIdx.x;
-            for (int i = 0; i < a.stages && row < a.M; ++i, row += gridDim.x) fill(i, row);
+            long long row = first;
+            for (int i = 0; i < a.stages && row < a.M; ++i, row += step) fill(i, row);
         }
     }
     uint64_t dw[VPT][4] = {};          // pairs of neighbouring columns
     Vec8<__nv_bfloat16> lw[VPT];
 #pragma unroll
     for (int g = 0; g < VPT; ++g) {
-        const int i = threadIdx.x + g * blockDim.x;
+        const int i = team.thread + g * team.threads;
         if (i < nvec) lw[g].load(a.w + 8 * i);
     }
     if constexpr (RING) __syncthreads();
@@ -368,15 +378,15 @@ __global__ void __launch_bounds__(THREADS, VPT == 1 ? 2 : 1) rms_norm_grad_kerne
     int flip = 0, stage = 0;
     uint32_t phase = 0;
     bool failed = false;
-    for (long long row = blockIdx.x; row < a.M; row += gridDim.x, flip ^= 1) {
+    for (long long row = first; row < a.M; row += step, flip ^= 1) {
         const float rstd = a.rstd[row];
         const __nv_bfloat16* dyp = a.dy + row * d;
         const T* sp = static_cast<const T*>(a.s) + row * d;
         const T* rp = static_cast<const T*>(a.dres) + (a.dres ? row * d : 0);
         if constexpr (RING) {
-            if (!mbar_wait(&full[stage], phase)) {         // every thread waits, so all leave,
+            if (!mbar_wait(&full[stage], phase)) {         // the whole team waits, so all leave,
                 failed = true;                             // none with a copy on its way
-                for (int i = 1; i < a.stages && row + (long long)i * gridDim.x < a.M; ++i) {
+                for (int i = 1; i < a.stages && row + i * step < a.M; ++i) {
                     if (++stage == a.stages) {
                         stage = 0;
                         phase ^= 1;
@@ -394,7 +404,7 @@ __global__ void __launch_bounds__(THREADS, VPT == 1 ? 2 : 1) rms_norm_grad_kerne
         Vec8<T> ls[VPT], lr[VPT];
 #pragma unroll
         for (int g = 0; g < VPT; ++g) {
-            const int i = threadIdx.x + g * blockDim.x;
+            const int i = team.thread + g * team.threads;
             if (i >= nvec) continue;
             ldy[g].load(dyp + 8 * i);
             ls[g].load(sp + 8 * i);
@@ -404,7 +414,7 @@ __global__ void __launch_bounds__(THREADS, VPT == 1 ? 2 : 1) rms_norm_grad_kerne
         uint64_t dot2 = 0;
 #pragma unroll
         for (int g = 0; g < VPT; ++g) {
-            if ((int)(threadIdx.x + g * blockDim.x) >= nvec) continue;
+            if (team.thread + g * team.threads >= nvec) continue;
             float dy[8], s[8], w[8];
             ldy[g].get(dy);
             ls[g].get(s);
@@ -423,10 +433,10 @@ __global__ void __launch_bounds__(THREADS, VPT == 1 ? 2 : 1) rms_norm_grad_kerne
         const float c = row_reduce<false>(dot, red[flip], team) * inv_d;
         const uint64_t k2 = pack2(-rstd * c, -rstd * c);
         if constexpr (RING) {
-            // every thread is past the row before this one
+            // every thread of the team is past the row before this one
             const int before = (stage ? stage : a.stages) - 1;
-            const long long next = row + (long long)(a.stages - 1) * gridDim.x;
-            if (threadIdx.x == 0 && row != blockIdx.x && next < a.M) fill(before, next);
+            const long long next = row + (a.stages - 1) * step;
+            if (team.thread == 0 && row != first && next < a.M) fill(before, next);
             if (++stage == a.stages) {
                 stage = 0;
                 phase ^= 1;
@@ -434,7 +444,7 @@ __global__ void __launch_bounds__(THREADS, VPT == 1 ? 2 : 1) rms_norm_grad_kerne
         }
 #pragma unroll
         for (int g = 0; g < VPT; ++g) {
-            const int i = threadIdx.x + g * blockDim.x;
+            const int i = team.thread + g * team.threads;
             if (i >= nvec) continue;
             float dy[8], s[8], w[8], r[8] = {};
             ldy[g].get(dy);
@@ -452,15 +462,29 @@ __global__ void __launch_bounds__(THREADS, VPT == 1 ? 2 : 1) rms_norm_grad_kerne
         }
     }
     if (failed) latch_error(a.err, CRC_ETIMEOUT);
-    if (!a.part || failed) return;
+    if (!a.part) return;
+    // the teams' sums, in order, through the ring's memory; one team writes its own
+    float* sums = reinterpret_cast<float*>(smem);
+    if (teams > 1) __syncthreads();    // every row is through the ring
 #pragma unroll
     for (int g = 0; g < VPT; ++g) {
-        const int i = threadIdx.x + g * blockDim.x;
+        const int i = team.thread + g * team.threads;
         if (i >= nvec) continue;
         float f[8];
 #pragma unroll
         for (int j = 0; j < 4; ++j) unpack2(dw[g][j], f[2 * j], f[2 * j + 1]);
-        store8(a.part + (size_t)blockIdx.x * d + 8 * i, f);
+        store8(teams > 1 ? sums + (size_t)team.id * d + 8 * i : a.part + (size_t)blockIdx.x * d + 8 * i,
+               f);
+    }
+    if (teams == 1) return;
+    __syncthreads();
+    for (int i = 4 * threadIdx.x; i < d; i += 4 * blockDim.x) {
+        float4 t = make_float4(0.f, 0.f, 0.f, 0.f);
+        for (int r = 0; r < teams; ++r) {
+            const float4 v = *reinterpret_cast<const float4*>(sums + (size_t)r * d + i);
+            t.x += v.x, t.y += v.y, t.z += v.z, t.w += v.w;
+        }
+        *reinterpret_cast<float4*>(a.part + (size_t)blockIdx.x * d + i) = t;
     }
 }
 
@@ -500,25 +524,26 @@ RowShape row_shape(int d, long long M, int most) {
     const int warps = (nvec + 32 * vpt - 1) / (32 * vpt);
     return {warps, vpt, warps < 8 ? 8 / warps : 1};
 }
-// A gradient's CTAs take whole rows one after the other, through a ring (stages 0:
-// none).  Three rows ahead and as many CTAs as registers leave: 8000 x 2048 bf16, us
-// without dw, by the ring of a CTA: 72 KB (3 CTAs an SM) 26, 36 KB (4) 23.5, 24 KB
-// (two rows) 27.
+// A gradient's rows, through rings of three or more (stages 0: none); 8000 x 2048 bf16,
+// us without dw, four teams an SM: three stages 23.5, two 27.
 struct GradShape : RowShape {
     int stages, stage_bytes;
+    int smem() const { return rows * stages * stage_bytes; }
 };
 GradShape grad_shape(int d, int elem, bool dres) {
     const int nvec = d / 8;
     GradShape g;
     g.vpt = nvec <= 512 ? 1 : nvec <= 1024 ? 2 : 4;
     g.warps = (nvec + 32 * g.vpt - 1) / (32 * g.vpt);
-    g.rows = 1;
     g.stage_bytes = (d * (2 + elem * (dres ? 2 : 1)) + 127) / 128 * 128;
-    g.stages = 36 * 1024 / g.stage_bytes;
+    g.rows = 1;
+    g.rows = g.warps < 8 ? 8 / g.warps : 1;                      // teams
+    const int cta = g.rows * g.stage_bytes;                      // bytes of a stage of all teams
+    g.stages = 36 * 1024 / cta;
     g.stages = g.stages < 3 ? 3 : g.stages < kMaxGradStages ? g.stages : kMaxGradStages;
-    if (g.stages * g.stage_bytes > kGradRing / 2) {              // two CTAs an SM, or one
-        g.stages = kGradRing / 2 / g.stage_bytes;
-        if (g.stages < 2) g.stages = kGradRing / g.stage_bytes;
+    if (g.stages * cta > kGradRing / 2) {                        // two CTAs an SM, or one
+        g.stages = kGradRing / 2 / cta;
+        if (g.stages < 2) g.stages = kGradRing / cta;
         if (g.stages < 2) g.stages = 0;
         if (g.stages > 4) g.stages = 4;
     }
@@ -529,8 +554,8 @@ inline bool aligned(const void* p, size_t a) { return reinterpret_cast<uintptr_t
 
 // The most CTAs of a gradient call (the rows of its workspace); as many of them run
 // as stay resident.
-int grad_ctas(int M, int d) {
-    const long long most = (long long)(d <= 1024 ? 8 : 4) * sm_count();
+int grad_ctas(int M) {
+    const long long most = 4ll * sm_count();
     return (int)(M < most ? M : most);
 }
 
@@ -553,16 +578,18 @@ int check_rows(int64_t M, int32_t d) {
         else K(4, 512, __VA_ARGS__);                                     \
     } while (0)
 
-template <typename T, int VPT, int THREADS, bool RING>
+template <typename T, int VPT, int THREADS, bool RING, bool TEAMS = false>
 int launch_grad_t(const GradShape& sh, int& G, const NormGradArgs& a, cudaStream_t stream) {
-    auto kern = rms_norm_grad_kernel<T, VPT, THREADS, RING>;
-    const int smem = RING ? sh.stages * sh.stage_bytes : 0;
+    auto kern = rms_norm_grad_kernel<T, VPT, THREADS, RING, TEAMS>;
+    const int smem = RING ? sh.smem() : 0;
     static PerDevice ready;
     const int up = ready.get(current_device(), [&] {
         return cuda_status(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize,
                                                 RING ? kGradRing : 0)) == CRC_OK;
     });
     if (!up) return CRC_ECUDA;
+    const long long ctas = sh.grid(a.M);
+    if (ctas < G) G = (int)ctas;
     if (G > sm_count()) {
         int fit = 0;
         if (const int rc = cuda_status(
@@ -585,7 +612,9 @@ int launch_grad(const GradShape& sh, int& G, const NormGradArgs& a, cudaStream_t
     if (!sh.stages)
         return sh.threads() > 512 ? launch_grad_t<T, 4, 1024, false>(sh, G, a, stream)
                                   : launch_grad_t<T, 4, 512, false>(sh, G, a, stream);
-    if (sh.vpt == 1) return launch_grad_t<T, 1, 512, true>(sh, G, a, stream);
+    if (sh.vpt == 1)
+        return sh.rows > 1 ? launch_grad_t<T, 1, 512, true, true>(sh, G, a, stream)
+                           : launch_grad_t<T, 1, 512, true>(sh, G, a, stream);
     if (sh.vpt == 2) return launch_grad_t<T, 2, 512, true>(sh, G, a, stream);
     return sh.threads() > 512 ? launch_grad_t<T, 4, 1024, true>(sh, G, a, stream)
                               : launch_grad_t<T, 4, 512, true>(sh, G, a, stream);
@@ -650,7 +679,7 @@ int crc_rms_norm(const void *x_dev, int64_t x_stride, const void* residual_dev,
 
 size_t crc_rms_norm_grad_workspace_bytes(int64_t M, int32_t d) {
     if (check_rows(M, d) != CRC_OK || M < 1) return 0;
-    return ((size_t)grad_ctas((int)M, d) * d * sizeof(float) + 255) / 256 * 256;
+    return ((size_t)grad_ctas((int)M) * d * sizeof(float) + 255) / 256 * 256;
 }
 
 int crc_rms_norm_grad(const uint16_t* dy_dev, const void* s_dev, const uint16_t* weight_dev,
@@ -682,8 +711,9 @@ int crc_rms_norm_grad(const uint16_t* dy_dev, const void* s_dev, const uint16_t*
     a.M = (int)M;
     a.d = d;
     const GradShape sh = grad_shape(d, stream_type == CRC_BF16 ? 2 : 4, dres_dev != nullptr);
-    int G = grad_ctas((int)M, d);
+    int G = grad_ctas((int)M);
     a.err = device_error_word();
+    a.warps = sh.warps;
     a.stages = sh.stages;
     a.stage_bytes = sh.stage_bytes;
     const int rg = stream_type == CRC_BF16 ? launch_grad<__nv_bfloat16>(sh, G, a, st)
