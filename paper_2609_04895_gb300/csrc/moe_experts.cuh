@@ -22,6 +22,11 @@
 //      weights are on their way meanwhile), y goes to the workspace in fp32;
 //   then all CTAs add up the choices of their share of the tokens, in rank order.
 //
+// What bounds it is memory: 64 Qwen3-shaped tokens read 1208 MB in 178 us, 6.8 TB/s; a
+// call is 8 us longer before the first block (routing, tables) and 3 behind the last.
+// One token (75 MB, 24 us with its routing) is a chain of latencies: weights 8 us, h to
+// the other CTAs 4, y and its sum 4.
+//
 // Rows wider than the weights go in two pieces, hi and lo, as two columns of the same
 // product (columns cost nothing: an MMA reads 128 weight rows for 16 as for 64).  h is
 // kept in fp32 and multiplied as hi + lo in bf16 (16 significant bits); one bf16 would

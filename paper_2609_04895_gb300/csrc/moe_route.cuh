@@ -6,10 +6,13 @@
 //
 // A cluster of eight CTAs takes 16 tokens: each CTA multiplies one eighth of d
 // for all experts and puts its partial logits into the shared memory of the CTA
-// that owns the token (rank = token mod 8), where a warp sums them in rank order.  Splitting d
-// reads every element of x and W^R once per cluster (one token of N = 128,
-// d = 2048: 64 KB of W^R a CTA, against 512 KB on one), and the sum of eight short
-// chains is nearer to the exact logit than one long one.
+// that owns the token (rank = token mod 8), where a warp sums them in rank order.
+// Splitting d reads every element of x and W^R once per cluster (N = 128, d = 2048: 64 KB
+// of W^R a CTA, against 512 KB on one), and the sum of eight short chains is nearer to
+// the exact logit than one long one.  mma.sync and not tcgen05: 16 tokens are an eighth
+// of its smallest full tile, and what bounds this kernel is latency: 64 tokens, N = 128,
+// d = 2048 take 5 us, 2 of them the trip to memory, 1 the Top-K's rounds of two
+// reductions each.
 #pragma once
 
 #include "crc_device.cuh"

@@ -439,3 +439,22 @@ def test_a_chain_of_calls_needs_no_waits_between_them(P, kind, M):
         fast = run(lambda: None)
         assert torch.equal(fast[0], slow[0]) and torch.equal(fast[1], slow[1])
     assert torch.isfinite(slow[0].float()).all()
+
+
+def test_calls_on_two_streams_at_once(P):
+    """Layers that run at the same time, each with a workspace, wait for nothing of each
+    other's."""
+    cases = [Case(P, 64, 4, 1024, 512, 33, seed=1), Case(P, 64, 4, 1024, 512, 5, w8=True, seed=2),
+             Case(P, 128, 8, 512, 256, 200, w8=True, seed=3)]
+    ref = [c.run()[0].clone() for c in cases]
+    ws = [torch.empty(c.layer.workspace_bytes(c.M), dtype=torch.uint8, device="cuda") for c in cases]
+    outs = [torch.empty_like(r) for r in ref]
+    streams = [torch.cuda.Stream() for _ in cases]
+    torch.cuda.synchronize()
+    for _ in range(30):
+        for c, w, o, st in zip(cases, ws, outs, streams):
+            c.layer(c.x, out=o, workspace=w, stream=st)
+    torch.cuda.synchronize()
+    for o, r in zip(outs, ref):
+        assert torch.equal(o, r)
+    assert P.crc.crc_device_error() == 0
