@@ -20,13 +20,16 @@ constexpr int kMoeMaxEntries = 8192;      // M K
 inline bool aligned(const void* p, size_t a) { return reinterpret_cast<uintptr_t>(p) % a == 0; }
 inline size_t up256(size_t n) { return (n + 255) & ~(size_t)255; }
 
-// Rows of a tile: twice an expert's mean share of the choices, so that few experts
-// need a second pass over their weights, or the tokens if that is fewer.
-// Narrow tiles leave room for more row blocks in flight.
+// Rows of a tile, by an expert's mean share of the choices, with room for a few more so
+// that few experts need a second pass over their weights, or the tokens if that is fewer.
+// Narrow tiles leave room for more row blocks in flight.  8-bit weights, 16 / 32 / 64 rows:
+// mean 6.25 (d = 2048, f = 768) 116 / 118 / 128 us, 7.5 (d = 4096, f = 1536) 396 / 381 / 387,
+// 18.75 (d = 2048, f = 1024) 120 / 95 / 101, 25 (d = f = 2880) 238 / 162 / 169; bf16 at 25:
+// 322 / 262 / 261.
 int row_tile(int M, int K, int N) {
     const int E = M * K;
-    for (int nt = 16; nt < 64; nt *= 2)
-        if (E <= 128 * nt && (M <= nt || 2 * E <= nt * N)) return nt;
+    if (E <= 128 * 16 && (M <= 16 || E <= 6 * N)) return 16;
+    if (E <= 128 * 32 && (M <= 32 || E <= 26 * N)) return 32;
     return 64;
 }
 
@@ -126,7 +129,8 @@ int launch_experts(const crc_moe& m, const MoeArgs& a, cudaStream_t stream) {
     // no more CTAs than items there can be
     const long long experts = (long long)a.M * a.K < a.N ? (long long)a.M * a.K : a.N;
     const long long items =
-        (experts + (long long)a.M * a.K / NT) * (a.ft + a.dt + 1) + a.M / kSplitTokens + 1;
+        (experts + (long long)a.M * a.K / NT) * (a.ft + a.dt + 1) +
+        (long long)a.M * (a.d / 16) / kSplitUnits + 1;
     cudaError_t e;
     {
         ProfScope prof(CRC_KERNEL_MOE, stream);

@@ -54,7 +54,7 @@ constexpr int kItemRing = 4;
 constexpr int kCtrlNext = 0, kCtrlDone2 = 1, kCtrlXSplit = 2, kCtrlDone1 = 3;
 constexpr int kCtrlHSplit = kCtrlDone1 + kMoeMaxTiles;
 constexpr int kCtrlWords = kCtrlHSplit + kMoeMaxTiles;
-constexpr int kSplitTokens = 16;     // of an item that splits x
+constexpr int kSplitUnits = 512;     // 16-element units that an item splits, at least
 // Choices of which a warp has one a lane, of tokens of which each warp has one at most.
 constexpr int kFewChoices = 32, kFewTokens = 16;
 __host__ __device__ inline bool few_choices(int M, int K) {
@@ -107,6 +107,18 @@ struct MoeArgs {
     int kb1, kb2;                    // blocks of d, of f
     int ft, dt;                      // items a row tile: ceil(f / 64), ceil(d / 128)
 };
+
+// All of 128 threads, with their writes and reads before it ordered before those after.
+__device__ __forceinline__ bool group_all(bool ok, int id) {
+    uint32_t all;
+    asm volatile(
+        "{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %1, 0;\n\t"
+        "barrier.cta.red.and.pred q, %2, 128, p;\n\tselp.u32 %0, 1, 0, q;\n\t}\n"
+        : "=r"(all)
+        : "r"((uint32_t)ok), "r"(id)
+        : "memory");
+    return all != 0;
+}
 
 // One lane of a converged warp.
 __device__ __forceinline__ uint32_t elect_lane() {
@@ -471,19 +483,28 @@ __device__ __forceinline__ void build_tables(const MoeArgs& a, const MoeShared<W
 enum { kGateUp = 0, kDown = 1, kSplitX = 2, kSplitH = 3 };
 struct MoeItem {
     int kind, tile, j;       // kGateUp: 64 elements of f; kDown: 128 elements of d;
-    int e, row0, rows;       // kSplitX: tokens from row0 on; kSplitH: the tile's rows
+    int e, row0, rows;       // kSplitX: all tokens; kSplitH: the tile's rows; j: the part of them
     bool ok;                 // checking builds: within the arrays
 };
-// First items of the kinds, in the order kSplitX, kGateUp, kSplitH, kDown.
+// First items of the kinds, in the order kSplitX, kGateUp, kSplitH, kDown.  Everything
+// that follows waits for the splits, so they are cut into items for all CTAs, x as a
+// whole, h each tile's rows into `parts` (200 tokens of d = f = 2880, 32 experts, 8-bit:
+// 174 us with 16 tokens of x and one tile of h an item, 168 so).
 struct MoeItems {
-    int gate_up, split_h, down, end;
+    int gate_up, split_h, down, end, parts;
     template <bool W8, int NT>
     __device__ __forceinline__ static MoeItems of(const MoeArgs& a, int tiles) {
         MoeItems n;
-        n.gate_up = MoeCfg<W8, NT>::PRE && a.x_split && tiles ? (a.M + kSplitTokens - 1) / kSplitTokens
-                                                              : 0;
+        const int ctas = (int)gridDim.x;
+        n.gate_up = MoeCfg<W8, NT>::PRE && a.x_split && tiles
+                        ? min(ctas, (a.M * (a.d / 16) + kSplitUnits - 1) / kSplitUnits)
+                        : 0;
+        n.parts = MoeCfg<W8, NT>::PRE && tiles
+                      ? max(1, min((ctas + tiles - 1) / tiles,
+                                   a.M * a.K / tiles * (a.f / 16) / kSplitUnits))
+                      : 1;
         n.split_h = n.gate_up + tiles * a.ft;
-        n.down = n.split_h + (MoeCfg<W8, NT>::PRE ? tiles : 0);
+        n.down = n.split_h + (MoeCfg<W8, NT>::PRE ? tiles * n.parts : 0);
         n.end = n.down + tiles * a.dt;
         return n;
     }
@@ -499,17 +520,18 @@ __device__ __forceinline__ MoeItem moe_item(const MoeArgs& a, const MoeShared<W8
         it.j = i - n.down - it.tile * a.dt;
     } else if (MoeCfg<W8, NT>::PRE && i >= n.split_h) {
         it.kind = kSplitH;
-        it.tile = i - n.split_h;
+        it.tile = (i - n.split_h) / n.parts;
+        it.j = i - n.split_h - it.tile * n.parts;
     } else if (!MoeCfg<W8, NT>::PRE || i >= n.gate_up) {
         it.kind = kGateUp;
         it.tile = (i - n.gate_up) / a.ft;
         it.j = i - n.gate_up - it.tile * a.ft;
     } else {
         it.kind = kSplitX;
-        it.tile = it.e = 0;
-        it.row0 = i * kSplitTokens;
-        it.rows = min(kSplitTokens, a.M - it.row0);
-        it.ok = CRC_IN_BOUNDS(it.rows > 0, a.err);
+        it.tile = it.e = it.row0 = 0;
+        it.j = i;
+        it.rows = a.M;
+        it.ok = true;
         return it;
     }
     it.e = s.tile_e[it.tile];
@@ -621,18 +643,32 @@ __device__ __forceinline__ bool produce_rows(const MoeShared<W8, NT>& s, const u
 template <int V, class Src, class Inv>
 __device__ __forceinline__ void split_rows(int rows, int n, int thread, int threads, Src src, Inv inv,
                                            uint8_t* dst) {
-    const int chunks = n / 16;
-    for (int i = thread; i < rows * chunks; i += threads) {
-        const int r = i / chunks, c = i - r * chunks;
-        const uint4* at = reinterpret_cast<const uint4*>(src(r)) + V * c;
-        uint4 v[V];
+    constexpr int D = 4 / V;                        // chunks in flight
+    const int chunks = n / 16, all = rows * chunks;
+    for (int i0 = thread; i0 < all; i0 += D * threads) {
+        uint4 v[D][V];
+        float s[D];
 #pragma unroll
-        for (int j = 0; j < V; ++j) v[j] = __ldcg(at + j);
-        uint4 hi, lo;
-        split16(v, inv(r), hi, lo);
-        uint8_t* to = dst + (size_t)r * 2 * n + 16 * c;
-        *reinterpret_cast<uint4*>(to) = hi;
-        *reinterpret_cast<uint4*>(to + n) = lo;
+        for (int u = 0; u < D; ++u) {
+            const int i = i0 + u * threads;
+            if (i >= all) break;
+            const int r = i / chunks, c = i - r * chunks;
+            const uint4* at = reinterpret_cast<const uint4*>(src(r)) + V * c;
+#pragma unroll
+            for (int j = 0; j < V; ++j) v[u][j] = __ldcg(at + j);
+            s[u] = inv(r);
+        }
+#pragma unroll
+        for (int u = 0; u < D; ++u) {
+            const int i = i0 + u * threads;
+            if (i >= all) break;
+            const int r = i / chunks, c = i - r * chunks;
+            uint4 hi, lo;
+            split16(v[u], s[u], hi, lo);
+            uint8_t* to = dst + (size_t)r * 2 * n + 16 * c;
+            *reinterpret_cast<uint4*>(to) = hi;
+            *reinterpret_cast<uint4*>(to + n) = lo;
+        }
     }
 }
 
@@ -761,10 +797,11 @@ __global__ void __launch_bounds__(kMoeThreads, 1)
                     }
                 }
                 if (failed) break;
-                // The next item is claimed once this one's first block is consumed: a
-                // CTA that waits for h would otherwise take items that idle CTAs could
-                // have (one Qwen3-shaped token: all 128 down items on 56 CTAs).
-                if (kb <= Cfg::SA && !mbar_wait(&s.a_empty[first], first_phase)) {
+                // Of the last items, the next is claimed once this one's first block is
+                // consumed: a CTA that waits for h would otherwise take items that idle CTAs
+                // could have (one Qwen3-shaped token: all 128 down items on 56 CTAs).
+                if (kb <= Cfg::SA && items.end - item <= 2 * (int)gridDim.x &&
+                    !mbar_wait(&s.a_empty[first], first_phase)) {
                     failed = true;
                     break;
                 }
@@ -886,25 +923,28 @@ __global__ void __launch_bounds__(kMoeThreads, 1)
                                              : Cfg::PRE && it.kind == kDown ? kCtrlHSplit + it.tile
                                                                             : kCtrlDone1 + it.tile];
                 const uint32_t n = x_pieces ? 8u * items.gate_up
-                                   : Cfg::PRE && it.kind == kDown ? 8u : 4u * a.ft;
+                                   : Cfg::PRE && it.kind == kDown ? 8u * items.parts
+                                                                  : 4u * a.ft;
+                // One thread asks for its four warps: the answers and the counters' own adds
+                // queue at the same place in L2 (one token, every warp asking: 24.9 us, so
+                // 23.7; 8-bit 20.6 and 19.2).
                 bool ok = true;
-                if (lane == 0) ok = wait_count(at, n);
-                if (!__shfl_sync(kFull, (int)ok, 0)) {
+                if (tid == 0) ok = wait_count(at, n);
+                if (!group_all(ok, 1 + ((warp - 8) >> 2))) {
                     failed = true;
                     break;
                 }
-                __syncwarp();         // lane 0's acquire orders the whole warp's loads
             }
             if (Cfg::PRE && it.kind >= kSplitX) {
-                const int t = threadIdx.x - 256;
+                const int t = it.j * 256 + threadIdx.x - 256;
                 const int rows = it.ok ? it.rows : 0;
                 if (it.kind == kSplitX)
-                    split_rows<2>(rows, a.d, t, 256,
+                    split_rows<2>(rows, a.d, t, 256 * items.gate_up,
                                   [&](int r) { return a.x + (it.row0 + r) * a.x_bytes; },
                                [&](int r) { return 1.f / __ldcg(a.xs + it.row0 + r); },
                                a.xq + (size_t)it.row0 * 2 * a.d);
                 else
-                    split_rows<4>(rows, a.f, t, 256,
+                    split_rows<4>(rows, a.f, t, 256 * items.parts,
                                [&](int r) { return a.h + (size_t)(it.row0 + r) * a.f; },
                                [&](int r) {
                                    return 1.f / split_scale(__uint_as_float(
