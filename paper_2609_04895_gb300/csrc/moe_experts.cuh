@@ -109,6 +109,8 @@ struct MoeArgs {
 };
 
 // All of 128 threads, with their writes and reads before it ordered before those after.
+// It has no limit of its own: every warp of a group makes the same calls, and one last
+// call when it has ended or given up, after which (all false) nobody makes another.
 __device__ __forceinline__ bool group_all(bool ok, int id) {
     uint32_t all;
     asm volatile(
@@ -901,9 +903,10 @@ __global__ void __launch_bounds__(kMoeThreads, 1)
         RowRing<W8, NT> ring((warp - 8) >> 2);
         int islot = 0, base = 0;
         uint32_t iphase = 0;
-        bool failed = false;
+        bool failed = false, apart = true;   // apart: the group does not know of it yet
+        const int group = 1 + ((warp - 8) >> 2);
         while (true) {
-            if (!mbar_wait(&s.i_full[islot], iphase)) {
+            if (!__all_sync(kFull, mbar_wait(&s.i_full[islot], iphase))) {
                 failed = true;
                 break;
             }
@@ -930,8 +933,9 @@ __global__ void __launch_bounds__(kMoeThreads, 1)
                 // 23.7; 8-bit 20.6 and 19.2).
                 bool ok = true;
                 if (tid == 0) ok = wait_count(at, n);
-                if (!group_all(ok, 1 + ((warp - 8) >> 2))) {
+                if (!group_all(ok, group)) {
                     failed = true;
+                    apart = false;
                     break;
                 }
             }
@@ -996,12 +1000,13 @@ __global__ void __launch_bounds__(kMoeThreads, 1)
             else
                 ok = produce_rows<W8, NT, Cfg::PRE ? kPieces : kSplitF>(s, src, inv, have, n8, base,
                                                                         kb, K, tid, ring);
-            if (!ok) {
+            if (!__all_sync(kFull, ok)) {
                 failed = true;
                 break;
             }
             base += kb;
         }
+        if (apart) group_all(!failed, group);
         if (failed && lane == 0) latch_error(a.err, CRC_ETIMEOUT);
     } else if (warp >= 4) {
         // ------------------------------------------------------ epilogue
