@@ -25,7 +25,7 @@
 // What bounds it is memory: 64 Qwen3-shaped tokens read 1208 MB in 178 us, 6.8 TB/s; a
 // call is 8 us longer before the first block (routing, tables) and 3 behind the last.
 // One token (75 MB, 24 us with its routing) is a chain of latencies: weights 8 us, h to
-// the other CTAs 4, y and its sum 4.
+// the other CTAs 3, y and its sum 4.
 //
 // Rows wider than the weights go in two pieces, hi and lo, as two columns of the same
 // product (columns cost nothing: an MMA reads 128 weight rows for 16 as for 64).  h is
@@ -49,8 +49,8 @@ namespace crc {
 constexpr int kMoeThreads = 512;     // warps 0 TMA, 1 MMA, 2-3 idle, 4-7 epilogue, 8-15 rows
 constexpr int kMoeMaxTiles = 256;    // row tiles of NT: N + M K / NT at most, M K <= 128 NT
 constexpr int kItemRing = 4;
-// Control words: the next item; phase-2 warps done; warps done splitting x; phase-1
-// warps done and warps done splitting h, by row tile.
+// Control words: the next item; phase-2 items done; warps done splitting x; phase-1
+// items done and warps done splitting h, by row tile.
 constexpr int kCtrlNext = 0, kCtrlDone2 = 1, kCtrlXSplit = 2, kCtrlDone1 = 3;
 constexpr int kCtrlHSplit = kCtrlDone1 + kMoeMaxTiles;
 constexpr int kCtrlWords = kCtrlHSplit + kMoeMaxTiles;
@@ -203,6 +203,15 @@ __device__ __forceinline__ uint32_t ld_acquire(const uint32_t* p) {
     asm volatile("ld.acquire.gpu.global.u32 %0, [%1];" : "=r"(v) : "l"(p) : "memory");
     return v;
 }
+// Adds one to a word in shared memory; acquires what was released there before.
+__device__ __forceinline__ uint32_t add_cta(uint32_t* p) {
+    uint32_t was;
+    asm volatile("atom.acq_rel.cta.shared::cta.add.u32 %0, [%1], 1;"
+                 : "=r"(was)
+                 : "r"(smem_u32(p))
+                 : "memory");
+    return was;
+}
 // Wait until *p reaches n; false on timeout.
 __device__ __forceinline__ bool wait_count(const uint32_t* p, uint32_t n) {
     if (ld_acquire(p) >= n) return true;
@@ -287,6 +296,7 @@ struct MoeShared {
     uint64_t *a_full, *a_empty, *b_full, *t_full, *t_empty, *i_full, *i_empty, *drain;
     uint32_t* tmem_slot;
     int* items;
+    uint32_t* ended;       // [4] epilogue warps that have ended an item, by its turn
     float* hscale;         // [kItemRing][NT] scales of h's rows (8-bit weights)
     float* few_gates;      // [kFewChoices]
     uint8_t* few_ids;      // [kFewChoices]
@@ -310,7 +320,8 @@ struct MoeShared {
         drain = i_empty + kItemRing;
         tmem_slot = reinterpret_cast<uint32_t*>(drain + 1);
         items = reinterpret_cast<int*>(tmem_slot + 1);
-        static_assert((2 * Cfg::SA + Cfg::SB + 4 + 2 * kItemRing + 1) * 8 + 4 + 4 * kItemRing <=
+        ended = reinterpret_cast<uint32_t*>(items + kItemRing);
+        static_assert((2 * Cfg::SA + Cfg::SB + 4 + 2 * kItemRing + 1) * 8 + 20 + 4 * kItemRing <=
                           Cfg::BAR_BYTES,
                       "barrier space");
         slot = reinterpret_cast<int*>(p + Cfg::BAR_BYTES);
@@ -720,6 +731,7 @@ __global__ void __launch_bounds__(kMoeThreads, 1)
             mbar_init(&s.i_full[i], 1);
             mbar_init(&s.i_empty[i], 13);        // MMA, 4 epilogue, 8 row warps
         }
+        for (int i = 0; i < 4; ++i) s.ended[i] = 0;
         mbar_init(s.drain, 1);
         fence_mbar_init();
         tma_prefetch_desc(&map13);
@@ -927,7 +939,7 @@ __global__ void __launch_bounds__(kMoeThreads, 1)
                                                                             : kCtrlDone1 + it.tile];
                 const uint32_t n = x_pieces ? 8u * items.gate_up
                                    : Cfg::PRE && it.kind == kDown ? 8u * items.parts
-                                                                  : 4u * a.ft;
+                                                                  : (uint32_t)a.ft;
                 // One thread asks for its four warps: the answers and the counters' own adds
                 // queue at the same place in L2 (one token, every warp asking: 24.9 us, so
                 // 23.7; 8-bit 20.6 and 19.2).
@@ -1011,7 +1023,7 @@ __global__ void __launch_bounds__(kMoeThreads, 1)
     } else if (warp >= 4) {
         // ------------------------------------------------------ epilogue
         const int quarter = warp & 3;
-        int islot = 0, acc = 0;
+        int islot = 0, acc = 0, turn = 0;
         uint32_t iphase = 0, aphase = 0;
         bool failed = false;
         while (true) {
@@ -1146,7 +1158,10 @@ __global__ void __launch_bounds__(kMoeThreads, 1)
             acc ^= 1;
             if (acc == 0) aphase ^= 1;
             __syncwarp();
-            if (lane == 0) add_release(&a.ctrl[down ? kCtrlDone2 : kCtrlDone1 + it.tile]);
+            // the last of the four warps adds for all
+            if (lane == 0 && add_cta(&s.ended[turn & 3]) % 4 == 3)
+                add_release(&a.ctrl[down ? kCtrlDone2 : kCtrlDone1 + it.tile]);
+            ++turn;
         }
         if (failed && lane == 0) latch_error(a.err, CRC_ETIMEOUT);
     }
@@ -1168,7 +1183,7 @@ __global__ void __launch_bounds__(kMoeThreads, 1)
     Gates gates;
     if (i < all) gates.load(a, s, tok * a.K, a.K);
     if (threadIdx.x == 0) {
-        const bool ok = wait_count(&a.ctrl[kCtrlDone2], 4u * (uint32_t)(tiles * a.dt));
+        const bool ok = wait_count(&a.ctrl[kCtrlDone2], (uint32_t)(tiles * a.dt));
         if (!ok) latch_error(a.err, CRC_ETIMEOUT);
         s.items[0] = ok;
     }
