@@ -447,8 +447,9 @@ int crc_transfer_replay(const crc_problem *p, const crc_transfer *plan, int64_t 
 
 /* Element types.  CRC_E4M3 (sign, 4 exponent, 3 mantissa bits; largest value
  * 448, no infinities) always comes with one fp32 scale a row: a row stands
- * for q * scale, scale = max |row| / 448 as this library writes it (1 for a
- * row of zeros; a NaN or an infinity in the row goes on to the scale). */
+ * for q * scale, scale = max |row| / 448 as this library writes it (1 where
+ * that is zero in fp32: a row of zeros, or of values below 3.2e-43; a NaN or an
+ * infinity in the row goes on to the scale). */
 enum { CRC_BF16 = 1, CRC_F32 = 2, CRC_E4M3 = 3 };
 
 /* Root-mean-square norm of M rows of d elements, with the residual's addition:

@@ -139,10 +139,11 @@ __device__ __forceinline__ float row_reduce(float v, float* buf, const RowTeam& 
     return v;
 }
 
-// The row's scale.  A row of zeros has scale 1; a NaN or an infinity in it goes on to the
-// scale.
+// The row's scale.  A row of zeros has scale 1, as has one so small that the quotient is
+// zero (which would make NaN of the row's zeros); a NaN or an infinity goes on to the scale.
 __device__ __forceinline__ float row_scale(float amax) {
-    return amax == 0.f ? 1.f : amax / kE4m3Max;
+    const float s = amax / kE4m3Max;
+    return s == 0.f ? 1.f : s;
 }
 // e4m3(y / scale) of a row's values, the quotient that of a division: v = y inv(scale) is
 // off by less than two units of its last place, and Markstein's correction

@@ -50,3 +50,16 @@ def test_every_bf16_against_scales_of_many_rows(P):
         q, sc = P.quantize_rows(x)
         assert torch.equal(sc, (top[:, 0].double() / 448.0).float())
         assert torch.equal(bits(q), bits((x.float() / sc[:, None]).to(torch.float8_e4m3fn)))
+
+
+def test_a_row_too_small_for_a_scale_is_zero(P):
+    """max |y| / 448 is zero in fp32 below 3.2e-43: the zeros of such a row stay zeros."""
+    d = 256
+    x = torch.zeros((3, d), device="cuda")
+    x[0, ::3], x[1, 5], x[2] = 1e-3, -1e-3, 1.0
+    w = torch.ones(d, dtype=torch.int16, device="cuda").view(torch.bfloat16)       # 9.2e-41
+    q = torch.empty((3, d), dtype=torch.float8_e4m3fn, device="cuda")
+    sc, h = torch.empty(3, device="cuda"), torch.empty((3, d), dtype=torch.bfloat16, device="cuda")
+    P.rms_norm(x, w, 1.0, out=h, out8=q, scale8=sc)
+    assert (sc[:2] == 1.0).all() and (q[:2].float() == 0).all()
+    assert 0.0 < float(sc[2]) < 1e-42 and (q[2].float() > 400).all()
