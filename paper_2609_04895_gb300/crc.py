@@ -175,6 +175,37 @@ def _ptr(t) -> int:
     return t.data_ptr()
 
 
+def _on(stream, device):
+    """`stream` (None: the current one) as a torch stream, None for the current one."""
+    if stream is None:
+        return None
+    import torch
+    ptr = _stream(stream)
+    current = torch.cuda.current_stream(device)
+    if ptr == current.cuda_stream:
+        return None
+    if isinstance(stream, torch.cuda.Stream):
+        return stream
+    if ptr == 0:
+        return torch.cuda.default_stream(device)
+    return torch.cuda.ExternalStream(ptr, device)
+
+
+def _new(stream, device, shape, dtype, zeros: bool = False):
+    """A tensor that a call on `stream` writes.  It comes from that stream's pool: what was
+    in its memory before is used up when the call's kernels run, and after the caller's
+    last reference the memory waits for them.  The current stream may read it too."""
+    import torch
+    make = torch.zeros if zeros else torch.empty
+    on = _on(stream, device)
+    if on is None:
+        return make(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(on):
+        t = make(shape, dtype=dtype, device=device)
+    t.record_stream(torch.cuda.current_stream(device))
+    return t
+
+
 # --------------------------------------------------------------------------- #
 # C-ABI names
 # --------------------------------------------------------------------------- #
@@ -406,6 +437,10 @@ def crc_moe_layer(m: crc_moe, x_ptr, x_stride: int, x8_ptr, x8_scale_ptr, scores
 
 # --------------------------------------------------------------------------- #
 # torch conveniences (allocation and marshalling only)
+#
+# `stream`: a torch stream or a raw handle; None is the current one.  Tensors that are
+# made for a call (outputs, workspaces) come from its stream's pool and may be read on
+# the current stream; tensors that are passed in are the caller's to keep and to order.
 # --------------------------------------------------------------------------- #
 def problem(L, N, K, d, C, R, B, expert_bytes) -> crc_problem:
     return crc_problem(L=L, N=N, K=K, d=d, C=C, R=R, B=B, reserved=0,
@@ -426,7 +461,7 @@ class State:
         self.nbytes = crc_state_bytes(p)
         if self.nbytes == 0:
             raise CrcError(CRC_EINVAL, "crc_state_bytes")
-        self.buf = torch.empty(self.nbytes, dtype=torch.uint8, device=device)
+        self.buf = _new(stream, torch.device(device), self.nbytes, torch.uint8)
         assert self.buf.data_ptr() % 256 == 0
         self.init(stream)
 
@@ -509,7 +544,7 @@ def route_scores(p: crc_problem, hidden, w_cat, heads: int = 3, out=None, stream
     import torch
     B, T, L, d = hidden.shape
     if out is None:
-        out = torch.empty((B, T, L, 3, p.N), dtype=torch.float32, device=hidden.device)
+        out = _new(stream, hidden.device, (B, T, L, 3, p.N), torch.float32)
     crc_route_scores(p, hidden.data_ptr(), w_cat.data_ptr(), T, heads, out.data_ptr(), stream)
     return out
 
@@ -540,14 +575,13 @@ def cache_loss(p: crc_problem, probs, top_b: int, tau: float, w_T: float = 1.0,
     B, T, L, H, N = probs.shape
     dev = probs.device
     if loss is None:
-        loss = torch.empty((B, T, L, 2), dtype=torch.float32, device=dev)
+        loss = _new(stream, dev, (B, T, L, 2), torch.float32)
     if means is None:
-        means = torch.empty(2, dtype=torch.float64, device=dev)
+        means = _new(stream, dev, 2, torch.float64)
     if grad and grad_out is None:
-        grad_out = torch.zeros((B, T, L, 3, N), dtype=torch.float32, device=dev)
+        grad_out = _new(stream, dev, (B, T, L, 3, N), torch.float32, zeros=True)
     if workspace is None:
-        workspace = torch.empty(max(crc_loss_workspace_bytes(p, T), 256), dtype=torch.uint8,
-                                device=dev)
+        workspace = _new(stream, dev, max(crc_loss_workspace_bytes(p, T), 256), torch.uint8)
     crc_cache_loss(p, probs.data_ptr(), T, heads, top_b, tau, w_T, w_ST, loss.data_ptr(),
                    means.data_ptr(), grad_out.data_ptr() if grad else None, workspace.data_ptr(),
                    workspace.numel(), stream)
@@ -559,8 +593,7 @@ def route_and_cache(p: crc_problem, hidden, w_cat, state: State, trace: Trace | 
     T = hidden.size(1)
     if workspace is None:
         import torch
-        workspace = torch.empty(crc_workspace_bytes(p, T), dtype=torch.uint8,
-                                device=hidden.device)
+        workspace = _new(stream, hidden.device, crc_workspace_bytes(p, T), torch.uint8)
     crc_route_and_cache(p, hidden.data_ptr(), w_cat.data_ptr(), T, state.buf.data_ptr(),
                         state.nbytes, None if trace is None else trace.c(),
                         workspace.data_ptr(), workspace.nbytes, stream)
@@ -579,9 +612,9 @@ def route_and_cache_host(p: crc_problem, hidden_host, w_cat, state: State, chunk
     dev = w_cat.device
     chunk = max(1, min(chunk_tokens, T))
     if staging is None:
-        staging = torch.empty(crc_host_staging_bytes(p, chunk), dtype=torch.uint8, device=dev)
+        staging = _new(stream, dev, crc_host_staging_bytes(p, chunk), torch.uint8)
     if workspace is None:
-        workspace = torch.empty(crc_fused_workspace_bytes(p), dtype=torch.uint8, device=dev)
+        workspace = _new(stream, dev, crc_fused_workspace_bytes(p), torch.uint8)
     crc_route_and_cache_host(p, hidden_host.data_ptr(), w_cat.data_ptr(), T, chunk_tokens,
                              state.ptr, state.nbytes, staging.data_ptr(),
                              staging.numel() * staging.element_size(), workspace.data_ptr(),
@@ -591,7 +624,7 @@ def route_and_cache_host(p: crc_problem, hidden_host, w_cat, state: State, chunk
 
 def synth_weights(L, N, d, seed=0, copy_init=False, device="cuda", stream=None):
     import torch
-    w = torch.empty((L, 3 * N, d), dtype=torch.bfloat16, device=device)
+    w = _new(stream, torch.device(device), (L, 3 * N, d), torch.bfloat16)
     crc_synth_weights(L, N, d, seed, copy_init, w.data_ptr(), stream)
     return w
 
@@ -601,9 +634,9 @@ def synth_hidden(B, T, L, d, seed=0, rho_t=0.9, rho_l=0.8, t0=0, carry=None, att
     """Tokens [t0, t0+T) of the synthetic hidden-state field; returns (hidden, carry)."""
     import torch
     if out is None:
-        out = torch.empty((B, T, L, d), dtype=torch.bfloat16, device=device)
+        out = _new(stream, torch.device(device), (B, T, L, d), torch.bfloat16)
     if carry is None:
-        carry = torch.zeros((B, L, d), dtype=torch.float32, device=device)
+        carry = _new(stream, torch.device(device), (B, L, d), torch.float32, zeros=True)
     crc_synth_hidden(B, T, L, d, t0, seed, rho_t, rho_l, _ptr(attempts), out.data_ptr(),
                      carry.data_ptr(), stream)
     return out, carry
@@ -652,7 +685,7 @@ def rms_norm(x, weight, eps: float = 1e-6, residual=None, residual_out=None, out
     bf16, f32, dtype = torch.bfloat16, torch.float32, x.dtype
     M, d, ldx = _rows(x, "x")
     if out is None and out8 is None:
-        out = torch.empty((M, d), dtype=bf16, device=x.device)
+        out = _new(stream, x.device, (M, d), bf16)
     rows = x.shape
     rc = load().crc_rms_norm(
         x.data_ptr(), ldx, _check(residual, "residual", rows, dtype),
@@ -673,12 +706,11 @@ def rms_norm_grad(dy, s, weight, rstd, dres=None, dx=None, dw=None, want_dw: boo
     M, d = rows = dy.shape
     bf16, f32 = torch.bfloat16, torch.float32
     if dx is None:
-        dx = torch.empty_like(s)
+        dx = _new(stream, s.device, s.shape, s.dtype)
     if want_dw and dw is None:
-        dw = torch.empty(d, dtype=f32, device=dy.device)
+        dw = _new(stream, dy.device, d, f32)
     if dw is not None and workspace is None:
-        workspace = torch.empty(crc_rms_norm_grad_workspace_bytes(M, d), dtype=torch.uint8,
-                                device=dy.device)
+        workspace = _new(stream, dy.device, crc_rms_norm_grad_workspace_bytes(M, d), torch.uint8)
     crc_rms_norm_grad(_check(dy, "dy", rows, bf16), _check(s, "s", rows, s.dtype),
                       _check(weight, "weight", (d,), bf16), _check(rstd, "rstd", (M,), f32),
                       _check(dres, "dres", rows, s.dtype), _stream_type(s), M, d,
@@ -700,9 +732,9 @@ def quantize_rows(x, out8=None, scale=None, stream=None):
         x = x.reshape(-1, d)
     M, d, ldx = _rows(x, "x")
     if out8 is None:
-        out8 = torch.empty((*lead, d), dtype=torch.float8_e4m3fn, device=x.device)
+        out8 = _new(stream, x.device, (*lead, d), torch.float8_e4m3fn)
     if scale is None:
-        scale = torch.empty(lead, dtype=torch.float32, device=x.device)
+        scale = _new(stream, x.device, lead, torch.float32)
     crc_quantize_rows(x.data_ptr(), ldx, M, d,
                       _check(out8, "out8", (*lead, d), torch.float8_e4m3fn),
                       _check(scale, "scale", lead, torch.float32), stream)
@@ -792,9 +824,9 @@ class MoeLayer:
         if scores is not None:
             lds = max(_rows(scores, "scores")[2], self.N)
         if out is None:
-            out = torch.empty(rows, dtype=torch.bfloat16, device=src.device)
+            out = _new(stream, src.device, rows, torch.bfloat16)
         if workspace is None:
-            workspace = torch.empty(self.workspace_bytes(M), dtype=torch.uint8, device=src.device)
+            workspace = _new(stream, src.device, self.workspace_bytes(M), torch.uint8)
         rc = load().crc_moe_layer(
             self._ref, _check(x, "x", rows, torch.bfloat16, False), ldx,
             _check(x8, "x8", rows, torch.float8_e4m3fn), _check(x_scale, "x_scale", (M,), f32),
