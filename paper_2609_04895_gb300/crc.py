@@ -820,9 +820,7 @@ class MoeLayer:
             raise ValueError("x or x8 is wanted")
         M, _, ldx = _rows(src, "x")
         rows, f32 = (M, self.d), torch.float32
-        lds = 0
-        if scores is not None:
-            lds = max(_rows(scores, "scores")[2], self.N)
+        lds = 0 if scores is None else _rows(scores, "scores")[2]
         if out is None:
             out = _new(stream, src.device, rows, torch.bfloat16)
         if workspace is None:
