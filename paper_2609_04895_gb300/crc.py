@@ -651,23 +651,43 @@ def _stream_type(t) -> int:
     raise ValueError(f"the residual stream is bfloat16 or float32, not {t.dtype}")
 
 
-def _check(t, name: str, shape, dtype, dense: bool = True):
-    """The address of a tensor argument of the stated shape and type on the GPU, or
+def _here(t, name: str) -> int:
+    """The current device, where calls are launched; `t` has to lie there."""
+    import torch
+    dev = t.get_device()
+    if dev < 0:
+        raise ValueError(f"{name} must be a CUDA tensor")
+    if dev != torch.cuda.current_device():
+        raise ValueError(f"{name} lies on {t.device}, which is not the current device")
+    return dev
+
+
+def _check(t, name: str, shape, dtype, dev: int, dense: bool = True):
+    """The address of a tensor argument of the stated shape and type on device `dev`, or
     None.  (Short on purpose: a one-row norm has six of them, and takes the GPU 2 us.)"""
     if t is None:
         return None
-    if t.dtype is not dtype or t.shape != shape or not t.is_cuda:
-        raise ValueError(f"{name}: a {dtype} CUDA tensor of shape {tuple(shape)} is wanted, "
-                         f"got {t.dtype} {tuple(t.shape)} on {t.device}")
+    if t.dtype is not dtype or t.shape != shape or t.get_device() != dev:
+        raise ValueError(f"{name}: a {dtype} tensor of shape {tuple(shape)} on cuda:{dev} is "
+                         f"wanted, got {t.dtype} {tuple(t.shape)} on {t.device}")
     if dense and not t.is_contiguous():
         raise ValueError(f"{name} must be contiguous")
     return t.data_ptr()
 
 
+def _workspace(t, dev: int):
+    """Address and bytes of a workspace: any contiguous tensor on device `dev`."""
+    if t is None:
+        return None, 0
+    if t.get_device() != dev or not t.is_contiguous():
+        raise ValueError(f"workspace must be a contiguous tensor on cuda:{dev}")
+    return t.data_ptr(), t.nbytes
+
+
 def _rows(t, name: str):
     """(rows, elements a row, elements between rows) of a 2-D tensor."""
-    if t.dim() != 2 or not t.is_cuda:
-        raise ValueError(f"{name} must be a 2-D CUDA tensor")
+    if t.dim() != 2:
+        raise ValueError(f"{name} must be a 2-D tensor")
     M, d = t.shape
     if t.stride(1) != 1 and d != 1:
         raise ValueError(f"the rows of {name} must be contiguous")
@@ -683,16 +703,18 @@ def rms_norm(x, weight, eps: float = 1e-6, residual=None, residual_out=None, out
     residual_out and the rows' statistic to rstd (fp32 [M]).  Returns out."""
     import torch
     bf16, f32, dtype = torch.bfloat16, torch.float32, x.dtype
+    dev = _here(x, "x")
     M, d, ldx = _rows(x, "x")
     if out is None and out8 is None:
         out = _new(stream, x.device, (M, d), bf16)
     rows = x.shape
     rc = load().crc_rms_norm(
-        x.data_ptr(), ldx, _check(residual, "residual", rows, dtype),
-        _check(weight, "weight", (d,), bf16), _stream_type(x), M, d, eps,
-        _check(residual_out, "residual_out", rows, dtype), _check(out, "out", rows, bf16),
-        _check(out8, "out8", rows, torch.float8_e4m3fn), _check(scale8, "scale8", (M,), f32),
-        _check(rstd, "rstd", (M,), f32), _stream(stream))
+        x.data_ptr(), ldx, _check(residual, "residual", rows, dtype, dev),
+        _check(weight, "weight", (d,), bf16, dev), _stream_type(x), M, d, eps,
+        _check(residual_out, "residual_out", rows, dtype, dev), _check(out, "out", rows, bf16, dev),
+        _check(out8, "out8", rows, torch.float8_e4m3fn, dev),
+        _check(scale8, "scale8", (M,), f32, dev), _check(rstd, "rstd", (M,), f32, dev),
+        _stream(stream))
     if rc:
         raise CrcError(rc, "crc_rms_norm")
     return out
@@ -704,6 +726,7 @@ def rms_norm_grad(dy, s, weight, rstd, dres=None, dx=None, dw=None, want_dw: boo
     forward call, and dres, the gradient that arrives at s directly."""
     import torch
     M, d = rows = dy.shape
+    dev = _here(dy, "dy")
     bf16, f32 = torch.bfloat16, torch.float32
     if dx is None:
         dx = _new(stream, s.device, s.shape, s.dtype)
@@ -711,11 +734,12 @@ def rms_norm_grad(dy, s, weight, rstd, dres=None, dx=None, dw=None, want_dw: boo
         dw = _new(stream, dy.device, d, f32)
     if dw is not None and workspace is None:
         workspace = _new(stream, dy.device, crc_rms_norm_grad_workspace_bytes(M, d), torch.uint8)
-    crc_rms_norm_grad(_check(dy, "dy", rows, bf16), _check(s, "s", rows, s.dtype),
-                      _check(weight, "weight", (d,), bf16), _check(rstd, "rstd", (M,), f32),
-                      _check(dres, "dres", rows, s.dtype), _stream_type(s), M, d,
-                      _check(dx, "dx", rows, s.dtype), _check(dw, "dw", (d,), f32),
-                      _ptr(workspace), 0 if workspace is None else workspace.nbytes, stream)
+    crc_rms_norm_grad(_check(dy, "dy", rows, bf16, dev), _check(s, "s", rows, s.dtype, dev),
+                      _check(weight, "weight", (d,), bf16, dev),
+                      _check(rstd, "rstd", (M,), f32, dev),
+                      _check(dres, "dres", rows, s.dtype, dev), _stream_type(s), M, d,
+                      _check(dx, "dx", rows, s.dtype, dev), _check(dw, "dw", (d,), f32, dev),
+                      *_workspace(workspace, dev), stream)
     return dx, dw
 
 
@@ -725,6 +749,7 @@ def quantize_rows(x, out8=None, scale=None, stream=None):
     import torch
     if x.dtype != torch.bfloat16:
         raise ValueError("x must be bfloat16")
+    dev = _here(x, "x")
     lead, d = x.shape[:-1], x.shape[-1]
     if x.dim() != 2:
         if not x.is_contiguous():
@@ -736,8 +761,8 @@ def quantize_rows(x, out8=None, scale=None, stream=None):
     if scale is None:
         scale = _new(stream, x.device, lead, torch.float32)
     crc_quantize_rows(x.data_ptr(), ldx, M, d,
-                      _check(out8, "out8", (*lead, d), torch.float8_e4m3fn),
-                      _check(scale, "scale", lead, torch.float32), stream)
+                      _check(out8, "out8", (*lead, d), torch.float8_e4m3fn, dev),
+                      _check(scale, "scale", lead, torch.float32, dev), stream)
     return out8, scale
 
 
@@ -771,26 +796,27 @@ class MoeLayer:
         kinds = {torch.bfloat16: BF16, torch.float8_e4m3fn: E4M3}
         if gate_up.dtype not in kinds or not gate_up.is_cuda:
             raise ValueError("gate_up must be a bfloat16 or float8_e4m3fn CUDA tensor")
-        _check(down, "down", (slots, d, f), gate_up.dtype, dense=False)
+        dev = gate_up.get_device()
+        _check(down, "down", (slots, d, f), gate_up.dtype, dev, dense=False)
         if gate_up.stride()[1:] != (f * d, d, 1) or down.stride()[1:] != (f, 1):
             raise ValueError("an expert's matrices must be contiguous")
         if N is None:
             N = (router.shape[0] if router is not None else
                  expert_slot.shape[0] if expert_slot is not None else slots)
-        _check(router, "router", (N, d), torch.bfloat16)
-        _check(expert_slot, "expert_slot", (N,), torch.int32)
+        _check(router, "router", (N, d), torch.bfloat16, dev)
+        _check(expert_slot, "expert_slot", (N,), torch.int32, dev)
         if expert_slot is None and N > slots:
             raise ValueError("more experts than slots: an expert_slot map is wanted")
         for t, name, shape in ((gate_up_scale, "gate_up_scale", (slots, 2, f)),
                                (down_scale, "down_scale", (slots, d))):
             if (t is None) != (gate_up.dtype == torch.bfloat16):
                 raise ValueError(f"{name} belongs to 8-bit experts")
-            _check(t, name, shape, torch.float32, dense=False)
+            _check(t, name, shape, torch.float32, dev, dense=False)
         if gate_up_scale is not None and (gate_up_scale.stride()[1:] != (f, 1)
                                           or down_scale.stride(1) != 1):
             raise ValueError("an expert's scales must be contiguous")
         es = gate_up.element_size()
-        self.N, self.K, self.d, self.f = N, K, d, f
+        self.N, self.K, self.d, self.f, self.device = N, K, d, f, dev
         self.tensors = (gate_up, down, router, expert_slot, gate_up_scale, down_scale)
         self.c = crc_moe(N=N, K=K, d=d, f=f, slots=slots, weight_type=kinds[gate_up.dtype],
                          renormalize=int(renormalize), reserved=0,
@@ -818,6 +844,9 @@ class MoeLayer:
         src = x if x is not None else x8
         if src is None:
             raise ValueError("x or x8 is wanted")
+        dev = _here(src, "x")
+        if dev != self.device:
+            raise ValueError(f"x lies on cuda:{dev}, the experts on cuda:{self.device}")
         M, _, ldx = _rows(src, "x")
         rows, f32 = (M, self.d), torch.float32
         lds = 0 if scores is None else _rows(scores, "scores")[2]
@@ -826,12 +855,13 @@ class MoeLayer:
         if workspace is None:
             workspace = _new(stream, src.device, self.workspace_bytes(M), torch.uint8)
         rc = load().crc_moe_layer(
-            self._ref, _check(x, "x", rows, torch.bfloat16, False), ldx,
-            _check(x8, "x8", rows, torch.float8_e4m3fn), _check(x_scale, "x_scale", (M,), f32),
-            _check(scores, "scores", (M, self.N), f32, False), lds, M,
-            _check(out, "out", rows, torch.bfloat16),
-            _check(topk, "topk", (M, self.K), torch.uint8),
-            _check(gates, "gates", (M, self.K), f32), workspace.data_ptr(), workspace.nbytes,
+            self._ref, _check(x, "x", rows, torch.bfloat16, dev, False), ldx,
+            _check(x8, "x8", rows, torch.float8_e4m3fn, dev),
+            _check(x_scale, "x_scale", (M,), f32, dev),
+            _check(scores, "scores", (M, self.N), f32, dev, False), lds, M,
+            _check(out, "out", rows, torch.bfloat16, dev),
+            _check(topk, "topk", (M, self.K), torch.uint8, dev),
+            _check(gates, "gates", (M, self.K), f32, dev), *_workspace(workspace, dev),
             _stream(stream))
         if rc:
             raise CrcError(rc, "crc_moe_layer")
