@@ -238,7 +238,7 @@ KERNEL_SOURCES = {
                "crc_device.cuh"],
     "loss": ["loss.cu", "cache_scan.cuh", "crc_device.cuh"],
     "moe": ["moe.cu", "moe_experts.cuh", "moe_route.cuh", "pdl.cuh", "crc_device.cuh"],
-    "norm": ["norm.cu", "pdl.cuh", "crc_device.cuh"],
+    "norm": ["norm.cu", "row_team.cuh", "pdl.cuh", "crc_device.cuh"],
 }
 
 

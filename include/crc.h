@@ -561,7 +561,8 @@ int crc_moe_layer(const crc_moe *m, const uint16_t *x_dev, int64_t x_stride, con
                   void *workspace_dev, size_t workspace_bytes, void *stream);
 
 /* Synchronises the device and returns (then clears) the error latched by
- * calls without a state (crc_route_scores, crc_moe_layer), CRC_OK if none. */
+ * calls without a state (crc_route_scores, crc_rms_norm_grad, crc_moe_layer),
+ * CRC_OK if none. */
 int crc_device_error(void);
 
 /* Number of kernels the library has launched in this process. */

@@ -17,18 +17,13 @@
 #include "crc_device.cuh"
 #include "crc_internal.h"
 #include "pdl.cuh"
+#include "row_team.cuh"
 
 namespace crc {
 namespace {
 
 constexpr float kE4m3Max = 448.0f;
 constexpr int kMaxRow = 32768;       // 1024 threads x 4 groups of 8 elements
-
-__device__ __forceinline__ float max_nan(float a, float b) {   // a NaN stays
-    float r;
-    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
-    return r;
-}
 
 // Two fp32 operations an instruction, each rounded like its scalar form.
 __device__ __forceinline__ uint64_t pack2(float a, float b) {
@@ -104,39 +99,6 @@ __device__ __forceinline__ uint2 to_e4m3(const float (&f)[8]) {
             : "=h"(h[i])
             : "f"(f[2 * i + 1]), "f"(f[2 * i]));
     return make_uint2(h[0] | ((uint32_t)h[1] << 16), h[2] | ((uint32_t)h[3] << 16));
-}
-
-// The warps that share a row: `warps` of them, `id` the row's number in the CTA.
-struct RowTeam {
-    int warps, id, thread, threads;
-    __device__ __forceinline__ explicit RowTeam(int w)
-        : warps(w), id((threadIdx.x >> 5) / w), thread(threadIdx.x - id * 32 * w), threads(32 * w) {}
-    // the whole CTA
-    __device__ __forceinline__ RowTeam()
-        : warps(blockDim.x >> 5), id(0), thread(threadIdx.x), threads(blockDim.x) {}
-};
-
-// Sum (or NaN-keeping maximum) of v over a row's warps, in one fixed order; every
-// thread gets it.  `buf`: a float a warp of the CTA, not in use by an earlier
-// reduction that a thread may still be reading.
-template <bool MAX>
-__device__ __forceinline__ float row_reduce(float v, float* buf, const RowTeam& t) {
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) {
-        const float u = __shfl_xor_sync(0xffffffffu, v, o);
-        v = MAX ? max_nan(v, u) : v + u;
-    }
-    if (t.warps == 1) return v;
-    const int lane = threadIdx.x & 31;
-    if (lane == 0) buf[threadIdx.x >> 5] = v;
-    asm volatile("bar.sync %0, %1;" ::"r"(1 + t.id), "r"(t.threads) : "memory");
-    v = lane < t.warps ? buf[t.id * t.warps + lane] : 0.f;
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) {
-        const float u = __shfl_xor_sync(0xffffffffu, v, o);
-        v = MAX ? max_nan(v, u) : v + u;
-    }
-    return v;
 }
 
 // The row's scale.  A row of zeros has scale 1, as has one so small that the quotient is
@@ -375,6 +337,7 @@ __global__ void __launch_bounds__(THREADS, VPT == 1 ? 2 : 1) rms_norm_grad_kerne
     pdl_begin();
     __shared__ float red[2][32];
     __shared__ __align__(8) uint64_t bars[TEAMS ? kMaxGradTeams : 1][kMaxGradStages];
+    __shared__ uint32_t lost[2][TEAMS ? kMaxGradTeams : 1];    // row_tell's, by turns
     const RowTeam team = TEAMS ? RowTeam(a.warps) : RowTeam();
     const int d = a.d, nvec = d >> 3, teams = TEAMS ? blockDim.x / team.threads : 1;
     const long long first = (long long)blockIdx.x * teams + team.id, step = (long long)gridDim.x * teams;
@@ -393,6 +356,7 @@ __global__ void __launch_bounds__(THREADS, VPT == 1 ? 2 : 1) rms_norm_grad_kerne
     };
     if constexpr (RING) {
         if (team.thread == 0) {
+            lost[0][team.id] = lost[1][team.id] = 0u;
             for (int i = 0; i < a.stages; ++i) mbar_init(&full[i], 1);
             fence_mbar_init();
             long long row = first;
@@ -410,24 +374,14 @@ __global__ void __launch_bounds__(THREADS, VPT == 1 ? 2 : 1) rms_norm_grad_kerne
     const float inv_d = 1.f / (float)d;
     int flip = 0, stage = 0;
     uint32_t phase = 0;
-    bool failed = false;
+    bool arrived = true;
     for (long long row = first; row < a.M; row += step, flip ^= 1) {
         const float rstd = a.rstd[row];
         const __nv_bfloat16* dyp = a.dy + row * d;
         const T* sp = static_cast<const T*>(a.s) + row * d;
         const T* rp = static_cast<const T*>(a.dres) + (a.dres ? row * d : 0);
         if constexpr (RING) {
-            if (!mbar_wait(&full[stage], phase)) {         // the whole team waits, so all leave,
-                failed = true;                             // none with a copy on its way
-                for (int i = 1; i < a.stages && row + i * step < a.M; ++i) {
-                    if (++stage == a.stages) {
-                        stage = 0;
-                        phase ^= 1;
-                    }
-                    (void)mbar_wait(&full[stage], phase);
-                }
-                break;
-            }
+            arrived = row_tell(mbar_wait(&full[stage], phase), &lost[flip][team.id]);
             const uint8_t* at = ring + (size_t)stage * a.stage_bytes;
             dyp = reinterpret_cast<const __nv_bfloat16*>(at);
             sp = reinterpret_cast<const T*>(at + dy_bytes);
@@ -466,6 +420,20 @@ __global__ void __launch_bounds__(THREADS, VPT == 1 ? 2 : 1) rms_norm_grad_kerne
         const float c = row_reduce<false>(dot, red[flip], team) * inv_d;
         const uint64_t k2 = pack2(-rstd * c, -rstd * c);
         if constexpr (RING) {
+            arrived = row_all(arrived, &lost[flip][team.id], team);
+            if (!arrived) {
+                // all of the team leave here, none with a copy on its way: rows up to
+                // stages - 2 ahead are asked for, one more at the first
+                const int asked = a.stages - (row != first);
+                for (int i = 0; i < asked && row + i * step < a.M; ++i) {
+                    (void)mbar_wait(&full[stage], phase);
+                    if (++stage == a.stages) {
+                        stage = 0;
+                        phase ^= 1;
+                    }
+                }
+                break;
+            }
             // every thread of the team is past the row before this one
             const int before = (stage ? stage : a.stages) - 1;
             const long long next = row + (a.stages - 1) * step;
@@ -494,7 +462,7 @@ __global__ void __launch_bounds__(THREADS, VPT == 1 ? 2 : 1) rms_norm_grad_kerne
             store8(static_cast<T*>(a.dx) + row * d + 8 * i, r);
         }
     }
-    if (failed) latch_error(a.err, CRC_ETIMEOUT);
+    if (!arrived) latch_error(a.err, CRC_ETIMEOUT);
     if (!a.part) return;
     // the teams' sums, in order, through the ring's memory; one team writes its own
     float* sums = reinterpret_cast<float*>(smem);
