@@ -139,6 +139,14 @@ __device__ __forceinline__ bool mbar_wait(uint64_t* bar, uint32_t parity,
     }
 }
 
+// As mbar_wait, for a whole warp that goes on together: one outcome for all lanes.  Each
+// has a clock of its own, and a phase that completes near the limit is seen by some lanes
+// and not by others; those must not part before a shuffle or a __syncwarp.
+__device__ __forceinline__ bool mbar_wait_warp(uint64_t* bar, uint32_t parity,
+                                               uint64_t limit_ns = kWaitLimitNs) {
+    return __all_sync(kFull, mbar_wait(bar, parity, limit_ns));
+}
+
 // As mbar_wait, with cluster-scope acquire: for phases completed from the
 // other CTA of a pair (remote arrivals, multicast commits).
 __device__ __forceinline__ bool mbar_try_wait_cluster(uint64_t* bar, uint32_t parity) {

@@ -619,7 +619,7 @@ __device__ __forceinline__ bool produce_rows(const MoeShared<W8, NT>& s, const u
         for (int i = 0; i < D; ++i) {
             const int k = k0 + 2 * i;
             if (k >= kb) break;
-            if (ring.next >= Cfg::SB && !mbar_wait(&s.a_empty[ring.free], ring.free_phase))
+            if (ring.next >= Cfg::SB && !mbar_wait_warp(&s.a_empty[ring.free], ring.free_phase))
                 return false;
             uint8_t* dst = s.b + ring.stage * Cfg::B_BYTES + (chunk >> 3) * Cfg::B_HALF;
 #pragma unroll
@@ -918,7 +918,7 @@ __global__ void __launch_bounds__(kMoeThreads, 1)
         bool failed = false, apart = true;   // apart: the group does not know of it yet
         const int group = 1 + ((warp - 8) >> 2);
         while (true) {
-            if (!__all_sync(kFull, mbar_wait(&s.i_full[islot], iphase))) {
+            if (!mbar_wait_warp(&s.i_full[islot], iphase)) {
                 failed = true;
                 break;
             }
@@ -1012,7 +1012,7 @@ __global__ void __launch_bounds__(kMoeThreads, 1)
             else
                 ok = produce_rows<W8, NT, Cfg::PRE ? kPieces : kSplitF>(s, src, inv, have, n8, base,
                                                                         kb, K, tid, ring);
-            if (!__all_sync(kFull, ok)) {
+            if (!ok) {
                 failed = true;
                 break;
             }
@@ -1027,7 +1027,7 @@ __global__ void __launch_bounds__(kMoeThreads, 1)
         uint32_t iphase = 0, aphase = 0;
         bool failed = false;
         while (true) {
-            if (!mbar_wait(&s.i_full[islot], iphase)) {
+            if (!mbar_wait_warp(&s.i_full[islot], iphase)) {
                 failed = true;
                 break;
             }
@@ -1066,7 +1066,7 @@ __global__ void __launch_bounds__(kMoeThreads, 1)
                     rs[u] = r < it.rows ? __ldcg(a.xs + s.list[it.row0 + r] / a.K) : 0.f;
                 }
             }
-            if (!mbar_wait(&s.t_full[acc], aphase)) {
+            if (!mbar_wait_warp(&s.t_full[acc], aphase)) {
                 failed = true;
                 break;
             }

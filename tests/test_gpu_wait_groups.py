@@ -48,3 +48,14 @@ def test_a_team_leaves_at_one_row(lib, threads, warps):
         assert lib.row_team_run(threads, warps, rows, ctypes.c_void_p(dev.data_ptr()),
                                 ctypes.c_void_p(left.data_ptr())) == 0
         assert torch.equal(left.cpu(), want)
+
+
+@pytest.mark.parametrize("few", [0, 1, 16, 31, 32])
+def test_a_warp_has_one_outcome(lib, few):
+    def run(together):
+        got = torch.full((32,), -7, dtype=torch.int32, device="cuda")
+        assert lib.warp_wait_run(few, together, ctypes.c_void_p(got.data_ptr())) == 0
+        return got.tolist()
+
+    assert run(0) == [0] * few + [1] * (32 - few)          # each lane on its own: they part
+    assert run(1) == [int(few == 0)] * 32
