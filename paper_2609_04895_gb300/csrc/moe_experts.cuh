@@ -497,7 +497,7 @@ enum { kGateUp = 0, kDown = 1, kSplitX = 2, kSplitH = 3 };
 struct MoeItem {
     int kind, tile, j;       // kGateUp: 64 elements of f; kDown: 128 elements of d;
     int e, row0, rows;       // kSplitX: all tokens; kSplitH: the tile's rows; j: the part of them
-    bool ok;                 // checking builds: within the arrays
+    bool ok;                 // checking builds: within the arrays (else nothing is written)
 };
 // First items of the kinds, in the order kSplitX, kGateUp, kSplitH, kDown.  Everything
 // that follows waits for the splits, so they are cut into items for all CTAs, x as a
@@ -554,6 +554,10 @@ __device__ __forceinline__ MoeItem moe_item(const MoeArgs& a, const MoeShared<W8
                               s.slot[it.e] < a.slots && it.rows > 0 && it.rows <= NT &&
                               it.row0 + it.rows <= a.M * a.K,
                           a.err);
+    if (!it.ok) {                    // what is read with it all the same is in the tables
+        it.e = it.row0 = 0;
+        it.rows = 1;
+    }
     return it;
 }
 
