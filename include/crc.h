@@ -548,11 +548,14 @@ typedef struct crc_moe {
  *   gates_dev  fp32 [M][K], g in rank order, or NULL
  *   workspace_dev  crc_moe_workspace_bytes(m, M) bytes, 256-byte aligned; calls
  *              that may overlap on the GPU need one each
- * Two kernels.  Products are summed in fp32; the product of silu and up enters the
- * second product in two pieces (bf16 weights: 16 significant bits of it; e4m3: two
- * e4m3 pieces, 6e-4 off), as does a bf16 x with e4m3 weights (exact down to 2^-13 of
- * the row's largest value); the K experts are summed in fp32 in rank
- * order and out is rounded once.  Results do not depend on the order in which
+ * Two kernels.  Products are summed in fp32.  h, the product of silu (in fp32, by
+ * the fast exponential and division) and up, enters the second product in two
+ * pieces: with bf16 weights 16 significant bits of it; with e4m3 weights two e4m3
+ * pieces, each element off by at most 2^-9 of itself and 2^-21 of its row's largest
+ * (6e-4 of itself in the mean square: the output is off by 1.8e-3 of itself where
+ * its own rounding alone is 1.7e-3).  So does a bf16 x with e4m3 weights (exact
+ * down to 2^-13 of the row's largest value).  The K experts are summed in fp32 in
+ * rank order and out is rounded once.  Results do not depend on the order in which
  * blocks run.  M = 0 is a no-op. */
 size_t crc_moe_workspace_bytes(const crc_moe *m, int32_t M);
 int crc_moe_layer(const crc_moe *m, const uint16_t *x_dev, int64_t x_stride, const uint8_t *x8_dev,

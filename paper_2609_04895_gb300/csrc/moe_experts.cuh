@@ -29,10 +29,11 @@
 //
 // Rows wider than the weights go in two pieces, hi and lo, as two columns of the same
 // product (columns cost nothing: an MMA reads 128 weight rows for 16 as for 64).  h is
-// kept in fp32 and multiplied as hi + lo in bf16 (16 significant bits); one bf16 would
-// double the error of the bf16 output.  With 8-bit weights a row is x / s = hi + lo / 16
-// in e4m3, s a power of two from the row's largest value: a bf16 x exactly down to
-// 2^-13 of that value, h to 6e-4.  No weight is converted.  With tiles of
+// kept in fp32 and multiplied as hi + lo in bf16 (16 significant bits); one bf16 made
+// the error of the bf16 output 1.4 times that of its own rounding.  With 8-bit weights a
+// row is x / s = hi + lo / 16 in e4m3, s a power of two from the row's largest value: a
+// bf16 x exactly down to 2^-13 of that value, h to 2^-9 of each element and 2^-21 of the
+// largest (6e-4 of an element in the mean square).  No weight is converted.  With tiles of
 // 16 rows the row warps split on the way into shared memory, for every item anew.  With
 // more rows that would bound the kernel (three conversions a pair of elements), so
 // rows are split once, by items of their own before either phase, and the pieces are
