@@ -158,12 +158,15 @@ def _ck(rc: int, what: str):
         raise CrcError(rc, what)
 
 
-def _stream(stream) -> int:
+def _stream(stream, dev: int | None = None) -> int:
+    """The raw handle; dev: the current device, where the caller has asked for it."""
     if stream is None:
         # the current stream's handle without the Stream object around it, which
         # took 3 of a one-token call's 13 us on the host
         import torch
-        return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
+        if dev is None:
+            dev = torch.cuda.current_device()
+        return torch._C._cuda_getCurrentRawStream(dev)
     if isinstance(stream, int):
         return stream
     return stream.cuda_stream
@@ -176,13 +179,10 @@ def _ptr(t) -> int:
 
 
 def _on(stream, device):
-    """`stream` (None: the current one) as a torch stream, None for the current one."""
-    if stream is None:
-        return None
+    """`stream` as a torch stream, None if it is the current one."""
     import torch
     ptr = _stream(stream)
-    current = torch.cuda.current_stream(device)
-    if ptr == current.cuda_stream:
+    if ptr == torch.cuda.current_stream(device).cuda_stream:
         return None
     if isinstance(stream, torch.cuda.Stream):
         return stream
@@ -197,7 +197,7 @@ def _new(stream, device, shape, dtype, zeros: bool = False):
     last reference the memory waits for them.  The current stream may read it too."""
     import torch
     make = torch.zeros if zeros else torch.empty
-    on = _on(stream, device)
+    on = None if stream is None else _on(stream, device)
     if on is None:
         return make(shape, dtype=dtype, device=device)
     with torch.cuda.stream(on):
@@ -657,7 +657,8 @@ def _here(t, name: str) -> int:
     dev = t.get_device()
     if dev < 0:
         raise ValueError(f"{name} must be a CUDA tensor")
-    if dev != torch.cuda.current_device():
+    # not torch.cuda.current_device(): t shows that CUDA is up, and a call takes 8 us in all
+    if dev != torch._C._cuda_getDevice():
         raise ValueError(f"{name} lies on {t.device}, which is not the current device")
     return dev
 
@@ -714,7 +715,7 @@ def rms_norm(x, weight, eps: float = 1e-6, residual=None, residual_out=None, out
         _check(residual_out, "residual_out", rows, dtype, dev), _check(out, "out", rows, bf16, dev),
         _check(out8, "out8", rows, torch.float8_e4m3fn, dev),
         _check(scale8, "scale8", (M,), f32, dev), _check(rstd, "rstd", (M,), f32, dev),
-        _stream(stream))
+        _stream(stream, dev))
     if rc:
         raise CrcError(rc, "crc_rms_norm")
     return out
@@ -739,7 +740,7 @@ def rms_norm_grad(dy, s, weight, rstd, dres=None, dx=None, dw=None, want_dw: boo
                       _check(rstd, "rstd", (M,), f32, dev),
                       _check(dres, "dres", rows, s.dtype, dev), _stream_type(s), M, d,
                       _check(dx, "dx", rows, s.dtype, dev), _check(dw, "dw", (d,), f32, dev),
-                      *_workspace(workspace, dev), stream)
+                      *_workspace(workspace, dev), _stream(stream, dev))
     return dx, dw
 
 
@@ -762,7 +763,7 @@ def quantize_rows(x, out8=None, scale=None, stream=None):
         scale = _new(stream, x.device, lead, torch.float32)
     crc_quantize_rows(x.data_ptr(), ldx, M, d,
                       _check(out8, "out8", (*lead, d), torch.float8_e4m3fn, dev),
-                      _check(scale, "scale", lead, torch.float32, dev), stream)
+                      _check(scale, "scale", lead, torch.float32, dev), _stream(stream, dev))
     return out8, scale
 
 
@@ -862,7 +863,7 @@ class MoeLayer:
             _check(out, "out", rows, torch.bfloat16, dev),
             _check(topk, "topk", (M, self.K), torch.uint8, dev),
             _check(gates, "gates", (M, self.K), f32, dev), *_workspace(workspace, dev),
-            _stream(stream))
+            _stream(stream, dev))
         if rc:
             raise CrcError(rc, "crc_moe_layer")
         return out

@@ -40,7 +40,7 @@ def P(monkeypatch):
     import paper_2609_04895_gb300 as P
     rec = Recorder(P.crc.load())
     monkeypatch.setattr(P.crc, "_lib", rec)
-    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+    monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: 0, raising=False)
     monkeypatch.setattr(torch._C, "_cuda_getCurrentRawStream", lambda dev: 0, raising=False)
     P.calls = rec.calls
     return P
@@ -127,7 +127,7 @@ def test_every_tensor_lies_on_one_device(P, name):
 @pytest.mark.parametrize("name", NAMES[:4])
 def test_tensors_of_a_device_that_is_not_current(P, name, monkeypatch):
     call_it, args = row_calls(P)[name]
-    monkeypatch.setattr(torch.cuda, "current_device", lambda: 1)
+    monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: 1)
     n = len(P.calls)
     with pytest.raises(ValueError):
         call_it(**args)
