@@ -22,10 +22,11 @@ inline size_t up256(size_t n) { return (n + 255) & ~(size_t)255; }
 
 // Rows of a tile, by an expert's mean share of the choices, with room for a few more so
 // that few experts need a second pass over their weights, or the tokens if that is fewer.
-// Narrow tiles leave room for more row blocks in flight.  8-bit weights, 16 / 32 / 64 rows:
-// mean 6.25 (d = 2048, f = 768) 116 / 118 / 128 us, 7.5 (d = 4096, f = 1536) 396 / 381 / 387,
-// 18.75 (d = 2048, f = 1024) 120 / 95 / 101, 25 (d = f = 2880) 238 / 162 / 169; bf16 at 25:
-// 322 / 262 / 261.
+// Narrow tiles leave room for more row blocks in flight.  us with 16 / 32 / 64 rows, 8-bit
+// weights: mean 6.25 (d = 2048, f = 768) 116 / 118 / 128, 7.5 (d = 4096, f = 1536)
+// 396 / 381 / 387, 18.75 (d = 2048, f = 1024) 120 / 95 / 101, 25 (d = f = 2880)
+// 238 / 162 / 169; bf16: 6.25 187 / 188 / 189, 7.5 699 / 705 / 710, 18.75 150 / 133 / 136, 25
+// 319 / 261 / 257, 31 (d = 2048, f = 768) 232 / 243 / 231.
 int row_tile(int M, int K, int N) {
     const int E = M * K;
     if (E <= 128 * 16 && (M <= 16 || E <= 6 * N)) return 16;

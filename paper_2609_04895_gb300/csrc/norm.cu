@@ -739,10 +739,15 @@ int crc_quantize_rows(const uint16_t* x_dev, int64_t x_stride, int64_t M, int32_
     if (M == 0) return CRC_OK;
     if (!x_dev || !out8_dev || !scale8_dev) return CRC_EINVAL;
     if (!aligned(x_dev, 16) || !aligned(out8_dev, 8) || !aligned(scale8_dev, 4)) return CRC_EINVAL;
-    // us with 2, 3, 4 groups a thread: 184320 x 2880 276, 235, 314; 65536 x 1024 35, 36, 36;
-    // 30000 x 6000 104, 81, 109 (four groups and the next four leave too few threads)
-    const RowShape sh = row_shape(d, M, 3);
-    // as many CTAs as stay resident, 2048 threads an SM
+    // Three or four groups a thread, by which leaves fewer lanes idle.  us with 2, 3, 4:
+    // 184320 x 2880 336, 243, 265; 65536 x 1024 37, 39, 33; 20000 x 6144 3: 57, 4: 62;
+    // 20000 x 8192 88, 93, 79; 30000 x 6000 97, 87, 91.
+    const int nvec = d / 8;
+    const auto idle = [nvec](int g) { return (nvec + 32 * g - 1) / (32 * g) * (32 * g) - nvec; };
+    const RowShape sh = row_shape(d, M, idle(4) < idle(3) ? 4 : 3);
+    // CTAs for 2048 threads an SM.  Of three or four groups (64 registers a thread) 1024 are
+    // resident, and the rest begin where others end; with the resident ones alone
+    // 184320 x 2880 took 244 us in place of 243, 65536 x 2048 (in threes) 85 in place of 75.
     const long long most = (long long)sm_count() * (2048 / sh.threads());
     const unsigned grid = (unsigned)(sh.grid(M) < most ? sh.grid(M) : most);
     cudaStream_t st = static_cast<cudaStream_t>(stream);
