@@ -579,7 +579,9 @@ uint64_t crc_launch_count(void);
  * crc_route_and_cache call that ran as one kernel, and SHORT those among them
  * that ran as the short-call kernel (counted in both).  Host-side bookkeeping
  * only; off by default.  Not thread-safe against concurrent library calls from
- * other host threads. */
+ * other host threads.  crc_kernel_times grows with CRC_KERNEL_KINDS (8 before the
+ * norm and MoE kernels, 12 with them) and crc_profile_end() writes all of it: a
+ * program is compiled against the header of the library that it loads. */
 enum { CRC_KERNEL_ROUTER = 0, CRC_KERNEL_SCAN = 1, CRC_KERNEL_STATE = 2, CRC_KERNEL_SYNTH = 3,
        CRC_KERNEL_FUSED = 4, CRC_KERNEL_LOSS = 5, CRC_KERNEL_LOSS_MEANS = 6,
        CRC_KERNEL_SHORT = 7, CRC_KERNEL_NORM = 8, CRC_KERNEL_QUANTIZE = 9,

@@ -37,7 +37,8 @@
 // 16 rows the row warps split on the way into shared memory, for every item anew.  With
 // more rows that would bound the kernel (three conversions a pair of elements), so
 // rows are split once, by items of their own before either phase, and the pieces are
-// copied: 200 tokens of the d = 4096 shape 423 -> 378 us, 1000 Qwen3-shaped 423 -> 287.
+// copied: 200 tokens of the d = 4096 shape 423 -> 378 us, 1000 Qwen3-shaped 423 -> 288
+// (with h in fp32 between the products, as now, 386 and 333).
 #pragma once
 
 #include <cuda_bf16.h>
