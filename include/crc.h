@@ -490,7 +490,8 @@ int crc_rms_norm_grad(const uint16_t *dy_dev, const void *s_dev, const uint16_t 
                       int32_t d, void *dx_dev, float *dw_dev, void *workspace_dev,
                       size_t workspace_bytes, void *stream);
 
-/* bf16 rows in 8 bits: out8 = e4m3(x / scale), scale = max |row| / 448.
+/* bf16 rows in 8 bits: out8 = e4m3(x / scale), scale = max |row| / 448, both
+ * quotients rounded to fp32 (as those of crc_rms_norm's 8-bit rows are).
  *   x_dev bf16, rows x_stride elements apart (>= d, a multiple of 8), 16-byte
  *   aligned; out8_dev e4m3 [M][d], 8-byte aligned; scale8_dev fp32 [M].
  * d as in crc_rms_norm.  M = 0 is a no-op. */

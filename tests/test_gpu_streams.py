@@ -121,3 +121,32 @@ def test_calls_on_several_streams_without_workspaces(P):
         for a, b in zip(got, ref):
             assert torch.equal(a, b)
     assert P.crc.crc_device_error() == 0
+
+
+@pytest.mark.parametrize("as_int", [False, True])
+def test_a_state_and_its_calls_on_a_named_stream(P, as_int):
+    """State, synthetic inputs, router heads, scan, step and losses on a stream that is
+    not the current one, nothing passed in but the stream, equal those on the current one."""
+    p = P.crc.problem(2, 32, 4, 256, 8, 1, 3, 0)
+
+    def run(stream):
+        w = P.synth_weights(2, 32, 256, seed=1, stream=stream)
+        h, _ = P.synth_hidden(3, 16, 2, 256, seed=2, stream=stream)
+        probs = P.route_scores(p, h, w, stream=stream)
+        a, b = P.State(p, stream=stream), P.State(p, stream=stream)
+        P.cache_scan(p, probs, a, stream=stream)
+        P.route_and_cache(p, h, w, b, stream=stream)
+        loss, means, grad = P.cache_loss(p, probs, 8, 0.05, stream=stream)
+        # blocks that the calls gave back, asked for again by the current stream
+        held = [torch.full((1 << k,), 255, dtype=torch.uint8, device="cuda") for k in range(8, 22)]
+        torch.cuda.synchronize()
+        del held
+        return [probs, loss, means, grad], a.read(stream), b.read(stream)
+
+    side = torch.cuda.Stream()
+    ref, a0, b0 = run(None)
+    got, a1, b1 = run(side.cuda_stream if as_int else side)
+    for x, y in zip(got, ref):
+        assert torch.equal(x, y)
+    for x, y in ((a1, a0), (b1, b0)):
+        assert x["error"] == 0 and x["misses"] == y["misses"] and x["proactive"] == y["proactive"]
