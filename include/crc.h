@@ -564,9 +564,158 @@ int crc_moe_layer(const crc_moe *m, const uint16_t *x_dev, int64_t x_stride, con
                   int32_t M, uint16_t *out_dev, uint8_t *topk_dev, float *gates_dev,
                   void *workspace_dev, size_t workspace_bytes, void *stream);
 
+/* ------------------------------------------------------------------------ */
+/* Prompts and training batches: far more tokens than crc_moe_layer takes.   */
+/* Their choices go in the order of their experts, each expert's matrices    */
+/* multiply that expert's rows, and every token sums its choices:            */
+/*   crc_group_choices, crc_group_matmul (gate and up, with rows), the same  */
+/*   (down, in order), crc_sum_choices.                                      */
+/* ------------------------------------------------------------------------ */
+
+/* Choices in the order of their experts (stable).  Choice c = m K + j of expert
+ * id = topk[c] < N comes to place
+ *   place[c] = #{c' : id' < id} + #{c' < c : id' = id},   rows[place[c]] = c,
+ * and offsets[e] = #{c : id < e}.  A choice whose id is N or more has no expert (a
+ * padded token's 255): place[c] = -1, and rows[offsets[N]] .. rows[M K - 1] = -1.
+ *   topk_dev   uint8 [M][K], e.g. crc_trace's or crc_moe_layer's
+ *   offsets_dev  int32 [N + 1];  rows_dev int32 [M K];  place_dev int32 [M][K] or NULL
+ *   workspace_dev  crc_group_choices_workspace_bytes(M, K, N) bytes (0 for up to 8192
+ *              choices), 256-byte aligned; calls that may overlap need one each
+ * N <= 256, K <= 32, M K <= 2^30, else CRC_EUNSUPPORTED.  M = 0 sets offsets to 0. */
+size_t crc_group_choices_workspace_bytes(int32_t M, int32_t K, int32_t N);
+int crc_group_choices(const uint8_t *topk_dev, int32_t M, int32_t K, int32_t N,
+                      int32_t *offsets_dev, int32_t *rows_dev, int32_t *place_dev,
+                      void *workspace_dev, size_t workspace_bytes, void *stream);
+
+/* One matrix (or gate and up) of each of N experts. */
+typedef struct crc_group_weights {
+    int32_t N;                   /* experts, N <= 256                            */
+    int32_t n;                   /* rows of a matrix (with glu: of each of the
+                                    two), n % 8 == 0 (glu: n % 16 == 0)          */
+    int32_t k;                   /* columns, k % 8 == 0 (CRC_E4M3: k % 16 == 0)  */
+    int32_t glu;                 /* 1: gate and up [2][n][k], y = silu(G x) * (U x) */
+    int32_t weight_type;         /* CRC_BF16 or CRC_E4M3                         */
+    int32_t reserved;            /* must be 0                                    */
+    const void *w_dev;           /* [N][n][k] (glu: [N][2][n][k]), 16-byte aligned */
+    int64_t w_stride;            /* bytes between experts, a multiple of 16      */
+    const float *scale_dev;      /* CRC_E4M3: [N][n] (glu: [N][2][n]), else NULL */
+    int64_t scale_stride;        /* bytes between experts, a multiple of 4       */
+} crc_group_weights;
+
+/* Products of E rows in the order of their experts: for offsets[e] <= i < offsets[e+1]
+ *   y_i = W_e x_r   (glu: silu(G_e x_r) * (U_e x_r)),
+ *   r = rows[i] / K with rows_dev (a token's row for its choice rows[i]), else r = i.
+ *   x_dev        the type of the matrices, x_rows rows x_stride elements apart (>= k,
+ *                a multiple of 16 bytes), 16-byte aligned
+ *   x_scale_dev  fp32 [x_rows], the scales of e4m3 rows; NULL for bf16
+ *   offsets_dev  int32 [N + 1], rising, within 0 .. E
+ *   rows_dev     int32 [E] or NULL (then K = 1 and x_rows >= E)
+ *   y_dev        bf16 [E][n], 16-byte aligned, not overlapping the inputs
+ * Products are summed in fp32 (silu by the fast exponential and division) and rounded
+ * once.  Rows of y before offsets[0] and from offsets[N] on are left as they were.
+ * Offsets that are not as stated, or a row outside x, are reported by
+ * crc_device_error (CRC_EDEVICE; no expert's rows there, row 0).  n, k <= 65536.
+ * E = 0 is a no-op. */
+int crc_group_matmul(const crc_group_weights *w, const void *x_dev, int64_t x_stride,
+                     int64_t x_rows, const float *x_scale_dev, const int32_t *offsets_dev,
+                     const int32_t *rows_dev, int32_t K, int64_t E, uint16_t *y_dev,
+                     void *stream);
+
+/* Its gradients, bf16 without glu: for the rows i of expert e
+ *   dx_i = W_e^T dy_i,   dW_e = sum over i of dy_i x_r^T.
+ *   dy_dev    bf16 [E][n], 16-byte aligned
+ *   dx_dev    bf16 [E][k], 16-byte aligned, one row for each row of dy (crc_sum_choices
+ *             sums those of a token's choices), or NULL (w_dev is not read then).
+ *             Rows outside the offsets are left as they were.
+ *   dw_dev    dw_type (CRC_F32 or CRC_BF16) [N][n][k], 16-byte aligned, zeros for an
+ *             expert without rows, or NULL (x_dev is not read then)
+ * Sums in fp32, in the order of the rows, without atomics; each output is rounded once.
+ * E = 0 sets dw to zero. */
+int crc_group_matmul_grad(const crc_group_weights *w, const uint16_t *dy_dev,
+                          const uint16_t *x_dev, int64_t x_stride, int64_t x_rows,
+                          const int32_t *offsets_dev, const int32_t *rows_dev, int32_t K,
+                          int64_t E, uint16_t *dx_dev, void *dw_dev, int32_t dw_type,
+                          void *stream);
+
+/* The sum over a token's choices: out_m = sum over j of g_mj y[place_mj].
+ *   y_dev      bf16 [y_rows][d], 16-byte aligned
+ *   place_dev  int32 [M][K] from crc_group_choices; a place outside 0 .. y_rows - 1 adds
+ *              nothing; NULL: choice c is row c (y_rows >= M K)
+ *   gates_dev  fp32 [M][K], or NULL (1)
+ *   out_dev    bf16 [M][d], 16-byte aligned, not overlapping the inputs
+ * In fp32, in rank order, rounded once.  d % 8 == 0, d <= 32768, K <= 32.
+ * M = 0 is a no-op. */
+int crc_sum_choices(const uint16_t *y_dev, int64_t y_rows, const int32_t *place_dev,
+                    const float *gates_dev, int32_t M, int32_t K, int32_t d, uint16_t *out_dev,
+                    void *stream);
+
+/* Its gradient: dy[place_mj] = g_mj dout_m and dg_mj = <dout_m, y[place_mj]>.
+ *   dout_dev  bf16 [M][d];  y_dev as above (for dgates_dev only, else NULL)
+ *   dy_dev    bf16 [y_rows][d] or NULL; rows that no choice has are left as they were
+ *             (two choices with one place are not a sum's: either's row is written)
+ *   dgates_dev  fp32 [M][K] or NULL; 0 for a choice without a place */
+int crc_sum_choices_grad(const uint16_t *dout_dev, const uint16_t *y_dev, int64_t y_rows,
+                         const int32_t *place_dev, const float *gates_dev, int32_t M, int32_t K,
+                         int32_t d, uint16_t *dy_dev, float *dgates_dev, void *stream);
+
+/* ------------------------------------------------------------------------ */
+/* Experts in 4 bits: half of the bytes of an 8-bit transfer (plus scales).  */
+/* ------------------------------------------------------------------------ */
+
+/* bf16 matrices in 4 bits: the columns of a row in groups of `group` (32, 64 or 128),
+ *   scale = bf16(max |group| / 7)   (1 where that is zero),
+ *   code = x / scale to the nearest whole number, ties to even, -7 .. 7,
+ * two's complement, two codes a byte, the even column in the low half.  A group that
+ * holds a NaN or an infinity has that as its scale, and codes 0.
+ *   x_dev      bf16, `matrices` times n rows of k elements, x_stride elements apart
+ *              (>= k, a multiple of 8), 16-byte aligned
+ *   out4_dev   [matrices][n][k / 2] bytes, 16-byte aligned
+ *   scale_dev  bf16 [matrices][k / group][n], 16-byte aligned: the rows of a matrix
+ *              side by side, as crc_matvec4 reads them
+ * k % group == 0, k <= 32768, matrices <= 65535.  matrices = 0 or n = 0 is a no-op. */
+int crc_quantize_rows4(const uint16_t *x_dev, int64_t x_stride, int32_t matrices, int32_t n,
+                       int32_t k, int32_t group, uint8_t *out4_dev, uint16_t *scale_dev,
+                       void *stream);
+
+/* One 4-bit matrix (or gate and up) of each expert, and where it lies. */
+typedef struct crc_matvec4_weights {
+    int32_t N;                   /* experts, N <= 256                            */
+    int32_t n;                   /* rows of a matrix, n % 8 == 0                 */
+    int32_t k;                   /* columns, k % group == 0                      */
+    int32_t slots;               /* expert slots in the arrays below             */
+    int32_t glu;                 /* 1: gate and up, y = silu(G x) * (U x)        */
+    int32_t group;               /* 32, 64 or 128                                */
+    int64_t reserved;            /* must be 0                                    */
+    const uint8_t *codes_dev;    /* [slots][n][k / 2] (glu: [slots][2][n][k / 2]),
+                                    16-byte aligned                              */
+    const uint16_t *scale_dev;   /* bf16 [slots][k / group][n] (glu: [slots][2][..]),
+                                    16-byte aligned                              */
+    int64_t codes_stride;        /* bytes between slots, multiples of 16         */
+    int64_t scale_stride;
+    const int32_t *expert_slot_dev;   /* [N]: each expert's slot, -1 (or any value
+                                    outside 0 .. slots - 1) if it has none;
+                                    NULL: expert e is in slot e                  */
+} crc_matvec4_weights;
+
+/* Products of a few rows with their choices' 4-bit matrices: for choice c = m K + j of
+ * expert id = topk[c]
+ *   y_c = W_id x_r   (glu: silu(G_id x_r) * (U_id x_r)),  r = c with x_per_choice, else m.
+ *   x_dev     bf16, rows x_stride elements apart (>= k, a multiple of 8), 16-byte aligned
+ *   topk_dev  uint8 [M][K]; NULL: every row takes the matrix in slot 0 (K = 1, no
+ *             expert_slot_dev)
+ *   y_dev     bf16 [M][K][n], 16-byte aligned, not overlapping the inputs; zeros for an
+ *             expert without a slot, or an id of N or more
+ * No weight is rounded: a group's codes are summed with x in fp32 and scaled then.  (By
+ * way of 136 x, which is taken off again: x needs to be finite, and below 1e36, for a
+ * finite result, and a group's sum is off by up to 2^-16 of the largest code x in it.)
+ * M <= 1024, K <= 32, M K <= 8192, n <= 65536, k <= 32768.  M = 0 is a no-op. */
+int crc_matvec4(const crc_matvec4_weights *w, const uint16_t *x_dev, int64_t x_stride,
+                int32_t x_per_choice, const uint8_t *topk_dev, int32_t M, int32_t K,
+                uint16_t *y_dev, void *stream);
+
 /* Synchronises the device and returns (then clears) the error latched by
- * calls without a state (crc_route_scores, crc_rms_norm_grad, crc_moe_layer),
- * CRC_OK if none. */
+ * calls without a state (crc_route_scores, crc_rms_norm_grad, crc_moe_layer,
+ * crc_group_matmul, crc_group_matmul_grad, crc_matvec4), CRC_OK if none. */
 int crc_device_error(void);
 
 /* Number of kernels the library has launched in this process. */
@@ -581,13 +730,14 @@ uint64_t crc_launch_count(void);
  * that ran as the short-call kernel (counted in both).  Host-side bookkeeping
  * only; off by default.  Not thread-safe against concurrent library calls from
  * other host threads.  crc_kernel_times grows with CRC_KERNEL_KINDS (8 before the
- * norm and MoE kernels, 12 with them) and crc_profile_end() writes all of it: a
+ * norm and MoE kernels, 12 with them, 16 with those of prompts and 4-bit experts) and crc_profile_end() writes all of it: a
  * program is compiled against the header of the library that it loads. */
 enum { CRC_KERNEL_ROUTER = 0, CRC_KERNEL_SCAN = 1, CRC_KERNEL_STATE = 2, CRC_KERNEL_SYNTH = 3,
        CRC_KERNEL_FUSED = 4, CRC_KERNEL_LOSS = 5, CRC_KERNEL_LOSS_MEANS = 6,
        CRC_KERNEL_SHORT = 7, CRC_KERNEL_NORM = 8, CRC_KERNEL_QUANTIZE = 9,
-       CRC_KERNEL_MOE_ROUTE = 10, CRC_KERNEL_MOE = 11,
-       CRC_KERNEL_KINDS = 12 };
+       CRC_KERNEL_MOE_ROUTE = 10, CRC_KERNEL_MOE = 11, CRC_KERNEL_CHOICES = 12,
+       CRC_KERNEL_SUM = 13, CRC_KERNEL_GROUP = 14, CRC_KERNEL_MATVEC4 = 15,
+       CRC_KERNEL_KINDS = 16 };
 typedef struct crc_kernel_times {
     uint64_t launches[CRC_KERNEL_KINDS];
     double ms[CRC_KERNEL_KINDS];

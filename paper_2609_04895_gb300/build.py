@@ -21,7 +21,8 @@ UNITS = ["api.cu", "router.cu", "scan.cu", "scan_traced.cu", "synth.cu", "noallo
          "short.cu", "short_n128.cu",
          "fused_n16.cu", "fused_n32.cu", "fused_n64.cu", "fused_n128.cu", "policy.cu",
          "policy_lru.cu", "policy_lfu.cu", "policy_lrfu.cu", "policy_spatio.cu", "loss.cu",
-         "transfer.cu", "probe.cu", "norm.cu", "moe.cu"]
+         "transfer.cu", "probe.cu", "norm.cu", "moe.cu",
+         "choices.cu", "rows4.cu", "matvec4.cu", "group.cu"]
 
 
 def nvcc() -> str:

@@ -58,11 +58,13 @@ class crc_report(ctypes.Structure):
 
 
 KERNEL_KINDS = {"router": 0, "scan": 1, "state": 2, "synth": 3, "fused": 4, "loss": 5,
-                "loss_means": 6, "short": 7, "norm": 8, "quantize": 9, "moe_route": 10, "moe": 11}
+                "loss_means": 6, "short": 7, "norm": 8, "quantize": 9, "moe_route": 10, "moe": 11,
+                "choices": 12, "sum": 13, "group": 14, "matvec4": 15}
 
 
 class crc_kernel_times(ctypes.Structure):
-    _fields_ = [("launches", ctypes.c_uint64 * 12), ("ms", ctypes.c_double * 12)]
+    _fields_ = [("launches", ctypes.c_uint64 * len(KERNEL_KINDS)),
+                ("ms", ctypes.c_double * len(KERNEL_KINDS))]
 
 
 class crc_moe(ctypes.Structure):
@@ -75,6 +77,22 @@ class crc_moe(ctypes.Structure):
                 ("down_scale_dev", ctypes.c_void_p), ("gate_up_scale_stride", ctypes.c_int64),
                 ("down_scale_stride", ctypes.c_int64), ("router_dev", ctypes.c_void_p),
                 ("expert_slot_dev", ctypes.c_void_p)]
+
+
+class crc_group_weights(ctypes.Structure):
+    _fields_ = [("N", ctypes.c_int32), ("n", ctypes.c_int32), ("k", ctypes.c_int32),
+                ("glu", ctypes.c_int32), ("weight_type", ctypes.c_int32),
+                ("reserved", ctypes.c_int32), ("w_dev", ctypes.c_void_p),
+                ("w_stride", ctypes.c_int64), ("scale_dev", ctypes.c_void_p),
+                ("scale_stride", ctypes.c_int64)]
+
+
+class crc_matvec4_weights(ctypes.Structure):
+    _fields_ = [("N", ctypes.c_int32), ("n", ctypes.c_int32), ("k", ctypes.c_int32),
+                ("slots", ctypes.c_int32), ("glu", ctypes.c_int32), ("group", ctypes.c_int32),
+                ("reserved", ctypes.c_int64), ("codes_dev", ctypes.c_void_p),
+                ("scale_dev", ctypes.c_void_p), ("codes_stride", ctypes.c_int64),
+                ("scale_stride", ctypes.c_int64), ("expert_slot_dev", ctypes.c_void_p)]
 
 
 class CrcError(RuntimeError):
@@ -131,6 +149,17 @@ EXPORTS = [
     ("crc_moe_workspace_bytes", SZ, [ctypes.POINTER(crc_moe), I32]),
     ("crc_moe_layer", ctypes.c_int,
      [ctypes.POINTER(crc_moe), P, I64, P, P, P, I64, I32, P, P, P, P, SZ, P]),
+    ("crc_group_choices_workspace_bytes", SZ, [I32, I32, I32]),
+    ("crc_group_choices", ctypes.c_int, [P, I32, I32, I32, P, P, P, P, SZ, P]),
+    ("crc_group_matmul", ctypes.c_int,
+     [ctypes.POINTER(crc_group_weights), P, I64, I64, P, P, P, I32, I64, P, P]),
+    ("crc_group_matmul_grad", ctypes.c_int,
+     [ctypes.POINTER(crc_group_weights), P, P, I64, I64, P, P, I32, I64, P, P, I32, P]),
+    ("crc_sum_choices", ctypes.c_int, [P, I64, P, P, I32, I32, I32, P, P]),
+    ("crc_sum_choices_grad", ctypes.c_int, [P, P, I64, P, P, I32, I32, I32, P, P, P]),
+    ("crc_quantize_rows4", ctypes.c_int, [P, I64, I32, I32, I32, I32, P, P, P]),
+    ("crc_matvec4", ctypes.c_int,
+     [ctypes.POINTER(crc_matvec4_weights), P, I64, I32, P, I32, I32, P, P]),
 ]
 
 
@@ -441,6 +470,55 @@ def crc_moe_layer(m: crc_moe, x_ptr, x_stride: int, x8_ptr, x8_scale_ptr, scores
 # `stream`: a torch stream or a raw handle; None is the current one.  Tensors that are
 # made for a call (outputs, workspaces) come from its stream's pool and may be read on
 # the current stream; tensors that are passed in are the caller's to keep and to order.
+def crc_group_choices_workspace_bytes(M: int, K: int, N: int) -> int:
+    return int(load().crc_group_choices_workspace_bytes(M, K, N))
+
+
+def crc_group_choices(topk_ptr, M: int, K: int, N: int, offsets_ptr, rows_ptr, place_ptr, ws_ptr,
+                      ws_bytes: int, stream=None):
+    _ck(load().crc_group_choices(topk_ptr, M, K, N, offsets_ptr, rows_ptr, place_ptr, ws_ptr,
+                                 ws_bytes, _stream(stream)), "crc_group_choices")
+
+
+def crc_group_matmul(w: crc_group_weights, x_ptr, x_stride: int, x_rows: int, x_scale_ptr,
+                     offsets_ptr, rows_ptr, K: int, E: int, y_ptr, stream=None):
+    _ck(load().crc_group_matmul(ctypes.byref(w), x_ptr, x_stride, x_rows, x_scale_ptr,
+                                offsets_ptr, rows_ptr, K, E, y_ptr, _stream(stream)),
+        "crc_group_matmul")
+
+
+def crc_group_matmul_grad(w: crc_group_weights, dy_ptr, x_ptr, x_stride: int, x_rows: int,
+                          offsets_ptr, rows_ptr, K: int, E: int, dx_ptr, dw_ptr, dw_type: int,
+                          stream=None):
+    _ck(load().crc_group_matmul_grad(ctypes.byref(w), dy_ptr, x_ptr, x_stride, x_rows,
+                                     offsets_ptr, rows_ptr, K, E, dx_ptr, dw_ptr, dw_type,
+                                     _stream(stream)), "crc_group_matmul_grad")
+
+
+def crc_sum_choices(y_ptr, y_rows: int, place_ptr, gates_ptr, M: int, K: int, d: int, out_ptr,
+                    stream=None):
+    _ck(load().crc_sum_choices(y_ptr, y_rows, place_ptr, gates_ptr, M, K, d, out_ptr,
+                               _stream(stream)), "crc_sum_choices")
+
+
+def crc_sum_choices_grad(dout_ptr, y_ptr, y_rows: int, place_ptr, gates_ptr, M: int, K: int,
+                         d: int, dy_ptr, dgates_ptr, stream=None):
+    _ck(load().crc_sum_choices_grad(dout_ptr, y_ptr, y_rows, place_ptr, gates_ptr, M, K, d,
+                                    dy_ptr, dgates_ptr, _stream(stream)), "crc_sum_choices_grad")
+
+
+def crc_quantize_rows4(x_ptr, x_stride: int, matrices: int, n: int, k: int, group: int, out4_ptr,
+                       scale_ptr, stream=None):
+    _ck(load().crc_quantize_rows4(x_ptr, x_stride, matrices, n, k, group, out4_ptr, scale_ptr,
+                                  _stream(stream)), "crc_quantize_rows4")
+
+
+def crc_matvec4(w: crc_matvec4_weights, x_ptr, x_stride: int, x_per_choice: int, topk_ptr, M: int,
+                K: int, y_ptr, stream=None):
+    _ck(load().crc_matvec4(ctypes.byref(w), x_ptr, x_stride, x_per_choice, topk_ptr, M, K, y_ptr,
+                           _stream(stream)), "crc_matvec4")
+
+
 # --------------------------------------------------------------------------- #
 def problem(L, N, K, d, C, R, B, expert_bytes) -> crc_problem:
     return crc_problem(L=L, N=N, K=K, d=d, C=C, R=R, B=B, reserved=0,
@@ -867,6 +945,231 @@ class MoeLayer:
         if rc:
             raise CrcError(rc, "crc_moe_layer")
         return out
+
+
+def group_choices(topk, N: int, offsets=None, rows=None, place=None, workspace=None,
+                  stream=None):
+    """crc_group_choices: the choices topk uint8 [M][K] in the order of their experts, as
+    (offsets int32 [N + 1], rows int32 [M * K], place int32 [M][K])."""
+    import torch
+    if topk.dim() != 2:
+        raise ValueError("topk must be a 2-D tensor")
+    dev, i32 = _here(topk, "topk"), torch.int32
+    M, K = topk.shape
+    if offsets is None:
+        offsets = _new(stream, topk.device, (N + 1,), i32)
+    if rows is None:
+        rows = _new(stream, topk.device, (M * K,), i32)
+    if place is None:
+        place = _new(stream, topk.device, (M, K), i32)
+    if workspace is None:
+        need = crc_group_choices_workspace_bytes(M, K, N)
+        if need:
+            workspace = _new(stream, topk.device, (need,), torch.uint8)
+    crc_group_choices(_check(topk, "topk", (M, K), torch.uint8, dev), M, K, N,
+                      _check(offsets, "offsets", (N + 1,), i32, dev),
+                      _check(rows, "rows", (M * K,), i32, dev),
+                      _check(place, "place", (M, K), i32, dev), *_workspace(workspace, dev),
+                      _stream(stream, dev))
+    return offsets, rows, place
+
+
+def _group_weights(w, w_scale, dev: int):
+    """crc_group_weights of matrices w [N][n][k], or gate and up [N][2][n][k]."""
+    import torch
+    kinds = {torch.bfloat16: BF16, torch.float8_e4m3fn: E4M3}
+    if w.dtype not in kinds:
+        raise ValueError("w must be bfloat16 or float8_e4m3fn")
+    if w.dim() not in (3, 4) or (w.dim() == 4 and w.shape[1] != 2):
+        raise ValueError("w has the shape [N][n][k], or [N][2][n][k] with gate and up")
+    if w.get_device() != dev:
+        raise ValueError(f"w lies on {w.device}, the other tensors on cuda:{dev}")
+    n, k = w.shape[-2:]
+    if w.stride()[1:] != ((k, 1) if w.dim() == 3 else (n * k, k, 1)):
+        raise ValueError("an expert's matrices must be contiguous")
+    if (w_scale is None) != (w.dtype == torch.bfloat16):
+        raise ValueError("w_scale belongs to 8-bit matrices")
+    _check(w_scale, "w_scale", w.shape[:-1], torch.float32, dev, dense=False)
+    if w_scale is not None and w_scale.stride()[1:] != ((1,) if w.dim() == 3 else (n, 1)):
+        raise ValueError("an expert's scales must be contiguous")
+    return crc_group_weights(
+        N=w.shape[0], n=n, k=k, glu=int(w.dim() == 4), weight_type=kinds[w.dtype], reserved=0,
+        w_dev=w.data_ptr(), w_stride=w.stride(0) * w.element_size(), scale_dev=_ptr(w_scale),
+        scale_stride=0 if w_scale is None else w_scale.stride(0) * 4)
+
+
+def group_matmul(x, w, offsets, rows=None, K: int = 1, x_scale=None, w_scale=None, y=None,
+                 stream=None):
+    """crc_group_matmul: y [E][n] (bf16), row i the product of its expert's matrix with the
+    row rows[i] // K of x (row i without `rows`); the rows of expert e are offsets[e] ..
+    offsets[e + 1] - 1.  w [N][n][k], or gate and up [N][2][n][k] for silu(G x) * (U x);
+    x and w bf16, or float8_e4m3fn with x_scale [rows of x] and w_scale [N][n] ([N][2][n]).
+    x may have strided rows, w strided experts."""
+    import torch
+    dev, i32, f32 = _here(x, "x"), torch.int32, torch.float32
+    x_rows, k, ldx = _rows(x, "x")
+    c = _group_weights(w, w_scale, dev)
+    if x.dtype != w.dtype or k != c.k:
+        raise ValueError(f"x must be {w.dtype} with rows of {c.k}, got {x.dtype} {tuple(x.shape)}")
+    if (x_scale is None) != (w_scale is None):
+        raise ValueError("x_scale belongs to 8-bit rows")
+    E = x_rows if rows is None else rows.numel()
+    if y is None:
+        y = _new(stream, x.device, (E, c.n), torch.bfloat16)
+    rc = load().crc_group_matmul(
+        ctypes.byref(c), x.data_ptr(), ldx if x_rows > 1 else (k + 15) // 16 * 16, x_rows,
+        _check(x_scale, "x_scale", (x_rows,), f32, dev),
+        _check(offsets, "offsets", (c.N + 1,), i32, dev), _check(rows, "rows", (E,), i32, dev),
+        K, E, _check(y, "y", (E, c.n), torch.bfloat16, dev), _stream(stream, dev))
+    if rc:
+        raise CrcError(rc, "crc_group_matmul")
+    return y
+
+
+def group_matmul_grad(dy, x, w, offsets, rows=None, K: int = 1, dx=None, dw=None,
+                      want_dx: bool = True, want_dw: bool = True, stream=None):
+    """crc_group_matmul_grad: (dx [E][k] bf16, dw [N][n][k], fp32 unless a bf16 one is given)
+    of y = group_matmul(x, w, offsets, rows, K) from dy [E][n], all bf16."""
+    import torch
+    bf16, i32 = torch.bfloat16, torch.int32
+    dev = _here(dy, "dy")
+    x_rows, k, ldx = _rows(x, "x")
+    c = _group_weights(w, None, dev)
+    if c.glu:
+        raise ValueError("w has the shape [N][n][k]: the gradient is that of the products alone")
+    E = x_rows if rows is None else rows.numel()
+    if want_dx and dx is None:
+        dx = _new(stream, dy.device, (E, c.k), bf16)
+    if want_dw and dw is None:
+        dw = _new(stream, dy.device, (c.N, c.n, c.k), torch.float32)
+    if dw is not None and dw.dtype not in (torch.float32, bf16):
+        raise ValueError("dw must be float32 or bfloat16")
+    crc_group_matmul_grad(
+        c, _check(dy, "dy", (E, c.n), bf16, dev),
+        _check(x, "x", (x_rows, c.k), bf16, dev, dense=False), ldx, x_rows,
+        _check(offsets, "offsets", (c.N + 1,), i32, dev), _check(rows, "rows", (E,), i32, dev),
+        K, E, _check(dx, "dx", (E, c.k), bf16, dev),
+        None if dw is None else _check(dw, "dw", (c.N, c.n, c.k), dw.dtype, dev),
+        BF16 if dw is not None and dw.dtype == bf16 else F32, _stream(stream, dev))
+    return dx, dw
+
+
+def sum_choices(y, place, gates=None, out=None, stream=None):
+    """crc_sum_choices: out [M][d], the sum over j of gates[m][j] * y[place[m][j]] (place int32
+    [M][K] of group_choices, gates fp32 [M][K] or None), y and out bf16."""
+    import torch
+    bf16 = torch.bfloat16
+    if y.dim() != 2 or place.dim() != 2:
+        raise ValueError("y and place must be 2-D tensors")
+    dev = _here(y, "y")
+    (n, d), (M, K) = y.shape, place.shape
+    if out is None:
+        out = _new(stream, y.device, (M, d), bf16)
+    crc_sum_choices(_check(y, "y", (n, d), bf16, dev), n,
+                    _check(place, "place", (M, K), torch.int32, dev),
+                    _check(gates, "gates", (M, K), torch.float32, dev), M, K, d,
+                    _check(out, "out", (M, d), bf16, dev), _stream(stream, dev))
+    return out
+
+
+def sum_choices_grad(dout, place, gates=None, y=None, dy=None, dgates=None, y_rows=None,
+                     stream=None):
+    """crc_sum_choices_grad: (dy [y_rows][d], dgates [M][K]) from dout [M][d].  dgates is made
+    when y is given (and is None without); y_rows: M * K unless y or dy says."""
+    import torch
+    bf16, f32 = torch.bfloat16, torch.float32
+    if dout.dim() != 2 or place.dim() != 2:
+        raise ValueError("dout and place must be 2-D tensors")
+    dev = _here(dout, "dout")
+    (M, d), K = dout.shape, place.shape[1]
+    if y_rows is None:
+        y_rows = y.shape[0] if y is not None else dy.shape[0] if dy is not None else M * K
+    if dy is None:
+        dy = _new(stream, dout.device, (y_rows, d), bf16)
+    if y is not None and dgates is None:
+        dgates = _new(stream, dout.device, (M, K), f32)
+    crc_sum_choices_grad(_check(dout, "dout", (M, d), bf16, dev),
+                         _check(y, "y", (y_rows, d), bf16, dev), y_rows,
+                         _check(place, "place", (M, K), torch.int32, dev),
+                         _check(gates, "gates", (M, K), f32, dev), M, K, d,
+                         _check(dy, "dy", (y_rows, d), bf16, dev),
+                         _check(dgates, "dgates", (M, K), f32, dev), _stream(stream, dev))
+    return dy, dgates
+
+
+def quantize_rows4(x, group: int = 32, out4=None, scale=None, stream=None):
+    """crc_quantize_rows4: bf16 matrices [..][n][k] in 4 bits, as (uint8 [..][n][k / 2], bf16
+    scales [..][k / group][n]).  A 2-D x may have strided rows; more dimensions must be
+    contiguous."""
+    import torch
+    bf16 = torch.bfloat16
+    if x.dtype != bf16 or x.dim() < 2:
+        raise ValueError("x must be bfloat16 with two dimensions or more")
+    dev = _here(x, "x")
+    *lead, n, k = x.shape
+    if x.dim() != 2 and not x.is_contiguous():
+        raise ValueError("x must be contiguous, or have two dimensions")
+    if group not in (32, 64, 128) or k % group:
+        raise CrcError(CRC_EUNSUPPORTED, "crc_quantize_rows4")
+    _, _, ldx = _rows(x.reshape(-1, k) if x.dim() != 2 else x, "x")
+    codes, scales = (*lead, n, k // 2), (*lead, k // group, n)
+    if out4 is None:
+        out4 = _new(stream, x.device, codes, torch.uint8)
+    if scale is None:
+        scale = _new(stream, x.device, scales, bf16)
+    crc_quantize_rows4(x.data_ptr(), ldx, math.prod(lead), n, k, group,
+                       _check(out4, "out4", codes, torch.uint8, dev),
+                       _check(scale, "scale", scales, bf16, dev), _stream(stream, dev))
+    return out4, scale
+
+
+def matvec4(x, codes, scale, topk=None, expert_slot=None, y=None, N: int | None = None,
+            stream=None):
+    """crc_matvec4: y [M][K][n] (bf16), the products of rows x with the 4-bit matrices of
+    their choices topk uint8 [M][K].  codes uint8 [slots][n][k / 2] and scale bf16
+    [slots][k / group][n] as quantize_rows4 makes them, or with gate and up [slots][2][..]
+    for silu(G x) * (U x); x [M][k], or [M][K][k] with a row for each choice; expert_slot
+    int32 [N] (None: expert e is in slot e).  Without topk all rows take slot 0, y [M][1][n].
+    The slots and 2-D x's rows may be strided."""
+    import torch
+    bf16 = torch.bfloat16
+    dev = _here(x, "x")
+    if codes.dim() not in (3, 4) or (codes.dim() == 4 and codes.shape[1] != 2):
+        raise ValueError("codes has the shape [slots][n][k / 2], or [slots][2][n][k / 2]")
+    slots, n, k = codes.shape[0], codes.shape[-2], 2 * codes.shape[-1]
+    if scale.dim() != codes.dim() or scale.shape[-2] < 1 or k % scale.shape[-2]:
+        raise ValueError("scale has the shape [slots][k / group][n], or [slots][2][k / group][n]")
+    groups = scale.shape[-2]
+    lead = tuple(codes.shape[:-2])
+    _check(codes, "codes", (*lead, n, k // 2), torch.uint8, dev, dense=False)
+    _check(scale, "scale", (*lead, groups, n), bf16, dev, dense=False)
+    inner = (lambda r, c: (c, 1) if len(lead) == 1 else (r * c, c, 1))
+    if codes.stride()[1:] != inner(n, k // 2) or scale.stride()[1:] != inner(groups, n):
+        raise ValueError("a slot's codes and scales must be contiguous")
+    if N is None:
+        N = expert_slot.shape[0] if expert_slot is not None else slots
+    M = x.shape[0]
+    K = 1 if topk is None else topk.shape[-1]
+    per_choice = x.dim() == 3
+    if per_choice:
+        _check(x, "x", (M, K, k), bf16, dev)
+        ldx = k
+    else:
+        _check(x, "x", (M, k), bf16, dev, dense=False)
+        ldx = _rows(x, "x")[2]
+    if y is None:
+        y = _new(stream, x.device, (M, K, n), bf16)
+    c = crc_matvec4_weights(
+        N=N, n=n, k=k, slots=slots, glu=int(len(lead) == 2), group=k // groups, reserved=0,
+        codes_dev=codes.data_ptr(), scale_dev=scale.data_ptr(), codes_stride=codes.stride(0),
+        scale_stride=scale.stride(0) * 2,
+        expert_slot_dev=_check(expert_slot, "expert_slot", (N,), torch.int32, dev))
+    rc = load().crc_matvec4(ctypes.byref(c), x.data_ptr(), ldx, int(per_choice),
+                            _check(topk, "topk", (M, K), torch.uint8, dev), M, K,
+                            _check(y, "y", (M, K, n), bf16, dev), _stream(stream, dev))
+    if rc:
+        raise CrcError(rc, "crc_matvec4")
+    return y
 
 
 def _stats_struct(stats: dict) -> crc_stats:

@@ -1,0 +1,194 @@
+// Matrix products grouped by expert: what their kernels share.  The rows of a call lie in
+// their experts' order, expert e's are offsets[e] .. offsets[e + 1] - 1, known on the device
+// only, so every CTA plans its own share of the work from them.
+#pragma once
+
+#include <cuda_bf16.h>
+
+#include "crc_device.cuh"
+#include "pdl.cuh"
+
+namespace crc {
+
+constexpr int kGroupMaxExperts = 256;
+
+// ---------------------------------------------------------------------------
+// tcgen05 operands whose rows lie across the contraction (MN-major)
+// ---------------------------------------------------------------------------
+// 64 elements of M (or N) a 128-byte row, one row for each step of the contraction, 128-byte
+// swizzle: the layout that TMA writes for a box of 64 columns x 64 rows.  The next 64 elements
+// of M are `chunk` bytes on, the next eight steps of the contraction 1024; 16 steps further
+// the start address is 2048 bytes on.
+__device__ __forceinline__ uint64_t sw128_mnmajor_desc(uint32_t smem_addr, uint32_t chunk) {
+    uint64_t d = 0;
+    d |= (uint64_t)((smem_addr >> 4) & 0x3FFFu);  // start address
+    d |= (uint64_t)((chunk >> 4) & 0x3FFFu) << 16;
+    d |= (uint64_t)(1024u >> 4) << 32;
+    d |= (uint64_t)1u << 46;                      // descriptor version for tcgen05
+    d |= (uint64_t)2u << 61;                      // 128-byte swizzle
+    return d;
+}
+// Bits of the instruction descriptor: A, B with their rows across the contraction.
+constexpr uint32_t kIdescMnA = 1u << 15, kIdescMnB = 1u << 16;
+
+// e4m3 A and B, fp32 D.
+__host__ __device__ constexpr uint32_t idesc_e4m3_f32_mn(int M, int N) {
+    return (1u << 4) | ((uint32_t)(N >> 3) << 17) | ((uint32_t)(M >> 4) << 24);
+}
+
+__device__ __forceinline__ void umma_e4m3_pair(uint32_t d_tmem, uint64_t adesc, uint64_t bdesc,
+                                               uint32_t idesc, uint32_t accumulate) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::2.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}\n" ::"r"(d_tmem),
+        "l"(adesc), "l"(bdesc), "r"(idesc), "r"(accumulate)
+        : "memory");
+}
+
+// ---------------------------------------------------------------------------
+// TMA
+// ---------------------------------------------------------------------------
+__device__ __forceinline__ uint64_t l2_normal_policy() {
+    uint64_t p;
+    asm volatile("createpolicy.fractional.L2::evict_normal.b64 %0, 1.0;" : "=l"(p));
+    return p;
+}
+// (bar: a shared::cluster address, of either CTA of the pair)
+__device__ __forceinline__ void tma_load_5d_pair(void* dst, const CUtensorMap* map, uint32_t bar,
+                                                 int c0, int c1, int c2, int c3, int c4,
+                                                 uint64_t policy) {
+    asm volatile(
+        "cp.async.bulk.tensor.5d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes"
+        ".L2::cache_hint [%0], [%1, {%2, %3, %4, %5, %6}], [%7], %8;" ::"r"(smem_u32(dst)),
+        "l"(reinterpret_cast<uint64_t>(map)), "r"(c0), "r"(c1), "r"(c2), "r"(c3), "r"(c4), "r"(bar),
+        "l"(policy)
+        : "memory");
+}
+__device__ __forceinline__ void tma_load_2d_pair(void* dst, const CUtensorMap* map, uint32_t bar,
+                                                 int c0, int c1, uint64_t policy) {
+    asm volatile(
+        "cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes"
+        ".L2::cache_hint [%0], [%1, {%2, %3}], [%4], %5;" ::"r"(smem_u32(dst)),
+        "l"(reinterpret_cast<uint64_t>(map)), "r"(c0), "r"(c1), "r"(bar), "l"(policy)
+        : "memory");
+}
+// Four rows of a matrix, columns c0 on (the map's box is one row high).
+__device__ __forceinline__ void tma_gather4_pair(void* dst, const CUtensorMap* map, uint32_t bar,
+                                                 int c0, int r0, int r1, int r2, int r3,
+                                                 uint64_t policy) {
+    asm volatile(
+        "cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.tile::gather4"
+        ".mbarrier::complete_tx::bytes.L2::cache_hint [%0], [%1, {%2, %3, %4, %5, %6}], [%7], %8;"
+        ::"r"(smem_u32(dst)),
+        "l"(reinterpret_cast<uint64_t>(map)), "r"(c0), "r"(r0), "r"(r1), "r"(r2), "r"(r3), "r"(bar),
+        "l"(policy)
+        : "memory");
+}
+__device__ __forceinline__ void tma_load_2d(void* dst, const CUtensorMap* map, uint64_t* bar,
+                                            int c0, int c1, uint64_t policy) {
+    asm volatile(
+        "cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes"
+        ".L2::cache_hint [%0], [%1, {%2, %3}], [%4], %5;" ::"r"(smem_u32(dst)),
+        "l"(reinterpret_cast<uint64_t>(map)), "r"(c0), "r"(c1), "r"(smem_u32(bar)), "l"(policy)
+        : "memory");
+}
+__device__ __forceinline__ void tma_gather4(void* dst, const CUtensorMap* map, uint64_t* bar,
+                                            int c0, int r0, int r1, int r2, int r3,
+                                            uint64_t policy) {
+    asm volatile(
+        "cp.async.bulk.tensor.2d.shared::cluster.global.tile::gather4"
+        ".mbarrier::complete_tx::bytes.L2::cache_hint [%0], [%1, {%2, %3, %4, %5, %6}], [%7], %8;"
+        ::"r"(smem_u32(dst)),
+        "l"(reinterpret_cast<uint64_t>(map)), "r"(c0), "r"(r0), "r"(r1), "r"(r2), "r"(r3),
+        "r"(smem_u32(bar)), "l"(policy)
+        : "memory");
+}
+__device__ __forceinline__ void tma_store_3d(const CUtensorMap* map, const void* src, int c0,
+                                             int c1, int c2) {
+    asm volatile(
+        "cp.async.bulk.tensor.3d.global.shared::cta.tile.bulk_group [%0, {%2, %3, %4}], [%1];" ::"l"(
+            reinterpret_cast<uint64_t>(map)),
+        "r"(smem_u32(src)), "r"(c0), "r"(c1), "r"(c2)
+        : "memory");
+}
+
+// ---------------------------------------------------------------------------
+// the rows of every expert, and a share of the work
+// ---------------------------------------------------------------------------
+struct GroupRows {
+    const int32_t* offsets;      // [N + 1]
+    const int32_t* rows;         // [E] or NULL: row i of x
+    uint32_t* err;
+    int E, N, K;                 // row i reads x's row rows[i] / K, or i
+    int x_rows;
+};
+
+// The row of x that sorted row i reads.  What is out of x is an error, and reads row 0.
+__device__ __forceinline__ int source_row(const GroupRows& r, int i) {
+    if (!r.rows) return i;
+    const int c = r.rows[i];
+    const int s = c / r.K;
+    if (c >= 0 && s < r.x_rows) return s;
+    latch_error(r.err, CRC_EDEVICE);
+    return 0;
+}
+
+struct GroupPlan {                         // shared memory
+    long long cost[kGroupMaxExperts + 1];  // of the experts before each
+    int begin[kGroupMaxExperts], count[kGroupMaxExperts];
+};
+
+// Fills the plan: cost_of(rows) is an expert's.  All threads of the CTA; ends in a barrier.
+template <class F>
+__device__ __forceinline__ void make_plan(GroupPlan& p, const GroupRows& r, F cost_of) {
+    for (int e = threadIdx.x; e < r.N; e += blockDim.x) {
+        int b = r.offsets[e], n = r.offsets[e + 1];
+        if (b < 0 || n < b || n > r.E) {                 // not offsets of these rows
+            latch_error(r.err, CRC_EDEVICE);
+            b = n = 0;
+        }
+        p.begin[e] = b;
+        p.count[e] = n - b;
+    }
+    __syncthreads();
+    if (threadIdx.x < 32) {
+        constexpr int kEach = kGroupMaxExperts / 32;
+        const int lane = threadIdx.x;
+        long long v[kEach], sum = 0;
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) {
+            const int e = lane * kEach + i;
+            v[i] = sum;
+            if (e < r.N) sum += cost_of(p.count[e]);
+        }
+        long long incl = sum;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const long long u = __shfl_up_sync(kFull, incl, o);
+            if (lane >= o) incl += u;
+        }
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) {
+            const int e = lane * kEach + i;
+            if (e < r.N) p.cost[e] = incl - sum + v[i];
+        }
+        if (lane == 31) p.cost[r.N] = incl;
+    }
+    __syncthreads();
+}
+
+// The expert in whose share of the cost `at` lies, at < cost[N].
+__device__ __forceinline__ int expert_at(const GroupPlan& p, int N, long long at) {
+    int lo = 0, hi = N;                                  // cost[lo] <= at < cost[hi]
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) / 2;
+        if (p.cost[mid] <= at)
+            lo = mid;
+        else
+            hi = mid;
+    }
+    return lo;
+}
+
+}  // namespace crc

@@ -1,0 +1,409 @@
+// Products of ragged groups of rows with their expert's matrix, D = W_e X_e^T, on CTA pairs.
+//
+//   y_i = W_e x_row(i)                         (or silu(G_e x) * (U_e x), gate and up in W)
+//   dx_i = W_e^T dy_i                          (TW: the matrix's rows lie across the contraction)
+//
+// The matrix's rows are the 256 rows (A) of the pair's tcgen05.mma, the expert's rows its N
+// columns, 16 to 256 of them in steps of 16: rows come in ragged numbers, so a tile is as wide
+// as they are, to the next 16.  (With the rows as A, an expert's last tile of 128 or 256 would
+// be half empty on average.)  TMA stages 128-byte pieces of the contraction: 128 matrix rows a
+// CTA, and half of the tile's rows, gathered four at a time where they are a token's.  Two
+// accumulators in TMEM, so that one is drained while the next tile's products run.
+//
+// Work: tiles of (expert, 256 matrix rows, up to 256 rows), in that order, in one row of
+// equal shares for the pairs.  A share may end inside an expert's rows, at any 16 of them:
+// a tile's products do not depend on the rows beside them.  So no pair waits for a last tile
+// of another, without a counter or a workspace.
+#pragma once
+
+#include "group.cuh"
+
+namespace crc {
+
+constexpr int kGmThreads = 256;            // warps 0 weights, 1 MMA, 2 rows, 4-7 epilogue
+constexpr int kGmStages = 6;
+constexpr int kGmA = 128 * 128, kGmB = 128 * 128, kGmStage = kGmA + kGmB;   // bytes, a CTA
+constexpr int kGmUnit = 16, kGmTileUnits = 16;       // rows of a unit, units of a tile at most
+constexpr int kGmFixed = 12;               // cost of a tile beside its rows, in units
+constexpr int kGmStaging = 4 * 32 * 64;    // an epilogue warp: 32 rows x 32 columns of y
+constexpr int kGmScales = 4 * 256 * 4;     // an epilogue warp's copy of its rows' scales
+constexpr int kGmBoxRows = 32;             // rows of a TMA box of x in order
+
+struct GroupArgs {
+    GroupRows r;
+    uint16_t* y;                 // [E][out]
+    const float* xs;             // [x_rows] scales of e4m3 rows
+    const float* ws;             // e4m3: [N][out], with gate and up [N][2][out]
+    long long ws_stride;         // floats
+    int kblocks;                 // 128-byte pieces of the contraction
+    int out;                     // columns of y
+    int ftiles;                  // tiles of 256 matrix rows
+};
+
+struct GroupTile {
+    int e, ft, row, rows;        // expert, tile of matrix rows, first row of x in order, rows
+};
+
+// A pair's share of the work as a walk over its tiles.
+struct GroupWalk {
+    int e, ft, unit;             // the next piece
+    int ee, eft, eunit;          // the end, exclusive
+
+    __device__ __forceinline__ bool next(const GroupPlan& p, int ftiles, GroupTile& t) {
+        while (true) {
+            if (e > ee || (e == ee && (ft > eft || (ft == eft && unit >= eunit)))) return false;
+            const int units = (p.count[e] + kGmUnit - 1) / kGmUnit;
+            if (unit < units) {
+                const int last = e == ee && ft == eft ? min(eunit, units) : units;
+                const int pieces = (last - unit + kGmTileUnits - 1) / kGmTileUnits;
+                const int size = (last - unit + pieces - 1) / pieces;
+                t.e = e;
+                t.ft = ft;
+                t.row = p.begin[e] + unit * kGmUnit;
+                t.rows = min(size * kGmUnit, p.count[e] - unit * kGmUnit);
+                unit += size;
+                return true;
+            }
+            unit = 0;
+            if (units == 0 || ++ft == ftiles) {
+                ft = 0;
+                ++e;
+            }
+        }
+    }
+};
+
+__device__ __forceinline__ long long group_cost(int count, int ftiles) {
+    const int units = (count + kGmUnit - 1) / kGmUnit;
+    return units ? (long long)ftiles * (units + kGmFixed) : 0;
+}
+
+// Where share `i` of `n` begins.  A cut close to an end of an expert's rows (a sixteenth of
+// a share) goes there: a piece of a few rows would read its matrix rows for little.
+__device__ __forceinline__ void share_begin(const GroupPlan& p, int N, int ftiles, int i, int n,
+                                            int& e, int& ft, int& unit) {
+    const long long total = p.cost[N];
+    const long long at = total / n * i + total % n * i / n;
+    if (i >= n || at >= total) {
+        e = N;
+        ft = unit = 0;
+        return;
+    }
+    e = expert_at(p, N, at);
+    const int units = (p.count[e] + kGmUnit - 1) / kGmUnit;
+    const int each = units + kGmFixed;
+    const long long in = at - p.cost[e];
+    ft = (int)(in / each);
+    unit = (int)(in % each) - kGmFixed / 2;
+    const long long snap = total / n / 16 + kGmFixed / 2;
+    if (unit <= snap) {
+        unit = 0;
+    } else if (units - unit <= snap) {
+        unit = 0;
+        if (++ft == ftiles) {
+            ft = 0;
+            ++e;
+        }
+    }
+}
+
+__device__ __forceinline__ float gm_silu_up(float gate, float up) {
+    return __fdividef(gate, 1.f + __expf(-gate)) * up;
+}
+
+struct GroupSmem {
+    static constexpr size_t bytes() {
+        return 1024 + (size_t)kGmStages * kGmStage + kGmStaging + kGmScales + sizeof(GroupPlan) + 512;
+    }
+};
+
+// W8: e4m3 rows and matrices.  GLU: gate and up, 16 and 16 rows of a quarter of TMEM.
+// TW: the matrix is [contraction][matrix rows].
+template <bool W8, bool GLU, bool TW>
+__global__ void __launch_bounds__(kGmThreads, 1)
+    group_matmul_kernel(const __grid_constant__ CUtensorMap mw,
+                        const __grid_constant__ CUtensorMap mx, GroupArgs a) {
+    constexpr int kElems = W8 ? 128 : 64;              // elements of a 128-byte piece
+    extern __shared__ __align__(1024) uint8_t smem_raw[];
+    uint8_t* smem = reinterpret_cast<uint8_t*>(
+        (reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+    uint8_t* staging = smem + kGmStages * kGmStage;
+    float* scales = reinterpret_cast<float*>(staging + kGmStaging);
+    GroupPlan& plan = *reinterpret_cast<GroupPlan*>(staging + kGmStaging + kGmScales);
+    uint64_t* full_bar = reinterpret_cast<uint64_t*>(
+        reinterpret_cast<uint8_t*>(&plan) + (sizeof(GroupPlan) + 15) / 16 * 16);
+    uint64_t* empty_bar = full_bar + kGmStages;
+    uint64_t* tfull_bar = empty_bar + kGmStages;
+    uint64_t* tempty_bar = tfull_bar + 2;
+    uint64_t* drain_bar = tempty_bar + 2;
+    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(drain_bar + 1);
+
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint32_t rank = cluster_ctarank();
+    const bool leader = rank == 0u;
+
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < kGmStages; ++s) {
+            mbar_init(&full_bar[s], 2);                // the weights' producer and the rows'
+            mbar_init(&empty_bar[s], 1);
+        }
+        for (int s = 0; s < 2; ++s) {
+            mbar_init(&tfull_bar[s], 1);
+            mbar_init(&tempty_bar[s], 8);              // four warps of each CTA
+        }
+        mbar_init(drain_bar, 1);
+        fence_mbar_init();
+        tma_prefetch_desc(&mw);
+        tma_prefetch_desc(&mx);
+    }
+    if (warp == 1) {
+        tmem_alloc_pair(tmem_slot, 512);
+        tmem_relinquish_pair();
+    }
+    pdl_begin();
+    make_plan(plan, a.r, [&](int n) { return group_cost(n, a.ftiles); });
+    tc_fence_before();
+    __syncthreads();
+    cluster_sync();                     // the peer's barriers exist before any remote use
+    tc_fence_after();
+    const uint32_t tmem_base = *tmem_slot;
+
+    GroupWalk walk;
+    const int pair = (int)blockIdx.x >> 1, pairs = (int)gridDim.x >> 1;
+    share_begin(plan, a.r.N, a.ftiles, pair, pairs, walk.e, walk.ft, walk.unit);
+    share_begin(plan, a.r.N, a.ftiles, pair + 1, pairs, walk.ee, walk.eft, walk.eunit);
+    GroupTile t;
+
+    if (warp == 0) {
+        // ---------------------------------------------------------- matrix rows
+        if (lane == 0) {
+            const uint64_t pol = l2_normal_policy();
+            // both CTAs' loads of a stage complete on the even CTA's barrier
+            const uint32_t lead_full = cluster_map(&full_bar[0], 0u);
+            int stage = 0, issued = 0, failed = 0;
+            uint32_t phase = 0;
+            while (!failed && walk.next(plan, a.ftiles, t)) {
+                for (int kb = 0; kb < a.kblocks; ++kb) {
+                    if (!mbar_wait_cluster(&empty_bar[stage], phase ^ 1)) {
+                        latch_error(a.r.err, CRC_ETIMEOUT);
+                        failed = 1;
+                        break;
+                    }
+                    uint8_t* sa = smem + stage * kGmStage;
+                    if (leader) mbar_arrive_expect_tx(&full_bar[stage], 2 * kGmA);
+                    const uint32_t fb = lead_full + (uint32_t)(stage * 8);
+                    if constexpr (TW) {
+                        const int f0 = t.ft * 256 + (int)rank * 128;
+                        tma_load_3d_pair(sa, &mw, fb, f0, kb * 64, t.e, pol);
+                        tma_load_3d_pair(sa + 8192, &mw, fb, f0 + 64, kb * 64, t.e, pol);
+                    } else if constexpr (GLU) {
+                        // four times 16 gate rows and the 16 up rows beside them
+                        tma_load_5d_pair(sa, &mw, fb, kb * kElems, 0, 0, t.ft * 8 + (int)rank * 4,
+                                         t.e, pol);
+                    } else {
+                        tma_load_3d_pair(sa, &mw, fb, kb * kElems, t.ft * 256 + (int)rank * 128,
+                                         t.e, pol);
+                    }
+                    ++issued;
+                    if (++stage == kGmStages) {
+                        stage = 0;
+                        phase ^= 1;
+                    }
+                }
+            }
+            // Never leave with copies in flight (the even CTA's barriers see both CTAs'
+            // loads; the odd one stays for the final cluster barrier).
+            int s = stage;
+            uint32_t ph = phase;
+            for (int k = 0; k < (leader ? min(issued, kGmStages) : 0); ++k) {
+                if (--s < 0) {
+                    s = kGmStages - 1;
+                    ph ^= 1;
+                }
+                if (!mbar_wait_cluster(&full_bar[s], ph)) latch_error(a.r.err, CRC_ETIMEOUT);
+            }
+        }
+    } else if (warp == 2) {
+        // ---------------------------------------------------------- rows of x
+        const uint64_t pol = l2_normal_policy();
+        const uint32_t lead_full = cluster_map(&full_bar[0], 0u);
+        int stage = 0;
+        uint32_t phase = 0;
+        bool ok = true;
+        while (ok && walk.next(plan, a.ftiles, t)) {
+            const int half = (t.rows + kGmUnit - 1) / kGmUnit * (kGmUnit / 2);   // rows of a CTA
+            const int first = (int)rank * half;
+            const int boxes = (half + kGmBoxRows - 1) / kGmBoxRows;
+            const uint32_t bytes = a.r.rows ? half * 128 : boxes * kGmBoxRows * 128;
+            int src[4] = {0, 0, 0, 0};
+            if (a.r.rows && lane < half / 4)
+#pragma unroll
+                for (int i = 0; i < 4; ++i)             // behind the last row: that row again
+                    src[i] = source_row(a.r, t.row + min(first + lane * 4 + i, t.rows - 1));
+            for (int kb = 0; kb < a.kblocks; ++kb) {
+                ok = __all_sync(kFull, lane != 0 || mbar_wait_cluster(&empty_bar[stage], phase ^ 1));
+                if (!ok) {
+                    latch_error(a.r.err, CRC_ETIMEOUT);
+                    break;
+                }
+                if (leader && lane == 0) mbar_arrive_expect_tx(&full_bar[stage], 2 * bytes);
+                __syncwarp();
+                uint8_t* sb = smem + stage * kGmStage + kGmA;
+                const uint32_t fb = lead_full + (uint32_t)(stage * 8);
+                if (a.r.rows) {
+                    if (lane < half / 4)
+                        tma_gather4_pair(sb + lane * 512, &mx, fb, kb * kElems, src[0], src[1],
+                                         src[2], src[3], pol);
+                } else if (lane < boxes) {
+                    tma_load_2d_pair(sb + lane * kGmBoxRows * 128, &mx, fb, kb * kElems,
+                                     t.row + first + lane * kGmBoxRows, pol);
+                }
+                if (++stage == kGmStages) {
+                    stage = 0;
+                    phase ^= 1;
+                }
+            }
+        }
+    } else if (warp == 1) {
+        // ---------------------------------------------------------- MMA
+        if (lane == 0 && leader) {
+            int stage = 0, acc = 0, failed = 0;
+            uint32_t phase = 0, acc_phase = 0;
+            while (!failed && walk.next(plan, a.ftiles, t)) {
+                if (!mbar_wait_cluster(&tempty_bar[acc], acc_phase ^ 1)) {
+                    latch_error(a.r.err, CRC_ETIMEOUT);
+                    break;
+                }
+                tc_fence_after();
+                const int cols = (t.rows + kGmUnit - 1) / kGmUnit * kGmUnit;
+                const uint32_t idesc = W8 ? idesc_e4m3_f32_mn(256, cols)
+                                          : idesc_bf16_f32(256, cols) | (TW ? kIdescMnA : 0);
+                const uint32_t d_tmem = tmem_base + (uint32_t)(acc * 256);
+                for (int kb = 0; kb < a.kblocks; ++kb) {
+                    if (!mbar_wait_cluster(&full_bar[stage], phase)) {
+                        latch_error(a.r.err, CRC_ETIMEOUT);
+                        failed = 1;
+                        break;
+                    }
+                    tc_fence_after();
+                    const uint32_t sa = smem_u32(smem + stage * kGmStage);
+                    const uint32_t sb = sa + kGmA;
+#pragma unroll
+                    for (int kk = 0; kk < 4; ++kk) {
+                        const uint64_t ad = TW ? sw128_mnmajor_desc(sa + kk * 2048, 8192)
+                                               : sw128_kmajor_desc(sa + kk * 32);
+                        const uint64_t bd = sw128_kmajor_desc(sb + kk * 32);
+                        if constexpr (W8)
+                            umma_e4m3_pair(d_tmem, ad, bd, idesc, (kb | kk) != 0);
+                        else
+                            umma_bf16_pair(d_tmem, ad, bd, idesc, (kb | kk) != 0);
+                    }
+                    umma_commit_pair(&empty_bar[stage]);
+                    if (++stage == kGmStages) {
+                        stage = 0;
+                        phase ^= 1;
+                    }
+                }
+                if (failed) break;
+                umma_commit_pair(&tfull_bar[acc]);
+                acc ^= 1;
+                if (acc == 0) acc_phase ^= 1;
+            }
+            umma_commit_pair_local(drain_bar);
+            if (!mbar_wait(drain_bar, 0)) latch_error(a.r.err, CRC_ETIMEOUT);
+        }
+    } else if (warp >= 4) {
+        // ---------------------------------------------------------- epilogue
+        const int quarter = warp & 3;
+        uint16_t* stage_y = reinterpret_cast<uint16_t*>(staging + quarter * 32 * 64);
+        const uint32_t tempty_lead = cluster_map(&tempty_bar[0], 0u);
+        constexpr int kOut = GLU ? 16 : 32;             // columns of y of a warp
+        int acc = 0;
+        uint32_t acc_phase = 0;
+        while (walk.next(plan, a.ftiles, t)) {
+            // this warp's first column of y, and this lane's (its gate's or its up's)
+            const int col0 = t.ft * (8 * kOut) + (int)rank * (4 * kOut) + quarter * kOut;
+            const int col = col0 + (GLU ? lane & 15 : lane);
+            float ws = 1.f;
+            if (W8 && col < a.out)
+                ws = a.ws[(long long)t.e * a.ws_stride +
+                          (GLU && lane >= 16 ? (long long)a.out : 0) + col];
+            float* xs = scales + quarter * 256;
+            if constexpr (W8) {
+                float s[8] = {};
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    if (i * 32 + lane < t.rows)
+                        s[i] = a.xs[source_row(a.r, t.row + i * 32 + lane)];
+                __syncwarp();
+#pragma unroll
+                for (int i = 0; i < 8; ++i) xs[i * 32 + lane] = s[i];
+                __syncwarp();
+            }
+            if (!__all_sync(kFull, mbar_wait_cluster(&tfull_bar[acc], acc_phase))) {
+                latch_error(a.r.err, CRC_ETIMEOUT);
+                break;
+            }
+            tc_fence_after();
+            const uint32_t tbase =
+                tmem_base + (uint32_t)(acc * 256) + ((uint32_t)(quarter * 32) << 16);
+            for (int c0 = 0; c0 < t.rows; c0 += 32) {
+                float v[32];
+                tmem_ld32(tbase + (uint32_t)c0, v);
+                tmem_ld_wait();
+                pin16(v);
+                pin16(v + 16);
+#pragma unroll
+                for (int c = 0; c < 32; c += GLU ? 2 : 1) {
+                    if constexpr (W8) {
+                        v[c] *= ws * xs[c0 + c];
+                        if constexpr (GLU) v[c + 1] *= ws * xs[c0 + c + 1];
+                    }
+                    if constexpr (GLU) {
+                        // gate lanes keep row c and take its up, up lanes row c + 1 and its gate
+                        const bool up = lane >= 16;
+                        const float other = __shfl_xor_sync(kFull, up ? v[c] : v[c + 1], 16);
+                        const float y = up ? gm_silu_up(other, v[c + 1]) : gm_silu_up(v[c], other);
+                        stage_y[(c + (up ? 1 : 0)) * kOut + (lane & 15)] =
+                            __bfloat16_as_ushort(__float2bfloat16_rn(y));
+                    } else {
+                        stage_y[c * kOut + lane] = __bfloat16_as_ushort(__float2bfloat16_rn(v[c]));
+                    }
+                }
+                __syncwarp();
+                constexpr int kPieces = kOut / 8;       // 16-byte pieces of a row
+#pragma unroll
+                for (int i = lane; i < 32 * kPieces; i += 32) {
+                    const int c = c0 + i / kPieces, at = col0 + i % kPieces * 8;
+                    if (c < t.rows && at < a.out &&
+                        CRC_IN_BOUNDS(t.row + c < a.r.E && t.e < a.r.N, a.r.err))
+                        *reinterpret_cast<uint4*>(a.y + (long long)(t.row + c) * a.out + at) =
+                            reinterpret_cast<const uint4*>(stage_y)[i];
+                }
+                __syncwarp();
+            }
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) {
+                if (leader)
+                    mbar_arrive(&tempty_bar[acc]);
+                else
+                    mbar_arrive_remote(tempty_lead + (uint32_t)(acc * 8));
+            }
+            acc ^= 1;
+            if (acc == 0) acc_phase ^= 1;
+        }
+    }
+
+    tc_fence_before();
+    __syncthreads();
+    // neither CTA leaves (or frees TMEM) while the other may still arrive on its
+    // barriers or have MMAs write its TMEM
+    cluster_sync();
+    if (warp == 1) {
+        tc_fence_after();
+        tmem_dealloc_pair(tmem_base, 512);
+    }
+}
+
+}  // namespace crc

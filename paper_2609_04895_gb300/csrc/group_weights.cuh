@@ -1,0 +1,299 @@
+// Gradients of the experts' matrices, dW_e = sum over its rows of dy_i x_row(i)^T.
+//
+// The contraction runs over an expert's rows, so both operands lie across it (MN-major): a
+// block is 64 rows of dy and x as they are in memory, 128 columns of dy (the 128 rows of
+// tcgen05.mma's A) and 256 of x (its N).  The last block of an expert holds rows of the next
+// one: those up to the next 16 are zeroed in shared memory (both operands: a product with
+// another expert's infinity would not be zero), and the steps behind them are left out.
+//
+// What bounds it: an expert has some hundred rows, so a tile's 32768 sums are written after a
+// few blocks, 128 KB in fp32; the writes of dW are most of its bytes.  Tiles leave through
+// shared memory by TMA.  An expert without rows has zeros.
+//
+// Work: tiles of (expert, 128 rows, 256 columns of dW) in one row of shares for the CTAs, equal
+// in their cost (a constant for the output, and the blocks).
+#pragma once
+
+#include "group.cuh"
+
+namespace crc {
+
+constexpr int kGwThreads = 256;            // warps 0 dy, 1 MMA, 2 x, 4-7 epilogue
+constexpr int kGwRows = 64;                // rows of a block
+constexpr int kGwM = 128, kGwN = 256;
+constexpr int kGwA = kGwRows * kGwM * 2, kGwB = kGwRows * kGwN * 2, kGwStage = kGwA + kGwB;
+constexpr int kGwChunk = kGwRows * 128;    // 64 columns of a block
+constexpr int kGwStages = 4;
+constexpr int kGwBufs = 1;                 // pieces of 32 rows x 128 bytes of an epilogue warp
+constexpr int kGwStaging = 4 * kGwBufs * 4096;
+
+struct GroupGradArgs {
+    GroupRows r;
+    int mtiles, ntiles;          // of an expert's matrix [n][k]
+    int n, k;
+};
+
+struct GroupGradSmem {
+    static constexpr size_t bytes() {
+        return 1024 + (size_t)kGwStages * kGwStage + kGwStaging + 256;
+    }
+};
+static_assert(GroupGradSmem::bytes() + sizeof(GroupPlan) < 232448, "shared memory");
+
+// Rows `tail` .. of a block's six pieces of 64 columns, to the next 16: zeros.
+__device__ __forceinline__ void clear_rows(uint8_t* stage, int tail, int lane) {
+    const int end = (tail + 15) / 16 * 16, pieces = (end - tail) * 8;      // of 16 bytes
+#pragma unroll 1
+    for (int c = 0; c < kGwStage / kGwChunk; ++c)
+        for (int i = lane; i < pieces; i += 32)
+            *reinterpret_cast<uint4*>(stage + c * kGwChunk + tail * 128 + i * 16) =
+                make_uint4(0, 0, 0, 0);
+    fence_proxy_async_smem();
+    __syncwarp();
+}
+
+template <bool F32>
+__global__ void __launch_bounds__(kGwThreads, 1)
+    group_weights_grad_kernel(const __grid_constant__ CUtensorMap mdy,
+                              const __grid_constant__ CUtensorMap mx,
+                              const __grid_constant__ CUtensorMap mdw, GroupGradArgs a) {
+    extern __shared__ __align__(1024) uint8_t smem_raw[];
+    __shared__ GroupPlan plan;
+    uint8_t* smem = reinterpret_cast<uint8_t*>(
+        (reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+    uint8_t* staging = smem + kGwStages * kGwStage;
+    uint64_t* full_bar = reinterpret_cast<uint64_t*>(staging + kGwStaging);
+    uint64_t* empty_bar = full_bar + kGwStages;
+    uint64_t* tfull_bar = empty_bar + kGwStages;
+    uint64_t* tempty_bar = tfull_bar + 2;
+    uint64_t* drain_bar = tempty_bar + 2;
+    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(drain_bar + 1);
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < kGwStages; ++s) {
+            mbar_init(&full_bar[s], 2);
+            mbar_init(&empty_bar[s], 1);
+        }
+        for (int s = 0; s < 2; ++s) {
+            mbar_init(&tfull_bar[s], 1);
+            mbar_init(&tempty_bar[s], 4);
+        }
+        mbar_init(drain_bar, 1);
+        fence_mbar_init();
+        tma_prefetch_desc(&mdy);
+        tma_prefetch_desc(&mx);
+        tma_prefetch_desc(&mdw);
+    }
+    if (warp == 1) {
+        tmem_alloc(tmem_slot, 512);
+        tmem_relinquish();
+    }
+    pdl_begin();
+    const int tiles = a.mtiles * a.ntiles;               // of an expert
+    constexpr int kOut = F32 ? 12 : 6;                   // a tile's output, in blocks of rows
+    const auto each = [](int rows) { return kOut + (rows + kGwRows - 1) / kGwRows; };
+    make_plan(plan, a.r, [&](int rows) { return (long long)tiles * each(rows); });
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem_base = *tmem_slot;
+    // this CTA's tiles: from the first that begins in its share to the first of the next one
+    const long long total = plan.cost[a.r.N];
+    const auto first_of = [&](int i) {
+        const long long at = total / gridDim.x * i + total % gridDim.x * i / gridDim.x;
+        if (at >= total) return (long long)a.r.N * tiles;
+        const int e = expert_at(plan, a.r.N, at);
+        const int c = each(plan.count[e]);
+        return (long long)e * tiles + (at - plan.cost[e] + c - 1) / c;
+    };
+    const long long begin = first_of(blockIdx.x), end = first_of(blockIdx.x + 1);
+
+    if (warp == 0 || warp == 2) {
+        // ---------------------------------------------------------- rows of dy, of x
+        const uint64_t pol = l2_normal_policy();
+        const bool is_x = warp == 2, gather = is_x && a.r.rows;
+        int stage = 0, issued = 0;
+        uint32_t phase = 0;
+        bool ok = true;
+        for (long long w = begin; w < end && ok; ++w) {
+            const int e = (int)(w / tiles), tile = (int)(w % tiles);
+            const int count = plan.count[e], row0 = plan.begin[e];
+            const int col = is_x ? tile % a.ntiles * kGwN : tile / a.ntiles * kGwM;
+            for (int r = 0; r < count; r += kGwRows) {
+                ok = __all_sync(kFull, lane != 0 || mbar_wait(&empty_bar[stage], phase ^ 1));
+                if (!ok) {
+                    latch_error(a.r.err, CRC_ETIMEOUT);
+                    break;
+                }
+                uint8_t* s = smem + stage * kGwStage + (is_x ? kGwA : 0);
+                if (lane == 0) mbar_arrive_expect_tx(&full_bar[stage], is_x ? kGwB : kGwA);
+                __syncwarp();
+                if (!gather) {
+                    if (lane < (is_x ? kGwN : kGwM) / 64)
+                        tma_load_2d(s + lane * kGwChunk, is_x ? &mx : &mdy, &full_bar[stage],
+                                    col + lane * 64, row0 + r, pol);
+                } else {
+                    // sixteen fours of rows, of four pieces of 64 columns: two a lane
+                    int src[4];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        src[i] = source_row(a.r, row0 + min(r + (lane & 15) * 4 + i, count - 1));
+#pragma unroll
+                    for (int c = lane >> 4; c < kGwN / 64; c += 2)
+                        tma_gather4(s + c * kGwChunk + (lane & 15) * 512, &mx, &full_bar[stage],
+                                    col + c * 64, src[0], src[1], src[2], src[3], pol);
+                }
+                ++issued;
+                if (++stage == kGwStages) {
+                    stage = 0;
+                    phase ^= 1;
+                }
+            }
+        }
+        // Never leave with copies in flight.
+        if (lane == 0) {
+            int s = stage;
+            uint32_t ph = phase;
+            for (int k = 0; k < min(issued, kGwStages); ++k) {
+                if (--s < 0) {
+                    s = kGwStages - 1;
+                    ph ^= 1;
+                }
+                if (!mbar_wait(&full_bar[s], ph)) latch_error(a.r.err, CRC_ETIMEOUT);
+            }
+        }
+    } else if (warp == 1) {
+        // ---------------------------------------------------------- MMA
+        constexpr uint32_t kIdesc = idesc_bf16_f32(kGwM, kGwN) | kIdescMnA | kIdescMnB;
+        int stage = 0, acc = 0;
+        uint32_t phase = 0, acc_phase = 0;
+        bool ok = true;
+        for (long long w = begin; w < end && ok; ++w) {
+            const int count = plan.count[(int)(w / tiles)];
+            if (count == 0) continue;
+            ok = mbar_wait_warp(&tempty_bar[acc], acc_phase ^ 1);
+            if (!ok) {
+                latch_error(a.r.err, CRC_ETIMEOUT);
+                break;
+            }
+            tc_fence_after();
+            const uint32_t d_tmem = tmem_base + (uint32_t)(acc * 256);
+            for (int r = 0; r < count; r += kGwRows) {
+                ok = mbar_wait_warp(&full_bar[stage], phase);
+                if (!ok) {
+                    latch_error(a.r.err, CRC_ETIMEOUT);
+                    break;
+                }
+                const int some = min(count - r, kGwRows);
+                uint8_t* s = smem + stage * kGwStage;
+                if (some % 16) clear_rows(s, some, lane);
+                tc_fence_after();
+                if (lane == 0) {
+                    const uint32_t sa = smem_u32(s), sb = sa + kGwA;
+                    for (int kk = 0; kk * 16 < some; ++kk)
+                        umma_bf16(d_tmem, sw128_mnmajor_desc(sa + kk * 2048, kGwChunk),
+                                  sw128_mnmajor_desc(sb + kk * 2048, kGwChunk), kIdesc,
+                                  (r | kk) != 0);
+                    umma_commit(&empty_bar[stage]);
+                }
+                __syncwarp();
+                if (++stage == kGwStages) {
+                    stage = 0;
+                    phase ^= 1;
+                }
+            }
+            if (!ok) break;
+            if (lane == 0) umma_commit(&tfull_bar[acc]);
+            __syncwarp();
+            acc ^= 1;
+            if (acc == 0) acc_phase ^= 1;
+        }
+        if (lane == 0) {
+            umma_commit(drain_bar);
+            if (!mbar_wait(drain_bar, 0)) latch_error(a.r.err, CRC_ETIMEOUT);
+        }
+    } else if (warp >= 4) {
+        // ---------------------------------------------------------- epilogue
+        const int quarter = warp & 3;
+        uint8_t* my_stage = staging + quarter * kGwBufs * 4096;
+        constexpr int kCols = F32 ? 32 : 64;             // columns of a 128-byte piece
+        int acc = 0, buf = 0;
+        uint32_t acc_phase = 0;
+        for (long long w = begin; w < end; ++w) {
+            const int e = (int)(w / tiles), tile = (int)(w % tiles);
+            const int row = tile / a.ntiles * kGwM + quarter * 32, col = tile % a.ntiles * kGwN;
+            const bool some = plan.count[e] > 0;
+            if (some) {
+                if (!mbar_wait_warp(&tfull_bar[acc], acc_phase)) {
+                    latch_error(a.r.err, CRC_ETIMEOUT);
+                    break;
+                }
+                tc_fence_after();
+            }
+            const uint32_t tbase =
+                tmem_base + (uint32_t)(acc * 256) + ((uint32_t)(quarter * 32) << 16);
+#pragma unroll 1
+            for (int c = 0; c < kGwN; c += kCols) {
+                uint4 q[8];
+                if (some) {
+                    float v[kCols];
+#pragma unroll
+                    for (int i = 0; i < kCols; i += 32) tmem_ld32(tbase + (uint32_t)(c + i), v + i);
+                    tmem_ld_wait();
+#pragma unroll
+                    for (int i = 0; i < kCols; i += 16) pin16(v + i);
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) {
+                        uint32_t u[4];
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            if constexpr (F32) {
+                                u[i] = __float_as_uint(v[4 * j + i]);
+                            } else {
+                                const __nv_bfloat162 h =
+                                    __floats2bfloat162_rn(v[8 * j + 2 * i], v[8 * j + 2 * i + 1]);
+                                u[i] = *reinterpret_cast<const uint32_t*>(&h);
+                            }
+                        }
+                        q[j] = make_uint4(u[0], u[1], u[2], u[3]);
+                    }
+                } else {
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) q[j] = make_uint4(0, 0, 0, 0);
+                }
+                uint8_t* sbuf = my_stage + buf * 4096;
+                buf = (buf + 1) % kGwBufs;
+                if (lane == 0) bulk_wait_read<kGwBufs - 1>();      // the store that used sbuf is done
+                __syncwarp();
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+                    *reinterpret_cast<uint4*>(sbuf + lane * 128 + ((j ^ (lane & 7)) << 4)) = q[j];
+                fence_proxy_async_smem();
+                __syncwarp();
+                if (lane == 0 && row < a.n && col + c < a.k &&
+                    CRC_IN_BOUNDS(e < a.r.N && row >= 0, a.r.err)) {
+                    tma_store_3d(&mdw, sbuf, col + c, row, e);
+                    bulk_commit();
+                }
+            }
+            if (some) {
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&tempty_bar[acc]);
+                acc ^= 1;
+                if (acc == 0) acc_phase ^= 1;
+            }
+        }
+        if (lane == 0) bulk_wait<0>();                   // every store has landed
+    }
+
+    tc_fence_before();
+    __syncthreads();
+    if (warp == 1) {
+        tc_fence_after();
+        tmem_dealloc(tmem_base, 512);
+    }
+}
+
+}  // namespace crc
