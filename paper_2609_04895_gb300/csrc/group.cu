@@ -25,7 +25,7 @@ bool encode(CUtensorMap* m, CUtensorMapDataType type, int rank, const void* base
 
 constexpr CUtensorMapDataType kBf16Map = CU_TENSOR_MAP_DATA_TYPE_BFLOAT16;
 
-// Rows of x: four gathered (a box of one row), or `rows` in order.
+// `rows` rows of x in order; 1: four gathered.
 bool rows_map(CUtensorMap* m, bool w8, const void* x, int64_t x_rows, int k, int64_t x_stride,
               int rows) {
     const int es = w8 ? 1 : 2;

@@ -20,7 +20,9 @@
 
 namespace crc {
 
-constexpr int kGmThreads = 256;            // warps 0 weights, 1 MMA, 2 rows, 4-7 epilogue
+// Warps 0 weights, 1 MMA, 2 rows in order, 4-7 epilogue, 8-15 gathered rows.
+constexpr int kGmThreads = 512;
+constexpr int kGmGatherWarps = 8;
 constexpr int kGmStages = 6;
 constexpr int kGmA = 128 * 128, kGmB = 128 * 128, kGmStage = kGmA + kGmB;   // bytes, a CTA
 constexpr int kGmUnit = 16, kGmTileUnits = 16;       // rows of a unit, units of a tile at most
@@ -44,67 +46,26 @@ struct GroupTile {
     int e, ft, row, rows;        // expert, tile of matrix rows, first row of x in order, rows
 };
 
-// A pair's share of the work as a walk over its tiles.
-struct GroupWalk {
-    int e, ft, unit;             // the next piece
-    int ee, eft, eunit;          // the end, exclusive
-
-    __device__ __forceinline__ bool next(const GroupPlan& p, int ftiles, GroupTile& t) {
-        while (true) {
-            if (e > ee || (e == ee && (ft > eft || (ft == eft && unit >= eunit)))) return false;
-            const int units = (p.count[e] + kGmUnit - 1) / kGmUnit;
-            if (unit < units) {
-                const int last = e == ee && ft == eft ? min(eunit, units) : units;
-                const int pieces = (last - unit + kGmTileUnits - 1) / kGmTileUnits;
-                const int size = (last - unit + pieces - 1) / pieces;
-                t.e = e;
-                t.ft = ft;
-                t.row = p.begin[e] + unit * kGmUnit;
-                t.rows = min(size * kGmUnit, p.count[e] - unit * kGmUnit);
-                unit += size;
-                return true;
-            }
-            unit = 0;
-            if (units == 0 || ++ft == ftiles) {
-                ft = 0;
-                ++e;
-            }
-        }
-    }
-};
-
-__device__ __forceinline__ long long group_cost(int count, int ftiles) {
-    const int units = (count + kGmUnit - 1) / kGmUnit;
-    return units ? (long long)ftiles * (units + kGmFixed) : 0;
+// Tiles of an expert with `count` rows.
+__device__ __forceinline__ long long group_tiles(int count, int ftiles) {
+    constexpr int kRows = kGmUnit * kGmTileUnits;
+    return (long long)ftiles * ((count + kRows - 1) / kRows);
 }
 
-// Where share `i` of `n` begins.  A cut close to an end of an expert's rows (a sixteenth of
-// a share) goes there: a piece of a few rows would read its matrix rows for little.
-__device__ __forceinline__ void share_begin(const GroupPlan& p, int N, int ftiles, int i, int n,
-                                            int& e, int& ft, int& unit) {
-    const long long total = p.cost[N];
-    const long long at = total / n * i + total % n * i / n;
-    if (i >= n || at >= total) {
-        e = N;
-        ft = unit = 0;
-        return;
-    }
-    e = expert_at(p, N, at);
-    const int units = (p.count[e] + kGmUnit - 1) / kGmUnit;
-    const int each = units + kGmFixed;
-    const long long in = at - p.cost[e];
-    ft = (int)(in / each);
-    unit = (int)(in % each) - kGmFixed / 2;
-    const long long snap = total / n / 16 + kGmFixed / 2;
-    if (unit <= snap) {
-        unit = 0;
-    } else if (units - unit <= snap) {
-        unit = 0;
-        if (++ft == ftiles) {
-            ft = 0;
-            ++e;
-        }
-    }
+// Tile `i` of the call, i < cost[N]: an expert's rows in equal tiles, one after the other for
+// each tile of its matrix.
+__device__ __forceinline__ GroupTile group_tile(const GroupPlan& p, int N, int ftiles,
+                                                long long i) {
+    GroupTile t;
+    t.e = expert_at(p, N, i);
+    const int count = p.count[t.e], units = (count + kGmUnit - 1) / kGmUnit;
+    const int pieces = (units + kGmTileUnits - 1) / kGmTileUnits;
+    const int in = (int)(i - p.cost[t.e]);
+    const int size = (units + pieces - 1) / pieces, unit = in % pieces * size;
+    t.ft = in / pieces;
+    t.row = p.begin[t.e] + unit * kGmUnit;
+    t.rows = min(size * kGmUnit, count - unit * kGmUnit);
+    return t;
 }
 
 __device__ __forceinline__ float gm_silu_up(float gate, float up) {
@@ -161,18 +122,15 @@ __global__ void __launch_bounds__(kGmThreads, 1)
         tmem_relinquish_pair();
     }
     pdl_begin();
-    make_plan(plan, a.r, [&](int n) { return group_cost(n, a.ftiles); });
+    make_plan(plan, a.r, [&](int n) { return group_tiles(n, a.ftiles); });
     tc_fence_before();
     __syncthreads();
     cluster_sync();                     // the peer's barriers exist before any remote use
     tc_fence_after();
     const uint32_t tmem_base = *tmem_slot;
 
-    GroupWalk walk;
     const int pair = (int)blockIdx.x >> 1, pairs = (int)gridDim.x >> 1;
-    share_begin(plan, a.r.N, a.ftiles, pair, pairs, walk.e, walk.ft, walk.unit);
-    share_begin(plan, a.r.N, a.ftiles, pair + 1, pairs, walk.ee, walk.eft, walk.eunit);
-    GroupTile t;
+    const long long tiles = plan.cost[a.r.N];
 
     if (warp == 0) {
         // ---------------------------------------------------------- matrix rows
@@ -182,7 +140,8 @@ __global__ void __launch_bounds__(kGmThreads, 1)
             const uint32_t lead_full = cluster_map(&full_bar[0], 0u);
             int stage = 0, issued = 0, failed = 0;
             uint32_t phase = 0;
-            while (!failed && walk.next(plan, a.ftiles, t)) {
+            for (long long i = pair; i < tiles && !failed; i += pairs) {
+                const GroupTile t = group_tile(plan, a.r.N, a.ftiles, i);
                 for (int kb = 0; kb < a.kblocks; ++kb) {
                     if (!mbar_wait_cluster(&empty_bar[stage], phase ^ 1)) {
                         latch_error(a.r.err, CRC_ETIMEOUT);
@@ -223,41 +182,70 @@ __global__ void __launch_bounds__(kGmThreads, 1)
                 if (!mbar_wait_cluster(&full_bar[s], ph)) latch_error(a.r.err, CRC_ETIMEOUT);
             }
         }
-    } else if (warp == 2) {
-        // ---------------------------------------------------------- rows of x
+    } else if (warp == 2 && !a.r.rows) {
+        // ---------------------------------------------------------- rows in order
+        if (lane == 0) {
+            const uint64_t pol = l2_normal_policy();
+            const uint32_t lead_full = cluster_map(&full_bar[0], 0u);
+            int stage = 0, failed = 0;
+            uint32_t phase = 0;
+            for (long long i = pair; i < tiles && !failed; i += pairs) {
+                const GroupTile t = group_tile(plan, a.r.N, a.ftiles, i);
+                const int half = (t.rows + kGmUnit - 1) / kGmUnit * (kGmUnit / 2);
+                const int first = t.row + (int)rank * half;            // this CTA's rows
+                const int boxes = (half + kGmBoxRows - 1) / kGmBoxRows;
+                for (int kb = 0; kb < a.kblocks; ++kb) {
+                    if (!mbar_wait_cluster(&empty_bar[stage], phase ^ 1)) {
+                        latch_error(a.r.err, CRC_ETIMEOUT);
+                        failed = 1;
+                        break;
+                    }
+                    uint8_t* sb = smem + stage * kGmStage + kGmA;
+                    if (leader)
+                        mbar_arrive_expect_tx(&full_bar[stage], 2 * boxes * kGmBoxRows * 128);
+                    const uint32_t fb = lead_full + (uint32_t)(stage * 8);
+                    for (int b = 0; b < boxes; ++b)
+                        tma_load_2d_pair(sb + b * kGmBoxRows * 128, &mx, fb, kb * kElems,
+                                         first + b * kGmBoxRows, pol);
+                    if (++stage == kGmStages) {
+                        stage = 0;
+                        phase ^= 1;
+                    }
+                }
+            }
+        }
+    } else if (warp >= 8 && a.r.rows) {
+        // ---------------------------------------------------------- gathered rows
+        // lane l of warp w: the four rows 4 f .., f = 8 l + w
         const uint64_t pol = l2_normal_policy();
         const uint32_t lead_full = cluster_map(&full_bar[0], 0u);
+        const int f = lane * kGmGatherWarps + warp - 8;
         int stage = 0;
         uint32_t phase = 0;
         bool ok = true;
-        while (ok && walk.next(plan, a.ftiles, t)) {
-            const int half = (t.rows + kGmUnit - 1) / kGmUnit * (kGmUnit / 2);   // rows of a CTA
-            const int first = (int)rank * half;
-            const int boxes = (half + kGmBoxRows - 1) / kGmBoxRows;
-            const uint32_t bytes = a.r.rows ? half * 128 : boxes * kGmBoxRows * 128;
+        for (long long i = pair; i < tiles && ok; i += pairs) {
+            const GroupTile t = group_tile(plan, a.r.N, a.ftiles, i);
+            const int half = (t.rows + kGmUnit - 1) / kGmUnit * (kGmUnit / 2);
+            const bool mine = f < half / 4;
             int src[4] = {0, 0, 0, 0};
-            if (a.r.rows && lane < half / 4)
+            if (mine)
 #pragma unroll
-                for (int i = 0; i < 4; ++i)             // behind the last row: that row again
-                    src[i] = source_row(a.r, t.row + min(first + lane * 4 + i, t.rows - 1));
+                for (int q = 0; q < 4; ++q)             // behind the last row: that row again
+                    src[q] = source_row(a.r,
+                                        t.row + min((int)rank * half + f * 4 + q, t.rows - 1));
             for (int kb = 0; kb < a.kblocks; ++kb) {
-                ok = __all_sync(kFull, lane != 0 || mbar_wait_cluster(&empty_bar[stage], phase ^ 1));
+                ok = __all_sync(kFull,
+                                lane != 0 || mbar_wait_cluster(&empty_bar[stage], phase ^ 1));
                 if (!ok) {
                     latch_error(a.r.err, CRC_ETIMEOUT);
                     break;
                 }
-                if (leader && lane == 0) mbar_arrive_expect_tx(&full_bar[stage], 2 * bytes);
+                if (leader && f == 0) mbar_arrive_expect_tx(&full_bar[stage], 2 * half * 128);
+                if (mine)
+                    tma_gather4_pair(smem + stage * kGmStage + kGmA + f * 512, &mx,
+                                     lead_full + (uint32_t)(stage * 8), kb * kElems, src[0],
+                                     src[1], src[2], src[3], pol);
                 __syncwarp();
-                uint8_t* sb = smem + stage * kGmStage + kGmA;
-                const uint32_t fb = lead_full + (uint32_t)(stage * 8);
-                if (a.r.rows) {
-                    if (lane < half / 4)
-                        tma_gather4_pair(sb + lane * 512, &mx, fb, kb * kElems, src[0], src[1],
-                                         src[2], src[3], pol);
-                } else if (lane < boxes) {
-                    tma_load_2d_pair(sb + lane * kGmBoxRows * 128, &mx, fb, kb * kElems,
-                                     t.row + first + lane * kGmBoxRows, pol);
-                }
                 if (++stage == kGmStages) {
                     stage = 0;
                     phase ^= 1;
@@ -266,11 +254,13 @@ __global__ void __launch_bounds__(kGmThreads, 1)
         }
     } else if (warp == 1) {
         // ---------------------------------------------------------- MMA
-        if (lane == 0 && leader) {
+        if (leader) {
+            const uint32_t lead = elected();
             int stage = 0, acc = 0, failed = 0;
             uint32_t phase = 0, acc_phase = 0;
-            while (!failed && walk.next(plan, a.ftiles, t)) {
-                if (!mbar_wait_cluster(&tempty_bar[acc], acc_phase ^ 1)) {
+            for (long long i = pair; i < tiles && !failed; i += pairs) {
+                const GroupTile t = group_tile(plan, a.r.N, a.ftiles, i);
+                if (!__all_sync(kFull, mbar_wait_cluster(&tempty_bar[acc], acc_phase ^ 1))) {
                     latch_error(a.r.err, CRC_ETIMEOUT);
                     break;
                 }
@@ -280,39 +270,37 @@ __global__ void __launch_bounds__(kGmThreads, 1)
                                           : idesc_bf16_f32(256, cols) | (TW ? kIdescMnA : 0);
                 const uint32_t d_tmem = tmem_base + (uint32_t)(acc * 256);
                 for (int kb = 0; kb < a.kblocks; ++kb) {
-                    if (!mbar_wait_cluster(&full_bar[stage], phase)) {
+                    if (!__all_sync(kFull, mbar_wait_cluster(&full_bar[stage], phase))) {
                         latch_error(a.r.err, CRC_ETIMEOUT);
                         failed = 1;
                         break;
                     }
                     tc_fence_after();
-                    const uint32_t sa = smem_u32(smem + stage * kGmStage);
-                    const uint32_t sb = sa + kGmA;
+                    const uint32_t sa = smem_u32(smem + stage * kGmStage), sb = sa + kGmA;
 #pragma unroll
-                    for (int kk = 0; kk < 4; ++kk) {
-                        const uint64_t ad = TW ? sw128_mnmajor_desc(sa + kk * 2048, 8192)
-                                               : sw128_kmajor_desc(sa + kk * 32);
-                        const uint64_t bd = sw128_kmajor_desc(sb + kk * 32);
-                        if constexpr (W8)
-                            umma_e4m3_pair(d_tmem, ad, bd, idesc, (kb | kk) != 0);
-                        else
-                            umma_bf16_pair(d_tmem, ad, bd, idesc, (kb | kk) != 0);
-                    }
-                    umma_commit_pair(&empty_bar[stage]);
+                    for (int kk = 0; kk < 4; ++kk)
+                        umma_pair_by<W8>(d_tmem,
+                                         TW ? sw128_mnmajor_desc(sa + kk * 2048, 8192)
+                                            : sw128_kmajor_desc(sa + kk * 32),
+                                         sw128_kmajor_desc(sb + kk * 32), idesc, (kb | kk) != 0,
+                                         lead);
+                    commit_pair_by(&empty_bar[stage], lead);
                     if (++stage == kGmStages) {
                         stage = 0;
                         phase ^= 1;
                     }
                 }
                 if (failed) break;
-                umma_commit_pair(&tfull_bar[acc]);
+                commit_pair_by(&tfull_bar[acc], lead);
                 acc ^= 1;
                 if (acc == 0) acc_phase ^= 1;
             }
-            umma_commit_pair_local(drain_bar);
-            if (!mbar_wait(drain_bar, 0)) latch_error(a.r.err, CRC_ETIMEOUT);
+            if (lead) {
+                umma_commit_pair_local(drain_bar);
+                if (!mbar_wait(drain_bar, 0)) latch_error(a.r.err, CRC_ETIMEOUT);
+            }
         }
-    } else if (warp >= 4) {
+    } else if (warp >= 4 && warp < 8) {
         // ---------------------------------------------------------- epilogue
         const int quarter = warp & 3;
         uint16_t* stage_y = reinterpret_cast<uint16_t*>(staging + quarter * 32 * 64);
@@ -320,7 +308,8 @@ __global__ void __launch_bounds__(kGmThreads, 1)
         constexpr int kOut = GLU ? 16 : 32;             // columns of y of a warp
         int acc = 0;
         uint32_t acc_phase = 0;
-        while (walk.next(plan, a.ftiles, t)) {
+        for (long long i = pair; i < tiles; i += pairs) {
+            const GroupTile t = group_tile(plan, a.r.N, a.ftiles, i);
             // this warp's first column of y, and this lane's (its gate's or its up's)
             const int col0 = t.ft * (8 * kOut) + (int)rank * (4 * kOut) + quarter * kOut;
             const int col = col0 + (GLU ? lane & 15 : lane);

@@ -10,15 +10,17 @@
 // few blocks, 128 KB in fp32; the writes of dW are most of its bytes.  Tiles leave through
 // shared memory by TMA.  An expert without rows has zeros.
 //
-// Work: tiles of (expert, 128 rows, 256 columns of dW) in one row of shares for the CTAs, equal
-// in their cost (a constant for the output, and the blocks).
+// Work: tiles of (expert, 128 rows, 256 columns of dW), dealt to the CTAs in turn, so that
+// those running together share an expert's rows in L2.
 #pragma once
 
 #include "group.cuh"
 
 namespace crc {
 
-constexpr int kGwThreads = 256;            // warps 0 dy, 1 MMA, 2 x, 4-7 epilogue
+// Warps 0 dy, 1 MMA, 2 x in order, 4-7 epilogue, 8-15 gathered rows of x.
+constexpr int kGwThreads = 512;
+constexpr int kGwGatherWarps = 8;
 constexpr int kGwRows = 64;                // rows of a block
 constexpr int kGwM = 128, kGwN = 256;
 constexpr int kGwA = kGwRows * kGwM * 2, kGwB = kGwRows * kGwN * 2, kGwStage = kGwA + kGwB;
@@ -72,7 +74,7 @@ __global__ void __launch_bounds__(kGwThreads, 1)
 
     if (threadIdx.x == 0) {
         for (int s = 0; s < kGwStages; ++s) {
-            mbar_init(&full_bar[s], 2);
+            mbar_init(&full_bar[s], 2);                // dy and x
             mbar_init(&empty_bar[s], 1);
         }
         for (int s = 0; s < 2; ++s) {
@@ -91,32 +93,21 @@ __global__ void __launch_bounds__(kGwThreads, 1)
     }
     pdl_begin();
     const int tiles = a.mtiles * a.ntiles;               // of an expert
-    constexpr int kOut = F32 ? 12 : 6;                   // a tile's output, in blocks of rows
-    const auto each = [](int rows) { return kOut + (rows + kGwRows - 1) / kGwRows; };
-    make_plan(plan, a.r, [&](int rows) { return (long long)tiles * each(rows); });
+    make_plan(plan, a.r, [&](int) { return (long long)tiles; });
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem_base = *tmem_slot;
-    // this CTA's tiles: from the first that begins in its share to the first of the next one
-    const long long total = plan.cost[a.r.N];
-    const auto first_of = [&](int i) {
-        const long long at = total / gridDim.x * i + total % gridDim.x * i / gridDim.x;
-        if (at >= total) return (long long)a.r.N * tiles;
-        const int e = expert_at(plan, a.r.N, at);
-        const int c = each(plan.count[e]);
-        return (long long)e * tiles + (at - plan.cost[e] + c - 1) / c;
-    };
-    const long long begin = first_of(blockIdx.x), end = first_of(blockIdx.x + 1);
+    const long long all = (long long)a.r.N * tiles;
 
-    if (warp == 0 || warp == 2) {
+    if (warp == 0 || (warp == 2 && !a.r.rows)) {
         // ---------------------------------------------------------- rows of dy, of x
         const uint64_t pol = l2_normal_policy();
-        const bool is_x = warp == 2, gather = is_x && a.r.rows;
+        const bool is_x = warp == 2;
         int stage = 0, issued = 0;
         uint32_t phase = 0;
         bool ok = true;
-        for (long long w = begin; w < end && ok; ++w) {
+        for (long long w = blockIdx.x; w < all && ok; w += gridDim.x) {
             const int e = (int)(w / tiles), tile = (int)(w % tiles);
             const int count = plan.count[e], row0 = plan.begin[e];
             const int col = is_x ? tile % a.ntiles * kGwN : tile / a.ntiles * kGwM;
@@ -129,21 +120,9 @@ __global__ void __launch_bounds__(kGwThreads, 1)
                 uint8_t* s = smem + stage * kGwStage + (is_x ? kGwA : 0);
                 if (lane == 0) mbar_arrive_expect_tx(&full_bar[stage], is_x ? kGwB : kGwA);
                 __syncwarp();
-                if (!gather) {
-                    if (lane < (is_x ? kGwN : kGwM) / 64)
-                        tma_load_2d(s + lane * kGwChunk, is_x ? &mx : &mdy, &full_bar[stage],
-                                    col + lane * 64, row0 + r, pol);
-                } else {
-                    // sixteen fours of rows, of four pieces of 64 columns: two a lane
-                    int src[4];
-#pragma unroll
-                    for (int i = 0; i < 4; ++i)
-                        src[i] = source_row(a.r, row0 + min(r + (lane & 15) * 4 + i, count - 1));
-#pragma unroll
-                    for (int c = lane >> 4; c < kGwN / 64; c += 2)
-                        tma_gather4(s + c * kGwChunk + (lane & 15) * 512, &mx, &full_bar[stage],
-                                    col + c * 64, src[0], src[1], src[2], src[3], pol);
-                }
+                if (lane < (is_x ? kGwN : kGwM) / 64)
+                    tma_load_2d(s + lane * kGwChunk, is_x ? &mx : &mdy, &full_bar[stage],
+                                col + lane * 64, row0 + r, pol);
                 ++issued;
                 if (++stage == kGwStages) {
                     stage = 0;
@@ -163,13 +142,47 @@ __global__ void __launch_bounds__(kGwThreads, 1)
                 if (!mbar_wait(&full_bar[s], ph)) latch_error(a.r.err, CRC_ETIMEOUT);
             }
         }
+    } else if (warp >= 8 && a.r.rows) {
+        // ---------------------------------------------------------- gathered rows of x
+        // lane l of warp w: the four rows 4 f .. of 64 columns, f = 2 w + (l & 1)
+        const uint64_t pol = l2_normal_policy();
+        const int f = (warp - 8) * 2 + (lane & 1), c = lane >> 1;
+        int stage = 0;
+        uint32_t phase = 0;
+        bool ok = true;
+        for (long long w = blockIdx.x; w < all && ok; w += gridDim.x) {
+            const int e = (int)(w / tiles), tile = (int)(w % tiles);
+            const int count = plan.count[e], row0 = plan.begin[e];
+            const int col = tile % a.ntiles * kGwN + c * 64;
+            for (int r = 0; r < count; r += kGwRows) {
+                int src[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i)             // behind the last row: that row again
+                    src[i] = source_row(a.r, row0 + min(r + f * 4 + i, count - 1));
+                ok = __all_sync(kFull, lane != 0 || mbar_wait(&empty_bar[stage], phase ^ 1));
+                if (!ok) {
+                    latch_error(a.r.err, CRC_ETIMEOUT);
+                    break;
+                }
+                if (warp == 8 && lane == 0) mbar_arrive_expect_tx(&full_bar[stage], kGwB);
+                if (c < kGwN / 64)
+                    tma_gather4(smem + stage * kGwStage + kGwA + c * kGwChunk + f * 512, &mx,
+                                &full_bar[stage], col, src[0], src[1], src[2], src[3], pol);
+                __syncwarp();
+                if (++stage == kGwStages) {
+                    stage = 0;
+                    phase ^= 1;
+                }
+            }
+        }
     } else if (warp == 1) {
         // ---------------------------------------------------------- MMA
         constexpr uint32_t kIdesc = idesc_bf16_f32(kGwM, kGwN) | kIdescMnA | kIdescMnB;
+        const uint32_t lead = elected();
         int stage = 0, acc = 0;
         uint32_t phase = 0, acc_phase = 0;
         bool ok = true;
-        for (long long w = begin; w < end && ok; ++w) {
+        for (long long w = blockIdx.x; w < all && ok; w += gridDim.x) {
             const int count = plan.count[(int)(w / tiles)];
             if (count == 0) continue;
             ok = mbar_wait_warp(&tempty_bar[acc], acc_phase ^ 1);
@@ -189,38 +202,36 @@ __global__ void __launch_bounds__(kGwThreads, 1)
                 uint8_t* s = smem + stage * kGwStage;
                 if (some % 16) clear_rows(s, some, lane);
                 tc_fence_after();
-                if (lane == 0) {
-                    const uint32_t sa = smem_u32(s), sb = sa + kGwA;
-                    for (int kk = 0; kk * 16 < some; ++kk)
-                        umma_bf16(d_tmem, sw128_mnmajor_desc(sa + kk * 2048, kGwChunk),
-                                  sw128_mnmajor_desc(sb + kk * 2048, kGwChunk), kIdesc,
-                                  (r | kk) != 0);
-                    umma_commit(&empty_bar[stage]);
-                }
-                __syncwarp();
+                const uint32_t sa = smem_u32(s), sb = sa + kGwA;
+#pragma unroll
+                for (int kk = 0; kk < kGwRows / 16; ++kk)
+                    if (kk * 16 < some)
+                        umma_bf16_by(d_tmem, sw128_mnmajor_desc(sa + kk * 2048, kGwChunk),
+                                     sw128_mnmajor_desc(sb + kk * 2048, kGwChunk), kIdesc,
+                                     (r | kk) != 0, lead);
+                commit_by(&empty_bar[stage], lead);
                 if (++stage == kGwStages) {
                     stage = 0;
                     phase ^= 1;
                 }
             }
             if (!ok) break;
-            if (lane == 0) umma_commit(&tfull_bar[acc]);
-            __syncwarp();
+            commit_by(&tfull_bar[acc], lead);
             acc ^= 1;
             if (acc == 0) acc_phase ^= 1;
         }
-        if (lane == 0) {
+        if (lead) {
             umma_commit(drain_bar);
             if (!mbar_wait(drain_bar, 0)) latch_error(a.r.err, CRC_ETIMEOUT);
         }
-    } else if (warp >= 4) {
+    } else if (warp >= 4 && warp < 8) {
         // ---------------------------------------------------------- epilogue
         const int quarter = warp & 3;
         uint8_t* my_stage = staging + quarter * kGwBufs * 4096;
         constexpr int kCols = F32 ? 32 : 64;             // columns of a 128-byte piece
         int acc = 0, buf = 0;
         uint32_t acc_phase = 0;
-        for (long long w = begin; w < end; ++w) {
+        for (long long w = blockIdx.x; w < all; w += gridDim.x) {
             const int e = (int)(w / tiles), tile = (int)(w % tiles);
             const int row = tile / a.ntiles * kGwM + quarter * 32, col = tile % a.ntiles * kGwN;
             const bool some = plan.count[e] > 0;
