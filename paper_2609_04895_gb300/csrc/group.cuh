@@ -104,55 +104,78 @@ __device__ __forceinline__ uint64_t l2_normal_policy() {
     asm volatile("createpolicy.fractional.L2::evict_normal.b64 %0, 1.0;" : "=l"(p));
     return p;
 }
-// (bar: a shared::cluster address, of either CTA of the pair)
-__device__ __forceinline__ void tma_load_5d_pair(void* dst, const CUtensorMap* map, uint32_t bar,
-                                                 int c0, int c1, int c2, int c3, int c4,
-                                                 uint64_t policy) {
+// (bar: a shared::cluster address, of either CTA of the pair.  Issued by the lane whose `lead` is
+// set, in code that the whole warp runs.)
+__device__ __forceinline__ void tma_load_5d_pair_by(uint32_t lead, void* dst,
+                                                    const CUtensorMap* map, uint32_t bar, int c0,
+                                                    int c1, int c2, int c3, int c4,
+                                                    uint64_t policy) {
     asm volatile(
-        "cp.async.bulk.tensor.5d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes"
-        ".L2::cache_hint [%0], [%1, {%2, %3, %4, %5, %6}], [%7], %8;" ::"r"(smem_u32(dst)),
+        "{\n\t.reg .pred e;\n\tsetp.ne.b32 e, %9, 0;\n\t"
+        "@e cp.async.bulk.tensor.5d.cta_group::2.shared::cluster.global.tile"
+        ".mbarrier::complete_tx::bytes.L2::cache_hint [%0], [%1, {%2, %3, %4, %5, %6}], [%7], "
+        "%8;\n\t}" ::"r"(smem_u32(dst)),
         "l"(reinterpret_cast<uint64_t>(map)), "r"(c0), "r"(c1), "r"(c2), "r"(c3), "r"(c4), "r"(bar),
-        "l"(policy)
+        "l"(policy), "r"(lead)
         : "memory");
 }
-__device__ __forceinline__ void tma_load_2d_pair(void* dst, const CUtensorMap* map, uint32_t bar,
-                                                 int c0, int c1, uint64_t policy) {
+__device__ __forceinline__ void tma_load_3d_pair_by(uint32_t lead, void* dst,
+                                                    const CUtensorMap* map, uint32_t bar, int c0,
+                                                    int c1, int c2, uint64_t policy) {
     asm volatile(
-        "cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes"
-        ".L2::cache_hint [%0], [%1, {%2, %3}], [%4], %5;" ::"r"(smem_u32(dst)),
-        "l"(reinterpret_cast<uint64_t>(map)), "r"(c0), "r"(c1), "r"(bar), "l"(policy)
+        "{\n\t.reg .pred e;\n\tsetp.ne.b32 e, %7, 0;\n\t"
+        "@e cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.tile"
+        ".mbarrier::complete_tx::bytes.L2::cache_hint [%0], [%1, {%2, %3, %4}], [%5], %6;\n\t}" ::"r"(
+            smem_u32(dst)),
+        "l"(reinterpret_cast<uint64_t>(map)), "r"(c0), "r"(c1), "r"(c2), "r"(bar), "l"(policy),
+        "r"(lead)
         : "memory");
 }
-// Four rows of a matrix, columns c0 on (the map's box is one row high).  Several warps share a
-// tile's: an instruction of a lane of its own takes some 46 ns to issue.
-__device__ __forceinline__ void tma_gather4_pair(void* dst, const CUtensorMap* map, uint32_t bar,
-                                                 int c0, int r0, int r1, int r2, int r3,
-                                                 uint64_t policy) {
+__device__ __forceinline__ void tma_load_2d_pair_by(uint32_t lead, void* dst,
+                                                    const CUtensorMap* map, uint32_t bar, int c0,
+                                                    int c1, uint64_t policy) {
     asm volatile(
-        "cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.tile::gather4"
-        ".mbarrier::complete_tx::bytes.L2::cache_hint [%0], [%1, {%2, %3, %4, %5, %6}], [%7], %8;"
-        ::"r"(smem_u32(dst)),
-        "l"(reinterpret_cast<uint64_t>(map)), "r"(c0), "r"(r0), "r"(r1), "r"(r2), "r"(r3), "r"(bar),
-        "l"(policy)
+        "{\n\t.reg .pred e;\n\tsetp.ne.b32 e, %6, 0;\n\t"
+        "@e cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.tile"
+        ".mbarrier::complete_tx::bytes.L2::cache_hint [%0], [%1, {%2, %3}], [%4], %5;\n\t}" ::"r"(
+            smem_u32(dst)),
+        "l"(reinterpret_cast<uint64_t>(map)), "r"(c0), "r"(c1), "r"(bar), "l"(policy), "r"(lead)
         : "memory");
 }
-__device__ __forceinline__ void tma_gather4(void* dst, const CUtensorMap* map, uint64_t* bar,
-                                            int c0, int r0, int r1, int r2, int r3,
-                                            uint64_t policy) {
+// Four rows of a matrix, columns c0 on (the map's box is one row high).
+__device__ __forceinline__ void tma_gather4_pair_by(uint32_t lead, void* dst,
+                                                    const CUtensorMap* map, uint32_t bar, int c0,
+                                                    const int (&r)[4], uint64_t policy) {
     asm volatile(
-        "cp.async.bulk.tensor.2d.shared::cluster.global.tile::gather4"
-        ".mbarrier::complete_tx::bytes.L2::cache_hint [%0], [%1, {%2, %3, %4, %5, %6}], [%7], %8;"
-        ::"r"(smem_u32(dst)),
-        "l"(reinterpret_cast<uint64_t>(map)), "r"(c0), "r"(r0), "r"(r1), "r"(r2), "r"(r3),
-        "r"(smem_u32(bar)), "l"(policy)
+        "{\n\t.reg .pred e;\n\tsetp.ne.b32 e, %9, 0;\n\t"
+        "@e cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.tile::gather4"
+        ".mbarrier::complete_tx::bytes.L2::cache_hint [%0], [%1, {%2, %3, %4, %5, %6}], [%7], "
+        "%8;\n\t}" ::"r"(smem_u32(dst)),
+        "l"(reinterpret_cast<uint64_t>(map)), "r"(c0), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]),
+        "r"(bar), "l"(policy), "r"(lead)
         : "memory");
 }
-__device__ __forceinline__ void tma_load_2d(void* dst, const CUtensorMap* map, uint64_t* bar,
-                                            int c0, int c1, uint64_t policy) {
+__device__ __forceinline__ void tma_gather4_by(uint32_t lead, void* dst, const CUtensorMap* map,
+                                               uint64_t* bar, int c0, const int (&r)[4],
+                                               uint64_t policy) {
     asm volatile(
-        "cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes"
-        ".L2::cache_hint [%0], [%1, {%2, %3}], [%4], %5;" ::"r"(smem_u32(dst)),
-        "l"(reinterpret_cast<uint64_t>(map)), "r"(c0), "r"(c1), "r"(smem_u32(bar)), "l"(policy)
+        "{\n\t.reg .pred e;\n\tsetp.ne.b32 e, %9, 0;\n\t"
+        "@e cp.async.bulk.tensor.2d.shared::cluster.global.tile::gather4"
+        ".mbarrier::complete_tx::bytes.L2::cache_hint [%0], [%1, {%2, %3, %4, %5, %6}], [%7], "
+        "%8;\n\t}" ::"r"(smem_u32(dst)),
+        "l"(reinterpret_cast<uint64_t>(map)), "r"(c0), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]),
+        "r"(smem_u32(bar)), "l"(policy), "r"(lead)
+        : "memory");
+}
+__device__ __forceinline__ void tma_load_2d_by(uint32_t lead, void* dst, const CUtensorMap* map,
+                                               uint64_t* bar, int c0, int c1, uint64_t policy) {
+    asm volatile(
+        "{\n\t.reg .pred e;\n\tsetp.ne.b32 e, %6, 0;\n\t"
+        "@e cp.async.bulk.tensor.2d.shared::cluster.global.tile"
+        ".mbarrier::complete_tx::bytes.L2::cache_hint [%0], [%1, {%2, %3}], [%4], %5;\n\t}" ::"r"(
+            smem_u32(dst)),
+        "l"(reinterpret_cast<uint64_t>(map)), "r"(c0), "r"(c1), "r"(smem_u32(bar)), "l"(policy),
+        "r"(lead)
         : "memory");
 }
 __device__ __forceinline__ void tma_store_3d(const CUtensorMap* map, const void* src, int c0,
@@ -162,6 +185,29 @@ __device__ __forceinline__ void tma_store_3d(const CUtensorMap* map, const void*
             reinterpret_cast<uint64_t>(map)),
         "r"(smem_u32(src)), "r"(c0), "r"(c1), "r"(c2)
         : "memory");
+}
+
+// ---------------------------------------------------------------------------
+// an accumulator's transpose
+// ---------------------------------------------------------------------------
+// 16 lanes x 32 columns of TMEM: v[4 i + 2 h + b] is lane t / 4 + 8 h, column 8 i + 2 (t % 4) + b
+// of thread t, the fragments of 8 x 8 matrices that stmatrix takes.
+__device__ __forceinline__ void tmem_ld_frag(uint32_t taddr, float (&v)[16]) {
+    asm volatile(
+        "tcgen05.ld.sync.aligned.16x256b.x4.b32 "
+        "{%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
+        : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]), "=f"(v[4]), "=f"(v[5]), "=f"(v[6]),
+          "=f"(v[7]), "=f"(v[8]), "=f"(v[9]), "=f"(v[10]), "=f"(v[11]), "=f"(v[12]),
+          "=f"(v[13]), "=f"(v[14]), "=f"(v[15])
+        : "r"(taddr));
+}
+// Four 8 x 8 matrices of bf16, stored by columns: 16 bytes at the address that lane 8 m + c
+// gives are column c of matrix m.
+__device__ __forceinline__ void store_transposed(uint32_t addr, const uint32_t (&r)[4]) {
+    asm volatile("stmatrix.sync.aligned.m8n8.x4.trans.shared.b16 [%0], {%1, %2, %3, %4};" ::"r"(
+                     addr),
+                 "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3])
+                 : "memory");
 }
 
 // ---------------------------------------------------------------------------

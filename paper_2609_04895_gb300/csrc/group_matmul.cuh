@@ -27,8 +27,8 @@ constexpr int kGmStages = 6;
 constexpr int kGmA = 128 * 128, kGmB = 128 * 128, kGmStage = kGmA + kGmB;   // bytes, a CTA
 constexpr int kGmUnit = 16, kGmTileUnits = 16;       // rows of a unit, units of a tile at most
 constexpr int kGmFixed = 12;               // cost of a tile beside its rows, in units
-constexpr int kGmStaging = 4 * 32 * 64;    // an epilogue warp: 32 rows x 32 columns of y
-constexpr int kGmScales = 4 * 256 * 4;     // an epilogue warp's copy of its rows' scales
+constexpr int kGmStaging = 2 * 32 * 256;   // two pieces of 32 rows x 128 columns of y
+constexpr int kGmScales = 2 * 256 * 4;     // the scales of a tile's rows, of two tiles
 constexpr int kGmBoxRows = 32;             // rows of a TMA box of x in order
 
 struct GroupArgs {
@@ -66,6 +66,19 @@ __device__ __forceinline__ GroupTile group_tile(const GroupPlan& p, int N, int f
     t.row = p.begin[t.e] + unit * kGmUnit;
     t.rows = min(size * kGmUnit, count - unit * kGmUnit);
     return t;
+}
+
+// All of 128 threads; orders what they did before it before what they do after.  It has no
+// limit of its own: the epilogue's warps make the same calls until one outcome is false.
+__device__ __forceinline__ bool group4_all(bool ok, int id) {
+    uint32_t all;
+    asm volatile(
+        "{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %1, 0;\n\t"
+        "barrier.cta.red.and.pred q, %2, 128, p;\n\tselp.u32 %0, 1, 0, q;\n\t}\n"
+        : "=r"(all)
+        : "r"((uint32_t)ok), "r"(id)
+        : "memory");
+    return all != 0;
 }
 
 __device__ __forceinline__ float gm_silu_up(float gate, float up) {
@@ -134,47 +147,49 @@ __global__ void __launch_bounds__(kGmThreads, 1)
 
     if (warp == 0) {
         // ---------------------------------------------------------- matrix rows
-        if (lane == 0) {
-            const uint64_t pol = l2_normal_policy();
-            // both CTAs' loads of a stage complete on the even CTA's barrier
-            const uint32_t lead_full = cluster_map(&full_bar[0], 0u);
-            int stage = 0, issued = 0, failed = 0;
-            uint32_t phase = 0;
-            for (long long i = pair; i < tiles && !failed; i += pairs) {
-                const GroupTile t = group_tile(plan, a.r.N, a.ftiles, i);
-                for (int kb = 0; kb < a.kblocks; ++kb) {
-                    if (!mbar_wait_cluster(&empty_bar[stage], phase ^ 1)) {
-                        latch_error(a.r.err, CRC_ETIMEOUT);
-                        failed = 1;
-                        break;
-                    }
-                    uint8_t* sa = smem + stage * kGmStage;
-                    if (leader) mbar_arrive_expect_tx(&full_bar[stage], 2 * kGmA);
-                    const uint32_t fb = lead_full + (uint32_t)(stage * 8);
-                    if constexpr (TW) {
-                        const int f0 = t.ft * 256 + (int)rank * 128;
-                        tma_load_3d_pair(sa, &mw, fb, f0, kb * 64, t.e, pol);
-                        tma_load_3d_pair(sa + 8192, &mw, fb, f0 + 64, kb * 64, t.e, pol);
-                    } else if constexpr (GLU) {
-                        // four times 16 gate rows and the 16 up rows beside them
-                        tma_load_5d_pair(sa, &mw, fb, kb * kElems, 0, 0, t.ft * 8 + (int)rank * 4,
-                                         t.e, pol);
-                    } else {
-                        tma_load_3d_pair(sa, &mw, fb, kb * kElems, t.ft * 256 + (int)rank * 128,
-                                         t.e, pol);
-                    }
-                    ++issued;
-                    if (++stage == kGmStages) {
-                        stage = 0;
-                        phase ^= 1;
-                    }
+        const uint32_t lead = elected();
+        const uint64_t pol = l2_normal_policy();
+        // both CTAs' loads of a stage complete on the even CTA's barrier
+        const uint32_t lead_full = cluster_map(&full_bar[0], 0u);
+        int stage = 0, issued = 0;
+        uint32_t phase = 0;
+        bool ok = true;
+        for (long long i = pair; i < tiles && ok; i += pairs) {
+            const GroupTile t = group_tile(plan, a.r.N, a.ftiles, i);
+            for (int kb = 0; kb < a.kblocks; ++kb) {
+                ok = __all_sync(kFull, mbar_wait_cluster(&empty_bar[stage], phase ^ 1));
+                if (!ok) {
+                    latch_error(a.r.err, CRC_ETIMEOUT);
+                    break;
+                }
+                uint8_t* sa = smem + stage * kGmStage;
+                if (leader && lead) mbar_arrive_expect_tx(&full_bar[stage], 2 * kGmA);
+                const uint32_t fb = lead_full + (uint32_t)(stage * 8);
+                if constexpr (TW) {
+                    const int f0 = t.ft * 256 + (int)rank * 128;
+                    tma_load_3d_pair_by(lead, sa, &mw, fb, f0, kb * 64, t.e, pol);
+                    tma_load_3d_pair_by(lead, sa + 8192, &mw, fb, f0 + 64, kb * 64, t.e, pol);
+                } else if constexpr (GLU) {
+                    // four times 16 gate rows and the 16 up rows beside them
+                    tma_load_5d_pair_by(lead, sa, &mw, fb, kb * kElems, 0, 0,
+                                        t.ft * 8 + (int)rank * 4, t.e, pol);
+                } else {
+                    tma_load_3d_pair_by(lead, sa, &mw, fb, kb * kElems,
+                                        t.ft * 256 + (int)rank * 128, t.e, pol);
+                }
+                ++issued;
+                if (++stage == kGmStages) {
+                    stage = 0;
+                    phase ^= 1;
                 }
             }
-            // Never leave with copies in flight (the even CTA's barriers see both CTAs'
-            // loads; the odd one stays for the final cluster barrier).
+        }
+        // Never leave with copies in flight (the even CTA's barriers see both CTAs'
+        // loads; the odd one stays for the final cluster barrier).
+        if (leader && lead) {
             int s = stage;
             uint32_t ph = phase;
-            for (int k = 0; k < (leader ? min(issued, kGmStages) : 0); ++k) {
+            for (int k = 0; k < min(issued, kGmStages); ++k) {
                 if (--s < 0) {
                     s = kGmStages - 1;
                     ph ^= 1;
@@ -184,68 +199,74 @@ __global__ void __launch_bounds__(kGmThreads, 1)
         }
     } else if (warp == 2 && !a.r.rows) {
         // ---------------------------------------------------------- rows in order
-        if (lane == 0) {
-            const uint64_t pol = l2_normal_policy();
-            const uint32_t lead_full = cluster_map(&full_bar[0], 0u);
-            int stage = 0, failed = 0;
-            uint32_t phase = 0;
-            for (long long i = pair; i < tiles && !failed; i += pairs) {
-                const GroupTile t = group_tile(plan, a.r.N, a.ftiles, i);
-                const int half = (t.rows + kGmUnit - 1) / kGmUnit * (kGmUnit / 2);
-                const int first = t.row + (int)rank * half;            // this CTA's rows
-                const int boxes = (half + kGmBoxRows - 1) / kGmBoxRows;
-                for (int kb = 0; kb < a.kblocks; ++kb) {
-                    if (!mbar_wait_cluster(&empty_bar[stage], phase ^ 1)) {
-                        latch_error(a.r.err, CRC_ETIMEOUT);
-                        failed = 1;
-                        break;
-                    }
-                    uint8_t* sb = smem + stage * kGmStage + kGmA;
-                    if (leader)
-                        mbar_arrive_expect_tx(&full_bar[stage], 2 * boxes * kGmBoxRows * 128);
-                    const uint32_t fb = lead_full + (uint32_t)(stage * 8);
-                    for (int b = 0; b < boxes; ++b)
-                        tma_load_2d_pair(sb + b * kGmBoxRows * 128, &mx, fb, kb * kElems,
-                                         first + b * kGmBoxRows, pol);
-                    if (++stage == kGmStages) {
-                        stage = 0;
-                        phase ^= 1;
-                    }
-                }
-            }
-        }
-    } else if (warp >= 8 && a.r.rows) {
-        // ---------------------------------------------------------- gathered rows
-        // lane l of warp w: the four rows 4 f .., f = 8 l + w
+        const uint32_t lead = elected();
         const uint64_t pol = l2_normal_policy();
         const uint32_t lead_full = cluster_map(&full_bar[0], 0u);
-        const int f = lane * kGmGatherWarps + warp - 8;
         int stage = 0;
         uint32_t phase = 0;
         bool ok = true;
         for (long long i = pair; i < tiles && ok; i += pairs) {
             const GroupTile t = group_tile(plan, a.r.N, a.ftiles, i);
             const int half = (t.rows + kGmUnit - 1) / kGmUnit * (kGmUnit / 2);
-            const bool mine = f < half / 4;
-            int src[4] = {0, 0, 0, 0};
-            if (mine)
-#pragma unroll
-                for (int q = 0; q < 4; ++q)             // behind the last row: that row again
-                    src[q] = source_row(a.r,
-                                        t.row + min((int)rank * half + f * 4 + q, t.rows - 1));
+            const int first = t.row + (int)rank * half;                // this CTA's rows
+            const int boxes = (half + kGmBoxRows - 1) / kGmBoxRows;
             for (int kb = 0; kb < a.kblocks; ++kb) {
-                ok = __all_sync(kFull,
-                                lane != 0 || mbar_wait_cluster(&empty_bar[stage], phase ^ 1));
+                ok = __all_sync(kFull, mbar_wait_cluster(&empty_bar[stage], phase ^ 1));
                 if (!ok) {
                     latch_error(a.r.err, CRC_ETIMEOUT);
                     break;
                 }
-                if (leader && f == 0) mbar_arrive_expect_tx(&full_bar[stage], 2 * half * 128);
-                if (mine)
-                    tma_gather4_pair(smem + stage * kGmStage + kGmA + f * 512, &mx,
-                                     lead_full + (uint32_t)(stage * 8), kb * kElems, src[0],
-                                     src[1], src[2], src[3], pol);
-                __syncwarp();
+                uint8_t* sb = smem + stage * kGmStage + kGmA;
+                if (leader && lead)
+                    mbar_arrive_expect_tx(&full_bar[stage], 2 * boxes * kGmBoxRows * 128);
+                const uint32_t fb = lead_full + (uint32_t)(stage * 8);
+                for (int b = 0; b < boxes; ++b)
+                    tma_load_2d_pair_by(lead, sb + b * kGmBoxRows * 128, &mx, fb, kb * kElems,
+                                        first + b * kGmBoxRows, pol);
+                if (++stage == kGmStages) {
+                    stage = 0;
+                    phase ^= 1;
+                }
+            }
+        }
+    } else if (warp >= 8 && a.r.rows) {
+        // ---------------------------------------------------------- gathered rows
+        // warp w: the four rows 4 f .., f = w, w + 8, w + 16, w + 24 of this CTA's
+        const uint32_t lead = elected();
+        const uint64_t pol = l2_normal_policy();
+        const uint32_t lead_full = cluster_map(&full_bar[0], 0u);
+        const int w = warp - 8;
+        int stage = 0;
+        uint32_t phase = 0;
+        bool ok = true;
+        for (long long i = pair; i < tiles && ok; i += pairs) {
+            const GroupTile t = group_tile(plan, a.r.N, a.ftiles, i);
+            const int half = (t.rows + kGmUnit - 1) / kGmUnit * (kGmUnit / 2);
+            int mine = 0, src[4][4];
+            {
+                const int f = w + kGmGatherWarps * ((lane >> 2) & 3);
+                if (f < half / 4)                       // behind the last row: that row again
+                    mine = source_row(a.r, t.row + min((int)rank * half + f * 4 + (lane & 3),
+                                                       t.rows - 1));
+            }
+#pragma unroll
+            for (int q = 0; q < 16; ++q) src[q / 4][q % 4] = __shfl_sync(kFull, mine, q);
+            for (int kb = 0; kb < a.kblocks; ++kb) {
+                ok = __all_sync(kFull, mbar_wait_cluster(&empty_bar[stage], phase ^ 1));
+                if (!ok) {
+                    latch_error(a.r.err, CRC_ETIMEOUT);
+                    break;
+                }
+                if (leader && w == 0 && lead)
+                    mbar_arrive_expect_tx(&full_bar[stage], 2 * half * 128);
+                uint8_t* sb = smem + stage * kGmStage + kGmA;
+                const uint32_t fb = lead_full + (uint32_t)(stage * 8);
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const int f = w + kGmGatherWarps * q;
+                    if (f < half / 4)
+                        tma_gather4_pair_by(lead, sb + f * 512, &mx, fb, kb * kElems, src[q], pol);
+                }
                 if (++stage == kGmStages) {
                     stage = 0;
                     phase ^= 1;
@@ -303,33 +324,36 @@ __global__ void __launch_bounds__(kGmThreads, 1)
     } else if (warp >= 4 && warp < 8) {
         // ---------------------------------------------------------- epilogue
         const int quarter = warp & 3;
-        uint16_t* stage_y = reinterpret_cast<uint16_t*>(staging + quarter * 32 * 64);
         const uint32_t tempty_lead = cluster_map(&tempty_bar[0], 0u);
-        constexpr int kOut = GLU ? 16 : 32;             // columns of y of a warp
-        int acc = 0;
+        constexpr int kCols = GLU ? 64 : 128;           // columns of y of this CTA
+        constexpr int kRow = kCols * 2;                 // bytes of a staged row
+        int acc = 0, buf = 0;
         uint32_t acc_phase = 0;
-        for (long long i = pair; i < tiles; i += pairs) {
+        bool ok = true;
+        for (long long i = pair; i < tiles && ok; i += pairs) {
             const GroupTile t = group_tile(plan, a.r.N, a.ftiles, i);
-            // this warp's first column of y, and this lane's (its gate's or its up's)
-            const int col0 = t.ft * (8 * kOut) + (int)rank * (4 * kOut) + quarter * kOut;
-            const int col = col0 + (GLU ? lane & 15 : lane);
-            float ws = 1.f;
-            if (W8 && col < a.out)
-                ws = a.ws[(long long)t.e * a.ws_stride +
-                          (GLU && lane >= 16 ? (long long)a.out : 0) + col];
-            float* xs = scales + quarter * 256;
+            const int col0 = t.ft * (2 * kCols) + (int)rank * kCols;
+            // this thread's rows of W: lanes t / 4 + 8 h of the quarter's two halves
+            float ws[2][2] = {};
+            float* xs = scales + acc * 256;
             if constexpr (W8) {
-                float s[8] = {};
 #pragma unroll
-                for (int i = 0; i < 8; ++i)
-                    if (i * 32 + lane < t.rows)
-                        s[i] = a.xs[source_row(a.r, t.row + i * 32 + lane)];
-                __syncwarp();
+                for (int g = 0; g < 2; ++g)
 #pragma unroll
-                for (int i = 0; i < 8; ++i) xs[i * 32 + lane] = s[i];
-                __syncwarp();
+                    for (int h = 0; h < 2; ++h) {
+                        const int col = col0 + quarter * (kCols / 4) + (GLU ? 0 : g * 16) + h * 8 +
+                                        lane / 4;
+                        if (col < a.out)
+                            ws[g][h] = a.ws[(long long)t.e * a.ws_stride +
+                                            (GLU && g ? (long long)a.out : 0) + col];
+                    }
+                // (written two tiles after its last use, with that tile's barriers between)
+                for (int r = quarter * 32 + lane; r < 256; r += 128)
+                    xs[r] = r < t.rows ? a.xs[source_row(a.r, t.row + r)] : 0.f;
             }
-            if (!__all_sync(kFull, mbar_wait_cluster(&tfull_bar[acc], acc_phase))) {
+            // one outcome for the four warps, which go on together
+            ok = group4_all(mbar_wait_cluster(&tfull_bar[acc], acc_phase), 1);
+            if (!ok) {
                 latch_error(a.r.err, CRC_ETIMEOUT);
                 break;
             }
@@ -337,47 +361,69 @@ __global__ void __launch_bounds__(kGmThreads, 1)
             const uint32_t tbase =
                 tmem_base + (uint32_t)(acc * 256) + ((uint32_t)(quarter * 32) << 16);
             for (int c0 = 0; c0 < t.rows; c0 += 32) {
-                float v[32];
-                tmem_ld32(tbase + (uint32_t)c0, v);
+                float v[2][16];
+                tmem_ld_frag(tbase + (uint32_t)c0, v[0]);
+                tmem_ld_frag(tbase + (uint32_t)c0 + (16u << 16), v[1]);
                 tmem_ld_wait();
-                pin16(v);
-                pin16(v + 16);
-#pragma unroll
-                for (int c = 0; c < 32; c += GLU ? 2 : 1) {
-                    if constexpr (W8) {
-                        v[c] *= ws * xs[c0 + c];
-                        if constexpr (GLU) v[c + 1] *= ws * xs[c0 + c + 1];
-                    }
-                    if constexpr (GLU) {
-                        // gate lanes keep row c and take its up, up lanes row c + 1 and its gate
-                        const bool up = lane >= 16;
-                        const float other = __shfl_xor_sync(kFull, up ? v[c] : v[c + 1], 16);
-                        const float y = up ? gm_silu_up(other, v[c + 1]) : gm_silu_up(v[c], other);
-                        stage_y[(c + (up ? 1 : 0)) * kOut + (lane & 15)] =
-                            __bfloat16_as_ushort(__float2bfloat16_rn(y));
-                    } else {
-                        stage_y[c * kOut + lane] = __bfloat16_as_ushort(__float2bfloat16_rn(v[c]));
+                pin16(v[0]);
+                pin16(v[1]);
+                if (c0 + 32 >= t.rows) {               // all read: the next tile but one may go on
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) {
+                        if (leader)
+                            mbar_arrive(&tempty_bar[acc]);
+                        else
+                            mbar_arrive_remote(tempty_lead + (uint32_t)(acc * 8));
                     }
                 }
-                __syncwarp();
-                constexpr int kPieces = kOut / 8;       // 16-byte pieces of a row
+                if constexpr (W8) {
 #pragma unroll
-                for (int i = lane; i < 32 * kPieces; i += 32) {
-                    const int c = c0 + i / kPieces, at = col0 + i % kPieces * 8;
-                    if (c < t.rows && at < a.out &&
+                    for (int k = 0; k < 16; ++k) {
+                        const float x = xs[c0 + k / 4 * 8 + (lane & 3) * 2 + (k & 1)];
+                        v[0][k] *= ws[0][(k >> 1) & 1] * x;
+                        v[1][k] *= ws[1][(k >> 1) & 1] * x;
+                    }
+                }
+                if constexpr (GLU) {
+#pragma unroll
+                    for (int k = 0; k < 16; ++k) v[0][k] = gm_silu_up(v[0][k], v[1][k]);
+                }
+                const uint32_t st = smem_u32(staging) + buf * (32 * 256);
+                // matrices of a store: rows 8 i .. of y and 8 columns, twice two of either
+                const int r = (lane >> 4) * 8 + (lane & 7), part = (lane >> 3) & 1;
+#pragma unroll
+                for (int g = 0; g < (GLU ? 1 : 2); ++g)
+#pragma unroll
+                    for (int p = 0; p < 2; ++p) {       // rows 16 p .. of y
+                        uint32_t m[4];
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) {
+                            const int at = 4 * (2 * p + k / 2) + 2 * (k % 2);
+                            const __nv_bfloat162 h =
+                                __floats2bfloat162_rn(v[g][at], v[g][at + 1]);
+                            m[k] = *reinterpret_cast<const uint32_t*>(&h);
+                        }
+                        const int row = p * 16 + r;
+                        const int chunk = quarter * (kCols / 32) + g * 2 + part;
+                        store_transposed(st + row * kRow + ((chunk ^ (row & 7)) << 4), m);
+                    }
+                named_sync(2, 128);
+                constexpr int kChunks = kCols / 8;
+#pragma unroll
+                for (int k = 0; k < 32 * kChunks / 128; ++k) {
+                    const int n = k * 128 + quarter * 32 + lane;
+                    const int row = n / kChunks, chunk = n % kChunks;
+                    const int c = c0 + row, col = col0 + chunk * 8;
+                    if (c < t.rows && col < a.out &&
                         CRC_IN_BOUNDS(t.row + c < a.r.E && t.e < a.r.N, a.r.err))
-                        *reinterpret_cast<uint4*>(a.y + (long long)(t.row + c) * a.out + at) =
-                            reinterpret_cast<const uint4*>(stage_y)[i];
+                        *reinterpret_cast<uint4*>(a.y + (long long)(t.row + c) * a.out + col) =
+                            *reinterpret_cast<const uint4*>(staging + buf * (32 * 256) +
+                                                            row * kRow +
+                                                            ((chunk ^ (row & 7)) << 4));
                 }
-                __syncwarp();
-            }
-            tc_fence_before();
-            __syncwarp();
-            if (lane == 0) {
-                if (leader)
-                    mbar_arrive(&tempty_bar[acc]);
-                else
-                    mbar_arrive_remote(tempty_lead + (uint32_t)(acc * 8));
+                // (the buffer is written again behind the next piece's barrier)
+                buf ^= 1;
             }
             acc ^= 1;
             if (acc == 0) acc_phase ^= 1;

@@ -103,6 +103,7 @@ __global__ void __launch_bounds__(kGwThreads, 1)
     if (warp == 0 || (warp == 2 && !a.r.rows)) {
         // ---------------------------------------------------------- rows of dy, of x
         const uint64_t pol = l2_normal_policy();
+        const uint32_t lead = elected();
         const bool is_x = warp == 2;
         int stage = 0, issued = 0;
         uint32_t phase = 0;
@@ -112,17 +113,18 @@ __global__ void __launch_bounds__(kGwThreads, 1)
             const int count = plan.count[e], row0 = plan.begin[e];
             const int col = is_x ? tile % a.ntiles * kGwN : tile / a.ntiles * kGwM;
             for (int r = 0; r < count; r += kGwRows) {
-                ok = __all_sync(kFull, lane != 0 || mbar_wait(&empty_bar[stage], phase ^ 1));
+                ok = __all_sync(kFull, mbar_wait(&empty_bar[stage], phase ^ 1));
                 if (!ok) {
                     latch_error(a.r.err, CRC_ETIMEOUT);
                     break;
                 }
                 uint8_t* s = smem + stage * kGwStage + (is_x ? kGwA : 0);
-                if (lane == 0) mbar_arrive_expect_tx(&full_bar[stage], is_x ? kGwB : kGwA);
-                __syncwarp();
-                if (lane < (is_x ? kGwN : kGwM) / 64)
-                    tma_load_2d(s + lane * kGwChunk, is_x ? &mx : &mdy, &full_bar[stage],
-                                col + lane * 64, row0 + r, pol);
+                if (lead) mbar_arrive_expect_tx(&full_bar[stage], is_x ? kGwB : kGwA);
+#pragma unroll
+                for (int c = 0; c < kGwN / 64; ++c)
+                    if (is_x || c < kGwM / 64)
+                        tma_load_2d_by(lead, s + c * kGwChunk, is_x ? &mx : &mdy,
+                                       &full_bar[stage], col + c * 64, row0 + r, pol);
                 ++issued;
                 if (++stage == kGwStages) {
                     stage = 0;
@@ -144,31 +146,41 @@ __global__ void __launch_bounds__(kGwThreads, 1)
         }
     } else if (warp >= 8 && a.r.rows) {
         // ---------------------------------------------------------- gathered rows of x
-        // lane l of warp w: the four rows 4 f .. of 64 columns, f = 2 w + (l & 1)
+        // warp w: the rows 8 w .. 8 w + 7 of a block, two fours of 64 columns at a time.  The next
+        // block's are looked up while this one waits for its stage.
+        const uint32_t lead = elected();
         const uint64_t pol = l2_normal_policy();
-        const int f = (warp - 8) * 2 + (lane & 1), c = lane >> 1;
+        const int at = (warp - 8) * 8;
         int stage = 0;
         uint32_t phase = 0;
         bool ok = true;
         for (long long w = blockIdx.x; w < all && ok; w += gridDim.x) {
             const int e = (int)(w / tiles), tile = (int)(w % tiles);
             const int count = plan.count[e], row0 = plan.begin[e];
-            const int col = tile % a.ntiles * kGwN + c * 64;
+            const int col = tile % a.ntiles * kGwN;
+            // behind the last row: that row again
+            const auto look = [&](int r) {
+                return source_row(a.r, row0 + min(r + at + (lane & 7), count - 1));
+            };
+            int next = count > 0 ? look(0) : 0;
             for (int r = 0; r < count; r += kGwRows) {
-                int src[4];
+                int src[2][4];
 #pragma unroll
-                for (int i = 0; i < 4; ++i)             // behind the last row: that row again
-                    src[i] = source_row(a.r, row0 + min(r + f * 4 + i, count - 1));
-                ok = __all_sync(kFull, lane != 0 || mbar_wait(&empty_bar[stage], phase ^ 1));
+                for (int q = 0; q < 8; ++q) src[q / 4][q % 4] = __shfl_sync(kFull, next, q);
+                if (r + kGwRows < count) next = look(r + kGwRows);
+                ok = __all_sync(kFull, mbar_wait(&empty_bar[stage], phase ^ 1));
                 if (!ok) {
                     latch_error(a.r.err, CRC_ETIMEOUT);
                     break;
                 }
-                if (warp == 8 && lane == 0) mbar_arrive_expect_tx(&full_bar[stage], kGwB);
-                if (c < kGwN / 64)
-                    tma_gather4(smem + stage * kGwStage + kGwA + c * kGwChunk + f * 512, &mx,
-                                &full_bar[stage], col, src[0], src[1], src[2], src[3], pol);
-                __syncwarp();
+                if (warp == 8 && lead) mbar_arrive_expect_tx(&full_bar[stage], kGwB);
+                uint8_t* s = smem + stage * kGwStage + kGwA + at * 128;
+#pragma unroll
+                for (int c = 0; c < kGwN / 64; ++c)
+#pragma unroll
+                    for (int q = 0; q < 2; ++q)
+                        tma_gather4_by(lead, s + c * kGwChunk + q * 512, &mx, &full_bar[stage],
+                                       col + c * 64, src[q], pol);
                 if (++stage == kGwStages) {
                     stage = 0;
                     phase ^= 1;
