@@ -3,10 +3,9 @@
 //
 // Mathematics.  For a group q of columns, part = sum over it of code * x is formed first,
 // exactly as products (4 by 8 significant bits) and in fp32 as a sum, and y += scale_q part
-// in fp32, so no weight is rounded.  A code becomes a bf16 number by two bit operations: its
-// four bits with the top one turned over, put below the exponent of 128, are 136 + code.  The
-// 136 is taken off as a product of its own, -136 x, whose tile starts the group's sum (or is
-// added to it) and serves both row tiles of the warp.
+// in fp32, so no weight is rounded.  A code becomes a bf16 number by two bit operations (its
+// four bits with the top one turned over, put below the exponent of 128, are 136 + code) and
+// the subtraction of 136, which is exact.
 //
 // What bounds it.  A decoded token reads its experts' codes once, so the bytes do: half a
 // byte a weight and 2 / G for the scale.  At 6.8 TB/s an SM has to turn over some 47 weights a
@@ -16,9 +15,11 @@
 // memory: codes would have to be widened to bf16 and written back there, 4 bytes of
 // traffic for each half byte that came in, for a product that the bytes bound anyway.)
 //
-// A CTA takes 32, 64, 128 or 256 rows (with gate and up: half of them each), its eight warps
-// 32 rows and a share of the columns each; a warp's codes and scales come by TMA into a ring
-// of its own, 256 columns a time, and the shares are summed in a fixed order at the end.
+// A persistent grid: each CTA brings the choices into their experts' order once, and its
+// warps take tiles of 32 rows (with gate and up: 16 rows of each) of the active experts in
+// turn.  A warp's codes and scales come by TMA into a ring of its own, 256 columns a time,
+// across the ends of its tiles; with too few tiles for the warps, 2, 4 or 8 warps share a
+// tile's columns and their sums are added in a fixed order.
 #include <cudaTypedefs.h>
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
@@ -34,14 +35,17 @@ PFN_cuTensorMapEncodeTiled_v12000 encode_fn();      // router.cu
 namespace {
 
 constexpr int kThreads = 256, kWarps = kThreads / 32;
+constexpr int kCtas = 2;                             // CTAs of an SM
 constexpr int kBoxCols = 256;                        // columns of a stage: 128 bytes a row
 constexpr int kCodeBytes = 32 * 128;                 // a stage's codes: two tiles of 16 rows
-constexpr int kScaleBytes = 2 * 256;                 // and scales, at most 8 groups x 16 rows x 2
+constexpr int kScaleBytes = 2 * 256;                 // and scales, at most 8 groups x 32 rows
 constexpr int kStageBytes = kCodeBytes + kScaleBytes;
-constexpr int kMaxStages = 4;
+constexpr int kStages = 2;
 constexpr int kMaxChoices = 8192;
 constexpr int kMaxTokens = 1024;
 constexpr int kMaxExperts = 256;
+constexpr int kBins = kMaxExperts + 1;               // the last: choices without a slot
+constexpr int kSums = kWarps * 8 * 33;               // floats: what the warps of a tile found
 
 inline bool aligned(const void* p, size_t a) { return reinterpret_cast<uintptr_t>(p) % a == 0; }
 
@@ -54,11 +58,10 @@ struct Matvec4Args {
     long long ldx;
     int x_div;                   // the row of x of choice c is c / x_div
     int E, N, slots;
-    int n, k, out;               // rows of a tile's matrix, columns, columns of y
+    int n, k;                    // rows (of y too) and columns of a matrix
     int glu;
-    int row_warps;               // 1, 2, 4, 8; the other factor of kWarps splits the columns
-    int stages;
-    int by_choice;               // grid.y: choices (a choice whose expert came before leaves)
+    int splits;                  // warps that share a tile's columns: 1, 2, 4, 8
+    int tiles;                   // tiles of 32 (glu: 16) rows of an expert
 };
 
 __device__ __forceinline__ void mma_bf16(float (&d)[4], const uint32_t (&a)[4], uint32_t b0,
@@ -71,11 +74,13 @@ __device__ __forceinline__ void mma_bf16(float (&d)[4], const uint32_t (&a)[4], 
           "f"(c[2]), "f"(c[3]));
 }
 
-// Codes i and i + 4 of a word (i by the shift before) as bf16 136 + code.
+// Codes i and i + 4 of a word (i by the shift before) as bf16.
 __device__ __forceinline__ uint32_t widen2(uint32_t w) {
     uint32_t r;
     asm("lop3.b32 %0, %1, 0x000f000f, 0x43084308, 0x6a;" : "=r"(r) : "r"(w));
-    return r;
+    const __nv_bfloat162 v = __hsub2(*reinterpret_cast<const __nv_bfloat162*>(&r),
+                                     __floats2bfloat162_rn(136.f, 136.f));
+    return *reinterpret_cast<const uint32_t*>(&v);
 }
 
 __device__ __forceinline__ float lds_bf16(uint32_t addr) {
@@ -89,254 +94,355 @@ __device__ __forceinline__ uint32_t lds32(uint32_t addr) {
     return v;
 }
 
-constexpr uint32_t kMinus136 = 0xC308C308u;          // two bf16 -136
+// One lane of a converged warp.
+__device__ __forceinline__ uint32_t elected() {
+    uint32_t r;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(r));
+    return r;
+}
+// Issued by the lane whose `lead` is set, in code that the whole warp runs.
+__device__ __forceinline__ void tma_load_4d_by(uint32_t lead, void* dst, const CUtensorMap* map,
+                                               uint64_t* bar, int c0, int c1, int c2, int c3,
+                                               uint64_t policy) {
+    asm volatile(
+        "{\n\t.reg .pred e;\n\tsetp.ne.b32 e, %8, 0;\n\t"
+        "@e cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes"
+        ".L2::cache_hint [%0], [%1, {%2, %3, %4, %5}], [%6], %7;\n\t}" ::"r"(smem_u32(dst)),
+        "l"(reinterpret_cast<uint64_t>(map)), "r"(c0), "r"(c1), "r"(c2), "r"(c3),
+        "r"(smem_u32(bar)), "l"(policy), "r"(lead)
+        : "memory");
+}
 
-// One warp's columns of its two row tiles for NT * 8 choices: boxes first, first + step, ...
-// acc[tile][nt][4] in the fragments' order.  False if a wait ran out.
+// The choices in their experts' order, and the tiles before each expert's: shared memory.
+struct Order {
+    int first[kBins + 1];        // of an expert's choices in the list
+    int tile[kBins];             // tiles of the experts before
+    int next[kBins];
+    int slot[kMaxExperts];
+};
+
+// A tile of an expert's rows, for all of its choices: one pass over the weights for NT * 8.
+struct Item {
+    int slot, tile, at, count;   // the matrix, its rows' tile, the choices in the list
+};
+
+__device__ __forceinline__ Item item_of(const Order& o, const Matvec4Args& a, int i) {
+    int lo = 0, hi = a.N;                            // tile[lo] <= i < tile[hi]
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) / 2;
+        if (o.tile[mid] <= i)
+            lo = mid;
+        else
+            hi = mid;
+    }
+    Item r;
+    r.slot = o.slot[lo];
+    r.tile = i - o.tile[lo];
+    r.at = o.first[lo];
+    r.count = o.first[lo + 1] - r.at;
+    return r;
+}
+
+// 256 columns of a warp's two row tiles for NT * 8 choices; acc[tile][nt][4] in the
+// fragments' order.  steps: of 32 columns.
 template <int G, int NT>
-__device__ __forceinline__ bool warp_products(const Matvec4Args& a, const CUtensorMap* mw,
-                                              const CUtensorMap* ms, uint8_t* codes,
-                                              uint8_t* scales, uint64_t* full, uint32_t& turn,
-                                              const uint16_t* const (&xrow)[NT], int slot, int row,
-                                              int first, int step, int boxes,
-                                              float (&acc)[2][NT][4]) {
+__device__ __forceinline__ void box_products(const Matvec4Args& a, uint32_t codes,
+                                             uint32_t scales, int tile_scales, int group_scales,
+                                             const uint16_t* const (&xrow)[NT], int col0,
+                                             int steps, float (&acc)[2][NT][4]) {
     const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
-    const int mine = first < boxes ? (boxes - first + step - 1) / step : 0;
-    const int row1 = a.glu ? row : row + 16, half1 = a.glu ? 1 : 0;
-    constexpr uint32_t kBytes = kCodeBytes + 2 * 32 * (kBoxCols / G);
-    const auto issue = [&](int i, uint32_t use) {
-        if (lane == 0) {
-            const int s = use % a.stages;
-            const int box = first + i * step;
-            uint8_t* c = codes + s * kCodeBytes;
-            uint8_t* q = scales + s * kScaleBytes;
-            const uint64_t pol = l2_evict_first_policy();
-            mbar_arrive_expect_tx(&full[s], kBytes);
-            tma_load_4d(c, mw, &full[s], box * 128, row, 0, slot, pol);
-            tma_load_4d(c + 2048, mw, &full[s], box * 128, row1, half1, slot, pol);
-            tma_load_4d(q, ms, &full[s], row, box * (kBoxCols / G), 0, slot, pol);
-            tma_load_4d(q + 256, ms, &full[s], row1, box * (kBoxCols / G), half1, slot, pol);
-        }
-    };
-    for (int i = 0; i < a.stages && i < mine; ++i) issue(i, turn + i);
-    const uint32_t m136[4] = {kMinus136, kMinus136, kMinus136, kMinus136};
     const float none[4] = {0.f, 0.f, 0.f, 0.f};
-    for (int i = 0; i < mine; ++i, ++turn) {
-        const int s = turn % a.stages;
-        const int col0 = (first + i * step) * kBoxCols;
-        const int steps = min(8, (a.k - col0) / 32);
-        if (!mbar_wait_warp(&full[s], (turn / a.stages) & 1)) {
-            latch_error(a.err, CRC_ETIMEOUT);
-            return false;
-        }
-        // tile rows g and g + 8: 128-byte rows, 16-byte pieces at piece ^ (row % 8)
-        const uint32_t cw = smem_u32(codes + s * kCodeBytes) + g * 128 + t * 4;
-        const uint32_t cs = smem_u32(scales + s * kScaleBytes) + g * 2;
-        float part[2][NT][4], base[NT][4];
+    // tile rows g and g + 8: 128-byte rows, 16-byte pieces at piece ^ (row % 8)
+    const uint32_t cw = codes + g * 128 + t * 4, cs = scales + g * 2;
+    float part[2][NT][4];
 #pragma unroll
-        for (int c = 0; c < 8; ++c) {
-            if (c < steps) {
-                constexpr int kPer = G / 32;             // steps of a group
-                uint32_t b[NT][4];
+    for (int c = 0; c < 8; ++c) {
+        if (c < steps) {
+            constexpr int kPer = G / 32;             // steps of a group
+            uint32_t b[NT][4];
+#pragma unroll
+            for (int j = 0; j < NT; ++j) {
+                uint4 v = make_uint4(0, 0, 0, 0);
+                if (xrow[j])
+                    v = __ldg(reinterpret_cast<const uint4*>(xrow[j] + col0 + c * 32 + t * 8));
+                // columns i and i + 4 of the eight, as the codes of a word lie
+                b[j][0] = __byte_perm(v.x, v.z, 0x5410);
+                b[j][1] = __byte_perm(v.x, v.z, 0x7632);
+                b[j][2] = __byte_perm(v.y, v.w, 0x5410);
+                b[j][3] = __byte_perm(v.y, v.w, 0x7632);
+            }
+#pragma unroll
+            for (int tile = 0; tile < 2; ++tile) {
+                const uint32_t at = cw + tile * 2048 + ((c ^ g) << 4);
+                const uint32_t w0 = lds32(at), w1 = lds32(at + 1024);
+                const uint32_t lo[4] = {widen2(w0), widen2(w1), widen2(w0 >> 4), widen2(w1 >> 4)};
+                const uint32_t hi[4] = {widen2(w0 >> 8), widen2(w1 >> 8), widen2(w0 >> 12),
+                                        widen2(w1 >> 12)};
 #pragma unroll
                 for (int j = 0; j < NT; ++j) {
-                    uint4 v = make_uint4(0, 0, 0, 0);
-                    if (xrow[j])
-                        v = __ldg(reinterpret_cast<const uint4*>(xrow[j] + col0 + c * 32 + t * 8));
-                    // columns i and i + 4 of the eight, as the codes of a word lie
-                    b[j][0] = __byte_perm(v.x, v.z, 0x5410);
-                    b[j][1] = __byte_perm(v.x, v.z, 0x7632);
-                    b[j][2] = __byte_perm(v.y, v.w, 0x5410);
-                    b[j][3] = __byte_perm(v.y, v.w, 0x7632);
+                    if (c % kPer == 0)
+                        mma_bf16(part[tile][j], lo, b[j][0], b[j][1], none);
+                    else
+                        mma_bf16(part[tile][j], lo, b[j][0], b[j][1], part[tile][j]);
+                    mma_bf16(part[tile][j], hi, b[j][2], b[j][3], part[tile][j]);
                 }
-                uint32_t lo[2][4], hi[2][4];
+            }
+            if (c % kPer == kPer - 1) {
 #pragma unroll
                 for (int tile = 0; tile < 2; ++tile) {
-                    const uint32_t at = cw + tile * 2048 + ((c ^ g) << 4);
-                    const uint32_t w0 = lds32(at), w1 = lds32(at + 1024);
-                    lo[tile][0] = widen2(w0);
-                    lo[tile][1] = widen2(w1);
-                    lo[tile][2] = widen2(w0 >> 4);
-                    lo[tile][3] = widen2(w1 >> 4);
-                    hi[tile][0] = widen2(w0 >> 8);
-                    hi[tile][1] = widen2(w1 >> 8);
-                    hi[tile][2] = widen2(w0 >> 12);
-                    hi[tile][3] = widen2(w1 >> 12);
-                }
+                    const uint32_t at = cs + tile * tile_scales + (c / kPer) * group_scales;
+                    const float s0 = lds_bf16(at), s1 = lds_bf16(at + 16);
 #pragma unroll
-                for (int j = 0; j < NT; ++j) {
-                    if (c % kPer == 0) {
-                        mma_bf16(base[j], m136, b[j][0], b[j][1], none);
-                        mma_bf16(base[j], m136, b[j][2], b[j][3], base[j]);
-                        mma_bf16(part[0][j], lo[0], b[j][0], b[j][1], base[j]);
-                        mma_bf16(part[1][j], lo[1], b[j][0], b[j][1], base[j]);
-                    } else {
-                        if (c % kPer == 1)
-                            mma_bf16(base[j], m136, b[j][0], b[j][1], none);
-                        else
-                            mma_bf16(base[j], m136, b[j][0], b[j][1], base[j]);
-                        mma_bf16(base[j], m136, b[j][2], b[j][3], base[j]);
-                        mma_bf16(part[0][j], lo[0], b[j][0], b[j][1], part[0][j]);
-                        mma_bf16(part[1][j], lo[1], b[j][0], b[j][1], part[1][j]);
-                    }
-                    mma_bf16(part[0][j], hi[0], b[j][2], b[j][3], part[0][j]);
-                    mma_bf16(part[1][j], hi[1], b[j][2], b[j][3], part[1][j]);
-                }
-                if (c % kPer == kPer - 1) {
+                    for (int j = 0; j < NT; ++j)
 #pragma unroll
-                    for (int tile = 0; tile < 2; ++tile) {
-                        const uint32_t at = cs + tile * 256 + (c / kPer) * 32;
-                        const float s0 = lds_bf16(at), s1 = lds_bf16(at + 16);
-#pragma unroll
-                        for (int j = 0; j < NT; ++j)
-#pragma unroll
-                            for (int v = 0; v < 4; ++v) {
-                                const float p =
-                                    kPer > 1 ? part[tile][j][v] + base[j][v] : part[tile][j][v];
-                                acc[tile][j][v] = fmaf(v < 2 ? s0 : s1, p, acc[tile][j][v]);
-                            }
-                    }
+                        for (int v = 0; v < 4; ++v)
+                            acc[tile][j][v] =
+                                fmaf(v < 2 ? s0 : s1, part[tile][j][v], acc[tile][j][v]);
                 }
             }
         }
-        __syncwarp();                                  // every lane has read the stage
-        if (i + a.stages < mine) issue(i + a.stages, turn + a.stages);
     }
-    return true;
 }
 
 __device__ __forceinline__ float silu_up(float gate, float up) {
     return __fdividef(gate, 1.f + __expf(-gate)) * up;
 }
 
-// The products of list[at .. at + NT * 8) choices, and their outputs.
-template <int G, int NT>
-__device__ __forceinline__ bool choices_products(const Matvec4Args& a, const CUtensorMap* mw,
-                                                 const CUtensorMap* ms, uint8_t* codes,
-                                                 uint8_t* scales, float* sums, uint64_t* full,
-                                                 uint32_t& turn, const uint16_t* list, int count,
-                                                 int slot, int tile0) {
+struct Ring {
+    uint8_t* codes;
+    uint8_t* scales;
+    uint64_t* full;
+    uint32_t turn;               // boxes consumed
+};
+
+// The choices list[0 .. count): the products of this warp's boxes of the item, then y.  Before
+// each box's stage is free, `refill` issues the next box of the warp's stream into it.
+// `ok` turns false when a wait runs out: the warp then only keeps the barriers of the warps
+// that share its tiles.
+template <int G, int NT, class F>
+__device__ __forceinline__ void item_products(const Matvec4Args& a, Ring& ring, const Item& it,
+                                              const uint16_t* list, float* sums, int& buf,
+                                              bool& ok, F refill) {
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
-    const int splits = kWarps / a.row_warps;
-    const int rw = warp / splits, split = warp % splits;
-    const int each = a.glu ? 16 : 32;                   // rows of y of a warp
+    const int split = warp % a.splits;
+    const int boxes = (a.k + kBoxCols - 1) / kBoxCols;
     const uint16_t* xrow[NT];
 #pragma unroll
     for (int j = 0; j < NT; ++j) {
         const int i = j * 8 + g;
-        xrow[j] = i < count ? a.x + (long long)(list[i] / a.x_div) * a.ldx : nullptr;
+        xrow[j] = i < it.count ? a.x + (long long)(list[i] / a.x_div) * a.ldx : nullptr;
     }
     float acc[2][NT][4] = {};
-    const int boxes = (a.k + kBoxCols - 1) / kBoxCols;
-    const bool ok = warp_products<G, NT>(a, mw, ms, codes, scales, full, turn, xrow, slot,
-                                         (tile0 + rw) * each, split, splits, boxes, acc);
-    // sums[warp][choice][32 rows]: what the warps that share the rows found
-#pragma unroll
-    for (int tile = 0; tile < 2; ++tile)
+    // a stage's scales: [groups][32], with gate and up [2][groups][16]
+    const int tile_scales = a.glu ? kBoxCols / G * 32 : 32, group_scales = a.glu ? 32 : 64;
+    for (int box = split; box < boxes && ok; box += a.splits) {
+        const int s = ring.turn % kStages;
+        ok = mbar_wait_warp(&ring.full[s], (ring.turn / kStages) & 1);
+        if (!ok) {
+            latch_error(a.err, CRC_ETIMEOUT);
+            break;
+        }
+        box_products<G, NT>(a, smem_u32(ring.codes + s * kCodeBytes),
+                            smem_u32(ring.scales + s * kScaleBytes), tile_scales, group_scales,
+                            xrow, box * kBoxCols, min(8, (a.k - box * kBoxCols) / 32), acc);
+        ++ring.turn;
+        __syncwarp();                                  // every lane has read the stage
+        refill(s);
+    }
+    const int each = a.glu ? 16 : 32, row0 = it.tile * each;
+    if (a.splits == 1) {
 #pragma unroll
         for (int j = 0; j < NT; ++j)
 #pragma unroll
             for (int v = 0; v < 4; ++v) {
-                const int i = j * 8 + 2 * t + (v & 1), r = tile * 16 + g + (v >> 1) * 8;
-                sums[(warp * NT * 8 + i) * 33 + r] = acc[tile][j][v];
+                const int i = j * 8 + 2 * t + (v & 1), r = row0 + g + (v >> 1) * 8;
+                if (i >= it.count || !ok) continue;
+                uint16_t* y = a.y + (long long)list[i] * a.n;
+                if (a.glu) {
+                    if (r < a.n)
+                        y[r] = __bfloat16_as_ushort(
+                            __float2bfloat16_rn(silu_up(acc[0][j][v], acc[1][j][v])));
+                } else {
+                    if (r < a.n) y[r] = __bfloat16_as_ushort(__float2bfloat16_rn(acc[0][j][v]));
+                    if (r + 16 < a.n)
+                        y[r + 16] = __bfloat16_as_ushort(__float2bfloat16_rn(acc[1][j][v]));
+                }
             }
-    __syncthreads();
-    const int rows = a.row_warps * each;                // rows of y of this CTA
-    for (int o = threadIdx.x; o < rows * count; o += kThreads) {
-        const int i = o / rows, r = o % rows;
-        const int col = tile0 * each + r;
-        if (col >= a.out) continue;
-        const int w0 = r / each * splits, rr = r % each;
-        float v = 0.f, u = 0.f;
-        for (int w = w0; w < w0 + splits; ++w) {
-            v += sums[(w * NT * 8 + i) * 33 + rr];
-            if (a.glu) u += sums[(w * NT * 8 + i) * 33 + rr + 16];
-        }
-        if (a.glu) v = silu_up(v, u);
-        a.y[(long long)list[i] * a.out + col] = __bfloat16_as_ushort(__float2bfloat16_rn(v));
+        return;
     }
-    __syncthreads();
-    return ok;
+    if constexpr (NT == 1) {
+        // sums[buf][warp][choice][32 rows]; a buffer is written again behind the next barrier
+        float* mine = sums + buf * kSums;
+        buf ^= 1;
+#pragma unroll
+        for (int tile = 0; tile < 2; ++tile)
+#pragma unroll
+            for (int v = 0; v < 4; ++v)
+                mine[(warp * 8 + 2 * t + (v & 1)) * 33 + tile * 16 + g + (v >> 1) * 8] =
+                    acc[tile][0][v];
+        const int w0 = warp - split;
+        named_sync(1 + w0 / a.splits, a.splits * 32);
+        for (int o = split * 32 + lane; o < each * it.count; o += a.splits * 32) {
+            const int i = o / each, r = o % each;
+            if (row0 + r >= a.n) continue;
+            float v = 0.f, u = 0.f;
+            for (int w = w0; w < w0 + a.splits; ++w) {
+                v += mine[(w * 8 + i) * 33 + r];
+                if (a.glu) u += mine[(w * 8 + i) * 33 + r + 16];
+            }
+            if (a.glu) v = silu_up(v, u);
+            a.y[(long long)list[i] * a.n + row0 + r] =
+                __bfloat16_as_ushort(__float2bfloat16_rn(v));
+        }
+    }
 }
 
 // NT: choices of a pass over the weights, in eights.
 template <int G, int NT>
-__global__ void __launch_bounds__(kThreads) matvec4_kernel(const __grid_constant__ CUtensorMap mw,
-                                                           const __grid_constant__ CUtensorMap ms,
-                                                           Matvec4Args a) {
+__global__ void __launch_bounds__(kThreads, kCtas)
+    matvec4_kernel(const __grid_constant__ CUtensorMap mw, const __grid_constant__ CUtensorMap ms,
+                   Matvec4Args a) {
     extern __shared__ __align__(1024) uint8_t smem_raw[];
-    __shared__ uint64_t full[kWarps][kMaxStages];
-    __shared__ int found;
+    __shared__ uint64_t full[kWarps][kStages];
+    __shared__ Order order;
     uint8_t* smem = reinterpret_cast<uint8_t*>(
         (reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
-    const int warp = threadIdx.x >> 5;
-    uint8_t* codes = smem + warp * a.stages * kCodeBytes;
-    uint8_t* scales = smem + kWarps * a.stages * kCodeBytes + warp * a.stages * kScaleBytes;
-    float* sums = reinterpret_cast<float*>(smem + kWarps * a.stages * kStageBytes);
-    uint16_t* list = reinterpret_cast<uint16_t*>(sums + kWarps * NT * 8 * 33);
-    if (threadIdx.x < kWarps * kMaxStages) mbar_init(&full[0][0] + threadIdx.x, 1);
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    Ring ring;
+    ring.codes = smem + warp * kStages * kCodeBytes;
+    ring.scales = smem + kWarps * kStages * kCodeBytes + warp * kStages * kScaleBytes;
+    ring.full = full[warp];
+    ring.turn = 0;
+    float* sums = reinterpret_cast<float*>(smem + kWarps * kStages * kStageBytes);
+    uint16_t* list = reinterpret_cast<uint16_t*>(sums + (a.splits > 1 ? 2 * kSums : 0));
+    if (threadIdx.x < kWarps * kStages) mbar_init(&full[0][0] + threadIdx.x, 1);
+    for (int e = threadIdx.x; e <= a.N; e += kThreads) order.next[e] = 0;
     if (threadIdx.x == 0) {
-        found = 0;
         fence_mbar_init();
         tma_prefetch_desc(&mw);
         tma_prefetch_desc(&ms);
     }
-    __syncthreads();
     pdl_begin();
-    // the choices of this CTA's expert.  A choice without one (grid.y's last by expert, or
-    // its own by choice) has zeros for its product.
-    int e = blockIdx.y;
-    if (a.by_choice) {
-        e = a.topk[blockIdx.y];
-        bool again = false;
-        for (int c = threadIdx.x; c < (int)blockIdx.y; c += kThreads) again |= a.topk[c] == e;
-        if (__syncthreads_or(again)) return;            // an earlier choice of it has a CTA
+    for (int e = threadIdx.x; e < a.N; e += kThreads) {
+        const int slot = a.slot ? a.slot[e] : e;
+        order.slot[e] = slot >= 0 && slot < a.slots ? slot : -1;
     }
-    if (!a.topk) {
-        for (int c = threadIdx.x; c < a.E; c += kThreads) list[c] = (uint16_t)c;
-        if (threadIdx.x == 0) found = a.E;
-    } else {
-        // in any order: a choice's result does not depend on its column of the fragments
-        for (int c = threadIdx.x; c < a.E; c += kThreads) {
-            const int id = a.topk[c];
-            if (id == e || (id >= a.N && e >= a.N)) list[atomicAdd(&found, 1)] = (uint16_t)c;
+    __syncthreads();
+    const auto bin_of = [&](int c) {
+        const int id = a.topk ? a.topk[c] : 0;
+        return id < a.N && order.slot[id] >= 0 ? id : a.N;
+    };
+    for (int c = threadIdx.x; c < a.E; c += kThreads) atomicAdd(&order.next[bin_of(c)], 1);
+    __syncthreads();
+    if (warp == 0) {
+        constexpr int kEach = (kBins + 31) / 32;
+        int n = 0, tiles = 0;                          // this lane's bins
+        const auto tiles_of = [&](int count) { return count ? a.tiles : 0; };
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) {
+            const int e = lane * kEach + i;
+            if (e > a.N) continue;
+            n += order.next[e];
+            if (e < a.N) tiles += tiles_of(order.next[e]);
+        }
+        int n0 = n, t0 = tiles;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int un = __shfl_up_sync(kFull, n0, o), ut = __shfl_up_sync(kFull, t0, o);
+            if (lane >= o) {
+                n0 += un;
+                t0 += ut;
+            }
+        }
+        n0 -= n;
+        t0 -= tiles;
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) {
+            const int e = lane * kEach + i;
+            if (e > a.N) continue;
+            const int count = order.next[e];
+            order.first[e] = n0;
+            order.next[e] = n0;
+            order.tile[e] = t0;
+            n0 += count;
+            if (e < a.N) t0 += tiles_of(count);
+            if (e == a.N) order.first[e + 1] = n0;
         }
     }
     __syncthreads();
-    const int count = found;
-    if (count == 0) return;
-    int slot = -1;
-    if (e < a.N) slot = a.slot ? a.slot[e] : e;
+    // in any order, another one in each CTA: a choice's result does not depend on its column of
+    // the fragments, nor on its pass, and one warp makes all passes of a tile
+    for (int c = threadIdx.x; c < a.E; c += kThreads)
+        list[atomicAdd(&order.next[bin_of(c)], 1)] = (uint16_t)c;
+    __syncthreads();
+
+    // the choices without a slot: zeros
+    const int none = order.first[a.N], nones = order.first[a.N + 1] - none, pieces = a.n / 8;
+    for (long long o = (long long)blockIdx.x * kThreads + threadIdx.x;
+         o < (long long)nones * pieces; o += (long long)gridDim.x * kThreads)
+        *(reinterpret_cast<uint4*>(a.y + (long long)list[none + o / pieces] * a.n) +
+          o % pieces) = make_uint4(0, 0, 0, 0);
+
+    const int items = order.tile[a.N];
+    const int groups = kWarps / a.splits;              // groups of warps of a CTA
+    const int first = blockIdx.x * groups + warp / a.splits, step = gridDim.x * groups;
+    const int boxes = (a.k + kBoxCols - 1) / kBoxCols, split = warp % a.splits;
     const int each = a.glu ? 16 : 32;
-    const int tile0 = blockIdx.x * a.row_warps;
-    if (slot < 0 || slot >= a.slots) {
-        const int rows = a.row_warps * each;
-        for (int o = threadIdx.x; o < rows * count; o += kThreads) {
-            const int col = tile0 * each + o % rows;
-            if (col < a.out) a.y[(long long)list[o / rows] * a.out + col] = 0;
+    // the warp's stream of boxes, issued kStages before they are taken
+    const uint32_t lead = elected();
+    const uint64_t pol = l2_evict_first_policy();
+    Item next = {};
+    int ni = first - step, nbox = boxes, npass = 0;
+    uint32_t issued = 0;
+    const auto refill = [&](int s) {
+        if (nbox >= boxes) {
+            if (npass * (NT * 8) >= next.count) {
+                if (ni + step >= items) return;
+                ni += step;
+                npass = 0;
+                next = item_of(order, a, ni);
+            }
+            ++npass;
+            nbox = split;
         }
-        return;
+        if (lead)
+            mbar_arrive_expect_tx(&ring.full[s], kCodeBytes + 2 * 32 * (kBoxCols / G));
+        tma_load_4d_by(lead, ring.codes + s * kCodeBytes, &mw, &ring.full[s], nbox * 128,
+                       next.tile * each, 0, next.slot, pol);
+        tma_load_4d_by(lead, ring.scales + s * kScaleBytes, &ms, &ring.full[s], next.tile * each,
+                       nbox * (kBoxCols / G), 0, next.slot, pol);
+        nbox += a.splits;
+        ++issued;
+    };
+#pragma unroll
+    for (int s = 0; s < kStages; ++s) refill(s);
+    int buf = 0;
+    bool ok = true;
+    for (int i = first; i < items; i += step) {
+        const Item all = item_of(order, a, i);
+        for (int at = 0; at < all.count; at += NT * 8) {
+            Item it = all;
+            it.at += at;
+            it.count = min(NT * 8, all.count - at);
+            const uint16_t* some = list + it.at;
+            if (NT == 1 || it.count <= 8)
+                item_products<G, 1>(a, ring, it, some, sums, buf, ok, refill);
+            else if (NT == 2 || it.count <= 16)
+                item_products<G, (NT < 2 ? 1 : 2)>(a, ring, it, some, sums, buf, ok, refill);
+            else
+                item_products<G, NT>(a, ring, it, some, sums, buf, ok, refill);
+        }
     }
-    uint32_t turn = 0;
-    for (int at = 0; at < count; at += NT * 8) {
-        const int some = min(count - at, NT * 8);
-        bool ok;
-        if (NT == 1 || some <= 8)
-            ok = choices_products<G, 1>(a, &mw, &ms, codes, scales, sums, full[warp], turn,
-                                        list + at, some, slot, tile0);
-        else if (NT == 2 || some <= 16)
-            ok = choices_products<G, (NT < 2 ? 1 : 2)>(a, &mw, &ms, codes, scales, sums,
-                                                       full[warp], turn, list + at, some, slot,
-                                                       tile0);
-        else
-            ok = choices_products<G, NT>(a, &mw, &ms, codes, scales, sums, full[warp], turn,
-                                         list + at, some, slot, tile0);
-        if (!__syncthreads_and(ok)) return;
-    }
+    // never leave with copies in flight
+    if (!ok)
+        for (uint32_t n = ring.turn; n < issued; ++n)
+            mbar_wait_warp(&ring.full[n % kStages], (n / kStages) & 1);
 }
 
-size_t smem_bytes(int stages, int nt, int E) {
-    return 1024 + (size_t)kWarps * stages * kStageBytes + (size_t)kWarps * nt * 8 * 33 * 4 +
+size_t smem_bytes(int splits, int E) {
+    return 1024 + (size_t)kWarps * kStages * kStageBytes + (splits > 1 ? 2 * kSums * 4 : 0) +
            (size_t)E * 2 + 16;
 }
 
@@ -344,7 +450,7 @@ template <int G, int NT>
 int launch(const CUtensorMap& mw, const CUtensorMap& ms, const Matvec4Args& a, dim3 grid,
            cudaStream_t st) {
     auto kern = matvec4_kernel<G, NT>;
-    const size_t most = smem_bytes(kMaxStages, NT, kMaxChoices);
+    const size_t most = smem_bytes(8, kMaxChoices);
     static PerDevice ready;
     const int up = ready.get(current_device(), [&] {
         return cuda_status(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize,
@@ -354,7 +460,7 @@ int launch(const CUtensorMap& mw, const CUtensorMap& ms, const Matvec4Args& a, d
     cudaError_t e;
     {
         ProfScope prof(CRC_KERNEL_MATVEC4, st);
-        e = launch_dependent(kern, grid, kThreads, smem_bytes(a.stages, NT, a.E), st, 1, mw, ms,
+        e = launch_dependent(kern, grid, kThreads, smem_bytes(a.splits, a.E), st, 1, mw, ms,
                              a);
     }
     note_launch();
@@ -382,8 +488,8 @@ int check_matvec4(const crc_matvec4_weights* w) {
     return CRC_OK;
 }
 
-// Codes as (k / 2, n, gate / up, slots), a box of 128 bytes x 16 rows; scales as
-// (n, k / G, gate / up, slots), 16 rows x the groups of 256 columns.
+// Codes as (k / 2, n, gate / up, slots), a box of 128 bytes x 32 rows, with gate and up 16 of
+// each; scales as (n, k / G, gate / up, slots), the same rows x the groups of 256 columns.
 bool make_maps(CUtensorMap* mw, CUtensorMap* ms, const crc_matvec4_weights& w) {
     auto enc = encode_fn();
     if (!enc) return false;
@@ -392,10 +498,11 @@ bool make_maps(CUtensorMap* mw, CUtensorMap* ms, const crc_matvec4_weights& w) {
     const cuuint32_t ones[4] = {1, 1, 1, 1};
     const cuuint64_t dw[4] = {k2, n, parts, slots};
     const cuuint64_t sw[3] = {k2, n * k2, (cuuint64_t)w.codes_stride};
-    const cuuint32_t bw[4] = {128, 16, 1, 1};
+    const cuuint32_t rows = w.glu ? 16 : 32, halves = w.glu ? 2 : 1;
+    const cuuint32_t bw[4] = {128, rows, halves, 1};
     const cuuint64_t ds[4] = {n, groups, parts, slots};
     const cuuint64_t ss[3] = {n * 2, n * groups * 2, (cuuint64_t)w.scale_stride};
-    const cuuint32_t bs[4] = {16, (cuuint32_t)(kBoxCols / w.group), 1, 1};
+    const cuuint32_t bs[4] = {rows, (cuuint32_t)(kBoxCols / w.group), halves, 1};
     return enc(mw, CU_TENSOR_MAP_DATA_TYPE_UINT8, 4, const_cast<uint8_t*>(w.codes_dev), dw, sw, bw,
                ones, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
                CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
@@ -437,30 +544,25 @@ extern "C" int crc_matvec4(const crc_matvec4_weights* w, const uint16_t* x_dev, 
     a.slots = w->slots;
     a.n = w->n;
     a.k = w->k;
-    a.out = w->n;
     a.glu = w->glu;
-    // a grid row for every expert and one for choices without any, or for every choice
-    a.by_choice = topk_dev && a.E <= a.N;
-    const int groups = !topk_dev ? 1 : a.by_choice ? a.E : a.N + 1;
     const int each = a.glu ? 16 : 32;
-    const int tiles = (a.n + each - 1) / each;
+    a.tiles = (a.n + each - 1) / each;
+    // Warps share a tile's columns while there are more of them than tiles (experts taken by
+    // some choice are at most E and N)
     const int boxes = (a.k + kBoxCols - 1) / kBoxCols;
-    const int active = !topk_dev ? 1 : a.E < a.N ? a.E : a.N;
-    // More rows a CTA when there are enough CTAs without (and no warp without columns)
-    a.row_warps = 1;
-    while (a.row_warps < kWarps &&
-           (kWarps / a.row_warps > boxes ||
-            (long long)active * ((tiles + 2 * a.row_warps - 1) / (2 * a.row_warps)) >=
-                4ll * sm_count()))
-        a.row_warps *= 2;
-    const int splits = kWarps / a.row_warps;
-    const int each_warp = (boxes + splits - 1) / splits;
-    a.stages = each_warp < kMaxStages ? each_warp : kMaxStages;
-    const dim3 grid((unsigned)((tiles + a.row_warps - 1) / a.row_warps), (unsigned)groups);
-    cudaStream_t st = static_cast<cudaStream_t>(stream);
-    // Choices of one expert: no more than M (or all of them without a Top-K)
+    const long long items = (long long)(a.E < a.N ? a.E : a.N) * a.tiles;
+    const long long warps = (long long)sm_count() * kCtas * kWarps;
     const bool few = M <= 8;
-#define CRC_G(G) (few ? launch<G, 1>(mw, ms, a, grid, st) : launch<G, 4>(mw, ms, a, grid, st))
+    a.splits = 1;
+    while (few && a.splits < kWarps && 2 * a.splits <= boxes && items * 2 * a.splits <= warps)
+        a.splits *= 2;
+    // (a pass over the weights takes 8 choices, 24 with more rows: choices of one expert are
+    // no more than M unless an id comes twice)
+    const long long ctas = (items * a.splits + kWarps - 1) / kWarps;
+    const long long room = (long long)sm_count() * kCtas;
+    const dim3 grid((unsigned)(ctas < room ? ctas : room));
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+#define CRC_G(G) (few ? launch<G, 1>(mw, ms, a, grid, st) : launch<G, 3>(mw, ms, a, grid, st))
     return w->group == 32 ? CRC_G(32) : w->group == 64 ? CRC_G(64) : CRC_G(128);
 #undef CRC_G
 }
