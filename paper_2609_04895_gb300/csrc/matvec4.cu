@@ -66,8 +66,7 @@ struct Matvec4Args {
 
 __device__ __forceinline__ void mma_bf16(float (&d)[4], const uint32_t (&a)[4], uint32_t b0,
                                          uint32_t b1, const float (&c)[4]) {
-    asm volatile(
-        "mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, "
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, "
         "{%8,%9}, {%10,%11,%12,%13};"
         : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
         : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(c[0]), "f"(c[1]),
@@ -145,62 +144,87 @@ __device__ __forceinline__ Item item_of(const Order& o, const Matvec4Args& a, in
     return r;
 }
 
-// 256 columns of a warp's two row tiles for NT * 8 choices; acc[tile][nt][4] in the
-// fragments' order.  steps: of 32 columns.
+// The x of a half box (128 columns) for NT * 8 choices, as the fragments want it: lane (g, t)
+// has columns 8 t .. of each 32 of choice g.  Zeros behind the last column.
+template <int NT>
+struct Half {
+    uint4 v[NT][4];
+    __device__ __forceinline__ void load(const Matvec4Args& a, const uint16_t* const (&xrow)[NT],
+                                         int col0) {
+        const int t = threadIdx.x & 3;
+#pragma unroll
+        for (int j = 0; j < NT; ++j)
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+                v[j][c] = make_uint4(0, 0, 0, 0);
+                if (xrow[j] && col0 + c * 32 < a.k)
+                    v[j][c] =
+                        __ldg(reinterpret_cast<const uint4*>(xrow[j] + col0 + c * 32 + t * 8));
+            }
+    }
+};
+
+// 128 columns of a warp's two row tiles for NT * 8 choices; acc[tile][nt][4] in the
+// fragments' order.  (Columns behind the last are zeros in x, codes and scales.)
 template <int G, int NT>
-__device__ __forceinline__ void box_products(const Matvec4Args& a, uint32_t codes,
-                                             uint32_t scales, int tile_scales, int group_scales,
-                                             const uint16_t* const (&xrow)[NT], int col0,
-                                             int steps, float (&acc)[2][NT][4]) {
+__device__ __forceinline__ void half_products(uint32_t codes, uint32_t scales, int tile_scales,
+                                              int group_scales, int half, const Half<NT>& x,
+                                              float (&acc)[2][NT][4]) {
     const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
     const float none[4] = {0.f, 0.f, 0.f, 0.f};
+    constexpr int kPer = G / 32, kGroups = 4 / kPer;   // steps of a group, groups of a half
     // tile rows g and g + 8: 128-byte rows, 16-byte pieces at piece ^ (row % 8)
-    const uint32_t cw = codes + g * 128 + t * 4, cs = scales + g * 2;
+    const uint32_t cw = codes + g * 128 + t * 4;
+    const uint32_t cs = scales + g * 2 + half * kGroups * group_scales;
+    uint32_t w[4][2][2];
+    float sc[kGroups][2][2];
+#pragma unroll
+    for (int c = 0; c < 4; ++c)
+#pragma unroll
+        for (int tile = 0; tile < 2; ++tile) {
+            const uint32_t at = cw + tile * 2048 + (((half * 4 + c) ^ g) << 4);
+            w[c][tile][0] = lds32(at);
+            w[c][tile][1] = lds32(at + 1024);
+        }
+#pragma unroll
+    for (int q = 0; q < kGroups; ++q)
+#pragma unroll
+        for (int tile = 0; tile < 2; ++tile) {
+            const uint32_t at = cs + tile * tile_scales + q * group_scales;
+            sc[q][tile][0] = lds_bf16(at);
+            sc[q][tile][1] = lds_bf16(at + 16);
+        }
     float part[2][NT][4];
 #pragma unroll
-    for (int c = 0; c < 8; ++c) {
-        if (c < steps) {
-            constexpr int kPer = G / 32;             // steps of a group
-            uint32_t b[NT][4];
+    for (int c = 0; c < 4; ++c) {
+        uint32_t b[NT][4];
+#pragma unroll
+        for (int j = 0; j < NT; ++j) {
+            // columns i and i + 4 of the eight, as the codes of a word lie
+            const uint4 v = x.v[j][c];
+            b[j][0] = __byte_perm(v.x, v.z, 0x5410);
+            b[j][1] = __byte_perm(v.x, v.z, 0x7632);
+            b[j][2] = __byte_perm(v.y, v.w, 0x5410);
+            b[j][3] = __byte_perm(v.y, v.w, 0x7632);
+        }
+#pragma unroll
+        for (int tile = 0; tile < 2; ++tile) {
+            const uint32_t w0 = w[c][tile][0], w1 = w[c][tile][1];
+            const uint32_t lo[4] = {widen2(w0), widen2(w1), widen2(w0 >> 4), widen2(w1 >> 4)};
+            const uint32_t hi[4] = {widen2(w0 >> 8), widen2(w1 >> 8), widen2(w0 >> 12),
+                                    widen2(w1 >> 12)};
 #pragma unroll
             for (int j = 0; j < NT; ++j) {
-                uint4 v = make_uint4(0, 0, 0, 0);
-                if (xrow[j])
-                    v = __ldg(reinterpret_cast<const uint4*>(xrow[j] + col0 + c * 32 + t * 8));
-                // columns i and i + 4 of the eight, as the codes of a word lie
-                b[j][0] = __byte_perm(v.x, v.z, 0x5410);
-                b[j][1] = __byte_perm(v.x, v.z, 0x7632);
-                b[j][2] = __byte_perm(v.y, v.w, 0x5410);
-                b[j][3] = __byte_perm(v.y, v.w, 0x7632);
-            }
+                if (c % kPer == 0)
+                    mma_bf16(part[tile][j], lo, b[j][0], b[j][1], none);
+                else
+                    mma_bf16(part[tile][j], lo, b[j][0], b[j][1], part[tile][j]);
+                mma_bf16(part[tile][j], hi, b[j][2], b[j][3], part[tile][j]);
+                if (c % kPer == kPer - 1)
 #pragma unroll
-            for (int tile = 0; tile < 2; ++tile) {
-                const uint32_t at = cw + tile * 2048 + ((c ^ g) << 4);
-                const uint32_t w0 = lds32(at), w1 = lds32(at + 1024);
-                const uint32_t lo[4] = {widen2(w0), widen2(w1), widen2(w0 >> 4), widen2(w1 >> 4)};
-                const uint32_t hi[4] = {widen2(w0 >> 8), widen2(w1 >> 8), widen2(w0 >> 12),
-                                        widen2(w1 >> 12)};
-#pragma unroll
-                for (int j = 0; j < NT; ++j) {
-                    if (c % kPer == 0)
-                        mma_bf16(part[tile][j], lo, b[j][0], b[j][1], none);
-                    else
-                        mma_bf16(part[tile][j], lo, b[j][0], b[j][1], part[tile][j]);
-                    mma_bf16(part[tile][j], hi, b[j][2], b[j][3], part[tile][j]);
-                }
-            }
-            if (c % kPer == kPer - 1) {
-#pragma unroll
-                for (int tile = 0; tile < 2; ++tile) {
-                    const uint32_t at = cs + tile * tile_scales + (c / kPer) * group_scales;
-                    const float s0 = lds_bf16(at), s1 = lds_bf16(at + 16);
-#pragma unroll
-                    for (int j = 0; j < NT; ++j)
-#pragma unroll
-                        for (int v = 0; v < 4; ++v)
-                            acc[tile][j][v] =
-                                fmaf(v < 2 ? s0 : s1, part[tile][j][v], acc[tile][j][v]);
-                }
+                    for (int v = 0; v < 4; ++v)
+                        acc[tile][j][v] = fmaf(sc[c / kPer][tile][v / 2], part[tile][j][v],
+                                               acc[tile][j][v]);
             }
         }
     }
@@ -237,16 +261,24 @@ __device__ __forceinline__ void item_products(const Matvec4Args& a, Ring& ring, 
     float acc[2][NT][4] = {};
     // a stage's scales: [groups][32], with gate and up [2][groups][16]
     const int tile_scales = a.glu ? kBoxCols / G * 32 : 32, group_scales = a.glu ? 32 : 64;
+    Half<NT> x;
+    x.load(a, xrow, split * kBoxCols);                 // on its way while the codes are
     for (int box = split; box < boxes && ok; box += a.splits) {
-        const int s = ring.turn % kStages;
+        const int s = ring.turn % kStages, col0 = box * kBoxCols;
         ok = mbar_wait_warp(&ring.full[s], (ring.turn / kStages) & 1);
         if (!ok) {
             latch_error(a.err, CRC_ETIMEOUT);
             break;
         }
-        box_products<G, NT>(a, smem_u32(ring.codes + s * kCodeBytes),
-                            smem_u32(ring.scales + s * kScaleBytes), tile_scales, group_scales,
-                            xrow, box * kBoxCols, min(8, (a.k - box * kBoxCols) / 32), acc);
+        const uint32_t codes = smem_u32(ring.codes + s * kCodeBytes);
+        const uint32_t scales = smem_u32(ring.scales + s * kScaleBytes);
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+            Half<NT> ahead;
+            ahead.load(a, xrow, half ? (box + a.splits) * kBoxCols : col0 + 128);
+            half_products<G, NT>(codes, scales, tile_scales, group_scales, half, x, acc);
+            x = ahead;
+        }
         ++ring.turn;
         __syncwarp();                                  // every lane has read the stage
         refill(s);
@@ -429,8 +461,6 @@ __global__ void __launch_bounds__(kThreads, kCtas)
             const uint16_t* some = list + it.at;
             if (NT == 1 || it.count <= 8)
                 item_products<G, 1>(a, ring, it, some, sums, buf, ok, refill);
-            else if (NT == 2 || it.count <= 16)
-                item_products<G, (NT < 2 ? 1 : 2)>(a, ring, it, some, sums, buf, ok, refill);
             else
                 item_products<G, NT>(a, ring, it, some, sums, buf, ok, refill);
         }
@@ -556,13 +586,13 @@ extern "C" int crc_matvec4(const crc_matvec4_weights* w, const uint16_t* x_dev, 
     a.splits = 1;
     while (few && a.splits < kWarps && 2 * a.splits <= boxes && items * 2 * a.splits <= warps)
         a.splits *= 2;
-    // (a pass over the weights takes 8 choices, 24 with more rows: choices of one expert are
+    // (a pass over the weights takes 8 choices, 16 with more rows: choices of one expert are
     // no more than M unless an id comes twice)
     const long long ctas = (items * a.splits + kWarps - 1) / kWarps;
     const long long room = (long long)sm_count() * kCtas;
     const dim3 grid((unsigned)(ctas < room ? ctas : room));
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-#define CRC_G(G) (few ? launch<G, 1>(mw, ms, a, grid, st) : launch<G, 3>(mw, ms, a, grid, st))
+#define CRC_G(G) (few ? launch<G, 1>(mw, ms, a, grid, st) : launch<G, 2>(mw, ms, a, grid, st))
     return w->group == 32 ? CRC_G(32) : w->group == 64 ? CRC_G(64) : CRC_G(128);
 #undef CRC_G
 }
