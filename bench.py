@@ -239,11 +239,17 @@ KERNEL_SOURCES = {
     "loss": ["loss.cu", "cache_scan.cuh", "crc_device.cuh"],
     "moe": ["moe.cu", "moe_experts.cuh", "moe_route.cuh", "pdl.cuh", "crc_device.cuh"],
     "norm": ["norm.cu", "row_team.cuh", "pdl.cuh", "crc_device.cuh"],
+    "group": ["group.cu", "group.cuh", "group_matmul.cuh", "group_weights.cuh", "pdl.cuh",
+              "crc_device.cuh"],
+    "choices": ["choices.cu", "pdl.cuh", "crc_device.cuh"],
+    "rows4": ["rows4.cu", "pdl.cuh", "crc_device.cuh"],
+    "matvec4": ["matvec4.cu", "pdl.cuh", "crc_device.cuh"],
 }
 
 
 def kernel_family(kernel: str) -> str:
-    for fam in ("moe", "norm", "policy", "fused", "short", "router", "loss"):
+    for fam in ("moe", "norm", "policy", "fused", "short", "router", "loss", "group", "choices",
+                "rows4", "matvec4"):
         if fam in kernel:
             return fam
     return "scan"

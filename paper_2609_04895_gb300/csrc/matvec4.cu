@@ -73,7 +73,9 @@ __device__ __forceinline__ void mma_bf16(float (&d)[4], const uint32_t (&a)[4], 
           "f"(c[2]), "f"(c[3]));
 }
 
-// Codes i and i + 4 of a word (i by the shift before) as bf16.
+// Codes i and i + 4 of a word (i by the shift before) as bf16.  (Taken as steps of 2^-133 in the
+// low bits of a bf16 and scaled up by an fma, two codes need no shift, but that took 5 to 9%
+// longer.)
 __device__ __forceinline__ uint32_t widen2(uint32_t w) {
     uint32_t r;
     asm("lop3.b32 %0, %1, 0x000f000f, 0x43084308, 0x6a;" : "=r"(r) : "r"(w));
@@ -114,35 +116,20 @@ __device__ __forceinline__ void tma_load_4d_by(uint32_t lead, void* dst, const C
         : "memory");
 }
 
-// The choices in their experts' order, and the tiles before each expert's: shared memory.
+// The choices in their experts' order: shared memory.
 struct Order {
     int first[kBins + 1];        // of an expert's choices in the list
-    int tile[kBins];             // tiles of the experts before
     int next[kBins];
     int slot[kMaxExperts];
+    uint16_t active[kMaxExperts];   // experts with choices and a slot
+    int actives;
 };
 
-// A tile of an expert's rows, for all of its choices: one pass over the weights for NT * 8.
-struct Item {
-    int slot, tile, at, count;   // the matrix, its rows' tile, the choices in the list
+// A tile of an expert's rows for up to NT * 8 of its choices: one pass over the weights.
+struct Pass {
+    int item;                    // of the warp's turns; its expert's tile has a pass or more
+    int slot, tile, at, end;     // the matrix, its rows' tile, the choices in the list
 };
-
-__device__ __forceinline__ Item item_of(const Order& o, const Matvec4Args& a, int i) {
-    int lo = 0, hi = a.N;                            // tile[lo] <= i < tile[hi]
-    while (hi - lo > 1) {
-        const int mid = (lo + hi) / 2;
-        if (o.tile[mid] <= i)
-            lo = mid;
-        else
-            hi = mid;
-    }
-    Item r;
-    r.slot = o.slot[lo];
-    r.tile = i - o.tile[lo];
-    r.at = o.first[lo];
-    r.count = o.first[lo + 1] - r.at;
-    return r;
-}
 
 // The x of a half box (128 columns) for NT * 8 choices, as the fragments want it: lane (g, t)
 // has columns 8 t .. of each 32 of choice g.  Zeros behind the last column.
@@ -151,16 +138,22 @@ struct Half {
     uint4 v[NT][4];
     __device__ __forceinline__ void load(const Matvec4Args& a, const uint16_t* const (&xrow)[NT],
                                          int col0) {
-        const int t = threadIdx.x & 3;
+        if (col0 + 128 <= a.k) {
 #pragma unroll
-        for (int j = 0; j < NT; ++j)
+            for (int j = 0; j < NT; ++j)
 #pragma unroll
-            for (int c = 0; c < 4; ++c) {
-                v[j][c] = make_uint4(0, 0, 0, 0);
-                if (xrow[j] && col0 + c * 32 < a.k)
-                    v[j][c] =
-                        __ldg(reinterpret_cast<const uint4*>(xrow[j] + col0 + c * 32 + t * 8));
-            }
+                for (int c = 0; c < 4; ++c)
+                    v[j][c] = __ldg(reinterpret_cast<const uint4*>(xrow[j] + col0 + c * 32));
+        } else {
+#pragma unroll
+            for (int j = 0; j < NT; ++j)
+#pragma unroll
+                for (int c = 0; c < 4; ++c) {
+                    v[j][c] = make_uint4(0, 0, 0, 0);
+                    if (col0 + c * 32 < a.k)
+                        v[j][c] = __ldg(reinterpret_cast<const uint4*>(xrow[j] + col0 + c * 32));
+                }
+        }
     }
 };
 
@@ -241,35 +234,28 @@ struct Ring {
     uint32_t turn;               // boxes consumed
 };
 
-// The choices list[0 .. count): the products of this warp's boxes of the item, then y.  Before
-// each box's stage is free, `refill` issues the next box of the warp's stream into it.
-// `ok` turns false when a wait runs out: the warp then only keeps the barriers of the warps
-// that share its tiles.
-template <int G, int NT, class F>
-__device__ __forceinline__ void item_products(const Matvec4Args& a, Ring& ring, const Item& it,
-                                              const uint16_t* list, float* sums, int& buf,
-                                              bool& ok, F refill) {
+// One pass: the products of this warp's boxes, then y.  x is the first half box's, and the next
+// pass's when it returns (`advance` goes there, false at the end).  `refill` issues the next box
+// of the warp's stream into a stage that was read.  `ok` turns false when a wait runs out: the
+// warp then only keeps the barriers of the warps that share its tiles.
+template <int G, int NT, class F, class N>
+__device__ __forceinline__ bool pass_products(const Matvec4Args& a, Ring& ring, Pass& pass,
+                                              const uint16_t* (&xrow)[NT], Half<NT>& x,
+                                              const uint32_t* list, float* sums, int& buf,
+                                              bool& ok, F refill, N advance) {
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
     const int split = warp % a.splits;
     const int boxes = (a.k + kBoxCols - 1) / kBoxCols;
-    const uint16_t* xrow[NT];
-#pragma unroll
-    for (int j = 0; j < NT; ++j) {
-        const int i = j * 8 + g;
-        xrow[j] = i < it.count ? a.x + (long long)(list[i] / a.x_div) * a.ldx : nullptr;
-    }
+    const Pass it = pass;
+    const int count = min(NT * 8, it.end - it.at);
+    list += it.at;
     float acc[2][NT][4] = {};
     // a stage's scales: [groups][32], with gate and up [2][groups][16]
     const int tile_scales = a.glu ? kBoxCols / G * 32 : 32, group_scales = a.glu ? 32 : 64;
-    Half<NT> x;
-    x.load(a, xrow, split * kBoxCols);                 // on its way while the codes are
-    for (int box = split; box < boxes && ok; box += a.splits) {
+    for (int box = split; box < boxes; box += a.splits) {
         const int s = ring.turn % kStages, col0 = box * kBoxCols;
-        ok = mbar_wait_warp(&ring.full[s], (ring.turn / kStages) & 1);
-        if (!ok) {
-            latch_error(a.err, CRC_ETIMEOUT);
-            break;
-        }
+        if (ok) ok = mbar_wait_warp(&ring.full[s], (ring.turn / kStages) & 1);
+        if (!ok) latch_error(a.err, CRC_ETIMEOUT);
         const uint32_t codes = smem_u32(ring.codes + s * kCodeBytes);
         const uint32_t scales = smem_u32(ring.scales + s * kScaleBytes);
 #pragma unroll
@@ -279,10 +265,15 @@ __device__ __forceinline__ void item_products(const Matvec4Args& a, Ring& ring, 
             half_products<G, NT>(codes, scales, tile_scales, group_scales, half, x, acc);
             x = ahead;
         }
-        ++ring.turn;
-        __syncwarp();                                  // every lane has read the stage
-        refill(s);
+        if (ok) {
+            ++ring.turn;
+            __syncwarp();                              // every lane has read the stage
+            refill(s);
+        }
     }
+    // (between the halves of the last box it came 5% dearer: 44 us, not 41, for 64 tokens)
+    const bool more = advance();
+    if (more) x.load(a, xrow, split * kBoxCols);
     const int each = a.glu ? 16 : 32, row0 = it.tile * each;
     if (a.splits == 1) {
 #pragma unroll
@@ -290,8 +281,8 @@ __device__ __forceinline__ void item_products(const Matvec4Args& a, Ring& ring, 
 #pragma unroll
             for (int v = 0; v < 4; ++v) {
                 const int i = j * 8 + 2 * t + (v & 1), r = row0 + g + (v >> 1) * 8;
-                if (i >= it.count || !ok) continue;
-                uint16_t* y = a.y + (long long)list[i] * a.n;
+                if (i >= count || !ok) continue;
+                uint16_t* y = a.y + (long long)(list[i] & 0xffffu) * a.n;
                 if (a.glu) {
                     if (r < a.n)
                         y[r] = __bfloat16_as_ushort(
@@ -302,7 +293,7 @@ __device__ __forceinline__ void item_products(const Matvec4Args& a, Ring& ring, 
                         y[r + 16] = __bfloat16_as_ushort(__float2bfloat16_rn(acc[1][j][v]));
                 }
             }
-        return;
+        return more;
     }
     if constexpr (NT == 1) {
         // sums[buf][warp][choice][32 rows]; a buffer is written again behind the next barrier
@@ -316,7 +307,7 @@ __device__ __forceinline__ void item_products(const Matvec4Args& a, Ring& ring, 
                     acc[tile][0][v];
         const int w0 = warp - split;
         named_sync(1 + w0 / a.splits, a.splits * 32);
-        for (int o = split * 32 + lane; o < each * it.count; o += a.splits * 32) {
+        for (int o = split * 32 + lane; o < each * count; o += a.splits * 32) {
             const int i = o / each, r = o % each;
             if (row0 + r >= a.n) continue;
             float v = 0.f, u = 0.f;
@@ -325,10 +316,11 @@ __device__ __forceinline__ void item_products(const Matvec4Args& a, Ring& ring, 
                 if (a.glu) u += mine[(w * 8 + i) * 33 + r + 16];
             }
             if (a.glu) v = silu_up(v, u);
-            a.y[(long long)list[i] * a.n + row0 + r] =
+            a.y[(long long)(list[i] & 0xffffu) * a.n + row0 + r] =
                 __bfloat16_as_ushort(__float2bfloat16_rn(v));
         }
     }
+    return more;
 }
 
 // NT: choices of a pass over the weights, in eights.
@@ -348,7 +340,7 @@ __global__ void __launch_bounds__(kThreads, kCtas)
     ring.full = full[warp];
     ring.turn = 0;
     float* sums = reinterpret_cast<float*>(smem + kWarps * kStages * kStageBytes);
-    uint16_t* list = reinterpret_cast<uint16_t*>(sums + (a.splits > 1 ? 2 * kSums : 0));
+    uint32_t* list = reinterpret_cast<uint32_t*>(sums + (a.splits > 1 ? 2 * kSums : 0));
     if (threadIdx.x < kWarps * kStages) mbar_init(&full[0][0] + threadIdx.x, 1);
     for (int e = threadIdx.x; e <= a.N; e += kThreads) order.next[e] = 0;
     if (threadIdx.x == 0) {
@@ -370,26 +362,26 @@ __global__ void __launch_bounds__(kThreads, kCtas)
     __syncthreads();
     if (warp == 0) {
         constexpr int kEach = (kBins + 31) / 32;
-        int n = 0, tiles = 0;                          // this lane's bins
-        const auto tiles_of = [&](int count) { return count ? a.tiles : 0; };
+        int n = 0, active = 0;                         // this lane's bins
 #pragma unroll
         for (int i = 0; i < kEach; ++i) {
             const int e = lane * kEach + i;
             if (e > a.N) continue;
             n += order.next[e];
-            if (e < a.N) tiles += tiles_of(order.next[e]);
+            active += e < a.N && order.next[e] > 0;
         }
-        int n0 = n, t0 = tiles;
+        int n0 = n, a0 = active;
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
-            const int un = __shfl_up_sync(kFull, n0, o), ut = __shfl_up_sync(kFull, t0, o);
+            const int un = __shfl_up_sync(kFull, n0, o), ua = __shfl_up_sync(kFull, a0, o);
             if (lane >= o) {
                 n0 += un;
-                t0 += ut;
+                a0 += ua;
             }
         }
+        if (lane == 31) order.actives = a0;
         n0 -= n;
-        t0 -= tiles;
+        a0 -= active;
 #pragma unroll
         for (int i = 0; i < kEach; ++i) {
             const int e = lane * kEach + i;
@@ -397,54 +389,65 @@ __global__ void __launch_bounds__(kThreads, kCtas)
             const int count = order.next[e];
             order.first[e] = n0;
             order.next[e] = n0;
-            order.tile[e] = t0;
             n0 += count;
-            if (e < a.N) t0 += tiles_of(count);
-            if (e == a.N) order.first[e + 1] = n0;
+            if (e == a.N)
+                order.first[e + 1] = n0;
+            else if (count)
+                order.active[a0++] = (uint16_t)e;
         }
     }
     __syncthreads();
-    // in any order, another one in each CTA: a choice's result does not depend on its column of
-    // the fragments, nor on its pass, and one warp makes all passes of a tile
+    // (the row of x, the choice), in any order, another one in each CTA: a choice's result does
+    // not depend on its column of the fragments, nor on its pass, and one warp makes all passes
+    // of a tile
     for (int c = threadIdx.x; c < a.E; c += kThreads)
-        list[atomicAdd(&order.next[bin_of(c)], 1)] = (uint16_t)c;
+        list[atomicAdd(&order.next[bin_of(c)], 1)] = (uint32_t)(c / a.x_div) << 16 | (uint32_t)c;
     __syncthreads();
 
     // the choices without a slot: zeros
     const int none = order.first[a.N], nones = order.first[a.N + 1] - none, pieces = a.n / 8;
     for (long long o = (long long)blockIdx.x * kThreads + threadIdx.x;
          o < (long long)nones * pieces; o += (long long)gridDim.x * kThreads)
-        *(reinterpret_cast<uint4*>(a.y + (long long)list[none + o / pieces] * a.n) +
+        *(reinterpret_cast<uint4*>(a.y + (long long)(list[none + o / pieces] & 0xffffu) * a.n) +
           o % pieces) = make_uint4(0, 0, 0, 0);
 
-    const int items = order.tile[a.N];
+    const int items = order.actives * a.tiles;
     const int groups = kWarps / a.splits;              // groups of warps of a CTA
-    const int first = blockIdx.x * groups + warp / a.splits, step = gridDim.x * groups;
+    // (the warps of the last, partial turn lie in all CTAs)
+    const int first = warp / a.splits * gridDim.x + blockIdx.x, step = gridDim.x * groups;
     const int boxes = (a.k + kBoxCols - 1) / kBoxCols, split = warp % a.splits;
     const int each = a.glu ? 16 : 32;
+    // To the warp's next pass, from item `first - step` with nothing left on the way.
+    const auto advance = [&](Pass& p) {
+        p.at += NT * 8;
+        if (p.at < p.end) return true;
+        if (p.item + step >= items) return false;
+        p.item += step;
+        const int e = order.active[p.item / a.tiles];
+        p.tile = p.item % a.tiles;
+        p.slot = order.slot[e];
+        p.at = order.first[e];
+        p.end = order.first[e + 1];
+        return true;
+    };
     // the warp's stream of boxes, issued kStages before they are taken
     const uint32_t lead = elected();
     const uint64_t pol = l2_evict_first_policy();
-    Item next = {};
-    int ni = first - step, nbox = boxes, npass = 0;
+    Pass ahead = {};
+    ahead.item = first - step;
+    int nbox = boxes;
     uint32_t issued = 0;
     const auto refill = [&](int s) {
         if (nbox >= boxes) {
-            if (npass * (NT * 8) >= next.count) {
-                if (ni + step >= items) return;
-                ni += step;
-                npass = 0;
-                next = item_of(order, a, ni);
-            }
-            ++npass;
+            if (!advance(ahead)) return;
             nbox = split;
         }
         if (lead)
             mbar_arrive_expect_tx(&ring.full[s], kCodeBytes + 2 * 32 * (kBoxCols / G));
         tma_load_4d_by(lead, ring.codes + s * kCodeBytes, &mw, &ring.full[s], nbox * 128,
-                       next.tile * each, 0, next.slot, pol);
-        tma_load_4d_by(lead, ring.scales + s * kScaleBytes, &ms, &ring.full[s], next.tile * each,
-                       nbox * (kBoxCols / G), 0, next.slot, pol);
+                       ahead.tile * each, 0, ahead.slot, pol);
+        tma_load_4d_by(lead, ring.scales + s * kScaleBytes, &ms, &ring.full[s], ahead.tile * each,
+                       nbox * (kBoxCols / G), 0, ahead.slot, pol);
         nbox += a.splits;
         ++issued;
     };
@@ -452,19 +455,26 @@ __global__ void __launch_bounds__(kThreads, kCtas)
     for (int s = 0; s < kStages; ++s) refill(s);
     int buf = 0;
     bool ok = true;
-    for (int i = first; i < items; i += step) {
-        const Item all = item_of(order, a, i);
-        for (int at = 0; at < all.count; at += NT * 8) {
-            Item it = all;
-            it.at += at;
-            it.count = min(NT * 8, all.count - at);
-            const uint16_t* some = list + it.at;
-            if (NT == 1 || it.count <= 8)
-                item_products<G, 1>(a, ring, it, some, sums, buf, ok, refill);
-            else
-                item_products<G, NT>(a, ring, it, some, sums, buf, ok, refill);
+    Pass pass = {};
+    pass.item = first - step;
+    const uint16_t* xrow[NT];
+    const auto next_pass = [&] {
+        if (!advance(pass)) return false;
+#pragma unroll
+        for (int j = 0; j < NT; ++j) {
+            // (columns of the fragments without a choice: the first one's x, not stored)
+            const int i = pass.at + j * 8 + (lane >> 2);
+            xrow[j] = a.x + (long long)(list[i < pass.end ? i : pass.at] >> 16) * a.ldx +
+                      (lane & 3) * 8;
         }
-    }
+        return true;
+    };
+    bool more = next_pass();
+    Half<NT> x;
+    if (more) x.load(a, xrow, split * kBoxCols);       // on its way while the codes are
+    while (more)
+        more = pass_products<G, NT>(a, ring, pass, xrow, x, list, sums, buf, ok, refill,
+                                    next_pass);
     // never leave with copies in flight
     if (!ok)
         for (uint32_t n = ring.turn; n < issued; ++n)
@@ -473,7 +483,7 @@ __global__ void __launch_bounds__(kThreads, kCtas)
 
 size_t smem_bytes(int splits, int E) {
     return 1024 + (size_t)kWarps * kStages * kStageBytes + (splits > 1 ? 2 * kSums * 4 : 0) +
-           (size_t)E * 2 + 16;
+           (size_t)E * 4 + 16;
 }
 
 template <int G, int NT>
@@ -577,17 +587,24 @@ extern "C" int crc_matvec4(const crc_matvec4_weights* w, const uint16_t* x_dev, 
     a.glu = w->glu;
     const int each = a.glu ? 16 : 32;
     a.tiles = (a.n + each - 1) / each;
-    // Warps share a tile's columns while there are more of them than tiles (experts taken by
-    // some choice are at most E and N)
+    // 2, 4 or 8 warps share a tile's columns where that ends the last turn of the warps earlier:
+    // turns times boxes, and one more for a turn's beginning and end.  (Experts that some choice
+    // takes are at most E and N.)
     const int boxes = (a.k + kBoxCols - 1) / kBoxCols;
     const long long items = (long long)(a.E < a.N ? a.E : a.N) * a.tiles;
     const long long warps = (long long)sm_count() * kCtas * kWarps;
-    const bool few = M <= 8;
+    const bool few = a.E < 8ll * a.N;              // choices of an expert, on average
     a.splits = 1;
-    while (few && a.splits < kWarps && 2 * a.splits <= boxes && items * 2 * a.splits <= warps)
-        a.splits *= 2;
-    // (a pass over the weights takes 8 choices, 16 with more rows: choices of one expert are
-    // no more than M unless an id comes twice)
+    long long least = 0;
+    for (int s = 1; s <= (few ? kWarps : 1) && s <= boxes; s *= 2) {
+        const long long turns = (items * s + warps - 1) / warps;
+        const long long cost = turns * ((boxes + s - 1) / s + 1);
+        if (s == 1 || cost < least) {
+            least = cost;
+            a.splits = s;
+        }
+    }
+    // (a pass over the weights takes 8 choices, 16 where an expert has that many)
     const long long ctas = (items * a.splits + kWarps - 1) / kWarps;
     const long long room = (long long)sm_count() * kCtas;
     const dim3 grid((unsigned)(ctas < room ? ctas : room));
