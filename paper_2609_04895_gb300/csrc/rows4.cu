@@ -32,17 +32,29 @@ struct Quantize4Args {
     int n, k;                    // rows and columns of a matrix
 };
 
-// The whole number nearest to v / a, ties to the even one, from an approximate inverse.
-// v has 8 significant bits and so has a: v / a is a tie exactly or at least 2^-10 away from
-// one, and t is within 2^-20 of it, so only an exact tie can round the other way.  v - r a
-// is exact (r < 8).
-__device__ __forceinline__ int code_of(float v, float a, float inv) {
-    const float t = v * inv;
-    float r = rintf(t);
-    const float rest = fmaf(-r, a, v);
-    const int odd = (int)r & 1;
-    if (2.f * fabsf(rest) == a && odd) r += rest > 0.f ? 1.f : -1.f;
-    return (int)fminf(fmaxf(r, -7.f), 7.f);
+// 1.5 * 2^23 plus the whole number nearest to v / a, ties to the even one: its low bits are the
+// code's.  v inv is within 2^-23 of the quotient's value, and one step from there rounds it to
+// fp32 as a division would (v - q a is exact, a >= 2^-100).  With 8 significant bits each, v / a
+// is a tie exactly or at least 2^-10 away from one, so the rounding to fp32 changes no code.
+__device__ __forceinline__ uint32_t code_bits(float v, float a, float inv) {
+    const float q = v * inv;
+    return __float_as_uint(fmaf(fmaf(-q, a, v), inv, q) + 12582912.f);
+}
+__device__ __forceinline__ float low_half(uint32_t w) { return __uint_as_float(w << 16); }
+__device__ __forceinline__ float high_half(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
+// The codes of eight bf16 numbers, two a byte.
+__device__ __forceinline__ uint32_t eight_codes(const uint32_t (&w)[4], float a, float inv) {
+    uint32_t e[4], o[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        e[i] = code_bits(low_half(w[i]), a, inv);
+        o[i] = code_bits(high_half(w[i]), a, inv);
+    }
+    const uint32_t even = __byte_perm(__byte_perm(e[0], e[1], 0x0040),
+                                      __byte_perm(e[2], e[3], 0x0040), 0x5410);
+    const uint32_t odd = __byte_perm(__byte_perm(o[0], o[1], 0x0040),
+                                     __byte_perm(o[2], o[3], 0x0040), 0x5410);
+    return (even & 0x0f0f0f0fu) | ((odd << 4) & 0xf0f0f0f0u);
 }
 
 template <int G>
@@ -83,20 +95,12 @@ __global__ void __launch_bounds__(kQThreads) quantize_rows4_kernel(Quantize4Args
         if (__bfloat162float(s) == 0.f) s = __float2bfloat16_rn(1.f);
         const float af = __bfloat162float(s);
         uint32_t lo = 0, hi = 0;
-        if (af >= 1.1754944e-38f && af < 3.e38f) {
+        if (af >= 0x1p-100f && af < 3.e38f) {
             const float inv = __frcp_rn(af);
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const int c0 = code_of(__uint_as_float(w[j] << 16), af, inv);
-                const int c1 = code_of(__uint_as_float(w[j] & 0xffff0000u), af, inv);
-                const uint32_t b = (uint32_t)(c0 & 15) | (uint32_t)(c1 & 15) << 4;
-                if (j < 4)
-                    lo |= b << (8 * j);
-                else
-                    hi |= b << (8 * j - 32);
-            }
+            lo = eight_codes({w[0], w[1], w[2], w[3]}, af, inv);
+            hi = eight_codes({w[4], w[5], w[6], w[7]}, af, inv);
         } else if (af < 1.f) {
-            // a subnormal scale has fewer bits and perhaps no inverse: the division itself
+            // a tiny scale has a rest that is not exact, or no inverse: the division itself
 #pragma unroll 1
             for (int j = 0; j < 8; ++j) {
                 const float q0 = rintf(__fdiv_rn(__uint_as_float(w[j] << 16), af));
