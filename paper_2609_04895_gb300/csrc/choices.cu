@@ -24,10 +24,10 @@ namespace {
 
 constexpr int kOrderThreads = 1024;
 constexpr int kWarps = kOrderThreads / 32;
-constexpr int kSteps = 4;                                   // choices a lane and sub-chunk
-constexpr int kSub = kOrderThreads * kSteps;                // choices of a sub-chunk
-constexpr int kOneChunk = 2 * kSub;
-constexpr int kMaxChunks = 128;
+constexpr int kSteps = 8;                                   // choices of a lane at a time
+constexpr int kSub = kOrderThreads * kSteps;                // choices of a CTA at a time
+constexpr int kOneChunk = 4096;          // (8 us in one CTA; 13 for 8192, and 8 in two launches)
+constexpr int kMaxChunks = 128, kMinChunk = 2048;
 constexpr int kMaxExperts = 256;
 constexpr int kBins = kMaxExperts + 1;                      // the last: no expert
 
@@ -38,7 +38,8 @@ struct OrderArgs {
     int32_t* offsets;
     int32_t* rows;
     int32_t* place;
-    int32_t* counts;        // [N + 1][chunks], NULL: one chunk
+    int32_t* counts;        // [chunks][N + 1], NULL: one chunk
+    uint32_t* err;
     int E, N, chunk, chunks;
 };
 
@@ -47,7 +48,7 @@ __device__ __forceinline__ int bin_of(const OrderArgs& a, int c) {
     return e < a.N ? e : a.N;
 }
 
-// counts[bin][chunk]
+// counts[chunk][bin]
 __global__ void __launch_bounds__(kOrderThreads) count_choices_kernel(OrderArgs a) {
     __shared__ int hist[kBins];
     for (int b = threadIdx.x; b <= a.N; b += kOrderThreads) hist[b] = 0;
@@ -58,78 +59,91 @@ __global__ void __launch_bounds__(kOrderThreads) count_choices_kernel(OrderArgs 
     for (int c = c0 + threadIdx.x; c < c1; c += kOrderThreads) atomicAdd(&hist[bin_of(a, c)], 1);
     __syncthreads();
     for (int b = threadIdx.x; b <= a.N; b += kOrderThreads)
-        a.counts[b * a.chunks + blockIdx.x] = hist[b];
+        a.counts[blockIdx.x * (a.N + 1) + b] = hist[b];
+}
+
+// The bins' exclusive sum, in place: start[0 .. kBins + 30], zeros behind the last.  One warp.
+__device__ __forceinline__ void scan_bins(int* start) {
+    constexpr int kEach = (kBins + 31) / 32;
+    const int lane = threadIdx.x & 31;
+    int v[kEach], sum = 0;
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+        v[i] = sum;
+        sum += start[lane * kEach + i];
+    }
+    int incl = sum;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const int u = __shfl_up_sync(kFull, incl, o);
+        if (lane >= o) incl += u;
+    }
+    __syncwarp();
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) start[lane * kEach + i] = incl - sum + v[i];
 }
 
 __global__ void __launch_bounds__(kOrderThreads) order_choices_kernel(OrderArgs a) {
-    __shared__ int start[kBins + 31], before[kBins];
-    __shared__ int count[kWarps][kBins];        // a warp's choices of each expert, then its first place
+    __shared__ int start[kBins + 31];           // each expert's first place, of this CTA's in turn
+    __shared__ int total[kBins + 31];           // and its choices
+    __shared__ int count[kWarps][kBins];        // a warp's choices of each, then those before it
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int bins = a.N + 1;
-    for (int b = threadIdx.x; b < kBins + 31; b += kOrderThreads) start[b] = 0;
-    __syncthreads();
+    for (int b = threadIdx.x; b < kBins + 31; b += kOrderThreads) start[b] = total[b] = 0;
     pdl_begin();
     const int c0 = blockIdx.x * a.chunk;
     const int c1 = min(a.E, c0 + a.chunk);
-    // totals of every expert, and those of the chunks before this one
-    if (a.counts) {
-        for (int b = warp; b < bins; b += kWarps) {
-            int all = 0, mine = 0;
+    const int steps = (min(a.chunk, kSub) + kOrderThreads - 1) / kOrderThreads;
+    const auto choice = [&](int s0, int i) { return s0 + (warp * steps + i) * 32 + lane; };
+    int bin[kSteps], rank[kSteps];
+    const auto load = [&](int s0) {
 #pragma unroll
-            for (int i = 0; i < kMaxChunks / 32; ++i) {
-                const int k = i * 32 + lane;
-                const int v = k < a.chunks ? a.counts[b * a.chunks + k] : 0;
+        for (int i = 0; i < kSteps; ++i) {
+            const int c = choice(s0, i);
+            bin[i] = i < steps && c < c1 ? bin_of(a, c) : -1;
+        }
+    };
+    load(c0);
+    if (a.counts) {
+        // every expert's choices, and those of the chunks before this one: a thread a part of
+        // the chunks for one expert
+        const int wide = (bins + 31) / 32 * 32, parts = kOrderThreads / wide;
+        const int part = threadIdx.x / wide, b = threadIdx.x % wide;
+        int all = 0, mine = 0;
+        if (part < parts && b < bins)
+#pragma unroll 8
+            for (int k = part; k < a.chunks; k += parts) {
+                const int v = a.counts[k * bins + b];
                 all += v;
                 if (k < (int)blockIdx.x) mine += v;
             }
-            all = __reduce_add_sync(kFull, all);
-            mine = __reduce_add_sync(kFull, mine);
-            if (lane == 0) {
-                start[b] = all;
-                before[b] = mine;
+        int* scratch = &count[0][0];
+        scratch[threadIdx.x] = all;
+        scratch[kOrderThreads + threadIdx.x] = mine;
+        __syncthreads();
+        all = mine = 0;
+        if ((int)threadIdx.x < bins) {
+            for (int p = 0; p < parts; ++p) {
+                all += scratch[p * wide + threadIdx.x];
+                mine += scratch[kOrderThreads + p * wide + threadIdx.x];
             }
+            start[threadIdx.x] = all;
         }
-    } else {
-        for (int c = c0 + threadIdx.x; c < c1; c += kOrderThreads) atomicAdd(&start[bin_of(a, c)], 1);
-        for (int b = threadIdx.x; b < bins; b += kOrderThreads) before[b] = 0;
+        __syncthreads();
+        if (warp == 0) scan_bins(start);
+        __syncthreads();
+        if ((int)threadIdx.x < bins) {
+            if (blockIdx.x == 0) a.offsets[threadIdx.x] = start[threadIdx.x];
+            start[threadIdx.x] += mine;
+        }
     }
-    __syncthreads();
-    // exclusive sum over the experts: nine a lane
-    if (warp == 0) {
-        constexpr int kEach = (kBins + 31) / 32;
-        int v[kEach], sum = 0;
-#pragma unroll
-        for (int i = 0; i < kEach; ++i) {
-            v[i] = sum;
-            sum += start[lane * kEach + i];
-        }
-        int incl = sum;
-#pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-            const int u = __shfl_up_sync(kFull, incl, o);
-            if (lane >= o) incl += u;
-        }
-        __syncwarp();
-#pragma unroll
-        for (int i = 0; i < kEach; ++i) start[lane * kEach + i] = incl - sum + v[i];
-    }
-    __syncthreads();
-    if (blockIdx.x == 0)
-        for (int b = threadIdx.x; b < bins; b += kOrderThreads) a.offsets[b] = start[b];
-    __syncthreads();
-    for (int b = threadIdx.x; b < bins; b += kOrderThreads) start[b] += before[b];
-
     for (int s0 = c0; s0 < c1; s0 += kSub) {
+        if (s0 > c0) load(s0);
         for (int b = lane; b < bins; b += 32) count[warp][b] = 0;
         __syncwarp();
-        int bin[kSteps], rank[kSteps];
 #pragma unroll
         for (int i = 0; i < kSteps; ++i) {
-            const int c = s0 + warp * (32 * kSteps) + i * 32 + lane;
-            bin[i] = c < c1 ? bin_of(a, c) : -1;
-        }
-#pragma unroll
-        for (int i = 0; i < kSteps; ++i) {
+            if (i >= steps) break;
             const unsigned same = __match_any_sync(kFull, bin[i]);
             const unsigned below = same & ((1u << lane) - 1);
             if (bin[i] >= 0) rank[i] = count[warp][bin[i]] + __popc(below);
@@ -138,7 +152,7 @@ __global__ void __launch_bounds__(kOrderThreads) order_choices_kernel(OrderArgs 
             __syncwarp();
         }
         __syncthreads();
-        // each expert's counts over the warps: its first place in every warp
+        // each expert's choices in the warps before
         for (int b = warp; b < bins; b += kWarps) {
             const int v = count[lane][b];
             int incl = v;
@@ -147,21 +161,28 @@ __global__ void __launch_bounds__(kOrderThreads) order_choices_kernel(OrderArgs 
                 const int u = __shfl_up_sync(kFull, incl, o);
                 if (lane >= o) incl += u;
             }
-            const int first = start[b];
-            count[lane][b] = first + incl - v;
-            __syncwarp();
-            if (lane == 31) start[b] = first + incl;
+            count[lane][b] = incl - v;
+            if (lane == 31) total[b] = incl;
         }
         __syncthreads();
+        if (!a.counts) {                        // one chunk: these are all choices
+            if ((int)threadIdx.x < bins) start[threadIdx.x] = total[threadIdx.x];
+            __syncthreads();
+            if (warp == 0) scan_bins(start);
+            __syncthreads();
+            if ((int)threadIdx.x < bins) a.offsets[threadIdx.x] = start[threadIdx.x];
+        }
 #pragma unroll
         for (int i = 0; i < kSteps; ++i) {
             if (bin[i] < 0) continue;
-            const int c = s0 + warp * (32 * kSteps) + i * 32 + lane;
-            const int at = count[warp][bin[i]] + rank[i];
+            const int c = choice(s0, i);
+            const int at = start[bin[i]] + count[warp][bin[i]] + rank[i];
             const bool real = bin[i] < a.N;
-            if (CRC_IN_BOUNDS(at >= 0 && at < a.E, (uint32_t*)nullptr)) a.rows[at] = real ? c : -1;
+            if (CRC_IN_BOUNDS(at >= 0 && at < a.E, a.err)) a.rows[at] = real ? c : -1;
             if (a.place) a.place[c] = real ? at : -1;
         }
+        __syncthreads();
+        if ((int)threadIdx.x < bins) start[threadIdx.x] += total[threadIdx.x];
         __syncthreads();
     }
 }
@@ -169,8 +190,8 @@ __global__ void __launch_bounds__(kOrderThreads) order_choices_kernel(OrderArgs 
 // ---------------------------------------------------------------------------
 // the sum over a token's choices
 // ---------------------------------------------------------------------------
-constexpr int kBatch = 8;                    // choices whose loads are in flight together
 constexpr int kSumThreads = 256;
+constexpr int kManyTokens = 6000;
 
 struct SumArgs {
     const uint16_t* y;           // [rows][d]
@@ -208,102 +229,163 @@ __device__ __forceinline__ long long row_of(const SumArgs& a, int m, int j) {
     return r >= 0 && r < a.rows ? r : -1;
 }
 
+// kBatch: choices of a token whose loads are in flight together; kTok: tokens of a team.
+template <int kBatch, int kTok>
 __global__ void __launch_bounds__(kSumThreads) sum_choices_kernel(SumArgs a) {
     pdl_begin();
     const int t = threadIdx.x % a.team;
-    const int m = blockIdx.x * (blockDim.x / a.team) + threadIdx.x / a.team;
+    const int m = (blockIdx.x * (blockDim.x / a.team) + threadIdx.x / a.team) * kTok;
     if (m >= a.M) return;
     for (int v = t; v < a.d / 8; v += a.team) {
-        float sum[8] = {};
+        float sum[kTok][8] = {};
         for (int j0 = 0; j0 < a.K; j0 += kBatch) {
-            uint4 u[kBatch];
-            float g[kBatch];
-            bool on[kBatch];
+            uint4 u[kTok][kBatch];
+            float g[kTok][kBatch];
+            bool on[kTok][kBatch];
 #pragma unroll
-            for (int j = 0; j < kBatch; ++j) {
-                const long long r = j0 + j < a.K ? row_of(a, m, j0 + j) : -1;
-                on[j] = r >= 0;
-                g[j] = on[j] && a.gates ? a.gates[(long long)m * a.K + j0 + j] : 1.f;
-                if (on[j]) u[j] = __ldcs(reinterpret_cast<const uint4*>(a.y + r * a.d) + v);
-            }
+            for (int k = 0; k < kTok; ++k)
 #pragma unroll
-            for (int j = 0; j < kBatch; ++j) {
-                if (!on[j]) continue;
-                float f[8];
-                widen(u[j], f);
+                for (int j = 0; j < kBatch; ++j) {
+                    const bool has = m + k < a.M && j0 + j < a.K;
+                    const long long r = has ? row_of(a, m + k, j0 + j) : -1;
+                    on[k][j] = r >= 0;
+                    g[k][j] = r >= 0 && a.gates ? a.gates[(long long)(m + k) * a.K + j0 + j] : 1.f;
+                    if (r >= 0) u[k][j] = __ldcs(reinterpret_cast<const uint4*>(a.y + r * a.d) + v);
+                }
 #pragma unroll
-                for (int i = 0; i < 8; ++i) sum[i] = fmaf(g[j], f[i], sum[i]);
-            }
+            for (int k = 0; k < kTok; ++k)
+#pragma unroll
+                for (int j = 0; j < kBatch; ++j) {
+                    if (!on[k][j]) continue;
+                    float f[8];
+                    widen(u[k][j], f);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) sum[k][i] = fmaf(g[k][j], f[i], sum[k][i]);
+                }
         }
-        *(reinterpret_cast<uint4*>(a.out + (long long)m * a.d) + v) = narrow(sum);
+#pragma unroll
+        for (int k = 0; k < kTok; ++k)
+            if (m + k < a.M)
+                *(reinterpret_cast<uint4*>(a.out + (long long)(m + k) * a.d) + v) = narrow(sum[k]);
     }
 }
 
 // dy[place] = gate dout, dgates = <dout, y[place]>: a token's threads share its rows, and
-// the dot products of eight choices are summed over the lanes and then the warps.
+// the dot products are summed over the lanes and then the warps.
+template <int kBatch, int kTok>
 __global__ void __launch_bounds__(kSumThreads) sum_choices_grad_kernel(SumArgs a) {
-    __shared__ float part[kSumThreads / 32][kBatch];
+    constexpr int kDots = kTok * kBatch;
+    __shared__ float part[kSumThreads / 32][kDots];
     pdl_begin();
     const int t = threadIdx.x % a.team;
-    const int m = blockIdx.x * (blockDim.x / a.team) + threadIdx.x / a.team;
+    const int m = (blockIdx.x * (blockDim.x / a.team) + threadIdx.x / a.team) * kTok;
     const bool real = m < a.M;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     for (int j0 = 0; j0 < a.K; j0 += kBatch) {
-        long long r[kBatch];
-        float g[kBatch], dot[kBatch];
+        long long r[kTok][kBatch];
+        float g[kTok][kBatch], dot[kTok][kBatch];
 #pragma unroll
-        for (int j = 0; j < kBatch; ++j) {
-            r[j] = real && j0 + j < a.K ? row_of(a, m, j0 + j) : -1;
-            g[j] = r[j] >= 0 && a.gates ? a.gates[(long long)m * a.K + j0 + j] : 1.f;
-            dot[j] = 0.f;
-        }
+        for (int k = 0; k < kTok; ++k)
+#pragma unroll
+            for (int j = 0; j < kBatch; ++j) {
+                const bool has = m + k < a.M && j0 + j < a.K;
+                r[k][j] = has ? row_of(a, m + k, j0 + j) : -1;
+                g[k][j] = r[k][j] >= 0 && a.gates
+                              ? a.gates[(long long)(m + k) * a.K + j0 + j]
+                              : 1.f;
+                dot[k][j] = 0.f;
+            }
         if (real)
             for (int v = t; v < a.d / 8; v += a.team) {
-                float f[8];
-                widen(*(reinterpret_cast<const uint4*>(a.dout + (long long)m * a.d) + v), f);
-                uint4 u[kBatch];
+                uint4 d[kTok], u[kTok][kBatch];
+#pragma unroll
+                for (int k = 0; k < kTok; ++k)
+                    if (m + k < a.M)
+                        d[k] = *(reinterpret_cast<const uint4*>(a.dout + (long long)(m + k) * a.d) +
+                                 v);
                 if (a.dgates)
 #pragma unroll
-                    for (int j = 0; j < kBatch; ++j)
-                        if (r[j] >= 0)
-                            u[j] = __ldcs(reinterpret_cast<const uint4*>(a.y + r[j] * a.d) + v);
+                    for (int k = 0; k < kTok; ++k)
 #pragma unroll
-                for (int j = 0; j < kBatch; ++j) {
-                    if (r[j] < 0) continue;
-                    if (a.dgates) {
-                        float y[8];
-                        widen(u[j], y);
+                        for (int j = 0; j < kBatch; ++j)
+                            if (r[k][j] >= 0)
+                                u[k][j] = __ldcs(
+                                    reinterpret_cast<const uint4*>(a.y + r[k][j] * a.d) + v);
 #pragma unroll
-                        for (int i = 0; i < 8; ++i) dot[j] = fmaf(f[i], y[i], dot[j]);
-                    }
-                    if (a.out) {
-                        float w[8];
+                for (int k = 0; k < kTok; ++k) {
+                    if (m + k >= a.M) break;
+                    float f[8];
+                    widen(d[k], f);
 #pragma unroll
-                        for (int i = 0; i < 8; ++i) w[i] = g[j] * f[i];
-                        *(reinterpret_cast<uint4*>(a.out + r[j] * a.d) + v) = narrow(w);
+                    for (int j = 0; j < kBatch; ++j) {
+                        if (r[k][j] < 0) continue;
+                        if (a.dgates) {
+                            float y[8];
+                            widen(u[k][j], y);
+#pragma unroll
+                            for (int i = 0; i < 8; ++i) dot[k][j] = fmaf(f[i], y[i], dot[k][j]);
+                        }
+                        if (a.out) {
+                            float w[8];
+#pragma unroll
+                            for (int i = 0; i < 8; ++i) w[i] = g[k][j] * f[i];
+                            *(reinterpret_cast<uint4*>(a.out + r[k][j] * a.d) + v) = narrow(w);
+                        }
                     }
                 }
             }
         if (!a.dgates) continue;
 #pragma unroll
-        for (int j = 0; j < kBatch; ++j) {
+        for (int q = 0; q < kDots; ++q) {
+            float s = dot[q / kBatch][q % kBatch];
 #pragma unroll
-            for (int o = 16; o; o >>= 1) dot[j] += __shfl_xor_sync(kFull, dot[j], o);
-            if (lane == 0) part[warp][j] = dot[j];
+            for (int o = 16; o; o >>= 1) s += __shfl_xor_sync(kFull, s, o);
+            if (lane == 0) part[warp][q] = s;
         }
         __syncthreads();
-        if (real && t < kBatch && j0 + t < a.K) {
+        const int k = t / kBatch, j = j0 + t % kBatch;
+        if (t < kDots && m + k < a.M && j < a.K) {
             float s = 0.f;
             for (int w = 0; w < a.team / 32; ++w) s += part[warp + w][t];
-            a.dgates[(long long)m * a.K + j0 + t] = s;
+            a.dgates[(long long)(m + k) * a.K + j] = s;
         }
         __syncthreads();
     }
 }
 
+// Threads of a token: as few as leave no 16-byte piece more than the other threads have.
+template <bool Grad, int kBatch, int kTok>
+cudaError_t launch_sum_of(SumArgs& a, cudaStream_t st) {
+    const int vec = a.d / 8;
+    const int turns = (vec + kSumThreads - 1) / kSumThreads;
+    a.team = ((vec + turns - 1) / turns + 31) / 32 * 32;
+    const int teams = kSumThreads / a.team, tokens = teams * kTok;
+    const unsigned grid = (unsigned)((a.M + tokens - 1) / tokens);
+    if constexpr (Grad)
+        return launch_dependent(sum_choices_grad_kernel<kBatch, kTok>, dim3(grid), teams * a.team,
+                                0, st, 1, a);
+    else
+        return launch_dependent(sum_choices_kernel<kBatch, kTok>, dim3(grid), teams * a.team, 0, st,
+                                1, a);
+}
+template <bool Grad>
+cudaError_t launch_sum(SumArgs& a, cudaStream_t st) {
+    // One or two choices: several tokens' loads together.  Us, one / several tokens: gradient of
+    // 14400 tokens of d = 816, K = 1, 22.6 / 21.5, of 4000 of d = 1280, K = 2, 14.3 / 13.4; sum,
+    // K = 1, d = 816, 14400 tokens 15.3 / 12.6, 4000 tokens 4.4 / 4.5, 2000 2.6 / 3.0; K = 2,
+    // d = 1280, 4000 tokens 7.3 / 8.1.
+    if (a.K == 1)
+        return Grad || a.M >= kManyTokens ? launch_sum_of<Grad, 1, 4>(a, st)
+                                          : launch_sum_of<Grad, 1, 1>(a, st);
+    if (a.K == 2) return launch_sum_of<Grad, 2, Grad ? 2 : 1>(a, st);
+    if (Grad || a.K <= 4) return launch_sum_of<Grad, 4, 1>(a, st);
+    return launch_sum_of<Grad, 8, 1>(a, st);
+}
+
 int order_chunk(long long E) {
     const long long each = (E + kMaxChunks - 1) / kMaxChunks;
-    return (int)((each + kSub - 1) / kSub * kSub);
+    const long long chunk = (each + kOrderThreads - 1) / kOrderThreads * kOrderThreads;
+    return (int)(chunk < kMinChunk ? kMinChunk : chunk);
 }
 
 int check_order(int32_t M, int32_t K, int32_t N) {
@@ -318,16 +400,6 @@ int check_sum(int64_t rows, int32_t M, int32_t K, int32_t d, const void* place) 
         return CRC_EUNSUPPORTED;
     if (!place && rows < (int64_t)M * K) return CRC_EINVAL;
     return CRC_OK;
-}
-
-// Threads of a token: as few as leave no 16-byte piece more than the other threads have.
-void sum_shape(SumArgs& a, unsigned* grid, unsigned* threads) {
-    const int vec = a.d / 8;
-    const int turns = (vec + kSumThreads - 1) / kSumThreads;
-    a.team = ((vec + turns - 1) / turns + 31) / 32 * 32;
-    const int tokens = kSumThreads / a.team;
-    *threads = tokens * a.team;
-    *grid = (unsigned)((a.M + tokens - 1) / tokens);
 }
 
 }  // namespace
@@ -365,6 +437,7 @@ int crc_group_choices(const uint8_t* topk_dev, int32_t M, int32_t K, int32_t N,
     a.rows = rows_dev;
     a.place = place_dev;
     a.counts = need ? static_cast<int32_t*>(workspace_dev) : nullptr;
+    a.err = device_error_word();
     a.E = E;
     a.N = N;
     a.chunk = need ? order_chunk(E) : E;
@@ -406,13 +479,11 @@ int crc_sum_choices(const uint16_t* y_dev, int64_t y_rows, const int32_t* place_
     a.M = M;
     a.K = K;
     a.d = d;
-    unsigned grid, threads;
-    sum_shape(a, &grid, &threads);
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     cudaError_t e;
     {
         ProfScope prof(CRC_KERNEL_SUM, st);
-        e = launch_dependent(sum_choices_kernel, dim3(grid), threads, 0, st, 1, a);
+        e = launch_sum<false>(a, st);
     }
     note_launch();
     return cuda_status(e);
@@ -439,13 +510,11 @@ int crc_sum_choices_grad(const uint16_t* dout_dev, const uint16_t* y_dev, int64_
     a.M = M;
     a.K = K;
     a.d = d;
-    unsigned grid, threads;
-    sum_shape(a, &grid, &threads);
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     cudaError_t e;
     {
         ProfScope prof(CRC_KERNEL_SUM, st);
-        e = launch_dependent(sum_choices_grad_kernel, dim3(grid), threads, 0, st, 1, a);
+        e = launch_sum<true>(a, st);
     }
     note_launch();
     return cuda_status(e);
