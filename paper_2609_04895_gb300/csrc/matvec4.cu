@@ -404,12 +404,13 @@ __global__ void __launch_bounds__(kThreads, kCtas)
         list[atomicAdd(&order.next[bin_of(c)], 1)] = (uint32_t)(c / a.x_div) << 16 | (uint32_t)c;
     __syncthreads();
 
-    // the choices without a slot: zeros
-    const int none = order.first[a.N], nones = order.first[a.N + 1] - none, pieces = a.n / 8;
-    for (long long o = (long long)blockIdx.x * kThreads + threadIdx.x;
-         o < (long long)nones * pieces; o += (long long)gridDim.x * kThreads)
-        *(reinterpret_cast<uint4*>(a.y + (long long)(list[none + o / pieces] & 0xffffu) * a.n) +
-          o % pieces) = make_uint4(0, 0, 0, 0);
+    // the choices without a slot: zeros.  (By their numbers: the list's order is this CTA's.)
+    if (order.first[a.N + 1] > order.first[a.N])
+        for (int c = blockIdx.x; c < a.E; c += gridDim.x)
+            if (bin_of(c) == a.N)
+                for (int o = threadIdx.x; o < a.n / 8; o += kThreads)
+                    *(reinterpret_cast<uint4*>(a.y + (long long)c * a.n) + o) =
+                        make_uint4(0, 0, 0, 0);
 
     const int items = order.actives * a.tiles;
     const int groups = kWarps / a.splits;              // groups of warps of a CTA
@@ -565,8 +566,8 @@ extern "C" int crc_matvec4(const crc_matvec4_weights* w, const uint16_t* x_dev, 
     if (rc) return rc;
     if (M < 0 || K < 1 || (x_per_choice != 0 && x_per_choice != 1)) return CRC_EINVAL;
     if (x_stride < w->k || x_stride % 8 != 0) return CRC_EINVAL;
-    if (!topk_dev && (K != 1 || w->expert_slot_dev)) return CRC_EINVAL;
     if (M == 0) return CRC_OK;
+    if (!topk_dev && (K != 1 || w->expert_slot_dev)) return CRC_EINVAL;
     if (M > kMaxTokens || K > 32 || M * K > kMaxChoices) return CRC_EUNSUPPORTED;
     if (!x_dev || !y_dev || !aligned(x_dev, 16) || !aligned(y_dev, 16)) return CRC_EINVAL;
     CUtensorMap mw, ms;
