@@ -10,6 +10,7 @@ from __future__ import annotations
 import ctypes
 import math
 import os
+import struct
 import threading
 from dataclasses import dataclass
 
@@ -95,6 +96,10 @@ class crc_matvec4_weights(ctypes.Structure):
                 ("scale_stride", ctypes.c_int64), ("expert_slot_dev", ctypes.c_void_p)]
 
 
+_GROUP_WEIGHTS = struct.Struct("6iqqqq")               # crc_group_weights
+_MATVEC4_WEIGHTS = struct.Struct("6iqqqqqq")           # crc_matvec4_weights
+
+
 class CrcError(RuntimeError):
     def __init__(self, code: int, what: str):
         self.code = code
@@ -151,15 +156,16 @@ EXPORTS = [
      [ctypes.POINTER(crc_moe), P, I64, P, P, P, I64, I32, P, P, P, P, SZ, P]),
     ("crc_group_choices_workspace_bytes", SZ, [I32, I32, I32]),
     ("crc_group_choices", ctypes.c_int, [P, I32, I32, I32, P, P, P, P, SZ, P]),
+    # (the structs of these three may also come as their bytes, which are quicker to make)
     ("crc_group_matmul", ctypes.c_int,
-     [ctypes.POINTER(crc_group_weights), P, I64, I64, P, P, P, I32, I64, P, P]),
+     [P, P, I64, I64, P, P, P, I32, I64, P, P]),
     ("crc_group_matmul_grad", ctypes.c_int,
-     [ctypes.POINTER(crc_group_weights), P, P, I64, I64, P, P, I32, I64, P, P, I32, P]),
+     [P, P, P, I64, I64, P, P, I32, I64, P, P, I32, P]),
     ("crc_sum_choices", ctypes.c_int, [P, I64, P, P, I32, I32, I32, P, P]),
     ("crc_sum_choices_grad", ctypes.c_int, [P, P, I64, P, P, I32, I32, I32, P, P, P]),
     ("crc_quantize_rows4", ctypes.c_int, [P, I64, I32, I32, I32, I32, P, P, P]),
     ("crc_matvec4", ctypes.c_int,
-     [ctypes.POINTER(crc_matvec4_weights), P, I64, I32, P, I32, I32, P, P]),
+     [P, P, I64, I32, P, I32, I32, P, P]),
 ]
 
 
@@ -966,36 +972,47 @@ def group_choices(topk, N: int, offsets=None, rows=None, place=None, workspace=N
         need = crc_group_choices_workspace_bytes(M, K, N)
         if need:
             workspace = _new(stream, topk.device, (need,), torch.uint8)
-    crc_group_choices(_check(topk, "topk", (M, K), torch.uint8, dev), M, K, N,
-                      _check(offsets, "offsets", (N + 1,), i32, dev),
-                      _check(rows, "rows", (M * K,), i32, dev),
-                      _check(place, "place", (M, K), i32, dev), *_workspace(workspace, dev),
-                      _stream(stream, dev))
+    rc = load().crc_group_choices(
+        _check(topk, "topk", (M, K), torch.uint8, dev), M, K, N,
+        _check(offsets, "offsets", (N + 1,), i32, dev), _check(rows, "rows", (M * K,), i32, dev),
+        _check(place, "place", (M, K), i32, dev), *_workspace(workspace, dev),
+        _stream(stream, dev))
+    if rc:
+        raise CrcError(rc, "crc_group_choices")
     return offsets, rows, place
 
 
 def _group_weights(w, w_scale, dev: int):
-    """crc_group_weights of matrices w [N][n][k], or gate and up [N][2][n][k]."""
+    """(bytes of a crc_group_weights, N, n, k, glu) of matrices w [N][n][k], or gate and up
+    [N][2][n][k]."""
     import torch
-    kinds = {torch.bfloat16: BF16, torch.float8_e4m3fn: E4M3}
-    if w.dtype not in kinds:
+    shape, dtype = w.shape, w.dtype
+    if dtype is torch.bfloat16:
+        kind = BF16
+    elif dtype is torch.float8_e4m3fn:
+        kind = E4M3
+    else:
         raise ValueError("w must be bfloat16 or float8_e4m3fn")
-    if w.dim() not in (3, 4) or (w.dim() == 4 and w.shape[1] != 2):
+    dims = len(shape)
+    if dims not in (3, 4) or (dims == 4 and shape[1] != 2):
         raise ValueError("w has the shape [N][n][k], or [N][2][n][k] with gate and up")
     if w.get_device() != dev:
         raise ValueError(f"w lies on {w.device}, the other tensors on cuda:{dev}")
-    n, k = w.shape[-2:]
-    if w.stride()[1:] != ((k, 1) if w.dim() == 3 else (n * k, k, 1)):
+    N, n, k = shape[0], shape[-2], shape[-1]
+    stride = w.stride()
+    if stride[1:] != ((k, 1) if dims == 3 else (n * k, k, 1)):
         raise ValueError("an expert's matrices must be contiguous")
-    if (w_scale is None) != (w.dtype == torch.bfloat16):
+    if (w_scale is None) != (kind == BF16):
         raise ValueError("w_scale belongs to 8-bit matrices")
-    _check(w_scale, "w_scale", w.shape[:-1], torch.float32, dev, dense=False)
-    if w_scale is not None and w_scale.stride()[1:] != ((1,) if w.dim() == 3 else (n, 1)):
-        raise ValueError("an expert's scales must be contiguous")
-    return crc_group_weights(
-        N=w.shape[0], n=n, k=k, glu=int(w.dim() == 4), weight_type=kinds[w.dtype], reserved=0,
-        w_dev=w.data_ptr(), w_stride=w.stride(0) * w.element_size(), scale_dev=_ptr(w_scale),
-        scale_stride=0 if w_scale is None else w_scale.stride(0) * 4)
+    scale = scale_stride = 0
+    if w_scale is not None:
+        scale = _check(w_scale, "w_scale", shape[:-1], torch.float32, dev, False)
+        scale_stride, *inner = w_scale.stride()
+        if inner != ([1] if dims == 3 else [n, 1]):
+            raise ValueError("an expert's scales must be contiguous")
+    return (_GROUP_WEIGHTS.pack(N, n, k, dims - 3, kind, 0, w.data_ptr(),
+                                stride[0] * (2 if kind == BF16 else 1), scale, scale_stride * 4),
+            N, n, k, dims == 4)
 
 
 def group_matmul(x, w, offsets, rows=None, K: int = 1, x_scale=None, w_scale=None, y=None,
@@ -1006,21 +1023,21 @@ def group_matmul(x, w, offsets, rows=None, K: int = 1, x_scale=None, w_scale=Non
     x and w bf16, or float8_e4m3fn with x_scale [rows of x] and w_scale [N][n] ([N][2][n]).
     x may have strided rows, w strided experts."""
     import torch
-    dev, i32, f32 = _here(x, "x"), torch.int32, torch.float32
-    x_rows, k, ldx = _rows(x, "x")
-    c = _group_weights(w, w_scale, dev)
-    if x.dtype != w.dtype or k != c.k:
-        raise ValueError(f"x must be {w.dtype} with rows of {c.k}, got {x.dtype} {tuple(x.shape)}")
+    dev, i32 = _here(x, "x"), torch.int32
+    x_rows, d, ldx = _rows(x, "x")
+    c, N, n, k, _ = _group_weights(w, w_scale, dev)
+    if x.dtype is not w.dtype or d != k:
+        raise ValueError(f"x must be {w.dtype} with rows of {k}, got {x.dtype} {tuple(x.shape)}")
     if (x_scale is None) != (w_scale is None):
         raise ValueError("x_scale belongs to 8-bit rows")
     E = x_rows if rows is None else rows.numel()
     if y is None:
-        y = _new(stream, x.device, (E, c.n), torch.bfloat16)
+        y = _new(stream, x.device, (E, n), torch.bfloat16)
     rc = load().crc_group_matmul(
-        ctypes.byref(c), x.data_ptr(), ldx if x_rows > 1 else (k + 15) // 16 * 16, x_rows,
-        _check(x_scale, "x_scale", (x_rows,), f32, dev),
-        _check(offsets, "offsets", (c.N + 1,), i32, dev), _check(rows, "rows", (E,), i32, dev),
-        K, E, _check(y, "y", (E, c.n), torch.bfloat16, dev), _stream(stream, dev))
+        c, x.data_ptr(), ldx if x_rows > 1 else (d + 15) // 16 * 16, x_rows,
+        _check(x_scale, "x_scale", (x_rows,), torch.float32, dev),
+        _check(offsets, "offsets", (N + 1,), i32, dev), _check(rows, "rows", (E,), i32, dev),
+        K, E, _check(y, "y", (E, n), torch.bfloat16, dev), _stream(stream, dev))
     if rc:
         raise CrcError(rc, "crc_group_matmul")
     return y
@@ -1033,24 +1050,26 @@ def group_matmul_grad(dy, x, w, offsets, rows=None, K: int = 1, dx=None, dw=None
     import torch
     bf16, i32 = torch.bfloat16, torch.int32
     dev = _here(dy, "dy")
-    x_rows, k, ldx = _rows(x, "x")
-    c = _group_weights(w, None, dev)
-    if c.glu:
+    x_rows, _, ldx = _rows(x, "x")
+    c, N, n, k, glu = _group_weights(w, None, dev)
+    if glu:
         raise ValueError("w has the shape [N][n][k]: the gradient is that of the products alone")
     E = x_rows if rows is None else rows.numel()
     if want_dx and dx is None:
-        dx = _new(stream, dy.device, (E, c.k), bf16)
+        dx = _new(stream, dy.device, (E, k), bf16)
     if want_dw and dw is None:
-        dw = _new(stream, dy.device, (c.N, c.n, c.k), torch.float32)
-    if dw is not None and dw.dtype not in (torch.float32, bf16):
-        raise ValueError("dw must be float32 or bfloat16")
-    crc_group_matmul_grad(
-        c, _check(dy, "dy", (E, c.n), bf16, dev),
-        _check(x, "x", (x_rows, c.k), bf16, dev, dense=False), ldx, x_rows,
-        _check(offsets, "offsets", (c.N + 1,), i32, dev), _check(rows, "rows", (E,), i32, dev),
-        K, E, _check(dx, "dx", (E, c.k), bf16, dev),
-        None if dw is None else _check(dw, "dw", (c.N, c.n, c.k), dw.dtype, dev),
-        BF16 if dw is not None and dw.dtype == bf16 else F32, _stream(stream, dev))
+        dw = _new(stream, dy.device, (N, n, k), torch.float32)
+    kind = F32
+    if dw is not None and dw.dtype is bf16:
+        kind = BF16
+    rc = load().crc_group_matmul_grad(
+        c, _check(dy, "dy", (E, n), bf16, dev), _check(x, "x", (x_rows, k), bf16, dev, False), ldx,
+        x_rows, _check(offsets, "offsets", (N + 1,), i32, dev), _check(rows, "rows", (E,), i32, dev),
+        K, E, _check(dx, "dx", (E, k), bf16, dev),
+        _check(dw, "dw", (N, n, k), bf16 if kind == BF16 else torch.float32, dev), kind,
+        _stream(stream, dev))
+    if rc:
+        raise CrcError(rc, "crc_group_matmul_grad")
     return dx, dw
 
 
@@ -1065,10 +1084,12 @@ def sum_choices(y, place, gates=None, out=None, stream=None):
     (n, d), (M, K) = y.shape, place.shape
     if out is None:
         out = _new(stream, y.device, (M, d), bf16)
-    crc_sum_choices(_check(y, "y", (n, d), bf16, dev), n,
-                    _check(place, "place", (M, K), torch.int32, dev),
-                    _check(gates, "gates", (M, K), torch.float32, dev), M, K, d,
-                    _check(out, "out", (M, d), bf16, dev), _stream(stream, dev))
+    rc = load().crc_sum_choices(
+        _check(y, "y", (n, d), bf16, dev), n, _check(place, "place", (M, K), torch.int32, dev),
+        _check(gates, "gates", (M, K), torch.float32, dev), M, K, d,
+        _check(out, "out", (M, d), bf16, dev), _stream(stream, dev))
+    if rc:
+        raise CrcError(rc, "crc_sum_choices")
     return out
 
 
@@ -1088,12 +1109,13 @@ def sum_choices_grad(dout, place, gates=None, y=None, dy=None, dgates=None, y_ro
         dy = _new(stream, dout.device, (y_rows, d), bf16)
     if y is not None and dgates is None:
         dgates = _new(stream, dout.device, (M, K), f32)
-    crc_sum_choices_grad(_check(dout, "dout", (M, d), bf16, dev),
-                         _check(y, "y", (y_rows, d), bf16, dev), y_rows,
-                         _check(place, "place", (M, K), torch.int32, dev),
-                         _check(gates, "gates", (M, K), f32, dev), M, K, d,
-                         _check(dy, "dy", (y_rows, d), bf16, dev),
-                         _check(dgates, "dgates", (M, K), f32, dev), _stream(stream, dev))
+    rc = load().crc_sum_choices_grad(
+        _check(dout, "dout", (M, d), bf16, dev), _check(y, "y", (y_rows, d), bf16, dev), y_rows,
+        _check(place, "place", (M, K), torch.int32, dev), _check(gates, "gates", (M, K), f32, dev),
+        M, K, d, _check(dy, "dy", (y_rows, d), bf16, dev),
+        _check(dgates, "dgates", (M, K), f32, dev), _stream(stream, dev))
+    if rc:
+        raise CrcError(rc, "crc_sum_choices_grad")
     return dy, dgates
 
 
@@ -1107,19 +1129,24 @@ def quantize_rows4(x, group: int = 32, out4=None, scale=None, stream=None):
         raise ValueError("x must be bfloat16 with two dimensions or more")
     dev = _here(x, "x")
     *lead, n, k = x.shape
-    if x.dim() != 2 and not x.is_contiguous():
-        raise ValueError("x must be contiguous, or have two dimensions")
+    if len(lead):
+        if not x.is_contiguous():
+            raise ValueError("x must be contiguous, or have two dimensions")
+        ldx = k
+    else:
+        ldx = _rows(x, "x")[2]
     if group not in (32, 64, 128) or k % group:
         raise CrcError(CRC_EUNSUPPORTED, "crc_quantize_rows4")
-    _, _, ldx = _rows(x.reshape(-1, k) if x.dim() != 2 else x, "x")
     codes, scales = (*lead, n, k // 2), (*lead, k // group, n)
     if out4 is None:
         out4 = _new(stream, x.device, codes, torch.uint8)
     if scale is None:
         scale = _new(stream, x.device, scales, bf16)
-    crc_quantize_rows4(x.data_ptr(), ldx, math.prod(lead), n, k, group,
-                       _check(out4, "out4", codes, torch.uint8, dev),
-                       _check(scale, "scale", scales, bf16, dev), _stream(stream, dev))
+    rc = load().crc_quantize_rows4(x.data_ptr(), ldx, math.prod(lead), n, k, group,
+                                   _check(out4, "out4", codes, torch.uint8, dev),
+                                   _check(scale, "scale", scales, bf16, dev), _stream(stream, dev))
+    if rc:
+        raise CrcError(rc, "crc_quantize_rows4")
     return out4, scale
 
 
@@ -1134,38 +1161,38 @@ def matvec4(x, codes, scale, topk=None, expert_slot=None, y=None, N: int | None 
     import torch
     bf16 = torch.bfloat16
     dev = _here(x, "x")
-    if codes.dim() not in (3, 4) or (codes.dim() == 4 and codes.shape[1] != 2):
+    cs, ss = codes.shape, scale.shape
+    dims = len(cs)
+    if dims not in (3, 4) or (dims == 4 and cs[1] != 2):
         raise ValueError("codes has the shape [slots][n][k / 2], or [slots][2][n][k / 2]")
-    slots, n, k = codes.shape[0], codes.shape[-2], 2 * codes.shape[-1]
-    if scale.dim() != codes.dim() or scale.shape[-2] < 1 or k % scale.shape[-2]:
+    slots, n, k = cs[0], cs[-2], 2 * cs[-1]
+    groups = ss[-2] if len(ss) == dims else 0
+    if groups < 1 or k % groups:
         raise ValueError("scale has the shape [slots][k / group][n], or [slots][2][k / group][n]")
-    groups = scale.shape[-2]
-    lead = tuple(codes.shape[:-2])
-    _check(codes, "codes", (*lead, n, k // 2), torch.uint8, dev, dense=False)
-    _check(scale, "scale", (*lead, groups, n), bf16, dev, dense=False)
-    inner = (lambda r, c: (c, 1) if len(lead) == 1 else (r * c, c, 1))
-    if codes.stride()[1:] != inner(n, k // 2) or scale.stride()[1:] != inner(groups, n):
+    pc = _check(codes, "codes", cs, torch.uint8, dev, False)
+    ps = _check(scale, "scale", (*cs[:-2], groups, n), bf16, dev, False)
+    (codes_stride, *ci), (scale_stride, *si) = codes.stride(), scale.stride()
+    if dims == 3:
+        dense = ci == [k // 2, 1] and si == [n, 1]
+    else:
+        dense = ci == [n * k // 2, k // 2, 1] and si == [groups * n, n, 1]
+    if not dense:
         raise ValueError("a slot's codes and scales must be contiguous")
     if N is None:
         N = expert_slot.shape[0] if expert_slot is not None else slots
-    M = x.shape[0]
-    K = 1 if topk is None else topk.shape[-1]
-    per_choice = x.dim() == 3
-    if per_choice:
-        _check(x, "x", (M, K, k), bf16, dev)
-        ldx = k
+    M, K = x.shape[0], 1
+    if topk is not None:
+        K = topk.shape[-1]
+    if x.dim() == 3:
+        px, ldx, each = _check(x, "x", (M, K, k), bf16, dev), k, 1
     else:
-        _check(x, "x", (M, k), bf16, dev, dense=False)
-        ldx = _rows(x, "x")[2]
+        px, ldx, each = _check(x, "x", (M, k), bf16, dev, False), _rows(x, "x")[2], 0
     if y is None:
         y = _new(stream, x.device, (M, K, n), bf16)
-    c = crc_matvec4_weights(
-        N=N, n=n, k=k, slots=slots, glu=int(len(lead) == 2), group=k // groups, reserved=0,
-        codes_dev=codes.data_ptr(), scale_dev=scale.data_ptr(), codes_stride=codes.stride(0),
-        scale_stride=scale.stride(0) * 2,
-        expert_slot_dev=_check(expert_slot, "expert_slot", (N,), torch.int32, dev))
-    rc = load().crc_matvec4(ctypes.byref(c), x.data_ptr(), ldx, int(per_choice),
-                            _check(topk, "topk", (M, K), torch.uint8, dev), M, K,
+    c = _MATVEC4_WEIGHTS.pack(N, n, k, slots, dims - 3, k // groups, 0, pc, ps, codes_stride,
+                              scale_stride * 2,
+                              _check(expert_slot, "expert_slot", (N,), torch.int32, dev) or 0)
+    rc = load().crc_matvec4(c, px, ldx, each, _check(topk, "topk", (M, K), torch.uint8, dev), M, K,
                             _check(y, "y", (M, K, n), bf16, dev), _stream(stream, dev))
     if rc:
         raise CrcError(rc, "crc_matvec4")

@@ -222,7 +222,7 @@ int crc_group_matmul_grad(const crc_group_weights* w, const uint16_t* dy_dev,
         if (rc) return rc;
     }
     if (!dw_dev) return CRC_OK;
-    CUtensorMap mdy, mx, mdw;
+    CUtensorMap mdy, mx, mdy16, mx16, mdw;
     const bool f32 = dw_type == CRC_F32;
     const cuuint64_t es = f32 ? 4 : 2;
     const cuuint64_t dims[3] = {(cuuint64_t)v.k, (cuuint64_t)v.n, (cuuint64_t)v.N};
@@ -230,6 +230,8 @@ int crc_group_matmul_grad(const crc_group_weights* w, const uint16_t* dy_dev,
     const cuuint32_t box[3] = {f32 ? 32u : 64u, 32, 1};
     if (!rows_map(&mdy, false, dy_dev, E, v.n, v.n, kGwRows) ||
         !rows_map(&mx, false, x_dev, x_rows, v.k, x_stride, rows_dev ? 1 : kGwRows) ||
+        !rows_map(&mdy16, false, dy_dev, E, v.n, v.n, 16) ||
+        !rows_map(&mx16, false, x_dev, x_rows, v.k, x_stride, 16) ||
         !encode(&mdw, f32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : kBf16Map, 3, dw_dev, dims, strides,
                 box))
         return CRC_ECUDA;
@@ -251,7 +253,7 @@ int crc_group_matmul_grad(const crc_group_weights* w, const uint16_t* dy_dev,
     {
         ProfScope prof(CRC_KERNEL_GROUP, st);
         e = launch_dependent(kern, dim3((unsigned)sm_count()), kGwThreads, smem, st, 1, mdy, mx,
-                             mdw, a);
+                             mdy16, mx16, mdw, a);
     }
     note_launch();
     return cuda_status(e);

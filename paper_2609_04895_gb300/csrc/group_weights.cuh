@@ -4,7 +4,8 @@
 // block is 64 rows of dy and x as they are in memory, 128 columns of dy (the 128 rows of
 // tcgen05.mma's A) and 256 of x (its N).  The last block of an expert holds rows of the next
 // one: those up to the next 16 are zeroed in shared memory (both operands: a product with
-// another expert's infinity would not be zero), and the steps behind them are left out.
+// another expert's infinity would not be zero), and the steps behind them are left out, as
+// their loads are.
 //
 // What bounds it: an expert has some hundred rows, so a tile's 32768 sums are written after a
 // few blocks, 128 KB in fp32; the writes of dW are most of its bytes.  Tiles leave through
@@ -42,6 +43,11 @@ struct GroupGradSmem {
 };
 static_assert(GroupGradSmem::bytes() + sizeof(GroupPlan) < 232448, "shared memory");
 
+// Rows of a block that has `left` of them, to the next 16.
+__device__ __forceinline__ int round16(int left) {
+    return left >= kGwRows ? kGwRows : (left + 15) / 16 * 16;
+}
+
 // Rows `tail` .. of a block's six pieces of 64 columns, to the next 16: zeros.
 __device__ __forceinline__ void clear_rows(uint8_t* stage, int tail, int lane) {
     const int end = (tail + 15) / 16 * 16, pieces = (end - tail) * 8;      // of 16 bytes
@@ -58,6 +64,8 @@ template <bool F32>
 __global__ void __launch_bounds__(kGwThreads, 1)
     group_weights_grad_kernel(const __grid_constant__ CUtensorMap mdy,
                               const __grid_constant__ CUtensorMap mx,
+                              const __grid_constant__ CUtensorMap mdy16,
+                              const __grid_constant__ CUtensorMap mx16,
                               const __grid_constant__ CUtensorMap mdw, GroupGradArgs a) {
     extern __shared__ __align__(1024) uint8_t smem_raw[];
     __shared__ GroupPlan plan;
@@ -85,6 +93,8 @@ __global__ void __launch_bounds__(kGwThreads, 1)
         fence_mbar_init();
         tma_prefetch_desc(&mdy);
         tma_prefetch_desc(&mx);
+        tma_prefetch_desc(&mdy16);
+        tma_prefetch_desc(&mx16);
         tma_prefetch_desc(&mdw);
     }
     if (warp == 1) {
@@ -119,12 +129,24 @@ __global__ void __launch_bounds__(kGwThreads, 1)
                     break;
                 }
                 uint8_t* s = smem + stage * kGwStage + (is_x ? kGwA : 0);
-                if (lead) mbar_arrive_expect_tx(&full_bar[stage], is_x ? kGwB : kGwA);
+                const int some = round16(count - r);
+                if (lead)
+                    mbar_arrive_expect_tx(&full_bar[stage], (is_x ? kGwN : kGwM) / 64 * some * 128);
+                if (some == kGwRows) {
 #pragma unroll
-                for (int c = 0; c < kGwN / 64; ++c)
-                    if (is_x || c < kGwM / 64)
-                        tma_load_2d_by(lead, s + c * kGwChunk, is_x ? &mx : &mdy,
-                                       &full_bar[stage], col + c * 64, row0 + r, pol);
+                    for (int c = 0; c < kGwN / 64; ++c)
+                        if (is_x || c < kGwM / 64)
+                            tma_load_2d_by(lead, s + c * kGwChunk, is_x ? &mx : &mdy,
+                                           &full_bar[stage], col + c * 64, row0 + r, pol);
+                } else {
+                    for (int q = 0; q < some; q += 16)
+#pragma unroll
+                        for (int c = 0; c < kGwN / 64; ++c)
+                            if (is_x || c < kGwM / 64)
+                                tma_load_2d_by(lead, s + c * kGwChunk + q * 128,
+                                               is_x ? &mx16 : &mdy16, &full_bar[stage],
+                                               col + c * 64, row0 + r + q, pol);
+                }
                 ++issued;
                 if (++stage == kGwStages) {
                     stage = 0;
@@ -173,14 +195,17 @@ __global__ void __launch_bounds__(kGwThreads, 1)
                     latch_error(a.r.err, CRC_ETIMEOUT);
                     break;
                 }
-                if (warp == 8 && lead) mbar_arrive_expect_tx(&full_bar[stage], kGwB);
+                const int some = round16(count - r);
+                if (warp == 8 && lead)
+                    mbar_arrive_expect_tx(&full_bar[stage], kGwN / 64 * some * 128);
                 uint8_t* s = smem + stage * kGwStage + kGwA + at * 128;
+                if (at < some)
 #pragma unroll
-                for (int c = 0; c < kGwN / 64; ++c)
+                    for (int c = 0; c < kGwN / 64; ++c)
 #pragma unroll
-                    for (int q = 0; q < 2; ++q)
-                        tma_gather4_by(lead, s + c * kGwChunk + q * 512, &mx, &full_bar[stage],
-                                       col + c * 64, src[q], pol);
+                        for (int q = 0; q < 2; ++q)
+                            tma_gather4_by(lead, s + c * kGwChunk + q * 512, &mx, &full_bar[stage],
+                                           col + c * 64, src[q], pol);
                 if (++stage == kGwStages) {
                     stage = 0;
                     phase ^= 1;

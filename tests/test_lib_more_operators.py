@@ -339,10 +339,14 @@ def test_strides_and_slots_reach_the_library(P):
     w = OnGpu(slots.as_strided((4, 32, 64), (3 * 32 * 64, 64, 1)))
     P.group_matmul(big, w, new(5, dtype=I), y=new(6, 32))
     args = P.calls[-1][1]
-    assert args[2] == 96 and args[0]._obj.w_stride == 3 * 32 * 64 * 2
+    w = P.crc.crc_group_weights.from_buffer_copy(args[0])
+    assert args[2] == 96 and w.w_stride == 3 * 32 * 64 * 2
+    assert (w.N, w.n, w.k, w.glu, w.weight_type, w.scale_dev) == (4, 32, 64, 0, 1, None)
     P.matvec4(OnGpu(torch.zeros((5, 96), dtype=B)[:, :64]), new(4, 2, 8, 32, dtype=U),
               new(4, 2, 2, 8), topk=new(5, 2, dtype=U), expert_slot=new(9, dtype=I), y=new(5, 2, 8))
-    c, args = P.calls[-1][1][0]._obj, P.calls[-1][1]
+    args = P.calls[-1][1]
+    c = P.crc.crc_matvec4_weights.from_buffer_copy(args[0])
+    assert c.expert_slot_dev and c.codes_stride == 2 * 8 * 32 and c.scale_stride == 2 * 2 * 8 * 2
     assert (c.N, c.slots, c.glu, c.group, args[2], args[3]) == (9, 4, 1, 32, 96, 0)
     P.matvec4(new(5, 2, 64), new(4, 8, 32, dtype=U), new(4, 2, 8), topk=new(5, 2, dtype=U),
               y=new(5, 2, 8))
