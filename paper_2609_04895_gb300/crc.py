@@ -952,6 +952,30 @@ class MoeLayer:
             raise CrcError(rc, "crc_moe_layer")
         return out
 
+    def prompt(self, x, topk, gates=None, out=None, stream=None):
+        """out [M][d] of any number of tokens x [M][d] (bf16, rows may be strided) whose choices
+        topk uint8 [M][K] and gates fp32 [M][K] (None: 1) are given: group_choices, the two
+        grouped products and sum_choices.  A token's id of N or more has no expert.  Every
+        expert e has to lie in slot e (no expert_slot).  With 8-bit experts x and the rows
+        between the products are brought to 8 bits, a scale a row."""
+        gate_up, down, _, slots, s13, s2 = self.tensors
+        if slots is not None:
+            raise ValueError("prompts want every expert in its own slot: no expert_slot map")
+        if s13 is None:
+            x8, xs = x, None
+        else:
+            x8, xs = quantize_rows(x, stream=stream)
+        gate_up, down = gate_up[:self.N], down[:self.N]
+        offsets, rows, place = group_choices(topk, self.N, stream=stream)
+        h = group_matmul(x8, gate_up, offsets, rows=rows, K=topk.shape[1], x_scale=xs,
+                         w_scale=None if s13 is None else s13[:self.N], stream=stream)
+        hs = None
+        if s2 is not None:
+            h, hs = quantize_rows(h, stream=stream)
+        y = group_matmul(h, down, offsets, x_scale=hs,
+                         w_scale=None if s2 is None else s2[:self.N], stream=stream)
+        return sum_choices(y, place, gates=gates, out=out, stream=stream)
+
 
 def group_choices(topk, N: int, offsets=None, rows=None, place=None, workspace=None,
                   stream=None):

@@ -349,13 +349,15 @@ __global__ void __launch_bounds__(kThreads, kCtas)
         tma_prefetch_desc(&ms);
     }
     pdl_begin();
+    // (this thread's first choice and slot are asked for together)
+    const int id0 = a.topk && (int)threadIdx.x < a.E ? a.topk[threadIdx.x] : 0;
     for (int e = threadIdx.x; e < a.N; e += kThreads) {
         const int slot = a.slot ? a.slot[e] : e;
         order.slot[e] = slot >= 0 && slot < a.slots ? slot : -1;
     }
     __syncthreads();
     const auto bin_of = [&](int c) {
-        const int id = a.topk ? a.topk[c] : 0;
+        const int id = c == (int)threadIdx.x ? id0 : a.topk ? a.topk[c] : 0;
         return id < a.N && order.slot[id] >= 0 ? id : a.N;
     };
     for (int c = threadIdx.x; c < a.E; c += kThreads) atomicAdd(&order.next[bin_of(c)], 1);

@@ -378,6 +378,36 @@ def test_layer_agrees_with_the_decode_layer(P):
     assert e <= 4 * 2.0 ** -9 / 3 ** 0.5
 
 
+@pytest.mark.parametrize("w8", [False, True])
+def test_a_decode_layers_prompt(P, w8):
+    """MoeLayer.prompt against the same layer's call for as many tokens as that takes, and more
+    tokens than it takes; a slot's matrices one after the other."""
+    M, N, K, d, f = 1024, 32, 4, 512, 256
+    a = layer_inputs(M, N, K, d, f, 2)
+    g13, g2, s13, s2 = a["gate_up"], a["down"], None, None
+    if w8:
+        (g13, s13), (g2, s2) = P.quantize_rows(g13), P.quantize_rows(g2)
+    slots = torch.zeros((N, 3 * f * d), dtype=g13.dtype, device="cuda")
+    slots[:, :2 * f * d], slots[:, 2 * f * d:] = g13.flatten(1), g2.flatten(1)
+    lay = P.MoeLayer(*P.expert_views(slots, f, d), K=K, N=N, gate_up_scale=s13, down_scale=s2)
+    scores = torch.softmax(torch.randn((M, N), device="cuda") * 2, -1)
+    topk = torch.empty((M, K), dtype=torch.uint8, device="cuda")
+    gates = torch.empty((M, K), device="cuda")
+    want = lay(a["x"], scores=scores, topk=topk, gates=gates).double()
+    out = lay.prompt(a["x"], topk, gates)
+    # bf16: three roundings of some 2^-9 / sqrt(3) each in the mean square (h, y, out) and one;
+    # 8 bits: x and h have four significant bits, an error of at most 2^-4 of each element
+    # (2^-4 / sqrt(3) in the mean square), where the call keeps eight and more
+    e = (out.double() - want).norm() / want.norm()
+    assert e <= (3 * 2.0 ** -4 / 3 ** 0.5 if w8 else 4 * 2.0 ** -9 / 3 ** 0.5)
+    many = lay.prompt(a["x"].repeat(3, 1), topk.repeat(3, 1), gates.repeat(3, 1))
+    assert many.shape == (3 * M, d) and torch.equal(many[M:2 * M], out)
+    slot = torch.arange(N, dtype=torch.int32, device="cuda")
+    with pytest.raises(ValueError):
+        P.MoeLayer(*P.expert_views(slots, f, d), K=K, expert_slot=slot, gate_up_scale=s13,
+                   down_scale=s2).prompt(a["x"], topk, gates)
+
+
 def test_layer_captured_twice_and_on_other_streams(P):
     """Two graphs of the layer replayed at once on their streams, with new data each time."""
     N, K = 64, 4
