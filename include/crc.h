@@ -579,7 +579,7 @@ int crc_moe_layer(const crc_moe *m, const uint16_t *x_dev, int64_t x_stride, con
  * padded token's 255): place[c] = -1, and rows[offsets[N]] .. rows[M K - 1] = -1.
  *   topk_dev   uint8 [M][K], e.g. crc_trace's or crc_moe_layer's
  *   offsets_dev  int32 [N + 1];  rows_dev int32 [M K];  place_dev int32 [M][K] or NULL
- *   workspace_dev  crc_group_choices_workspace_bytes(M, K, N) bytes (0 for up to 4096
+ *   workspace_dev  crc_group_choices_workspace_bytes(M, K, N) bytes (0 for up to 2048
  *              choices), 256-byte aligned; calls that may overlap need one each
  * N <= 256, K <= 32, M K <= 2^30, else CRC_EUNSUPPORTED.  M = 0 sets offsets to 0. */
 size_t crc_group_choices_workspace_bytes(int32_t M, int32_t K, int32_t N);

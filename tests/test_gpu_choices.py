@@ -41,7 +41,7 @@ def check_order(P, topk, N, **kw):
 
 
 # one CTA, its last size and the first of two launches; more than a CTA ranks at a time
-SIZES = [(1, 1), (1, 32), (31, 1), (33, 1), (37, 4), (1023, 3), (1024, 4), (1025, 4), (4096, 1),
+SIZES = [(1, 1), (1, 32), (31, 1), (33, 1), (37, 4), (2048, 1), (2049, 1), (1023, 3), (1024, 4), (1025, 4), (4096, 1),
          (4097, 1), (2049, 2), (9001, 7), (32768, 8), (160001, 7)]
 
 

@@ -41,7 +41,7 @@ def test_choices_arguments(C, bad, code):
 
 def test_choices_workspace(C):
     need = C.crc_group_choices_workspace_bytes
-    assert need(512, 8, 128) == 0 and need(513, 8, 128) >= 129 * 4
+    assert need(256, 8, 128) == 0 and need(257, 8, 128) >= 129 * 4
     assert need(-1, 8, 128) == 0 and need(4096, 8, 257) == 0
     assert need(1 << 25, 32, 256) < 1 << 20              # it does not grow with the choices
 
