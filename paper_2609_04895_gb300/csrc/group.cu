@@ -23,6 +23,8 @@ bool encode(CUtensorMap* m, CUtensorMapDataType type, int rank, const void* base
                       CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+constexpr int kSingleRows = 48, kShortRows = 8;
+
 constexpr CUtensorMapDataType kBf16Map = CU_TENSOR_MAP_DATA_TYPE_BFLOAT16;
 
 // `rows` rows of x in order; 1: four gathered.
@@ -56,13 +58,19 @@ bool glu_map(CUtensorMap* m, const crc_group_weights& w) {
                   box);
 }
 
-template <bool W8, bool GLU, bool TW>
-int launch_products(const CUtensorMap& mw, const CUtensorMap& mx, const GroupArgs& a,
-                    cudaStream_t st) {
-    auto kern = group_matmul_kernel<W8, GLU, TW>;
+template <bool W8, bool GLU, bool TW, bool Pair>
+int launch_products_on(const CUtensorMap& mw, const CUtensorMap& mx, GroupArgs& a,
+                       cudaStream_t st) {
+    auto kern = group_matmul_kernel<W8, GLU, TW, Pair>;
     constexpr size_t smem = GroupSmem::bytes();
-    static PerDevice resident;                 // pairs that fit the GPU at once
+    constexpr int kRows = (GLU ? 64 : 128) * (Pair ? 2 : 1);      // columns of y of a tile
+    a.ftiles = (a.out + kRows - 1) / kRows;
+    static PerDevice resident;                 // CTAs or pairs that fit the GPU at once
     const int fit = resident.get(current_device(), [&] {
+        if (cuda_status(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                             (int)smem)))
+            return 0;
+        if (!Pair) return sm_count() > 0 ? sm_count() : -1;
         cudaLaunchAttribute at[1];
         at[0].id = cudaLaunchAttributeClusterDimension;
         at[0].val.clusterDim.x = 2;
@@ -75,20 +83,33 @@ int launch_products(const CUtensorMap& mw, const CUtensorMap& mx, const GroupArg
         c.attrs = at;
         c.numAttrs = 1;
         int n = 0;
-        if (cuda_status(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                             (int)smem)) ||
-            cuda_status(cudaOccupancyMaxActiveClusters(&n, (const void*)kern, &c)))
-            return 0;
+        if (cuda_status(cudaOccupancyMaxActiveClusters(&n, (const void*)kern, &c))) return 0;
         return n > 0 ? n : -1;
     });
     if (fit < 1) return CRC_ECUDA;
     cudaError_t e;
     {
         ProfScope prof(CRC_KERNEL_GROUP, st);
-        e = launch_dependent(kern, dim3((unsigned)(2 * fit)), kGmThreads, smem, st, 2, mw, mx, a);
+        e = launch_dependent(kern, dim3((unsigned)(Pair ? 2 * fit : fit)), kGmThreads, smem, st,
+                             Pair ? 2 : 1, mw, mx, a);
     }
     note_launch();
     return cuda_status(e);
+}
+
+template <bool W8, bool GLU, bool TW>
+int launch_products(const CUtensorMap& mw, const CUtensorMap& mx, GroupArgs& a, cudaStream_t st) {
+    // CTAs by themselves for few rows an expert, in order, or gathered from short rows.  Us, by
+    // themselves / pairs: the second product of 60 tokens of the 32-expert shape (7 rows an
+    // expert) 68.6 / 76.7, in 8 bits 36.9 / 41.8, its gradient's rows 66.2 / 73.4; of 200 tokens
+    // of the 128-expert shape 58.0 / 58.9, 8 bits 32.6 / 41.8; with 62 rows an expert 71.8 / 69.9,
+    // with 93 53.7 / 53.1, gradient 51.3 / 51.8.  The first product, gathered: 60 tokens of the
+    // 32-expert shape in 8 bits 80.9 / 72.9, one token 25.5 / 20.2, but 5.5 / 7.4 for 300 tokens
+    // of d = 256.
+    const bool single = (long long)a.r.E <= (long long)kSingleRows * a.r.N &&
+                        (!a.r.rows || a.kblocks <= kShortRows);
+    return single ? launch_products_on<W8, GLU, TW, false>(mw, mx, a, st)
+                  : launch_products_on<W8, GLU, TW, true>(mw, mx, a, st);
 }
 
 int check_weights(const crc_group_weights* w) {
@@ -172,7 +193,6 @@ int crc_group_matmul(const crc_group_weights* w, const void* x_dev, int64_t x_st
     a.ws_stride = w->scale_stride / 4;
     a.kblocks = (w->k + (w8 ? 127 : 63)) / (w8 ? 128 : 64);
     a.out = w->n;
-    a.ftiles = (w->n + (w->glu ? 127 : 255)) / (w->glu ? 128 : 256);
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     if (w8)
         return w->glu ? launch_products<true, true, false>(mw, mx, a, st)
@@ -217,7 +237,6 @@ int crc_group_matmul_grad(const crc_group_weights* w, const uint16_t* dy_dev,
         a.y = dx_dev;
         a.kblocks = (v.n + 63) / 64;
         a.out = v.k;
-        a.ftiles = (v.k + 255) / 256;
         rc = launch_products<false, false, true>(mw, mdy, a, st);
         if (rc) return rc;
     }

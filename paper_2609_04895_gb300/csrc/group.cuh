@@ -47,35 +47,25 @@ __device__ __forceinline__ uint32_t elected() {
 // Issued by the lane whose `lead` is set, in code that the whole warp runs: the descriptors
 // stay in uniform registers, where the instruction wants them.  (In a branch of one lane each
 // MMA took 85 ns, whatever its columns.)
-template <bool W8>
-__device__ __forceinline__ void umma_pair_by(uint32_t d_tmem, uint64_t adesc, uint64_t bdesc,
-                                             uint32_t idesc, uint32_t accumulate, uint32_t lead) {
-    if constexpr (W8)
-        asm volatile(
-            "{\n\t.reg .pred p, e;\n\t"
-            "setp.ne.b32 p, %4, 0;\n\t"
-            "setp.ne.b32 e, %5, 0;\n\t"
-            "@e tcgen05.mma.cta_group::2.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}\n" ::"r"(d_tmem),
-            "l"(adesc), "l"(bdesc), "r"(idesc), "r"(accumulate), "r"(lead)
-            : "memory");
+template <bool W8, bool Pair>
+__device__ __forceinline__ void umma_by(uint32_t d_tmem, uint64_t adesc, uint64_t bdesc,
+                                        uint32_t idesc, uint32_t accumulate, uint32_t lead) {
+#define CRC_UMMA(group, kind)                                                                 \
+    asm volatile("{\n\t.reg .pred p, e;\n\t"                                                 \
+                 "setp.ne.b32 p, %4, 0;\n\t"                                                  \
+                 "setp.ne.b32 e, %5, 0;\n\t"                                                  \
+                 "@e tcgen05.mma." group "." kind " [%0], %1, %2, %3, p;\n\t}\n" ::"r"(d_tmem), \
+                 "l"(adesc), "l"(bdesc), "r"(idesc), "r"(accumulate), "r"(lead)               \
+                 : "memory")
+    if constexpr (Pair && W8)
+        CRC_UMMA("cta_group::2", "kind::f8f6f4");
+    else if constexpr (Pair)
+        CRC_UMMA("cta_group::2", "kind::f16");
+    else if constexpr (W8)
+        CRC_UMMA("cta_group::1", "kind::f8f6f4");
     else
-        asm volatile(
-            "{\n\t.reg .pred p, e;\n\t"
-            "setp.ne.b32 p, %4, 0;\n\t"
-            "setp.ne.b32 e, %5, 0;\n\t"
-            "@e tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}\n" ::"r"(d_tmem),
-            "l"(adesc), "l"(bdesc), "r"(idesc), "r"(accumulate), "r"(lead)
-            : "memory");
-}
-__device__ __forceinline__ void umma_bf16_by(uint32_t d_tmem, uint64_t adesc, uint64_t bdesc,
-                                             uint32_t idesc, uint32_t accumulate, uint32_t lead) {
-    asm volatile(
-        "{\n\t.reg .pred p, e;\n\t"
-        "setp.ne.b32 p, %4, 0;\n\t"
-        "setp.ne.b32 e, %5, 0;\n\t"
-        "@e tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}\n" ::"r"(d_tmem),
-        "l"(adesc), "l"(bdesc), "r"(idesc), "r"(accumulate), "r"(lead)
-        : "memory");
+        CRC_UMMA("cta_group::1", "kind::f16");
+#undef CRC_UMMA
 }
 __device__ __forceinline__ void commit_pair_by(uint64_t* bar, uint32_t lead) {
     asm volatile(
@@ -96,6 +86,14 @@ __device__ __forceinline__ void commit_by(uint64_t* bar, uint32_t lead) {
         : "memory");
 }
 
+template <bool Pair>
+__device__ __forceinline__ void commit_of(uint64_t* bar, uint32_t lead) {
+    if constexpr (Pair)
+        commit_pair_by(bar, lead);
+    else
+        commit_by(bar, lead);
+}
+
 // ---------------------------------------------------------------------------
 // TMA
 // ---------------------------------------------------------------------------
@@ -104,79 +102,55 @@ __device__ __forceinline__ uint64_t l2_normal_policy() {
     asm volatile("createpolicy.fractional.L2::evict_normal.b64 %0, 1.0;" : "=l"(p));
     return p;
 }
-// (bar: a shared::cluster address, of either CTA of the pair.  Issued by the lane whose `lead` is
+// (bar: a shared::cluster address, with Pair of either CTA.  Issued by the lane whose `lead` is
 // set, in code that the whole warp runs.)
-__device__ __forceinline__ void tma_load_5d_pair_by(uint32_t lead, void* dst,
-                                                    const CUtensorMap* map, uint32_t bar, int c0,
-                                                    int c1, int c2, int c3, int c4,
-                                                    uint64_t policy) {
-    asm volatile(
-        "{\n\t.reg .pred e;\n\tsetp.ne.b32 e, %9, 0;\n\t"
-        "@e cp.async.bulk.tensor.5d.cta_group::2.shared::cluster.global.tile"
-        ".mbarrier::complete_tx::bytes.L2::cache_hint [%0], [%1, {%2, %3, %4, %5, %6}], [%7], "
-        "%8;\n\t}" ::"r"(smem_u32(dst)),
-        "l"(reinterpret_cast<uint64_t>(map)), "r"(c0), "r"(c1), "r"(c2), "r"(c3), "r"(c4), "r"(bar),
-        "l"(policy), "r"(lead)
-        : "memory");
+#define CRC_TMA_LOAD(dim, group, mode, coords, ...)                                        \
+    asm volatile("{\n\t.reg .pred e;\n\tsetp.ne.b32 e, %3, 0;\n\t"                          \
+                 "@e cp.async.bulk.tensor." dim group ".shared::cluster.global." mode          \
+                 ".mbarrier::complete_tx::bytes.L2::cache_hint [%0], [%1, " coords "], [%2], " \
+                 "%4;\n\t}" ::"r"(smem_u32(dst)),                                             \
+                 "l"(reinterpret_cast<uint64_t>(map)), "r"(bar), "r"(lead), "l"(policy),      \
+                 __VA_ARGS__                                                                  \
+                 : "memory")
+template <bool Pair>
+__device__ __forceinline__ void tma_load_5d_of(uint32_t lead, void* dst, const CUtensorMap* map,
+                                               uint32_t bar, int c0, int c1, int c2, int c3,
+                                               int c4, uint64_t policy) {
+    if constexpr (Pair)
+        CRC_TMA_LOAD("5d", ".cta_group::2", "tile", "{%5, %6, %7, %8, %9}", "r"(c0), "r"(c1),
+                     "r"(c2), "r"(c3), "r"(c4));
+    else
+        CRC_TMA_LOAD("5d", "", "tile", "{%5, %6, %7, %8, %9}", "r"(c0), "r"(c1), "r"(c2),
+                     "r"(c3), "r"(c4));
 }
-__device__ __forceinline__ void tma_load_3d_pair_by(uint32_t lead, void* dst,
-                                                    const CUtensorMap* map, uint32_t bar, int c0,
-                                                    int c1, int c2, uint64_t policy) {
-    asm volatile(
-        "{\n\t.reg .pred e;\n\tsetp.ne.b32 e, %7, 0;\n\t"
-        "@e cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.tile"
-        ".mbarrier::complete_tx::bytes.L2::cache_hint [%0], [%1, {%2, %3, %4}], [%5], %6;\n\t}" ::"r"(
-            smem_u32(dst)),
-        "l"(reinterpret_cast<uint64_t>(map)), "r"(c0), "r"(c1), "r"(c2), "r"(bar), "l"(policy),
-        "r"(lead)
-        : "memory");
+template <bool Pair>
+__device__ __forceinline__ void tma_load_3d_of(uint32_t lead, void* dst, const CUtensorMap* map,
+                                               uint32_t bar, int c0, int c1, int c2,
+                                               uint64_t policy) {
+    if constexpr (Pair)
+        CRC_TMA_LOAD("3d", ".cta_group::2", "tile", "{%5, %6, %7}", "r"(c0), "r"(c1), "r"(c2));
+    else
+        CRC_TMA_LOAD("3d", "", "tile", "{%5, %6, %7}", "r"(c0), "r"(c1), "r"(c2));
 }
-__device__ __forceinline__ void tma_load_2d_pair_by(uint32_t lead, void* dst,
-                                                    const CUtensorMap* map, uint32_t bar, int c0,
-                                                    int c1, uint64_t policy) {
-    asm volatile(
-        "{\n\t.reg .pred e;\n\tsetp.ne.b32 e, %6, 0;\n\t"
-        "@e cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.tile"
-        ".mbarrier::complete_tx::bytes.L2::cache_hint [%0], [%1, {%2, %3}], [%4], %5;\n\t}" ::"r"(
-            smem_u32(dst)),
-        "l"(reinterpret_cast<uint64_t>(map)), "r"(c0), "r"(c1), "r"(bar), "l"(policy), "r"(lead)
-        : "memory");
+template <bool Pair>
+__device__ __forceinline__ void tma_load_2d_of(uint32_t lead, void* dst, const CUtensorMap* map,
+                                               uint32_t bar, int c0, int c1, uint64_t policy) {
+    if constexpr (Pair)
+        CRC_TMA_LOAD("2d", ".cta_group::2", "tile", "{%5, %6}", "r"(c0), "r"(c1));
+    else
+        CRC_TMA_LOAD("2d", "", "tile", "{%5, %6}", "r"(c0), "r"(c1));
 }
 // Four rows of a matrix, columns c0 on (the map's box is one row high).
-__device__ __forceinline__ void tma_gather4_pair_by(uint32_t lead, void* dst,
-                                                    const CUtensorMap* map, uint32_t bar, int c0,
-                                                    const int (&r)[4], uint64_t policy) {
-    asm volatile(
-        "{\n\t.reg .pred e;\n\tsetp.ne.b32 e, %9, 0;\n\t"
-        "@e cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.tile::gather4"
-        ".mbarrier::complete_tx::bytes.L2::cache_hint [%0], [%1, {%2, %3, %4, %5, %6}], [%7], "
-        "%8;\n\t}" ::"r"(smem_u32(dst)),
-        "l"(reinterpret_cast<uint64_t>(map)), "r"(c0), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]),
-        "r"(bar), "l"(policy), "r"(lead)
-        : "memory");
-}
-__device__ __forceinline__ void tma_gather4_by(uint32_t lead, void* dst, const CUtensorMap* map,
-                                               uint64_t* bar, int c0, const int (&r)[4],
+template <bool Pair>
+__device__ __forceinline__ void tma_gather4_of(uint32_t lead, void* dst, const CUtensorMap* map,
+                                               uint32_t bar, int c0, const int (&r)[4],
                                                uint64_t policy) {
-    asm volatile(
-        "{\n\t.reg .pred e;\n\tsetp.ne.b32 e, %9, 0;\n\t"
-        "@e cp.async.bulk.tensor.2d.shared::cluster.global.tile::gather4"
-        ".mbarrier::complete_tx::bytes.L2::cache_hint [%0], [%1, {%2, %3, %4, %5, %6}], [%7], "
-        "%8;\n\t}" ::"r"(smem_u32(dst)),
-        "l"(reinterpret_cast<uint64_t>(map)), "r"(c0), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]),
-        "r"(smem_u32(bar)), "l"(policy), "r"(lead)
-        : "memory");
-}
-__device__ __forceinline__ void tma_load_2d_by(uint32_t lead, void* dst, const CUtensorMap* map,
-                                               uint64_t* bar, int c0, int c1, uint64_t policy) {
-    asm volatile(
-        "{\n\t.reg .pred e;\n\tsetp.ne.b32 e, %6, 0;\n\t"
-        "@e cp.async.bulk.tensor.2d.shared::cluster.global.tile"
-        ".mbarrier::complete_tx::bytes.L2::cache_hint [%0], [%1, {%2, %3}], [%4], %5;\n\t}" ::"r"(
-            smem_u32(dst)),
-        "l"(reinterpret_cast<uint64_t>(map)), "r"(c0), "r"(c1), "r"(smem_u32(bar)), "l"(policy),
-        "r"(lead)
-        : "memory");
+    if constexpr (Pair)
+        CRC_TMA_LOAD("2d", ".cta_group::2", "tile::gather4", "{%5, %6, %7, %8, %9}", "r"(c0),
+                     "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]));
+    else
+        CRC_TMA_LOAD("2d", "", "tile::gather4", "{%5, %6, %7, %8, %9}", "r"(c0), "r"(r[0]),
+                     "r"(r[1]), "r"(r[2]), "r"(r[3]));
 }
 __device__ __forceinline__ void tma_store_3d(const CUtensorMap* map, const void* src, int c0,
                                              int c1, int c2) {

@@ -1,19 +1,26 @@
-// Products of ragged groups of rows with their expert's matrix, D = W_e X_e^T, on CTA pairs.
+// Products of ragged groups of rows with their expert's matrix, D = W_e X_e^T.
 //
 //   y_i = W_e x_row(i)                         (or silu(G_e x) * (U_e x), gate and up in W)
 //   dx_i = W_e^T dy_i                          (TW: the matrix's rows lie across the contraction)
 //
-// The matrix's rows are the 256 rows (A) of the pair's tcgen05.mma, the expert's rows its N
+// The matrix's rows are the 256 rows (A) of a CTA pair's tcgen05.mma, the expert's rows its N
 // columns, 16 to 256 of them in steps of 16: rows come in ragged numbers, so a tile is as wide
 // as they are, to the next 16.  (With the rows as A, an expert's last tile of 128 or 256 would
 // be half empty on average.)  TMA stages 128-byte pieces of the contraction: 128 matrix rows a
 // CTA, and half of the tile's rows, gathered four at a time where they are a token's.  Two
-// accumulators in TMEM, so that one is drained while the next tile's products run.
+// accumulators in TMEM, so that one is drained while the next tile's products run.  With few
+// rows the matrices bound the call, and CTAs by themselves (128 matrix rows, up to 128 rows)
+// leave fewer of them without a tile.
 //
-// Work: tiles of (expert, 256 matrix rows, up to 256 rows), in that order, in one row of
-// equal shares for the pairs.  A share may end inside an expert's rows, at any 16 of them:
-// a tile's products do not depend on the rows beside them.  So no pair waits for a last tile
-// of another, without a counter or a workspace.
+// Work: tiles of (expert, matrix rows, rows), in that order, dealt to the CTAs in turn: those
+// running together work on the same experts and find their rows and matrices in L2.  (In equal
+// shares of neighbouring tiles, each pair on experts of its own, the first product of 4096 tokens
+// took 348 us, not 189.)
+//
+// What bounds it: up to some hundred tokens the matrices' bytes (1000 tokens of the d = 4096
+// shape 466 us, 6.5 TB/s).  With a few hundred rows an expert, loads in flight: six stages of
+// 32 KB (three: 253 us, four 215, five 198, six 191 for 4096 tokens' gate and up, whose bytes
+// and flops take 128 and 106).
 #pragma once
 
 #include "group.cuh"
@@ -25,8 +32,7 @@ constexpr int kGmThreads = 512;
 constexpr int kGmGatherWarps = 8;
 constexpr int kGmStages = 6;
 constexpr int kGmA = 128 * 128, kGmB = 128 * 128, kGmStage = kGmA + kGmB;   // bytes, a CTA
-constexpr int kGmUnit = 16, kGmTileUnits = 16;       // rows of a unit, units of a tile at most
-constexpr int kGmFixed = 12;               // cost of a tile beside its rows, in units
+constexpr int kGmUnit = 16, kGmTileUnits = 16;       // rows of a unit, units of a pair's tile
 constexpr int kGmStaging = 2 * 32 * 256;   // two pieces of 32 rows x 128 columns of y
 constexpr int kGmScales = 2 * 256 * 4;     // the scales of a tile's rows, of two tiles
 constexpr int kGmBoxRows = 32;             // rows of a TMA box of x in order
@@ -39,7 +45,7 @@ struct GroupArgs {
     long long ws_stride;         // floats
     int kblocks;                 // 128-byte pieces of the contraction
     int out;                     // columns of y
-    int ftiles;                  // tiles of 256 matrix rows
+    int ftiles;                  // tiles of 256 matrix rows, 128 of a CTA by itself
 };
 
 struct GroupTile {
@@ -47,19 +53,22 @@ struct GroupTile {
 };
 
 // Tiles of an expert with `count` rows.
+template <bool Pair>
 __device__ __forceinline__ long long group_tiles(int count, int ftiles) {
-    constexpr int kRows = kGmUnit * kGmTileUnits;
+    constexpr int kRows = kGmUnit * kGmTileUnits / (Pair ? 1 : 2);
     return (long long)ftiles * ((count + kRows - 1) / kRows);
 }
 
 // Tile `i` of the call, i < cost[N]: an expert's rows in equal tiles, one after the other for
 // each tile of its matrix.
+template <bool Pair>
 __device__ __forceinline__ GroupTile group_tile(const GroupPlan& p, int N, int ftiles,
                                                 long long i) {
+    constexpr int kUnits = kGmTileUnits / (Pair ? 1 : 2);
     GroupTile t;
     t.e = expert_at(p, N, i);
     const int count = p.count[t.e], units = (count + kGmUnit - 1) / kGmUnit;
-    const int pieces = (units + kGmTileUnits - 1) / kGmTileUnits;
+    const int pieces = (units + kUnits - 1) / kUnits;
     const int in = (int)(i - p.cost[t.e]);
     const int size = (units + pieces - 1) / pieces, unit = in % pieces * size;
     t.ft = in / pieces;
@@ -92,12 +101,13 @@ struct GroupSmem {
 };
 
 // W8: e4m3 rows and matrices.  GLU: gate and up, 16 and 16 rows of a quarter of TMEM.
-// TW: the matrix is [contraction][matrix rows].
-template <bool W8, bool GLU, bool TW>
+// TW: the matrix is [contraction][matrix rows].  Pair: on CTA pairs, else on CTAs by themselves.
+template <bool W8, bool GLU, bool TW, bool Pair>
 __global__ void __launch_bounds__(kGmThreads, 1)
     group_matmul_kernel(const __grid_constant__ CUtensorMap mw,
                         const __grid_constant__ CUtensorMap mx, GroupArgs a) {
     constexpr int kElems = W8 ? 128 : 64;              // elements of a 128-byte piece
+    constexpr int kCtas = Pair ? 2 : 1;                // CTAs of a tile
     extern __shared__ __align__(1024) uint8_t smem_raw[];
     uint8_t* smem = reinterpret_cast<uint8_t*>(
         (reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
@@ -113,7 +123,7 @@ __global__ void __launch_bounds__(kGmThreads, 1)
     uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(drain_bar + 1);
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const uint32_t rank = cluster_ctarank();
+    const uint32_t rank = Pair ? cluster_ctarank() : 0u;
     const bool leader = rank == 0u;
 
     if (threadIdx.x == 0) {
@@ -123,7 +133,7 @@ __global__ void __launch_bounds__(kGmThreads, 1)
         }
         for (int s = 0; s < 2; ++s) {
             mbar_init(&tfull_bar[s], 1);
-            mbar_init(&tempty_bar[s], 8);              // four warps of each CTA
+            mbar_init(&tempty_bar[s], 4 * kCtas);      // four warps of each CTA
         }
         mbar_init(drain_bar, 1);
         fence_mbar_init();
@@ -131,18 +141,23 @@ __global__ void __launch_bounds__(kGmThreads, 1)
         tma_prefetch_desc(&mx);
     }
     if (warp == 1) {
-        tmem_alloc_pair(tmem_slot, 512);
-        tmem_relinquish_pair();
+        if constexpr (Pair) {
+            tmem_alloc_pair(tmem_slot, 512);
+            tmem_relinquish_pair();
+        } else {
+            tmem_alloc(tmem_slot, 512);
+            tmem_relinquish();
+        }
     }
     pdl_begin();
-    make_plan(plan, a.r, [&](int n) { return group_tiles(n, a.ftiles); });
+    make_plan(plan, a.r, [&](int n) { return group_tiles<Pair>(n, a.ftiles); });
     tc_fence_before();
     __syncthreads();
-    cluster_sync();                     // the peer's barriers exist before any remote use
+    if constexpr (Pair) cluster_sync();   // the peer's barriers exist before any remote use
     tc_fence_after();
     const uint32_t tmem_base = *tmem_slot;
 
-    const int pair = (int)blockIdx.x >> 1, pairs = (int)gridDim.x >> 1;
+    const int pair = (int)blockIdx.x / kCtas, pairs = (int)gridDim.x / kCtas;
     const long long tiles = plan.cost[a.r.N];
 
     if (warp == 0) {
@@ -150,12 +165,12 @@ __global__ void __launch_bounds__(kGmThreads, 1)
         const uint32_t lead = elected();
         const uint64_t pol = l2_normal_policy();
         // both CTAs' loads of a stage complete on the even CTA's barrier
-        const uint32_t lead_full = cluster_map(&full_bar[0], 0u);
+        const uint32_t lead_full = Pair ? cluster_map(&full_bar[0], 0u) : smem_u32(&full_bar[0]);
         int stage = 0, issued = 0;
         uint32_t phase = 0;
         bool ok = true;
         for (long long i = pair; i < tiles && ok; i += pairs) {
-            const GroupTile t = group_tile(plan, a.r.N, a.ftiles, i);
+            const GroupTile t = group_tile<Pair>(plan, a.r.N, a.ftiles, i);
             for (int kb = 0; kb < a.kblocks; ++kb) {
                 ok = __all_sync(kFull, mbar_wait_cluster(&empty_bar[stage], phase ^ 1));
                 if (!ok) {
@@ -163,19 +178,19 @@ __global__ void __launch_bounds__(kGmThreads, 1)
                     break;
                 }
                 uint8_t* sa = smem + stage * kGmStage;
-                if (leader && lead) mbar_arrive_expect_tx(&full_bar[stage], 2 * kGmA);
+                if (leader && lead) mbar_arrive_expect_tx(&full_bar[stage], kCtas * kGmA);
                 const uint32_t fb = lead_full + (uint32_t)(stage * 8);
                 if constexpr (TW) {
-                    const int f0 = t.ft * 256 + (int)rank * 128;
-                    tma_load_3d_pair_by(lead, sa, &mw, fb, f0, kb * 64, t.e, pol);
-                    tma_load_3d_pair_by(lead, sa + 8192, &mw, fb, f0 + 64, kb * 64, t.e, pol);
+                    const int f0 = (t.ft * kCtas + (int)rank) * 128;
+                    tma_load_3d_of<Pair>(lead, sa, &mw, fb, f0, kb * 64, t.e, pol);
+                    tma_load_3d_of<Pair>(lead, sa + 8192, &mw, fb, f0 + 64, kb * 64, t.e, pol);
                 } else if constexpr (GLU) {
                     // four times 16 gate rows and the 16 up rows beside them
-                    tma_load_5d_pair_by(lead, sa, &mw, fb, kb * kElems, 0, 0,
-                                        t.ft * 8 + (int)rank * 4, t.e, pol);
+                    tma_load_5d_of<Pair>(lead, sa, &mw, fb, kb * kElems, 0, 0,
+                                        (t.ft * kCtas + (int)rank) * 4, t.e, pol);
                 } else {
-                    tma_load_3d_pair_by(lead, sa, &mw, fb, kb * kElems,
-                                        t.ft * 256 + (int)rank * 128, t.e, pol);
+                    tma_load_3d_of<Pair>(lead, sa, &mw, fb, kb * kElems,
+                                        (t.ft * kCtas + (int)rank) * 128, t.e, pol);
                 }
                 ++issued;
                 if (++stage == kGmStages) {
@@ -201,13 +216,13 @@ __global__ void __launch_bounds__(kGmThreads, 1)
         // ---------------------------------------------------------- rows in order
         const uint32_t lead = elected();
         const uint64_t pol = l2_normal_policy();
-        const uint32_t lead_full = cluster_map(&full_bar[0], 0u);
+        const uint32_t lead_full = Pair ? cluster_map(&full_bar[0], 0u) : smem_u32(&full_bar[0]);
         int stage = 0;
         uint32_t phase = 0;
         bool ok = true;
         for (long long i = pair; i < tiles && ok; i += pairs) {
-            const GroupTile t = group_tile(plan, a.r.N, a.ftiles, i);
-            const int half = (t.rows + kGmUnit - 1) / kGmUnit * (kGmUnit / 2);
+            const GroupTile t = group_tile<Pair>(plan, a.r.N, a.ftiles, i);
+            const int half = (t.rows + kGmUnit - 1) / kGmUnit * (kGmUnit / kCtas);
             const int first = t.row + (int)rank * half;                // this CTA's rows
             const int boxes = (half + kGmBoxRows - 1) / kGmBoxRows;
             for (int kb = 0; kb < a.kblocks; ++kb) {
@@ -218,10 +233,10 @@ __global__ void __launch_bounds__(kGmThreads, 1)
                 }
                 uint8_t* sb = smem + stage * kGmStage + kGmA;
                 if (leader && lead)
-                    mbar_arrive_expect_tx(&full_bar[stage], 2 * boxes * kGmBoxRows * 128);
+                    mbar_arrive_expect_tx(&full_bar[stage], kCtas * boxes * kGmBoxRows * 128);
                 const uint32_t fb = lead_full + (uint32_t)(stage * 8);
                 for (int b = 0; b < boxes; ++b)
-                    tma_load_2d_pair_by(lead, sb + b * kGmBoxRows * 128, &mx, fb, kb * kElems,
+                    tma_load_2d_of<Pair>(lead, sb + b * kGmBoxRows * 128, &mx, fb, kb * kElems,
                                         first + b * kGmBoxRows, pol);
                 if (++stage == kGmStages) {
                     stage = 0;
@@ -234,14 +249,14 @@ __global__ void __launch_bounds__(kGmThreads, 1)
         // warp w: the four rows 4 f .., f = w, w + 8, w + 16, w + 24 of this CTA's
         const uint32_t lead = elected();
         const uint64_t pol = l2_normal_policy();
-        const uint32_t lead_full = cluster_map(&full_bar[0], 0u);
+        const uint32_t lead_full = Pair ? cluster_map(&full_bar[0], 0u) : smem_u32(&full_bar[0]);
         const int w = warp - 8;
         int stage = 0;
         uint32_t phase = 0;
         bool ok = true;
         for (long long i = pair; i < tiles && ok; i += pairs) {
-            const GroupTile t = group_tile(plan, a.r.N, a.ftiles, i);
-            const int half = (t.rows + kGmUnit - 1) / kGmUnit * (kGmUnit / 2);
+            const GroupTile t = group_tile<Pair>(plan, a.r.N, a.ftiles, i);
+            const int half = (t.rows + kGmUnit - 1) / kGmUnit * (kGmUnit / kCtas);
             int mine = 0, src[4][4];
             {
                 const int f = w + kGmGatherWarps * ((lane >> 2) & 3);
@@ -258,14 +273,14 @@ __global__ void __launch_bounds__(kGmThreads, 1)
                     break;
                 }
                 if (leader && w == 0 && lead)
-                    mbar_arrive_expect_tx(&full_bar[stage], 2 * half * 128);
+                    mbar_arrive_expect_tx(&full_bar[stage], kCtas * half * 128);
                 uint8_t* sb = smem + stage * kGmStage + kGmA;
                 const uint32_t fb = lead_full + (uint32_t)(stage * 8);
 #pragma unroll
                 for (int q = 0; q < 4; ++q) {
                     const int f = w + kGmGatherWarps * q;
                     if (f < half / 4)
-                        tma_gather4_pair_by(lead, sb + f * 512, &mx, fb, kb * kElems, src[q], pol);
+                        tma_gather4_of<Pair>(lead, sb + f * 512, &mx, fb, kb * kElems, src[q], pol);
                 }
                 if (++stage == kGmStages) {
                     stage = 0;
@@ -280,15 +295,15 @@ __global__ void __launch_bounds__(kGmThreads, 1)
             int stage = 0, acc = 0, failed = 0;
             uint32_t phase = 0, acc_phase = 0;
             for (long long i = pair; i < tiles && !failed; i += pairs) {
-                const GroupTile t = group_tile(plan, a.r.N, a.ftiles, i);
+                const GroupTile t = group_tile<Pair>(plan, a.r.N, a.ftiles, i);
                 if (!__all_sync(kFull, mbar_wait_cluster(&tempty_bar[acc], acc_phase ^ 1))) {
                     latch_error(a.r.err, CRC_ETIMEOUT);
                     break;
                 }
                 tc_fence_after();
                 const int cols = (t.rows + kGmUnit - 1) / kGmUnit * kGmUnit;
-                const uint32_t idesc = W8 ? idesc_e4m3_f32_mn(256, cols)
-                                          : idesc_bf16_f32(256, cols) | (TW ? kIdescMnA : 0);
+                const uint32_t idesc = W8 ? idesc_e4m3_f32_mn(128 * kCtas, cols)
+                                          : idesc_bf16_f32(128 * kCtas, cols) | (TW ? kIdescMnA : 0);
                 const uint32_t d_tmem = tmem_base + (uint32_t)(acc * 256);
                 for (int kb = 0; kb < a.kblocks; ++kb) {
                     if (!__all_sync(kFull, mbar_wait_cluster(&full_bar[stage], phase))) {
@@ -300,39 +315,42 @@ __global__ void __launch_bounds__(kGmThreads, 1)
                     const uint32_t sa = smem_u32(smem + stage * kGmStage), sb = sa + kGmA;
 #pragma unroll
                     for (int kk = 0; kk < 4; ++kk)
-                        umma_pair_by<W8>(d_tmem,
+                        umma_by<W8, Pair>(d_tmem,
                                          TW ? sw128_mnmajor_desc(sa + kk * 2048, 8192)
                                             : sw128_kmajor_desc(sa + kk * 32),
                                          sw128_kmajor_desc(sb + kk * 32), idesc, (kb | kk) != 0,
                                          lead);
-                    commit_pair_by(&empty_bar[stage], lead);
+                    commit_of<Pair>(&empty_bar[stage], lead);
                     if (++stage == kGmStages) {
                         stage = 0;
                         phase ^= 1;
                     }
                 }
                 if (failed) break;
-                commit_pair_by(&tfull_bar[acc], lead);
+                commit_of<Pair>(&tfull_bar[acc], lead);
                 acc ^= 1;
                 if (acc == 0) acc_phase ^= 1;
             }
             if (lead) {
-                umma_commit_pair_local(drain_bar);
+                if constexpr (Pair)
+                    umma_commit_pair_local(drain_bar);
+                else
+                    umma_commit(drain_bar);
                 if (!mbar_wait(drain_bar, 0)) latch_error(a.r.err, CRC_ETIMEOUT);
             }
         }
     } else if (warp >= 4 && warp < 8) {
         // ---------------------------------------------------------- epilogue
         const int quarter = warp & 3;
-        const uint32_t tempty_lead = cluster_map(&tempty_bar[0], 0u);
+        const uint32_t tempty_lead = Pair ? cluster_map(&tempty_bar[0], 0u) : 0u;
         constexpr int kCols = GLU ? 64 : 128;           // columns of y of this CTA
         constexpr int kRow = kCols * 2;                 // bytes of a staged row
         int acc = 0, buf = 0;
         uint32_t acc_phase = 0;
         bool ok = true;
         for (long long i = pair; i < tiles && ok; i += pairs) {
-            const GroupTile t = group_tile(plan, a.r.N, a.ftiles, i);
-            const int col0 = t.ft * (2 * kCols) + (int)rank * kCols;
+            const GroupTile t = group_tile<Pair>(plan, a.r.N, a.ftiles, i);
+            const int col0 = (t.ft * kCtas + (int)rank) * kCols;
             // this thread's rows of W: lanes t / 4 + 8 h of the quarter's two halves
             float ws[2][2] = {};
             float* xs = scales + acc * 256;
@@ -434,10 +452,13 @@ __global__ void __launch_bounds__(kGmThreads, 1)
     __syncthreads();
     // neither CTA leaves (or frees TMEM) while the other may still arrive on its
     // barriers or have MMAs write its TMEM
-    cluster_sync();
+    if constexpr (Pair) cluster_sync();
     if (warp == 1) {
         tc_fence_after();
-        tmem_dealloc_pair(tmem_base, 512);
+        if constexpr (Pair)
+            tmem_dealloc_pair(tmem_base, 512);
+        else
+            tmem_dealloc(tmem_base, 512);
     }
 }
 

@@ -136,15 +136,15 @@ __global__ void __launch_bounds__(kGwThreads, 1)
 #pragma unroll
                     for (int c = 0; c < kGwN / 64; ++c)
                         if (is_x || c < kGwM / 64)
-                            tma_load_2d_by(lead, s + c * kGwChunk, is_x ? &mx : &mdy,
-                                           &full_bar[stage], col + c * 64, row0 + r, pol);
+                            tma_load_2d_of<false>(lead, s + c * kGwChunk, is_x ? &mx : &mdy,
+                                           smem_u32(&full_bar[stage]), col + c * 64, row0 + r, pol);
                 } else {
                     for (int q = 0; q < some; q += 16)
 #pragma unroll
                         for (int c = 0; c < kGwN / 64; ++c)
                             if (is_x || c < kGwM / 64)
-                                tma_load_2d_by(lead, s + c * kGwChunk + q * 128,
-                                               is_x ? &mx16 : &mdy16, &full_bar[stage],
+                                tma_load_2d_of<false>(lead, s + c * kGwChunk + q * 128,
+                                               is_x ? &mx16 : &mdy16, smem_u32(&full_bar[stage]),
                                                col + c * 64, row0 + r + q, pol);
                 }
                 ++issued;
@@ -204,7 +204,7 @@ __global__ void __launch_bounds__(kGwThreads, 1)
                     for (int c = 0; c < kGwN / 64; ++c)
 #pragma unroll
                         for (int q = 0; q < 2; ++q)
-                            tma_gather4_by(lead, s + c * kGwChunk + q * 512, &mx, &full_bar[stage],
+                            tma_gather4_of<false>(lead, s + c * kGwChunk + q * 512, &mx, smem_u32(&full_bar[stage]),
                                            col + c * 64, src[q], pol);
                 if (++stage == kGwStages) {
                     stage = 0;
@@ -243,7 +243,7 @@ __global__ void __launch_bounds__(kGwThreads, 1)
 #pragma unroll
                 for (int kk = 0; kk < kGwRows / 16; ++kk)
                     if (kk * 16 < some)
-                        umma_bf16_by(d_tmem, sw128_mnmajor_desc(sa + kk * 2048, kGwChunk),
+                        umma_by<false, false>(d_tmem, sw128_mnmajor_desc(sa + kk * 2048, kGwChunk),
                                      sw128_mnmajor_desc(sb + kk * 2048, kGwChunk), kIdesc,
                                      (r | kk) != 0, lead);
                 commit_by(&empty_bar[stage], lead);
