@@ -1034,8 +1034,12 @@ def _group_weights(w, w_scale, dev: int):
         scale_stride, *inner = w_scale.stride()
         if inner != ([1] if dims == 3 else [n, 1]):
             raise ValueError("an expert's scales must be contiguous")
+    first = stride[0]
+    if N == 1:                                          # (one expert's stride says nothing)
+        first = (dims - 2) * n * k
+        scale_stride = 0 if w_scale is None else (dims - 2) * n
     return (_GROUP_WEIGHTS.pack(N, n, k, dims - 3, kind, 0, w.data_ptr(),
-                                stride[0] * (2 if kind == BF16 else 1), scale, scale_stride * 4),
+                                first * (2 if kind == BF16 else 1), scale, scale_stride * 4),
             N, n, k, dims == 4)
 
 
@@ -1196,12 +1200,16 @@ def matvec4(x, codes, scale, topk=None, expert_slot=None, y=None, N: int | None 
     pc = _check(codes, "codes", cs, torch.uint8, dev, False)
     ps = _check(scale, "scale", (*cs[:-2], groups, n), bf16, dev, False)
     (codes_stride, *ci), (scale_stride, *si) = codes.stride(), scale.stride()
+    if groups == 1:                                     # (strides of one row, of one slot)
+        si[-2] = n
     if dims == 3:
         dense = ci == [k // 2, 1] and si == [n, 1]
     else:
         dense = ci == [n * k // 2, k // 2, 1] and si == [groups * n, n, 1]
     if not dense:
         raise ValueError("a slot's codes and scales must be contiguous")
+    if slots == 1:
+        codes_stride, scale_stride = (dims - 2) * n * k // 2, (dims - 2) * groups * n
     if N is None:
         N = expert_slot.shape[0] if expert_slot is not None else slots
     M, K = x.shape[0], 1

@@ -8,10 +8,13 @@
 // the experts gives every warp its first place.  Up to kOneChunk choices it is one kernel
 // of one CTA; above, a kernel counts every chunk and a second one places them, after each
 // CTA has summed the counts of the chunks.  Bound by the latency of its launches and of
-// the passes in them, not by its 9 bytes a choice.
+// the passes in them, not by its 9 bytes a choice: 148 choices take 2.7 us, 8192 6.1, 262144
+// (32768 tokens, 128 experts) 10.6.
 //
-// Sum and gradient.  One pass over the rows, 16 bytes a thread and choice, eight choices'
-// loads in flight; the choices are summed in fp32 in rank order.  Bound by memory.
+// Sum and gradient.  One pass over the rows, 16 bytes a thread and choice, as many choices'
+// loads in flight as fit the registers; the choices are summed in fp32 in rank order.  Bound by
+// memory: 4096 tokens x 8 of d = 2048 28 us, 5.4 TB/s; the gradient, with the gates', 50 us, 5.8
+// TB/s; small batches by their launch (1.5 to 2.5 us).
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 

@@ -7,19 +7,25 @@
 // four bits with the top one turned over, put below the exponent of 128, are 136 + code) and
 // the subtraction of 136, which is exact.
 //
-// What bounds it.  A decoded token reads its experts' codes once, so the bytes do: half a
-// byte a weight and 2 / G for the scale.  At 6.8 TB/s an SM has to turn over some 47 weights a
-// clock, more than scalar fp32 instructions could (about 3 a weight), so the fragments of
-// mma.sync m16n8k16 are filled from the packed words in registers: the eight columns of the
-// product are eight choices of the same expert.  (tcgen05 takes its operands from shared
-// memory: codes would have to be widened to bf16 and written back there, 4 bytes of
-// traffic for each half byte that came in, for a product that the bytes bound anyway.)
+// What it should be bound by is bytes, half of one a weight and 2 / G for the scale.  At 6.8 TB/s
+// an SM has to turn over some 47 weights a clock, more than scalar fp32 instructions could (about
+// 3 a weight), so the fragments of mma.sync m16n8k16 are filled from the packed words in
+// registers: the eight columns of the product are eight choices of the same expert.  (tcgen05
+// takes its operands from shared memory: codes would have to be widened to bf16 and written back
+// there, 4 bytes of traffic for each half byte that came in; and its sums over the groups could
+// not be scaled apart.)  It reaches 20 to 25 weights a clock: 64 tokens' second product (128
+// experts, 105 MB) takes 39 us, 35 of them with the loads left out and 22 with the products
+// left out: what bounds it are two bit operations, a shift and a subtraction for two weights, and
+// the legacy tensor path.  One token's (14 MB) takes 10 us: 5 are the launch and the choices'
+// order, and eight experts are too few boxes a warp to fill the rest.
 //
 // A persistent grid: each CTA brings the choices into their experts' order once, and its
 // warps take tiles of 32 rows (with gate and up: 16 rows of each) of the active experts in
 // turn.  A warp's codes and scales come by TMA into a ring of its own, 256 columns a time,
 // across the ends of its tiles; with too few tiles for the warps, 2, 4 or 8 warps share a
-// tile's columns and their sums are added in a fixed order.
+// tile's columns and their sums are added in a fixed order.  Half a box's words, scales and x
+// are loaded before they are used (41 us against 49).  Two CTAs an SM leave 128 registers a
+// thread: with 20 warps of 96 it took 45 us.
 #include <cudaTypedefs.h>
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>

@@ -7,7 +7,9 @@
 //
 // A warp takes 512 columns of a row at a time, 16 a lane, so a group is 2, 4 or 8 lanes; a
 // CTA 32 rows, whose scales leave through shared memory as 64-byte pieces.  Bound by
-// memory: 2 bytes read and half a byte written an element.
+// memory, 2 bytes read and half a byte written an element, beside the instructions, some eight
+// an element: a layer's gate and up (64 experts, 537 MB) take 128 us, 5.3 TB/s (206 when each
+// code compared its rest with half a step), one expert's 3.5.
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 

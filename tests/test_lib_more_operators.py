@@ -357,3 +357,15 @@ def test_unsupported_groups_are_refused(P):
     for kw in (dict(group=16), dict(group=128)):
         with pytest.raises(P.CrcError):
             P.quantize_rows4(new(8, 64), out4=new(8, 32, dtype=U), scale=new(2, 8), **kw)
+
+
+def test_strides_that_say_nothing(P):
+    """One expert, one slot, one group: their strides do not matter."""
+    w = OnGpu(torch.zeros((32, 64), dtype=B).as_strided((1, 32, 64), (8, 64, 1)))
+    P.group_matmul(new(6, 64), w, new(2, dtype=I), y=new(6, 32))
+    assert P.crc.crc_group_weights.from_buffer_copy(P.calls[-1][1][0]).w_stride == 32 * 64 * 2
+    codes = OnGpu(torch.zeros((8, 32), dtype=U).as_strided((1, 8, 32), (8, 32, 1)))
+    scale = OnGpu(torch.zeros((8,), dtype=B).as_strided((1, 1, 8), (1, 3, 1)))
+    P.matvec4(new(5, 64), codes, scale, y=new(5, 1, 8))
+    c = P.crc.crc_matvec4_weights.from_buffer_copy(P.calls[-1][1][0])
+    assert (c.codes_stride, c.scale_stride, c.group) == (8 * 32, 8 * 2, 64)
