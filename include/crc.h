@@ -630,8 +630,8 @@ int crc_group_matmul(const crc_group_weights *w, const void *x_dev, int64_t x_st
  *   dw_dev    dw_type (CRC_F32 or CRC_BF16) [N][n][k], 16-byte aligned, zeros for an
  *             expert without rows, or NULL (x_dev is not read then)
  * Sums in fp32, in the order of the rows, without atomics; each output is rounded once.  (The
- * tensor cores cut a sum's low bits where an fp32 addition rounds: every 16 rows, or columns of
- * n, it is off by up to 2^-23 of itself; dW of 256 rows by 9e-7 in the mean square.)
+ * tensor cores cut a sum's low bits where an fp32 addition rounds, every 16 rows, or columns of
+ * n: dW is off by up to 1e-6 in the mean square.)
  * E = 0 sets dw to zero. */
 int crc_group_matmul_grad(const crc_group_weights *w, const uint16_t *dy_dev,
                           const uint16_t *x_dev, int64_t x_stride, int64_t x_rows,

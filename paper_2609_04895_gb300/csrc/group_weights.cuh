@@ -30,6 +30,11 @@ constexpr int kGwRows = 64;                // rows of a block
 constexpr int kGwM = 128, kGwN = 256;
 constexpr int kGwA = kGwRows * kGwM * 2, kGwB = kGwRows * kGwN * 2, kGwStage = kGwA + kGwB;
 constexpr int kGwChunk = kGwRows * 128;    // 64 columns of a block
+// Rows that one accumulator sums for fp32 gradients; of more, the second half goes to the other
+// one and the two are added in fp32, because the tensor cores cut a sum's low bits at each step of
+// 16 rows.  Error of dW in the mean square and time, 4096 tokens x 8: always one accumulator 0.8 to
+// 1.0e-6, 189 us; two above 1024 rows 0.55e-6, 195; above 512 0.45e-6, 207; above 256 0.4e-6, 225.
+constexpr int kGwPart = 1024;
 constexpr int kGwStages = 4;
 constexpr int kGwBufs = 1;                 // pieces of 32 rows x 128 bytes of an epilogue warp
 constexpr int kGwStaging = 4 * kGwBufs * 4096;
@@ -50,6 +55,13 @@ static_assert(GroupGradSmem::bytes() + sizeof(GroupPlan) < 232448, "shared memor
 // Rows of a block that has `left` of them, to the next 16.
 __device__ __forceinline__ int round16(int left) {
     return left >= kGwRows ? kGwRows : (left + 15) / 16 * 16;
+}
+
+// The first row of an expert's second accumulator, `count` where it has one.
+template <bool F32>
+__device__ __forceinline__ int half_of(int count) {
+    if (!F32 || count <= kGwPart) return count;
+    return ((count + kGwRows - 1) / kGwRows + 1) / 2 * kGwRows;
 }
 
 // Rows `tail` .. of a block's six pieces of 64 columns, to the next 16: zeros.
@@ -232,8 +244,21 @@ __global__ void __launch_bounds__(kGwThreads, 1)
                 break;
             }
             tc_fence_after();
-            const uint32_t d_tmem = tmem_base + (uint32_t)(acc * 256);
+            const int half = half_of<F32>(count);
             for (int r = 0; r < count; r += kGwRows) {
+                if (r == half) {
+                    commit_by(&tfull_bar[acc], lead);
+                    acc ^= 1;
+                    if (acc == 0) acc_phase ^= 1;
+                    ok = mbar_wait_warp(&tempty_bar[acc], acc_phase ^ 1);
+                    if (!ok) {
+                        latch_error(a.r.err, CRC_ETIMEOUT);
+                        break;
+                    }
+                    tc_fence_after();
+                }
+                const uint32_t d_tmem = tmem_base + (uint32_t)(acc * 256);
+                const bool first = r == 0 || r == half;
                 ok = mbar_wait_warp(&full_bar[stage], phase);
                 if (!ok) {
                     latch_error(a.r.err, CRC_ETIMEOUT);
@@ -249,7 +274,7 @@ __global__ void __launch_bounds__(kGwThreads, 1)
                     if (kk * 16 < some)
                         umma_by<false, false>(d_tmem, sw128_mnmajor_desc(sa + kk * 2048, kGwChunk),
                                      sw128_mnmajor_desc(sb + kk * 2048, kGwChunk), kIdesc,
-                                     (r | kk) != 0, lead);
+                                     !first || kk != 0, lead);
                 commit_by(&empty_bar[stage], lead);
                 if (++stage == kGwStages) {
                     stage = 0;
@@ -285,6 +310,17 @@ __global__ void __launch_bounds__(kGwThreads, 1)
             }
             const uint32_t tbase =
                 tmem_base + (uint32_t)(acc * 256) + ((uint32_t)(quarter * 32) << 16);
+            const bool two = half_of<F32>(plan.count[e]) < plan.count[e];
+            const int acc1 = acc ^ 1;
+            if (two) {
+                if (!mbar_wait_warp(&tfull_bar[acc1], acc_phase ^ (acc1 == 0))) {
+                    latch_error(a.r.err, CRC_ETIMEOUT);
+                    break;
+                }
+                tc_fence_after();
+            }
+            const uint32_t tbase1 =
+                tmem_base + (uint32_t)(acc1 * 256) + ((uint32_t)(quarter * 32) << 16);
 #pragma unroll 1
             for (int c = 0; c < kGwN; c += kCols) {
                 uint4 q[8];
@@ -295,6 +331,17 @@ __global__ void __launch_bounds__(kGwThreads, 1)
                     tmem_ld_wait();
 #pragma unroll
                     for (int i = 0; i < kCols; i += 16) pin16(v + i);
+                    if constexpr (F32) {
+                        if (two) {
+                            float u[kCols];
+                            tmem_ld32(tbase1 + (uint32_t)c, u);
+                            tmem_ld_wait();
+                            pin16(u);
+                            pin16(u + 16);
+#pragma unroll
+                            for (int i = 0; i < kCols; ++i) v[i] += u[i];
+                        }
+                    }
 #pragma unroll
                     for (int j = 0; j < 8; ++j) {
                         uint32_t u[4];
@@ -332,9 +379,11 @@ __global__ void __launch_bounds__(kGwThreads, 1)
             if (some) {
                 tc_fence_before();
                 __syncwarp();
-                if (lane == 0) mbar_arrive(&tempty_bar[acc]);
-                acc ^= 1;
-                if (acc == 0) acc_phase ^= 1;
+                for (int k = 0; k < (two ? 2 : 1); ++k) {
+                    if (lane == 0) mbar_arrive(&tempty_bar[acc]);
+                    acc ^= 1;
+                    if (acc == 0) acc_phase ^= 1;
+                }
             }
         }
         if (lane == 0) bulk_wait<0>();                   // every store has landed

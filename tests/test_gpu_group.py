@@ -34,6 +34,7 @@ SHAPES = [
     (256, 128, [16]), (8, 8, [1, 0, 2]), (16, 16, [0, 0, 3, 1]), (48, 72, [17, 0, 15, 33]),
     (512, 320, [1, 2, 0, 300]), (264, 200, [255, 256, 257, 0]), (1024, 512, [31, 129, 0, 64, 513]),
     (80, 2880, [5, 40]), (528, 64, [0, 1000, 7]), (128, 136, [100] * 12),
+    (64, 72, [1025, 2500, 0, 30, 1024]),
 ]
 
 
