@@ -13,7 +13,7 @@
 //
 // Sum and gradient.  One pass over the rows, 16 bytes a thread and choice, as many choices'
 // loads in flight as fit the registers; the choices are summed in fp32 in rank order.  Bound by
-// memory: 4096 tokens x 8 of d = 2048 28 us, 5.4 TB/s; the gradient, with the gates', 50 us, 5.8
+// memory: 4096 tokens x 8 of d = 2048 25.4 us, 6.0 TB/s; the gradient, with the gates', 50 us, 5.8
 // TB/s; small batches by their launch (1.5 to 2.5 us).
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
@@ -213,7 +213,7 @@ __global__ void __launch_bounds__(kOrderThreads) order_choices_kernel(OrderArgs 
 // the sum over a token's choices
 // ---------------------------------------------------------------------------
 constexpr int kSumThreads = 256;
-constexpr int kManyTokens = 6000;
+constexpr int kManyTokens = 12000;
 
 struct SumArgs {
     const uint16_t* y;           // [rows][d]
@@ -251,49 +251,59 @@ __device__ __forceinline__ long long row_of(const SumArgs& a, int m, int j) {
     return r >= 0 && r < a.rows ? r : -1;
 }
 
-// kBatch: choices of a token whose loads are in flight together; kTok: tokens of a team.
-template <int kBatch, int kTok>
+// kBatch: choices of a token whose loads are in flight together.  A CTA takes kTurns tokens for
+// each team of threads; their rows and gates are looked up once, into shared memory (from global
+// memory in each thread 4096 tokens x 8 of d = 2048 took 27.7 us, 25.4 so).
+constexpr int kCtaChoices = 256;
+template <int kBatch, int kTurns>
 __global__ void __launch_bounds__(kSumThreads) sum_choices_kernel(SumArgs a) {
+    __shared__ int rows[kCtaChoices];
+    __shared__ float gates[kCtaChoices];
     pdl_begin();
-    const int t = threadIdx.x % a.team;
-    const int m = (blockIdx.x * (blockDim.x / a.team) + threadIdx.x / a.team) * kTok;
-    if (m >= a.M) return;
-    for (int v = t; v < a.d / 8; v += a.team) {
-        float sum[kTok][8] = {};
-        for (int j0 = 0; j0 < a.K; j0 += kBatch) {
-            uint4 u[kTok][kBatch];
-            float g[kTok][kBatch];
-            bool on[kTok][kBatch];
-#pragma unroll
-            for (int k = 0; k < kTok; ++k)
+    const int teams = blockDim.x / a.team;
+    const int t = threadIdx.x % a.team, team = threadIdx.x / a.team;
+    const int m0 = blockIdx.x * teams * kTurns;
+    const int choices = min(teams * kTurns, a.M - m0) * a.K;
+    for (int i = threadIdx.x; i < choices; i += blockDim.x) {
+        const long long r = row_of(a, m0, i);
+        rows[i] = (int)r;
+        gates[i] = a.gates ? a.gates[(long long)m0 * a.K + i] : 1.f;
+    }
+    __syncthreads();
+#pragma unroll 1
+    for (int turn = 0; turn < kTurns; ++turn) {
+        const int at = turn * teams + team, m = m0 + at;
+        if (m >= a.M) return;
+        const int* r = rows + at * a.K;
+        const float* g = gates + at * a.K;
+        for (int v = t; v < a.d / 8; v += a.team) {
+            float sum[8] = {};
+            for (int j0 = 0; j0 < a.K; j0 += kBatch) {
+                uint4 u[kBatch];
 #pragma unroll
                 for (int j = 0; j < kBatch; ++j) {
-                    const bool has = m + k < a.M && j0 + j < a.K;
-                    const long long r = has ? row_of(a, m + k, j0 + j) : -1;
-                    on[k][j] = r >= 0;
-                    g[k][j] = r >= 0 && a.gates ? a.gates[(long long)(m + k) * a.K + j0 + j] : 1.f;
-                    if (r >= 0) u[k][j] = __ldcs(reinterpret_cast<const uint4*>(a.y + r * a.d) + v);
+                    u[j] = make_uint4(0, 0, 0, 0);
+                    if (j0 + j < a.K && r[j0 + j] >= 0)
+                        u[j] = __ldcs(reinterpret_cast<const uint4*>(
+                                          a.y + (long long)r[j0 + j] * a.d) + v);
                 }
 #pragma unroll
-            for (int k = 0; k < kTok; ++k)
-#pragma unroll
                 for (int j = 0; j < kBatch; ++j) {
-                    if (!on[k][j]) continue;
+                    if (j0 + j >= a.K || r[j0 + j] < 0) continue;
                     float f[8];
-                    widen(u[k][j], f);
+                    widen(u[j], f);
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) sum[k][i] = fmaf(g[k][j], f[i], sum[k][i]);
+                    for (int i = 0; i < 8; ++i) sum[i] = fmaf(g[j0 + j], f[i], sum[i]);
                 }
+            }
+            *(reinterpret_cast<uint4*>(a.out + (long long)m * a.d) + v) = narrow(sum);
         }
-#pragma unroll
-        for (int k = 0; k < kTok; ++k)
-            if (m + k < a.M)
-                *(reinterpret_cast<uint4*>(a.out + (long long)(m + k) * a.d) + v) = narrow(sum[k]);
     }
 }
 
 // dy[place] = gate dout, dgates = <dout, y[place]>: a token's threads share its rows, and
 // the dot products are summed over the lanes and then the warps.
+// kBatch: choices of a token whose loads are in flight together; kTok: tokens of a team.
 template <int kBatch, int kTok>
 __global__ void __launch_bounds__(kSumThreads) sum_choices_grad_kernel(SumArgs a) {
     constexpr int kDots = kTok * kBatch;
@@ -376,32 +386,44 @@ __global__ void __launch_bounds__(kSumThreads) sum_choices_grad_kernel(SumArgs a
 }
 
 // Threads of a token: as few as leave no 16-byte piece more than the other threads have.
-template <bool Grad, int kBatch, int kTok>
-cudaError_t launch_sum_of(SumArgs& a, cudaStream_t st) {
-    const int vec = a.d / 8;
+int team_of(int d) {
+    const int vec = d / 8;
     const int turns = (vec + kSumThreads - 1) / kSumThreads;
-    a.team = ((vec + turns - 1) / turns + 31) / 32 * 32;
-    const int teams = kSumThreads / a.team, tokens = teams * kTok;
-    const unsigned grid = (unsigned)((a.M + tokens - 1) / tokens);
-    if constexpr (Grad)
-        return launch_dependent(sum_choices_grad_kernel<kBatch, kTok>, dim3(grid), teams * a.team,
-                                0, st, 1, a);
-    else
-        return launch_dependent(sum_choices_kernel<kBatch, kTok>, dim3(grid), teams * a.team, 0, st,
-                                1, a);
+    return ((vec + turns - 1) / turns + 31) / 32 * 32;
 }
-template <bool Grad>
+
+template <int kBatch, int kTurns>
+cudaError_t launch_sum_of(SumArgs& a, cudaStream_t st) {
+    a.team = team_of(a.d);
+    const int teams = kSumThreads / a.team, tokens = teams * kTurns;
+    return launch_dependent(sum_choices_kernel<kBatch, kTurns>,
+                            dim3((unsigned)((a.M + tokens - 1) / tokens)), teams * a.team, 0, st, 1,
+                            a);
+}
 cudaError_t launch_sum(SumArgs& a, cudaStream_t st) {
-    // One or two choices: several tokens' loads together.  Us, one / several tokens: gradient of
-    // 14400 tokens of d = 816, K = 1, 22.6 / 21.5, of 4000 of d = 1280, K = 2, 14.3 / 13.4; sum,
-    // K = 1, d = 816, 14400 tokens 15.3 / 12.6, 4000 tokens 4.4 / 4.5, 2000 2.6 / 3.0; K = 2,
-    // d = 1280, 4000 tokens 7.3 / 8.1.
+    // One choice and many tokens: several tokens a team.  Us, one / eight: d = 816, 14400 tokens
+    // 14.1 / 12.2, 8000 8.6 / 10.0, 4000 4.2 / 6.4; d = 2048, 14400 tokens 27.5 / 23.9.
     if (a.K == 1)
-        return Grad || a.M >= kManyTokens ? launch_sum_of<Grad, 1, 4>(a, st)
-                                          : launch_sum_of<Grad, 1, 1>(a, st);
-    if (a.K == 2) return launch_sum_of<Grad, 2, Grad ? 2 : 1>(a, st);
-    if (Grad || a.K <= 4) return launch_sum_of<Grad, 4, 1>(a, st);
-    return launch_sum_of<Grad, 8, 1>(a, st);
+        return a.M >= kManyTokens ? launch_sum_of<1, 8>(a, st) : launch_sum_of<1, 1>(a, st);
+    if (a.K == 2) return launch_sum_of<2, 1>(a, st);
+    if (a.K <= 4) return launch_sum_of<4, 1>(a, st);
+    return launch_sum_of<8, 1>(a, st);
+}
+
+template <int kBatch, int kTok>
+cudaError_t launch_grad_of(SumArgs& a, cudaStream_t st) {
+    a.team = team_of(a.d);
+    const int teams = kSumThreads / a.team, tokens = teams * kTok;
+    return launch_dependent(sum_choices_grad_kernel<kBatch, kTok>,
+                            dim3((unsigned)((a.M + tokens - 1) / tokens)), teams * a.team, 0, st, 1,
+                            a);
+}
+cudaError_t launch_grad(SumArgs& a, cudaStream_t st) {
+    // One or two choices: several tokens' loads together.  Us, one / several tokens: 14400
+    // tokens of d = 816, K = 1, 22.6 / 21.5; 4000 of d = 1280, K = 2, 14.3 / 13.4.
+    if (a.K == 1) return launch_grad_of<1, 4>(a, st);
+    if (a.K == 2) return launch_grad_of<2, 2>(a, st);
+    return launch_grad_of<4, 1>(a, st);
 }
 
 int order_chunk(long long E) {
@@ -505,7 +527,7 @@ int crc_sum_choices(const uint16_t* y_dev, int64_t y_rows, const int32_t* place_
     cudaError_t e;
     {
         ProfScope prof(CRC_KERNEL_SUM, st);
-        e = launch_sum<false>(a, st);
+        e = launch_sum(a, st);
     }
     note_launch();
     return cuda_status(e);
@@ -536,7 +558,7 @@ int crc_sum_choices_grad(const uint16_t* dout_dev, const uint16_t* y_dev, int64_
     cudaError_t e;
     {
         ProfScope prof(CRC_KERNEL_SUM, st);
-        e = launch_sum<true>(a, st);
+        e = launch_grad(a, st);
     }
     note_launch();
     return cuda_status(e);

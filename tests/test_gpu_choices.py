@@ -102,7 +102,7 @@ def randn(g, *shape, scale=1.0, dtype=torch.bfloat16):
 
 
 SUMS = [(1, 1, 8), (3, 32, 16), (7, 9, 264), (301, 4, 2880), (64, 8, 2048), (1001, 2, 1000),
-        (6500, 1, 88), (13, 5, 32768), (2, 17, 2056), (4, 6, 4096)]
+        (6500, 1, 88), (13, 5, 32768), (2, 17, 2056), (4, 6, 4096), (13001, 1, 264), (12000, 1, 8)]
 
 
 def sum_inputs(M, K, d, seed, holes):
