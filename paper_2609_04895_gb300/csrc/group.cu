@@ -241,16 +241,18 @@ int crc_group_matmul_grad(const crc_group_weights* w, const uint16_t* dy_dev,
         if (rc) return rc;
     }
     if (!dw_dev) return CRC_OK;
-    CUtensorMap mdy, mx, mdy16, mx16, mdw;
+    CUtensorMap mdy, mx, mdy16, mx16, mdy1, mx1, mdw;
     const bool f32 = dw_type == CRC_F32;
     const cuuint64_t es = f32 ? 4 : 2;
     const cuuint64_t dims[3] = {(cuuint64_t)v.k, (cuuint64_t)v.n, (cuuint64_t)v.N};
     const cuuint64_t strides[2] = {v.k * es, (cuuint64_t)v.n * v.k * es};
     const cuuint32_t box[3] = {f32 ? 32u : 64u, 32, 1};
     if (!rows_map(&mdy, false, dy_dev, E, v.n, v.n, kGwRows) ||
-        !rows_map(&mx, false, x_dev, x_rows, v.k, x_stride, rows_dev ? 1 : kGwRows) ||
+        !rows_map(&mx, false, x_dev, x_rows, v.k, x_stride, kGwRows) ||
         !rows_map(&mdy16, false, dy_dev, E, v.n, v.n, 16) ||
         !rows_map(&mx16, false, x_dev, x_rows, v.k, x_stride, 16) ||
+        !rows_map(&mdy1, false, dy_dev, E, v.n, v.n, 1) ||
+        !rows_map(&mx1, false, x_dev, x_rows, v.k, x_stride, 1) ||
         !encode(&mdw, f32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : kBf16Map, 3, dw_dev, dims, strides,
                 box))
         return CRC_ECUDA;
@@ -272,7 +274,7 @@ int crc_group_matmul_grad(const crc_group_weights* w, const uint16_t* dy_dev,
     {
         ProfScope prof(CRC_KERNEL_GROUP, st);
         e = launch_dependent(kern, dim3((unsigned)sm_count()), kGwThreads, smem, st, 1, mdy, mx,
-                             mdy16, mx16, mdw, a);
+                             mdy16, mx16, mdy1, mx1, mdw, a);
     }
     note_launch();
     return cuda_status(e);

@@ -2,19 +2,20 @@
 //
 // The contraction runs over an expert's rows, so both operands lie across it (MN-major): a
 // block is 64 rows of dy and x as they are in memory, 128 columns of dy (the 128 rows of
-// tcgen05.mma's A) and 256 of x (its N).  The last block of an expert holds rows of the next
-// one: those up to the next 16 are zeroed in shared memory (both operands: a product with
-// another expert's infinity would not be zero), and the steps behind them are left out, as
-// their loads are.
+// tcgen05.mma's A) and 256 of x (its N).  An expert's last rows, when they are not sixteen, come
+// four at a time by their numbers, out of range behind the last one, where TMA fills in zeros: no
+// product has another expert's rows in it.  (With zeros in one operand alone their infinities would
+// not vanish.  Cleared in shared memory instead, the fence behind it, which waits for copies in
+// flight, cost 4%.)
 //
 // What bounds it: an expert has some hundred rows, so a tile's 32768 sums are written after a
 // few blocks, 128 KB in fp32; the writes of dW are most of its bytes.  Tiles leave through
 // shared memory by TMA.  An expert without rows has zeros.  4096 tokens x 8 (128 experts of
-// 2048 x 768, fp32) take 190 us, 121 without the stores, of 146 that the bytes take; 613 tokens x
-// 4, gathered (32 experts of 5760 x 2880, bf16), 255 of 160: TMA takes some 20 ns for four
-// gathered rows of 64 columns, 198 us in all.  (On CTA pairs, which gather half as much, the
-// blocks went through another warp and barrier and it took 321; with x as the 128 rows of A,
-// stores of 64-byte rows, 295.)
+// 2048 x 768, fp32) take 186 us, 111 without the stores, of 146 that the bytes take; 613 tokens x
+// 4, gathered (32 experts of 5760 x 2880, bf16), 249 of 160: TMA takes some 20 ns for four
+// gathered rows of 64 columns, 198 us in all.  (On CTA pairs, which gather half as much, 311 and
+// 207: a tile is a few blocks, and two CTAs wait for each other at each; with x as the 128 rows of
+// A, stores of 64-byte rows, 295.)
 //
 // Work: tiles of (expert, 128 rows, 256 columns of dW), dealt to the CTAs in turn, so that
 // those running together share an expert's rows in L2.
@@ -32,8 +33,9 @@ constexpr int kGwA = kGwRows * kGwM * 2, kGwB = kGwRows * kGwN * 2, kGwStage = k
 constexpr int kGwChunk = kGwRows * 128;    // 64 columns of a block
 // Rows that one accumulator sums for fp32 gradients; of more, the second half goes to the other
 // one and the two are added in fp32, because the tensor cores cut a sum's low bits at each step of
-// 16 rows.  Error of dW in the mean square and time, 4096 tokens x 8: always one accumulator 0.8 to
-// 1.0e-6, 189 us; two above 1024 rows 0.55e-6, 195; above 512 0.45e-6, 207; above 256 0.4e-6, 225.
+// 16 rows.  Error of dW in the mean square for 4096 tokens x 8 with one accumulator always 0.8 to
+// 1.0e-6; with two above 1024 rows 0.55e-6 for 3% more time, above 512 0.45e-6 for 10%, above 256
+// 0.4e-6 for 19%.
 constexpr int kGwPart = 1024;
 constexpr int kGwStages = 4;
 constexpr int kGwBufs = 1;                 // pieces of 32 rows x 128 bytes of an epilogue warp
@@ -64,24 +66,14 @@ __device__ __forceinline__ int half_of(int count) {
     return ((count + kGwRows - 1) / kGwRows + 1) / 2 * kGwRows;
 }
 
-// Rows `tail` .. of a block's six pieces of 64 columns, to the next 16: zeros.
-__device__ __forceinline__ void clear_rows(uint8_t* stage, int tail, int lane) {
-    const int end = (tail + 15) / 16 * 16, pieces = (end - tail) * 8;      // of 16 bytes
-#pragma unroll 1
-    for (int c = 0; c < kGwStage / kGwChunk; ++c)
-        for (int i = lane; i < pieces; i += 32)
-            *reinterpret_cast<uint4*>(stage + c * kGwChunk + tail * 128 + i * 16) =
-                make_uint4(0, 0, 0, 0);
-    fence_proxy_async_smem();
-    __syncwarp();
-}
-
 template <bool F32>
 __global__ void __launch_bounds__(kGwThreads, 1)
     group_weights_grad_kernel(const __grid_constant__ CUtensorMap mdy,
                               const __grid_constant__ CUtensorMap mx,
                               const __grid_constant__ CUtensorMap mdy16,
                               const __grid_constant__ CUtensorMap mx16,
+                              const __grid_constant__ CUtensorMap mdy1,
+                              const __grid_constant__ CUtensorMap mx1,
                               const __grid_constant__ CUtensorMap mdw, GroupGradArgs a) {
     extern __shared__ __align__(1024) uint8_t smem_raw[];
     __shared__ GroupPlan plan;
@@ -111,6 +103,8 @@ __global__ void __launch_bounds__(kGwThreads, 1)
         tma_prefetch_desc(&mx);
         tma_prefetch_desc(&mdy16);
         tma_prefetch_desc(&mx16);
+        tma_prefetch_desc(&mdy1);
+        tma_prefetch_desc(&mx1);
         tma_prefetch_desc(&mdw);
     }
     if (warp == 1) {
@@ -145,23 +139,36 @@ __global__ void __launch_bounds__(kGwThreads, 1)
                     break;
                 }
                 uint8_t* s = smem + stage * kGwStage + (is_x ? kGwA : 0);
-                const int some = round16(count - r);
+                const int left = min(count - r, kGwRows), some = round16(left);
                 if (lead)
                     mbar_arrive_expect_tx(&full_bar[stage], (is_x ? kGwN : kGwM) / 64 * some * 128);
-                if (some == kGwRows) {
+                const uint32_t fb = smem_u32(&full_bar[stage]);
+                if (left == kGwRows) {
 #pragma unroll
                     for (int c = 0; c < kGwN / 64; ++c)
                         if (is_x || c < kGwM / 64)
-                            tma_load_2d_of<false>(lead, s + c * kGwChunk, is_x ? &mx : &mdy,
-                                           smem_u32(&full_bar[stage]), col + c * 64, row0 + r, pol);
+                            tma_load_2d_of<false>(lead, s + c * kGwChunk, is_x ? &mx : &mdy, fb,
+                                                  col + c * 64, row0 + r, pol);
                 } else {
-                    for (int q = 0; q < some; q += 16)
+                    int q = 0;
+                    for (; q + 16 <= left; q += 16)
 #pragma unroll
                         for (int c = 0; c < kGwN / 64; ++c)
                             if (is_x || c < kGwM / 64)
                                 tma_load_2d_of<false>(lead, s + c * kGwChunk + q * 128,
-                                               is_x ? &mx16 : &mdy16, smem_u32(&full_bar[stage]),
-                                               col + c * 64, row0 + r + q, pol);
+                                                      is_x ? &mx16 : &mdy16, fb, col + c * 64,
+                                                      row0 + r + q, pol);
+                    for (; q < some; q += 4) {
+                        int src[4];
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) src[i] = q + i < left ? row0 + r + q + i : -1;
+#pragma unroll
+                        for (int c = 0; c < kGwN / 64; ++c)
+                            if (is_x || c < kGwM / 64)
+                                tma_gather4_of<false>(lead, s + c * kGwChunk + q * 128,
+                                                      is_x ? &mx1 : &mdy1, fb, col + c * 64, src,
+                                                      pol);
+                    }
                 }
                 ++issued;
                 if (++stage == kGwStages) {
@@ -196,9 +203,10 @@ __global__ void __launch_bounds__(kGwThreads, 1)
             const int e = (int)(w / tiles), tile = (int)(w % tiles);
             const int count = plan.count[e], row0 = plan.begin[e];
             const int col = tile % a.ntiles * kGwN;
-            // behind the last row: that row again
+            // behind the last row: out of range
             const auto look = [&](int r) {
-                return source_row(a.r, row0 + min(r + at + (lane & 7), count - 1));
+                const int i = r + at + (lane & 7);
+                return i < count ? source_row(a.r, row0 + i) : -1;
             };
             int next = count > 0 ? look(0) : 0;
             for (int r = 0; r < count; r += kGwRows) {
@@ -220,7 +228,7 @@ __global__ void __launch_bounds__(kGwThreads, 1)
                     for (int c = 0; c < kGwN / 64; ++c)
 #pragma unroll
                         for (int q = 0; q < 2; ++q)
-                            tma_gather4_of<false>(lead, s + c * kGwChunk + q * 512, &mx, smem_u32(&full_bar[stage]),
+                            tma_gather4_of<false>(lead, s + c * kGwChunk + q * 512, &mx1, smem_u32(&full_bar[stage]),
                                            col + c * 64, src[q], pol);
                 if (++stage == kGwStages) {
                     stage = 0;
@@ -266,7 +274,6 @@ __global__ void __launch_bounds__(kGwThreads, 1)
                 }
                 const int some = min(count - r, kGwRows);
                 uint8_t* s = smem + stage * kGwStage;
-                if (some % 16) clear_rows(s, some, lane);
                 tc_fence_after();
                 const uint32_t sa = smem_u32(s), sb = sa + kGwA;
 #pragma unroll
