@@ -44,6 +44,15 @@ __device__ __forceinline__ uint32_t elected() {
         : "=r"(r));
     return r;
 }
+// An arrival by the lane whose `lead` is set.  (As a branch of that lane, in the warps that gather
+// rows: 217 us instead of 189 for the first product of 4096 tokens of 128 experts.)
+__device__ __forceinline__ void arrive_by(uint64_t* bar, uint32_t lead) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %1, 0;\n\t"
+        "@p mbarrier.arrive.shared::cta.b64 _, [%0];\n\t}" ::"r"(smem_u32(bar)),
+        "r"(lead)
+        : "memory");
+}
 // Issued by the lane whose `lead` is set, in code that the whole warp runs: the descriptors
 // stay in uniform registers, where the instruction wants them.  (In a branch of one lane each
 // MMA took 85 ns, whatever its columns.)

@@ -128,8 +128,8 @@ __global__ void __launch_bounds__(kGmThreads, 1)
 
     if (threadIdx.x == 0) {
         for (int s = 0; s < kGmStages; ++s) {
-            mbar_init(&full_bar[s], 2);                // the weights' producer and the rows'
-            mbar_init(&empty_bar[s], 1);
+            mbar_init(&full_bar[s], 2);                // the matrix's producer and the rows'
+            mbar_init(&empty_bar[s], 1 + (a.r.rows ? kGmGatherWarps : 0));
         }
         for (int s = 0; s < 2; ++s) {
             mbar_init(&tfull_bar[s], 1);
@@ -272,16 +272,19 @@ __global__ void __launch_bounds__(kGmThreads, 1)
                     latch_error(a.r.err, CRC_ETIMEOUT);
                     break;
                 }
-                if (leader && w == 0 && lead)
-                    mbar_arrive_expect_tx(&full_bar[stage], kCtas * half * 128);
                 uint8_t* sb = smem + stage * kGmStage + kGmA;
                 const uint32_t fb = lead_full + (uint32_t)(stage * 8);
+                if (leader && w == 0 && lead)
+                    mbar_arrive_expect_tx(&full_bar[stage], kCtas * half * 128);
 #pragma unroll
                 for (int q = 0; q < 4; ++q) {
                     const int f = w + kGmGatherWarps * q;
                     if (f < half / 4)
                         tma_gather4_of<Pair>(lead, sb + f * 512, &mx, fb, kb * kElems, src[q], pol);
                 }
+                // A warp without rows in this tile would hold nothing back, and miss a turn if it
+                // came late by a whole one: the stage is not empty again before each has been here.
+                arrive_by(&empty_bar[stage], lead);
                 if (++stage == kGmStages) {
                     stage = 0;
                     phase ^= 1;

@@ -91,7 +91,7 @@ __global__ void __launch_bounds__(kGwThreads, 1)
     if (threadIdx.x == 0) {
         for (int s = 0; s < kGwStages; ++s) {
             mbar_init(&full_bar[s], 2);                // dy and x
-            mbar_init(&empty_bar[s], 1);
+            mbar_init(&empty_bar[s], 1 + (a.r.rows ? 8 : 0));
         }
         for (int s = 0; s < 2; ++s) {
             mbar_init(&tfull_bar[s], 1);
@@ -230,6 +230,9 @@ __global__ void __launch_bounds__(kGwThreads, 1)
                         for (int q = 0; q < 2; ++q)
                             tma_gather4_of<false>(lead, s + c * kGwChunk + q * 512, &mx1, smem_u32(&full_bar[stage]),
                                            col + c * 64, src[q], pol);
+                // A warp without rows in this block would hold nothing back, and miss a turn if it
+                // came late by a whole one: the stage is not empty again before each has been here.
+                arrive_by(&empty_bar[stage], lead);
                 if (++stage == kGwStages) {
                     stage = 0;
                     phase ^= 1;

@@ -474,3 +474,26 @@ def test_training_step_of_the_layer(P):
         # the choice's row, the sum), each 2^-8 of its value at most, in sums of either sign
         e = (got.double() - w).norm() / w.norm()
         assert e <= 7 * U16, name
+
+
+@pytest.mark.parametrize("N,k,n,counts", [
+    (128, 2048, 256, [1]), (128, 2048, 256, [9, 1, 2]), (32, 256, 512, [1]), (4, 1024, 2048, [3]),
+    (2, 640, 512, [1, 130]), (8, 4096, 128, [16, 1]),
+])
+def test_few_gathered_rows_again_and_again(P, N, k, n, counts):
+    """Some of the warps that gather have no rows; none of them misses a turn of the ring."""
+    g = torch.Generator(device="cuda").manual_seed(N + k)
+    counts = (counts * N)[:N]
+    E = sum(counts)
+    x, w = randn(g, E, k), randn(g, N, n, k)
+    rows = torch.randperm(E, device="cuda", generator=g).to(torch.int32)
+    off = offsets_of(counts)
+    dy = randn(g, E, n)
+    first = P.group_matmul(x, w, off, rows=rows, K=1)
+    _, dw = P.group_matmul_grad(dy, x, w, off, rows=rows, K=1, want_dx=False)
+    again, dwa = torch.empty_like(first), torch.empty_like(dw)
+    for _ in range(1000):
+        P.group_matmul(x, w, off, rows=rows, K=1, y=again)
+        P.group_matmul_grad(dy, x, w, off, rows=rows, K=1, want_dx=False, dw=dwa)
+    assert P.crc.crc_device_error() == 0
+    assert torch.equal(first, again) and torch.equal(dw, dwa)
