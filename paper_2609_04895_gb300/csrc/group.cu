@@ -59,8 +59,8 @@ bool glu_map(CUtensorMap* m, const crc_group_weights& w) {
 }
 
 template <bool W8, bool GLU, bool TW, bool Pair>
-int launch_products_on(const CUtensorMap& mw, const CUtensorMap& mx, GroupArgs& a,
-                       cudaStream_t st) {
+int launch_products_on(const CUtensorMap& mw, const CUtensorMap& mx, const CUtensorMap& mx8,
+                       GroupArgs& a, cudaStream_t st) {
     auto kern = group_matmul_kernel<W8, GLU, TW, Pair>;
     constexpr size_t smem = GroupSmem::bytes();
     constexpr int kRows = (GLU ? 64 : 128) * (Pair ? 2 : 1);      // columns of y of a tile
@@ -91,14 +91,15 @@ int launch_products_on(const CUtensorMap& mw, const CUtensorMap& mx, GroupArgs& 
     {
         ProfScope prof(CRC_KERNEL_GROUP, st);
         e = launch_dependent(kern, dim3((unsigned)(Pair ? 2 * fit : fit)), kGmThreads, smem, st,
-                             Pair ? 2 : 1, mw, mx, a);
+                             Pair ? 2 : 1, mw, mx, mx8, a);
     }
     note_launch();
     return cuda_status(e);
 }
 
 template <bool W8, bool GLU, bool TW>
-int launch_products(const CUtensorMap& mw, const CUtensorMap& mx, GroupArgs& a, cudaStream_t st) {
+int launch_products(const CUtensorMap& mw, const CUtensorMap& mx, const CUtensorMap& mx8,
+                    GroupArgs& a, cudaStream_t st) {
     // CTAs by themselves for few rows an expert, in order, or gathered from short rows.  Us, by
     // themselves / pairs: the second product of 60 tokens of the 32-expert shape (7 rows an
     // expert) 68.6 / 76.7, in 8 bits 36.9 / 41.8, its gradient's rows 66.2 / 73.4; of 200 tokens
@@ -108,8 +109,8 @@ int launch_products(const CUtensorMap& mw, const CUtensorMap& mx, GroupArgs& a, 
     // of d = 256.
     const bool single = (long long)a.r.E <= (long long)kSingleRows * a.r.N &&
                         (!a.r.rows || a.kblocks <= kShortRows);
-    return single ? launch_products_on<W8, GLU, TW, false>(mw, mx, a, st)
-                  : launch_products_on<W8, GLU, TW, true>(mw, mx, a, st);
+    return single ? launch_products_on<W8, GLU, TW, false>(mw, mx, mx8, a, st)
+                  : launch_products_on<W8, GLU, TW, true>(mw, mx, mx8, a, st);
 }
 
 int check_weights(const crc_group_weights* w) {
@@ -181,10 +182,12 @@ int crc_group_matmul(const crc_group_weights* w, const void* x_dev, int64_t x_st
     if (!x_dev || !aligned(x_dev, 16) || !offsets_dev || !aligned(offsets_dev, 4) || !y_dev ||
         !aligned(y_dev, 16))
         return CRC_EINVAL;
-    CUtensorMap mw, mx;
+    CUtensorMap mw, mx, mx8;
     if (!(w->glu ? glu_map(&mw, *w) : matrix_map(&mw, *w, w8 ? 128 : 64, 128)) ||
-        !rows_map(&mx, w8, x_dev, x_rows, w->k, x_stride, rows_dev ? 1 : kGmBoxRows))
+        !rows_map(&mx, w8, x_dev, x_rows, w->k, x_stride, rows_dev ? 1 : kGmBoxRows) ||
+        !(rows_dev || rows_map(&mx8, w8, x_dev, x_rows, w->k, x_stride, kGmLastRows)))
         return CRC_ECUDA;
+    if (rows_dev) mx8 = mx;                    // (not used)
     GroupArgs a = {};
     a.r = group_rows(*w, offsets_dev, rows_dev, K, x_rows, E);
     a.y = y_dev;
@@ -195,10 +198,10 @@ int crc_group_matmul(const crc_group_weights* w, const void* x_dev, int64_t x_st
     a.out = w->n;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     if (w8)
-        return w->glu ? launch_products<true, true, false>(mw, mx, a, st)
-                      : launch_products<true, false, false>(mw, mx, a, st);
-    return w->glu ? launch_products<false, true, false>(mw, mx, a, st)
-                  : launch_products<false, false, false>(mw, mx, a, st);
+        return w->glu ? launch_products<true, true, false>(mw, mx, mx8, a, st)
+                      : launch_products<true, false, false>(mw, mx, mx8, a, st);
+    return w->glu ? launch_products<false, true, false>(mw, mx, mx8, a, st)
+                  : launch_products<false, false, false>(mw, mx, mx8, a, st);
 }
 
 int crc_group_matmul_grad(const crc_group_weights* w, const uint16_t* dy_dev,
@@ -229,15 +232,16 @@ int crc_group_matmul_grad(const crc_group_weights* w, const uint16_t* dy_dev,
         (dw_dev && (!x_dev || !aligned(x_dev, 16))))
         return CRC_EINVAL;
     if (dx_dev) {
-        CUtensorMap mw, mdy;
-        if (!matrix_map(&mw, v, 64, 64) || !rows_map(&mdy, false, dy_dev, E, v.n, v.n, kGmBoxRows))
+        CUtensorMap mw, mdy, mdy8;
+        if (!matrix_map(&mw, v, 64, 64) || !rows_map(&mdy, false, dy_dev, E, v.n, v.n, kGmBoxRows) ||
+            !rows_map(&mdy8, false, dy_dev, E, v.n, v.n, kGmLastRows))
             return CRC_ECUDA;
         GroupArgs a = {};
         a.r = group_rows(v, offsets_dev, nullptr, 1, E, E);
         a.y = dx_dev;
         a.kblocks = (v.n + 63) / 64;
         a.out = v.k;
-        rc = launch_products<false, false, true>(mw, mdy, a, st);
+        rc = launch_products<false, false, true>(mw, mdy, mdy8, a, st);
         if (rc) return rc;
     }
     if (!dw_dev) return CRC_OK;

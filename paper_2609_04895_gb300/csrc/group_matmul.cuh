@@ -35,7 +35,10 @@ constexpr int kGmA = 128 * 128, kGmB = 128 * 128, kGmStage = kGmA + kGmB;   // b
 constexpr int kGmUnit = 16, kGmTileUnits = 16;       // rows of a unit, units of a pair's tile
 constexpr int kGmStaging = 2 * 32 * 256;   // two pieces of 32 rows x 128 columns of y
 constexpr int kGmScales = 2 * 256 * 4;     // the scales of a tile's rows, of two tiles
-constexpr int kGmBoxRows = 32;             // rows of a TMA box of x in order
+// Rows of a TMA box of x in order: eight for a CTA with less than 32, which load in time what they
+// hold (the second product of one token of 32 experts of 5760 x 2880, 4 of them read, 22 us with
+// boxes of 32 and 12.3 now; of 128 of 1536 x 2048, 9.0 and 6.3).
+constexpr int kGmBoxRows = 32, kGmLastRows = 8;
 
 struct GroupArgs {
     GroupRows r;
@@ -94,6 +97,13 @@ __device__ __forceinline__ float gm_silu_up(float gate, float up) {
     return __fdividef(gate, 1.f + __expf(-gate)) * up;
 }
 
+// Rows that a CTA of the tile loads, of `half` that are its: those there are, to the next `unit`,
+// one of them at least, so that the ring waits for it.  (What the columns behind them hold does
+// not matter: a column of the product is a row's own.)
+__device__ __forceinline__ int loaded_rows(const GroupTile& t, int half, int rank, int unit) {
+    return (min(max(t.rows - rank * half, 1), half) + unit - 1) / unit * unit;
+}
+
 struct GroupSmem {
     static constexpr size_t bytes() {
         return 1024 + (size_t)kGmStages * kGmStage + kGmStaging + kGmScales + sizeof(GroupPlan) + 512;
@@ -105,7 +115,8 @@ struct GroupSmem {
 template <bool W8, bool GLU, bool TW, bool Pair>
 __global__ void __launch_bounds__(kGmThreads, 1)
     group_matmul_kernel(const __grid_constant__ CUtensorMap mw,
-                        const __grid_constant__ CUtensorMap mx, GroupArgs a) {
+                        const __grid_constant__ CUtensorMap mx,
+                        const __grid_constant__ CUtensorMap mx8, GroupArgs a) {
     constexpr int kElems = W8 ? 128 : 64;              // elements of a 128-byte piece
     constexpr int kCtas = Pair ? 2 : 1;                // CTAs of a tile
     extern __shared__ __align__(1024) uint8_t smem_raw[];
@@ -139,6 +150,7 @@ __global__ void __launch_bounds__(kGmThreads, 1)
         fence_mbar_init();
         tma_prefetch_desc(&mw);
         tma_prefetch_desc(&mx);
+        tma_prefetch_desc(&mx8);
     }
     if (warp == 1) {
         if constexpr (Pair) {
@@ -224,7 +236,10 @@ __global__ void __launch_bounds__(kGmThreads, 1)
             const GroupTile t = group_tile<Pair>(plan, a.r.N, a.ftiles, i);
             const int half = (t.rows + kGmUnit - 1) / kGmUnit * (kGmUnit / kCtas);
             const int first = t.row + (int)rank * half;                // this CTA's rows
-            const int boxes = (half + kGmBoxRows - 1) / kGmBoxRows;
+            const int unit = half < kGmBoxRows ? kGmLastRows : kGmBoxRows;
+            const int mine = loaded_rows(t, half, (int)rank, unit);
+            const int all = loaded_rows(t, half, 0, unit) +
+                            (Pair ? loaded_rows(t, half, 1, unit) : 0);
             for (int kb = 0; kb < a.kblocks; ++kb) {
                 ok = __all_sync(kFull, mbar_wait_cluster(&empty_bar[stage], phase ^ 1));
                 if (!ok) {
@@ -233,11 +248,11 @@ __global__ void __launch_bounds__(kGmThreads, 1)
                 }
                 uint8_t* sb = smem + stage * kGmStage + kGmA;
                 if (leader && lead)
-                    mbar_arrive_expect_tx(&full_bar[stage], kCtas * boxes * kGmBoxRows * 128);
+                    mbar_arrive_expect_tx(&full_bar[stage], all * 128);
                 const uint32_t fb = lead_full + (uint32_t)(stage * 8);
-                for (int b = 0; b < boxes; ++b)
-                    tma_load_2d_of<Pair>(lead, sb + b * kGmBoxRows * 128, &mx, fb, kb * kElems,
-                                        first + b * kGmBoxRows, pol);
+                for (int b = 0; b < mine; b += unit)
+                    tma_load_2d_of<Pair>(lead, sb + b * 128, unit == kGmBoxRows ? &mx : &mx8, fb,
+                                         kb * kElems, first + b, pol);
                 if (++stage == kGmStages) {
                     stage = 0;
                     phase ^= 1;
@@ -257,10 +272,12 @@ __global__ void __launch_bounds__(kGmThreads, 1)
         for (long long i = pair; i < tiles && ok; i += pairs) {
             const GroupTile t = group_tile<Pair>(plan, a.r.N, a.ftiles, i);
             const int half = (t.rows + kGmUnit - 1) / kGmUnit * (kGmUnit / kCtas);
+            const int fours = loaded_rows(t, half, (int)rank, 4) / 4;
+            const int all = loaded_rows(t, half, 0, 4) + (Pair ? loaded_rows(t, half, 1, 4) : 0);
             int mine = 0, src[4][4];
             {
                 const int f = w + kGmGatherWarps * ((lane >> 2) & 3);
-                if (f < half / 4)                       // behind the last row: that row again
+                if (f < fours)                          // behind the last row: that row again
                     mine = source_row(a.r, t.row + min((int)rank * half + f * 4 + (lane & 3),
                                                        t.rows - 1));
             }
@@ -275,11 +292,11 @@ __global__ void __launch_bounds__(kGmThreads, 1)
                 uint8_t* sb = smem + stage * kGmStage + kGmA;
                 const uint32_t fb = lead_full + (uint32_t)(stage * 8);
                 if (leader && w == 0 && lead)
-                    mbar_arrive_expect_tx(&full_bar[stage], kCtas * half * 128);
+                    mbar_arrive_expect_tx(&full_bar[stage], all * 128);
 #pragma unroll
                 for (int q = 0; q < 4; ++q) {
                     const int f = w + kGmGatherWarps * q;
-                    if (f < half / 4)
+                    if (f < fours)
                         tma_gather4_of<Pair>(lead, sb + f * 512, &mx, fb, kb * kElems, src[q], pol);
                 }
                 // A warp without rows in this tile would hold nothing back, and miss a turn if it
