@@ -23,7 +23,7 @@ bool encode(CUtensorMap* m, CUtensorMapDataType type, int rank, const void* base
                       CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-constexpr int kSingleRows = 48, kShortRows = 8;
+constexpr int kSingleRows = 48, kGatheredRows = 16, kShortRows = 8;
 
 constexpr CUtensorMapDataType kBf16Map = CU_TENSOR_MAP_DATA_TYPE_BFLOAT16;
 
@@ -100,15 +100,16 @@ int launch_products_on(const CUtensorMap& mw, const CUtensorMap& mx, const CUten
 template <bool W8, bool GLU, bool TW>
 int launch_products(const CUtensorMap& mw, const CUtensorMap& mx, const CUtensorMap& mx8,
                     GroupArgs& a, cudaStream_t st) {
-    // CTAs by themselves for few rows an expert, in order, or gathered from short rows.  Us, by
-    // themselves / pairs: the second product of 60 tokens of the 32-expert shape (7 rows an
-    // expert) 68.6 / 76.7, in 8 bits 36.9 / 41.8, its gradient's rows 66.2 / 73.4; of 200 tokens
-    // of the 128-expert shape 58.0 / 58.9, 8 bits 32.6 / 41.8; with 62 rows an expert 71.8 / 69.9,
-    // with 93 53.7 / 53.1, gradient 51.3 / 51.8.  The first product, gathered: 60 tokens of the
-    // 32-expert shape in 8 bits 80.9 / 72.9, one token 25.5 / 20.2, but 5.5 / 7.4 for 300 tokens
-    // of d = 256.
-    const bool single = (long long)a.r.E <= (long long)kSingleRows * a.r.N &&
-                        (!a.r.rows || a.kblocks <= kShortRows);
+    // CTAs by themselves for few rows an expert, fewer if they are gathered from long rows (a
+    // pair gathers a tile's rows once, two CTAs by themselves twice).  Us, by themselves / pairs:
+    // the second product of 60 tokens of the 32-expert shape (7 rows an expert) 68.6 / 76.7, in 8
+    // bits 36.9 / 41.8, its gradient's rows 66.2 / 73.4; of 200 tokens of the 128-expert shape
+    // 58.0 / 58.9, 8 bits 32.6 / 41.8; with 62 rows an expert 71.8 / 69.9, with 93 53.7 / 53.1,
+    // gradient 51.3 / 51.8.  The first product, gathered: one token of the 128-expert shape 12.8 /
+    // 13.7, in 8 bits 8.5 / 9.5, 200 tokens (12 rows an expert) 112.9 / 114.8, 500 (31) 129.8 /
+    // 125.8, 300 of the d = 4096 shape (18) 459 / 453; 5.5 / 7.4 for 300 tokens of d = 256.
+    const int most = a.r.rows && a.kblocks > kShortRows ? kGatheredRows : kSingleRows;
+    const bool single = (long long)a.r.E <= (long long)most * a.r.N;
     return single ? launch_products_on<W8, GLU, TW, false>(mw, mx, mx8, a, st)
                   : launch_products_on<W8, GLU, TW, true>(mw, mx, mx8, a, st);
 }
