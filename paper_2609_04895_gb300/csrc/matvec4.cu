@@ -347,9 +347,11 @@ __global__ void __launch_bounds__(kThreads, kCtas)
     ring.turn = 0;
     float* sums = reinterpret_cast<float*>(smem + kWarps * kStages * kStageBytes);
     uint32_t* list = reinterpret_cast<uint32_t*>(sums + (a.splits > 1 ? 2 * kSums : 0));
-    if (threadIdx.x < kWarps * kStages) mbar_init(&full[0][0] + threadIdx.x, 1);
     for (int e = threadIdx.x; e <= a.N; e += kThreads) order.next[e] = 0;
     if (threadIdx.x == 0) {
+        // (one thread: the fence, without which TMA need not see a barrier, is for those that the
+        // thread itself has set up)
+        for (int i = 0; i < kWarps * kStages; ++i) mbar_init(&full[0][0] + i, 1);
         fence_mbar_init();
         tma_prefetch_desc(&mw);
         tma_prefetch_desc(&ms);
