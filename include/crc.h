@@ -629,9 +629,11 @@ int crc_group_matmul(const crc_group_weights *w, const void *x_dev, int64_t x_st
  *             Rows outside the offsets are left as they were.
  *   dw_dev    dw_type (CRC_F32 or CRC_BF16) [N][n][k], 16-byte aligned, zeros for an
  *             expert without rows, or NULL (x_dev is not read then)
- * Sums in fp32, in the order of the rows, without atomics; each output is rounded once.  (The
- * tensor cores cut a sum's low bits where an fp32 addition rounds, every 16 rows, or columns of
- * n: dW is off by up to 1e-6 in the mean square.)
+ * Sums in fp32, in a fixed order, without atomics; each output is rounded once.  The tensor cores
+ * cut a sum's low bits where an fp32 addition rounds, every 16 rows (or columns of n), which
+ * shrinks the sum; an expert's rows are therefore summed in parts of up to 1024 (for dW in bf16
+ * 16384), and the parts added in fp32.  fp32 dW is off by 1.0e-6 of itself in the mean square where
+ * the products have either sign, by 2.2e-6 where they have one, however many rows there are.
  * E = 0 sets dw to zero. */
 int crc_group_matmul_grad(const crc_group_weights *w, const uint16_t *dy_dev,
                           const uint16_t *x_dev, int64_t x_stride, int64_t x_rows,

@@ -31,12 +31,18 @@ constexpr int kGwRows = 64;                // rows of a block
 constexpr int kGwM = 128, kGwN = 256;
 constexpr int kGwA = kGwRows * kGwM * 2, kGwB = kGwRows * kGwN * 2, kGwStage = kGwA + kGwB;
 constexpr int kGwChunk = kGwRows * 128;    // 64 columns of a block
-// Rows that one accumulator sums for fp32 gradients; of more, the second half goes to the other
-// one and the two are added in fp32, because the tensor cores cut a sum's low bits at each step of
-// 16 rows.  Error of dW in the mean square for 4096 tokens x 8 with one accumulator always 0.8 to
-// 1.0e-6; with two above 1024 rows 0.55e-6 for 3% more time, above 512 0.45e-6 for 10%, above 256
-// 0.4e-6 for 19%.
-constexpr int kGwPart = 1024;
+// Rows that one accumulator sums, at most: the tensor cores cut a sum's low bits at each step of 16
+// rows, so a sum shrinks by an error that grows with its steps.  More rows are parts of one size,
+// the first in one accumulator, the others in turn in the second one, and are added in fp32.
+// Error of fp32 dW in the mean square, of itself, for operands of either sign (of one sign): 256 rows
+// 2.3e-7, 1024 and more 1.0e-6 (2.2e-6); in two accumulators whatever the rows 8192 had 4.4e-6
+// (1.4e-5), 32768 1.9e-5 (8.3e-5).  Above two parts the second accumulator is drained between parts
+// while the tensor cores wait.  Us for 32 experts of 2048 x 768, two accumulators whatever the
+// rows / parts: 1024 rows each 91 / 91, 2048 175 / 180, 4096 312 / 324, 8192 587 / 609.  (Parts of 512
+// rows: 0.45e-6 for 10% from there on.)
+// bf16 dW is off by half a step of 2^-8 anyway: 16384 rows shrink a sum by 8e-5 of itself at most.
+template <bool F32>
+constexpr int kGwPart = F32 ? 1024 : 16384;
 constexpr int kGwStages = 4;
 constexpr int kGwBufs = 1;                 // pieces of 32 rows x 128 bytes of an epilogue warp
 constexpr int kGwStaging = 4 * kGwBufs * 4096;
@@ -59,11 +65,12 @@ __device__ __forceinline__ int round16(int left) {
     return left >= kGwRows ? kGwRows : (left + 15) / 16 * 16;
 }
 
-// The first row of an expert's second accumulator, `count` where it has one.
+// Rows of a part of an expert's `count`, a multiple of kGwRows where there are several parts.
 template <bool F32>
-__device__ __forceinline__ int half_of(int count) {
-    if (!F32 || count <= kGwPart) return count;
-    return ((count + kGwRows - 1) / kGwRows + 1) / 2 * kGwRows;
+__device__ __forceinline__ int part_of(int count) {
+    if (count <= kGwPart<F32>) return count;
+    const int parts = (count + kGwPart<F32> - 1) / kGwPart<F32>;
+    return ((count + parts - 1) / parts + kGwRows - 1) / kGwRows * kGwRows;
 }
 
 template <bool F32>
@@ -244,32 +251,31 @@ __global__ void __launch_bounds__(kGwThreads, 1)
         constexpr uint32_t kIdesc = idesc_bf16_f32(kGwM, kGwN) | kIdescMnA | kIdescMnB;
         const uint32_t lead = elected();
         int stage = 0, acc = 0;
-        uint32_t phase = 0, acc_phase = 0;
+        uint32_t phase = 0, used = 0;                    // used: bit a, accumulator a's phase
         bool ok = true;
+        const auto take = [&](int at) {
+            ok = mbar_wait_warp(&tempty_bar[at], (used >> at & 1) ^ 1);
+            if (!ok) latch_error(a.r.err, CRC_ETIMEOUT);
+            tc_fence_after();
+        };
         for (long long w = blockIdx.x; w < all && ok; w += gridDim.x) {
             const int count = plan.count[(int)(w / tiles)];
             if (count == 0) continue;
-            ok = mbar_wait_warp(&tempty_bar[acc], acc_phase ^ 1);
-            if (!ok) {
-                latch_error(a.r.err, CRC_ETIMEOUT);
-                break;
-            }
-            tc_fence_after();
-            const int half = half_of<F32>(count);
-            for (int r = 0; r < count; r += kGwRows) {
-                if (r == half) {
-                    commit_by(&tfull_bar[acc], lead);
-                    acc ^= 1;
-                    if (acc == 0) acc_phase ^= 1;
-                    ok = mbar_wait_warp(&tempty_bar[acc], acc_phase ^ 1);
-                    if (!ok) {
-                        latch_error(a.r.err, CRC_ETIMEOUT);
-                        break;
-                    }
-                    tc_fence_after();
+            take(acc);
+            const int part = part_of<F32>(count);
+            int cur = acc, next = part;                  // next: the first row of the next part
+            bool first = true;
+            for (int r = 0; r < count && ok; r += kGwRows) {
+                if (r == next) {
+                    commit_by(&tfull_bar[cur], lead);
+                    used ^= 1u << cur;
+                    cur = acc ^ 1;
+                    next += part;
+                    first = true;
+                    take(cur);
+                    if (!ok) break;
                 }
-                const uint32_t d_tmem = tmem_base + (uint32_t)(acc * 256);
-                const bool first = r == 0 || r == half;
+                const uint32_t d_tmem = tmem_base + (uint32_t)(cur * 256);
                 ok = mbar_wait_warp(&full_bar[stage], phase);
                 if (!ok) {
                     latch_error(a.r.err, CRC_ETIMEOUT);
@@ -285,6 +291,7 @@ __global__ void __launch_bounds__(kGwThreads, 1)
                         umma_by<false, false>(d_tmem, sw128_mnmajor_desc(sa + kk * 2048, kGwChunk),
                                      sw128_mnmajor_desc(sb + kk * 2048, kGwChunk), kIdesc,
                                      !first || kk != 0, lead);
+                first = false;
                 commit_by(&empty_bar[stage], lead);
                 if (++stage == kGwStages) {
                     stage = 0;
@@ -292,9 +299,9 @@ __global__ void __launch_bounds__(kGwThreads, 1)
                 }
             }
             if (!ok) break;
-            commit_by(&tfull_bar[acc], lead);
-            acc ^= 1;
-            if (acc == 0) acc_phase ^= 1;
+            commit_by(&tfull_bar[cur], lead);
+            used ^= 1u << cur;
+            if (cur == acc) acc ^= 1;
         }
         if (lead) {
             umma_commit(drain_bar);
@@ -306,31 +313,53 @@ __global__ void __launch_bounds__(kGwThreads, 1)
         uint8_t* my_stage = staging + quarter * kGwBufs * 4096;
         constexpr int kCols = F32 ? 32 : 64;             // columns of a 128-byte piece
         int acc = 0, buf = 0;
-        uint32_t acc_phase = 0;
+        uint32_t used = 0;                               // as the MMA warp's
+        const auto full = [&](int at) {
+            const bool ok = mbar_wait_warp(&tfull_bar[at], used >> at & 1);
+            if (!ok) latch_error(a.r.err, CRC_ETIMEOUT);
+            tc_fence_after();
+            return ok;
+        };
+        const auto release = [&](int at) {
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&tempty_bar[at]);
+            used ^= 1u << at;
+        };
         for (long long w = blockIdx.x; w < all; w += gridDim.x) {
             const int e = (int)(w / tiles), tile = (int)(w % tiles);
             const int row = tile / a.ntiles * kGwM + quarter * 32, col = tile % a.ntiles * kGwN;
-            const bool some = plan.count[e] > 0;
-            if (some) {
-                if (!mbar_wait_warp(&tfull_bar[acc], acc_phase)) {
-                    latch_error(a.r.err, CRC_ETIMEOUT);
-                    break;
-                }
-                tc_fence_after();
-            }
-            const uint32_t tbase =
-                tmem_base + (uint32_t)(acc * 256) + ((uint32_t)(quarter * 32) << 16);
-            const bool two = half_of<F32>(plan.count[e]) < plan.count[e];
-            const int acc1 = acc ^ 1;
+            const int count = plan.count[e], part = part_of<F32>(count);
+            const bool some = count > 0, two = part < count;
+            const uint32_t quarters = (uint32_t)(quarter * 32) << 16;
+            const uint32_t tbase = tmem_base + (uint32_t)(acc * 256) + quarters;
+            const uint32_t tbase1 = tmem_base + (uint32_t)((acc ^ 1) * 256) + quarters;
+            if (some && !full(acc)) break;
             if (two) {
-                if (!mbar_wait_warp(&tfull_bar[acc1], acc_phase ^ (acc1 == 0))) {
-                    latch_error(a.r.err, CRC_ETIMEOUT);
-                    break;
+                // every part but the first and the last goes to the first one's accumulator
+                bool ok = true;
+                for (int r = part; ok && r + part < count; r += part) {
+                    ok = full(acc ^ 1);
+                    if (!ok) break;
+#pragma unroll 1
+                    for (int c = 0; c < kGwN; c += 32) {
+                        float v[32], u[32];
+                        tmem_ld32(tbase + (uint32_t)c, v);
+                        tmem_ld32(tbase1 + (uint32_t)c, u);
+                        tmem_ld_wait();
+                        pin16(v);
+                        pin16(v + 16);
+                        pin16(u);
+                        pin16(u + 16);
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) v[i] += u[i];
+                        tmem_st32(tbase + (uint32_t)c, v);
+                    }
+                    tmem_st_wait();
+                    release(acc ^ 1);
                 }
-                tc_fence_after();
+                if (!ok || !full(acc ^ 1)) break;
             }
-            const uint32_t tbase1 =
-                tmem_base + (uint32_t)(acc1 * 256) + ((uint32_t)(quarter * 32) << 16);
 #pragma unroll 1
             for (int c = 0; c < kGwN; c += kCols) {
                 uint4 q[8];
@@ -341,17 +370,16 @@ __global__ void __launch_bounds__(kGwThreads, 1)
                     tmem_ld_wait();
 #pragma unroll
                     for (int i = 0; i < kCols; i += 16) pin16(v + i);
-                    if constexpr (F32) {
-                        if (two) {
-                            float u[kCols];
-                            tmem_ld32(tbase1 + (uint32_t)c, u);
+                    if (two)
+#pragma unroll
+                        for (int i = 0; i < kCols; i += 16) {
+                            float u[16];
+                            tmem_ld16(tbase1 + (uint32_t)(c + i), u);
                             tmem_ld_wait();
                             pin16(u);
-                            pin16(u + 16);
 #pragma unroll
-                            for (int i = 0; i < kCols; ++i) v[i] += u[i];
+                            for (int j = 0; j < 16; ++j) v[i + j] += u[j];
                         }
-                    }
 #pragma unroll
                     for (int j = 0; j < 8; ++j) {
                         uint32_t u[4];
@@ -386,15 +414,11 @@ __global__ void __launch_bounds__(kGwThreads, 1)
                     bulk_commit();
                 }
             }
-            if (some) {
-                tc_fence_before();
-                __syncwarp();
-                for (int k = 0; k < (two ? 2 : 1); ++k) {
-                    if (lane == 0) mbar_arrive(&tempty_bar[acc]);
-                    acc ^= 1;
-                    if (acc == 0) acc_phase ^= 1;
-                }
-            }
+            if (some) release(acc);
+            if (two)
+                release(acc ^ 1);
+            else if (some)
+                acc ^= 1;
         }
         if (lane == 0) bulk_wait<0>();                   // every store has landed
     }
