@@ -958,16 +958,28 @@ class MoeLayer:
         grouped products and sum_choices.  A token's id of N or more has no expert.  Every
         expert e has to lie in slot e (no expert_slot).  With 8-bit experts x and the rows
         between the products are brought to 8 bits, a scale a row."""
+        import torch
         gate_up, down, _, slots, s13, s2 = self.tensors
         if slots is not None:
             raise ValueError("prompts want every expert in its own slot: no expert_slot map")
+        dev = _here(x, "x")
+        if dev != self.device:
+            raise ValueError(f"x lies on cuda:{dev}, the experts on cuda:{self.device}")
+        if topk.dim() != 2:
+            raise ValueError("topk must be a 2-D tensor")
+        # (a topk of other tokens than x's would only show in a call that is under way)
+        M, K = _rows(x, "x")[0], topk.shape[1]
+        _check(x, "x", (M, self.d), torch.bfloat16, dev, False)
+        _check(topk, "topk", (M, K), torch.uint8, dev)
+        _check(gates, "gates", (M, K), torch.float32, dev)
+        _check(out, "out", (M, self.d), torch.bfloat16, dev)
         if s13 is None:
             x8, xs = x, None
         else:
             x8, xs = quantize_rows(x, stream=stream)
         gate_up, down = gate_up[:self.N], down[:self.N]
         offsets, rows, place = group_choices(topk, self.N, stream=stream)
-        h = group_matmul(x8, gate_up, offsets, rows=rows, K=topk.shape[1], x_scale=xs,
+        h = group_matmul(x8, gate_up, offsets, rows=rows, K=K, x_scale=xs,
                          w_scale=None if s13 is None else s13[:self.N], stream=stream)
         hs = None
         if s2 is not None:
