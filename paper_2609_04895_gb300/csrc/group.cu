@@ -143,8 +143,9 @@ int check_rows(int64_t x_stride, int64_t x_rows, const int32_t* rows, int32_t K,
     if (E < 0 || x_rows < 0 || K < 1) return CRC_EINVAL;
     if (x_stride < k || x_stride * es % 16 != 0) return CRC_EINVAL;
     if (E > (1 << 30) || x_rows > (1 << 30) || x_stride > (1 << 30)) return CRC_EUNSUPPORTED;
+    if (E == 0) return CRC_OK;                 // (an array of no rows may have no address)
     if (rows ? !aligned(rows, 4) : (K != 1 || x_rows < E)) return CRC_EINVAL;
-    if (E > 0 && x_rows < 1) return CRC_EINVAL;
+    if (x_rows < 1) return CRC_EINVAL;
     return CRC_OK;
 }
 
