@@ -498,6 +498,14 @@ int crc_rms_norm_grad(const uint16_t *dy_dev, const void *s_dev, const uint16_t 
 int crc_quantize_rows(const uint16_t *x_dev, int64_t x_stride, int64_t M, int32_t d,
                       uint8_t *out8_dev, float *scale8_dev, void *stream);
 
+/* bf16 rows in two 8-bit pieces, x = scale (hi + lo): hi = e4m3(x / scale), lo =
+ * e4m3(x / scale - hi), scale the power of two (2^-126 at least) that brings the row's
+ * largest value into [128, 256).  Exact for elements down to 2^-9 of the row's largest,
+ * below that off by at most 2^-17 of the largest.  A row with a NaN or an infinity has
+ * NaN as its scale.  out8_dev e4m3 [M][2][d], the rest as in crc_quantize_rows. */
+int crc_split_rows(const uint16_t *x_dev, int64_t x_stride, int64_t M, int32_t d,
+                   uint8_t *out8_dev, float *scale8_dev, void *stream);
+
 /* One layer's experts and where they lie.  An expert is three matrices, gate
  * and up [f][d] and down [d][f] (3 d f elements, the expert_bytes of a
  * crc_problem); slot s of the arrays below holds one expert, so they may be the
@@ -621,6 +629,14 @@ int crc_group_matmul(const crc_group_weights *w, const void *x_dev, int64_t x_st
                      const int32_t *rows_dev, int32_t K, int64_t E, uint16_t *y_dev,
                      void *stream);
 
+/* The same with 8-bit matrices and rows that keep bf16's bits: x_dev e4m3 [x_rows][2][k] and
+ * x_scale_dev from crc_split_rows (x_stride >= 2 k), x = scale (hi + lo).  Twice the products,
+ * as many as in bf16, on half the bytes of matrices. */
+int crc_group_matmul_split(const crc_group_weights *w, const uint8_t *x_dev, int64_t x_stride,
+                           int64_t x_rows, const float *x_scale_dev, const int32_t *offsets_dev,
+                           const int32_t *rows_dev, int32_t K, int64_t E, uint16_t *y_dev,
+                           void *stream);
+
 /* Its gradients, bf16 without glu: for the rows i of expert e
  *   dx_i = W_e^T dy_i,   dW_e = sum over i of dy_i x_r^T.
  *   dy_dev    bf16 [E][n], 16-byte aligned
@@ -719,7 +735,8 @@ int crc_matvec4(const crc_matvec4_weights *w, const uint16_t *x_dev, int64_t x_s
 
 /* Synchronises the device and returns (then clears) the error latched by
  * calls without a state (crc_route_scores, crc_rms_norm_grad, crc_moe_layer,
- * crc_group_matmul, crc_group_matmul_grad, crc_matvec4), CRC_OK if none. */
+ * crc_group_matmul, crc_group_matmul_split, crc_group_matmul_grad, crc_matvec4), CRC_OK if
+ * none. */
 int crc_device_error(void);
 
 /* Number of kernels the library has launched in this process. */

@@ -9,12 +9,12 @@ from .crc import (CrcError, MoeLayer, State, Trace, cache_loss, cache_scan,  # n
                   expert_views, group_choices, group_matmul, group_matmul_grad, load_time,
                   matvec4, metrics, pinned_empty, problem, problem_of, quantize_rows,
                   quantize_rows4, rms_norm, rms_norm_grad, route_and_cache, route_and_cache_host,
-                  route_scores, sum_choices, sum_choices_grad, synth_hidden, synth_weights,
-                  transfer_plan, transfer_replay)
+                  route_scores, split_rows, sum_choices, sum_choices_grad, synth_hidden,
+                  synth_weights, transfer_plan, transfer_replay)
 
 __all__ = ["crc", "CrcError", "MoeLayer", "State", "Trace", "cache_loss", "cache_scan",
            "expert_views", "group_choices", "group_matmul", "group_matmul_grad", "load_time",
            "matvec4", "metrics", "pinned_empty", "problem", "problem_of", "quantize_rows",
            "quantize_rows4", "rms_norm", "rms_norm_grad", "route_and_cache",
-           "route_and_cache_host", "route_scores", "sum_choices", "sum_choices_grad",
+           "route_and_cache_host", "route_scores", "split_rows", "sum_choices", "sum_choices_grad",
            "synth_hidden", "synth_weights", "transfer_plan", "transfer_replay"]

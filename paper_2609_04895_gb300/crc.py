@@ -150,14 +150,17 @@ EXPORTS = [
     ("crc_rms_norm", ctypes.c_int, [P, I64, P, P, I32, I64, I32, D, P, P, P, P, P, P]),
     ("crc_rms_norm_grad_workspace_bytes", SZ, [I64, I32]),
     ("crc_rms_norm_grad", ctypes.c_int, [P, P, P, P, P, I32, I64, I32, P, P, P, SZ, P]),
+    ("crc_split_rows", ctypes.c_int, [P, I64, I64, I32, P, P, P]),
     ("crc_quantize_rows", ctypes.c_int, [P, I64, I64, I32, P, P, P]),
     ("crc_moe_workspace_bytes", SZ, [ctypes.POINTER(crc_moe), I32]),
     ("crc_moe_layer", ctypes.c_int,
      [ctypes.POINTER(crc_moe), P, I64, P, P, P, I64, I32, P, P, P, P, SZ, P]),
     ("crc_group_choices_workspace_bytes", SZ, [I32, I32, I32]),
     ("crc_group_choices", ctypes.c_int, [P, I32, I32, I32, P, P, P, P, SZ, P]),
-    # (the structs of these three may also come as their bytes, which are quicker to make)
+    # (the structs of these may also come as their bytes, which are quicker to make)
     ("crc_group_matmul", ctypes.c_int,
+     [P, P, I64, I64, P, P, P, I32, I64, P, P]),
+    ("crc_group_matmul_split", ctypes.c_int,
      [P, P, I64, I64, P, P, P, I32, I64, P, P]),
     ("crc_group_matmul_grad", ctypes.c_int,
      [P, P, P, I64, I64, P, P, I32, I64, P, P, I32, P]),
@@ -851,6 +854,26 @@ def quantize_rows(x, out8=None, scale=None, stream=None):
     return out8, scale
 
 
+def split_rows(x, out8=None, scale=None, stream=None):
+    """crc_split_rows: bf16 rows x [M][d] (rows may be strided) in two 8-bit pieces, as
+    (float8_e4m3fn [M][2][d], fp32 scale a row): x = scale (hi + lo)."""
+    import torch
+    dev = _here(x, "x")
+    M, d, ldx = _rows(x, "x")
+    _check(x, "x", (M, d), torch.bfloat16, dev, False)
+    if out8 is None:
+        out8 = _new(stream, x.device, (M, 2, d), torch.float8_e4m3fn)
+    if scale is None:
+        scale = _new(stream, x.device, (M,), torch.float32)
+    rc = load().crc_split_rows(x.data_ptr(), ldx, M, d,
+                               _check(out8, "out8", (M, 2, d), torch.float8_e4m3fn, dev),
+                               _check(scale, "scale", (M,), torch.float32, dev),
+                               _stream(stream, dev))
+    if rc:
+        raise CrcError(rc, "crc_split_rows")
+    return out8, scale
+
+
 def expert_views(slots, f: int, d: int):
     """The matrices in the expert slots [C][3 * f * d] of one layer (bf16 or
     float8_e4m3fn elements, e.g. `slots_dev[l]` of transfer_replay viewed in that
@@ -952,12 +975,14 @@ class MoeLayer:
             raise CrcError(rc, "crc_moe_layer")
         return out
 
-    def prompt(self, x, topk, gates=None, out=None, stream=None):
+    def prompt(self, x, topk, gates=None, out=None, pieces: int = 2, stream=None):
         """out [M][d] of any number of tokens x [M][d] (bf16, rows may be strided) whose choices
         topk uint8 [M][K] and gates fp32 [M][K] (None: 1) are given: group_choices, the two
         grouped products and sum_choices.  A token's id of N or more has no expert.  Every
         expert e has to lie in slot e (no expert_slot).  With 8-bit experts x and the rows
-        between the products are brought to 8 bits, a scale a row."""
+        between the products (bf16) go in two 8-bit pieces (split_rows), which keep what a
+        call of the layer keeps; pieces=1: in one (quantize_rows), half the products for an
+        error of up to 2^-4 of each element."""
         import torch
         gate_up, down, _, slots, s13, s2 = self.tensors
         if slots is not None:
@@ -973,17 +998,20 @@ class MoeLayer:
         _check(topk, "topk", (M, K), torch.uint8, dev)
         _check(gates, "gates", (M, K), torch.float32, dev)
         _check(out, "out", (M, self.d), torch.bfloat16, dev)
+        if pieces not in (1, 2):
+            raise ValueError("pieces is 1 or 2")
+        to8 = split_rows if pieces == 2 else quantize_rows
         if s13 is None:
             x8, xs = x, None
         else:
-            x8, xs = quantize_rows(x, stream=stream)
+            x8, xs = to8(x, stream=stream)
         gate_up, down = gate_up[:self.N], down[:self.N]
         offsets, rows, place = group_choices(topk, self.N, stream=stream)
         h = group_matmul(x8, gate_up, offsets, rows=rows, K=K, x_scale=xs,
                          w_scale=None if s13 is None else s13[:self.N], stream=stream)
         hs = None
         if s2 is not None:
-            h, hs = quantize_rows(h, stream=stream)
+            h, hs = to8(h, stream=stream)
         y = group_matmul(h, down, offsets, x_scale=hs,
                          w_scale=None if s2 is None else s2[:self.N], stream=stream)
         return sum_choices(y, place, gates=gates, out=out, stream=stream)
@@ -1060,12 +1088,18 @@ def group_matmul(x, w, offsets, rows=None, K: int = 1, x_scale=None, w_scale=Non
     """crc_group_matmul: y [E][n] (bf16), row i the product of its expert's matrix with the
     row rows[i] // K of x (row i without `rows`); the rows of expert e are offsets[e] ..
     offsets[e + 1] - 1.  w [N][n][k], or gate and up [N][2][n][k] for silu(G x) * (U x);
-    x and w bf16, or float8_e4m3fn with x_scale [rows of x] and w_scale [N][n] ([N][2][n]).
-    x may have strided rows, w strided experts."""
+    x and w bf16, or float8_e4m3fn with x_scale [rows of x] and w_scale [N][n] ([N][2][n]), x
+    [rows][k] or in the two pieces of split_rows, [rows][2][k] (crc_group_matmul_split).
+    2-D x may have strided rows, w strided experts."""
     import torch
     dev, i32 = _here(x, "x"), torch.int32
-    x_rows, d, ldx = _rows(x, "x")
     c, N, n, k, _ = _group_weights(w, w_scale, dev)
+    split = x.dim() == 3
+    if split:
+        x_rows, d, ldx = x.shape[0], k, 2 * k
+        _check(x, "x", (x_rows, 2, k), torch.float8_e4m3fn, dev)
+    else:
+        x_rows, d, ldx = _rows(x, "x")
     if x.dtype is not w.dtype or d != k:
         raise ValueError(f"x must be {w.dtype} with rows of {k}, got {x.dtype} {tuple(x.shape)}")
     if (x_scale is None) != (w_scale is None):
@@ -1073,13 +1107,14 @@ def group_matmul(x, w, offsets, rows=None, K: int = 1, x_scale=None, w_scale=Non
     E = x_rows if rows is None else rows.numel()
     if y is None:
         y = _new(stream, x.device, (E, n), torch.bfloat16)
-    rc = load().crc_group_matmul(
-        c, x.data_ptr(), ldx if x_rows > 1 else (d + 15) // 16 * 16, x_rows,
+    call = load().crc_group_matmul_split if split else load().crc_group_matmul
+    rc = call(
+        c, x.data_ptr(), ldx if split or x_rows > 1 else (d + 15) // 16 * 16, x_rows,
         _check(x_scale, "x_scale", (x_rows,), torch.float32, dev),
         _check(offsets, "offsets", (N + 1,), i32, dev), _check(rows, "rows", (E,), i32, dev),
         K, E, _check(y, "y", (E, n), torch.bfloat16, dev), _stream(stream, dev))
     if rc:
-        raise CrcError(rc, "crc_group_matmul")
+        raise CrcError(rc, "crc_group_matmul_split" if split else "crc_group_matmul")
     return y
 
 

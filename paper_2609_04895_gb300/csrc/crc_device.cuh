@@ -467,6 +467,16 @@ template <int N>
 __device__ __forceinline__ void bulk_wait() {
     asm volatile("cp.async.bulk.wait_group %0;" ::"n"(N) : "memory");
 }
+// The power-of-two scale that brings a row's largest value into [128, 256), for the row in two
+// e4m3 pieces.  hi + lo / 16 hold a bf16 x exactly down to 2^-13 of the row's largest and to 2^-21
+// of it below, hi + lo down to 2^-9 and to 2^-17.
+// NaN for a row with an infinity or a NaN, which makes its results NaN.
+__device__ __forceinline__ float split_scale(float amax) {
+    const uint32_t ex = __float_as_uint(amax) >> 23;
+    if (ex >= 255u) return __uint_as_float(0x7fc00000u);
+    return __uint_as_float((ex < 8u ? 1u : ex - 7u) << 23);
+}
+
 // Make this thread's generic-proxy shared-memory writes visible to TMA.
 __device__ __forceinline__ void fence_proxy_async_smem() {
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");

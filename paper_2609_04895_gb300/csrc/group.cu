@@ -27,7 +27,7 @@ constexpr int kSingleRows = 48, kGatheredRows = 16, kShortRows = 8;
 
 constexpr CUtensorMapDataType kBf16Map = CU_TENSOR_MAP_DATA_TYPE_BFLOAT16;
 
-// `rows` rows of x in order; 1: four gathered.
+// `rows` rows of x in order; 1: four gathered.  k: columns of a row.
 bool rows_map(CUtensorMap* m, bool w8, const void* x, int64_t x_rows, int k, int64_t x_stride,
               int rows) {
     const int es = w8 ? 1 : 2;
@@ -162,6 +162,47 @@ GroupRows group_rows(const crc_group_weights& w, const int32_t* offsets, const i
     return r;
 }
 
+// crc_group_matmul; split: crc_group_matmul_split.
+int group_products(const crc_group_weights* w, bool split, const void* x_dev, int64_t x_stride,
+                   int64_t x_rows, const float* x_scale_dev, const int32_t* offsets_dev,
+                   const int32_t* rows_dev, int32_t K, int64_t E, uint16_t* y_dev, void* stream) {
+    int rc = check_weights(w);
+    if (rc) return rc;
+    const bool w8 = w->weight_type == CRC_E4M3;
+    if (split && !w8) return CRC_EINVAL;
+    const int columns = split ? 2 * w->k : w->k;
+    rc = check_rows(x_stride, x_rows, rows_dev, K, E, columns, w8 ? 1 : 2);
+    if (rc) return rc;
+    if (w8 ? (E > 0 && !x_scale_dev) || !aligned(x_scale_dev, 4) : x_scale_dev != nullptr)
+        return CRC_EINVAL;
+    if (E == 0) return CRC_OK;
+    if (!x_dev || !aligned(x_dev, 16) || !offsets_dev || !aligned(offsets_dev, 4) || !y_dev ||
+        !aligned(y_dev, 16))
+        return CRC_EINVAL;
+    CUtensorMap mw, mx, mx8;
+    if (!(w->glu ? glu_map(&mw, *w) : matrix_map(&mw, *w, w8 ? 128 : 64, 128)) ||
+        !rows_map(&mx, w8, x_dev, x_rows, columns, x_stride, rows_dev ? 1 : kGmBoxRows) ||
+        !(rows_dev || rows_map(&mx8, w8, x_dev, x_rows, columns, x_stride, kGmLastRows)))
+        return CRC_ECUDA;
+    if (rows_dev) mx8 = mx;                    // (not used)
+    GroupArgs a = {};
+    a.r = group_rows(*w, offsets_dev, rows_dev, K, x_rows, E);
+    a.y = y_dev;
+    a.xs = x_scale_dev;
+    a.ws = w->scale_dev;
+    a.ws_stride = w->scale_stride / 4;
+    a.split = split;
+    a.lo = w->k;
+    a.kblocks = (w->k + (w8 ? 127 : 63)) / (w8 ? 128 : 64) << a.split;
+    a.out = w->n;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    if (w8)
+        return w->glu ? launch_products<true, true, false>(mw, mx, mx8, a, st)
+                      : launch_products<true, false, false>(mw, mx, mx8, a, st);
+    return w->glu ? launch_products<false, true, false>(mw, mx, mx8, a, st)
+                  : launch_products<false, false, false>(mw, mx, mx8, a, st);
+}
+
 }  // namespace
 }  // namespace crc
 
@@ -173,37 +214,16 @@ int crc_group_matmul(const crc_group_weights* w, const void* x_dev, int64_t x_st
                      int64_t x_rows, const float* x_scale_dev, const int32_t* offsets_dev,
                      const int32_t* rows_dev, int32_t K, int64_t E, uint16_t* y_dev,
                      void* stream) {
-    int rc = check_weights(w);
-    if (rc) return rc;
-    const bool w8 = w->weight_type == CRC_E4M3;
-    rc = check_rows(x_stride, x_rows, rows_dev, K, E, w->k, w8 ? 1 : 2);
-    if (rc) return rc;
-    if (w8 ? (E > 0 && !x_scale_dev) || !aligned(x_scale_dev, 4) : x_scale_dev != nullptr)
-        return CRC_EINVAL;
-    if (E == 0) return CRC_OK;
-    if (!x_dev || !aligned(x_dev, 16) || !offsets_dev || !aligned(offsets_dev, 4) || !y_dev ||
-        !aligned(y_dev, 16))
-        return CRC_EINVAL;
-    CUtensorMap mw, mx, mx8;
-    if (!(w->glu ? glu_map(&mw, *w) : matrix_map(&mw, *w, w8 ? 128 : 64, 128)) ||
-        !rows_map(&mx, w8, x_dev, x_rows, w->k, x_stride, rows_dev ? 1 : kGmBoxRows) ||
-        !(rows_dev || rows_map(&mx8, w8, x_dev, x_rows, w->k, x_stride, kGmLastRows)))
-        return CRC_ECUDA;
-    if (rows_dev) mx8 = mx;                    // (not used)
-    GroupArgs a = {};
-    a.r = group_rows(*w, offsets_dev, rows_dev, K, x_rows, E);
-    a.y = y_dev;
-    a.xs = x_scale_dev;
-    a.ws = w->scale_dev;
-    a.ws_stride = w->scale_stride / 4;
-    a.kblocks = (w->k + (w8 ? 127 : 63)) / (w8 ? 128 : 64);
-    a.out = w->n;
-    cudaStream_t st = static_cast<cudaStream_t>(stream);
-    if (w8)
-        return w->glu ? launch_products<true, true, false>(mw, mx, mx8, a, st)
-                      : launch_products<true, false, false>(mw, mx, mx8, a, st);
-    return w->glu ? launch_products<false, true, false>(mw, mx, mx8, a, st)
-                  : launch_products<false, false, false>(mw, mx, mx8, a, st);
+    return group_products(w, false, x_dev, x_stride, x_rows, x_scale_dev, offsets_dev, rows_dev, K,
+                          E, y_dev, stream);
+}
+
+int crc_group_matmul_split(const crc_group_weights* w, const uint8_t* x_dev, int64_t x_stride,
+                           int64_t x_rows, const float* x_scale_dev, const int32_t* offsets_dev,
+                           const int32_t* rows_dev, int32_t K, int64_t E, uint16_t* y_dev,
+                           void* stream) {
+    return group_products(w, true, x_dev, x_stride, x_rows, x_scale_dev, offsets_dev, rows_dev, K,
+                          E, y_dev, stream);
 }
 
 int crc_group_matmul_grad(const crc_group_weights* w, const uint16_t* dy_dev,

@@ -137,16 +137,6 @@ __device__ __forceinline__ void zero_ctrl(const MoeRouteArgs& a) {
         for (int i = threadIdx.x; i < a.ctrl_words; i += blockDim.x) a.ctrl[i] = 0u;
 }
 
-// The power-of-two scale that brings a row's largest value into [128, 256): two
-// e4m3 pieces, hi + lo / 16, then hold a bf16 x exactly down to 2^-13 of the row's
-// largest and to 2^-21 of it below.
-// NaN for a row with an infinity or a NaN, which makes its results NaN.
-__device__ __forceinline__ float split_scale(float amax) {
-    const uint32_t ex = __float_as_uint(amax) >> 23;
-    if (ex >= 255u) return __uint_as_float(0x7fc00000u);
-    return __uint_as_float((ex < 8u ? 1u : ex - 7u) << 23);
-}
-
 // A warp multiplies two tiles of 8 experts; with fewer than 128 experts the
 // warps that are left split d further.
 __global__ void __launch_bounds__(kRouteThreads)

@@ -101,6 +101,22 @@ __device__ __forceinline__ uint2 to_e4m3(const float (&f)[8]) {
     return make_uint2(h[0] | ((uint32_t)h[1] << 16), h[2] | ((uint32_t)h[3] << 16));
 }
 
+// What eight e4m3 numbers leave of the values they were rounded from: exact in fp32.
+__device__ __forceinline__ void take_e4m3(float (&f)[8], const uint2& q) {
+    const uint32_t w[2] = {q.x, q.y};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        uint32_t h;
+        asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h) : "h"((uint16_t)(w[i / 2] >> (i % 2 * 16))));
+        float a, b;
+        asm("{\n\t.reg .b16 x, y;\n\tmov.b32 {x, y}, %2;\n\tcvt.f32.f16 %0, x;\n\tcvt.f32.f16 %1, y;\n\t}"
+            : "=f"(a), "=f"(b)
+            : "r"(h));
+        f[2 * i] -= a;
+        f[2 * i + 1] -= b;
+    }
+}
+
 // The row's scale.  A row of zeros has scale 1, as has one so small that the quotient is
 // zero (which would make NaN of the row's zeros); a NaN or an infinity goes on to the scale.
 __device__ __forceinline__ float row_scale(float amax) {
@@ -242,7 +258,10 @@ __global__ void __launch_bounds__(THREADS) rms_norm_kernel(NormArgs a) {
 // row, the next on its way while a row is reduced: there is so little to do for a
 // row that a CTA for every two of 2880 elements took 324 us where this took 235, and takes
 // 242 with the quotient of a division (184320 rows, 6.6 TB/s).
-template <int VPT, int THREADS>
+// Split: a row in two pieces, d elements of hi and d of lo, hi = e4m3(x / s) and lo = e4m3(x / s -
+// hi) with a power of two s.  hi has four significant bits of x's eight and the rest no more than
+// four, so lo is exact where it is not below e4m3's smallest steps (2^-9).
+template <bool Split, int VPT, int THREADS>
 __global__ void __launch_bounds__(THREADS)
     quantize_rows_kernel(const __nv_bfloat16* x, long long ldx, int M, int d, int warps, uint8_t* q,
                          float* scale) {
@@ -267,8 +286,27 @@ __global__ void __launch_bounds__(THREADS)
         for (int g = 0; g < VPT; ++g)
             if (team.thread + g * team.threads < nvec) m = max_abs8(m, l[g].v);
         const float amax = max_nan(__low2float(m), __high2float(m));
-        const float s = row_scale(row_reduce<true>(amax, buf, team));
+        const float most = row_reduce<true>(amax, buf, team);
+        const float s = Split ? split_scale(most) : row_scale(most);
         if (team.thread == 0) scale[row] = s;
+        if constexpr (Split) {
+            const float inv = 1.f / s;                  // s is 2^-126 .. 2^120
+#pragma unroll
+            for (int g = 0; g < VPT; ++g) {
+                const int i = team.thread + g * team.threads;
+                if (i >= nvec) continue;
+                float v[8];
+                l[g].get(v);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) v[j] *= inv;
+                uint2* to = reinterpret_cast<uint2*>(q + row * 2 * d + 8 * i);
+                const uint2 hi = to_e4m3(v);
+                take_e4m3(v, hi);
+                to[0] = hi;
+                to[nvec] = to_e4m3(v);
+            }
+            return;
+        }
         const RowDivide divide(s);
 #pragma unroll
         for (int g = 0; g < VPT; ++g) {
@@ -731,8 +769,8 @@ int crc_rms_norm_grad(const uint16_t* dy_dev, const void* s_dev, const uint16_t*
     return cuda_status(e);
 }
 
-int crc_quantize_rows(const uint16_t* x_dev, int64_t x_stride, int64_t M, int32_t d,
-                      uint8_t* out8_dev, float* scale8_dev, void* stream) {
+static int launch_quantize(bool split, const uint16_t* x_dev, int64_t x_stride, int64_t M,
+                           int32_t d, uint8_t* out8_dev, float* scale8_dev, void* stream) {
     const int rc = check_rows(M, d);
     if (rc) return rc;
     if (x_stride < d || x_stride % 8 != 0) return CRC_EINVAL;
@@ -755,14 +793,27 @@ int crc_quantize_rows(const uint16_t* x_dev, int64_t x_stride, int64_t M, int32_
     cudaError_t e;
     {
         ProfScope prof(CRC_KERNEL_QUANTIZE, st);
-#define CRC_K(V, B, unused)                                                                     \
-    e = launch_dependent(quantize_rows_kernel<V, B>, dim3(grid), sh.threads(), 0, st, 1, x,      \
+#define CRC_K(V, B, S)                                                                          \
+    e = launch_dependent(quantize_rows_kernel<S, V, B>, dim3(grid), sh.threads(), 0, st, 1, x,   \
                          (long long)x_stride, (int)M, (int)d, sh.warps, out8_dev, scale8_dev)
-        CRC_SHAPE(sh, CRC_K, 0);
+        if (split)
+            CRC_SHAPE(sh, CRC_K, true);
+        else
+            CRC_SHAPE(sh, CRC_K, false);
 #undef CRC_K
     }
     note_launch();
     return cuda_status(e);
+}
+
+int crc_quantize_rows(const uint16_t* x_dev, int64_t x_stride, int64_t M, int32_t d,
+                      uint8_t* out8_dev, float* scale8_dev, void* stream) {
+    return launch_quantize(false, x_dev, x_stride, M, d, out8_dev, scale8_dev, stream);
+}
+
+int crc_split_rows(const uint16_t* x_dev, int64_t x_stride, int64_t M, int32_t d,
+                   uint8_t* out8_dev, float* scale8_dev, void* stream) {
+    return launch_quantize(true, x_dev, x_stride, M, d, out8_dev, scale8_dev, stream);
 }
 
 }  // extern "C"

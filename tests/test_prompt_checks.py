@@ -58,7 +58,7 @@ GOOD = dict(x=new(6, 64), topk=new(6, 2, dtype=U), gates=new(6, 2, dtype=F), out
     dict(topk=new(6, 2, dtype=U, dev=1)), dict(x=new(6, 56)), dict(x=new(6, 64, dtype=F)),
     dict(x=new(64)), dict(x=new(6, 64, dev=1)), dict(gates=new(6, 3, dtype=F)),
     dict(gates=new(5, 2, dtype=F)), dict(gates=new(6, 2)), dict(out=new(5, 64)),
-    dict(out=new(6, 64, dtype=F)), dict(out=new(6, 64, dev=1)),
+    dict(out=new(6, 64, dtype=F)), dict(out=new(6, 64, dev=1)), dict(pieces=0), dict(pieces=3),
 ])
 def test_prompt_refuses_what_does_not_fit(layer, bad):
     with pytest.raises(ValueError):
