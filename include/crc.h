@@ -727,7 +727,9 @@ typedef struct crc_matvec4_weights {
  *             expert without a slot, or an id of N or more
  * No weight is rounded: the products of a group's codes with x are exact and summed in
  * fp32, the sum is scaled then, and y is rounded once.  A choice's row has no part in
- * another's result.
+ * another's result, and a call gives the same bits again; but for k > 256 the columns of a
+ * row are summed by 1, 2, 4 or 8 warps, as n, k, N and M K have it, so the same row may
+ * differ in its last bit between calls of different numbers of choices.
  * M <= 1024, K <= 32, M K <= 8192, n <= 65536, k <= 32768.  M = 0 is a no-op. */
 int crc_matvec4(const crc_matvec4_weights *w, const uint16_t *x_dev, int64_t x_stride,
                 int32_t x_per_choice, const uint8_t *topk_dev, int32_t M, int32_t K,

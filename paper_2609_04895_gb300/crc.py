@@ -1232,7 +1232,8 @@ def matvec4(x, codes, scale, topk=None, expert_slot=None, y=None, N: int | None 
     [slots][k / group][n] as quantize_rows4 makes them, or with gate and up [slots][2][..]
     for silu(G x) * (U x); x [M][k], or [M][K][k] with a row for each choice; expert_slot
     int32 [N] (None: expert e is in slot e).  Without topk all rows take slot 0, y [M][1][n].
-    The slots and 2-D x's rows may be strided."""
+    The slots and 2-D x's rows may be strided.  A row's last bits may depend on how many
+    choices a call has."""
     import torch
     bf16 = torch.bfloat16
     dev = _here(x, "x")
