@@ -213,7 +213,8 @@ __global__ void __launch_bounds__(kOrderThreads) order_choices_kernel(OrderArgs 
 // the sum over a token's choices
 // ---------------------------------------------------------------------------
 constexpr int kSumThreads = 256;
-constexpr int kManyTokens = 12000;
+constexpr int kManyTokens = 30000;
+constexpr long long kManyElements = 48ll << 20;
 
 struct SumArgs {
     const uint16_t* y;           // [rows][d]
@@ -401,10 +402,14 @@ cudaError_t launch_sum_of(SumArgs& a, cudaStream_t st) {
                             a);
 }
 cudaError_t launch_sum(SumArgs& a, cudaStream_t st) {
-    // One choice and many tokens: several tokens a team.  Us, one / eight: d = 816, 14400 tokens
-    // 14.1 / 12.2, 8000 8.6 / 10.0, 4000 4.2 / 6.4; d = 2048, 14400 tokens 27.5 / 23.9.
+    // One choice and many tokens: several tokens a team.  Us, one / eight: d = 256, 32000 tokens 5.9 /
+    // 7.4, 64000 11.8 / 12.9; d = 816, 16000 11.6 / 12.6, 32000 23.0 / 22.6, 64000 55.6 / 48.0; d =
+    // 2048, 16000 24.9 / 25.4, 32000 57.3 / 50.5, 64000 112 / 95; d = 4096, 16000 47.7 / 52.9, 32000
+    // 92.6 / 94.1, 64000 183 / 179.
     if (a.K == 1)
-        return a.M >= kManyTokens ? launch_sum_of<1, 8>(a, st) : launch_sum_of<1, 1>(a, st);
+        return a.M >= kManyTokens && (long long)a.M * a.d >= kManyElements
+                   ? launch_sum_of<1, 8>(a, st)
+                   : launch_sum_of<1, 1>(a, st);
     if (a.K == 2) return launch_sum_of<2, 1>(a, st);
     if (a.K <= 4) return launch_sum_of<4, 1>(a, st);
     return launch_sum_of<8, 1>(a, st);
