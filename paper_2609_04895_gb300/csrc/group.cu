@@ -23,7 +23,7 @@ bool encode(CUtensorMap* m, CUtensorMapDataType type, int rank, const void* base
                       CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-constexpr int kSingleRows = 48, kGatheredRows = 16, kShortRows = 8;
+constexpr int kSingleRows = 48, kGatheredRows = 40, kShortRows = 8;
 
 constexpr CUtensorMapDataType kBf16Map = CU_TENSOR_MAP_DATA_TYPE_BFLOAT16;
 
@@ -100,14 +100,17 @@ int launch_products_on(const CUtensorMap& mw, const CUtensorMap& mx, const CUten
 template <bool W8, bool GLU, bool TW>
 int launch_products(const CUtensorMap& mw, const CUtensorMap& mx, const CUtensorMap& mx8,
                     GroupArgs& a, cudaStream_t st) {
-    // CTAs by themselves for few rows an expert, fewer if they are gathered from long rows (a
-    // pair gathers a tile's rows once, two CTAs by themselves twice).  Us, by themselves / pairs:
-    // the second product of 60 tokens of the 32-expert shape (7 rows an expert) 68.6 / 76.7, in 8
-    // bits 36.9 / 41.8, its gradient's rows 66.2 / 73.4; of 200 tokens of the 128-expert shape
-    // 58.0 / 58.9, 8 bits 32.6 / 41.8; with 62 rows an expert 71.8 / 69.9, with 93 53.7 / 53.1,
-    // gradient 51.3 / 51.8.  The first product, gathered: one token of the 128-expert shape 12.8 /
-    // 13.7, in 8 bits 8.5 / 9.5, 200 tokens (12 rows an expert) 112.9 / 114.8, 500 (31) 129.8 /
-    // 125.8, 300 of the d = 4096 shape (18) 459 / 453; 5.5 / 7.4 for 300 tokens of d = 256.
+    // CTAs by themselves for few rows an expert on average, fewer if they are gathered from long rows
+    // (a pair gathers a tile's rows once, two CTAs by themselves twice).  What pairs take more than
+    // CTAs by themselves, at 16 / 32 / 48 / 64 / 96 rows an expert in bf16 (in 8 bits), per cent:
+    //   in order, 128 experts of 2048 x 768   2 (28) / 2 (23) / -1 (14) / -1 (14) / 2 (12)
+    //             32 of 2880 x 2880         10 (12) / 10 (11) / 4 (5) / 4 (3) / -6 (-13)
+    //             its gradient's rows           10 / 10 / 4 / 4 / -7
+    //   gathered, gate and up, 128 of 768 x 2048   1 (1) / 2 (0) / 4 (3) / -2 (-3)
+    //             64 of 1024 x 1024              2 (11) / 2 (11) / -4 (5) / -4 (6)
+    //             64 of 1024 x 512 (short rows)   4 (23) / 3 (23) / -3 (13) / -3 (16)
+    //             16 of 512 x 256 (short rows)  29 (33) / 25 (28) / 37 (40) / 28 (33)
+    // and at 36 and 40 rows gathered 2 to 4, 128 of 1536 x 4096 and of 768 x 2048, 64 of 1024 x 2048.
     const int most = a.r.rows && a.kblocks > kShortRows ? kGatheredRows : kSingleRows;
     const bool single = (long long)a.r.E <= (long long)most * a.r.N;
     return single ? launch_products_on<W8, GLU, TW, false>(mw, mx, mx8, a, st)

@@ -63,8 +63,8 @@ def around(mean, N):
     return c
 
 
-# rows an expert, on average: 16 gathered from more than 8 pieces of 128 bytes, else 48
-@pytest.mark.parametrize("mean", [1, 8, 15, 16, 17, 47, 48, 49])
+# rows an expert, on average: 40 gathered from more than 8 pieces of 128 bytes, else 48
+@pytest.mark.parametrize("mean", [1, 8, 17, 39, 40, 41, 47, 48, 49])
 @pytest.mark.parametrize("k", [64, 640, 2048])
 @pytest.mark.parametrize("gather", [False, True])
 @pytest.mark.parametrize("glu", [False, True])
