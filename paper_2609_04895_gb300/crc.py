@@ -461,6 +461,11 @@ def crc_quantize_rows(x_ptr, x_stride: int, M: int, d: int, out8_ptr, scale8_ptr
         "crc_quantize_rows")
 
 
+def crc_split_rows(x_ptr, x_stride: int, M: int, d: int, out8_ptr, scale8_ptr, stream=None):
+    _ck(load().crc_split_rows(x_ptr, x_stride, M, d, out8_ptr, scale8_ptr, _stream(stream)),
+        "crc_split_rows")
+
+
 def crc_moe_workspace_bytes(m: crc_moe, M: int) -> int:
     return int(load().crc_moe_workspace_bytes(ctypes.byref(m), M))
 
@@ -494,6 +499,13 @@ def crc_group_matmul(w: crc_group_weights, x_ptr, x_stride: int, x_rows: int, x_
     _ck(load().crc_group_matmul(ctypes.byref(w), x_ptr, x_stride, x_rows, x_scale_ptr,
                                 offsets_ptr, rows_ptr, K, E, y_ptr, _stream(stream)),
         "crc_group_matmul")
+
+
+def crc_group_matmul_split(w: crc_group_weights, x_ptr, x_stride: int, x_rows: int, x_scale_ptr,
+                           offsets_ptr, rows_ptr, K: int, E: int, y_ptr, stream=None):
+    _ck(load().crc_group_matmul_split(ctypes.byref(w), x_ptr, x_stride, x_rows, x_scale_ptr,
+                                      offsets_ptr, rows_ptr, K, E, y_ptr, _stream(stream)),
+        "crc_group_matmul_split")
 
 
 def crc_group_matmul_grad(w: crc_group_weights, dy_ptr, x_ptr, x_stride: int, x_rows: int,
@@ -865,12 +877,9 @@ def split_rows(x, out8=None, scale=None, stream=None):
         out8 = _new(stream, x.device, (M, 2, d), torch.float8_e4m3fn)
     if scale is None:
         scale = _new(stream, x.device, (M,), torch.float32)
-    rc = load().crc_split_rows(x.data_ptr(), ldx, M, d,
-                               _check(out8, "out8", (M, 2, d), torch.float8_e4m3fn, dev),
-                               _check(scale, "scale", (M,), torch.float32, dev),
-                               _stream(stream, dev))
-    if rc:
-        raise CrcError(rc, "crc_split_rows")
+    crc_split_rows(x.data_ptr(), ldx, M, d,
+                   _check(out8, "out8", (M, 2, d), torch.float8_e4m3fn, dev),
+                   _check(scale, "scale", (M,), torch.float32, dev), _stream(stream, dev))
     return out8, scale
 
 
