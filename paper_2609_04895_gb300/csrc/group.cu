@@ -292,9 +292,13 @@ int crc_group_matmul_grad(const crc_group_weights* w, const uint16_t* dy_dev,
     a.n = v.n;
     a.k = v.k;
     const size_t smem = GroupGradSmem::bytes();
-    auto kern = f32 ? group_weights_grad_kernel<true> : group_weights_grad_kernel<false>;
-    static PerDevice ready[2];
-    const int up = ready[f32].get(current_device(), [&] {
+    const bool parts = E > (f32 ? kGwPart<true> : kGwPart<false>);
+    auto kern = f32 ? (parts ? group_weights_grad_kernel<true, true>
+                             : group_weights_grad_kernel<true, false>)
+                    : (parts ? group_weights_grad_kernel<false, true>
+                             : group_weights_grad_kernel<false, false>);
+    static PerDevice ready[2][2];
+    const int up = ready[f32][parts].get(current_device(), [&] {
         return cuda_status(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize,
                                                 (int)smem)) == CRC_OK;
     });

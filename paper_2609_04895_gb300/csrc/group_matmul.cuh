@@ -88,11 +88,15 @@ __device__ __forceinline__ GroupTile group_tile(const GroupPlan& p, int N, int f
     return t;
 }
 
-// The first column of x that piece kb of the contraction reads: of a row's hi and lo in turn.  (Behind
-// the last column of hi, lo's begins; the matrix's are zeros there.)
-template <int kElems>
+// The first columns of the matrix and of x that piece kb of the contraction reads; of a split row's hi
+// and lo in turn.  (Behind the last column of hi, lo's begins; the matrix's are zeros there.)
+template <bool W8>
+__device__ __forceinline__ int w_column(const GroupArgs& a, int kb) {
+    return W8 ? (kb >> a.split) * 128 : kb * 64;
+}
+template <bool W8>
 __device__ __forceinline__ int x_column(const GroupArgs& a, int kb) {
-    return (kb >> a.split) * kElems + (kb & a.split) * a.lo;
+    return w_column<W8>(a, kb) + (W8 ? (kb & a.split) * a.lo : 0);
 }
 
 // All of 128 threads; orders what they did before it before what they do after.  It has no
@@ -132,7 +136,6 @@ __global__ void __launch_bounds__(kGmThreads, 1)
     group_matmul_kernel(const __grid_constant__ CUtensorMap mw,
                         const __grid_constant__ CUtensorMap mx,
                         const __grid_constant__ CUtensorMap mx8, GroupArgs a) {
-    constexpr int kElems = W8 ? 128 : 64;              // elements of a 128-byte piece
     constexpr int kCtas = Pair ? 2 : 1;                // CTAs of a tile
     extern __shared__ __align__(1024) uint8_t smem_raw[];
     uint8_t* smem = reinterpret_cast<uint8_t*>(
@@ -213,10 +216,10 @@ __global__ void __launch_bounds__(kGmThreads, 1)
                     tma_load_3d_of<Pair>(lead, sa + 8192, &mw, fb, f0 + 64, kb * 64, t.e, pol);
                 } else if constexpr (GLU) {
                     // four times 16 gate rows and the 16 up rows beside them
-                    tma_load_5d_of<Pair>(lead, sa, &mw, fb, (kb >> a.split) * kElems, 0, 0,
+                    tma_load_5d_of<Pair>(lead, sa, &mw, fb, w_column<W8>(a, kb), 0, 0,
                                         (t.ft * kCtas + (int)rank) * 4, t.e, pol);
                 } else {
-                    tma_load_3d_of<Pair>(lead, sa, &mw, fb, (kb >> a.split) * kElems,
+                    tma_load_3d_of<Pair>(lead, sa, &mw, fb, w_column<W8>(a, kb),
                                         (t.ft * kCtas + (int)rank) * 128, t.e, pol);
                 }
                 ++issued;
@@ -267,7 +270,7 @@ __global__ void __launch_bounds__(kGmThreads, 1)
                 const uint32_t fb = lead_full + (uint32_t)(stage * 8);
                 for (int b = 0; b < mine; b += unit)
                     tma_load_2d_of<Pair>(lead, sb + b * 128, unit == kGmBoxRows ? &mx : &mx8, fb,
-                                         x_column<kElems>(a, kb), first + b, pol);
+                                         x_column<W8>(a, kb), first + b, pol);
                 if (++stage == kGmStages) {
                     stage = 0;
                     phase ^= 1;
@@ -312,8 +315,8 @@ __global__ void __launch_bounds__(kGmThreads, 1)
                 for (int q = 0; q < 4; ++q) {
                     const int f = w + kGmGatherWarps * q;
                     if (f < fours)
-                        tma_gather4_of<Pair>(lead, sb + f * 512, &mx, fb, x_column<kElems>(a, kb),
-                                             src[q], pol);
+                        tma_gather4_of<Pair>(lead, sb + f * 512, &mx, fb, x_column<W8>(a, kb), src[q],
+                                             pol);
                 }
                 // A warp without rows in this tile would hold nothing back, and miss a turn if it
                 // came late by a whole one: the stage is not empty again before each has been here.

@@ -36,10 +36,10 @@ constexpr int kGwChunk = kGwRows * 128;    // 64 columns of a block
 // the first in one accumulator, the others in turn in the second one, and are added in fp32.
 // Error of fp32 dW in the mean square, of itself, for operands of either sign (of one sign): 256 rows
 // 2.3e-7, 1024 and more 1.0e-6 (2.2e-6); in two accumulators whatever the rows 8192 had 4.4e-6
-// (1.4e-5), 32768 1.9e-5 (8.3e-5).  Above two parts the second accumulator is drained between parts
-// while the tensor cores wait.  Us for 32 experts of 2048 x 768, two accumulators whatever the
-// rows / parts: 1024 rows each 91 / 91, 2048 175 / 180, 4096 312 / 324, 8192 587 / 609.  (Parts of 512
-// rows: 0.45e-6 for 10% from there on.)
+// (1.4e-5), 32768 1.9e-5 (8.3e-5).  The second accumulator is drained between parts while the tensor
+// cores wait.  Us for 32 experts of 2048 x 768, two accumulators whatever the rows / parts: 1024 rows
+// each 91 / 91, 2048 175 / 179, 4096 312 / 325, 8192 587 / 606.  (The last part added on the way out
+// took 2% less at 2048 rows, but 3% more for all calls of fewer: 128 registers a thread.)
 // bf16 dW is off by half a step of 2^-8 anyway: 16384 rows shrink a sum by 8e-5 of itself at most.
 template <bool F32>
 constexpr int kGwPart = F32 ? 1024 : 16384;
@@ -73,7 +73,9 @@ __device__ __forceinline__ int part_of(int count) {
     return ((count + parts - 1) / parts + kGwRows - 1) / kGwRows * kGwRows;
 }
 
-template <bool F32>
+// Parts: some expert may have more rows than an accumulator sums.  (Without, 249 us for 613
+// tokens' gathered bf16 gradient, 254 with.)
+template <bool F32, bool Parts>
 __global__ void __launch_bounds__(kGwThreads, 1)
     group_weights_grad_kernel(const __grid_constant__ CUtensorMap mdy,
                               const __grid_constant__ CUtensorMap mx,
@@ -262,16 +264,14 @@ __global__ void __launch_bounds__(kGwThreads, 1)
             const int count = plan.count[(int)(w / tiles)];
             if (count == 0) continue;
             take(acc);
-            const int part = part_of<F32>(count);
-            int cur = acc, next = part;                  // next: the first row of the next part
-            bool first = true;
+            const int part = Parts ? part_of<F32>(count) : count;
+            int cur = acc, start = 0;                    // start: the part's first row
             for (int r = 0; r < count && ok; r += kGwRows) {
-                if (r == next) {
+                if (Parts && r - start == part) {
                     commit_by(&tfull_bar[cur], lead);
                     used ^= 1u << cur;
                     cur = acc ^ 1;
-                    next += part;
-                    first = true;
+                    start = r;
                     take(cur);
                     if (!ok) break;
                 }
@@ -290,8 +290,7 @@ __global__ void __launch_bounds__(kGwThreads, 1)
                     if (kk * 16 < some)
                         umma_by<false, false>(d_tmem, sw128_mnmajor_desc(sa + kk * 2048, kGwChunk),
                                      sw128_mnmajor_desc(sb + kk * 2048, kGwChunk), kIdesc,
-                                     !first || kk != 0, lead);
-                first = false;
+                                     r != start || kk != 0, lead);
                 commit_by(&empty_bar[stage], lead);
                 if (++stage == kGwStages) {
                     stage = 0;
@@ -329,16 +328,16 @@ __global__ void __launch_bounds__(kGwThreads, 1)
         for (long long w = blockIdx.x; w < all; w += gridDim.x) {
             const int e = (int)(w / tiles), tile = (int)(w % tiles);
             const int row = tile / a.ntiles * kGwM + quarter * 32, col = tile % a.ntiles * kGwN;
-            const int count = plan.count[e], part = part_of<F32>(count);
-            const bool some = count > 0, two = part < count;
+            const int count = plan.count[e], part = Parts ? part_of<F32>(count) : count;
+            const bool some = count > 0, several = Parts && part < count;
             const uint32_t quarters = (uint32_t)(quarter * 32) << 16;
             const uint32_t tbase = tmem_base + (uint32_t)(acc * 256) + quarters;
-            const uint32_t tbase1 = tmem_base + (uint32_t)((acc ^ 1) * 256) + quarters;
             if (some && !full(acc)) break;
-            if (two) {
-                // every part but the first and the last goes to the first one's accumulator
+            if (several) {
+                // every part but the first is added to the first one's accumulator
+                const uint32_t tbase1 = tmem_base + (uint32_t)((acc ^ 1) * 256) + quarters;
                 bool ok = true;
-                for (int r = part; ok && r + part < count; r += part) {
+                for (int r = part; r < count; r += part) {
                     ok = full(acc ^ 1);
                     if (!ok) break;
 #pragma unroll 1
@@ -358,7 +357,7 @@ __global__ void __launch_bounds__(kGwThreads, 1)
                     tmem_st_wait();
                     release(acc ^ 1);
                 }
-                if (!ok || !full(acc ^ 1)) break;
+                if (!ok) break;
             }
 #pragma unroll 1
             for (int c = 0; c < kGwN; c += kCols) {
@@ -370,16 +369,6 @@ __global__ void __launch_bounds__(kGwThreads, 1)
                     tmem_ld_wait();
 #pragma unroll
                     for (int i = 0; i < kCols; i += 16) pin16(v + i);
-                    if (two)
-#pragma unroll
-                        for (int i = 0; i < kCols; i += 16) {
-                            float u[16];
-                            tmem_ld16(tbase1 + (uint32_t)(c + i), u);
-                            tmem_ld_wait();
-                            pin16(u);
-#pragma unroll
-                            for (int j = 0; j < 16; ++j) v[i + j] += u[j];
-                        }
 #pragma unroll
                     for (int j = 0; j < 8; ++j) {
                         uint32_t u[4];
@@ -414,11 +403,10 @@ __global__ void __launch_bounds__(kGwThreads, 1)
                     bulk_commit();
                 }
             }
-            if (some) release(acc);
-            if (two)
-                release(acc ^ 1);
-            else if (some)
-                acc ^= 1;
+            if (some) {
+                release(acc);
+                if (!several) acc ^= 1;
+            }
         }
         if (lane == 0) bulk_wait<0>();                   // every store has landed
     }
