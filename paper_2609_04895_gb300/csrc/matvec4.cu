@@ -10,10 +10,11 @@
 // What it should be bound by is bytes, half of one a weight and 2 / G for the scale.  At 6.8 TB/s
 // an SM has to turn over some 47 weights a clock, more than scalar fp32 instructions could (about
 // 3 a weight), so the fragments of mma.sync m16n8k16 are filled from the packed words in
-// registers: the eight columns of the product are eight choices of the same expert.  (tcgen05
-// takes its operands from shared memory: codes would have to be widened to bf16 and written back
-// there, 4 bytes of traffic for each half byte that came in; and its sums over the groups could
-// not be scaled apart.)  It reaches 20 to 25 weights a clock: 64 tokens' second product (128
+// registers: the eight columns of the product are eight choices of the same expert.  (tcgen05 was
+// not tried.  Widened codes could go to its A operand in shared memory or TMEM, a group's sums to
+// columns of their own.  But a step of 16 columns of a pair's 256 rows takes some 105 clocks in
+// group_matmul.cuh whatever its N up to 200, operands in shared memory: 20 weights a clock and SM,
+// no more than here.  How long one with A in TMEM takes has not been measured.)  It reaches 20 to 25 weights a clock: 64 tokens' second product (128
 // experts, 105 MB) takes 39 us, 35 of them with the loads left out and 22 with the products
 // left out: what bounds it are two bit operations, a shift and a subtraction for two weights, and
 // the legacy tensor path.  One token's (14 MB) takes 10 us: 5 are the launch and the choices'
@@ -616,7 +617,10 @@ extern "C" int crc_matvec4(const crc_matvec4_weights* w, const uint16_t* x_dev, 
             a.splits = s;
         }
     }
-    // (a pass over the weights takes 8 choices, 16 where an expert has that many)
+    // (A pass over the weights takes 8 choices, 16 where the mean over all N experts is 8 or more: it
+    // is not known here how many each has.  So a liked expert of a smaller batch is read, from L2,
+    // once for every 8 of its choices; and from that mean on a warp has a tile to itself, which leaves
+    // most of the GPU without work where the matrices are few and small.)
     const long long ctas = (items * a.splits + kWarps - 1) / kWarps;
     const long long room = (long long)sm_count() * kCtas;
     const dim3 grid((unsigned)(ctas < room ? ctas : room));
