@@ -1099,7 +1099,8 @@ def group_matmul(x, w, offsets, rows=None, K: int = 1, x_scale=None, w_scale=Non
     offsets[e + 1] - 1.  w [N][n][k], or gate and up [N][2][n][k] for silu(G x) * (U x);
     x and w bf16, or float8_e4m3fn with x_scale [rows of x] and w_scale [N][n] ([N][2][n]), x
     [rows][k] or in the two pieces of split_rows, [rows][2][k] (crc_group_matmul_split).
-    2-D x may have strided rows, w strided experts."""
+    2-D x may have strided rows, w strided experts.  Rows of y outside the offsets are left as they
+    were (anything, in a y that is made)."""
     import torch
     dev, i32 = _here(x, "x"), torch.int32
     c, N, n, k, _ = _group_weights(w, w_scale, dev)
@@ -1130,7 +1131,8 @@ def group_matmul(x, w, offsets, rows=None, K: int = 1, x_scale=None, w_scale=Non
 def group_matmul_grad(dy, x, w, offsets, rows=None, K: int = 1, dx=None, dw=None,
                       want_dx: bool = True, want_dw: bool = True, stream=None):
     """crc_group_matmul_grad: (dx [E][k] bf16, dw [N][n][k], fp32 unless a bf16 one is given)
-    of y = group_matmul(x, w, offsets, rows, K) from dy [E][n], all bf16."""
+    of y = group_matmul(x, w, offsets, rows, K) from dy [E][n], all bf16.  Rows of dx outside the
+    offsets are left as they were."""
     import torch
     bf16, i32 = torch.bfloat16, torch.int32
     dev = _here(dy, "dy")
@@ -1180,7 +1182,8 @@ def sum_choices(y, place, gates=None, out=None, stream=None):
 def sum_choices_grad(dout, place, gates=None, y=None, dy=None, dgates=None, y_rows=None,
                      stream=None):
     """crc_sum_choices_grad: (dy [y_rows][d], dgates [M][K]) from dout [M][d].  dgates is made
-    when y is given (and is None without); y_rows: M * K unless y or dy says."""
+    when y is given (and is None without); y_rows: M * K unless y or dy says.  Rows of dy that
+    no choice has are left as they were (anything, in a dy that is made)."""
     import torch
     bf16, f32 = torch.bfloat16, torch.float32
     if dout.dim() != 2 or place.dim() != 2:

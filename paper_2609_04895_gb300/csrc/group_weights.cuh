@@ -12,11 +12,10 @@
 // few blocks, 128 KB in fp32; the writes of dW are most of its bytes.  Tiles leave through
 // shared memory by TMA.  An expert without rows has zeros.  4096 tokens x 8 (128 experts of
 // 2048 x 768, fp32) take 191 us alone and 204 in a row (111 without the stores), of 146 that the
-// bytes take; 613 tokens x
-// 4, gathered (32 experts of 5760 x 2880, bf16), 249 of 160: TMA takes some 20 ns for four
-// gathered rows of 64 columns, 198 us in all.  (On CTA pairs, which gather half as much, 311 and
-// 207: a tile is a few blocks, and two CTAs wait for each other at each; with x as the 128 rows of
-// A, stores of 64-byte rows, 295.)
+// bytes take; 613 tokens x 4, gathered (32 experts of 5760 x 2880, bf16), 249 of 160: TMA takes some
+// 20 ns for four gathered rows of 64 columns, 198 us in all.  (On CTA pairs, which gather half as
+// much, 311 and 207: a tile is a few blocks, and two CTAs wait for each other at each; with x as the
+// 128 rows of A, stores of 64-byte rows, 295.)
 //
 // Work: tiles of (expert, 128 rows, 256 columns of dW), dealt to the CTAs in turn, so that
 // those running together share an expert's rows in L2.

@@ -8,26 +8,27 @@
 // the subtraction of 136, which is exact.
 //
 // What it should be bound by is bytes, half of one a weight and 2 / G for the scale.  At 6.8 TB/s
-// an SM has to turn over some 47 weights a clock, more than scalar fp32 instructions could (about
-// 3 a weight), so the fragments of mma.sync m16n8k16 are filled from the packed words in
-// registers: the eight columns of the product are eight choices of the same expert.  (tcgen05 was
-// not tried.  Widened codes could go to its A operand in shared memory or TMEM, a group's sums to
-// columns of their own.  But a step of 16 columns of a pair's 256 rows takes some 105 clocks in
+// an SM has to turn over some 47 weights a clock, more than scalar fp32 instructions could (about 3
+// a weight), so the fragments of mma.sync m16n8k16 are filled from the packed words in registers:
+// the eight columns of the product are eight choices of the same expert.  (tcgen05 was not tried.
+// Widened codes could go to its A operand in shared memory or TMEM, a group's sums to columns of
+// their own.  But a step of 16 columns of a pair's 256 rows takes some 105 clocks in
 // group_matmul.cuh whatever its N up to 200, operands in shared memory: 20 weights a clock and SM,
-// no more than here.  How long one with A in TMEM takes has not been measured.)  It reaches 20 to 25 weights a clock: 64 tokens' second product (128
-// experts, 105 MB) takes 39 us, 35 of them with the loads left out and 22 with the products
-// left out: what bounds it are two bit operations, a shift and a subtraction for two weights, and
-// the legacy tensor path.  One token's (14 MB) takes 10 us: 5 are the launch and the choices'
-// order, and eight experts are too few boxes a warp to fill the rest.
+// no more than here.  How long one with A in TMEM takes has not been measured.)  It reaches 20 to
+// 25 weights a clock: 64 tokens' second product (128 experts, 105 MB) takes 39 us, 35 of them with
+// the loads left out and 22 with the products left out: what bounds it are two bit operations, a
+// shift and a subtraction for two weights, and the legacy tensor path.  One token's (14 MB) takes
+// 10 us: 5 are the launch and the choices' order, and eight experts are too few boxes a warp to
+// fill the rest.
 //
-// A persistent grid: each CTA brings the choices into their experts' order once, and its
-// warps take tiles of 32 rows (with gate and up: 16 rows of each) of the active experts in
-// turn.  A warp's codes and scales come by TMA into a ring of its own, 256 columns a time,
-// across the ends of its tiles; with too few tiles for the warps, 2, 4 or 8 warps share a
-// tile's columns and their sums are added in a fixed order (another one for another number of
-// warps: of 2048 columns one bf16 result in 6000 rounds the other way).  Half a box's words, scales and x
-// are loaded before they are used (41 us against 49).  Two CTAs an SM leave 128 registers a
-// thread: with 20 warps of 96 it took 45 us.
+// A persistent grid: each CTA brings the choices into their experts' order once, and its warps take
+// tiles of 32 rows (with gate and up: 16 rows of each) of the active experts in turn.  A warp's
+// codes and scales come by TMA into a ring of its own, 256 columns a time, across the ends of its
+// tiles; with too few tiles for the warps, 2, 4 or 8 warps share a tile's columns and their sums
+// are added in a fixed order (another one for another number of warps: of 2048 columns one bf16
+// result in 6000 rounds the other way).  Half a box's words, scales and x are loaded before they
+// are used (41 us against 49).  Two CTAs an SM leave 128 registers a thread: with 20 warps of 96 it
+// took 45 us.
 #include <cudaTypedefs.h>
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>

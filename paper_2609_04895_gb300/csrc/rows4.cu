@@ -36,8 +36,9 @@ struct Quantize4Args {
 
 // 1.5 * 2^23 plus the whole number nearest to v / a, ties to the even one: its low bits are the
 // code's.  v inv is within 2^-23 of the quotient's value, and Markstein's correction from there
-// rounds it to fp32 as a division would (v - q a is exact, a >= 2^-100).  With 8 significant bits each, v / a
-// is a tie exactly or at least 2^-10 away from one, so the rounding to fp32 changes no code.
+// rounds it to fp32 as a division would (v - q a is exact, a >= 2^-100).  With 8 significant bits
+// each, v / a is a tie exactly or at least 2^-10 away from one, so the rounding to fp32 changes no
+// code.
 __device__ __forceinline__ uint32_t code_bits(float v, float a, float inv) {
     const float q = v * inv;
     return __float_as_uint(fmaf(fmaf(-q, a, v), inv, q) + 12582912.f);
