@@ -36,7 +36,7 @@ def definition(dy, x, offsets, src):
 
 
 # rows of the experts: of a part, of two, of three and more, whose last may be short
-COUNTS = [[1024], [1025, 3, 2049], [4103, 0, 5], [2048, 3072, 3073], [32768, 700], [8191, 0, 0, 6145]]
+COUNTS = [[1024], [1025, 3, 2049], [4103, 0, 5], [2048, 4096, 4097], [32768, 700], [8191, 0, 0, 6145]]
 
 
 @pytest.mark.parametrize("counts", COUNTS)
